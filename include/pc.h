@@ -178,6 +178,28 @@ typedef struct {
 int32_t pc_attend(pc_cache *c, const pc_call *calls, int32_t n_calls,
                   const void *q, void *out, float *lse, void *stream);
 
+/* Batched attention of a layer with a sliding window (of layers that alternate with full ones, say) and sinks, the first
+ * tokens of a call that stay visible however far a generation goes.  Arguments and results as for pc_attend, but a row
+ * at position p sees, of the tokens that pc_attend would show it,
+ *   those at positions above p - window (its own position and the window - 1 in front of it; parents placed behind it stay
+ *   visible, as in pc_attend), and
+ *   the first n_sink tokens of its call's list (parents in list order, then the new message; the new message's tokens, up to
+ *   the row's own one), wherever they are placed.
+ * The window is one of positions, as the model was trained with them: gaps count, and messages that overlap are all seen.
+ * A row with nothing visible yields zeros and -inf.  What a row does not see has no part in its result, whatever is stored there
+ * (infinities and NaN too).  window >= 1, n_sink >= 0; q and out 16-byte aligned, lse 4-byte; out must not overlap q
+ * (PC_ERR_INVALID_ARG otherwise, but for the overlap, which is not looked for).
+ * PC_BF16 caches: queries, once turned to their positions, and probabilities are rounded to bf16 for the matrix instructions;
+ * scores, sums and partial results are fp32.  PC_F32 caches: fp32 throughout.
+ * pc_attend_window refuses a stream that is being captured (the workspace it uses may move at a later call);
+ * pc_attend_window_static is for those and for callers that cannot allocate: it works in the fixed array of pc_attend_static,
+ * and what is said there of its size, its sharing, lists recorded into a graph and calls that overlap in time holds for it
+ * too.  (It keeps no counters.)  A recorded call holds the slots its messages had. */
+int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
+                         const void *q, void *out, float *lse, void *stream);
+int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
+                                const void *q, void *out, float *lse, void *stream);
+
 /* One decode step of parallel calls in one call (Sec. 2.4 "Parallel API Calls" and the interleaved decoding of
  * parallel calls): pc_append_tokens_batch(msg_ids, n_msgs, k, v) followed by pc_attend(calls, ...), with the same
  * arguments, results and errors as the two.  What the fused form saves is the append's launch and its item list: where

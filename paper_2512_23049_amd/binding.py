@@ -76,6 +76,9 @@ def lib():
         L.pc_decode_step.argtypes = [vp, C.POINTER(i32), i32, vp, vp, C.POINTER(pc_call), i32, vp, vp, vp, vp]
         L.pc_attend_static.restype = i32
         L.pc_attend_static.argtypes = [vp, C.POINTER(pc_call), i32, vp, vp, vp, vp]
+        for f in (L.pc_attend_window, L.pc_attend_window_static):
+            f.restype = i32
+            f.argtypes = [vp, C.POINTER(pc_call), i32, i32, i32, vp, vp, vp, vp]
         L.pc_build_tables.restype = i32
         L.pc_build_tables.argtypes = [vp, C.POINTER(pc_call), vp, vp, i64, C.POINTER(i64), vp]
         L.pc_resolve_call.restype = i32
@@ -201,6 +204,17 @@ class Cache:
         arr, keep = marshalled if marshalled is not None else marshal_calls(calls)
         self._check(lib().pc_attend_static(self.h, arr, len(calls), q_ptr or None, out_ptr or None,
                                            lse_ptr or None, stream or None))
+
+    def attend_window(self, calls, window: int, n_sink: int, q_ptr: int, out_ptr: int, lse_ptr: int = 0, stream: int = 0, marshalled=None):
+        arr, keep = marshalled if marshalled is not None else marshal_calls(calls)
+        self._check(lib().pc_attend_window(self.h, arr, len(calls), window, n_sink, q_ptr or None, out_ptr or None,
+                                           lse_ptr or None, stream or None))
+
+    def attend_window_static(self, calls, window: int, n_sink: int, q_ptr: int, out_ptr: int, lse_ptr: int = 0, stream: int = 0,
+                             marshalled=None):
+        arr, keep = marshalled if marshalled is not None else marshal_calls(calls)
+        self._check(lib().pc_attend_window_static(self.h, arr, len(calls), window, n_sink, q_ptr or None, out_ptr or None,
+                                                  lse_ptr or None, stream or None))
 
     def build_tables(self, call, kv_slot_ptr: int, kv_pos_ptr: int, cap: int, stream: int = 0) -> int:
         arr, keep = marshal_calls([call])

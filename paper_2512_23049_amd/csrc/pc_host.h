@@ -42,6 +42,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 struct pc_cache {
     pc_config cfg;
     bool host_only = false;
+    int device = 0;                                  // the GPU that was current when the cache was created
     bool grow_extents = false;
     int D = 0, half = 0, g = 0;
     int64_t slots = 0;
@@ -120,6 +121,28 @@ struct ProfScope {
         c->prof_recs.push_back({cls, a, b});
     }
 };
+
+// The cache's device is the current one while this lives.
+struct PcDeviceScope {
+    int before = -1; bool ok = true;
+    explicit PcDeviceScope(const pc_cache *c)
+    {
+        int now = -1;
+        if (hipGetDevice(&now) != hipSuccess) { ok = false; return; }
+        if (now == c->device) return;
+        ok = hipSetDevice(c->device) == hipSuccess;
+        before = now;
+    }
+    ~PcDeviceScope() { if (before >= 0) (void)hipSetDevice(before); }
+    PcDeviceScope(const PcDeviceScope &) = delete;
+};
+
+// What a C entry runs: no exception passes it (lists too long for the host's memory).
+template <class F> int32_t pc_guarded(pc_cache *c, F f) noexcept
+{
+    try { return f(); } catch (...) {}
+    try { return pc_fail(c, PC_ERR_NO_SPACE, "the host has no memory for the call's lists"); } catch (...) { return PC_ERR_NO_SPACE; }
+}
 
 // ---- validated, resolved form of one call -------------------------------------------
 struct Resolved {

@@ -155,6 +155,7 @@ int32_t pc_cache_create(const pc_config *cfg, pc_cache **out)
     c->msgs.reserve((size_t)cfg->max_messages);
     *out = c;
     if (c->host_only) return PC_OK;
+    (void)hipGetDevice(&c->device);
 
     const size_t bytes = pc_storage_bytes(cfg);
     auto bail = [&](int32_t code) { pc_cache_destroy(c); *out = nullptr; return code; };

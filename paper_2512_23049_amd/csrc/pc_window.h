@@ -1,0 +1,149 @@
+// Structures and launch wrappers of the windowed attention (internal to the library).
+//
+// Visibility.  A row at position p of a call sees a key at position x if the call lists the key (own tokens: up to the row's
+// own one) and x > p - window, or the key is one of the first n_sink tokens of the call's list.  The host turns that into
+// runs: for each group of rows and each listed extent the tiles that some row of the group sees (a suffix of the extent, its
+// sinks in front), so that the kernels walk what is needed and mask at its edges only.
+#ifndef PC_WINDOW_H_
+#define PC_WINDOW_H_
+
+#include "pc_internal.h"
+
+// Consecutive tiles of one extent.
+struct PcWinRun {
+    int32_t slot0;            // first slot (multiple of PC_TILE)
+    int32_t pos0;             // position the call gives the token in that slot
+    int32_t n_tok;            // tokens from there on that count
+    int32_t sink;             // the first of them that are visible at any distance
+    int32_t rot;              // row of the rotation table
+    int32_t self;             // 1: the new message (causal limit)
+    int64_t rot_pos;          // the extent's start - the position its keys are stored at: what the queries are turned back by
+};
+
+// One workgroup's share of a launch, for each KV head.
+struct PcWinItem {
+    int32_t q_off, n_q;       // the call's packed rows
+    int32_t unit0;            // bf16: first of four units (32 rows x head of the KV head, head fastest); fp32: block of 32 (row, head) columns
+    int32_t lim0;             // position of the last own token that row 0 of the call sees (row r: lim0 + r)
+    int32_t run0, skip;       // the first run, and its tiles that belong to the split before
+    int32_t n_tiles;
+    int32_t part;             // -1, or the partial row of the call's row 0 in this split
+};
+
+// What every launch of a call needs.
+struct PcWin {
+    const PcWinRun  *runs;
+    const PcWinItem *items;
+    const int32_t   *q_pos;   // [rows]
+    const float2    *rot_q;   // bf16: in the lanes' order (see win_rot_at); fp32: [rows][D/2]: (cos, sin)(q_pos theta_i)
+    const float2    *rot_run; // [rot][D/2]: (cos, sin)(rot_pos theta_i)
+    const double    *inv_freq;
+    const void      *k_store, *v_store, *q;
+    void            *out;
+    float           *lse;     // or null
+    float           *part_o;  // [part rows][H_q][D], not normalised
+    float           *part_ml; // [part rows][H_q][2]
+    int64_t          slots;
+    int32_t          n_q_heads, n_kv_heads;
+    int32_t          window;
+    float            scale_log2;
+};
+// Offsets of a decode launch's lists, where they travel in its arguments.
+struct PcWinDecode { int32_t off_items, off_runs, off_q_pos, n16; void *ws; };      // n16 > 0: so many pieces of 16 bytes are left in the workspace for the merge
+
+// float2 index of pair i of packed row R in the lanes' order of the bf16 prefill kernel (D = 128): 16 bytes a lane, lanes of
+// consecutive rows side by side
+__host__ __device__ __forceinline__ int64_t win_rot_at(int64_t R, int i)
+{
+    return ((R / 32 * 1024 + (i / 16) * 256 + (i % 8) / 2 * 64 + (i / 8 % 2) * 32 + R % 32) * 2) + i % 2;
+}
+
+// the least position a row at p sees (but for the sinks)
+__host__ __device__ __forceinline__ int32_t win_low(int32_t p, int32_t window)
+{
+    const int64_t low = (int64_t)p - window + 1;
+    return low < INT32_MIN ? INT32_MIN : (int32_t)low;
+}
+
+// lists (n16 pieces of 16 bytes, at `from`, or in the arguments where blob is not null) to ws, and the rotations of rows and runs
+struct PcWinTurns {
+    const void *from; void *ws; int n16;
+    int off_q_pos, n_rows, off_rot, n_rot;        // within the lists: int32 positions, int64 positions
+    int D, lanes_order;
+    float run_scale;                              // rides on the runs' rotations
+    float2 *rot_q, *rot_run;
+    const double *inv_freq;
+};
+void pc_launch_win_turns(const PcWinTurns &T, const PcArgBlob *blob, hipStream_t st);
+
+void pc_launch_win_prefill_bf16(const PcWin &W, int n_items, hipStream_t st);
+// blob: its lists (W.items, W.runs and W.q_pos are not read then), or null
+void pc_launch_win_decode_bf16(const PcWin &W, int n_items, const PcArgBlob *blob, const PcWinDecode &O, hipStream_t st);
+void pc_launch_win_attend_f32(const PcWin &W, int n_items, int D, hipStream_t st);
+void pc_launch_win_merge(const PcWin &W, const PcMergeRow *rows, int n_rows, int dtype, int D, hipStream_t st);
+
+#ifdef __HIPCC__
+// A walk over the tiles of an item, run after run (uniform over the wave: everything stays in scalar registers).
+struct WinTile { int slot0, pos0, valid, sink, rot, self; int64_t rot_pos; };
+typedef int win_i32x4 __attribute__((ext_vector_type(4)));
+struct WinWalk {
+    uintptr_t run;            // the present run
+    win_i32x4 a;              // slot0, pos0, n_tok, sink of what is left of it
+    int rot, self;
+    int64_t rot_pos;
+    __device__ __forceinline__ void load()
+    {
+        const auto *p = reinterpret_cast<const __attribute__((address_space(4))) win_i32x4 *>(run);
+        a = p[0];
+        const win_i32x4 b = p[1];
+        rot = b.x; self = b.y;
+        rot_pos = (int64_t)(((uint64_t)(uint32_t)b.w << 32) | (uint32_t)b.z);
+    }
+    __device__ __forceinline__ void pass(int tiles)      // tiles of the present run (fewer than it has)
+    {
+        a.x += PC_TILE * tiles; a.y += PC_TILE * tiles; a.z -= PC_TILE * tiles; a.w -= PC_TILE * tiles;
+    }
+    __device__ __forceinline__ WinWalk(const void *runs, int skip) : run(reinterpret_cast<uintptr_t>(runs))
+    {
+        load();
+        for (;;) {                                       // (a wave's or a split's share may begin some runs further on)
+            const int n = (a.z + PC_TILE - 1) / PC_TILE;
+            if (skip < n) break;
+            skip -= n;
+            run += sizeof(PcWinRun);
+            load();
+        }
+        pass(skip);
+    }
+    __device__ __forceinline__ WinTile tile() const { return WinTile{a.x, a.y, min(a.z, PC_TILE), min(max(a.w, 0), PC_TILE), rot, self, rot_pos}; }
+    __device__ __forceinline__ void next()               // (not behind the item's last tile: there may be no further run)
+    {
+        if (a.z > PC_TILE) { pass(1); return; }
+        run += sizeof(PcWinRun);
+        load();
+    }
+};
+// Values that are not finite, in a tile of which some row does not see every key: a probability of 0 would not take them out of
+// the product.  They are left out of it, and a second product adds up, over the keys a row sees, a number for each of them: its
+// digits say which there were, and with that what they make of the sum.
+#define PC_WIN_ODD_INF 1.f
+#define PC_WIN_ODD_NEG 256.f  // (at most 32 keys: no carry)
+#define PC_WIN_ODD_NAN 65536.f
+__device__ __forceinline__ float win_odd_sum(float z)
+{
+    const float neg = __builtin_truncf(z * (1.f / PC_WIN_ODD_NEG)), pos = z - neg * PC_WIN_ODD_NEG;
+    const bool none = (z >= PC_WIN_ODD_NAN) | ((neg > 0.f) & (pos > 0.f));
+    const float some = neg > 0.f ? -INFINITY : INFINITY, what = none ? __builtin_nanf("") : some;
+    return z == 0.f ? 0.f : what;
+}
+// bit j: the row with those limits sees key j of the tile (lo: its least position, lim: the last own position it sees)
+__device__ __forceinline__ uint32_t win_sees(int pos0, int valid, int sink, bool self, int lo, int lim)
+{
+    auto first = [](unsigned n) { return n >= 32u ? ~0u : (1u << n) - 1u; };          // bits 0 .. n - 1
+    const unsigned below = lo <= pos0 ? 0u : (unsigned)lo - (unsigned)pos0;             // (positions may lie 2^32 apart)
+    const unsigned own = !self ? 32u : lim < pos0 ? 0u : min((unsigned)lim - (unsigned)pos0, 31u) + 1u;
+    return first(min(own, (unsigned)valid)) & (~first(below) | first((unsigned)sink));
+}
+#endif
+
+#endif

@@ -1,0 +1,326 @@
+// Host side of the windowed attention: what each group of rows sees as runs of tiles, work items, staging, entry points.
+#include "pc_host.h"
+#include "pc_window.h"
+
+#include <new>
+
+namespace {
+
+// One listed extent of a call, in list order.
+struct Seg {
+    int64_t rot_pos;
+    int64_t before;           // tokens of the call's list in front of it
+    int32_t slot0, start, len;
+    int32_t rot;              // its row of the rotation table, -1: none yet
+    bool self;
+};
+struct WinCall {
+    int32_t q_off, n_q, lim0, own_first;      // own_first: index (within the last extent of the new message) of row 0's token
+    size_t seg0, n_seg;
+};
+struct WinPlan {
+    std::vector<Resolved> res;
+    std::vector<WinCall> calls;
+    std::vector<Seg> segs;
+    std::vector<int32_t> q_pos;
+    std::vector<PcWinItem> pre, dec;
+    std::vector<PcWinRun> runs;
+    std::vector<int64_t> rots;
+    std::vector<PcMergeRow> merge;
+    int64_t part_rows = 0;
+    int32_t window = 0, n_sink = 0;
+};
+
+int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan &P)
+{
+    P.res.resize((size_t)n_calls);
+    P.calls.resize((size_t)n_calls);
+    int64_t total_q = 0;
+    for (int i = 0; i < n_calls; ++i) {
+        const int32_t rc = pc_resolve(c, &calls[i], i, P.res[(size_t)i]);
+        if (rc != PC_OK) return rc;
+        const Resolved &r = P.res[(size_t)i];
+        WinCall &wc = P.calls[(size_t)i];
+        wc.q_off = (int32_t)total_q; wc.n_q = r.n_q;
+        wc.own_first = r.self_msg >= 0 ? r.self_len - r.n_q : 0;
+        wc.lim0 = r.self_msg >= 0 ? r.self_start + wc.own_first : 0;
+        wc.seg0 = P.segs.size();
+        int64_t before = 0;
+        auto add = [&](int32_t rec, int32_t start, int32_t len, bool self) {
+            const HostMsg &m = c->msgs[(size_t)rec];
+            P.segs.push_back(Seg{(int64_t)start - m.base_pos, before, (int32_t)m.slot_start, start, len, -1, self});
+            before += len;
+        };
+        for (const int2 &s : r.sel) add(s.x, s.y, c->msgs[(size_t)s.x].len, false);
+        if (r.self_msg >= 0) add(r.self_msg, r.self_start, r.self_len, true);
+        wc.n_seg = P.segs.size() - wc.seg0;
+        P.q_pos.insert(P.q_pos.end(), r.q_pos.begin(), r.q_pos.end());
+        total_q += r.n_q;
+        if (total_q > INT32_MAX / 2) return pc_fail(c, PC_ERR_SHAPE, "attend_window: too many query rows");
+    }
+    return PC_OK;
+}
+
+// The runs that rows [row0, row1) of a call see, behind those there are; the number of their tiles.
+int32_t add_runs(WinPlan &P, const WinCall &wc, int32_t row0, int32_t row1)
+{
+    int32_t p_min = P.q_pos[(size_t)wc.q_off + row0];
+    for (int32_t r = row0 + 1; r < row1; ++r) p_min = std::min(p_min, P.q_pos[(size_t)wc.q_off + r]);
+    const int64_t low = win_low(p_min, P.window);
+    int64_t tiles = 0;
+    for (size_t i = wc.seg0; i < wc.seg0 + wc.n_seg; ++i) {
+        Seg &s = P.segs[i];
+        const int32_t end = s.self ? std::min(s.len, wc.own_first + row1) : s.len;
+        const int64_t skip = std::max<int64_t>(0, low - s.start);       // tokens in front of the window
+        const int32_t sinks = (int32_t)std::min<int64_t>(std::max<int64_t>(0, P.n_sink - s.before), end);
+        if (skip >= end && sinks == 0) continue;
+        if (s.rot < 0) {
+            if (P.rots.empty() || P.rots.back() != s.rot_pos) P.rots.push_back(s.rot_pos);
+            s.rot = (int32_t)P.rots.size() - 1;
+        }
+        auto run = [&](int32_t first, int32_t n_tok) {                  // (first: a multiple of the tile)
+            P.runs.push_back(PcWinRun{s.slot0 + first, s.start + first, n_tok, std::max(0, sinks - first), s.rot, s.self ? 1 : 0, s.rot_pos});
+            tiles += (n_tok + PC_TILE - 1) / PC_TILE;
+        };
+        const int32_t t0 = skip >= end ? end : (int32_t)skip / PC_TILE * PC_TILE, sink_end = (sinks + PC_TILE - 1) / PC_TILE * PC_TILE;
+        if (skip < end && t0 <= sink_end) {
+            run(0, end);                                 // (sinks and window touch, or there are no tokens in front of the window)
+        } else {
+            if (sinks > 0) run(0, sinks);
+            if (skip < end) run(t0, end - t0);
+        }
+    }
+    return (int32_t)tiles;
+}
+
+// A call's work for one group of rows, to be cut into splits.
+struct Group { int32_t call, unit0, run0, tiles; };
+
+// target: workgroups (of all KV heads) that fill the chip; least: tiles a split is worth
+void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups, std::vector<PcWinItem> &items, int64_t target, int32_t least, bool may_split)
+{
+    const int H_kv = c->cfg.n_kv_heads;
+    int64_t all = 0;
+    for (const Group &gr : groups) all += gr.tiles;
+    // a split's tiles: what brings the launch to its target (groups that are many already stay whole)
+    const int64_t chunk = may_split ? std::max<int64_t>(least, (all * H_kv + target - 1) / target) : INT32_MAX;
+    for (size_t a = 0; a < groups.size();) {
+        size_t b = a;
+        int32_t most = 0;
+        while (b < groups.size() && groups[b].call == groups[a].call) most = std::max(most, groups[b++].tiles);
+        const WinCall &wc = P.calls[(size_t)groups[a].call];
+        const int32_t n = (int32_t)std::max<int64_t>(1, std::min<int64_t>((most + chunk - 1) / chunk, MAX_SPLITS));
+        const int64_t part0 = P.part_rows;
+        for (int32_t s = 0; s < n; ++s)
+            for (size_t i = a; i < b; ++i) {
+                const Group &gr = groups[i];
+                const int32_t t0 = (int32_t)((int64_t)gr.tiles * s / n), t1 = (int32_t)((int64_t)gr.tiles * (s + 1) / n);
+                items.push_back(PcWinItem{wc.q_off, wc.n_q, gr.unit0, wc.lim0, gr.run0, t0, t1 - t0, n == 1 ? -1 : (int32_t)(part0 + (int64_t)s * wc.n_q)});
+            }
+        if (n > 1) {
+            for (int32_t r = 0; r < wc.n_q; ++r) P.merge.push_back(PcMergeRow{wc.q_off + r, (int32_t)(part0 + r), n, wc.n_q});
+            P.part_rows += (int64_t)n * wc.n_q;
+        }
+        a = b;
+    }
+}
+
+// the rows of a call that units [unit0, unit0 + n) of the bf16 kernels, or block unit0 of 32 columns of the fp32 kernels, hold
+void plan_items(const pc_cache *c, WinPlan &P, bool may_split)
+{
+    const int g = c->g;
+    P.pre.clear(); P.dec.clear(); P.runs.clear(); P.rots.clear(); P.merge.clear();
+    P.part_rows = 0;
+    for (Seg &s : P.segs) s.rot = -1;
+    std::vector<Group> pre, dec;
+    for (size_t i = 0; i < P.calls.size(); ++i) {
+        const WinCall &wc = P.calls[i];
+        if (c->cfg.dtype == PC_F32) {
+            const int64_t cols = (int64_t)wc.n_q * g;
+            for (int64_t u = 0; u * 32 < cols; ++u) {
+                const int32_t run0 = (int32_t)P.runs.size(), row0 = (int32_t)(32 * u / g), row1 = (int32_t)(std::min(32 * u + 31, cols - 1) / g) + 1;
+                const int32_t tiles = add_runs(P, wc, row0, row1);
+                pre.push_back(Group{(int32_t)i, (int32_t)u, run0, tiles});
+            }
+        } else if (wc.n_q == 1) {
+            const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, wc, 0, 1);
+            dec.push_back(Group{(int32_t)i, 0, run0, tiles});
+        } else {
+            const int32_t n_units = (wc.n_q + 31) / 32 * g;
+            int32_t b0 = -1, b1 = -1, run0 = 0, tiles = 0;
+            for (int32_t u = 0; u < n_units; u += 4) {
+                const int32_t first = u / g, last = std::min(u + 3, n_units - 1) / g;
+                if (first != b0 || last != b1) {         // (workgroups over the same rows share a list)
+                    b0 = first; b1 = last;
+                    run0 = (int32_t)P.runs.size();
+                    tiles = add_runs(P, wc, 32 * first, std::min(32 * (last + 1), wc.n_q));
+                }
+                pre.push_back(Group{(int32_t)i, u, run0, tiles});
+            }
+        }
+    }
+    make_items(c, P, pre, P.pre, 512, c->cfg.dtype == PC_F32 ? 4 : 6, may_split);
+    make_items(c, P, dec, P.dec, 512, 8, may_split);
+}
+
+// lists as they are staged, then what the device makes of them
+struct WinLayout { size_t pre, dec, runs, merge, q_pos, rots, lists, rot_q, rot_run, part_o, part_ml, total; };
+
+WinLayout lay_out(const pc_cache *c, const WinPlan &P)
+{
+    WinLayout L;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 16); return a; };
+    L.pre = take(sizeof(PcWinItem) * P.pre.size());
+    L.dec = take(sizeof(PcWinItem) * P.dec.size());
+    L.runs = take(sizeof(PcWinRun) * P.runs.size());
+    L.merge = take(sizeof(PcMergeRow) * P.merge.size());
+    L.q_pos = take(sizeof(int32_t) * P.q_pos.size());
+    L.rots = take(sizeof(int64_t) * P.rots.size());
+    L.lists = at;
+    auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
+    const size_t rot = P.pre.empty() ? 0 : sizeof(float2) * (size_t)c->half;
+    L.rot_q = big(rot * align_up(P.q_pos.size(), 32));
+    L.rot_run = big(rot * P.rots.size());
+    L.part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads * (size_t)c->D);
+    L.part_ml = big(sizeof(float) * 2 * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads);
+    L.total = align_up(at, 256);
+    return L;
+}
+
+void write_lists(const WinPlan &P, const WinLayout &L, char *to)
+{
+    auto put = [&](size_t at, const auto &v) { if (!v.empty()) std::memcpy(to + at, v.data(), sizeof(v[0]) * v.size()); };
+    put(L.pre, P.pre); put(L.dec, P.dec); put(L.runs, P.runs); put(L.merge, P.merge); put(L.q_pos, P.q_pos); put(L.rots, P.rots);
+}
+
+int32_t check(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink)
+{
+    if (n_calls < 0 || (n_calls > 0 && !calls)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: bad call list", what);
+    if (window < 1) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: window = %d must be >= 1", what, window);
+    if (n_sink < 0) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: n_sink = %d must be >= 0", what, n_sink);
+    return PC_OK;
+}
+
+int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out,
+                      float *lse, hipStream_t st, void *fixed_ws)
+{
+    int32_t rc = check(c, what, calls, n_calls, window, n_sink);
+    if (rc != PC_OK || n_calls == 0) return rc;
+    if (!c->host_only && (!q || !out)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: null q or out", what);
+    if (!c->host_only && ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)))
+        return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
+    WinPlan P;
+    P.window = window; P.n_sink = n_sink;
+    rc = resolve_all(c, calls, n_calls, P);
+    if (rc != PC_OK || c->host_only) return rc;
+    PcDeviceScope on(c);
+    if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
+    const bool recorded = pc_recorded(st);
+    if (recorded && !fixed_ws)
+        return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move: use pc_attend_window_static", what);
+    plan_items(c, P, true);
+    WinLayout L = lay_out(c, P);
+    if (fixed_ws && L.total > PC_STATIC_WS_BYTES) {
+        plan_items(c, P, false);
+        L = lay_out(c, P);
+        if (L.total > PC_STATIC_WS_BYTES)
+            return pc_fail(c, PC_ERR_NO_SPACE, "%s: needs a workspace of %zu bytes, the fixed one has %zu", what, L.total, PC_STATIC_WS_BYTES);
+    }
+    const bool in_args = L.lists <= PC_ARG_BYTES;
+    StageSlot *slot = nullptr;
+    std::vector<char> held;                              // lists of a call that is recorded (see pc_recorded)
+    PcArgBlob blob;
+    if (!in_args && !recorded && fixed_ws && L.lists > STAGE_BYTES)
+        return pc_fail(c, PC_ERR_NO_SPACE, "%s: lists of %zu bytes, a staging slot has %zu", what, L.lists, STAGE_BYTES);
+    if (!in_args && recorded) held.resize(align_up(L.lists, 16));
+    if (!fixed_ws) {
+        rc = pc_ensure_ws(c, L.total, st);
+        if (rc != PC_OK) return rc;
+    }
+    if (!in_args && !recorded) {
+        rc = pc_stage_acquire(c, L.lists, &slot);
+        if (rc != PC_OK) return rc;
+    }
+    char *ws = (char *)(fixed_ws ? fixed_ws : c->ws);
+    char *from = in_args ? (char *)blob.w : recorded ? held.data() : (char *)slot->host;
+    write_lists(P, L, from);
+
+    const bool bf16 = c->cfg.dtype == PC_BF16;
+    PcWin W{};
+    W.runs = (const PcWinRun *)(ws + L.runs);
+    W.q_pos = (const int32_t *)(ws + L.q_pos);
+    W.rot_q = (const float2 *)(ws + L.rot_q); W.rot_run = (const float2 *)(ws + L.rot_run);
+    W.inv_freq = c->inv_freq_dev;
+    W.k_store = c->k_store; W.v_store = c->v_store; W.q = q; W.out = out; W.lse = lse;
+    W.part_o = (float *)(ws + L.part_o); W.part_ml = (float *)(ws + L.part_ml);
+    W.slots = c->slots; W.n_q_heads = c->cfg.n_q_heads; W.n_kv_heads = c->cfg.n_kv_heads;
+    W.window = window;
+    W.scale_log2 = c->scale * 1.4426950408889634f;
+    // Lists in the arguments of the decode launch are read there; everything else reads them from the workspace.
+    const bool direct = in_args && P.pre.empty();
+    if (!direct) {
+        ProfScope ps(c, 1, st);
+        if (recorded && !in_args) pc_launch_store_args(from, L.lists, ws, st);
+        const bool turns = !P.pre.empty();
+        PcWinTurns T{};
+        T.from = in_args || recorded ? ws : slot->host; T.ws = ws; T.n16 = (int)(L.lists / 16);
+        T.off_q_pos = (int)L.q_pos; T.n_rows = turns ? (int)P.q_pos.size() : 0;
+        T.off_rot = (int)L.rots; T.n_rot = turns ? (int)P.rots.size() : 0;
+        T.D = c->D; T.lanes_order = bf16;
+        T.run_scale = bf16 ? W.scale_log2 : 1.f;
+        T.rot_q = (float2 *)(ws + L.rot_q); T.rot_run = (float2 *)(ws + L.rot_run);
+        T.inv_freq = c->inv_freq_dev;
+        if (!(recorded && !in_args) || turns) pc_launch_win_turns(T, in_args ? &blob : nullptr, st);
+        PC_HIP(c, hipGetLastError());
+        if (slot) { rc = pc_stage_release(c, slot, st); if (rc != PC_OK) return rc; }
+    }
+    if (!P.dec.empty()) {
+        ProfScope ps(c, 3, st);
+        W.items = (const PcWinItem *)(ws + L.dec);
+        const PcWinDecode O{(int32_t)L.dec, (int32_t)L.runs, (int32_t)L.q_pos, direct && !P.merge.empty() ? (int32_t)(L.lists / 16) : 0, ws};
+        static_assert(PC_ARG_BYTES / 16 <= 256, "a thread for every 16 bytes");
+        pc_launch_win_decode_bf16(W, (int)P.dec.size(), direct ? &blob : nullptr, O, st);
+        PC_HIP(c, hipGetLastError());
+    }
+    if (!P.pre.empty()) {
+        ProfScope ps(c, bf16 ? 2 : 5, st);
+        W.items = (const PcWinItem *)(ws + L.pre);
+        if (bf16) pc_launch_win_prefill_bf16(W, (int)P.pre.size(), st);
+        else pc_launch_win_attend_f32(W, (int)P.pre.size(), c->D, st);
+        PC_HIP(c, hipGetLastError());
+    }
+    if (!P.merge.empty()) {
+        ProfScope ps(c, 4, st);
+        pc_launch_win_merge(W, (const PcMergeRow *)(ws + L.merge), (int)P.merge.size(), c->cfg.dtype, c->D, st);
+        PC_HIP(c, hipGetLastError());
+    }
+    return PC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out, float *lse,
+                         void *stream)
+{
+    if (!c) return PC_ERR_INVALID_ARG;
+    return pc_guarded(c, [&] { return attend_window(c, "attend_window", calls, n_calls, window, n_sink, q, out, lse, (hipStream_t)stream, nullptr); });
+}
+
+int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out, float *lse,
+                                void *stream)
+{
+    if (!c) return PC_ERR_INVALID_ARG;
+    if (!c->host_only && !c->static_ws) return pc_fail(c, PC_ERR_HIP, "attend_window_static: the fixed scratch array was not found on this device");
+    const bool prof = c->prof;                           // kernel timing takes events from a pool that may have to grow
+    c->prof = false;
+    const int32_t rc = pc_guarded(c, [&] {
+        return attend_window(c, "attend_window_static", calls, n_calls, window, n_sink, q, out, lse, (hipStream_t)stream, c->static_ws);
+    });
+    c->prof = prof;
+    return rc;
+}
+
+}  // extern "C"
