@@ -126,7 +126,7 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, h_q, h_kv, D,
         assert np.array_equal(np.isnan(g), np.isnan(w)) and np.array_equal(g == np.inf, w == np.inf) and np.array_equal(g == -np.inf, w == -np.inf)
         fine = np.isfinite(w)
         say(f"  w {window}: {dead.sum()} rows left out, {(~fine).sum()} values not finite, {fine.sum()} finite")
-        if n_q > 1:
+        if n_q > 1 and window == 30:
             assert dead.any() and fine.any() and (h_kv == 1 or (~fine).any())
         assert np.abs(g[fine] - w[fine]).max(initial=0) <= {"f32": 3e-5, "bf16": 4e-2}[dtype]
     layer.cache.close()
@@ -135,19 +135,20 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, h_q, h_kv, D,
 @pytest.mark.parametrize("dtype,h_q,h_kv,D", [("bf16", 8, 2, 128), ("f32", 6, 2, 64)])
 def test_large_scores_move_the_reference(dtype, h_q, h_kv, D):
     """Scores of several hundred in the logarithm's units, the largest first, last and in the middle, of one sign and both: exact scores
-    (one-token messages at the rows' own position), so that bf16's roundings of keys and queries have no part in them."""
+    (one-token messages at the rows' own position, a scale of a power of two in the logarithm's base), so that bf16's roundings of keys and
+    queries have no part in them."""
     from paper_2512_23049_amd import binding
     import torch
     from pc_inputs import Call
     for order in ([-400, 0, 400], [400, 0, -400], [0, 700, -100], [-900, -890, -880], [0, 90, 150, 300, 500]):
-        cache = binding.Cache(h_q, h_kv, D, binding.PC_BF16 if dtype == "bf16" else binding.PC_F32, 10000.0, 4096, 64, softmax_scale=0.25)
+        cache = binding.Cache(h_q, h_kv, D, binding.PC_BF16 if dtype == "bf16" else binding.PC_F32, 10000.0, 4096, 64, softmax_scale=0.25 * float(np.log(2.0)))
         kind = torch.bfloat16 if dtype == "bf16" else torch.float32
         vals = []
         for i, s in enumerate(order):
             k, v = torch.zeros(1, h_kv, D, device="cuda:0", dtype=kind), torch.full((1, h_kv, D), float(i + 1), device="cuda:0", dtype=kind)
             k[:, :, 0] = s / 2.0
             cache.append_message(k.data_ptr(), v.data_ptr(), 1)
-            vals.append(s * 2.0)                         # 0.25 x 16 x s / 2
+            vals.append(s * 2.0 * np.log(2.0))           # 0.25 ln 2 x 16 x s / 2
             torch.cuda.synchronize()
         for n_q in (1, 40):
             q = torch.zeros(n_q, h_q, D, device="cuda:0", dtype=kind)
