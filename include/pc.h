@@ -278,6 +278,33 @@ int32_t pc_resolve_call(pc_cache *c, const pc_call *call, int32_t *starts_out,
  * adjacent freed spans merge; a span freed at the end shrinks the used region. */
 int32_t pc_message_free(pc_cache *c, int32_t msg_id);
 
+/* Forks (Sec. 4, branching workflows: several continuations of one message; a search that goes on from its best lines; an
+ * answer taken up again from its middle).  Each fork makes a new message of the tokens [first, first + len) of a cached one,
+ * copied within the cache: K and V as if those tokens had been appended, with room to grow (reserve as for
+ * pc_append_message), on one extent of its own whatever extents the tokens lie in.  The source stays as it is, and may be
+ * freed at once.
+ *   base   the position its first token's key is stored at (see pc_reposition): PC_POS_AUTO keeps the keys turned as they are
+ *          (base of the source + first), an exact copy; another one turns them on the way, with one more rounding to the
+ *          cache dtype.  What pc_attend computes does not depend on it.
+ * One launch for all of them; all or nothing.  msg_ids receives n consecutive new ids in list order.
+ * Errors (nothing enqueued): unknown id, first < 0, len < 1, tokens past the message's end, |base| (also the kept one) >
+ * max_position (PC_ERR_INVALID_ARG); no room for one of them or in the message table (PC_ERR_NO_SPACE); a stream that is being
+ * captured (a replay would copy between slots that may be another message's by then). */
+typedef struct { int32_t msg_id, first, len, reserve, base; } pc_fork;
+int32_t pc_message_fork(pc_cache *c, const pc_fork *forks, int32_t n, int32_t *msg_ids, void *stream);
+
+/* Closing up: the extents of the messages in the cache (reserves included) are moved down over the gaps that freed and
+ * swapped-out messages left, in their order, until they lie one behind the other from slot 0 on; what pc_cache_info reports
+ * as used is then what they hold, and a message as long as all that is free fits.  Ids, lengths, reserves and stored bases stay,
+ * K and V are bit for bit what they were.  max_slots > 0 stops before more than that many slots have been moved (but never
+ * before the first extent that has to move), for a program that closes up a little between its steps; a further call goes on from there.
+ * slots_moved (may be NULL) receives the slots moved.  One launch, in which every moved slot is read once and written
+ * once; nothing is enqueued where there is no gap.
+ * Slots that a caller knows (pc_message_info, pc_message_extents, pc_build_tables, rows of a gradient's d_k and d_v before
+ * pc_grad_keys_finalize), and graphs that hold recorded calls, are void afterwards.  Errors: max_slots < 0; a stream that is
+ * being captured (PC_ERR_INVALID_ARG). */
+int32_t pc_cache_compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, void *stream);
+
 /* Swap (Sec. 2.2 "Simplifying Assumptions", the note on caches that do not fit GPU memory, and
  * the note to Sec. 2.4's append-only cache: messages may be moved out to CPU memory for a while).
  * pc_message_swap_out copies the stored K and V of a live message (its whole reserved span, as
@@ -317,7 +344,7 @@ int32_t pc_cache_info(pc_cache *c, int32_t *n_messages, int64_t *slots_used,
  * 4 split merge, 5 fp32 attention, 6 table expansion, 7 reposition, 8 key gather.
  * A decode batch that goes to one launch counts under 3 as a whole: plan, a step's tokens, attention and merge.  One that goes
  * message by message: 1 its preparation (with a step's tokens), 3, 4.  fp32 batches with short lists plan in their attention
- * launch: no 1. */
+ * launch: no 1.  Forks count under 0, a cache closing up under 7, the windowed attention under 1 to 5 (fp32: 5). */
 #define PC_N_KERNEL_CLASSES 9
 int32_t pc_profile_enable(pc_cache *c, int32_t on);
 int32_t pc_profile_read(pc_cache *c, double ms_total[PC_N_KERNEL_CLASSES],

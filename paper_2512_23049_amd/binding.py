@@ -42,6 +42,10 @@ class pc_call(C.Structure):
                 ("self_start", C.c_int32), ("n_q", C.c_int32), ("q_pos", C.POINTER(C.c_int32))]
 
 
+class pc_fork(C.Structure):
+    _fields_ = [("msg_id", C.c_int32), ("first", C.c_int32), ("len", C.c_int32), ("reserve", C.c_int32), ("base", C.c_int32)]
+
+
 _lib = None
 
 
@@ -113,6 +117,10 @@ def lib():
         L.pc_attend_backward.argtypes = [vp, C.POINTER(pc_call), i32, vp, vp, vp, vp, vp, vp, vp]
         L.pc_grad_keys_finalize.restype = i32
         L.pc_grad_keys_finalize.argtypes = [vp, vp, vp]
+        L.pc_message_fork.restype = i32
+        L.pc_message_fork.argtypes = [vp, C.POINTER(pc_fork), i32, C.POINTER(i32), vp]
+        L.pc_cache_compact.restype = i32
+        L.pc_cache_compact.argtypes = [vp, i64, C.POINTER(i64), vp]
         L.pc_set_decode_sharing.restype = i32
         L.pc_set_decode_sharing.argtypes = [vp, i32]
         L.pc_set_key_gather.restype = i32
@@ -254,6 +262,20 @@ class Cache:
 
     def message_free(self, msg_id: int):
         self._check(lib().pc_message_free(self.h, msg_id))
+
+    def message_fork(self, forks, stream: int = 0):
+        """forks: (message, first token, tokens, reserve, base or None to keep the keys turned as they are); the new ids."""
+        n = len(forks)
+        arr, ids = (pc_fork * max(n, 1))(), (C.c_int32 * max(n, 1))()
+        for j, (m, first, length, reserve, base) in enumerate(forks):
+            arr[j] = pc_fork(int(m), int(first), int(length), int(reserve), PC_POS_AUTO if base is None else int(base))
+        self._check(lib().pc_message_fork(self.h, arr, n, ids, stream or None))
+        return [ids[i] for i in range(n)]
+
+    def compact(self, max_slots: int = 0, stream: int = 0) -> int:
+        moved = C.c_int64(0)
+        self._check(lib().pc_cache_compact(self.h, max_slots, C.byref(moved), stream or None))
+        return moved.value
 
     def message_base(self, msg_id: int) -> int:
         b = C.c_int32(0)

@@ -64,6 +64,9 @@ struct pc_cache {
     void *tok_dev = nullptr; size_t tok_cap = 0;          // staged items of pc_append_tokens* / pc_reposition_batch (bytes)
     StageSlot stage[N_STAGE]; int stage_next = 0;
     uint32_t *stage_done = nullptr;                     // what the slots' done point to
+    // the cache closing up (pc_copies.hip): the extents' order as it last left it, and the flags of its launches
+    std::vector<int32_t> slot_order; size_t order_seen = 0; bool order_stale = true;
+    uint32_t *flags_dev = nullptr; size_t flag_words = 0; uint32_t flag_epoch = 0, tickets = 0;
     // profiling
     bool prof = false;
     std::vector<ProfRec> prof_recs;
@@ -218,6 +221,11 @@ struct Planned {
 extern "C" int32_t pc_check_token_batch(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, const void *k, const void *v);
 extern "C" int32_t pc_append_token_items(pc_cache *c, const std::vector<int32_t> &ids, const void *k, const void *v, hipStream_t st,
                                          std::vector<PcTokenItem> *defer);
+// Slots of one message out of (spans, next): the first freed span that holds the reserve rounded up to the slot alignment, else the
+// end of the used region.  False (nothing changed) if neither has room.
+bool pc_take_slots(std::vector<FreeSpan> &spans, int64_t &next, int64_t capacity, int32_t res, int64_t &start);
+// Slots a whole message's copy into [start, start + res) writes: its tokens, and zeros up to where the span may hold leftovers.
+int32_t pc_rows_to_write(const pc_cache *c, int64_t start, int32_t len, int32_t res);
 int32_t pc_ensure_ws(pc_cache *c, size_t bytes, hipStream_t st);
 int32_t pc_stage_acquire(pc_cache *c, size_t bytes, StageSlot **out);
 int32_t pc_stage_release(pc_cache *c, StageSlot *s, hipStream_t st);      // what reads the slot has been enqueued on st: its event

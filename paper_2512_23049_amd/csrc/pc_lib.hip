@@ -219,6 +219,7 @@ int32_t pc_cache_destroy(pc_cache *c)
         if (c->inv_freq_dev) (void)hipFree(c->inv_freq_dev);
         if (c->table_dev) (void)hipFree(c->table_dev);
         if (c->counters_dev) (void)hipFree(c->counters_dev);
+        if (c->flags_dev) (void)hipFree(c->flags_dev);
         if (c->owns_storage && c->storage) (void)hipFree(c->storage);
     }
     delete c;
@@ -266,6 +267,11 @@ static void clear_if_reused(pc_cache *c, int64_t start, int32_t res, hipStream_t
     pc_launch_zero_span(c->cfg.dtype, c->k_store, c->slots, c->cfg.n_kv_heads, c->D, start, n, st);
     pc_launch_zero_span(c->cfg.dtype, c->v_store, c->slots, c->cfg.n_kv_heads, c->D, start, n, st);
 }
+
+}  // extern "C"
+bool pc_take_slots(std::vector<FreeSpan> &spans, int64_t &next, int64_t capacity, int32_t res, int64_t &start) { return take_slots(spans, next, capacity, res, start); }
+int32_t pc_rows_to_write(const pc_cache *c, int64_t start, int32_t len, int32_t res) { return pc_append_rows(c, start, len, res); }
+extern "C" {
 
 int32_t pc_append_message(pc_cache *c, const void *k, const void *v, int32_t len, int32_t reserve,
                           int32_t *msg_id, void *stream)
@@ -733,6 +739,7 @@ int32_t pc_message_swap_in(pc_cache *c, int32_t msg_id, const void *blob, void *
         m.slot_start = pl.second; m.live = true; m.swapped = false;
     }
     c->slots_in_id_order = false;                       // an old id may now sit behind newer ones
+    c->order_stale = true;
     c->free_spans.swap(spans);
     c->next_slot = next;
     return PC_OK;
