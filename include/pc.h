@@ -200,6 +200,24 @@ int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int
 int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
                                 const void *q, void *out, float *lse, void *stream);
 
+/* Gradient of pc_attend_window, as pc_attend_backward's of pc_attend: for the scalar sum(out * d_out),
+ *   q, out, lse   what pc_attend_window was given and wrote (same cache state, calls, window and n_sink), d_out like out;
+ *   d_q           [sum n_q][n_q_heads][head_dim] fp32: written;
+ *   d_k, d_v      [capacity slots][n_kv_heads][head_dim] fp32, indexed by physical slot: ADDED to at the slots of listed tokens,
+ *                 others stay as they are; pc_grad_keys_finalize(d_k) turns them, as behind pc_attend_backward, whose calls may
+ *                 collect in the same buffers.
+ * Rows that saw nothing, or a score that was not a number, have no gradient.  Keys and values that a row does not see have no
+ * part in its gradient, whatever is stored there; d_out and out are taken to be finite.  No sum depends on the order in which
+ * workgroups run: the same calls give the same bits.
+ * PC_F32: fp32 throughout.  PC_BF16: probabilities, their gradients and turned queries and keys are rounded to bf16 for
+ * the matrix instructions and summed in fp32 (pc_attend_backward cuts them in three exact pieces instead, at three times the matrix work).
+ * Refuses a stream that is being captured; every tensor 16-byte aligned, lse 4-byte (PC_ERR_INVALID_ARG).  Workspace: 17 KB for each block of 32
+ * rows and query head of a PC_BF16 cache, of at most 256 MB at a time (longer batches go in several runs), and the parts of tiles
+ * of keys that many rows see. */
+int32_t pc_attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
+                                  const void *q, const void *out, const float *lse, const void *d_out, float *d_q, float *d_k,
+                                  float *d_v, void *stream);
+
 /* One decode step of parallel calls in one call (Sec. 2.4 "Parallel API Calls" and the interleaved decoding of
  * parallel calls): pc_append_tokens_batch(msg_ids, n_msgs, k, v) followed by pc_attend(calls, ...), with the same
  * arguments, results and errors as the two.  What the fused form saves is the append's launch and its item list: where

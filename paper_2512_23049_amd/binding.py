@@ -83,6 +83,8 @@ def lib():
         for f in (L.pc_attend_window, L.pc_attend_window_static):
             f.restype = i32
             f.argtypes = [vp, C.POINTER(pc_call), i32, i32, i32, vp, vp, vp, vp]
+        L.pc_attend_window_backward.restype = i32
+        L.pc_attend_window_backward.argtypes = [vp, C.POINTER(pc_call), i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.pc_build_tables.restype = i32
         L.pc_build_tables.argtypes = [vp, C.POINTER(pc_call), vp, vp, i64, C.POINTER(i64), vp]
         L.pc_resolve_call.restype = i32
@@ -223,6 +225,12 @@ class Cache:
         arr, keep = marshalled if marshalled is not None else marshal_calls(calls)
         self._check(lib().pc_attend_window_static(self.h, arr, len(calls), window, n_sink, q_ptr or None, out_ptr or None,
                                                   lse_ptr or None, stream or None))
+
+    def attend_window_backward(self, calls, window: int, n_sink: int, q_ptr: int, out_ptr: int, lse_ptr: int, d_out_ptr: int, d_q_ptr: int,
+                               d_k_ptr: int, d_v_ptr: int, stream: int = 0, marshalled=None):
+        arr, keep = marshalled if marshalled is not None else marshal_calls(calls)
+        self._check(lib().pc_attend_window_backward(self.h, arr, len(calls), window, n_sink, q_ptr or None, out_ptr or None, lse_ptr or None,
+                                                    d_out_ptr or None, d_q_ptr or None, d_k_ptr or None, d_v_ptr or None, stream or None))
 
     def build_tables(self, call, kv_slot_ptr: int, kv_pos_ptr: int, cap: int, stream: int = 0) -> int:
         arr, keep = marshal_calls([call])

@@ -12,7 +12,7 @@ PROBE_SOURCES = ["pc_probe.hip"]
 SOURCES = ["pc_lib.hip", "pc_plan.hip", "pc_attend.hip", "pc_kernels_basic.hip", "pc_kernels_f32.hip", "pc_kernels_backward.hip",
            "pc_kernels_bwd_mfma.hip", "pc_kernels_mfma.hip", "pc_kernels_prefill.hip",
            "pc_kernels_shared.hip", "pc_window.hip", "pc_kernels_window.hip", "pc_kernels_window_f32.hip",
-           "pc_copies.hip", "pc_kernels_copies.hip"]
+           "pc_kernels_window_bwd.hip", "pc_kernels_window_bwd_f32.hip", "pc_copies.hip", "pc_kernels_copies.hip"]
 # the prefill kernel never produces NaNs in its max reductions: let the compiler drop the
 # canonicalising v_max x, x in front of every fmax
 # the gradient's key kernels hold more than 256 registers: results of their matrix instructions stay in vector registers

@@ -1,0 +1,554 @@
+// Gradient of the windowed attention, bf16 caches (gfx950), and what both types share.
+//
+// With p = exp(s - LSE) from the forward's LSE, dp = dO . v and Delta = dO . out of a row:
+//   ds = p (dp - Delta),  dq = scale sum ds k,  dk = scale sum ds q,  dv = sum p dO.
+// p and ds are rounded to bf16 for the second products, as in the forward; what is summed is fp32, and no sum depends on the
+// order in which workgroups run: a row's gradient belongs to one item (or to its splits, added up in order), a tile of keys to one
+// item (or to its parts, likewise), so that the same call gives the same bits.
+//
+//   prep   per 32 rows and head: Delta, the queries turned by their positions, output gradients and statistics, laid out for keys
+//   dq     rows: the forward's walk, with 24 matrix instructions a tile and unit (scores 8, dp 8, dq 8)
+//   keys   four tiles of keys: a walk over the units that see them (40: scores twice)
+//
+// Rotations.  dq is collected in the frame of the present run's keys and turned when the rotation changes; dk in the frame of the
+// turned queries, in which a call's keys are turned once.
+#include "pc_window.h"
+#include "pc_bwd_tiles.h"
+
+namespace {
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ bool finite16(uint32_t bits) { return (bits & 0x7F80u) != 0x7F80u; }
+__device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 x)
+{
+    uint4 u = __builtin_bit_cast(uint4, x);
+    uint32_t *w = reinterpret_cast<uint32_t *>(&u);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = (finite16(w[j]) ? w[j] & 0xFFFFu : 0u) | (finite16(w[j] >> 16) ? w[j] & 0xFFFF0000u : 0u);
+    return __builtin_bit_cast(bf16x8, u);
+}
+// Accumulators of 32 columns, element (db, r) dim 32 db + 8 (r / 4) + 4 hh + r % 4: every column turned by the angles of `a` less
+// those of `b` (rows of (cos, sin), 64 pairs; b null: by those of a), times f.
+__device__ __forceinline__ void turn_columns(f32x16 (&acc)[4], const float2 *a, const float2 *b, int hh, float f)
+{
+#pragma unroll
+    for (int db = 0; db < 2; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int at = 32 * db + 8 * q4 + 4 * hh;
+            const float4 a0 = *reinterpret_cast<const float4 *>(a + at), a1 = *reinterpret_cast<const float4 *>(a + at + 2);
+            const float ac[4] = {a0.x, a0.z, a1.x, a1.z}, as[4] = {a0.y, a0.w, a1.y, a1.w};
+            float4 b0 = make_float4(1.f, 0.f, 1.f, 0.f), b1 = b0;
+            if (b) { b0 = *reinterpret_cast<const float4 *>(b + at); b1 = *reinterpret_cast<const float4 *>(b + at + 2); }
+            const float bc[4] = {b0.x, b0.z, b1.x, b1.z}, bs[4] = {b0.y, b0.w, b1.y, b1.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float c = (ac[j] * bc[j] + as[j] * bs[j]) * f, s = (as[j] * bc[j] - ac[j] * bs[j]) * f;
+                const float x = acc[db][4 * q4 + j], y = acc[db + 2][4 * q4 + j];
+                acc[db][4 * q4 + j] = x * c - y * s;
+                acc[db + 2][4 * q4 + j] = x * s + y * c;
+            }
+            __builtin_amdgcn_sched_barrier(0);           // (registers: a few loads at a time)
+        }
+}
+
+}  // namespace
+
+// -------------------------------------------------------------------------------------------------------------- prep
+// bf16: a block of 32 rows of a head, eight threads a row; fp32: 32 (row, head) columns of a KV head.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd B)
+{
+    constexpr int HALF = D / 2, PER = HALF / 8;          // pairs a thread takes
+    __shared__ int s_lo[32], s_dead[32];
+    const PcWinBlock blk = B.blocks[blockIdx.x];
+    const int g = W.n_q_heads / W.n_kv_heads;
+    const int r = threadIdx.x >> 3, c = threadIdx.x & 7;
+    const int64_t unit = (int64_t)blockIdx.x * gridDim.y + blockIdx.y;
+    int64_t row, h;
+    bool ok;
+    if constexpr (BF16) {
+        row = 32 * (int64_t)blk.block + r; h = blockIdx.y; ok = row < blk.n_q;
+    } else {
+        const int64_t col = 32 * (int64_t)blk.block + r;
+        row = col / g; h = (int64_t)blockIdx.y * g + col % g; ok = row < blk.n_q;
+    }
+    const int64_t R = (int64_t)blk.q_off + (ok ? row : 0), at = (R * W.n_q_heads + (ok ? h : 0)) * D + PER * c;
+    const float lse = ok ? B.lse[R * W.n_q_heads + h] : -INFINITY;
+    const bool live = lse > -INFINITY;                   // (a row that saw nothing, or whose scores were not numbers, has no gradient)
+    float x[PER], y[PER], gx[PER], gy[PER], delta = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const float2 cs = W.rot_q[R * HALF + PER * c + i];
+        float qx, qy, ox, oy, dx, dy;
+        auto get = [&](const void *p, int64_t i) { return BF16 ? __uint_as_float((uint32_t)((const uint16_t *)p)[i] << 16) : ((const float *)p)[i]; };
+        qx = get(W.q, at + i); qy = get(W.q, at + i + HALF);
+        ox = get(B.out, at + i); oy = get(B.out, at + i + HALF);
+        dx = get(B.d_out, at + i); dy = get(B.d_out, at + i + HALF);
+        x[i] = live ? qx * cs.x - qy * cs.y : 0.f; y[i] = live ? qx * cs.y + qy * cs.x : 0.f;
+        gx[i] = live ? dx : 0.f; gy[i] = live ? dy : 0.f;
+        delta += live ? dx * ox + dy * oy : 0.f;
+    }
+    delta += __shfl_xor(delta, 1); delta += __shfl_xor(delta, 2); delta += __shfl_xor(delta, 4);
+    const int64_t to = (unit * 32 + r) * D + PER * c;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if constexpr (BF16) {
+            ((uint16_t *)B.q_abs)[to + i] = to_bf16(x[i]); ((uint16_t *)B.q_abs)[to + i + HALF] = to_bf16(y[i]);
+            ((uint16_t *)B.d_o)[to + i] = to_bf16(gx[i]); ((uint16_t *)B.d_o)[to + i + HALF] = to_bf16(gy[i]);
+        } else {
+            ((float *)B.q_abs)[to + i] = x[i]; ((float *)B.q_abs)[to + i + HALF] = y[i];
+            ((float *)B.d_o)[to + i] = gx[i]; ((float *)B.d_o)[to + i + HALF] = gy[i];
+        }
+    }
+    const int lo = win_low(W.q_pos[R], W.window);
+    if (c == 0) {
+        char *st = B.stat + unit * PC_WIN_STAT_BYTES;
+        reinterpret_cast<PcWinStat *>(st)[r] = PcWinStat{live ? lse * 1.4426950408889634f : INFINITY, delta, lo, blk.lim0 + (int)(ok ? row : 0)};
+        if (ok) B.delta[R * W.n_q_heads + h] = delta;
+        s_lo[r] = ok ? lo : INT32_MAX;
+        s_dead[r] = !live;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int lo_min = INT32_MAX, lo_max = INT32_MIN;
+        for (int i = 0; i < 32; ++i) {
+            lo_min = min(lo_min, s_lo[i]);
+            lo_max = s_dead[i] ? INT32_MAX : max(lo_max, s_lo[i]);
+        }
+        const int64_t first = BF16 ? 32 * (int64_t)blk.block : 32 * (int64_t)blk.block / g;
+        const int64_t last = min((int64_t)blk.n_q - 1, BF16 ? first + 31 : (32 * (int64_t)blk.block + 31) / g);
+        *reinterpret_cast<PcWinStatHead *>(B.stat + unit * PC_WIN_STAT_BYTES + 32 * sizeof(PcWinStat)) =
+            PcWinStatHead{lo_min, lo_max, blk.lim0 + (int)first, blk.lim0 + (int)last};
+    }
+}
+
+void pc_launch_win_bwd_prep(const PcWin &W, const PcWinBwd &B, int dtype, int D, hipStream_t st)
+{
+    if (B.n_blocks <= 0) return;
+    const dim3 grid((unsigned)B.n_blocks, (unsigned)(dtype == 1 ? W.n_q_heads : W.n_kv_heads));
+    if (dtype == 1) pc_win_bwd_prep_kernel<128, true><<<grid, 256, 0, st>>>(W, B);
+    else if (D == 64) pc_win_bwd_prep_kernel<64, false><<<grid, 256, 0, st>>>(W, B);
+    else pc_win_bwd_prep_kernel<128, false><<<grid, 256, 0, st>>>(W, B);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- dq
+// As the forward's prefill kernel: 4 waves = 4 units, two workgroups a compute unit, K and V tiles in a ring of four.
+__global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcWinBwd B)
+{
+    constexpr int RING = 4, AHEAD = 3;
+    __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][2 * TILE_BYTES];
+
+    const int kh = blockIdx.x % W.n_kv_heads;
+    const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
+    const int g = W.n_q_heads / W.n_kv_heads;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int n_units = ((item.n_q + 31) >> 5) * g;
+    const bool unit_ok = item.unit0 + wave < n_units;
+    const int unit = unit_ok ? item.unit0 + wave : item.unit0;
+    const int ub = unit / g, h = kh * g + (unit - ub * g);
+    const int row = min(32 * ub + n, item.n_q - 1);
+    const bool row_ok = unit_ok && 32 * ub + n < item.n_q;
+    const int64_t R = (int64_t)item.q_off + row;
+    const float lse = B.lse[R * W.n_q_heads + h];
+    const bool live = row_ok && lse > -INFINITY;
+    const float lse2 = live ? lse * 1.4426950408889634f : INFINITY, delta = live ? B.delta[R * W.n_q_heads + h] : 0.f;
+    const int lo = win_low(W.q_pos[R], W.window), lim = item.lim0 + row;
+    int lo_max = live ? lo : INT32_MAX;                  // (a row without a gradient: every tile is masked)
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o));
+    lo_max = uniform(lo_max);
+    const bool some_dead = __builtin_amdgcn_ballot_w64(!live) != 0;
+    const int lim_first = item.lim0 + 32 * ub;
+
+    const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * W.slots * (PC_D * 2);
+    const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * W.slots * (PC_D * 2);
+    const unsigned ring = (unsigned)(uintptr_t)&s_kv[0][0], lds0 = ring + wave * 1024;
+    const unsigned k_src = (threadIdx.x >> 4) * 256 + (((threadIdx.x & 15) ^ swz(threadIdx.x >> 4)) << 4);
+    const unsigned v_src = (unsigned)v_src_chunk(threadIdx.x) * 16;
+    auto request = [&](const WinTile &d, int slot) __attribute__((always_inline)) {
+        const int64_t at = (int64_t)d.slot0 * (PC_D * 2);
+        const unsigned to = lds0 + slot * (2 * TILE_BYTES);
+        dma16(kb + at, k_src, to);
+        dma16(kb + at, k_src + 4096, to + 4096);         // (rows 16 up: the same order of chunks)
+        dma16(vb + at, v_src, to + TILE_BYTES);
+        dma16(vb + at, v_src + 4096, to + TILE_BYTES + 4096);
+    };
+    const RowMajor rk(perm_row(n), lane);
+    const ValuesByKey<true> rv(lane);
+
+    bf16x8 go[8];                                        // the lane's row of output gradients, dims 16 ks + 8 hh + 0..7
+    {
+        const unsigned char *p = (const unsigned char *)B.d_out + (R * W.n_q_heads + h) * (PC_D * 2) + 16 * hh;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) go[ks] = __builtin_bit_cast(bf16x8, live ? ldg16(p + 32 * ks) : make_uint4(0, 0, 0, 0));
+    }
+    bf16x8 qop[8];
+    auto turn = [&](int rot) __attribute__((always_inline)) {       // as in the forward: the same bits but for a rounding of the scale
+        const float4 *rq = reinterpret_cast<const float4 *>(W.rot_q + R * (PC_D / 2) + 8 * hh);
+        const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)rot * (PC_D / 2) + 8 * hh);
+        const unsigned char *qp = (const unsigned char *)W.q + (R * W.n_q_heads + h) * (PC_D * 2) + 16 * hh;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            uint4 lq = ldg16(qp + 32 * ks), hq = ldg16(qp + 32 * ks + 128);
+            if (!live) lq = hq = make_uint4(0, 0, 0, 0);
+            const uint32_t lw[4] = {lq.x, lq.y, lq.z, lq.w}, hw[4] = {hq.x, hq.y, hq.z, hq.w};
+            uint32_t a[4], b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float4 p = rq[8 * ks + j];
+                const float4 r = rr[8 * ks + j];
+                const float c0 = (p.x * r.x + p.y * r.y) * W.scale_log2, s0 = (p.y * r.x - p.x * r.y) * W.scale_log2;
+                const float c1 = (p.z * r.z + p.w * r.w) * W.scale_log2, s1 = (p.w * r.z - p.z * r.w) * W.scale_log2;
+                const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
+                a[j] = pack_bf16(x0 * c0 - y0 * s0, x1 * c1 - y1 * s1);
+                b[j] = pack_bf16(x0 * s0 + y0 * c0, x1 * s1 + y1 * c1);
+            }
+            qop[ks] = frag4(a[0], a[1], a[2], a[3]);
+            qop[ks + 4] = frag4(b[0], b[1], b[2], b[3]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    f32x16 acc[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+
+    const int T = item.n_tiles;
+    int cur = -1;
+    if (T > 0) {
+        WinWalk walk(W.runs + item.run0, item.skip);
+        WinTile d[AHEAD + 1];
+        int asked = 0;
+        auto ask = [&](WinTile &to, int slot) __attribute__((always_inline)) {
+            if (asked >= T) return;
+            if (asked > 0) walk.next();
+            ++asked;
+            to = walk.tile();
+            request(to, slot);
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) ask(d[i], i);
+#pragma unroll 1
+        for (int t = 0, u = 0; t < T; ++t, u = (u + 1) & (RING - 1)) {
+            const unsigned kt = ring + u * (2 * TILE_BYTES), vt = kt + TILE_BYTES;
+            if (t + AHEAD <= T) wait_vm<4 * (AHEAD - 1)>();
+            else wait_vm<0>();
+            ring_barrier();
+            const WinTile e = d[0];
+            if (e.rot != cur) {
+                if (cur >= 0) turn_columns(acc, W.rot_run + (int64_t)cur * (PC_D / 2), W.rot_run + (int64_t)e.rot * (PC_D / 2), hh, 1.f);
+                cur = e.rot;
+                turn(cur);
+            }
+            ask(d[AHEAD], (u + AHEAD) & (RING - 1));
+            f32x16 s, dp;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) s = MFMA32(rk.by_row(kt, ks), qop[ks], s);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) dp = MFMA32(rv.get(vt, ks), go[ks], dp);
+            const bool edge = some_dead || e.valid < PC_TILE || (e.self && lim_first - e.pos0 < PC_TILE - 1) || (lo_max > e.pos0 && e.sink < PC_TILE);
+            bool odd = false;
+            uint32_t sees = ~0u;
+            if (__builtin_expect(edge, 0)) {
+                sees = live ? win_sees(e.pos0, e.valid, e.sink, e.self != 0, lo, lim) : 0u;
+                f32x16 z;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[r] = 0.f;
+                const bf16x8 zero = frag4(0, 0, 0, 0);
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) z = MFMA32(rk.by_row(kt, ks), zero, z);
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += z[r];
+                odd = __builtin_amdgcn_ballot_w64(sum != 0.f) != 0;          // (a key that is not finite)
+            }
+            uint32_t pk[8];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = ex2(s[r] - lse2) * (dp[r] - delta);
+            if (__builtin_expect(edge, 0)) {
+                const int mine = (int)(sees >> (8 * hh));
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = (mine >> (16 * (r >> 3) + (r & 7))) & 1 ? s[r] : 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) pk[r] = pack_bf16(s[2 * r], s[2 * r + 1]);
+            const bf16x8 ds[2] = {frag4(pk[0], pk[1], pk[2], pk[3]), frag4(pk[4], pk[5], pk[6], pk[7])};
+            if (__builtin_expect(odd, 0)) {              // (the rows that see such a key have no gradient, or a probability of 0)
+#pragma unroll
+                for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(finite_or_zero(rk.by_col(kt, f >> 2, f & 3)), ds[f >> 2], acc[f & 3]);
+            } else {
+#pragma unroll
+                for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(rk.by_col(kt, f >> 2, f & 3), ds[f >> 2], acc[f & 3]);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) d[i] = d[i + 1];
+        }
+    }
+    // back from the last run's frame and the row's position, and out as whole lines (in two halves of a row, 256 bytes each)
+    if (cur >= 0) turn_columns(acc, W.rot_run + (int64_t)cur * (PC_D / 2), W.rot_q + R * (PC_D / 2), hh, B.scale);
+    ring_barrier();
+    unsigned char *stg = &s_kv[0][0] + wave * TILE_BYTES;
+    const int r4 = lane >> 4, c = lane & 15;
+    float *dst = (item.part < 0 ? B.d_q + (int64_t)item.q_off * W.n_q_heads * PC_D : W.part_o + (int64_t)item.part * W.n_q_heads * PC_D) + (int64_t)h * PC_D + 4 * c;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int db = 0; db < 2; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x16 &a = acc[2 * half + db];
+                *reinterpret_cast<float4 *>(stg + n * 256 + (((8 * db + 2 * q4 + hh) ^ (n & 15)) << 4)) = make_float4(a[4 * q4], a[4 * q4 + 1], a[4 * q4 + 2], a[4 * q4 + 3]);
+            }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + r4, rw = 32 * ub + r;
+            const float4 v = *reinterpret_cast<const float4 *>(stg + r * 256 + ((c ^ (r & 15)) << 4));
+            if (unit_ok && rw < item.n_q) *reinterpret_cast<float4 *>(dst + (int64_t)rw * W.n_q_heads * PC_D + 64 * half) = v;
+        }
+    }
+}
+
+void pc_launch_win_bwd_dq_bf16(const PcWin &W, const PcWinBwd &B, int n_items, hipStream_t st)
+{
+    if (n_items > 0) pc_win_bwd_dq_bf16_kernel<<<(unsigned)n_items * W.n_kv_heads, 256, 0, st>>>(W, B);
+}
+
+__global__ __launch_bounds__(256) void pc_win_bwd_rows_kernel(const PcMergeRow *__restrict__ rows, int64_t n, int row16, const float *__restrict__ part, float *__restrict__ d_q)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const PcMergeRow mr = rows[i / row16];
+    const int64_t at = i % row16;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < mr.n_splits; ++s) {
+        const float4 x = reinterpret_cast<const float4 *>(part)[((int64_t)mr.part_row0 + (int64_t)s * mr.n_q) * row16 + at];
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    }
+    reinterpret_cast<float4 *>(d_q)[(int64_t)mr.row * row16 + at] = sum;
+}
+
+void pc_launch_win_bwd_rows(const PcWin &W, const PcWinBwd &B, const PcMergeRow *rows, int n_rows, int D, hipStream_t st)
+{
+    if (n_rows <= 0) return;
+    const int row16 = W.n_q_heads * D / 4;
+    const int64_t n = (int64_t)n_rows * row16;
+    pc_win_bwd_rows_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(rows, n, row16, W.part_o, B.d_q);
+}
+
+// -------------------------------------------------------------------------------------------------------------- keys
+// A workgroup is 8 waves over four tiles of keys: waves 0 to 3 collect dv of a tile each, waves 4 to 7 dk (the scores are made
+// twice, which costs a fifth more matrix work; one wave with both sums would need 330 registers, and a SIMD would have one wave).
+// The units' turned queries, output gradients and statistics come by direct loads into a ring of four.
+__global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, PcWinBwd B)
+{
+    constexpr int RING = 4, AHEAD = 3, SLOT = 2 * TILE_BYTES + PC_WIN_STAT_BYTES;
+    __shared__ __attribute__((aligned(1024))) unsigned char s_ring[RING][SLOT];
+
+    const int kh = blockIdx.x % W.n_kv_heads;
+    const PcWinKeyItem item = B.key_items[blockIdx.x / W.n_kv_heads];
+    const int g = W.n_q_heads / W.n_kv_heads;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int tile = wave & 3;
+    const bool is_k = wave >= 4;
+    const unsigned ring = (unsigned)(uintptr_t)&s_ring[0][0];
+    const unsigned src = (threadIdx.x >> 4) * 256 + (((threadIdx.x & 15) ^ swz(threadIdx.x >> 4)) << 4);
+    const RowMajor by_row(perm_row(n), lane), by_col(n, lane);
+    const int my_keys = item.n_keys - PC_TILE * tile;    // of the wave's tile
+
+    f32x16 acc[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+    int cur = -1;
+    for (int a = 0; a < item.n_apps; ++a) {
+        const PcWinApp app = B.apps[item.app0 + a];
+        const int pos0 = app.pos0 + PC_TILE * tile, valid = min(app.n_tok - PC_TILE * tile, PC_TILE), sink = min(max(app.sink - PC_TILE * tile, 0), PC_TILE);
+        const bool active = valid > 0;
+        const int U = app.n_blocks * g;
+        auto unit_of = [&](int i) { return (int64_t)(app.block0 + i / g) * W.n_q_heads + kh * g + i % g; };
+        auto request = [&](int i, int slot) __attribute__((always_inline)) {
+            const int64_t u = unit_of(i);
+            const unsigned to = ring + slot * SLOT + wave * 1024;
+            dma16((const unsigned char *)B.q_abs + u * TILE_BYTES, src, to);
+            dma16((const unsigned char *)B.d_o + u * TILE_BYTES, src, to + TILE_BYTES);
+            if (wave == 0) dma16(B.stat + u * PC_WIN_STAT_BYTES, lane * 16, to + 2 * TILE_BYTES);
+        };
+        ring_barrier();                                  // (the last call's units are no longer read)
+        for (int i = 0; i < min(AHEAD, U); ++i) request(i, i);
+        bf16x8 kop[8], vop[8];                           // the lane's key, turned and scaled, and its value: dims 16 ks + 8 hh + 0..7
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) kop[ks] = vop[ks] = frag4(0, 0, 0, 0);
+        if (active) {
+            const int64_t slot = (int64_t)kh * W.slots + item.slot0 + PC_TILE * tile + n;
+            const unsigned char *kp = (const unsigned char *)W.k_store + slot * (PC_D * 2) + 16 * hh;
+            const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)app.rot * (PC_D / 2) + 8 * hh);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                const uint4 lk = ldg16(kp + 32 * ks), hk = ldg16(kp + 32 * ks + 128);
+                const uint32_t lw[4] = {lk.x, lk.y, lk.z, lk.w}, hw[4] = {hk.x, hk.y, hk.z, hk.w};
+                uint32_t x[4], y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float4 r = rr[8 * ks + j];
+                    r.x *= W.scale_log2; r.y *= W.scale_log2; r.z *= W.scale_log2; r.w *= W.scale_log2;
+                    const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
+                    x[j] = pack_bf16(x0 * r.x - y0 * r.y, x1 * r.z - y1 * r.w);
+                    y[j] = pack_bf16(x0 * r.y + y0 * r.x, x1 * r.w + y1 * r.z);
+                }
+                kop[ks] = frag4(x[0], x[1], x[2], x[3]);
+                kop[ks + 4] = frag4(y[0], y[1], y[2], y[3]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (is_k) {
+                const uint16_t *vp = (const uint16_t *)W.v_store + (slot / PC_VGROUP * PC_D + 8 * hh) * PC_VGROUP + slot % PC_VGROUP;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = (uint32_t)vp[(16 * ks + 2 * j) * PC_VGROUP] | ((uint32_t)vp[(16 * ks + 2 * j + 1) * PC_VGROUP] << 16);
+                    vop[ks] = frag4(w[0], w[1], w[2], w[3]);
+                }
+                // dk, kept in the frame of the queries: from the last call's to this one's
+                if (cur >= 0 && cur != app.rot) turn_columns(acc, W.rot_run + (int64_t)app.rot * (PC_D / 2), W.rot_run + (int64_t)cur * (PC_D / 2), hh, 1.f);
+                cur = app.rot;
+            }
+        }
+#pragma unroll 1
+        for (int i = 0, u = 0; i < U; ++i, u = (u + 1) & (RING - 1)) {
+            const unsigned qt = ring + u * SLOT, gt = qt + TILE_BYTES;
+            if (i + AHEAD > U) wait_vm<0>();
+            else if (wave == 0) wait_vm<3 * (AHEAD - 1)>();
+            else wait_vm<2 * (AHEAD - 1)>();
+            ring_barrier();
+            if (i + AHEAD < U) request(i + AHEAD, (u + AHEAD) & (RING - 1));
+            const unsigned char *stat = &s_ring[u][2 * TILE_BYTES];
+            const int4 hd = *reinterpret_cast<const int4 *>(stat + 32 * sizeof(PcWinStat));
+            const int lo_min = uniform(hd.x), lo_max = uniform(hd.y), lim_first = uniform(hd.z), lim_last = uniform(hd.w);
+            // nothing of the tile is seen by the unit
+            if (!active || (app.self && lim_last < pos0) || (sink == 0 && lo_min > pos0 && (unsigned)lo_min - (unsigned)pos0 > PC_TILE - 1u)) continue;
+            const bool edge = valid < PC_TILE || (app.self && lim_first - pos0 < PC_TILE - 1) || lo_max == INT32_MAX || (lo_max > pos0 && sink < PC_TILE);
+            f32x16 s;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) s = MFMA32(by_row.by_row(qt, ks), kop[ks], s);
+            // register r: row 16 (r / 8) + 8 hh + r % 8, column: the lane's key
+            const float4 *rows = reinterpret_cast<const float4 *>(stat) + 8 * hh;
+            float dl[16];
+            uint32_t seen = 0xFFFFu;                     // bit r
+            if (__builtin_expect(edge, 0)) {
+                seen = 0;
+                const int pos = pos0 + min(n, valid - 1);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float4 x = rows[16 * (r >> 3) + (r & 7)];
+                    const bool see = (n < valid) & (x.x < INFINITY) & ((pos >= __float_as_int(x.z)) | (n < sink)) & (!app.self | (pos <= __float_as_int(x.w)));
+                    seen |= see ? 1u << r : 0u;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float2 x = *reinterpret_cast<const float2 *>(rows + 16 * (r >> 3) + (r & 7));
+                s[r] = ex2(s[r] - x.x);
+                dl[r] = x.y;
+            }
+            if (is_k) {
+                f32x16 dp;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) dp = MFMA32(by_row.by_row(gt, ks), vop[ks], dp);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] *= dp[r] - dl[r];
+            }
+            if (__builtin_expect(edge, 0)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = (seen >> r) & 1 ? s[r] : 0.f;
+            }
+            uint32_t pk[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) pk[r] = pack_bf16(s[2 * r], s[2 * r + 1]);
+            const bf16x8 x[2] = {frag4(pk[0], pk[1], pk[2], pk[3]), frag4(pk[4], pk[5], pk[6], pk[7])};
+            const unsigned other = is_k ? qt : gt;
+#pragma unroll
+            for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(by_col.by_col(other, f >> 2, f & 3), x[f >> 2], acc[f & 3]);
+        }
+    }
+    if (my_keys <= 0) return;
+    if (is_k && cur >= 0) {                              // back by the run's rotation (keys as they are stored)
+        const float2 *rr = W.rot_run + (int64_t)cur * (PC_D / 2);
+#pragma unroll
+        for (int db = 0; db < 2; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const int at = 32 * db + 8 * q4 + 4 * hh;
+                const float4 a0 = *reinterpret_cast<const float4 *>(rr + at), a1 = *reinterpret_cast<const float4 *>(rr + at + 2);
+                const float c[4] = {a0.x, a0.z, a1.x, a1.z}, s[4] = {a0.y, a0.w, a1.y, a1.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = acc[db][4 * q4 + j] * B.scale, y = acc[db + 2][4 * q4 + j] * B.scale;
+                    acc[db][4 * q4 + j] = x * c[j] + y * s[j];
+                    acc[db + 2][4 * q4 + j] = y * c[j] - x * s[j];
+                }
+            }
+    }
+    if (item.part >= 0) {
+        float *to = B.key_part + ((((int64_t)item.part * W.n_kv_heads + kh) * 2 + (is_k ? 0 : 1)) * (PC_WIN_KEY_TILES * PC_TILE) + PC_TILE * tile + n) * PC_D + 4 * hh;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4)
+                *reinterpret_cast<float4 *>(to + 32 * db + 8 * q4) = make_float4(acc[db][4 * q4], acc[db][4 * q4 + 1], acc[db][4 * q4 + 2], acc[db][4 * q4 + 3]);
+        return;
+    }
+    if (n >= my_keys) return;
+    float *to = (is_k ? B.d_k : B.d_v) + (((int64_t)item.slot0 + PC_TILE * tile + n) * W.n_kv_heads + kh) * PC_D + 4 * hh;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            float4 *p = reinterpret_cast<float4 *>(to + 32 * db + 8 * q4), v = *p;
+            v.x += acc[db][4 * q4]; v.y += acc[db][4 * q4 + 1]; v.z += acc[db][4 * q4 + 2]; v.w += acc[db][4 * q4 + 3];
+            *p = v;
+        }
+}
+
+void pc_launch_win_bwd_keys_bf16(const PcWin &W, const PcWinBwd &B, hipStream_t st)
+{
+    if (B.n_key_items > 0) pc_win_bwd_keys_bf16_kernel<<<(unsigned)B.n_key_items * W.n_kv_heads, 512, 0, st>>>(W, B);
+}
+
+// The parts of tiles that several items collect, added up in their order and to what is there.
+template <int D>
+__global__ __launch_bounds__(256) void pc_win_bwd_sums_kernel(PcWinBwd B, int H)
+{
+    const PcWinSum sm = B.sums[blockIdx.x];
+    const int kh = blockIdx.y, which = blockIdx.z;       // keys, values
+    constexpr int KEYS = PC_WIN_KEY_TILES * PC_TILE;
+    for (int i = threadIdx.x; i < sm.n_keys * (D / 4); i += 256) {
+        const int key = i / (D / 4), d4 = i % (D / 4);
+        float4 *p = reinterpret_cast<float4 *>((which ? B.d_v : B.d_k) + (((int64_t)sm.slot0 + key) * H + kh) * D) + d4, v = *p;
+        for (int s = 0; s < sm.n_parts; ++s) {
+            const float4 x = reinterpret_cast<const float4 *>(B.key_part + ((((int64_t)(sm.part0 + s) * H + kh) * 2 + which) * KEYS + key) * D)[d4];
+            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        }
+        *p = v;
+    }
+}
+
+void pc_launch_win_bwd_sums(const PcWin &W, const PcWinBwd &B, int D, hipStream_t st)
+{
+    if (B.n_sums <= 0) return;
+    const dim3 grid((unsigned)B.n_sums, (unsigned)W.n_kv_heads, 2);
+    if (D == 64) pc_win_bwd_sums_kernel<64><<<grid, 256, 0, st>>>(B, W.n_kv_heads);
+    else pc_win_bwd_sums_kernel<128><<<grid, 256, 0, st>>>(B, W.n_kv_heads);
+}

@@ -51,6 +51,56 @@ struct PcWin {
 // Offsets of a decode launch's lists, where they travel in its arguments.
 struct PcWinDecode { int32_t off_items, off_runs, off_q_pos, n16; void *ws; };      // n16 > 0: so many pieces of 16 bytes are left in the workspace for the merge
 
+// ---- the gradient ----
+// 32 rows (fp32: 32 (row, head) columns of a KV head) of a call.
+struct PcWinBlock { int32_t q_off, n_q, lim0, block; };
+// A call that lists the extent a key item's tiles belong to.
+struct PcWinApp {
+    int32_t pos0;             // position the call gives the item's first token
+    int32_t n_tok;            // the call's tokens from there on
+    int32_t sink;             // the first of them that are visible at any distance
+    int32_t rot;              // row of the rotation table
+    int32_t self;             // 1: the call's new message
+    int32_t block0, n_blocks; // the blocks that may see some of the item's tokens
+    int32_t pad;
+};
+#define PC_WIN_KEY_TILES 4
+struct PcWinKeyItem {         // up to four tiles of an extent, and calls (or some of their blocks) that see them
+    int32_t slot0;
+    int32_t n_keys;           // tokens of the extent from there on (at most 128)
+    int32_t app0, n_apps;
+    int32_t part;             // -1: the only item of its tiles; else where its sums go
+    int32_t pad[3];
+};
+struct PcWinSum { int32_t slot0, n_keys, part0, n_parts; };       // tiles whose items' sums are added up
+struct PcWinStat { float lse2, delta; int32_t lo, lim; };         // of a row: lse log2 e (+inf: no gradient), Delta, the positions it sees
+struct PcWinStatHead { int32_t lo_min, lo_max, lim_first, lim_last; };       // of a block's rows; lo_max: INT32_MAX if some row has no gradient
+#define PC_WIN_STAT_BYTES 1024
+struct PcWinBwd {
+    const PcWinBlock   *blocks;
+    const PcWinApp     *apps;
+    const PcWinKeyItem *key_items;
+    const PcWinSum     *sums;
+    int32_t n_blocks, n_key_items, n_sums, pad;
+    const void  *out, *d_out;
+    const float *lse;
+    float       *delta;       // [rows][H_q]
+    void        *q_abs;       // [unit][32][D] queries turned by their positions, in the cache's type; unit: (block, head), fp32: (block, KV head)
+    void        *d_o;         // [unit][32][D] the output gradients, zeros for rows without
+    char        *stat;        // [unit][PC_WIN_STAT_BYTES]: PcWinStat of 32 rows, PcWinStatHead
+    float       *key_part;    // [part][KV head][keys, values][128][D]
+    float       *d_q, *d_k, *d_v;
+    float        scale;
+};
+void pc_launch_win_bwd_prep(const PcWin &W, const PcWinBwd &B, int dtype, int D, hipStream_t st);
+void pc_launch_win_bwd_dq_bf16(const PcWin &W, const PcWinBwd &B, int n_items, hipStream_t st);
+void pc_launch_win_bwd_dq_f32(const PcWin &W, const PcWinBwd &B, int n_items, int D, hipStream_t st);
+// the splits of a row's gradient, added up in their order
+void pc_launch_win_bwd_rows(const PcWin &W, const PcWinBwd &B, const PcMergeRow *rows, int n_rows, int D, hipStream_t st);
+void pc_launch_win_bwd_keys_bf16(const PcWin &W, const PcWinBwd &B, hipStream_t st);
+void pc_launch_win_bwd_keys_f32(const PcWin &W, const PcWinBwd &B, int D, hipStream_t st);
+void pc_launch_win_bwd_sums(const PcWin &W, const PcWinBwd &B, int D, hipStream_t st);
+
 // float2 index of pair i of packed row R in the lanes' order of the bf16 prefill kernel (D = 128): 16 bytes a lane, lanes of
 // consecutive rows side by side
 __host__ __device__ __forceinline__ int64_t win_rot_at(int64_t R, int i)

@@ -17,6 +17,7 @@ struct Seg {
 struct WinCall {
     int32_t q_off, n_q, lim0, own_first;      // own_first: index (within the last extent of the new message) of row 0's token
     size_t seg0, n_seg;
+    int32_t row0, row1;                       // the rows that are planned for
 };
 struct WinPlan {
     std::vector<Resolved> res;
@@ -42,6 +43,7 @@ int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan 
         const Resolved &r = P.res[(size_t)i];
         WinCall &wc = P.calls[(size_t)i];
         wc.q_off = (int32_t)total_q; wc.n_q = r.n_q;
+        wc.row0 = 0; wc.row1 = r.n_q;
         wc.own_first = r.self_msg >= 0 ? r.self_len - r.n_q : 0;
         wc.lim0 = r.self_msg >= 0 ? r.self_start + wc.own_first : 0;
         wc.seg0 = P.segs.size();
@@ -118,7 +120,7 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
                 items.push_back(PcWinItem{wc.q_off, wc.n_q, gr.unit0, wc.lim0, gr.run0, t0, t1 - t0, n == 1 ? -1 : (int32_t)(part0 + (int64_t)s * wc.n_q)});
             }
         if (n > 1) {
-            for (int32_t r = 0; r < wc.n_q; ++r) P.merge.push_back(PcMergeRow{wc.q_off + r, (int32_t)(part0 + r), n, wc.n_q});
+            for (int32_t r = wc.row0; r < wc.row1; ++r) P.merge.push_back(PcMergeRow{wc.q_off + r, (int32_t)(part0 + r), n, wc.n_q});
             P.part_rows += (int64_t)n * wc.n_q;
         }
         a = b;
@@ -192,6 +194,140 @@ void write_lists(const WinPlan &P, const WinLayout &L, char *to)
 {
     auto put = [&](size_t at, const auto &v) { if (!v.empty()) std::memcpy(to + at, v.data(), sizeof(v[0]) * v.size()); };
     put(L.pre, P.pre); put(L.dec, P.dec); put(L.runs, P.runs); put(L.merge, P.merge); put(L.q_pos, P.q_pos); put(L.rots, P.rots);
+}
+
+// ---- the gradient -------------------------------------------------------------------------------------------------
+constexpr size_t BWD_BYTES = (size_t)256 << 20;          // workspace that a run's blocks may take
+
+struct BwdPlan {
+    std::vector<PcWinBlock> blocks;
+    std::vector<PcWinApp> apps;
+    std::vector<PcWinKeyItem> keys;
+    std::vector<PcWinSum> sums;
+    int32_t parts = 0;
+};
+
+// One run over some blocks of the calls: call i's [range[i].x, range[i].y).
+void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<int2> &range)
+{
+    const int g = c->g, H_kv = c->cfg.n_kv_heads;
+    const bool f32 = c->cfg.dtype == PC_F32;
+    P.pre.clear(); P.dec.clear(); P.runs.clear(); P.rots.clear(); P.merge.clear();
+    P.part_rows = 0;
+    for (Seg &s : P.segs) s.rot = -1;
+    B = BwdPlan{};
+    std::vector<Group> groups;
+    std::vector<int32_t> block0(P.calls.size()), low;     // a call's first block in the run; the least position each block sees
+    auto rows_of = [&](const WinCall &wc, int32_t b) {
+        return f32 ? make_int2((int)((int64_t)32 * b / g), (int)std::min<int64_t>(wc.n_q, ((int64_t)32 * b + 31) / g + 1)) : make_int2(32 * b, std::min(32 * b + 32, wc.n_q));
+    };
+    for (size_t i = 0; i < P.calls.size(); ++i) {
+        WinCall &wc = P.calls[i];
+        block0[i] = (int32_t)B.blocks.size();
+        if (range[i].x >= range[i].y) { wc.row0 = wc.row1 = 0; continue; }
+        wc.row0 = rows_of(wc, range[i].x).x; wc.row1 = rows_of(wc, range[i].y - 1).y;
+        for (int32_t b = range[i].x; b < range[i].y; ++b) {
+            const int2 r = rows_of(wc, b);
+            int32_t p_min = INT32_MAX;
+            for (int32_t k = r.x; k < r.y; ++k) p_min = std::min(p_min, P.q_pos[(size_t)wc.q_off + k]);
+            low.push_back(win_low(p_min, P.window));
+            B.blocks.push_back(PcWinBlock{wc.q_off, wc.n_q, wc.lim0, b});
+            if (f32) {
+                const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, wc, r.x, r.y);
+                groups.push_back(Group{(int32_t)i, b, run0, tiles});
+            }
+        }
+        if (!f32) {
+            const int32_t n_units = range[i].y * g;
+            int32_t b0 = -1, b1 = -1, run0 = 0, tiles = 0;
+            for (int32_t u = range[i].x * g; u < n_units; u += 4) {
+                const int32_t first = u / g, last = std::min(u + 3, n_units - 1) / g;
+                if (first != b0 || last != b1) {
+                    b0 = first; b1 = last;
+                    run0 = (int32_t)P.runs.size();
+                    tiles = add_runs(P, wc, 32 * first, std::min(32 * (last + 1), wc.n_q));
+                }
+                groups.push_back(Group{(int32_t)i, u, run0, tiles});
+            }
+        }
+    }
+    make_items(c, P, groups, P.pre, 512, 6, true);
+
+    // keys: who lists each extent, extents in slot order
+    struct Listed { int32_t slot0; uint32_t call, seg; };
+    std::vector<Listed> listed;
+    for (size_t i = 0; i < P.calls.size(); ++i)
+        if (range[i].x < range[i].y)
+            for (size_t k = P.calls[i].seg0; k < P.calls[i].seg0 + P.calls[i].n_seg; ++k) listed.push_back(Listed{P.segs[k].slot0, (uint32_t)i, (uint32_t)k});
+    std::stable_sort(listed.begin(), listed.end(), [](const Listed &a, const Listed &b) { return a.slot0 < b.slot0; });
+    struct Tiles { int32_t slot0, n_keys; size_t app0, n_apps; int64_t blocks; };
+    std::vector<Tiles> all;
+    std::vector<PcWinApp> apps;
+    int64_t total = 0;
+    constexpr int32_t KEYS = PC_WIN_KEY_TILES * PC_TILE;
+    for (size_t a = 0; a < listed.size();) {
+        size_t b = a;
+        while (b < listed.size() && listed[b].slot0 == listed[a].slot0) ++b;
+        const int32_t len = P.segs[listed[a].seg].len;
+        for (int32_t first = 0; first < len; first += KEYS) {
+            Tiles t{listed[a].slot0 + first, std::min(KEYS, len - first), apps.size(), 0, 0};
+            for (size_t k = a; k < b; ++k) {
+                const WinCall &wc = P.calls[listed[k].call];
+                Seg &s = P.segs[listed[k].seg];
+                const int32_t end = s.self ? std::min(s.len, wc.own_first + wc.row1) : s.len;
+                if (first >= end) continue;
+                const int32_t sinks = (int32_t)std::min<int64_t>(std::max<int64_t>(0, P.n_sink - s.before - first), end - first);
+                const int32_t last_pos = s.start + std::min(first + KEYS, end) - 1;
+                const int2 rg = range[listed[k].call];
+                int32_t b0 = -1, b1 = -1;
+                for (int32_t bl = rg.x; bl < rg.y; ++bl) {
+                    const bool sees = (sinks > 0 || low[(size_t)(block0[listed[k].call] + bl - rg.x)] <= last_pos) && (!s.self || wc.own_first + rows_of(wc, bl).y - 1 >= first);
+                    if (!sees) continue;
+                    if (b0 < 0) b0 = bl;
+                    b1 = bl + 1;
+                }
+                if (b0 < 0) continue;
+                if (s.rot < 0) {
+                    if (P.rots.empty() || P.rots.back() != s.rot_pos) P.rots.push_back(s.rot_pos);
+                    s.rot = (int32_t)P.rots.size() - 1;
+                }
+                apps.push_back(PcWinApp{s.start + first, end - first, sinks, s.rot, s.self ? 1 : 0, block0[listed[k].call] + b0 - rg.x, b1 - b0, 0});
+                t.blocks += b1 - b0;
+            }
+            t.n_apps = apps.size() - t.app0;
+            total += t.blocks;
+            if (t.n_apps > 0) all.push_back(t);
+        }
+        a = b;
+    }
+    // An item's share: what brings the launch to two workgroups a compute unit; tiles with more (those that every row sees,
+    // messages that many calls list) are cut and their parts added up.
+    const int64_t share = std::max<int64_t>(4, (total * H_kv + 511) / 512);
+    for (const Tiles &t : all) {
+        const int64_t n = t.blocks * 4 > share * 5 ? std::min<int64_t>((t.blocks + share - 1) / share, 1024) : 1;
+        const int32_t part0 = B.parts;
+        size_t k = t.app0;
+        int32_t taken = 0;                               // blocks of app k that earlier parts have
+        int64_t done = 0;
+        for (int64_t part = 0; part < n; ++part) {
+            const int64_t upto = t.blocks * (part + 1) / n;
+            PcWinKeyItem it{t.slot0, t.n_keys, (int32_t)B.apps.size(), 0, n == 1 ? -1 : part0 + (int32_t)part, {0, 0, 0}};
+            while (done < upto) {
+                const int32_t m = (int32_t)std::min<int64_t>(apps[k].n_blocks - taken, upto - done);
+                PcWinApp app = apps[k];
+                app.block0 += taken; app.n_blocks = m;
+                B.apps.push_back(app);
+                done += m; taken += m;
+                if (taken == apps[k].n_blocks) { ++k; taken = 0; }
+            }
+            it.n_apps = (int32_t)B.apps.size() - it.app0;
+            B.keys.push_back(it);
+        }
+        if (n > 1) {
+            B.sums.push_back(PcWinSum{t.slot0, t.n_keys, part0, (int32_t)n});
+            B.parts += (int32_t)n;
+        }
+    }
 }
 
 int32_t check(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink)
@@ -298,9 +434,129 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     return PC_OK;
 }
 
+int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, PcWin W, PcWinBwd G, hipStream_t st)
+{
+    const bool bf16 = c->cfg.dtype == PC_BF16;
+    const int Hq = c->cfg.n_q_heads, H = c->cfg.n_kv_heads;
+    BwdPlan B;
+    plan_backward(c, P, B, range);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 16); return a; };
+    auto of = [](const auto &v) { return sizeof(v[0]) * v.size(); };
+    const size_t items = take(of(P.pre)), runs = take(of(P.runs)), merge = take(of(P.merge)), q_pos = take(of(P.q_pos)), rots = take(of(P.rots));
+    const size_t blocks = take(of(B.blocks)), apps = take(of(B.apps)), keys = take(of(B.keys)), sums = take(of(B.sums)), lists = at;
+    auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
+    const size_t rot = sizeof(float2) * (size_t)c->half, units = B.blocks.size() * (size_t)(bf16 ? Hq : H), unit = 32 * (size_t)c->D * c->esize;
+    const size_t rot_q = big(rot * P.q_pos.size()), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * P.q_pos.size() * (size_t)Hq);
+    const size_t q_abs = big(unit * units), d_o = big(unit * units), stat = big(PC_WIN_STAT_BYTES * units);
+    const size_t part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)Hq * (size_t)c->D);
+    const size_t key_part = big(sizeof(float) * 2 * PC_WIN_KEY_TILES * PC_TILE * (size_t)B.parts * (size_t)H * (size_t)c->D);
+    int32_t rc = pc_ensure_ws(c, align_up(at, 256), st);
+    if (rc != PC_OK) return rc;
+    char *ws = (char *)c->ws;
+    PcArgBlob blob;
+    StageSlot *slot = nullptr;
+    const bool in_args = lists <= PC_ARG_BYTES;
+    if (!in_args) {
+        rc = pc_stage_acquire(c, lists, &slot);
+        if (rc != PC_OK) return rc;
+    }
+    char *from = in_args ? (char *)blob.w : (char *)slot->host;
+    auto put = [&](size_t to, const auto &v) { if (!v.empty()) std::memcpy(from + to, v.data(), of(v)); };
+    put(items, P.pre); put(runs, P.runs); put(merge, P.merge); put(q_pos, P.q_pos); put(rots, P.rots);
+    put(blocks, B.blocks); put(apps, B.apps); put(keys, B.keys); put(sums, B.sums);
+
+    W.items = (const PcWinItem *)(ws + items); W.runs = (const PcWinRun *)(ws + runs); W.q_pos = (const int32_t *)(ws + q_pos);
+    W.rot_q = (const float2 *)(ws + rot_q); W.rot_run = (const float2 *)(ws + rot_run);
+    W.part_o = (float *)(ws + part_o);
+    G.blocks = (const PcWinBlock *)(ws + blocks); G.apps = (const PcWinApp *)(ws + apps);
+    G.key_items = (const PcWinKeyItem *)(ws + keys); G.sums = (const PcWinSum *)(ws + sums);
+    G.n_blocks = (int32_t)B.blocks.size(); G.n_key_items = (int32_t)B.keys.size(); G.n_sums = (int32_t)B.sums.size();
+    G.delta = (float *)(ws + delta); G.q_abs = ws + q_abs; G.d_o = ws + d_o; G.stat = ws + stat; G.key_part = (float *)(ws + key_part);
+    PcWinTurns T{};
+    T.from = in_args ? ws : slot->host; T.ws = ws; T.n16 = (int)(lists / 16);
+    T.off_q_pos = (int)q_pos; T.n_rows = (int)P.q_pos.size(); T.off_rot = (int)rots; T.n_rot = (int)P.rots.size();
+    T.D = c->D; T.lanes_order = 0; T.run_scale = 1.f;
+    T.rot_q = (float2 *)(ws + rot_q); T.rot_run = (float2 *)(ws + rot_run); T.inv_freq = c->inv_freq_dev;
+    ProfScope ps(c, 5, st);
+    pc_launch_win_turns(T, in_args ? &blob : nullptr, st);
+    PC_HIP(c, hipGetLastError());
+    if (slot) { rc = pc_stage_release(c, slot, st); if (rc != PC_OK) return rc; }
+    pc_launch_win_bwd_prep(W, G, c->cfg.dtype, c->D, st);
+    if (bf16) pc_launch_win_bwd_dq_bf16(W, G, (int)P.pre.size(), st);
+    else pc_launch_win_bwd_dq_f32(W, G, (int)P.pre.size(), c->D, st);
+    pc_launch_win_bwd_rows(W, G, (const PcMergeRow *)(ws + merge), (int)P.merge.size(), c->D, st);
+    if (bf16) pc_launch_win_bwd_keys_bf16(W, G, st);
+    else pc_launch_win_bwd_keys_f32(W, G, c->D, st);
+    pc_launch_win_bwd_sums(W, G, c->D, st);
+    PC_HIP(c, hipGetLastError());
+    return PC_OK;
+}
+
+int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, const void *out,
+                               const float *lse, const void *d_out, float *d_q, float *d_k, float *d_v, hipStream_t st)
+{
+    const char *what = "attend_window_backward";
+    int32_t rc = check(c, what, calls, n_calls, window, n_sink);
+    if (rc != PC_OK || n_calls == 0) return rc;
+    if (!c->host_only) {
+        if (!q || !out || !lse || !d_out || !d_q || !d_k || !d_v) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: null argument", what);
+        const uintptr_t all = (uintptr_t)q | (uintptr_t)out | (uintptr_t)d_out | (uintptr_t)d_q | (uintptr_t)d_k | (uintptr_t)d_v;
+        if ((all & 15) || ((uintptr_t)lse & 3)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned, lse 4-byte", what);
+    }
+    WinPlan P;
+    P.window = window; P.n_sink = n_sink;
+    rc = resolve_all(c, calls, n_calls, P);
+    if (rc != PC_OK || c->host_only) return rc;
+    PcDeviceScope on(c);
+    if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
+    if (pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move", what);
+    const bool bf16 = c->cfg.dtype == PC_BF16;
+    PcWin W{};
+    W.inv_freq = c->inv_freq_dev;
+    W.k_store = c->k_store; W.v_store = c->v_store; W.q = q;
+    W.slots = c->slots; W.n_q_heads = c->cfg.n_q_heads; W.n_kv_heads = c->cfg.n_kv_heads;
+    W.window = window;
+    W.scale_log2 = c->scale * 1.4426950408889634f;
+    PcWinBwd G{};
+    G.out = out; G.d_out = d_out; G.lse = lse; G.d_q = d_q; G.d_k = d_k; G.d_v = d_v; G.scale = c->scale;
+    // Runs of blocks whose workspace fits.  A run ends with a call, or where units and rows end together: after four blocks of 32 rows
+    // (a workgroup's units), or the columns of 32 rows.
+    const int64_t per_block = (int64_t)(bf16 ? c->cfg.n_q_heads : c->cfg.n_kv_heads) * (2 * 32 * c->D * (int64_t)c->esize + PC_WIN_STAT_BYTES);
+    const int64_t step = bf16 ? 4 : c->g, most = std::max<int64_t>(step, (int64_t)BWD_BYTES / per_block / step * step);
+    std::vector<int2> range(P.calls.size(), make_int2(0, 0));
+    int64_t in_run = 0;
+    for (size_t i = 0; i < P.calls.size(); ++i) {
+        const int64_t n = bf16 ? (P.calls[i].n_q + 31) / 32 : ((int64_t)P.calls[i].n_q * c->g + 31) / 32;
+        for (int64_t b = 0; b < n;) {
+            const int64_t room = (most - in_run) / step * step, m = std::min(n - b, room);
+            if (m > 0) {
+                range[i] = make_int2((int)b, (int)(b + m));
+                b += m; in_run += m;
+            }
+            if (b < n || m == 0) {
+                rc = backward_run(c, P, range, W, G, st);
+                if (rc != PC_OK) return rc;
+                std::fill(range.begin(), range.end(), make_int2(0, 0));
+                in_run = 0;
+            }
+        }
+    }
+    return in_run > 0 ? backward_run(c, P, range, W, G, st) : PC_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int32_t pc_attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, const void *out,
+                                  const float *lse, const void *d_out, float *d_q, float *d_k, float *d_v, void *stream)
+{
+    if (!c) return PC_ERR_INVALID_ARG;
+    return pc_guarded(c, [&] {
+        return attend_window_backward(c, calls, n_calls, window, n_sink, q, out, lse, d_out, d_q, d_k, d_v, (hipStream_t)stream);
+    });
+}
 
 int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out, float *lse,
                          void *stream)
