@@ -6,6 +6,8 @@
 #include "pc_window.h"
 #include "pc_mfma_common.h"
 
+#include <type_traits>
+
 #define TILE_BYTES 8192
 #define LAZY_LOG2 64.0f
 #define MFMA32(a, b, c) __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0)
@@ -103,6 +105,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
 {
     constexpr int RING = 4, AHEAD = 3;
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][2 * TILE_BYTES];
+    __shared__ int s_again;
 
     const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
     const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
@@ -116,29 +119,33 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
     const int last_row = min(32 * ub + 31, item.n_q - 1), row = min(32 * ub + n, last_row);
     const bool row_ok = unit_ok && 32 * ub + n < item.n_q;
     const int64_t R = (int64_t)item.q_off + row;
-    const int lo = win_low(W.q_pos[R], W.window), lim = item.lim0 + row;
-    int lo_max = lo;                                     // of the wave's rows
+    const int lim = item.lim0 + row, lim_first = item.lim0 + 32 * ub;       // (lim_first: uniform)
+    int lo = 0, lo_max = 0;                              // the least position the row sees; the largest such of the wave's rows
+    auto look_up_rows = [&]() __attribute__((always_inline)) {
+        lo = win_low(W.q_pos[R], W.window);
+        lo_max = lo;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o));
-    lo_max = uniform(lo_max);
-    const int lim_first = item.lim0 + 32 * ub;           // (uniform)
+        for (int o = 1; o < 32; o <<= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o));
+        lo_max = uniform(lo_max);
+    };
 
     const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * W.slots * (PC_D * 2);
     const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * W.slots * (PC_D * 2);
     // chunk position p of a K tile holds chunk (p & 15) ^ (p >> 4 & 15) of row p >> 4
     const unsigned lds0 = (unsigned)(uintptr_t)&s_kv[0][0] + wave * 1024;
     const unsigned k_src = (threadIdx.x >> 4) * 256 + (((threadIdx.x & 15) ^ (threadIdx.x >> 4 & 15)) << 4), v_src = threadIdx.x * 16;
-    auto request = [&](const WinTile &d, int slot) __attribute__((always_inline)) {
-        const int64_t at = (int64_t)d.slot0 * (PC_D * 2);
+    auto request = [&](int slot0, int slot) __attribute__((always_inline)) {
+        const int64_t at = (int64_t)slot0 * (PC_D * 2);
         const unsigned to = lds0 + slot * (2 * TILE_BYTES);
         dma16(kb + at, k_src, to);
-        dma16(kb + at, k_src + 4096, to + 4096);         // (rows 16 up: the same chunk order)
+        dma16(kb + at + 4096, k_src, to + 4096);         // (rows 16 up: the same chunk order)
         dma16(vb + at, v_src, to + TILE_BYTES);
-        dma16(vb + at, v_src + 4096, to + TILE_BYTES + 4096);
+        dma16(vb + at + 4096, v_src, to + TILE_BYTES + 4096);
     };
 
     bf16x8 qop[8];
-    auto turn = [&](int rot) __attribute__((always_inline)) {
+    // (few: in the walk, what is read for all of it at once would not fit the registers)
+    auto turn = [&](int rot, auto few) __attribute__((always_inline)) {
         const float4 *rq = reinterpret_cast<const float4 *>(W.rot_q) + (R >> 5) * 1024 + hh * 32 + (R & 31);
         const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)rot * (PC_D / 2) + 8 * hh);
         // the lane's row, as it came (from the cache each time: 32 registers): dims 16 ks + 8 hh + 0..7, then 64 up
@@ -159,59 +166,134 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
             }
             qop[ks] = __builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3]));
             qop[ks + 4] = __builtin_bit_cast(bf16x8, make_uint4(b[0], b[1], b[2], b[3]));
-            __builtin_amdgcn_sched_barrier(0);       // (what is read for all four at once would not fit the registers)
+            if (decltype(few)::value && (ks & 1)) __builtin_amdgcn_sched_barrier(0);
         }
     };
 
     // K row of the lane's MFMA row: permuted so that score registers 0..7 / 8..15 are keys 8 hh + 0..7 / 16 + 8 hh + 0..7
     const int krow = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
     typedef const __attribute__((address_space(3))) bf16x8 *lds_frag;
-    unsigned k_rd[8];
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-        k_rd[ks] = (unsigned)(uintptr_t)&s_kv[0][krow * 256 + (((2 * ks + hh) ^ (krow & 15)) << 4)];
-        asm volatile("" : "+v"(k_rd[ks]));
-    }
+    // fragment ks of a tile of keys at k_base ^ 32 ks
+    unsigned k_base = (unsigned)(uintptr_t)&s_kv[0][krow * 256 + ((hh ^ (krow & 15)) << 4)];
+    asm volatile("" : "+v"(k_base));
     unsigned v_rd = (unsigned)(uintptr_t)&s_kv[0][TILE_BYTES + (hh * PC_D + n) * 16];
     asm volatile("" : "+v"(v_rd));
 
     float m_ref = 0.f, l_run = 0.f;
-    bool seen = false, all_seen = false;                 // the row has met a key; every row of the wave has
-    f32x16 acc[4], start;                                // start: -m_ref
+    bool seen = false, all_seen = false, shifted = false;          // the row has met a key; every row of the wave has; some row's reference has moved
+    f32x16 acc[4];
+    const f32x16 zeros = (f32x16){0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        start[r] = 0.f;
-#pragma unroll
-        for (int db = 0; db < 4; ++db) acc[db][r] = 0.f;
-    }
+    for (int db = 0; db < 4; ++db) acc[db] = zeros;
 
+    auto fi = [](float x) { return __float_as_int(x); };
+    auto largest = [&](const f32x16 &s) __attribute__((always_inline)) {        // (on the bit patterns: right wherever some score is positive)
+        int m = imax3(fi(s[0]), fi(s[1]), fi(s[2]));
+#pragma unroll
+        for (int r = 3; r < 15; r += 2) m = imax3(m, fi(s[r]), fi(s[r + 1]));
+        return max(m, fi(s[15]));
+    };
+    // the reference moves, if a row's scores ask for it; s: scores less the reference
+    auto rebase = [&](f32x16 &s) __attribute__((always_inline)) {
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        mx = fmaxf(mx, other_half(mx));
+        const bool now = mx > -INFINITY, need = mx > LAZY_LOG2 || (!seen && now && mx < -LAZY_LOG2);
+        seen |= now;
+        all_seen = __builtin_amdgcn_ballot_w64(seen) == ~0ull;
+        if (__builtin_amdgcn_ballot_w64(need) != 0) {
+            const float shift = need ? mx : 0.f, alpha = ex2(-fmaxf(shift, 0.f));       // (down: nothing has been added yet)
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < 4; ++db) acc[db] *= alpha;
+            m_ref += shift;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] -= shift;
+            shifted = __builtin_amdgcn_ballot_w64(m_ref != 0.f) != 0;
+        }
+    };
+    auto less_reference = [&](f32x16 &s) __attribute__((always_inline)) {
+        if (__builtin_expect(shifted, 0)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] -= m_ref;
+        }
+    };
     const int T = item.n_tiles;
-    if (T > 0) {
-        WinWalk walk(W.runs + item.run0, item.skip);
-        WinTile d[AHEAD + 1];
+    bool met_odd = false;                                // a value that is not finite, in a tile that some row does not see all of
+    // The item's tiles.  ODD: with such values taken care of, as the first walk, which looks for them, does not: what that takes would
+    // cost it its registers.
+    auto walk_tiles = [&](auto odd_c) __attribute__((always_inline)) {
+        constexpr bool ODD = decltype(odd_c)::value;
+        // two walks over the same runs: of the tiles that are asked for, and of those that are worked on
+        WinWalk ahead(W.runs + item.run0, item.skip, T), walk = ahead;
         int asked = 0;
-        auto ask = [&](WinTile &to, int slot) __attribute__((always_inline)) {
+        auto ask = [&](int slot) __attribute__((always_inline)) {
             if (asked >= T) return;
-            if (asked > 0) walk.next();
-            ++asked;
-            to = walk.tile();
-            request(to, slot);
+            request(ahead.a.x, slot);
+            if (++asked < T) ahead.next();
         };
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) ask(d[i], i);
-        int cur = -1;
+        for (int i = 0; i < AHEAD; ++i) ask(i);
+        int cur = walk.rot;
+        turn(cur, std::false_type{});
+        look_up_rows();                                  // (behind the first requests: its latency is not theirs)
+        int t = 0;
 #pragma unroll 1
-        for (int t = 0, u = 0; t < T; ++t, u = (u + 1) & (RING - 1)) {
+        while (t < T) {
+            // Four tiles of which every row sees everything, the ring's slots as constants: nothing is looked up, masked or turned.
+            if (!ODD && (t & (RING - 1)) == 0 && walk.a.z >= RING * PC_TILE && walk.rot == cur && all_seen && !shifted &&
+                (lo_max <= walk.a.y || walk.a.w >= RING * PC_TILE) && (!walk.self || lim_first - walk.a.y >= RING * PC_TILE - 1) &&
+                T - asked >= RING && ahead.a.z > (RING - 1) * PC_TILE) {
+                const int slot0 = ahead.a.x;
+#pragma unroll
+                for (int u = 0; u < RING; ++u) {
+                    const int at = u * 2 * TILE_BYTES;
+                    wait_vm<4 * (AHEAD - 1)>();
+                    ring_barrier();
+                    request(slot0 + PC_TILE * u, (u + AHEAD) & (RING - 1));
+                    f32x16 s = zeros;
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) s = MFMA32(*(lds_frag)((k_base ^ (ks << 5)) + at), qop[ks], s);
+                    bf16x8 fr[8];
+#pragma unroll
+                    for (int f = 0; f < 8; ++f) fr[f] = *(lds_frag)(v_rd + at + ((f >> 2) * 2 * PC_D + 32 * (f & 3)) * 16);
+                    less_reference(s);
+                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(largest(s) > fi(LAZY_LOG2)) != 0, 0)) rebase(s);
+                    uint32_t pk[8];
+                    float ps = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const float a = ex2(s[2 * r]), b = ex2(s[2 * r + 1]);
+                        ps += a;
+                        ps += b;
+                        pk[r] = pack_bf16(a, b);
+                    }
+                    l_run += ps;
+                    const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
+#pragma unroll
+                    for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(fr[f], p[f >> 2], acc[f & 3]);
+                }
+                asked += RING;
+                ahead.pass(RING - 1);
+                if (asked < T) ahead.next();
+                t += RING;
+                walk.pass(RING - 1);
+                if (t < T) walk.next();
+                continue;
+            }
+            const int u = t & (RING - 1);
             const unsigned at = u * (2 * TILE_BYTES);
             if (t + AHEAD <= T) wait_vm<4 * (AHEAD - 1)>();        // this wave's share of tile t has landed
             else wait_vm<0>();
             ring_barrier();                              // ... every wave's has, and tile t - 1 is no longer read
-            const WinTile e = d[0];
-            if (e.rot != cur) { cur = e.rot; turn(cur); }
-            ask(d[AHEAD], (u + AHEAD) & (RING - 1));
-            f32x16 s = start;
+            const WinTile e = walk.tile();
+            if (__builtin_expect(e.rot != cur, 0)) { cur = e.rot; turn(cur, std::true_type{}); }
+            ask((u + AHEAD) & (RING - 1));
+            f32x16 s = zeros;
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) s = MFMA32(*(lds_frag)(k_rd[ks] + at), qop[ks], s);
+            for (int ks = 0; ks < 8; ++ks) s = MFMA32(*(lds_frag)((k_base ^ (ks << 5)) + at), qop[ks], s);
+            less_reference(s);
             const bool edge = e.valid < PC_TILE || (e.self && lim_first - e.pos0 < PC_TILE - 1) || (lo_max > e.pos0 && e.sink < PC_TILE);
             uint32_t sees = ~0u;
             bool none = false;
@@ -223,35 +305,14 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
                 for (int r = 0; r < 16; ++r) s[r] = (mine >> (16 * (r >> 3) + (r & 7))) & 1 ? s[r] : -INFINITY;
             }
             if (!none) {
-                auto fi = [](float x) { return __float_as_int(x); };
-                int mxi = imax3(fi(s[0]), fi(s[1]), fi(s[2]));
-#pragma unroll
-                for (int r = 3; r < 15; r += 2) mxi = imax3(mxi, fi(s[r]), fi(s[r + 1]));
-                mxi = max(mxi, fi(s[15]));
-                if (__builtin_expect(!all_seen || __builtin_amdgcn_ballot_w64(mxi > fi(LAZY_LOG2)) != 0, 0)) {
-                    float mx = s[0];
-#pragma unroll
-                    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-                    mx = fmaxf(mx, other_half(mx));
-                    const bool now = mx > -INFINITY, need = mx > LAZY_LOG2 || (!seen && now && mx < -LAZY_LOG2);
-                    seen |= now;
-                    all_seen = __builtin_amdgcn_ballot_w64(seen) == ~0ull;
-                    if (__builtin_amdgcn_ballot_w64(need) != 0) {
-                        const float shift = need ? mx : 0.f, alpha = ex2(-fmaxf(shift, 0.f));       // (down: nothing has been added yet)
-                        l_run *= alpha;
-#pragma unroll
-                        for (int db = 0; db < 4; ++db) acc[db] *= alpha;
-                        m_ref += shift;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) { s[r] -= shift; start[r] = -m_ref; }
-                    }
-                }
+                if (__builtin_expect(!all_seen || __builtin_amdgcn_ballot_w64(largest(s) > fi(LAZY_LOG2)) != 0, 0)) rebase(s);
                 uint32_t pk[8];
                 float ps = 0.f;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     const float a = ex2(s[2 * r]), b = ex2(s[2 * r + 1]);
-                    ps += a + b;
+                    ps += a;
+                    ps += b;
                     pk[r] = pack_bf16(a, b);
                 }
                 const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
@@ -263,9 +324,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
                     ps = 0.f;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) ps += bf_lo(pk[r]) + bf_hi(pk[r]);
-                    f32x16 z;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+                    f32x16 z = zeros;                    // 0 x value
                     const bf16x8 zero = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
 #pragma unroll
                     for (int f = 0; f < 8; ++f) z = MFMA32(fr[f], zero, z);
@@ -273,30 +332,31 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) odd += z[r];
                     if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0.f) != 0, 0)) {
-                        const int mine = (int)(sees >> (8 * hh));
-                        bf16x8 one[2];                   // the keys the row sees (0 x infinity is not a number: PC_WIN_ODD_NAN)
+                        met_odd = true;
+                        if constexpr (ODD) {
+                            const int mine = (int)(sees >> (8 * hh));
+                            bf16x8 one[2];               // the keys the row sees (0 x infinity is not a number: PC_WIN_ODD_NAN)
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            uint32_t w[4];
+                            for (int k = 0; k < 2; ++k) {
+                                uint32_t w[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const uint32_t x = pk[4 * k + j];
-                                w[j] = ((mine >> (16 * k + 2 * j)) & 1 ? ((x & 0xFFFFu) ? 0x3F80u : 0x4780u) : 0u) |
-                                       ((mine >> (16 * k + 2 * j + 1)) & 1 ? ((x >> 16) ? 0x3F800000u : 0x47800000u) : 0u);
+                                for (int j = 0; j < 4; ++j) {
+                                    const uint32_t x = pk[4 * k + j];
+                                    w[j] = ((mine >> (16 * k + 2 * j)) & 1 ? ((x & 0xFFFFu) ? 0x3F80u : 0x4780u) : 0u) |
+                                           ((mine >> (16 * k + 2 * j + 1)) & 1 ? ((x >> 16) ? 0x3F800000u : 0x47800000u) : 0u);
+                                }
+                                one[k] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
                             }
-                            one[k] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-                        }
 #pragma unroll
-                        for (int db = 0; db < 4; ++db) {
+                            for (int db = 0; db < 4; ++db) {
+                                z = MFMA32(odd_code(fr[db]), one[0], zeros);
+                                z = MFMA32(odd_code(fr[db + 4]), one[1], z);
+                                fr[db] = finite_or_zero(fr[db]);
+                                fr[db + 4] = finite_or_zero(fr[db + 4]);
 #pragma unroll
-                            for (int r = 0; r < 16; ++r) z[r] = 0.f;
-                            z = MFMA32(odd_code(fr[db]), one[0], z);
-                            z = MFMA32(odd_code(fr[db + 4]), one[1], z);
-                            fr[db] = finite_or_zero(fr[db]);
-                            fr[db + 4] = finite_or_zero(fr[db + 4]);
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[db][r] += win_odd_sum(z[r]);
-                            __builtin_amdgcn_sched_barrier(0);              // (one after the other: registers)
+                                for (int r = 0; r < 16; ++r) acc[db][r] += win_odd_sum(z[r]);
+                                __builtin_amdgcn_sched_barrier(0);          // (one after the other: registers)
+                            }
                         }
                     }
                 }
@@ -304,8 +364,21 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
 #pragma unroll
                 for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(fr[f], p[f >> 2], acc[f & 3]);
             }
+            ++t;
+            if (t < T) walk.next();
+        }
+    };
+    if (T > 0) {
+        if (threadIdx.x == 0) s_again = 0;
+        walk_tiles(std::false_type{});
+        if (__builtin_expect(met_odd, 0)) s_again = 1;   // (behind at least one barrier of the walk)
+        __syncthreads();
+        if (__builtin_expect(uniform(s_again), 0)) {
+            m_ref = l_run = 0.f;
+            seen = all_seen = shifted = false;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) d[i] = d[i + 1];
+            for (int db = 0; db < 4; ++db) acc[db] = zeros;
+            walk_tiles(std::true_type{});
         }
     }
     ring_barrier();
@@ -424,7 +497,7 @@ __device__ __forceinline__ void win_decode(const PcWin &W, const PcWinItem *item
     if (n_tiles > 0) {
         const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * W.slots * (PC_D * 2);
         const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * W.slots * (PC_D * 2);
-        WinWalk walk(runs + item.run0, skip);
+        WinWalk walk(runs + item.run0, skip, n_tiles);
         int asked = 0;
         auto fetch = [&](WinDecTile &T) __attribute__((always_inline)) {
             if (asked > 0 && asked < n_tiles) walk.next();

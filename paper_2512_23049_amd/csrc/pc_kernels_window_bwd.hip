@@ -77,34 +77,50 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
     const float lse = ok ? B.lse[R * W.n_q_heads + h] : -INFINITY;
     const bool live = lse > -INFINITY;                   // (a row that saw nothing, or whose scores were not numbers, has no gradient)
     float x[PER], y[PER], gx[PER], gy[PER], delta = 0.f;
+    // PER numbers at p: pairs' first halves, or (HALF further) their second
+    auto get = [&](const void *p, int64_t i, float (&v)[PER]) {
+        if constexpr (BF16) {
+            const uint4 w = ldg16((const uint16_t *)p + i);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const float2 cs = W.rot_q[R * HALF + PER * c + i];
-        float qx, qy, ox, oy, dx, dy;
-        auto get = [&](const void *p, int64_t i) { return BF16 ? __uint_as_float((uint32_t)((const uint16_t *)p)[i] << 16) : ((const float *)p)[i]; };
-        qx = get(W.q, at + i); qy = get(W.q, at + i + HALF);
-        ox = get(B.out, at + i); oy = get(B.out, at + i + HALF);
-        dx = get(B.d_out, at + i); dy = get(B.d_out, at + i + HALF);
-        x[i] = live ? qx * cs.x - qy * cs.y : 0.f; y[i] = live ? qx * cs.y + qy * cs.x : 0.f;
-        gx[i] = live ? dx : 0.f; gy[i] = live ? dy : 0.f;
-        delta += live ? dx * ox + dy * oy : 0.f;
+            for (int k = 0; k < PER / 2; ++k) { v[2 * k] = bf_lo(u[k]); v[2 * k + 1] = bf_hi(u[k]); }
+        } else {
+#pragma unroll
+            for (int k = 0; k < PER; k += 4) *reinterpret_cast<float4 *>(v + k) = *reinterpret_cast<const float4 *>((const float *)p + i + k);
+        }
+    };
+    auto put = [&](void *p, int64_t i, const float (&v)[PER]) {
+        if constexpr (BF16) *reinterpret_cast<uint4 *>((uint16_t *)p + i) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        else {
+#pragma unroll
+            for (int k = 0; k < PER; k += 4) *reinterpret_cast<float4 *>((float *)p + i + k) = *reinterpret_cast<const float4 *>(v + k);
+        }
+    };
+    {
+        float qx[PER], qy[PER], ox[PER], oy[PER];
+        get(W.q, at, qx); get(W.q, at + HALF, qy);
+        get(B.out, at, ox); get(B.out, at + HALF, oy);
+        get(B.d_out, at, gx); get(B.d_out, at + HALF, gy);
+        const float4 *rot = reinterpret_cast<const float4 *>(W.rot_q + R * HALF + PER * c);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const float4 cs2 = rot[i / 2];
+            const float co = i & 1 ? cs2.z : cs2.x, si = i & 1 ? cs2.w : cs2.y;
+            x[i] = live ? qx[i] * co - qy[i] * si : 0.f; y[i] = live ? qx[i] * si + qy[i] * co : 0.f;
+            delta += live ? gx[i] * ox[i] + gy[i] * oy[i] : 0.f;
+            gx[i] = live ? gx[i] : 0.f; gy[i] = live ? gy[i] : 0.f;
+        }
     }
     delta += __shfl_xor(delta, 1); delta += __shfl_xor(delta, 2); delta += __shfl_xor(delta, 4);
     const int64_t to = (unit * 32 + r) * D + PER * c;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if constexpr (BF16) {
-            ((uint16_t *)B.q_abs)[to + i] = to_bf16(x[i]); ((uint16_t *)B.q_abs)[to + i + HALF] = to_bf16(y[i]);
-            ((uint16_t *)B.d_o)[to + i] = to_bf16(gx[i]); ((uint16_t *)B.d_o)[to + i + HALF] = to_bf16(gy[i]);
-        } else {
-            ((float *)B.q_abs)[to + i] = x[i]; ((float *)B.q_abs)[to + i + HALF] = y[i];
-            ((float *)B.d_o)[to + i] = gx[i]; ((float *)B.d_o)[to + i + HALF] = gy[i];
-        }
-    }
+    put(B.q_abs, to, x); put(B.q_abs, to + HALF, y);
+    put(B.d_o, to, gx); put(B.d_o, to + HALF, gy);
     const int lo = win_low(W.q_pos[R], W.window);
     if (c == 0) {
         char *st = B.stat + unit * PC_WIN_STAT_BYTES;
-        reinterpret_cast<PcWinStat *>(st)[r] = PcWinStat{live ? lse * 1.4426950408889634f : INFINITY, delta, lo, blk.lim0 + (int)(ok ? row : 0)};
+        PcWinStat *const to_stat = reinterpret_cast<PcWinStat *>(st);
+        to_stat->lse2[r] = live ? lse * 1.4426950408889634f : INFINITY; to_stat->delta[r] = delta;
+        to_stat->lo[r] = lo; to_stat->lim[r] = blk.lim0 + (int)(ok ? row : 0);
         if (ok) B.delta[R * W.n_q_heads + h] = delta;
         s_lo[r] = ok ? lo : INT32_MAX;
         s_dead[r] = !live;
@@ -118,8 +134,14 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
         }
         const int64_t first = BF16 ? 32 * (int64_t)blk.block : 32 * (int64_t)blk.block / g;
         const int64_t last = min((int64_t)blk.n_q - 1, BF16 ? first + 31 : (32 * (int64_t)blk.block + 31) / g);
-        *reinterpret_cast<PcWinStatHead *>(B.stat + unit * PC_WIN_STAT_BYTES + 32 * sizeof(PcWinStat)) =
-            PcWinStatHead{lo_min, lo_max, blk.lim0 + (int)first, blk.lim0 + (int)last};
+        PcWinStat *const to_stat = reinterpret_cast<PcWinStat *>(B.stat + unit * PC_WIN_STAT_BYTES);
+        to_stat->head = make_int4(lo_min, lo_max, blk.lim0 + (int)first, blk.lim0 + (int)last);
+        uint32_t live_rows = 0, in_step = 1;
+        for (int i = 0; i < 32; ++i) {
+            live_rows |= s_dead[i] ? 0u : 1u << i;
+            if (!s_dead[i] && s_lo[i] != s_lo[0] + i) in_step = 0;          // (not where rows are columns, nor at stated positions)
+        }
+        to_stat->rows = make_int4((int)live_rows, BF16 ? (int)in_step : 0, s_lo[0], 0);
     }
 }
 
@@ -151,16 +173,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
     const int row = min(32 * ub + n, item.n_q - 1);
     const bool row_ok = unit_ok && 32 * ub + n < item.n_q;
     const int64_t R = (int64_t)item.q_off + row;
-    const float lse = B.lse[R * W.n_q_heads + h];
-    const bool live = row_ok && lse > -INFINITY;
-    const float lse2 = live ? lse * 1.4426950408889634f : INFINITY, delta = live ? B.delta[R * W.n_q_heads + h] : 0.f;
-    const int lo = win_low(W.q_pos[R], W.window), lim = item.lim0 + row;
-    int lo_max = live ? lo : INT32_MAX;                  // (a row without a gradient: every tile is masked)
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o));
-    lo_max = uniform(lo_max);
-    const bool some_dead = __builtin_amdgcn_ballot_w64(!live) != 0;
-    const int lim_first = item.lim0 + 32 * ub;
+    const int lim = item.lim0 + row, lim_first = item.lim0 + 32 * ub;
 
     const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * W.slots * (PC_D * 2);
     const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * W.slots * (PC_D * 2);
@@ -171,13 +184,35 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
         const int64_t at = (int64_t)d.slot0 * (PC_D * 2);
         const unsigned to = lds0 + slot * (2 * TILE_BYTES);
         dma16(kb + at, k_src, to);
-        dma16(kb + at, k_src + 4096, to + 4096);         // (rows 16 up: the same order of chunks)
+        dma16(kb + at + 4096, k_src, to + 4096);         // (rows 16 up: the same order of chunks)
         dma16(vb + at, v_src, to + TILE_BYTES);
-        dma16(vb + at, v_src + 4096, to + TILE_BYTES + 4096);
+        dma16(vb + at + 4096, v_src, to + TILE_BYTES + 4096);
     };
     const RowMajor rk(perm_row(n), lane);
     const ValuesByKey<true> rv(lane);
 
+    const int T = item.n_tiles;
+    WinWalk walk(W.runs + item.run0, item.skip, T);         // (not looked at where there is no tile)
+    WinTile d[AHEAD + 1];
+    int asked = 0;
+    auto ask = [&](WinTile &to, int slot) __attribute__((always_inline)) {
+        if (asked >= T) return;
+        if (asked > 0) walk.next();
+        ++asked;
+        to = walk.tile();
+        request(to, slot);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ask(d[i], i);
+    const float lse = B.lse[R * W.n_q_heads + h], delta_r = B.delta[R * W.n_q_heads + h];
+    const int lo = win_low(W.q_pos[R], W.window);
+    const bool live = row_ok && lse > -INFINITY;
+    const float lse2 = live ? lse * 1.4426950408889634f : INFINITY, delta = live ? delta_r : 0.f;
+    int lo_max = live ? lo : INT32_MAX;                  // (a row without a gradient: every tile is masked)
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o));
+    lo_max = uniform(lo_max);
+    const bool some_dead = __builtin_amdgcn_ballot_w64(!live) != 0;
     bf16x8 go[8];                                        // the lane's row of output gradients, dims 16 ks + 8 hh + 0..7
     {
         const unsigned char *p = (const unsigned char *)B.d_out + (R * W.n_q_heads + h) * (PC_D * 2) + 16 * hh;
@@ -207,7 +242,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
             }
             qop[ks] = frag4(a[0], a[1], a[2], a[3]);
             qop[ks + 4] = frag4(b[0], b[1], b[2], b[3]);
-            __builtin_amdgcn_sched_barrier(0);
+            if (ks & 1) __builtin_amdgcn_sched_barrier(0);         // (what is read for all of it at once would not fit the registers)
         }
     };
     f32x16 acc[4];
@@ -216,21 +251,8 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
 
-    const int T = item.n_tiles;
     int cur = -1;
     if (T > 0) {
-        WinWalk walk(W.runs + item.run0, item.skip);
-        WinTile d[AHEAD + 1];
-        int asked = 0;
-        auto ask = [&](WinTile &to, int slot) __attribute__((always_inline)) {
-            if (asked >= T) return;
-            if (asked > 0) walk.next();
-            ++asked;
-            to = walk.tile();
-            request(to, slot);
-        };
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) ask(d[i], i);
 #pragma unroll 1
         for (int t = 0, u = 0; t < T; ++t, u = (u + 1) & (RING - 1)) {
             const unsigned kt = ring + u * (2 * TILE_BYTES), vt = kt + TILE_BYTES;
@@ -238,7 +260,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
             else wait_vm<0>();
             ring_barrier();
             const WinTile e = d[0];
-            if (e.rot != cur) {
+            if (__builtin_expect(e.rot != cur, 0)) {
                 if (cur >= 0) turn_columns(acc, W.rot_run + (int64_t)cur * (PC_D / 2), W.rot_run + (int64_t)e.rot * (PC_D / 2), hh, 1.f);
                 cur = e.rot;
                 turn(cur);
@@ -350,6 +372,7 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
 {
     constexpr int RING = 4, AHEAD = 3, SLOT = 2 * TILE_BYTES + PC_WIN_STAT_BYTES;
     __shared__ __attribute__((aligned(1024))) unsigned char s_ring[RING][SLOT];
+    __shared__ __attribute__((aligned(1024))) unsigned char s_v[PC_WIN_KEY_TILES][TILE_BYTES];        // the call's values, in the store's order
 
     const int kh = blockIdx.x % W.n_kv_heads;
     const PcWinKeyItem item = B.key_items[blockIdx.x / W.n_kv_heads];
@@ -361,6 +384,7 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
     const unsigned ring = (unsigned)(uintptr_t)&s_ring[0][0];
     const unsigned src = (threadIdx.x >> 4) * 256 + (((threadIdx.x & 15) ^ swz(threadIdx.x >> 4)) << 4);
     const RowMajor by_row(perm_row(n), lane), by_col(n, lane);
+    const ValuesByKey<false> values(lane);               // by key, the lane's one
     const int my_keys = item.n_keys - PC_TILE * tile;    // of the wave's tile
 
     f32x16 acc[4];
@@ -382,7 +406,13 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
             dma16((const unsigned char *)B.d_o + u * TILE_BYTES, src, to + TILE_BYTES);
             if (wave == 0) dma16(B.stat + u * PC_WIN_STAT_BYTES, lane * 16, to + 2 * TILE_BYTES);
         };
-        ring_barrier();                                  // (the last call's units are no longer read)
+        ring_barrier();                                  // (the last call's units and values are no longer read)
+        if (!is_k && active) {
+            const unsigned char *v = (const unsigned char *)W.v_store + ((int64_t)kh * W.slots + item.slot0 + PC_TILE * tile) * (PC_D * 2);
+            const unsigned to = (unsigned)(uintptr_t)&s_v[tile][0];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dma16(v, (unsigned)v_src_chunk(64 * i + lane) * 16, to + 1024 * i);
+        }
         for (int i = 0; i < min(AHEAD, U); ++i) request(i, i);
         bf16x8 kop[8], vop[8];                           // the lane's key, turned and scaled, and its value: dims 16 ks + 8 hh + 0..7
 #pragma unroll
@@ -409,14 +439,6 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (is_k) {
-                const uint16_t *vp = (const uint16_t *)W.v_store + (slot / PC_VGROUP * PC_D + 8 * hh) * PC_VGROUP + slot % PC_VGROUP;
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = (uint32_t)vp[(16 * ks + 2 * j) * PC_VGROUP] | ((uint32_t)vp[(16 * ks + 2 * j + 1) * PC_VGROUP] << 16);
-                    vop[ks] = frag4(w[0], w[1], w[2], w[3]);
-                }
                 // dk, kept in the frame of the queries: from the last call's to this one's
                 if (cur >= 0 && cur != app.rot) turn_columns(acc, W.rot_run + (int64_t)app.rot * (PC_D / 2), W.rot_run + (int64_t)cur * (PC_D / 2), hh, 1.f);
                 cur = app.rot;
@@ -430,8 +452,12 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
             else wait_vm<2 * (AHEAD - 1)>();
             ring_barrier();
             if (i + AHEAD < U) request(i + AHEAD, (u + AHEAD) & (RING - 1));
-            const unsigned char *stat = &s_ring[u][2 * TILE_BYTES];
-            const int4 hd = *reinterpret_cast<const int4 *>(stat + 32 * sizeof(PcWinStat));
+            if (i == 0 && is_k) {                        // (the values were asked for in front of the first unit)
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) vop[ks] = values.get((unsigned)(uintptr_t)&s_v[tile][0], ks);
+            }
+            const PcWinStat *stat = reinterpret_cast<const PcWinStat *>(&s_ring[u][2 * TILE_BYTES]);
+            const int4 hd = stat->head;
             const int lo_min = uniform(hd.x), lo_max = uniform(hd.y), lim_first = uniform(hd.z), lim_last = uniform(hd.w);
             // nothing of the tile is seen by the unit
             if (!active || (app.self && lim_last < pos0) || (sink == 0 && lo_min > pos0 && (unsigned)lo_min - (unsigned)pos0 > PC_TILE - 1u)) continue;
@@ -442,24 +468,26 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) s = MFMA32(by_row.by_row(qt, ks), kop[ks], s);
             // register r: row 16 (r / 8) + 8 hh + r % 8, column: the lane's key
-            const float4 *rows = reinterpret_cast<const float4 *>(stat) + 8 * hh;
-            float dl[16];
-            uint32_t seen = 0xFFFFu;                     // bit r
+            auto row_of = [&](int r) { return 16 * (r >> 3) + 8 * hh + (r & 7); };
+            uint32_t seen = ~0u;                         // bit: row
             if (__builtin_expect(edge, 0)) {
-                seen = 0;
+                const int4 rw = stat->rows;
                 const int pos = pos0 + min(n, valid - 1);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float4 x = rows[16 * (r >> 3) + (r & 7)];
-                    const bool see = (n < valid) & (x.x < INFINITY) & ((pos >= __float_as_int(x.z)) | (n < sink)) & (!app.self | (pos <= __float_as_int(x.w)));
-                    seen |= see ? 1u << r : 0u;
+                if (uniform(rw.y)) {                     // rows at consecutive positions: from the first that may see its own token to the last whose window holds the key
+                    auto first = [](unsigned n) { return n >= 32u ? ~0u : (1u << n) - 1u; };
+                    const unsigned below = pos < rw.z ? 0u : (unsigned)pos - (unsigned)rw.z + 1u;
+                    const unsigned above = app.self && pos > lim_first ? (unsigned)pos - (unsigned)lim_first : 0u;
+                    seen = (n < sink ? ~0u : below == 0u && pos >= rw.z ? ~0u : first(below)) & ~first(above);
+                } else {
+                    seen = 0;
+                    for (int i = 0; i < 32; ++i) seen |= ((pos >= stat->lo[i]) | (n < sink)) & (!app.self | (pos <= stat->lim[i])) ? 1u << i : 0u;
                 }
+                seen &= n < valid ? (uint32_t)rw.x : 0u;
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float2 x = *reinterpret_cast<const float2 *>(rows + 16 * (r >> 3) + (r & 7));
-                s[r] = ex2(s[r] - x.x);
-                dl[r] = x.y;
+            for (int r = 0; r < 16; r += 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(&stat->lse2[row_of(r)]);
+                s[r] = ex2(s[r] - x.x); s[r + 1] = ex2(s[r + 1] - x.y); s[r + 2] = ex2(s[r + 2] - x.z); s[r + 3] = ex2(s[r + 3] - x.w);
             }
             if (is_k) {
                 f32x16 dp;
@@ -468,11 +496,14 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks) dp = MFMA32(by_row.by_row(gt, ks), vop[ks], dp);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] *= dp[r] - dl[r];
+                for (int r = 0; r < 16; r += 4) {
+                    const float4 x = *reinterpret_cast<const float4 *>(&stat->delta[row_of(r)]);
+                    s[r] *= dp[r] - x.x; s[r + 1] *= dp[r + 1] - x.y; s[r + 2] *= dp[r + 2] - x.z; s[r + 3] *= dp[r + 3] - x.w;
+                }
             }
             if (__builtin_expect(edge, 0)) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = (seen >> r) & 1 ? s[r] : 0.f;
+                for (int r = 0; r < 16; ++r) s[r] = (seen >> row_of(r)) & 1 ? s[r] : 0.f;
             }
             uint32_t pk[8];
 #pragma unroll
@@ -527,28 +558,33 @@ void pc_launch_win_bwd_keys_bf16(const PcWin &W, const PcWinBwd &B, hipStream_t 
     if (B.n_key_items > 0) pc_win_bwd_keys_bf16_kernel<<<(unsigned)B.n_key_items * W.n_kv_heads, 512, 0, st>>>(W, B);
 }
 
-// The parts of tiles that several items collect, added up in their order and to what is there.
+// The parts of tiles that several items collect, added up in their order and to what is there: a thread four numbers, eight parts a
+// round of loads.
 template <int D>
 __global__ __launch_bounds__(256) void pc_win_bwd_sums_kernel(PcWinBwd B, int H)
 {
     const PcWinSum sm = B.sums[blockIdx.x];
-    const int kh = blockIdx.y, which = blockIdx.z;       // keys, values
+    const int kh = blockIdx.y, which = blockIdx.z % 2;   // keys, values
     constexpr int KEYS = PC_WIN_KEY_TILES * PC_TILE;
-    for (int i = threadIdx.x; i < sm.n_keys * (D / 4); i += 256) {
-        const int key = i / (D / 4), d4 = i % (D / 4);
-        float4 *p = reinterpret_cast<float4 *>((which ? B.d_v : B.d_k) + (((int64_t)sm.slot0 + key) * H + kh) * D) + d4, v = *p;
-        for (int s = 0; s < sm.n_parts; ++s) {
-            const float4 x = reinterpret_cast<const float4 *>(B.key_part + ((((int64_t)(sm.part0 + s) * H + kh) * 2 + which) * KEYS + key) * D)[d4];
-            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-        }
-        *p = v;
+    const int i = (int)(blockIdx.z / 2) * 256 + threadIdx.x, key = i / (D / 4), d4 = i % (D / 4);
+    if (key >= sm.n_keys) return;
+    float4 *p = reinterpret_cast<float4 *>((which ? B.d_v : B.d_k) + (((int64_t)sm.slot0 + key) * H + kh) * D) + d4, v = *p;
+    const float4 *part = reinterpret_cast<const float4 *>(B.key_part + ((((int64_t)sm.part0 * H + kh) * 2 + which) * KEYS + key) * D) + d4;
+    const int64_t step = (int64_t)H * 2 * KEYS * D / 4;
+    for (int s0 = 0; s0 < sm.n_parts; s0 += 8) {
+        float4 x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = s0 + u < sm.n_parts ? part[(s0 + u) * step] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { v.x += x[u].x; v.y += x[u].y; v.z += x[u].z; v.w += x[u].w; }
     }
+    *p = v;
 }
 
 void pc_launch_win_bwd_sums(const PcWin &W, const PcWinBwd &B, int D, hipStream_t st)
 {
     if (B.n_sums <= 0) return;
-    const dim3 grid((unsigned)B.n_sums, (unsigned)W.n_kv_heads, 2);
+    const dim3 grid((unsigned)B.n_sums, (unsigned)W.n_kv_heads, (unsigned)(2 * PC_WIN_KEY_TILES * PC_TILE * D / 4 / 256));
     if (D == 64) pc_win_bwd_sums_kernel<64><<<grid, 256, 0, st>>>(B, W.n_kv_heads);
     else pc_win_bwd_sums_kernel<128><<<grid, 256, 0, st>>>(B, W.n_kv_heads);
 }

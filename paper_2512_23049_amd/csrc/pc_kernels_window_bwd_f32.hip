@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256, 1) void pc_win_bwd_dq_f32_kernel(PcWin W, PcWi
     if (n_tiles > 0) {
         unsigned char *const mine = s_mem + wave * 2 * RowTile<D>::BYTES;
         const RowTile<D> keys(mine, lane), values(mine + RowTile<D>::BYTES, lane);
-        WinWalk walk(W.runs + item.run0, skip);
+        WinWalk walk(W.runs + item.run0, skip, n_tiles);
         WinTile d = walk.tile();
         keys.request(kb + (int64_t)d.slot0 * D);
 #pragma unroll 1
@@ -252,9 +252,9 @@ __global__ __launch_bounds__(256, 1) void pc_win_bwd_keys_f32_kernel(PcWin W, Pc
             __syncthreads();
             if (i + 1 < app.n_blocks) request(i + 1, (i + 1) & 1);
             const unsigned qt = (unsigned)(uintptr_t)&s_ring[i & 1][0], gt = qt + RowTile<D>::BYTES;
-            const unsigned char *stat = &s_ring[i & 1][2 * RowTile<D>::BYTES];
-            const int4 hd = *reinterpret_cast<const int4 *>(stat + 32 * sizeof(PcWinStat));
-            const int lo_min = uniform(hd.x), lim_last = uniform(hd.w);
+            const PcWinStat *stat = reinterpret_cast<const PcWinStat *>(&s_ring[i & 1][2 * RowTile<D>::BYTES]);
+            const int4 hd = stat->head;
+            const int lo_min = uniform(hd.x), lo_max = uniform(hd.y), lim_first = uniform(hd.z), lim_last = uniform(hd.w);
             if (!active || (app.self && lim_last < pos0) || (sink == 0 && lo_min > pos0 && (unsigned)lo_min - (unsigned)pos0 > PC_TILE - 1u)) continue;
             f32x16 s = zeros(), dp = zeros();
 #pragma unroll
@@ -275,13 +275,26 @@ __global__ __launch_bounds__(256, 1) void pc_win_bwd_keys_f32_kernel(PcWin W, Pc
                 for (int e = 0; e < 4; ++e) dp = MFMA_F32(x[e], v[j + e], dp);
             }
             // register r: column 8 (r / 4) + 4 hh + r % 4 of the unit; the lane's key
-            const int pos = pos0 + min(n, valid - 1);
+            auto col_of = [&](int r) { return 8 * (r >> 2) + 4 * hh + (r & 3); };
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float4 x = *reinterpret_cast<const float4 *>(stat + (8 * (r >> 2) + 4 * hh + (r & 3)) * sizeof(PcWinStat));
-                const bool see = (n < valid) & (x.x < INFINITY) & ((pos >= __float_as_int(x.z)) | (n < sink)) & (!app.self | (pos <= __float_as_int(x.w)));
-                s[r] = see ? ex2(__builtin_fmaf(s[r], W.scale_log2, -x.x)) : 0.f;
-                dp[r] = see ? s[r] * (dp[r] - x.y) : 0.f;
+            for (int r = 0; r < 16; r += 4) {
+                const float4 l = *reinterpret_cast<const float4 *>(&stat->lse2[col_of(r)]), d = *reinterpret_cast<const float4 *>(&stat->delta[col_of(r)]);
+                const float lse2[4] = {l.x, l.y, l.z, l.w}, delta[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[r + e] = ex2(__builtin_fmaf(s[r + e], W.scale_log2, -lse2[e]));
+                    dp[r + e] = s[r + e] * (dp[r + e] - delta[e]);
+                }
+            }
+            if (valid < PC_TILE || (app.self && lim_first - pos0 < PC_TILE - 1) || lo_max == INT32_MAX || (lo_max > pos0 && sink < PC_TILE)) {
+                const int pos = pos0 + min(n, valid - 1);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int c = col_of(r);
+                    const bool see = (n < valid) & (stat->lse2[c] < INFINITY) & ((pos >= stat->lo[c]) | (n < sink)) & (!app.self | (pos <= stat->lim[c]));
+                    s[r] = see ? s[r] : 0.f;
+                    dp[r] = see ? dp[r] : 0.f;
+                }
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_attend_f32_kernel(PcWin W)
         unsigned char *const mine = s_mem + wave * RowTile<D>::BYTES;
         const RowTile<D> keys(mine, lane);
         const unsigned row_at = keys.lds + n * (D * 4);
-        WinWalk walk(W.runs + item.run0, skip);
+        WinWalk walk(W.runs + item.run0, skip, n_tiles);
         WinTile d = walk.tile();
         keys.request(kb + (int64_t)d.slot0 * D);
         int cur = -1;

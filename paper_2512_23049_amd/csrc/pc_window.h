@@ -73,9 +73,14 @@ struct PcWinKeyItem {         // up to four tiles of an extent, and calls (or so
     int32_t pad[3];
 };
 struct PcWinSum { int32_t slot0, n_keys, part0, n_parts; };       // tiles whose items' sums are added up
-struct PcWinStat { float lse2, delta; int32_t lo, lim; };         // of a row: lse log2 e (+inf: no gradient), Delta, the positions it sees
-struct PcWinStatHead { int32_t lo_min, lo_max, lim_first, lim_last; };       // of a block's rows; lo_max: INT32_MAX if some row has no gradient
+struct PcWinStat {            // of a unit's rows
+    float lse2[32], delta[32];        // lse log2 e (+inf: no gradient), Delta
+    int32_t lo[32], lim[32];          // the positions a row sees: from, up to (own)
+    int4 head;                // least lo; largest lo (INT32_MAX if some row has no gradient); first and last lim
+    int4 rows;                // bits of the rows with a gradient; 1: their lo rise by one from row to row; lo of row 0
+};
 #define PC_WIN_STAT_BYTES 1024
+static_assert(sizeof(PcWinStat) <= PC_WIN_STAT_BYTES, "");
 struct PcWinBwd {
     const PcWinBlock   *blocks;
     const PcWinApp     *apps;
@@ -87,7 +92,7 @@ struct PcWinBwd {
     float       *delta;       // [rows][H_q]
     void        *q_abs;       // [unit][32][D] queries turned by their positions, in the cache's type; unit: (block, head), fp32: (block, KV head)
     void        *d_o;         // [unit][32][D] the output gradients, zeros for rows without
-    char        *stat;        // [unit][PC_WIN_STAT_BYTES]: PcWinStat of 32 rows, PcWinStatHead
+    char        *stat;        // [unit][PC_WIN_STAT_BYTES]: PcWinStat
     float       *key_part;    // [part][KV head][keys, values][128][D]
     float       *d_q, *d_k, *d_v;
     float        scale;
@@ -153,8 +158,10 @@ struct WinWalk {
     {
         a.x += PC_TILE * tiles; a.y += PC_TILE * tiles; a.z -= PC_TILE * tiles; a.w -= PC_TILE * tiles;
     }
-    __device__ __forceinline__ WinWalk(const void *runs, int skip) : run(reinterpret_cast<uintptr_t>(runs))
+    // tiles: of the walk; where there is none there may be no run either, and nothing is read
+    __device__ __forceinline__ WinWalk(const void *runs, int skip, int tiles) : run(reinterpret_cast<uintptr_t>(runs)), a((win_i32x4){0, 0, 0, 0}), rot(0), self(0), rot_pos(0)
     {
+        if (tiles <= 0) return;
         load();
         for (;;) {                                       // (a wave's or a split's share may begin some runs further on)
             const int n = (a.z + PC_TILE - 1) / PC_TILE;

@@ -105,19 +105,26 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
     int64_t all = 0;
     for (const Group &gr : groups) all += gr.tiles;
     // a split's tiles: what brings the launch to its target (groups that are many already stay whole)
-    const int64_t chunk = may_split ? std::max<int64_t>(least, (all * H_kv + target - 1) / target) : INT32_MAX;
+    const int64_t chunk = may_split ? std::max<int64_t>(least, (all * H_kv + target - 1) / target) : INT32_MAX;      // (INT32_MAX: one)
     for (size_t a = 0; a < groups.size();) {
         size_t b = a;
         int32_t most = 0;
         while (b < groups.size() && groups[b].call == groups[a].call) most = std::max(most, groups[b++].tiles);
         const WinCall &wc = P.calls[(size_t)groups[a].call];
-        const int32_t n = (int32_t)std::max<int64_t>(1, std::min<int64_t>((most + chunk - 1) / chunk, MAX_SPLITS));
+        // (to the nearest: a group a little longer than the others is not worth a merge of its own)
+        const int32_t n = (int32_t)std::max<int64_t>(1, std::min<int64_t>((most + chunk / 2) / chunk, MAX_SPLITS));
         const int64_t part0 = P.part_rows;
         for (int32_t s = 0; s < n; ++s)
             for (size_t i = a; i < b; ++i) {
                 const Group &gr = groups[i];
                 const int32_t t0 = (int32_t)((int64_t)gr.tiles * s / n), t1 = (int32_t)((int64_t)gr.tiles * (s + 1) / n);
-                items.push_back(PcWinItem{wc.q_off, wc.n_q, gr.unit0, wc.lim0, gr.run0, t0, t1 - t0, n == 1 ? -1 : (int32_t)(part0 + (int64_t)s * wc.n_q)});
+                int32_t run = gr.run0, skip = t0;
+                while (t0 < t1) {                        // (found here: a workgroup would look the runs up one after the other)
+                    const int32_t has = (P.runs[(size_t)run].n_tok + PC_TILE - 1) / PC_TILE;
+                    if (skip < has) break;
+                    skip -= has; ++run;
+                }
+                items.push_back(PcWinItem{wc.q_off, wc.n_q, gr.unit0, wc.lim0, run, skip, t1 - t0, n == 1 ? -1 : (int32_t)(part0 + (int64_t)s * wc.n_q)});
             }
         if (n > 1) {
             for (int32_t r = wc.row0; r < wc.row1; ++r) P.merge.push_back(PcMergeRow{wc.q_off + r, (int32_t)(part0 + r), n, wc.n_q});
@@ -300,9 +307,9 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
         }
         a = b;
     }
-    // An item's share: what brings the launch to two workgroups a compute unit; tiles with more (those that every row sees,
-    // messages that many calls list) are cut and their parts added up.
-    const int64_t share = std::max<int64_t>(4, (total * H_kv + 511) / 512);
+    // An item's share: what brings the launch to one workgroup a compute unit; tiles with more (those that every row sees,
+    // messages that many calls list) are cut and their parts added up.  The longest items come first.
+    const int64_t share = std::max<int64_t>(4, (total * H_kv + 255) / 256);
     for (const Tiles &t : all) {
         const int64_t n = t.blocks * 4 > share * 5 ? std::min<int64_t>((t.blocks + share - 1) / share, 1024) : 1;
         const int32_t part0 = B.parts;
@@ -323,11 +330,21 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
             it.n_apps = (int32_t)B.apps.size() - it.app0;
             B.keys.push_back(it);
         }
-        if (n > 1) {
+        if (n > 1) {                                     // (parts stand where their numbers say, whatever their order in the launch)
             B.sums.push_back(PcWinSum{t.slot0, t.n_keys, part0, (int32_t)n});
             B.parts += (int32_t)n;
         }
     }
+    std::vector<int64_t> size(B.keys.size());
+    std::vector<uint32_t> by(B.keys.size());
+    for (size_t i = 0; i < B.keys.size(); ++i) {
+        by[i] = (uint32_t)i;
+        for (int32_t k = 0; k < B.keys[i].n_apps; ++k) size[i] += B.apps[(size_t)(B.keys[i].app0 + k)].n_blocks + 2;
+    }
+    std::stable_sort(by.begin(), by.end(), [&](uint32_t a, uint32_t b) { return size[a] > size[b]; });
+    std::vector<PcWinKeyItem> sorted(B.keys.size());
+    for (size_t i = 0; i < by.size(); ++i) sorted[i] = B.keys[by[i]];
+    B.keys.swap(sorted);
 }
 
 int32_t check(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink)
