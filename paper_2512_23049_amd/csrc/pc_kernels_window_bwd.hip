@@ -8,12 +8,13 @@
 //
 //   prep   per 32 rows and head: Delta, the queries turned by their positions, output gradients and statistics, laid out for keys
 //   dq     rows: the forward's walk, with 24 matrix instructions a tile and unit (scores 8, dp 8, dq 8)
-//   keys   four tiles of keys: a walk over the units that see them (40: scores twice)
+//   keys   four tiles of keys: a walk over the units that see them (32: scores and dv, dp and dk)
 //
 // Rotations.  dq is collected in the frame of the present run's keys and turned when the rotation changes; dk in the frame of the
 // turned queries, in which a call's keys are turned once.
 #include "pc_window.h"
 #include "pc_bwd_tiles.h"
+#include <type_traits>
 
 namespace {
 
@@ -60,7 +61,7 @@ template <int D, bool BF16>
 __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd B)
 {
     constexpr int HALF = D / 2, PER = HALF / 8;          // pairs a thread takes
-    __shared__ int s_lo[32], s_dead[32];
+    __shared__ int s_lo[32], s_state[32];                // of a row: 0 there is none, 1 it has a gradient, 2 it has none
     const PcWinBlock blk = B.blocks[blockIdx.x];
     const int g = W.n_q_heads / W.n_kv_heads;
     const int r = threadIdx.x >> 3, c = threadIdx.x & 7;
@@ -69,13 +70,18 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
     bool ok;
     if constexpr (BF16) {
         row = 32 * (int64_t)blk.block + r; h = blockIdx.y; ok = row < blk.n_q;
+        row = min(row, (int64_t)blk.n_q - 1);
     } else {
-        const int64_t col = 32 * (int64_t)blk.block + r;
-        row = col / g; h = (int64_t)blockIdx.y * g + col % g; ok = row < blk.n_q;
+        int64_t col = 32 * (int64_t)blk.block + r;
+        ok = col < (int64_t)blk.n_q * g;
+        col = min(col, (int64_t)blk.n_q * g - 1);
+        row = col / g; h = (int64_t)blockIdx.y * g + col % g;
     }
-    const int64_t R = (int64_t)blk.q_off + (ok ? row : 0), at = (R * W.n_q_heads + (ok ? h : 0)) * D + PER * c;
-    const float lse = ok ? B.lse[R * W.n_q_heads + h] : -INFINITY;
-    const bool live = lse > -INFINITY;                   // (a row that saw nothing, or whose scores were not numbers, has no gradient)
+    // Behind the last row: its queries again, without a gradient.  What the keys it sees make of it is what they make of the last
+    // row, and 0 times that, also where a key is not finite; no tile is masked for its sake.
+    const int64_t R = (int64_t)blk.q_off + row, at = (R * W.n_q_heads + h) * D + PER * c;
+    const float lse = B.lse[R * W.n_q_heads + h];
+    const bool some = lse > -INFINITY, live = ok && some;          // (a row that saw nothing, or whose scores were not numbers, has no gradient)
     float x[PER], y[PER], gx[PER], gy[PER], delta = 0.f;
     // PER numbers at p: pairs' first halves, or (HALF further) their second
     auto get = [&](const void *p, int64_t i, float (&v)[PER]) {
@@ -106,7 +112,7 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
         for (int i = 0; i < PER; ++i) {
             const float4 cs2 = rot[i / 2];
             const float co = i & 1 ? cs2.z : cs2.x, si = i & 1 ? cs2.w : cs2.y;
-            x[i] = live ? qx[i] * co - qy[i] * si : 0.f; y[i] = live ? qx[i] * si + qy[i] * co : 0.f;
+            x[i] = some ? qx[i] * co - qy[i] * si : 0.f; y[i] = some ? qx[i] * si + qy[i] * co : 0.f;
             delta += live ? gx[i] * ox[i] + gy[i] * oy[i] : 0.f;
             gx[i] = live ? gx[i] : 0.f; gy[i] = live ? gy[i] : 0.f;
         }
@@ -116,32 +122,28 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
     put(B.q_abs, to, x); put(B.q_abs, to + HALF, y);
     put(B.d_o, to, gx); put(B.d_o, to + HALF, gy);
     const int lo = win_low(W.q_pos[R], W.window);
+    char *const st = B.stat + unit * PC_WIN_STAT_BYTES;
+    PcWinStat *const to_stat = reinterpret_cast<PcWinStat *>(st);
     if (c == 0) {
-        char *st = B.stat + unit * PC_WIN_STAT_BYTES;
-        PcWinStat *const to_stat = reinterpret_cast<PcWinStat *>(st);
-        to_stat->lse2[r] = live ? lse * 1.4426950408889634f : INFINITY; to_stat->delta[r] = delta;
-        to_stat->lo[r] = lo; to_stat->lim[r] = blk.lim0 + (int)(ok ? row : 0);
+        to_stat->lse2[r] = live ? lse * 1.4426950408889634f : INFINITY; to_stat->delta[r] = live ? delta : 0.f;
+        to_stat->lo[r] = lo; to_stat->lim[r] = blk.lim0 + (int)row;
         if (ok) B.delta[R * W.n_q_heads + h] = delta;
-        s_lo[r] = ok ? lo : INT32_MAX;
-        s_dead[r] = !live;
+        s_lo[r] = lo;
+        s_state[r] = live ? 1 : ok ? 2 : 0;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int lo_min = INT32_MAX, lo_max = INT32_MIN;
-        for (int i = 0; i < 32; ++i) {
-            lo_min = min(lo_min, s_lo[i]);
-            lo_max = s_dead[i] ? INT32_MAX : max(lo_max, s_lo[i]);
+    if (threadIdx.x < 64) {                              // (lanes 32 up: the rows again)
+        const int at = threadIdx.x & 31, state = s_state[at];
+        int lo_min = s_state[at] ? s_lo[at] : INT32_MAX, lo_max = state == 2 ? INT32_MAX : state ? s_lo[at] : INT32_MIN;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { lo_min = min(lo_min, __shfl_xor(lo_min, o)); lo_max = max(lo_max, __shfl_xor(lo_max, o)); }
+        const uint32_t live_rows = (uint32_t)__builtin_amdgcn_ballot_w64(state == 1);
+        if (threadIdx.x == 0) {
+            const int64_t first = BF16 ? 32 * (int64_t)blk.block : 32 * (int64_t)blk.block / g;
+            const int64_t last = min((int64_t)blk.n_q - 1, BF16 ? first + 31 : (32 * (int64_t)blk.block + 31) / g);
+            to_stat->head = make_int4(lo_min, lo_max, blk.lim0 + (int)first, blk.lim0 + (int)last);
+            to_stat->live = (int)live_rows;
         }
-        const int64_t first = BF16 ? 32 * (int64_t)blk.block : 32 * (int64_t)blk.block / g;
-        const int64_t last = min((int64_t)blk.n_q - 1, BF16 ? first + 31 : (32 * (int64_t)blk.block + 31) / g);
-        PcWinStat *const to_stat = reinterpret_cast<PcWinStat *>(B.stat + unit * PC_WIN_STAT_BYTES);
-        to_stat->head = make_int4(lo_min, lo_max, blk.lim0 + (int)first, blk.lim0 + (int)last);
-        uint32_t live_rows = 0, in_step = 1;
-        for (int i = 0; i < 32; ++i) {
-            live_rows |= s_dead[i] ? 0u : 1u << i;
-            if (!s_dead[i] && s_lo[i] != s_lo[0] + i) in_step = 0;          // (not where rows are columns, nor at stated positions)
-        }
-        to_stat->rows = make_int4((int)live_rows, BF16 ? (int)in_step : 0, s_lo[0], 0);
     }
 }
 
@@ -208,11 +210,10 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
     const int lo = win_low(W.q_pos[R], W.window);
     const bool live = row_ok && lse > -INFINITY;
     const float lse2 = live ? lse * 1.4426950408889634f : INFINITY, delta = live ? delta_r : 0.f;
-    int lo_max = live ? lo : INT32_MAX;                  // (a row without a gradient: every tile is masked)
+    int lo_max = live ? lo : INT32_MIN;                  // (a row without a gradient gets zeros at the end)
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o));
     lo_max = uniform(lo_max);
-    const bool some_dead = __builtin_amdgcn_ballot_w64(!live) != 0;
     bf16x8 go[8];                                        // the lane's row of output gradients, dims 16 ks + 8 hh + 0..7
     {
         const unsigned char *p = (const unsigned char *)B.d_out + (R * W.n_q_heads + h) * (PC_D * 2) + 16 * hh;
@@ -273,11 +274,11 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
             for (int ks = 0; ks < 8; ++ks) s = MFMA32(rk.by_row(kt, ks), qop[ks], s);
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) dp = MFMA32(rv.get(vt, ks), go[ks], dp);
-            const bool edge = some_dead || e.valid < PC_TILE || (e.self && lim_first - e.pos0 < PC_TILE - 1) || (lo_max > e.pos0 && e.sink < PC_TILE);
+            const bool edge = e.valid < PC_TILE || (e.self && lim_first - e.pos0 < PC_TILE - 1) || (lo_max > e.pos0 && e.sink < PC_TILE);
             bool odd = false;
             uint32_t sees = ~0u;
             if (__builtin_expect(edge, 0)) {
-                sees = live ? win_sees(e.pos0, e.valid, e.sink, e.self != 0, lo, lim) : 0u;
+                sees = win_sees(e.pos0, e.valid, e.sink, e.self != 0, lo, lim);
                 f32x16 z;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) z[r] = 0.f;
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
                 const f32x16 &a = acc[2 * half + db];
-                *reinterpret_cast<float4 *>(stg + n * 256 + (((8 * db + 2 * q4 + hh) ^ (n & 15)) << 4)) = make_float4(a[4 * q4], a[4 * q4 + 1], a[4 * q4 + 2], a[4 * q4 + 3]);
+                *reinterpret_cast<float4 *>(stg + n * 256 + (((8 * db + 2 * q4 + hh) ^ (n & 15)) << 4)) = live ? make_float4(a[4 * q4], a[4 * q4 + 1], a[4 * q4 + 2], a[4 * q4 + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
         asm volatile("" ::: "memory");
 #pragma unroll
@@ -365,14 +366,16 @@ void pc_launch_win_bwd_rows(const PcWin &W, const PcWinBwd &B, const PcMergeRow 
 }
 
 // -------------------------------------------------------------------------------------------------------------- keys
-// A workgroup is 8 waves over four tiles of keys: waves 0 to 3 collect dv of a tile each, waves 4 to 7 dk (the scores are made
-// twice, which costs a fifth more matrix work; one wave with both sums would need 330 registers, and a SIMD would have one wave).
-// The units' turned queries, output gradients and statistics come by direct loads into a ring of four.
+// A workgroup is 8 waves over four tiles of keys: waves 0 to 3 make the probabilities of a tile and collect its dv, waves 4 to 7
+// collect its dk, a unit behind: they find the probabilities in shared memory (fp32).  A wave then has 16 matrix instructions a unit
+// and room for two waves a SIMD; with everything in one wave it would need 330 registers.  The units' turned queries, output
+// gradients and statistics come by direct loads into a ring of five.
 __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, PcWinBwd B)
 {
-    constexpr int RING = 4, AHEAD = 3, SLOT = 2 * TILE_BYTES + PC_WIN_STAT_BYTES;
+    constexpr int RING = 5, AHEAD = 3, SLOT = 2 * TILE_BYTES + PC_WIN_STAT_BYTES;
     __shared__ __attribute__((aligned(1024))) unsigned char s_ring[RING][SLOT];
     __shared__ __attribute__((aligned(1024))) unsigned char s_v[PC_WIN_KEY_TILES][TILE_BYTES];        // the call's values, in the store's order
+    __shared__ float4 s_p[2][PC_WIN_KEY_TILES][4][64];   // a unit's probabilities, in the lanes' order
 
     const int kh = blockIdx.x % W.n_kv_heads;
     const PcWinKeyItem item = B.key_items[blockIdx.x / W.n_kv_heads];
@@ -393,127 +396,172 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
     int cur = -1;
+    auto collect = [&](auto role) __attribute__((always_inline)) {
+    constexpr bool K = decltype(role)::value;
     for (int a = 0; a < item.n_apps; ++a) {
         const PcWinApp app = B.apps[item.app0 + a];
         const int pos0 = app.pos0 + PC_TILE * tile, valid = min(app.n_tok - PC_TILE * tile, PC_TILE), sink = min(max(app.sink - PC_TILE * tile, 0), PC_TILE);
         const bool active = valid > 0;
         const int U = app.n_blocks * g;
-        auto unit_of = [&](int i) { return (int64_t)(app.block0 + i / g) * W.n_q_heads + kh * g + i % g; };
-        auto request = [&](int i, int slot) __attribute__((always_inline)) {
-            const int64_t u = unit_of(i);
-            const unsigned to = ring + slot * SLOT + wave * 1024;
-            dma16((const unsigned char *)B.q_abs + u * TILE_BYTES, src, to);
-            dma16((const unsigned char *)B.d_o + u * TILE_BYTES, src, to + TILE_BYTES);
-            if (wave == 0) dma16(B.stat + u * PC_WIN_STAT_BYTES, lane * 16, to + 2 * TILE_BYTES);
+        int64_t next = (int64_t)app.block0 * W.n_q_heads + kh * g;       // the unit to ask for, and its head within the group
+        int next_j = 0, next_slot = 0;
+        auto request = [&]() __attribute__((always_inline)) {
+            const unsigned to = ring + next_slot * SLOT + wave * 1024;
+            dma16((const unsigned char *)B.q_abs + next * TILE_BYTES, src, to);
+            dma16((const unsigned char *)B.d_o + next * TILE_BYTES, src, to + TILE_BYTES);
+            if (!K && wave == 0) dma16(B.stat + next * PC_WIN_STAT_BYTES, lane * 16, to + 2 * TILE_BYTES);
+            ++next; ++next_j;
+            if (next_j == g) { next_j = 0; next += W.n_q_heads - g; }
+            next_slot = next_slot == RING - 1 ? 0 : next_slot + 1;
+        };
+        // all but the last N units that were asked for are there
+        auto landed = [&](auto N) __attribute__((always_inline)) {
+            constexpr int units = decltype(N)::value;
+            if (!K && wave == 0) wait_vm<3 * units>();
+            else wait_vm<2 * units>();
         };
         ring_barrier();                                  // (the last call's units and values are no longer read)
-        if (!is_k && active) {
+        if (!K && active) {
             const unsigned char *v = (const unsigned char *)W.v_store + ((int64_t)kh * W.slots + item.slot0 + PC_TILE * tile) * (PC_D * 2);
             const unsigned to = (unsigned)(uintptr_t)&s_v[tile][0];
 #pragma unroll
             for (int i = 0; i < 8; ++i) dma16(v, (unsigned)v_src_chunk(64 * i + lane) * 16, to + 1024 * i);
         }
-        for (int i = 0; i < min(AHEAD, U); ++i) request(i, i);
-        bf16x8 kop[8], vop[8];                           // the lane's key, turned and scaled, and its value: dims 16 ks + 8 hh + 0..7
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) kop[ks] = vop[ks] = frag4(0, 0, 0, 0);
-        if (active) {
-            const int64_t slot = (int64_t)kh * W.slots + item.slot0 + PC_TILE * tile + n;
-            const unsigned char *kp = (const unsigned char *)W.k_store + slot * (PC_D * 2) + 16 * hh;
-            const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)app.rot * (PC_D / 2) + 8 * hh);
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                const uint4 lk = ldg16(kp + 32 * ks), hk = ldg16(kp + 32 * ks + 128);
-                const uint32_t lw[4] = {lk.x, lk.y, lk.z, lk.w}, hw[4] = {hk.x, hk.y, hk.z, hk.w};
-                uint32_t x[4], y[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float4 r = rr[8 * ks + j];
-                    r.x *= W.scale_log2; r.y *= W.scale_log2; r.z *= W.scale_log2; r.w *= W.scale_log2;
-                    const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
-                    x[j] = pack_bf16(x0 * r.x - y0 * r.y, x1 * r.z - y1 * r.w);
-                    y[j] = pack_bf16(x0 * r.y + y0 * r.x, x1 * r.w + y1 * r.z);
-                }
-                kop[ks] = frag4(x[0], x[1], x[2], x[3]);
-                kop[ks + 4] = frag4(y[0], y[1], y[2], y[3]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (is_k) {
-                // dk, kept in the frame of the queries: from the last call's to this one's
+        for (int i = 0; i < min(AHEAD, U); ++i) request();
+        bf16x8 op[8];                                    // the lane's key, turned and scaled, or its value: dims 16 ks + 8 hh + 0..7
+        if constexpr (K) {
+            // dk, kept in the frame of the queries: from the last call's to this one's
+            if (active) {
                 if (cur >= 0 && cur != app.rot) turn_columns(acc, W.rot_run + (int64_t)app.rot * (PC_D / 2), W.rot_run + (int64_t)cur * (PC_D / 2), hh, 1.f);
                 cur = app.rot;
             }
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) op[ks] = frag4(0, 0, 0, 0);
+            if (active) {
+                const int64_t slot = (int64_t)kh * W.slots + item.slot0 + PC_TILE * tile + n;
+                const unsigned char *kp = (const unsigned char *)W.k_store + slot * (PC_D * 2) + 16 * hh;
+                const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)app.rot * (PC_D / 2) + 8 * hh);
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) {
+                    const uint4 lk = ldg16(kp + 32 * ks), hk = ldg16(kp + 32 * ks + 128);
+                    const uint32_t lw[4] = {lk.x, lk.y, lk.z, lk.w}, hw[4] = {hk.x, hk.y, hk.z, hk.w};
+                    uint32_t x[4], y[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float4 r = rr[8 * ks + j];
+                        r.x *= W.scale_log2; r.y *= W.scale_log2; r.z *= W.scale_log2; r.w *= W.scale_log2;
+                        const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
+                        x[j] = pack_bf16(x0 * r.x - y0 * r.y, x1 * r.z - y1 * r.w);
+                        y[j] = pack_bf16(x0 * r.y + y0 * r.x, x1 * r.w + y1 * r.z);
+                    }
+                    op[ks] = frag4(x[0], x[1], x[2], x[3]);
+                    op[ks + 4] = frag4(y[0], y[1], y[2], y[3]);
+                    if (ks & 1) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
-#pragma unroll 1
-        for (int i = 0, u = 0; i < U; ++i, u = (u + 1) & (RING - 1)) {
-            const unsigned qt = ring + u * SLOT, gt = qt + TILE_BYTES;
-            if (i + AHEAD > U) wait_vm<0>();
-            else if (wave == 0) wait_vm<3 * (AHEAD - 1)>();
-            else wait_vm<2 * (AHEAD - 1)>();
+        if (U >= AHEAD) landed(std::integral_constant<int, AHEAD - 1>());
+        else wait_vm<0>();
+        ring_barrier();
+        bf16x8 rows[8];                                  // the left operand of the wave's next unit, and that unit's limits
+        int4 head = make_int4(0, 0, 0, 0);
+        auto fetch = [&](int place) __attribute__((always_inline)) {
+            const unsigned left = ring + place * SLOT + (K ? TILE_BYTES : 0);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) rows[ks] = by_row.by_row(left, ks);
+            head = reinterpret_cast<const PcWinStat *>(&s_ring[place][2 * TILE_BYTES])->head;
+        };
+        if constexpr (K) {                               // (the values were asked for in front of the first unit)
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) op[ks] = values.get((unsigned)(uintptr_t)&s_v[tile][0], ks);
+        }
+        fetch(0);
+        // Step i: dv of unit i, dk of unit i - 1; unit i + 1 is there, and the left operand of the wave's next unit is read while the
+        // present one's second product runs (between two barriers all waves would else read first and multiply then).
+        auto step = [&](int i) __attribute__((always_inline)) {
+            if (i + AHEAD <= U) landed(std::integral_constant<int, AHEAD - 2>());
+            else wait_vm<0>();
+            if constexpr (!K) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // (the last unit's probabilities are written)
             ring_barrier();
-            if (i + AHEAD < U) request(i + AHEAD, (u + AHEAD) & (RING - 1));
-            if (i == 0 && is_k) {                        // (the values were asked for in front of the first unit)
+            if (i + AHEAD < U) request();
+        };
+        if constexpr (K) step(0);
+        int mine = 0, j = 0;                             // the unit's place in the ring, its head within the group
+        uint32_t seen = 0;                               // of the unit's block, where some row does not see some key: bit: register
+        bool have = false;
+#pragma unroll 1
+        for (int i = 0; i < U; ++i) {
+            step(K ? i + 1 : i);
+            const int lo_min = uniform(head.x), lo_max = uniform(head.y), lim_first = uniform(head.z), lim_last = uniform(head.w);
+            // something of the tile is seen by the unit; some row of it does not see all
+            const bool some = active && !(app.self && lim_last < pos0) && !(sink == 0 && lo_min > pos0 && (unsigned)lo_min - (unsigned)pos0 > PC_TILE - 1u);
+            const unsigned other = ring + mine * SLOT + (K ? 0 : TILE_BYTES);
+            const PcWinStat *stat = reinterpret_cast<const PcWinStat *>(&s_ring[mine][2 * TILE_BYTES]);
+            mine = mine == RING - 1 ? 0 : mine + 1;
+            bf16x8 cols[8], x[2];
+            if (some) {
+                const bool edge = valid < PC_TILE || (app.self && lim_first - pos0 < PC_TILE - 1) || lo_max == INT32_MAX || (lo_max > pos0 && sink < PC_TILE);
+                float4 *const probs = &s_p[i & 1][tile][0][lane];
+                f32x16 s;                                // scores or dp
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) vop[ks] = values.get((unsigned)(uintptr_t)&s_v[tile][0], ks);
-            }
-            const PcWinStat *stat = reinterpret_cast<const PcWinStat *>(&s_ring[u][2 * TILE_BYTES]);
-            const int4 hd = stat->head;
-            const int lo_min = uniform(hd.x), lo_max = uniform(hd.y), lim_first = uniform(hd.z), lim_last = uniform(hd.w);
-            // nothing of the tile is seen by the unit
-            if (!active || (app.self && lim_last < pos0) || (sink == 0 && lo_min > pos0 && (unsigned)lo_min - (unsigned)pos0 > PC_TILE - 1u)) continue;
-            const bool edge = valid < PC_TILE || (app.self && lim_first - pos0 < PC_TILE - 1) || lo_max == INT32_MAX || (lo_max > pos0 && sink < PC_TILE);
-            f32x16 s;
+                for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = 0.f;
+                for (int f = 0; f < 8; ++f) cols[f] = by_col.by_col(other, f >> 2, f & 3);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) s = MFMA32(by_row.by_row(qt, ks), kop[ks], s);
-            // register r: row 16 (r / 8) + 8 hh + r % 8, column: the lane's key
-            auto row_of = [&](int r) { return 16 * (r >> 3) + 8 * hh + (r & 7); };
-            uint32_t seen = ~0u;                         // bit: row
-            if (__builtin_expect(edge, 0)) {
-                const int4 rw = stat->rows;
-                const int pos = pos0 + min(n, valid - 1);
-                if (uniform(rw.y)) {                     // rows at consecutive positions: from the first that may see its own token to the last whose window holds the key
-                    auto first = [](unsigned n) { return n >= 32u ? ~0u : (1u << n) - 1u; };
-                    const unsigned below = pos < rw.z ? 0u : (unsigned)pos - (unsigned)rw.z + 1u;
-                    const unsigned above = app.self && pos > lim_first ? (unsigned)pos - (unsigned)lim_first : 0u;
-                    seen = (n < sink ? ~0u : below == 0u && pos >= rw.z ? ~0u : first(below)) & ~first(above);
-                } else {
-                    seen = 0;
-                    for (int i = 0; i < 32; ++i) seen |= ((pos >= stat->lo[i]) | (n < sink)) & (!app.self | (pos <= stat->lim[i])) ? 1u << i : 0u;
+                for (int ks = 0; ks < 8; ++ks) s = MFMA32(rows[ks], op[ks], s);
+                __builtin_amdgcn_sched_barrier(0);
+                // register r: row 16 (r / 8) + 8 hh + r % 8, column: the lane's key
+                const float4 *const st = reinterpret_cast<const float4 *>(K ? stat->delta : stat->lse2) + 2 * hh;
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    const float4 l = st[4 * (q4 >> 1) + (q4 & 1)];
+                    if constexpr (K) {
+                        const float4 p = probs[64 * q4];
+                        s[4 * q4] = p.x * (s[4 * q4] - l.x); s[4 * q4 + 1] = p.y * (s[4 * q4 + 1] - l.y);
+                        s[4 * q4 + 2] = p.z * (s[4 * q4 + 2] - l.z); s[4 * q4 + 3] = p.w * (s[4 * q4 + 3] - l.w);
+                    } else {
+                        s[4 * q4] = ex2(s[4 * q4] - l.x); s[4 * q4 + 1] = ex2(s[4 * q4 + 1] - l.y); s[4 * q4 + 2] = ex2(s[4 * q4 + 2] - l.z); s[4 * q4 + 3] = ex2(s[4 * q4 + 3] - l.w);
+                        probs[64 * q4] = make_float4(s[4 * q4], s[4 * q4 + 1], s[4 * q4 + 2], s[4 * q4 + 3]);
+                    }
                 }
-                seen &= n < valid ? (uint32_t)rw.x : 0u;
-            }
+                if (__builtin_expect(edge, 0)) {
+                    if (!have) {                         // (the heads of a group see the same)
+                        const int pos = pos0 + min(n, valid - 1), from = n < sink ? INT32_MAX : pos, upto = app.self ? pos : INT32_MIN;
+                        seen = 0;
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const float4 x = *reinterpret_cast<const float4 *>(&stat->lse2[row_of(r)]);
-                s[r] = ex2(s[r] - x.x); s[r + 1] = ex2(s[r + 1] - x.y); s[r + 2] = ex2(s[r + 2] - x.z); s[r + 3] = ex2(s[r + 3] - x.w);
-            }
-            if (is_k) {
-                f32x16 dp;
+                        for (int q4 = 0; q4 < 4; ++q4) {
+                            const int at = 4 * (q4 >> 1) + (q4 & 1) + 2 * hh;
+                            const int4 lo = reinterpret_cast<const int4 *>(stat->lo)[at], lim = reinterpret_cast<const int4 *>(stat->lim)[at];
+                            seen |= (uint32_t)((lo.x <= from) & (lim.x >= upto)) << (4 * q4) | (uint32_t)((lo.y <= from) & (lim.y >= upto)) << (4 * q4 + 1) |
+                                    (uint32_t)((lo.z <= from) & (lim.z >= upto)) << (4 * q4 + 2) | (uint32_t)((lo.w <= from) & (lim.w >= upto)) << (4 * q4 + 3);
+                        }
+                        if (n >= valid) seen = 0;
+                        have = true;
+                    }
+                    // (what is masked need not be finite: its bits are taken away)
+                    const uint32_t live = (uint32_t)stat->live >> (8 * hh), both = seen & ((live & 0xFFu) | (live >> 8 & 0xFF00u));
 #pragma unroll
-                for (int r = 0; r < 16; ++r) dp[r] = 0.f;
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) dp = MFMA32(by_row.by_row(gt, ks), vop[ks], dp);
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const float4 x = *reinterpret_cast<const float4 *>(&stat->delta[row_of(r)]);
-                    s[r] *= dp[r] - x.x; s[r + 1] *= dp[r + 1] - x.y; s[r + 2] *= dp[r + 2] - x.z; s[r + 3] *= dp[r + 3] - x.w;
+                    for (int r = 0; r < 16; ++r) s[r] = __uint_as_float(__float_as_uint(s[r]) & (uint32_t)((int32_t)(both << (31 - r)) >> 31));
                 }
+                uint32_t pk[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) pk[r] = pack_bf16(s[2 * r], s[2 * r + 1]);
+                x[0] = frag4(pk[0], pk[1], pk[2], pk[3]); x[1] = frag4(pk[4], pk[5], pk[6], pk[7]);
             }
-            if (__builtin_expect(edge, 0)) {
+            if (i + 1 < U) fetch(mine);
+            if (some) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = (seen >> row_of(r)) & 1 ? s[r] : 0.f;
+                for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(cols[f], x[f >> 2], acc[f & 3]);
             }
-            uint32_t pk[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) pk[r] = pack_bf16(s[2 * r], s[2 * r + 1]);
-            const bf16x8 x[2] = {frag4(pk[0], pk[1], pk[2], pk[3]), frag4(pk[4], pk[5], pk[6], pk[7])};
-            const unsigned other = is_k ? qt : gt;
-#pragma unroll
-            for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(by_col.by_col(other, f >> 2, f & 3), x[f >> 2], acc[f & 3]);
+            if (++j == g) { j = 0; have = false; }
         }
+        if constexpr (!K) step(U);
     }
+    };
+    if (is_k) collect(std::true_type());
+    else collect(std::false_type());
     if (my_keys <= 0) return;
     if (is_k && cur >= 0) {                              // back by the run's rotation (keys as they are stored)
         const float2 *rr = W.rot_run + (int64_t)cur * (PC_D / 2);

@@ -76,8 +76,8 @@ struct PcWinSum { int32_t slot0, n_keys, part0, n_parts; };       // tiles whose
 struct PcWinStat {            // of a unit's rows
     float lse2[32], delta[32];        // lse log2 e (+inf: no gradient), Delta
     int32_t lo[32], lim[32];          // the positions a row sees: from, up to (own)
-    int4 head;                // least lo; largest lo (INT32_MAX if some row has no gradient); first and last lim
-    int4 rows;                // bits of the rows with a gradient; 1: their lo rise by one from row to row; lo of row 0
+    int4 head;                // least lo; largest lo (INT32_MAX if some row that is there has no gradient); first and last lim
+    int32_t live;             // bits of the rows with a gradient
 };
 #define PC_WIN_STAT_BYTES 1024
 static_assert(sizeof(PcWinStat) <= PC_WIN_STAT_BYTES, "");
