@@ -19,6 +19,14 @@
 namespace {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// the lane's number, made where it stands: kept from the kernel's start it would wait in memory, and who fetches a register from
+// there waits for all loads before it
+__device__ __forceinline__ int lane_again()
+{
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+    return x;
+}
 __device__ __forceinline__ bool finite16(uint32_t bits) { return (bits & 0x7F80u) != 0x7F80u; }
 __device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 x)
 {
@@ -190,7 +198,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
         dma16(vb + at, v_src, to + TILE_BYTES);
         dma16(vb + at + 4096, v_src, to + TILE_BYTES + 4096);
     };
-    const RowMajor rk(perm_row(n), lane);
+    const RowMajor by_key(perm_row(n), lane);
     const ValuesByKey<true> rv(lane);
 
     const int T = item.n_tiles;
@@ -267,6 +275,8 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
                 turn(cur);
             }
             ask(d[AHEAD], (u + AHEAD) & (RING - 1));
+            RowMajor rk = by_key;
+            asm volatile("" : "+v"(rk.row_at), "+v"(rk.col_at[0]), "+v"(rk.col_at[1]));       // (sixteen addresses made once and kept would not fit the registers)
             f32x16 s, dp;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
@@ -378,7 +388,7 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
     __shared__ float4 s_p[2][PC_WIN_KEY_TILES][4][64];   // a unit's probabilities, in the lanes' order
 
     const int kh = blockIdx.x % W.n_kv_heads;
-    const PcWinKeyItem item = B.key_items[blockIdx.x / W.n_kv_heads];
+    const int bin = blockIdx.x / W.n_kv_heads;
     const int g = W.n_q_heads / W.n_kv_heads;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int n = lane & 31, hh = lane >> 5;
@@ -388,8 +398,11 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
     const unsigned src = (threadIdx.x >> 4) * 256 + (((threadIdx.x & 15) ^ swz(threadIdx.x >> 4)) << 4);
     const RowMajor by_row(perm_row(n), lane), by_col(n, lane);
     const ValuesByKey<false> values(lane);               // by key, the lane's one
+    const int item_end = B.bins[bin + 1];
+#pragma unroll 1
+    for (int i_item = B.bins[bin]; i_item < item_end; ++i_item) {
+    const PcWinKeyItem item = B.key_items[i_item];
     const int my_keys = item.n_keys - PC_TILE * tile;    // of the wave's tile
-
     f32x16 acc[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db)
@@ -468,8 +481,10 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
         int4 head = make_int4(0, 0, 0, 0);
         auto fetch = [&](int place) __attribute__((always_inline)) {
             const unsigned left = ring + place * SLOT + (K ? TILE_BYTES : 0);
+            RowMajor at = by_row;
+            asm volatile("" : "+v"(at.row_at));          // (eight addresses made once and kept would not fit the registers)
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) rows[ks] = by_row.by_row(left, ks);
+            for (int ks = 0; ks < 8; ++ks) rows[ks] = at.by_row(left, ks);
             head = reinterpret_cast<const PcWinStat *>(&s_ring[place][2 * TILE_BYTES])->head;
         };
         if constexpr (K) {                               // (the values were asked for in front of the first unit)
@@ -506,8 +521,10 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
                 f32x16 s;                                // scores or dp
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = 0.f;
+                RowMajor at = by_col;
+                asm volatile("" : "+v"(at.col_at[0]), "+v"(at.col_at[1]));
 #pragma unroll
-                for (int f = 0; f < 8; ++f) cols[f] = by_col.by_col(other, f >> 2, f & 3);
+                for (int f = 0; f < 8; ++f) cols[f] = at.by_col(other, f >> 2, f & 3);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks) s = MFMA32(rows[ks], op[ks], s);
@@ -527,6 +544,7 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
                     }
                 }
                 if (__builtin_expect(edge, 0)) {
+                    const int at_lane = lane_again(), n = at_lane & 31, hh = at_lane >> 5;
                     if (!have) {                         // (the heads of a group see the same)
                         const int pos = pos0 + min(n, valid - 1), from = n < sink ? INT32_MAX : pos, upto = app.self ? pos : INT32_MIN;
                         seen = 0;
@@ -562,7 +580,8 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
     };
     if (is_k) collect(std::true_type());
     else collect(std::false_type());
-    if (my_keys <= 0) return;
+    ring_barrier();                                      // (dk is a unit behind: the ring is free only now)
+    if (my_keys <= 0) continue;
     if (is_k && cur >= 0) {                              // back by the run's rotation (keys as they are stored)
         const float2 *rr = W.rot_run + (int64_t)cur * (PC_D / 2);
 #pragma unroll
@@ -580,30 +599,42 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
                 }
             }
     }
-    if (item.part >= 0) {
-        float *to = B.key_part + ((((int64_t)item.part * W.n_kv_heads + kh) * 2 + (is_k ? 0 : 1)) * (PC_WIN_KEY_TILES * PC_TILE) + PC_TILE * tile + n) * PC_D + 4 * hh;
+    // out as whole lines, in two halves of a row, over the ring
+    unsigned char *stg = &s_ring[0][0] + wave * TILE_BYTES;
+    const int at_lane = lane_again(), n = at_lane & 31, hh = at_lane >> 5, r4 = at_lane >> 4, c = at_lane & 15;
+    const bool whole = item.part < 0;
+    float *to = whole ? (is_k ? B.d_k : B.d_v) + (((int64_t)item.slot0 + PC_TILE * tile) * W.n_kv_heads + kh) * PC_D + 4 * c
+                      : B.key_part + ((((int64_t)item.part * W.n_kv_heads + kh) * 2 + (is_k ? 0 : 1)) * (PC_WIN_KEY_TILES * PC_TILE) + PC_TILE * tile) * PC_D + 4 * c;
+    const int64_t stride = whole ? (int64_t)W.n_kv_heads * PC_D : PC_D;
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
+    for (int half = 0; half < 2; ++half) {
+        asm volatile("" ::: "memory");
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)
-                *reinterpret_cast<float4 *>(to + 32 * db + 8 * q4) = make_float4(acc[db][4 * q4], acc[db][4 * q4 + 1], acc[db][4 * q4 + 2], acc[db][4 * q4 + 3]);
-        return;
-    }
-    if (n >= my_keys) return;
-    float *to = (is_k ? B.d_k : B.d_v) + (((int64_t)item.slot0 + PC_TILE * tile + n) * W.n_kv_heads + kh) * PC_D + 4 * hh;
+        for (int db = 0; db < 2; ++db)
 #pragma unroll
-    for (int db = 0; db < 4; ++db)
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x16 &a = acc[2 * half + db];
+                *reinterpret_cast<float4 *>(stg + n * 256 + (((8 * db + 2 * q4 + hh) ^ (n & 15)) << 4)) = make_float4(a[4 * q4], a[4 * q4 + 1], a[4 * q4 + 2], a[4 * q4 + 3]);
+            }
+        asm volatile("" ::: "memory");
+        float4 was[8];
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-            float4 *p = reinterpret_cast<float4 *>(to + 32 * db + 8 * q4), v = *p;
-            v.x += acc[db][4 * q4]; v.y += acc[db][4 * q4 + 1]; v.z += acc[db][4 * q4 + 2]; v.w += acc[db][4 * q4 + 3];
-            *p = v;
+        for (int i = 0; i < 8; ++i) was[i] = whole && 4 * i + r4 < my_keys ? *reinterpret_cast<const float4 *>(to + (4 * i + r4) * stride + 64 * half) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + r4;
+            float4 v = *reinterpret_cast<const float4 *>(stg + r * 256 + ((c ^ (r & 15)) << 4));
+            v.x += was[i].x; v.y += was[i].y; v.z += was[i].z; v.w += was[i].w;
+            if (r < my_keys) *reinterpret_cast<float4 *>(to + r * stride + 64 * half) = v;
         }
+    }
+    wait_vm<0>();                                        // (what is counted from here on are the next item's loads alone)
+    }
 }
 
 void pc_launch_win_bwd_keys_bf16(const PcWin &W, const PcWinBwd &B, hipStream_t st)
 {
-    if (B.n_key_items > 0) pc_win_bwd_keys_bf16_kernel<<<(unsigned)B.n_key_items * W.n_kv_heads, 512, 0, st>>>(W, B);
+    if (B.n_bins > 0) pc_win_bwd_keys_bf16_kernel<<<(unsigned)B.n_bins * W.n_kv_heads, 512, 0, st>>>(W, B);
 }
 
 // The parts of tiles that several items collect, added up in their order and to what is there: a thread four numbers, eight parts a

@@ -203,9 +203,12 @@ __global__ __launch_bounds__(256, 1) void pc_win_bwd_keys_f32_kernel(PcWin W, Pc
     constexpr int HALF = D / 2, P = D / 4, VW = D / 32, SLOT = 2 * RowTile<D>::BYTES + PC_WIN_STAT_BYTES;
     __shared__ __attribute__((aligned(1024))) unsigned char s_ring[2][SLOT];
     const int kh = blockIdx.x % W.n_kv_heads;
-    const PcWinKeyItem item = B.key_items[blockIdx.x / W.n_kv_heads];
+    const int bin = blockIdx.x / W.n_kv_heads, item_end = B.bins[bin + 1];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int n = lane & 31, hh = lane >> 5;
+#pragma unroll 1
+    for (int i_item = B.bins[bin]; i_item < item_end; ++i_item) {
+    const PcWinKeyItem item = B.key_items[i_item];
     const int my_keys = item.n_keys - PC_TILE * wave;
     f32x16 dk[VW], dv[VW];
 #pragma unroll
@@ -308,7 +311,7 @@ __global__ __launch_bounds__(256, 1) void pc_win_bwd_keys_f32_kernel(PcWin W, Pc
             }
         }
     }
-    if (my_keys <= 0) return;
+    if (my_keys <= 0) continue;
     if (cur >= 0) {                                      // back by the run's rotation (keys as they are stored): less its angles
         const float2 *rot = W.rot_run + (int64_t)cur * HALF;
 #pragma unroll
@@ -322,7 +325,7 @@ __global__ __launch_bounds__(256, 1) void pc_win_bwd_keys_f32_kernel(PcWin W, Pc
             }
     }
     const bool whole = item.part < 0;
-    if (whole && n >= my_keys) return;
+    if (whole && n >= my_keys) continue;
     const int64_t in_part = (int64_t)PC_TILE * wave + n;
     float *to_k, *to_v;
     if (whole) {
@@ -342,12 +345,13 @@ __global__ __launch_bounds__(256, 1) void pc_win_bwd_keys_f32_kernel(PcWin W, Pc
         if (whole) { x += *pk; y += *pv; }
         *pk = x; *pv = y;
     }
+    }
 }
 
 void pc_launch_win_bwd_keys_f32(const PcWin &W, const PcWinBwd &B, int D, hipStream_t st)
 {
-    if (B.n_key_items <= 0) return;
-    const unsigned grid = (unsigned)B.n_key_items * W.n_kv_heads;
+    if (B.n_bins <= 0) return;
+    const unsigned grid = (unsigned)B.n_bins * W.n_kv_heads;
     if (D == 64) pc_win_bwd_keys_f32_kernel<64><<<grid, 256, 0, st>>>(W, B);
     else pc_win_bwd_keys_f32_kernel<128><<<grid, 256, 0, st>>>(W, B);
 }

@@ -86,7 +86,8 @@ struct PcWinBwd {
     const PcWinApp     *apps;
     const PcWinKeyItem *key_items;
     const PcWinSum     *sums;
-    int32_t n_blocks, n_key_items, n_sums, pad;
+    const int32_t      *bins; // [n_bins + 1] the first of each workgroup's items
+    int32_t n_blocks, n_bins, n_sums, pad;
     const void  *out, *d_out;
     const float *lse;
     float       *delta;       // [rows][H_q]

@@ -3,6 +3,7 @@
 #include "pc_window.h"
 
 #include <new>
+#include <queue>
 
 namespace {
 
@@ -211,6 +212,7 @@ struct BwdPlan {
     std::vector<PcWinApp> apps;
     std::vector<PcWinKeyItem> keys;
     std::vector<PcWinSum> sums;
+    std::vector<int32_t> bins;                           // the first of each workgroup's items of keys, and their end
     int32_t parts = 0;
 };
 
@@ -270,7 +272,6 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
     struct Tiles { int32_t slot0, n_keys; size_t app0, n_apps; int64_t blocks; };
     std::vector<Tiles> all;
     std::vector<PcWinApp> apps;
-    int64_t total = 0;
     constexpr int32_t KEYS = PC_WIN_KEY_TILES * PC_TILE;
     for (size_t a = 0; a < listed.size();) {
         size_t b = a;
@@ -302,49 +303,77 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
                 t.blocks += b1 - b0;
             }
             t.n_apps = apps.size() - t.app0;
-            total += t.blocks;
             if (t.n_apps > 0) all.push_back(t);
         }
         a = b;
     }
-    // An item's share: what brings the launch to one workgroup a compute unit; tiles with more (those that every row sees,
-    // messages that many calls list) are cut and their parts added up.  The longest items come first.
-    const int64_t share = std::max<int64_t>(4, (total * H_kv + 255) / 256);
-    for (const Tiles &t : all) {
-        const int64_t n = t.blocks * 4 > share * 5 ? std::min<int64_t>((t.blocks + share - 1) / share, 1024) : 1;
-        const int32_t part0 = B.parts;
-        size_t k = t.app0;
-        int32_t taken = 0;                               // blocks of app k that earlier parts have
-        int64_t done = 0;
-        for (int64_t part = 0; part < n; ++part) {
-            const int64_t upto = t.blocks * (part + 1) / n;
-            PcWinKeyItem it{t.slot0, t.n_keys, (int32_t)B.apps.size(), 0, n == 1 ? -1 : part0 + (int32_t)part, {0, 0, 0}};
-            while (done < upto) {
-                const int32_t m = (int32_t)std::min<int64_t>(apps[k].n_blocks - taken, upto - done);
-                PcWinApp app = apps[k];
-                app.block0 += taken; app.n_blocks = m;
-                B.apps.push_back(app);
-                done += m; taken += m;
-                if (taken == apps[k].n_blocks) { ++k; taken = 0; }
+    // The items go to as many workgroups as run at once (a further one would wait for a place in a part of the chip that is not the
+    // first to have one): the longest first, each to the workgroup with the least.  Tiles with more than a share of the work (those
+    // that every row sees, messages that many calls list) are cut and their parts added up; smaller shares balance better and cost
+    // more starts, so the best of a few is taken.  Work is counted in units of bf16 (32 columns of fp32 take four
+    // times as long); an item's start and end are worth six, a call's two.
+    const int64_t per_block = f32 ? 4 : g, bins = std::max<int64_t>(1, 256 / H_kv);
+    auto cost = [&](int64_t n_blocks, int64_t n_apps) { return n_blocks * per_block + 2 * n_apps + 6; };
+    int64_t total = 0;
+    for (const Tiles &t : all) total += cost(t.blocks, (int64_t)t.n_apps);
+    struct Keys { std::vector<PcWinApp> apps; std::vector<PcWinKeyItem> items; std::vector<PcWinSum> sums; std::vector<int32_t> bins; int32_t parts = 0; int64_t worst = INT64_MAX; } best;
+    for (int64_t cut = 1; cut <= 3; ++cut) {
+        const int64_t share = std::max<int64_t>(16, (total + bins * cut - 1) / (bins * cut));
+        Keys K;
+        std::vector<int64_t> size;
+        for (const Tiles &t : all) {
+            const int64_t n = std::min<int64_t>({(cost(t.blocks, (int64_t)t.n_apps) + share - 1) / share, std::max<int64_t>(1, t.blocks / 2), 1024});
+            const int32_t part0 = K.parts;
+            size_t k = t.app0;
+            int32_t taken = 0;                           // blocks of app k that earlier parts have
+            int64_t done = 0;
+            for (int64_t part = 0; part < n; ++part) {
+                const int64_t first = done, upto = t.blocks * (part + 1) / n;
+                PcWinKeyItem it{t.slot0, t.n_keys, (int32_t)K.apps.size(), 0, n == 1 ? -1 : part0 + (int32_t)part, {0, 0, 0}};
+                while (done < upto) {
+                    const int32_t m = (int32_t)std::min<int64_t>(apps[k].n_blocks - taken, upto - done);
+                    PcWinApp app = apps[k];
+                    app.block0 += taken; app.n_blocks = m;
+                    K.apps.push_back(app);
+                    done += m; taken += m;
+                    if (taken == apps[k].n_blocks) { ++k; taken = 0; }
+                }
+                it.n_apps = (int32_t)K.apps.size() - it.app0;
+                K.items.push_back(it);
+                size.push_back(cost(done - first, it.n_apps));
             }
-            it.n_apps = (int32_t)B.apps.size() - it.app0;
-            B.keys.push_back(it);
+            if (n > 1) {                                 // (parts stand where their numbers say, whatever their order)
+                K.sums.push_back(PcWinSum{t.slot0, t.n_keys, part0, (int32_t)n});
+                K.parts += (int32_t)n;
+            }
         }
-        if (n > 1) {                                     // (parts stand where their numbers say, whatever their order in the launch)
-            B.sums.push_back(PcWinSum{t.slot0, t.n_keys, part0, (int32_t)n});
-            B.parts += (int32_t)n;
+        std::vector<uint32_t> by(K.items.size());
+        for (size_t i = 0; i < by.size(); ++i) by[i] = (uint32_t)i;
+        std::stable_sort(by.begin(), by.end(), [&](uint32_t x, uint32_t y) { return size[x] > size[y]; });
+        const size_t n_bins = std::min<size_t>(by.size(), (size_t)bins);
+        std::vector<std::vector<uint32_t>> in(n_bins);
+        std::priority_queue<std::pair<int64_t, uint32_t>, std::vector<std::pair<int64_t, uint32_t>>, std::greater<>> least;
+        for (size_t i = 0; i < n_bins; ++i) least.push({0, (uint32_t)i});
+        K.worst = 0;
+        for (uint32_t i : by) {
+            const auto [load, bin] = least.top();
+            least.pop();
+            in[bin].push_back(i);
+            K.worst = std::max(K.worst, load + size[i]);
+            least.push({load + size[i], bin});
         }
+        if (K.worst >= best.worst) continue;
+        std::vector<PcWinKeyItem> sorted;
+        for (const auto &list : in) {
+            K.bins.push_back((int32_t)sorted.size());
+            for (uint32_t i : list) sorted.push_back(K.items[i]);
+        }
+        K.bins.push_back((int32_t)sorted.size());
+        K.items.swap(sorted);
+        best = std::move(K);
     }
-    std::vector<int64_t> size(B.keys.size());
-    std::vector<uint32_t> by(B.keys.size());
-    for (size_t i = 0; i < B.keys.size(); ++i) {
-        by[i] = (uint32_t)i;
-        for (int32_t k = 0; k < B.keys[i].n_apps; ++k) size[i] += B.apps[(size_t)(B.keys[i].app0 + k)].n_blocks + 2;
-    }
-    std::stable_sort(by.begin(), by.end(), [&](uint32_t a, uint32_t b) { return size[a] > size[b]; });
-    std::vector<PcWinKeyItem> sorted(B.keys.size());
-    for (size_t i = 0; i < by.size(); ++i) sorted[i] = B.keys[by[i]];
-    B.keys.swap(sorted);
+    B.apps.swap(best.apps); B.keys.swap(best.items); B.sums.swap(best.sums); B.bins.swap(best.bins);
+    B.parts = best.parts;
 }
 
 int32_t check(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink)
@@ -461,7 +490,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 16); return a; };
     auto of = [](const auto &v) { return sizeof(v[0]) * v.size(); };
     const size_t items = take(of(P.pre)), runs = take(of(P.runs)), merge = take(of(P.merge)), q_pos = take(of(P.q_pos)), rots = take(of(P.rots));
-    const size_t blocks = take(of(B.blocks)), apps = take(of(B.apps)), keys = take(of(B.keys)), sums = take(of(B.sums)), lists = at;
+    const size_t blocks = take(of(B.blocks)), apps = take(of(B.apps)), keys = take(of(B.keys)), sums = take(of(B.sums)), bins = take(of(B.bins)), lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = sizeof(float2) * (size_t)c->half, units = B.blocks.size() * (size_t)(bf16 ? Hq : H), unit = 32 * (size_t)c->D * c->esize;
     const size_t rot_q = big(rot * P.q_pos.size()), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * P.q_pos.size() * (size_t)Hq);
@@ -481,14 +510,14 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     char *from = in_args ? (char *)blob.w : (char *)slot->host;
     auto put = [&](size_t to, const auto &v) { if (!v.empty()) std::memcpy(from + to, v.data(), of(v)); };
     put(items, P.pre); put(runs, P.runs); put(merge, P.merge); put(q_pos, P.q_pos); put(rots, P.rots);
-    put(blocks, B.blocks); put(apps, B.apps); put(keys, B.keys); put(sums, B.sums);
+    put(blocks, B.blocks); put(apps, B.apps); put(keys, B.keys); put(sums, B.sums); put(bins, B.bins);
 
     W.items = (const PcWinItem *)(ws + items); W.runs = (const PcWinRun *)(ws + runs); W.q_pos = (const int32_t *)(ws + q_pos);
     W.rot_q = (const float2 *)(ws + rot_q); W.rot_run = (const float2 *)(ws + rot_run);
     W.part_o = (float *)(ws + part_o);
     G.blocks = (const PcWinBlock *)(ws + blocks); G.apps = (const PcWinApp *)(ws + apps);
-    G.key_items = (const PcWinKeyItem *)(ws + keys); G.sums = (const PcWinSum *)(ws + sums);
-    G.n_blocks = (int32_t)B.blocks.size(); G.n_key_items = (int32_t)B.keys.size(); G.n_sums = (int32_t)B.sums.size();
+    G.key_items = (const PcWinKeyItem *)(ws + keys); G.sums = (const PcWinSum *)(ws + sums); G.bins = (const int32_t *)(ws + bins);
+    G.n_blocks = (int32_t)B.blocks.size(); G.n_bins = std::max<int32_t>(0, (int32_t)B.bins.size() - 1); G.n_sums = (int32_t)B.sums.size();
     G.delta = (float *)(ws + delta); G.q_abs = ws + q_abs; G.d_o = ws + d_o; G.stat = ws + stat; G.key_part = (float *)(ws + key_part);
     PcWinTurns T{};
     T.from = in_args ? ws : slot->host; T.ws = ws; T.n16 = (int)(lists / 16);
