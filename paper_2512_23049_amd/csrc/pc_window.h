@@ -51,6 +51,38 @@ struct PcWin {
 // Offsets of a decode launch's lists, where they travel in its arguments.
 struct PcWinDecode { int32_t off_items, off_runs, off_q_pos, n16; void *ws; };      // n16 > 0: so many pieces of 16 bytes are left in the workspace for the merge
 
+// ---- single tokens of calls that list the same messages ----
+#define PC_WIN_GROUPS 16      // groups of 16 columns (calls x heads of the KV head) a workgroup takes at most
+struct PcWinVisit {           // consecutive tiles, and who sees some of them
+    int32_t slot0, n_tiles;
+    int32_t e0;               // the first of its entries
+    int32_t off[PC_WIN_GROUPS + 1];   // of them: the first of each group of columns
+};
+struct PcWinSee {             // a call's view of a visit
+    int32_t pos0;             // position the call gives the visit's first token
+    int32_t n_tok;            // tokens from there on that count
+    int32_t sink, lo;         // as in PcWinRun; the least position that is visible but for the sinks
+    int64_t turn;             // the row's position less the run's rotation: what its queries are turned by
+    int32_t sub;              // the call's place in its group of columns
+    int32_t pad;
+};
+struct PcWinSharedItem {      // one workgroup's tiles, for each KV head
+    int32_t visit0, n_tiles;
+    int32_t call0, n_calls;   // its set of calls
+    int32_t waves;            // that hold all groups of columns (a power of two); the others take every second, fourth.. tile
+    int32_t split0;
+    int32_t pad[2];
+};
+struct PcWinSharedCall { int32_t row, part0; };         // packed row, partial row of split 0
+struct PcWinShared {
+    const PcWinSharedItem *items;
+    const PcWinVisit      *visits;
+    const PcWinSee        *sees;
+    const PcWinSharedCall *calls;
+    int32_t n_items;
+    int32_t wide;             // 1: two groups of columns a wave
+};
+
 // ---- the gradient ----
 // 32 rows (fp32: 32 (row, head) columns of a KV head) of a call.
 struct PcWinBlock { int32_t q_off, n_q, lim0, block; };
@@ -136,6 +168,7 @@ void pc_launch_win_prefill_bf16(const PcWin &W, int n_items, hipStream_t st);
 // blob: its lists (W.items, W.runs and W.q_pos are not read then), or null
 void pc_launch_win_decode_bf16(const PcWin &W, int n_items, const PcArgBlob *blob, const PcWinDecode &O, hipStream_t st);
 void pc_launch_win_attend_f32(const PcWin &W, int n_items, int D, hipStream_t st);
+void pc_launch_win_shared_decode_bf16(const PcWin &W, const PcWinShared &S, hipStream_t st);
 void pc_launch_win_merge(const PcWin &W, const PcMergeRow *rows, int n_rows, int dtype, int D, hipStream_t st);
 
 #ifdef __HIPCC__

@@ -31,6 +31,12 @@ struct WinPlan {
     std::vector<PcMergeRow> merge;
     int64_t part_rows = 0;
     int32_t window = 0, n_sink = 0;
+    // single tokens of calls that list the same messages
+    std::vector<PcWinSharedItem> sh_items;
+    std::vector<PcWinVisit> sh_visits;
+    std::vector<PcWinSee> sh_sees;
+    std::vector<PcWinSharedCall> sh_calls;
+    bool sh_wide = false;
 };
 
 int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan &P)
@@ -135,11 +141,115 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
     }
 }
 
+// Single tokens by what they see together: the tiles that the calls of a set see, each once, in as many ranges as workgroups run at
+// once.  False (and nothing is planned) where reading every call's own tiles is less.
+bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
+{
+    const int H = c->cfg.n_kv_heads, g = c->g, per = 16 / g;
+    const int32_t n_calls = (int32_t)dec.size(), n_groups = (n_calls + per - 1) / per;
+    if (n_groups < 3) return false;                      // (waves without columns would have every fourth tile at most)
+    const bool wide = n_groups > PC_WIN_GROUPS / 2;
+    const int32_t set_calls = std::min(n_groups, wide ? PC_WIN_GROUPS : PC_WIN_GROUPS / 2) * per, n_sets = (n_calls + set_calls - 1) / set_calls;
+    struct Piece { int32_t slot0, tiles; size_t run; int32_t call; };
+    std::vector<Piece> pieces;
+    std::vector<std::pair<size_t, size_t>> of_set;       // a set's pieces, in slot order
+    int64_t own = 0, shared = 0;
+    for (int32_t s = 0; s < n_sets; ++s) {
+        const size_t first = pieces.size();
+        for (int32_t j = s * set_calls; j < std::min(n_calls, (s + 1) * set_calls); ++j) {
+            int32_t left = dec[(size_t)j].tiles;
+            for (size_t r = (size_t)dec[(size_t)j].run0; left > 0; ++r) {
+                const int32_t t = (P.runs[r].n_tok + PC_TILE - 1) / PC_TILE;
+                pieces.push_back(Piece{P.runs[r].slot0, t, r, j});
+                left -= t;
+            }
+            own += dec[(size_t)j].tiles;
+        }
+        std::sort(pieces.begin() + (ptrdiff_t)first, pieces.end(), [](const Piece &x, const Piece &y) { return x.slot0 != y.slot0 ? x.slot0 < y.slot0 : x.run < y.run; });
+        int64_t end = -1;
+        for (size_t k = first; k < pieces.size(); ++k) {
+            const int64_t b = pieces[k].slot0, e = b + (int64_t)PC_TILE * pieces[k].tiles;
+            if (e > end) { shared += (e - std::max(b, end)) / PC_TILE; end = e; }
+        }
+        of_set.push_back({first, pieces.size()});
+    }
+    // What both ways read and write, in tiles: a workgroup's partial rows are worth 8 (16 with two groups a wave).
+    const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
+    if (own * 2 < 3 * (shared + bins * n_sets * (wide ? 16 : 8))) return false;
+    for (int32_t s = 0; s < n_sets; ++s) {
+        const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
+        int32_t waves = 1;
+        while (waves * (wide ? 2 : 1) < groups) waves *= 2;
+        // ranges of consecutive tiles
+        struct Visit { int32_t slot0, tiles; size_t p0, p1; };
+        std::vector<Visit> visits;
+        int64_t total = 0;
+        for (size_t k = of_set[(size_t)s].first; k < of_set[(size_t)s].second;) {
+            Visit v{pieces[k].slot0, 0, k, k};
+            for (; v.p1 < of_set[(size_t)s].second && (v.p1 == v.p0 || pieces[v.p1].slot0 < v.slot0 + PC_TILE * v.tiles); ++v.p1)
+                v.tiles = std::max(v.tiles, (pieces[v.p1].slot0 - v.slot0) / PC_TILE + pieces[v.p1].tiles);
+            total += v.tiles;
+            visits.push_back(v);
+            k = v.p1;
+        }
+        const int64_t n_bins = std::max<int64_t>(1, std::min(bins, total));
+        const int32_t splits = (int32_t)n_bins * (8 / waves);
+        size_t at = 0;
+        int32_t done = 0;                                // tiles of visits[at] that earlier workgroups have
+        for (int64_t b = 0; b < n_bins; ++b) {
+            int32_t left = (int32_t)(total * (b + 1) / n_bins - total * b / n_bins);
+            P.sh_items.push_back(PcWinSharedItem{(int32_t)P.sh_visits.size(), left, call0, in_set, waves, (int32_t)b * (8 / waves), {0, 0}});
+            while (left > 0) {
+                const Visit &v = visits[at];
+                const int32_t n = std::min(left, v.tiles - done), slot0 = v.slot0 + PC_TILE * done, slot1 = slot0 + PC_TILE * n;
+                std::vector<std::pair<int32_t, PcWinSee>> seen;                  // (call within the set, view)
+                for (size_t k = v.p0; k < v.p1; ++k) {
+                    const Piece &pc = pieces[k];
+                    if (pc.slot0 >= slot1 || pc.slot0 + PC_TILE * pc.tiles <= slot0) continue;
+                    const PcWinRun &r = P.runs[pc.run];
+                    const int32_t d = slot0 - r.slot0;   // (what lies in front of a run is left out by its window)
+                    const int32_t j = pc.call - call0, q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)pc.call].call].q_off];
+                    PcWinSee e{r.pos0 + d, r.n_tok - d, std::max(0, r.sink > 0 ? r.sink - d : 0), win_low(q_pos, P.window), (int64_t)q_pos - r.rot_pos, j % per, 0};
+                    bool joined = false;
+                    for (auto &o : seen)
+                        if (o.first == j) {              // the sinks of an extent and its end; or a message that is listed twice
+                            if (o.second.pos0 != e.pos0 || o.second.turn != e.turn) return false;
+                            o.second.n_tok = std::max(o.second.n_tok, e.n_tok); o.second.sink = std::max(o.second.sink, e.sink);
+                            joined = true;
+                        }
+                    if (!joined) seen.push_back({j, e});
+                }
+                std::sort(seen.begin(), seen.end(), [](const auto &x, const auto &y) { return x.first < y.first; });
+                PcWinVisit pv{slot0, n, (int32_t)P.sh_sees.size(), {}};
+                size_t k = 0;
+                for (int32_t gr = 0; gr <= PC_WIN_GROUPS; ++gr) {
+                    while (k < seen.size() && seen[k].first / per < gr) ++k;
+                    pv.off[gr] = (int32_t)k;
+                }
+                for (const auto &o : seen) P.sh_sees.push_back(o.second);
+                P.sh_visits.push_back(pv);
+                left -= n; done += n;
+                if (done == v.tiles) { ++at; done = 0; }
+            }
+        }
+        for (int32_t j = call0; j < call0 + in_set; ++j) {
+            const WinCall &wc = P.calls[(size_t)dec[(size_t)j].call];
+            P.sh_calls.push_back(PcWinSharedCall{wc.q_off, (int32_t)P.part_rows});
+            P.merge.push_back(PcMergeRow{wc.q_off, (int32_t)P.part_rows, splits, 1});
+            P.part_rows += splits;
+        }
+    }
+    P.sh_wide = wide;
+    return true;
+}
+
 // the rows of a call that units [unit0, unit0 + n) of the bf16 kernels, or block unit0 of 32 columns of the fp32 kernels, hold
 void plan_items(const pc_cache *c, WinPlan &P, bool may_split)
 {
     const int g = c->g;
     P.pre.clear(); P.dec.clear(); P.runs.clear(); P.rots.clear(); P.merge.clear();
+    auto no_shared = [&] { P.sh_items.clear(); P.sh_visits.clear(); P.sh_sees.clear(); P.sh_calls.clear(); };
+    no_shared();
     P.part_rows = 0;
     for (Seg &s : P.segs) s.rot = -1;
     std::vector<Group> pre, dec;
@@ -152,10 +262,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split)
                 const int32_t tiles = add_runs(P, wc, row0, row1);
                 pre.push_back(Group{(int32_t)i, (int32_t)u, run0, tiles});
             }
-        } else if (wc.n_q == 1) {
-            const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, wc, 0, 1);
-            dec.push_back(Group{(int32_t)i, 0, run0, tiles});
-        } else {
+        } else if (wc.n_q > 1) {
             const int32_t n_units = (wc.n_q + 31) / 32 * g;
             int32_t b0 = -1, b1 = -1, run0 = 0, tiles = 0;
             for (int32_t u = 0; u < n_units; u += 4) {
@@ -170,11 +277,23 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split)
         }
     }
     make_items(c, P, pre, P.pre, 512, c->cfg.dtype == PC_F32 ? 4 : 6, may_split);
+    if (c->cfg.dtype == PC_F32) return;
+    const size_t runs = P.runs.size(), rots = P.rots.size(), merge = P.merge.size();
+    const int64_t part_rows = P.part_rows;
+    for (size_t i = 0; i < P.calls.size(); ++i) {
+        if (P.calls[i].n_q != 1) continue;
+        const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, P.calls[i], 0, 1);
+        dec.push_back(Group{(int32_t)i, 0, run0, tiles});
+    }
+    P.rots.resize(rots);                                 // (single tokens' kernels make their rotations themselves)
+    if (may_split && plan_shared(c, P, dec)) { P.runs.resize(runs); return; }
+    no_shared();
+    P.merge.resize(merge); P.part_rows = part_rows;
     make_items(c, P, dec, P.dec, 512, 8, may_split);
 }
 
 // lists as they are staged, then what the device makes of them
-struct WinLayout { size_t pre, dec, runs, merge, q_pos, rots, lists, rot_q, rot_run, part_o, part_ml, total; };
+struct WinLayout { size_t pre, dec, runs, merge, q_pos, rots, sh_items, sh_visits, sh_sees, sh_calls, lists, rot_q, rot_run, part_o, part_ml, total; };
 
 WinLayout lay_out(const pc_cache *c, const WinPlan &P)
 {
@@ -187,6 +306,10 @@ WinLayout lay_out(const pc_cache *c, const WinPlan &P)
     L.merge = take(sizeof(PcMergeRow) * P.merge.size());
     L.q_pos = take(sizeof(int32_t) * P.q_pos.size());
     L.rots = take(sizeof(int64_t) * P.rots.size());
+    L.sh_items = take(sizeof(PcWinSharedItem) * P.sh_items.size());
+    L.sh_visits = take(sizeof(PcWinVisit) * P.sh_visits.size());
+    L.sh_sees = take(sizeof(PcWinSee) * P.sh_sees.size());
+    L.sh_calls = take(sizeof(PcWinSharedCall) * P.sh_calls.size());
     L.lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = P.pre.empty() ? 0 : sizeof(float2) * (size_t)c->half;
@@ -202,6 +325,7 @@ void write_lists(const WinPlan &P, const WinLayout &L, char *to)
 {
     auto put = [&](size_t at, const auto &v) { if (!v.empty()) std::memcpy(to + at, v.data(), sizeof(v[0]) * v.size()); };
     put(L.pre, P.pre); put(L.dec, P.dec); put(L.runs, P.runs); put(L.merge, P.merge); put(L.q_pos, P.q_pos); put(L.rots, P.rots);
+    put(L.sh_items, P.sh_items); put(L.sh_visits, P.sh_visits); put(L.sh_sees, P.sh_sees); put(L.sh_calls, P.sh_calls);
 }
 
 // ---- the gradient -------------------------------------------------------------------------------------------------
@@ -440,7 +564,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     W.window = window;
     W.scale_log2 = c->scale * 1.4426950408889634f;
     // Lists in the arguments of the decode launch are read there; everything else reads them from the workspace.
-    const bool direct = in_args && P.pre.empty();
+    const bool direct = in_args && P.pre.empty() && P.sh_items.empty();
     if (!direct) {
         ProfScope ps(c, 1, st);
         if (recorded && !in_args) pc_launch_store_args(from, L.lists, ws, st);
@@ -463,6 +587,13 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         const PcWinDecode O{(int32_t)L.dec, (int32_t)L.runs, (int32_t)L.q_pos, direct && !P.merge.empty() ? (int32_t)(L.lists / 16) : 0, ws};
         static_assert(PC_ARG_BYTES / 16 <= 256, "a thread for every 16 bytes");
         pc_launch_win_decode_bf16(W, (int)P.dec.size(), direct ? &blob : nullptr, O, st);
+        PC_HIP(c, hipGetLastError());
+    }
+    if (!P.sh_items.empty()) {
+        ProfScope ps(c, 3, st);
+        const PcWinShared S{(const PcWinSharedItem *)(ws + L.sh_items), (const PcWinVisit *)(ws + L.sh_visits), (const PcWinSee *)(ws + L.sh_sees),
+                            (const PcWinSharedCall *)(ws + L.sh_calls), (int32_t)P.sh_items.size(), P.sh_wide};
+        pc_launch_win_shared_decode_bf16(W, S, st);
         PC_HIP(c, hipGetLastError());
     }
     if (!P.pre.empty()) {
