@@ -1,8 +1,8 @@
 // Single tokens of many calls that list the same messages, under a window, bf16 caches (gfx950).
 //
-// On its own every call reads all that it sees; here a workgroup takes a range of the tiles that any of up to 16 * 16 columns' calls
-// see, reads each once, and multiplies it with the queries of those that see it.  A wave holds the columns of one or two groups of 16
-// (as many calls as have 16 heads of the KV head together) and their sums for its whole life; what a call sees of a range of
+// On its own every call reads all that it sees; here a workgroup takes a range of the tiles that any of a set of calls (up to 256 columns)
+// see, reads each once, and multiplies it with the queries of those that see it.  A wave holds a group of 16 columns (as many
+// calls as have 16 heads of the KV head together) and their sums for its whole life; what a call sees of a range of
 // consecutive tiles (a visit) stands in a list, with the angle its queries are turned by.  What a workgroup has of a row is a split
 // of it.  Tiles come by direct loads, in a ring of four pairs.
 //
@@ -12,6 +12,7 @@
 #include "pc_mfma_common.h"
 
 #define TILE_BYTES 8192
+#define LAZY_LOG2 64.0f
 #define MFMA16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
 
 namespace {
@@ -41,22 +42,23 @@ __device__ __forceinline__ win_i32x4 listed4(const void *p) { return *reinterpre
 
 }  // namespace
 
-template <int C>
-__global__ __launch_bounds__(512, 2) void pc_win_shared_decode_bf16_kernel(PcWin W, PcWinShared S)
+template <int NW>
+__global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_kernel(PcWin W, PcWinShared S)
 {
-    constexpr int RING = 4, AHEAD = 3, SLOT = 4 * TILE_BYTES;        // a step: two tiles
+    constexpr int RING = 4, AHEAD = 3, SLOT = 4 * TILE_BYTES, LOADS = NW == 8 ? 4 : 2;        // a step: two tiles
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][SLOT];
-    __shared__ __attribute__((aligned(16))) float2 s_rot[8][PC_D / 2];
-    __shared__ int4 s_see[8][C][16];                     // what a column's call sees of the wave's visit: pos0, n_tok, sink, lo
+    __shared__ __attribute__((aligned(16))) float2 s_rot[NW][PC_D / 2];
+    __shared__ int4 s_see[NW][16];                       // what a column's call sees of the wave's visit: pos0, n_tok, sink, lo
     __shared__ double s_freq[PC_D / 2];
+    __shared__ int s_odd[RING];
 
     const int kh = blockIdx.x % W.n_kv_heads;
     const win_i32x4 i0 = listed4(S.items + blockIdx.x / W.n_kv_heads), i1 = listed4((const char *)(S.items + blockIdx.x / W.n_kv_heads) + 16);
-    const int visit0 = i0.x, n_tiles = i0.y, call0 = i0.z, n_calls = i0.w, lanes_of = i1.x, split0 = i1.y;
+    const int visit0 = i0.x, n_steps = i0.y, call0 = i0.z, n_calls = i0.w, lanes_of = i1.x, split0 = i1.y;
     const int g = W.n_q_heads / W.n_kv_heads, per = 16 / g;          // calls a group of columns
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int n = lane & 15, a = lane >> 4, sub = n / g;
-    const int my = wave % lanes_of, rep = wave / lanes_of, reps = 8 / lanes_of;       // its groups of columns; its share of the tiles
+    const int my = wave % lanes_of, rep = wave / lanes_of, reps = NW / lanes_of;       // its groups of columns; its share of the tiles
 
     const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * W.slots * (PC_D * 2);
     const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * W.slots * (PC_D * 2);
@@ -65,232 +67,238 @@ __global__ __launch_bounds__(512, 2) void pc_win_shared_decode_bf16_kernel(PcWin
     auto turn_of = [](int r) { return ((r & 3) << 2) | (r >> 3); };
 
     // the columns' queries, as they came: dims 32 ks + 8 a + 0..7, then 64 up
-    uint4 q[C][4];
     if (wave == 0) s_freq[lane] = W.inv_freq[lane];
-    bool real[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int call = (my * C + c) * per + sub;
-        real[c] = sub < per && call < n_calls;
-        const int row = S.calls[call0 + (real[c] ? call : 0)].row;
+    const int call = my * per + sub;
+    const bool real = sub < per && call < n_calls;
+    uint4 q[4];
+    {
+        const int row = S.calls[call0 + (real ? call : 0)].row;
         const unsigned char *qp = (const unsigned char *)W.q + ((int64_t)row * W.n_q_heads + kh * g + n % g) * (PC_D * 2) + 16 * a;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) q[c][ks] = real[c] ? ldg16(qp + 64 * ks) : make_uint4(0, 0, 0, 0);
+        for (int ks = 0; ks < 4; ++ks) q[ks] = real ? ldg16(qp + 64 * ks) : make_uint4(0, 0, 0, 0);
     }
     // (they are here before the first direct load is asked for: the compiler's wait for them would be one for all of those)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(q[ks].x), "+v"(q[ks].y), "+v"(q[ks].z), "+v"(q[ks].w));
     __syncthreads();
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(q[c][ks].x), "+v"(q[c][ks].y), "+v"(q[c][ks].z), "+v"(q[c][ks].w));
 
-    const int n_steps = (n_tiles + 1) / 2;
     int to_visit = visit0, to_tile = 0, to_asked = 0, to_slot = 0, to_has = 0;
-    if (n_tiles > 0) { to_slot = listed(&S.visits[visit0].slot0); to_has = listed(&S.visits[visit0].n_tiles); }
+    if (n_steps > 0) { to_slot = listed(&S.visits[visit0].slot0); to_has = listed(&S.visits[visit0].n_tiles); }
     auto request = [&](int place) __attribute__((always_inline)) {
-        const int l = lane_again(), k_row = 4 * wave + (l >> 4);
-        const unsigned k_src = (unsigned)(k_row * 256 + (((l & 15) ^ turn_of(k_row)) << 4)), v_src = (unsigned)(wave * 1024 + l * 16);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (to_asked > 0 && to_asked < n_tiles) {    // (behind the last tile: it again, so that every step is four loads)
-                if (++to_tile == to_has) {
-                    ++to_visit; to_tile = 0;
-                    to_slot = listed(&S.visits[to_visit].slot0); to_has = listed(&S.visits[to_visit].n_tiles);
-                }
+        // (a tile's K and V are eight pieces each)
+        const int l = lane_again(), piece = wave % 8, k_row = 4 * piece + (l >> 4);
+        const unsigned k_src = (unsigned)(k_row * 256 + (((l & 15) ^ turn_of(k_row)) << 4)), v_src = (unsigned)(piece * 1024 + l * 16);
+        if (to_asked > 0) {
+            to_tile += 2;
+            if (to_tile >= to_has) {
+                ++to_visit; to_tile = 0;
+                to_slot = listed(&S.visits[to_visit].slot0); to_has = listed(&S.visits[to_visit].n_tiles);
             }
-            ++to_asked;
-            const int64_t at = ((int64_t)to_slot + PC_TILE * to_tile) * (PC_D * 2);
-            const unsigned to = ring + place * SLOT + half * 2 * TILE_BYTES + wave * 1024;
-            dma16(kb + at, k_src, to);
-            dma16(vb + at, v_src, to + TILE_BYTES);
+        }
+        ++to_asked;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {           // (behind a visit's last tile: it again, so that every step is as many loads)
+            const int64_t at = ((int64_t)to_slot + PC_TILE * min(to_tile + half, to_has - 1)) * (PC_D * 2);
+            const unsigned to = ring + place * SLOT + half * 2 * TILE_BYTES + piece * 1024;
+            if (NW == 8 || wave < 8) dma16(kb + at, k_src, to);
+            if (NW == 8 || wave >= 8) dma16(vb + at, v_src, to + TILE_BYTES);
         }
     };
+    // Whether a step's values are all finite: every wave looks at its piece of them a step ahead (s_odd: of a place in the ring,
+    // cleared two steps ahead).
+    auto look = [&](int place) __attribute__((always_inline)) {
+        const int l = lane_again();
+        win_i32x4 odd = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 16 / NW; ++i) {
+            const int piece = wave + NW * i;             // 16 pieces: the values of two tiles
+            const win_i32x4 w = *(lds16)(uintptr_t)(ring + place * SLOT + (piece >> 3) * 2 * TILE_BYTES + TILE_BYTES + (piece & 7) * 1024 + l * 16);
+            // a bf16 whose exponent is all ones carries into the bit above it when one is added to the exponent
+            odd |= ((w & 0x7F807F80) + 0x00800080) & (int)0x80008000;
+        }
+        const int any = odd.x | odd.y | odd.z | odd.w;
+        if (__builtin_amdgcn_ballot_w64(any != 0) != 0 && l == 0) s_odd[place] = 1;
+        if (wave == 0 && l == 1) s_odd[(place + 1) & (RING - 1)] = 0;
+    };
+    if (wave == 0 && lane < RING) s_odd[lane] = 0;
     for (int i = 0; i < min(AHEAD, n_steps); ++i) request(i);
+    if (n_steps >= AHEAD) wait_vm<LOADS * (AHEAD - 1)>();
+    else wait_vm<0>();
+    __syncthreads();
+    if (n_steps > 0) look(0);
 
-    float m_run[C], l_run[C];
-    f32x4 acc[C][8];
-    bf16x8 qop[C][4];                                    // turned and scaled
-    int listers[C];                                      // entries of the group (uniform)
+    float m_ref = -INFINITY;
+    f32x4 sums = {0.f, 0.f, 0.f, 0.f};                   // of the column's probabilities (four times the same)
+    f32x4 acc[8];
+    bf16x8 qop[4];                                       // turned and scaled
+    int listers = 0;                                     // entries of the group
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        m_run[c] = -INFINITY; l_run[c] = 0.f; listers[c] = 0;
+    for (int db = 0; db < 8; ++db) acc[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int db = 0; db < 8; ++db) acc[c][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) qop[c][ks] = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
-    }
-    int visit = visit0 - 1, tile = 0, has = 0;           // the walk of what is computed
+    for (int ks = 0; ks < 4; ++ks) qop[ks] = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
+    int visit = visit0 - 1, tile = 0, has = 0;           // the walk of what is computed: two tiles of a visit a step
 #pragma unroll 1
     for (int step = 0, place = 0; step < n_steps; ++step, place = (place + 1) & (RING - 1)) {
-        if (step + AHEAD <= n_steps) wait_vm<4 * (AHEAD - 1)>();
+        if (step + AHEAD <= n_steps) wait_vm<LOADS * (AHEAD - 2)>();
         else wait_vm<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         ring_barrier();
-        if (step + AHEAD < n_steps) request((place + AHEAD) & (RING - 1));
+        tile += 2;
+        if (tile >= has) {
+            ++visit; tile = 0;
+            has = listed(&S.visits[visit].n_tiles);
+            const int e0 = listed(&S.visits[visit].e0);
+            const int first = listed(&S.visits[visit].off[my]), end = listed(&S.visits[visit].off[my + 1]);
+            listers = end - first;
+            asm volatile("" ::: "memory");       // (a wave's own LDS accesses happen in order)
+            if (a == 0) s_see[wave][n] = make_int4(0, 0, 0, 0);
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-            const int t = 2 * step + half;
-            if (t >= n_tiles) break;
-            if (++tile >= has) {
-                ++visit; tile = 0;
-                has = listed(&S.visits[visit].n_tiles);
-                const int e0 = listed(&S.visits[visit].e0);
+            for (int e = first; e < end; ++e) {
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const int first = listed(&S.visits[visit].off[my * C + c]), end = listed(&S.visits[visit].off[my * C + c + 1]);
-                    listers[c] = end - first;
-                    asm volatile("" ::: "memory");       // (a wave's own LDS accesses happen in order)
-                    if (a == 0) s_see[wave][c][n] = make_int4(0, 0, 0, 0);
-#pragma unroll 1
-                    for (int e = first; e < end; ++e) {
+                for (int ks = 0; ks < 4; ++ks)   // (its 32 numbers, taken apart once and kept, would not fit the registers)
+                    asm volatile("" : "+v"(q[ks].x), "+v"(q[ks].y), "+v"(q[ks].z), "+v"(q[ks].w));
+                const win_i32x4 x = listed4(S.sees + e0 + e), y = listed4((const char *)(S.sees + e0 + e) + 16);
+                const bool mine = sub == y.z;
+                if (mine && a == 0) s_see[wave][n] = make_int4(x.x, x.y, x.z, x.w);
+                const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y.y << 32) | (uint32_t)y.x);
+                const float2 cs = rope_angle((double)turn * s_freq[lane]);
+                asm volatile("" ::: "memory");
+                s_rot[wave][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
+                asm volatile("" ::: "memory");
 #pragma unroll
-                        for (int ks = 0; ks < 4; ++ks)   // (its 32 numbers, taken apart once and kept, would not fit the registers)
-                            asm volatile("" : "+v"(q[c][ks].x), "+v"(q[c][ks].y), "+v"(q[c][ks].z), "+v"(q[c][ks].w));
-                        const win_i32x4 x = listed4(S.sees + e0 + e), y = listed4((const char *)(S.sees + e0 + e) + 16);
-                        const bool mine = sub == y.z;
-                        if (mine && a == 0) s_see[wave][c][n] = make_int4(x.x, x.y, x.z, x.w);
-                        const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y.y << 32) | (uint32_t)y.x);
-                        const float2 cs = rope_angle((double)turn * s_freq[lane]);
-                        asm volatile("" ::: "memory");
-                        s_rot[wave][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
-                        asm volatile("" ::: "memory");
+                for (int ks = 0; ks < 2; ++ks) {
+                    const uint32_t lw[4] = {q[ks].x, q[ks].y, q[ks].z, q[ks].w}, hw[4] = {q[ks + 2].x, q[ks + 2].y, q[ks + 2].z, q[ks + 2].w};
+                    uint4 was[2] = {__builtin_bit_cast(uint4, qop[ks]), __builtin_bit_cast(uint4, qop[ks + 2])};
+                    uint32_t xo[4] = {was[0].x, was[0].y, was[0].z, was[0].w}, yo[4] = {was[1].x, was[1].y, was[1].z, was[1].w};
 #pragma unroll
-                        for (int ks = 0; ks < 2; ++ks) {
-                            const uint32_t lw[4] = {q[c][ks].x, q[c][ks].y, q[c][ks].z, q[c][ks].w}, hw[4] = {q[c][ks + 2].x, q[c][ks + 2].y, q[c][ks + 2].z, q[c][ks + 2].w};
-                            uint4 was[2] = {__builtin_bit_cast(uint4, qop[c][ks]), __builtin_bit_cast(uint4, qop[c][ks + 2])};
-                            uint32_t xo[4] = {was[0].x, was[0].y, was[0].z, was[0].w}, yo[4] = {was[1].x, was[1].y, was[1].z, was[1].w};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float4 r = *reinterpret_cast<const float4 *>(&s_rot[wave][32 * ks + 8 * a + 2 * j]);
-                                const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
-                                const uint32_t px = pack_bf16(x0 * r.x - y0 * r.y, x1 * r.z - y1 * r.w), py = pack_bf16(x0 * r.y + y0 * r.x, x1 * r.w + y1 * r.z);
-                                xo[j] = mine ? px : xo[j]; yo[j] = mine ? py : yo[j];
-                            }
-                            qop[c][ks] = __builtin_bit_cast(bf16x8, make_uint4(xo[0], xo[1], xo[2], xo[3]));
-                            qop[c][ks + 2] = __builtin_bit_cast(bf16x8, make_uint4(yo[0], yo[1], yo[2], yo[3]));
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 r = *reinterpret_cast<const float4 *>(&s_rot[wave][32 * ks + 8 * a + 2 * j]);
+                        const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
+                        const uint32_t px = pack_bf16(x0 * r.x - y0 * r.y, x1 * r.z - y1 * r.w), py = pack_bf16(x0 * r.y + y0 * r.x, x1 * r.w + y1 * r.z);
+                        xo[j] = mine ? px : xo[j]; yo[j] = mine ? py : yo[j];
                     }
+                    qop[ks] = __builtin_bit_cast(bf16x8, make_uint4(xo[0], xo[1], xo[2], xo[3]));
+                    qop[ks + 2] = __builtin_bit_cast(bf16x8, make_uint4(yo[0], yo[1], yo[2], yo[3]));
                 }
             }
-            if (t % reps != rep) continue;
-            uint32_t sees[C];
-            bool some[C], any = false;
+        }
+        uint32_t sees[2] = {0, 0};
+        if (listers > 0 && (reps == 1 || step % reps == rep)) {
+            auto first = [](unsigned k) { return k >= 32u ? ~0u : (1u << k) - 1u; };
+            asm volatile("" ::: "memory");
+            const int4 w = s_see[wave][n];
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                auto first = [](unsigned k) { return k >= 32u ? ~0u : (1u << k) - 1u; };
-                if (listers[c] == 0) { sees[c] = 0; some[c] = false; continue; }
-                asm volatile("" ::: "memory");
-                const int4 w = s_see[wave][c][n];
-                const int p = w.x + PC_TILE * tile;
+            for (int half = 0; half < 2; ++half) {
+                const int skip = PC_TILE * (tile + half), p = w.x + skip;
                 const unsigned below = w.w <= p ? 0u : (unsigned)w.w - (unsigned)p;
-                sees[c] = first((unsigned)max(w.y - PC_TILE * tile, 0)) & (~first(below) | first((unsigned)max(w.z - PC_TILE * tile, 0)));
-                some[c] = __builtin_amdgcn_ballot_w64(sees[c] != 0) != 0;
-                any |= some[c];
+                sees[half] = first((unsigned)max(w.y - skip, 0)) & (~first(below) | first((unsigned)max(w.z - skip, 0)));
             }
-            if (!any) continue;
-            const unsigned kt = ring + place * SLOT + half * 2 * TILE_BYTES, vt = kt + TILE_BYTES;
-            f32x4 s[C][2];
+            if (tile + 1 >= has) sees[1] = 0;
+        }
+        if (__builtin_amdgcn_ballot_w64((sees[0] | sees[1]) != 0) != 0) {
+            const unsigned kt = ring + place * SLOT;
+            float sc[16];                                    // keys 32 half + 8 a + 0..7 of column n
             {
-                win_i32x4 k[2][4];
                 // (chunk a + 4 ks of a key stands where (a ^ turn) ^ 4 ks says)
                 const int l = lane_again(), r = 8 * ((l & 15) >> 2) + (l & 3);
                 const unsigned at = (unsigned)(r * 256 + (((l >> 4) ^ turn_of(r)) << 4));
 #pragma unroll
-                for (int tau = 0; tau < 2; ++tau) {
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) k[tau][ks] = *(lds16)(uintptr_t)(kt + (at ^ (ks << 6)) + tau * 1024);
-                }
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    if (!some[c]) continue;
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
                     for (int tau = 0; tau < 2; ++tau) {
-                        s[c][tau] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                        f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int ks = 0; ks < 4; ++ks) s[c][tau] = MFMA16(__builtin_bit_cast(bf16x8, k[tau][ks]), qop[c][ks], s[c][tau]);
+                        for (int ks = 0; ks < 4; ++ks)
+                            s = MFMA16(__builtin_bit_cast(bf16x8, *(lds16)(uintptr_t)(kt + half * 2 * TILE_BYTES + (at ^ (ks << 6)) + tau * 1024)), qop[ks], s);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sc[8 * half + 4 * tau + j] = s[j];
                     }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const bool whole = (sees[0] & sees[1]) == ~0u;
+            if (__builtin_amdgcn_ballot_w64((sees[0] | sees[1]) != 0 && !whole) == 0) {       // (all or nothing)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sc[j] = whole ? sc[j] : -INFINITY;
+            } else {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t mine = sees[half] >> (8 * a);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sc[8 * half + j] = (mine >> j) & 1 ? sc[8 * half + j] : -INFINITY;
                 }
             }
+            float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                __builtin_amdgcn_sched_barrier(0);
-                if (!some[c]) continue;
-                const int l = lane_again();
-                const unsigned v_at = (unsigned)(((l >> 4) * PC_D + (l & 15)) * 16);
-                win_i32x4 v[8];                          // (read again for the second group: registers)
-#pragma unroll
-                for (int db = 0; db < 8; ++db) v[db] = *(lds16)(uintptr_t)(vt + v_at + 256 * db);
-                const uint32_t mine = sees[c] >> (8 * a);
-                float sc[8];                             // keys 8 a + 0..7 of column n
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sc[j] = (mine >> j) & 1 ? s[c][j >> 2][j & 3] : -INFINITY;
-                float mx = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
+            for (int j = 4; j < 16; j += 4) mx = fmaxf(mx, fmaxf(fmaxf(sc[j], sc[j + 1]), fmaxf(sc[j + 2], sc[j + 3])));
+            // The reference of a column's exponents moves only where a score is 2^LAZY above it (a column's first always is): probabilities
+            // up to that are as exact, and the lanes of a column need not agree on a maximum step by step.
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_ref + LAZY_LOG2) != 0, 0)) {
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float m_new = fmaxf(m_run[c], mx), m_safe = m_new == -INFINITY ? 0.f : m_new, alpha = m_run[c] == m_new ? 1.f : ex2(m_run[c] - m_safe);
-                uint32_t pk[4];
-                float ps = 0.f;                          // (of the probabilities as the products take them: their rounding cancels)
+                const float m_new = mx > m_ref + LAZY_LOG2 ? mx : m_ref, f = m_new == m_ref ? 1.f : ex2(m_ref - m_new);
+                m_ref = m_new;
+                sums *= f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    pk[j] = pack_bf16(ex2(sc[2 * j] - m_safe), ex2(sc[2 * j + 1] - m_safe));
-                    ps += bf_lo(pk[j]) + bf_hi(pk[j]);
-                }
-                l_run[c] = l_run[c] * alpha + ps;
-                m_run[c] = m_new;
-                if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {       // rare once the running maxima have settled
+                for (int db = 0; db < 8; ++db) acc[db] *= f;
+            }
+            const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+            uint32_t pk[8];
 #pragma unroll
-                    for (int db = 0; db < 8; ++db) acc[c][db] *= alpha;
-                }
-                const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
-                const bool whole = sees[c] == ~0u;
-                if (__builtin_amdgcn_ballot_w64(real[c] && !whole) == 0) {
+            for (int j = 0; j < 8; ++j) pk[j] = pack_bf16(ex2(sc[2 * j] - ref), ex2(sc[2 * j + 1] - ref));
+            const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
+            // (the denominator: of the probabilities as the products take them, so that their rounding cancels)
+            const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+            sums = MFMA16(ones, p[0], sums);
+            sums = MFMA16(ones, p[1], sums);
+            __builtin_amdgcn_sched_barrier(0);               // (values read any earlier would not fit the registers)
+            const int lv = lane_again();
+            const unsigned vt = kt + TILE_BYTES + (unsigned)(((lv >> 4) * PC_D + (lv & 15)) * 16);
+            auto value = [&](int half, int db) __attribute__((always_inline)) { return *(lds16)(uintptr_t)(vt + half * 2 * TILE_BYTES + 256 * db); };
+            if (__builtin_expect(uniform(s_odd[place]) == 0, 1)) {
 #pragma unroll
-                    for (int db = 0; db < 8; ++db) acc[c][db] = MFMA16(__builtin_bit_cast(bf16x8, v[db]), p, acc[c][db]);
-                } else if (__builtin_amdgcn_ballot_w64(sees[c] != 0 && !whole) == 0) {
-                    // columns that see nothing of the tile keep what they have: a value need not be finite, and 0 times it would not be 0
+                for (int db = 0; db < 8; ++db)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) acc[db] = MFMA16(__builtin_bit_cast(bf16x8, value(half, db)), p[half], acc[db]);
+            } else {
+                // A value that is not finite: 0 times it would not be 0.  A call at a time, the values of keys that it does not see cleared,
+                // and the other columns keep what they have.
+#pragma unroll 1
+                for (int i = 0; i < per; ++i) {
+                    win_i32x4 keep[2];
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)sees[half], i * g), part = its >> (8 * a);
+                        any |= its;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) keep[half][j] = (int)(((part >> (2 * j)) & 1 ? 0xFFFFu : 0u) | ((part >> (2 * j + 1)) & 1 ? 0xFFFF0000u : 0u));
+                    }
+                    if (any == 0) continue;
 #pragma unroll
                     for (int db = 0; db < 8; ++db) {
-                        const f32x4 was = acc[c][db], x = MFMA16(__builtin_bit_cast(bf16x8, v[db]), p, was);
+                        const f32x4 was = acc[db], x = MFMA16(__builtin_bit_cast(bf16x8, value(1, db) & keep[1]), p[1], MFMA16(__builtin_bit_cast(bf16x8, value(0, db) & keep[0]), p[0], was));
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[c][db][j] = whole ? x[j] : was[j];
-                    }
-                } else {
-                    // a call at a time, the values of keys that it does not see cleared
-#pragma unroll 1
-                    for (int i = 0; i < per; ++i) {
-                        const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)sees[c], i * g);
-                        if (its == 0) continue;
-                        const uint32_t part = its >> (8 * a);
-                        win_i32x4 keep;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) keep[j] = (int)( ((part >> (2 * j)) & 1 ? 0xFFFFu : 0u) | ((part >> (2 * j + 1)) & 1 ? 0xFFFF0000u : 0u));
-#pragma unroll
-                        for (int db = 0; db < 8; ++db) {
-                            const f32x4 was = acc[c][db], x = MFMA16(__builtin_bit_cast(bf16x8, v[db] & keep), p, was);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[c][db][j] = sub == i ? x[j] : was[j];
-                        }
+                        for (int j = 0; j < 4; ++j) acc[db][j] = sub == i ? x[j] : was[j];
                     }
                 }
             }
         }
+        // (what is asked for and looked at for later steps comes behind this step's products: the waves that have none are at it meanwhile)
+        if (step + AHEAD < n_steps) request((place + AHEAD) & (RING - 1));
+        if (step + 1 < n_steps) look((place + 1) & (RING - 1));
     }
+    if (!real) return;
+    const int64_t at = ((int64_t)S.calls[call0 + call].part0 + split0 + rep) * W.n_q_heads + kh * g + n % g;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        l_run[c] += __shfl_xor(l_run[c], 16);
-        l_run[c] += __shfl_xor(l_run[c], 32);
-        if (!real[c]) continue;
-        const int64_t at = ((int64_t)S.calls[call0 + (my * C + c) * per + sub].part0 + split0 + rep) * W.n_q_heads + kh * g + n % g;
-#pragma unroll
-        for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(W.part_o + at * PC_D + 16 * db + 4 * a) = acc[c][db];
-        if (a == 0) *reinterpret_cast<float2 *>(W.part_ml + at * 2) = make_float2(l_run[c] == 0.f ? -INFINITY : m_run[c], l_run[c]);
-    }
+    for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(W.part_o + at * PC_D + 16 * db + 4 * a) = acc[db];
+    if (a == 0) *reinterpret_cast<float2 *>(W.part_ml + at * 2) = make_float2(sums[0] == 0.f ? -INFINITY : m_ref, sums[0]);
 }
 
 void pc_launch_win_shared_decode_bf16(const PcWin &W, const PcWinShared &S, hipStream_t st)
 {
     if (S.n_items <= 0) return;
     const unsigned grid = (unsigned)S.n_items * W.n_kv_heads;
-    if (S.wide) pc_win_shared_decode_bf16_kernel<2><<<grid, 512, 0, st>>>(W, S);
-    else pc_win_shared_decode_bf16_kernel<1><<<grid, 512, 0, st>>>(W, S);
+    if (S.wide) pc_win_shared_decode_bf16_kernel<16><<<grid, 1024, 0, st>>>(W, S);
+    else pc_win_shared_decode_bf16_kernel<8><<<grid, 512, 0, st>>>(W, S);
 }

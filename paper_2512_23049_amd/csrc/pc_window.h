@@ -67,9 +67,9 @@ struct PcWinSee {             // a call's view of a visit
     int32_t pad;
 };
 struct PcWinSharedItem {      // one workgroup's tiles, for each KV head
-    int32_t visit0, n_tiles;
+    int32_t visit0, n_steps;  // (a step: two tiles of a visit)
     int32_t call0, n_calls;   // its set of calls
-    int32_t waves;            // that hold all groups of columns (a power of two); the others take every second, fourth.. tile
+    int32_t waves;            // that hold all groups of columns (a power of two); the others share its steps
     int32_t split0;
     int32_t pad[2];
 };
@@ -80,7 +80,7 @@ struct PcWinShared {
     const PcWinSee        *sees;
     const PcWinSharedCall *calls;
     int32_t n_items;
-    int32_t wide;             // 1: two groups of columns a wave
+    int32_t wide;             // 1: 16 waves (groups of columns) a workgroup, 0: 8
 };
 
 // ---- the gradient ----

@@ -147,7 +147,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
 {
     const int H = c->cfg.n_kv_heads, g = c->g, per = 16 / g;
     const int32_t n_calls = (int32_t)dec.size(), n_groups = (n_calls + per - 1) / per;
-    if (n_groups < 3) return false;                      // (waves without columns would have every fourth tile at most)
+    if (n_groups < 3) return false;                      // (waves without columns would have every fourth step at most)
     const bool wide = n_groups > PC_WIN_GROUPS / 2;
     const int32_t set_calls = std::min(n_groups, wide ? PC_WIN_GROUPS : PC_WIN_GROUPS / 2) * per, n_sets = (n_calls + set_calls - 1) / set_calls;
     struct Piece { int32_t slot0, tiles; size_t run; int32_t call; };
@@ -173,13 +173,14 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
         }
         of_set.push_back({first, pieces.size()});
     }
-    // What both ways read and write, in tiles: a workgroup's partial rows are worth 8 (16 with two groups a wave).
+    // What both ways read and write, in tiles: a workgroup's partial rows are worth 8 (16 with 16 waves).
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
     if (own * 2 < 3 * (shared + bins * n_sets * (wide ? 16 : 8))) return false;
     for (int32_t s = 0; s < n_sets; ++s) {
         const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
         int32_t waves = 1;
-        while (waves * (wide ? 2 : 1) < groups) waves *= 2;
+        while (waves < groups) waves *= 2;
+        const int32_t reps = (wide ? 16 : 8) / waves;
         // ranges of consecutive tiles
         struct Visit { int32_t slot0, tiles; size_t p0, p1; };
         std::vector<Visit> visits;
@@ -193,12 +194,12 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
             k = v.p1;
         }
         const int64_t n_bins = std::max<int64_t>(1, std::min(bins, total));
-        const int32_t splits = (int32_t)n_bins * (8 / waves);
+        const int32_t splits = (int32_t)n_bins * reps;
         size_t at = 0;
         int32_t done = 0;                                // tiles of visits[at] that earlier workgroups have
         for (int64_t b = 0; b < n_bins; ++b) {
             int32_t left = (int32_t)(total * (b + 1) / n_bins - total * b / n_bins);
-            P.sh_items.push_back(PcWinSharedItem{(int32_t)P.sh_visits.size(), left, call0, in_set, waves, (int32_t)b * (8 / waves), {0, 0}});
+            P.sh_items.push_back(PcWinSharedItem{(int32_t)P.sh_visits.size(), 0, call0, in_set, waves, (int32_t)b * reps, {0, 0}});
             while (left > 0) {
                 const Visit &v = visits[at];
                 const int32_t n = std::min(left, v.tiles - done), slot0 = v.slot0 + PC_TILE * done, slot1 = slot0 + PC_TILE * n;
@@ -228,6 +229,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                 }
                 for (const auto &o : seen) P.sh_sees.push_back(o.second);
                 P.sh_visits.push_back(pv);
+                P.sh_items.back().n_steps += (n + 1) / 2;
                 left -= n; done += n;
                 if (done == v.tiles) { ++at; done = 0; }
             }
