@@ -4,7 +4,8 @@
 // see, reads each once, and multiplies it with the queries of those that see it.  A wave holds a group of 16 columns (as many
 // calls as have 16 heads of the KV head together) and their sums for its whole life; what a call sees of a range of
 // consecutive tiles (a visit) stands in a list, with the angle its queries are turned by.  What a workgroup has of a row is a split
-// of it.  Tiles come by direct loads, in a ring of four pairs.
+// of it.  Tiles come by direct loads, in a ring of
+// three steps.
 //
 // What bounds it is the memory behind the caches as long as several calls see a tile: 32 calls of 8 heads a KV head over 410 of 512
 // messages each, window 16 384: see the launch below.
@@ -45,20 +46,20 @@ __device__ __forceinline__ win_i32x4 listed4(const void *p) { return *reinterpre
 template <int NW>
 __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_kernel(PcWin W, PcWinShared S)
 {
-    constexpr int RING = 4, AHEAD = 3, SLOT = 4 * TILE_BYTES, LOADS = NW == 8 ? 4 : 2;        // a step: two tiles
+    constexpr int TILES = PC_WIN_STEP_TILES, RING = TILES == 2 ? 4 : 3, AHEAD = RING - 1, SLOT = 2 * TILES * TILE_BYTES, LOADS = 16 / NW * TILES;
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][SLOT];
     __shared__ __attribute__((aligned(16))) float2 s_rot[NW][PC_D / 2];
     __shared__ int4 s_see[NW][16];                       // what a column's call sees of the wave's visit: pos0, n_tok, sink, lo
     __shared__ double s_freq[PC_D / 2];
-    __shared__ int s_odd[RING];
+    __shared__ int s_odd[RING];                          // of a place in the ring: a value is not finite
 
     const int kh = blockIdx.x % W.n_kv_heads;
     const win_i32x4 i0 = listed4(S.items + blockIdx.x / W.n_kv_heads), i1 = listed4((const char *)(S.items + blockIdx.x / W.n_kv_heads) + 16);
-    const int visit0 = i0.x, n_steps = i0.y, call0 = i0.z, n_calls = i0.w, lanes_of = i1.x, split0 = i1.y;
+    const int visit0 = i0.x, n_steps = i0.y, call0 = i0.z, n_calls = i0.w, waves = i1.x, split0 = i1.y;
     const int g = W.n_q_heads / W.n_kv_heads, per = 16 / g;          // calls a group of columns
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int n = lane & 15, a = lane >> 4, sub = n / g;
-    const int my = wave % lanes_of, rep = wave / lanes_of, reps = NW / lanes_of;       // its groups of columns; its share of the tiles
+    const int my = wave % waves, rep = wave / waves, reps = NW / waves;      // its group of columns; its share of the steps
 
     const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * W.slots * (PC_D * 2);
     const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * W.slots * (PC_D * 2);
@@ -67,7 +68,6 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
     auto turn_of = [](int r) { return ((r & 3) << 2) | (r >> 3); };
 
     // the columns' queries, as they came: dims 32 ks + 8 a + 0..7, then 64 up
-    if (wave == 0) s_freq[lane] = W.inv_freq[lane];
     const int call = my * per + sub;
     const bool real = sub < per && call < n_calls;
     uint4 q[4];
@@ -77,7 +77,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) q[ks] = real ? ldg16(qp + 64 * ks) : make_uint4(0, 0, 0, 0);
     }
-    // (they are here before the first direct load is asked for: the compiler's wait for them would be one for all of those)
+    if (wave == 0) s_freq[lane] = W.inv_freq[lane];
+    if (wave == 0 && lane < RING) s_odd[lane] = 0;
+    // (all of it is here before the first direct load is asked for: the compiler's wait would be one for all of those)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(q[ks].x), "+v"(q[ks].y), "+v"(q[ks].z), "+v"(q[ks].w));
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
         const int l = lane_again(), piece = wave % 8, k_row = 4 * piece + (l >> 4);
         const unsigned k_src = (unsigned)(k_row * 256 + (((l & 15) ^ turn_of(k_row)) << 4)), v_src = (unsigned)(piece * 1024 + l * 16);
         if (to_asked > 0) {
-            to_tile += 2;
+            to_tile += TILES;
             if (to_tile >= to_has) {
                 ++to_visit; to_tile = 0;
                 to_slot = listed(&S.visits[to_visit].slot0); to_has = listed(&S.visits[to_visit].n_tiles);
@@ -98,35 +100,27 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
         }
         ++to_asked;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {           // (behind a visit's last tile: it again, so that every step is as many loads)
-            const int64_t at = ((int64_t)to_slot + PC_TILE * min(to_tile + half, to_has - 1)) * (PC_D * 2);
-            const unsigned to = ring + place * SLOT + half * 2 * TILE_BYTES + piece * 1024;
+        for (int t = 0; t < TILES; ++t) {                // (behind a visit's last tile: it again, so that every step is as many loads)
+            const int64_t at = ((int64_t)to_slot + PC_TILE * min(to_tile + t, to_has - 1)) * (PC_D * 2);
+            const unsigned to = ring + place * SLOT + t * 2 * TILE_BYTES + piece * 1024;
             if (NW == 8 || wave < 8) dma16(kb + at, k_src, to);
             if (NW == 8 || wave >= 8) dma16(vb + at, v_src, to + TILE_BYTES);
         }
     };
-    // Whether a step's values are all finite: every wave looks at its piece of them a step ahead (s_odd: of a place in the ring,
-    // cleared two steps ahead).
+    // whether a step's values are all finite: who asked for a piece of them looks at it once it is here
     auto look = [&](int place) __attribute__((always_inline)) {
+        if (NW == 16 && wave < 8) return;
         const int l = lane_again();
         win_i32x4 odd = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 16 / NW; ++i) {
-            const int piece = wave + NW * i;             // 16 pieces: the values of two tiles
-            const win_i32x4 w = *(lds16)(uintptr_t)(ring + place * SLOT + (piece >> 3) * 2 * TILE_BYTES + TILE_BYTES + (piece & 7) * 1024 + l * 16);
+        for (int t = 0; t < TILES; ++t) {
+            const win_i32x4 w = *(lds16)(uintptr_t)(ring + place * SLOT + t * 2 * TILE_BYTES + TILE_BYTES + (wave & 7) * 1024 + l * 16);
             // a bf16 whose exponent is all ones carries into the bit above it when one is added to the exponent
             odd |= ((w & 0x7F807F80) + 0x00800080) & (int)0x80008000;
         }
-        const int any = odd.x | odd.y | odd.z | odd.w;
-        if (__builtin_amdgcn_ballot_w64(any != 0) != 0 && l == 0) s_odd[place] = 1;
-        if (wave == 0 && l == 1) s_odd[(place + 1) & (RING - 1)] = 0;
+        if (__builtin_amdgcn_ballot_w64((odd.x | odd.y | odd.z | odd.w) != 0) != 0 && l == 0) s_odd[place] = 1;
     };
-    if (wave == 0 && lane < RING) s_odd[lane] = 0;
     for (int i = 0; i < min(AHEAD, n_steps); ++i) request(i);
-    if (n_steps >= AHEAD) wait_vm<LOADS * (AHEAD - 1)>();
-    else wait_vm<0>();
-    __syncthreads();
-    if (n_steps > 0) look(0);
 
     float m_ref = -INFINITY;
     f32x4 sums = {0.f, 0.f, 0.f, 0.f};                   // of the column's probabilities (four times the same)
@@ -137,26 +131,29 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
     for (int db = 0; db < 8; ++db) acc[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) qop[ks] = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
-    int visit = visit0 - 1, tile = 0, has = 0;           // the walk of what is computed: two tiles of a visit a step
+    int visit = visit0 - 1, tile = 0, has = 0;           // the walk of what is computed
 #pragma unroll 1
-    for (int step = 0, place = 0; step < n_steps; ++step, place = (place + 1) & (RING - 1)) {
-        if (step + AHEAD <= n_steps) wait_vm<LOADS * (AHEAD - 2)>();
+    for (int step = 0, place = 0; step < n_steps; ++step, place = place == RING - 1 ? 0 : place + 1) {
+        if (step + AHEAD <= n_steps) wait_vm<LOADS * (AHEAD - 1)>();
         else wait_vm<0>();
+        look(place);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         ring_barrier();
-        tile += 2;
+        const int before = place == 0 ? RING - 1 : place - 1;            // (free: the next but one step's)
+        if (wave == 0 && lane_again() == 0) s_odd[before] = 0;
+        tile += TILES;
         if (tile >= has) {
             ++visit; tile = 0;
             has = listed(&S.visits[visit].n_tiles);
             const int e0 = listed(&S.visits[visit].e0);
             const int first = listed(&S.visits[visit].off[my]), end = listed(&S.visits[visit].off[my + 1]);
             listers = end - first;
-            asm volatile("" ::: "memory");       // (a wave's own LDS accesses happen in order)
+            asm volatile("" ::: "memory");               // (a wave's own LDS accesses happen in order)
             if (a == 0) s_see[wave][n] = make_int4(0, 0, 0, 0);
 #pragma unroll 1
             for (int e = first; e < end; ++e) {
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)   // (its 32 numbers, taken apart once and kept, would not fit the registers)
+                for (int ks = 0; ks < 4; ++ks)           // (its 32 numbers, taken apart once and kept, would not fit the registers)
                     asm volatile("" : "+v"(q[ks].x), "+v"(q[ks].y), "+v"(q[ks].z), "+v"(q[ks].w));
                 const win_i32x4 x = listed4(S.sees + e0 + e), y = listed4((const char *)(S.sees + e0 + e) + 16);
                 const bool mine = sub == y.z;
@@ -169,7 +166,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) {
                     const uint32_t lw[4] = {q[ks].x, q[ks].y, q[ks].z, q[ks].w}, hw[4] = {q[ks + 2].x, q[ks + 2].y, q[ks + 2].z, q[ks + 2].w};
-                    uint4 was[2] = {__builtin_bit_cast(uint4, qop[ks]), __builtin_bit_cast(uint4, qop[ks + 2])};
+                    const uint4 was[2] = {__builtin_bit_cast(uint4, qop[ks]), __builtin_bit_cast(uint4, qop[ks + 2])};
                     uint32_t xo[4] = {was[0].x, was[0].y, was[0].z, was[0].w}, yo[4] = {was[1].x, was[1].y, was[1].z, was[1].w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -183,56 +180,59 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
                 }
             }
         }
-        uint32_t sees[2] = {0, 0};
+        uint32_t sees[TILES], some = 0, all = ~0u;       // bit: key of a tile; of any tile, of all there are
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) sees[t] = 0;
         if (listers > 0 && (reps == 1 || step % reps == rep)) {
             auto first = [](unsigned k) { return k >= 32u ? ~0u : (1u << k) - 1u; };
             asm volatile("" ::: "memory");
             const int4 w = s_see[wave][n];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int skip = PC_TILE * (tile + half), p = w.x + skip;
+            for (int t = 0; t < TILES; ++t) {
+                const int skip = PC_TILE * (tile + t), p = w.x + skip;
                 const unsigned below = w.w <= p ? 0u : (unsigned)w.w - (unsigned)p;
-                sees[half] = first((unsigned)max(w.y - skip, 0)) & (~first(below) | first((unsigned)max(w.z - skip, 0)));
+                sees[t] = tile + t >= has ? 0u : first((unsigned)max(w.y - skip, 0)) & (~first(below) | first((unsigned)max(w.z - skip, 0)));
             }
-            if (tile + 1 >= has) sees[1] = 0;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) { some |= sees[t]; all &= sees[t]; }
         }
-        if (__builtin_amdgcn_ballot_w64((sees[0] | sees[1]) != 0) != 0) {
+        if (__builtin_amdgcn_ballot_w64(some != 0) != 0) {
             const unsigned kt = ring + place * SLOT;
-            float sc[16];                                    // keys 32 half + 8 a + 0..7 of column n
+            float sc[8 * TILES];                         // keys 32 t + 8 a + 0..7 of column n
             {
                 // (chunk a + 4 ks of a key stands where (a ^ turn) ^ 4 ks says)
                 const int l = lane_again(), r = 8 * ((l & 15) >> 2) + (l & 3);
                 const unsigned at = (unsigned)(r * 256 + (((l >> 4) ^ turn_of(r)) << 4));
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                for (int t = 0; t < TILES; ++t)
 #pragma unroll
                     for (int tau = 0; tau < 2; ++tau) {
                         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int ks = 0; ks < 4; ++ks)
-                            s = MFMA16(__builtin_bit_cast(bf16x8, *(lds16)(uintptr_t)(kt + half * 2 * TILE_BYTES + (at ^ (ks << 6)) + tau * 1024)), qop[ks], s);
+                            s = MFMA16(__builtin_bit_cast(bf16x8, *(lds16)(uintptr_t)(kt + t * 2 * TILE_BYTES + (at ^ (ks << 6)) + tau * 1024)), qop[ks], s);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) sc[8 * half + 4 * tau + j] = s[j];
+                        for (int j = 0; j < 4; ++j) sc[8 * t + 4 * tau + j] = s[j];
                     }
             }
             __builtin_amdgcn_sched_barrier(0);
-            const bool whole = (sees[0] & sees[1]) == ~0u;
-            if (__builtin_amdgcn_ballot_w64((sees[0] | sees[1]) != 0 && !whole) == 0) {       // (all or nothing)
+            const bool whole = all == ~0u;
+            if (__builtin_amdgcn_ballot_w64(some != 0 && !whole) == 0) {     // (all or nothing)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sc[j] = whole ? sc[j] : -INFINITY;
+                for (int j = 0; j < 8 * TILES; ++j) sc[j] = whole ? sc[j] : -INFINITY;
             } else {
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t mine = sees[half] >> (8 * a);
+                for (int t = 0; t < TILES; ++t) {
+                    const uint32_t mine = sees[t] >> (8 * a);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sc[8 * half + j] = (mine >> j) & 1 ? sc[8 * half + j] : -INFINITY;
+                    for (int j = 0; j < 8; ++j) sc[8 * t + j] = (mine >> j) & 1 ? sc[8 * t + j] : -INFINITY;
                 }
             }
             float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
 #pragma unroll
-            for (int j = 4; j < 16; j += 4) mx = fmaxf(mx, fmaxf(fmaxf(sc[j], sc[j + 1]), fmaxf(sc[j + 2], sc[j + 3])));
-            // The reference of a column's exponents moves only where a score is 2^LAZY above it (a column's first always is): probabilities
-            // up to that are as exact, and the lanes of a column need not agree on a maximum step by step.
+            for (int j = 4; j < 8 * TILES; j += 4) mx = fmaxf(mx, fmaxf(fmaxf(sc[j], sc[j + 1]), fmaxf(sc[j + 2], sc[j + 3])));
+            // The reference of a column's exponents moves only where a score is 2^LAZY above it (a column's first always is):
+            // probabilities up to that are as exact, and the lanes of a column need not agree on a maximum step by step.
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_ref + LAZY_LOG2) != 0, 0)) {
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -243,50 +243,53 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_win_shared_decode_bf16_ker
                 for (int db = 0; db < 8; ++db) acc[db] *= f;
             }
             const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-            uint32_t pk[8];
+            bf16x8 p[TILES];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) pk[j] = pack_bf16(ex2(sc[2 * j] - ref), ex2(sc[2 * j + 1] - ref));
-            const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
+            for (int t = 0; t < TILES; ++t) {
+                uint32_t pk[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) pk[j] = pack_bf16(ex2(sc[8 * t + 2 * j] - ref), ex2(sc[8 * t + 2 * j + 1] - ref));
+                p[t] = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+            }
             // (the denominator: of the probabilities as the products take them, so that their rounding cancels)
             const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
-            sums = MFMA16(ones, p[0], sums);
-            sums = MFMA16(ones, p[1], sums);
-            __builtin_amdgcn_sched_barrier(0);               // (values read any earlier would not fit the registers)
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) sums = MFMA16(ones, p[t], sums);
+            __builtin_amdgcn_sched_barrier(0);           // (values read any earlier would not fit the registers)
             const int lv = lane_again();
             const unsigned vt = kt + TILE_BYTES + (unsigned)(((lv >> 4) * PC_D + (lv & 15)) * 16);
-            auto value = [&](int half, int db) __attribute__((always_inline)) { return *(lds16)(uintptr_t)(vt + half * 2 * TILE_BYTES + 256 * db); };
+            auto value = [&](int t, int db) __attribute__((always_inline)) { return *(lds16)(uintptr_t)(vt + t * 2 * TILE_BYTES + 256 * db); };
             if (__builtin_expect(uniform(s_odd[place]) == 0, 1)) {
 #pragma unroll
                 for (int db = 0; db < 8; ++db)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) acc[db] = MFMA16(__builtin_bit_cast(bf16x8, value(half, db)), p[half], acc[db]);
+                    for (int t = 0; t < TILES; ++t) acc[db] = MFMA16(__builtin_bit_cast(bf16x8, value(t, db)), p[t], acc[db]);
             } else {
-                // A value that is not finite: 0 times it would not be 0.  A call at a time, the values of keys that it does not see cleared,
-                // and the other columns keep what they have.
+                // A value that is not finite: 0 times it would not be 0.  A call at a time, the values of keys that it does not see
+                // cleared, and the other columns keep what they have.
 #pragma unroll 1
                 for (int i = 0; i < per; ++i) {
-                    win_i32x4 keep[2];
-                    uint32_t any = 0;
+                    if ((__builtin_amdgcn_readlane((int)some, i * g)) == 0) continue;
+                    const bool mine = sub == i;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const uint32_t its = (uint32_t)__builtin_amdgcn_readlane((int)sees[half], i * g), part = its >> (8 * a);
-                        any |= its;
+                    for (int t = 0; t < TILES; ++t) {
+                        const uint32_t part = (uint32_t)__builtin_amdgcn_readlane((int)sees[t], i * g) >> (8 * a);
+                        win_i32x4 keep;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) keep[half][j] = (int)(((part >> (2 * j)) & 1 ? 0xFFFFu : 0u) | ((part >> (2 * j + 1)) & 1 ? 0xFFFF0000u : 0u));
-                    }
-                    if (any == 0) continue;
+                        for (int j = 0; j < 4; ++j) keep[j] = (int)(((part >> (2 * j)) & 1 ? 0xFFFFu : 0u) | ((part >> (2 * j + 1)) & 1 ? 0xFFFF0000u : 0u));
 #pragma unroll
-                    for (int db = 0; db < 8; ++db) {
-                        const f32x4 was = acc[db], x = MFMA16(__builtin_bit_cast(bf16x8, value(1, db) & keep[1]), p[1], MFMA16(__builtin_bit_cast(bf16x8, value(0, db) & keep[0]), p[0], was));
+                        for (int db = 0; db < 8; ++db) {
+                            const f32x4 x = MFMA16(__builtin_bit_cast(bf16x8, value(t, db) & keep), p[t], acc[db]);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[db][j] = sub == i ? x[j] : was[j];
+                            for (int j = 0; j < 4; ++j) acc[db][j] = mine ? x[j] : acc[db][j];
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
                     }
                 }
             }
         }
-        // (what is asked for and looked at for later steps comes behind this step's products: the waves that have none are at it meanwhile)
-        if (step + AHEAD < n_steps) request((place + AHEAD) & (RING - 1));
-        if (step + 1 < n_steps) look((place + 1) & (RING - 1));
+        // (what is asked for comes behind this step's products: the waves that have none are at it meanwhile)
+        if (step + AHEAD < n_steps) request(before);
     }
     if (!real) return;
     const int64_t at = ((int64_t)S.calls[call0 + call].part0 + split0 + rep) * W.n_q_heads + kh * g + n % g;

@@ -52,6 +52,7 @@ struct PcWin {
 struct PcWinDecode { int32_t off_items, off_runs, off_q_pos, n16; void *ws; };      // n16 > 0: so many pieces of 16 bytes are left in the workspace for the merge
 
 // ---- single tokens of calls that list the same messages ----
+#define PC_WIN_STEP_TILES 2   // tiles of a visit that are multiplied between two barriers
 #define PC_WIN_GROUPS 16      // groups of 16 columns (calls x heads of the KV head) a workgroup takes at most
 struct PcWinVisit {           // consecutive tiles, and who sees some of them
     int32_t slot0, n_tiles;
@@ -67,7 +68,7 @@ struct PcWinSee {             // a call's view of a visit
     int32_t pad;
 };
 struct PcWinSharedItem {      // one workgroup's tiles, for each KV head
-    int32_t visit0, n_steps;  // (a step: two tiles of a visit)
+    int32_t visit0, n_steps;  // (a step: PC_WIN_STEP_TILES tiles of a visit)
     int32_t call0, n_calls;   // its set of calls
     int32_t waves;            // that hold all groups of columns (a power of two); the others share its steps
     int32_t split0;

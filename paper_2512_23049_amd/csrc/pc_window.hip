@@ -229,7 +229,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                 }
                 for (const auto &o : seen) P.sh_sees.push_back(o.second);
                 P.sh_visits.push_back(pv);
-                P.sh_items.back().n_steps += (n + 1) / 2;
+                P.sh_items.back().n_steps += (n + PC_WIN_STEP_TILES - 1) / PC_WIN_STEP_TILES;
                 left -= n; done += n;
                 if (done == v.tiles) { ++at; done = 0; }
             }
