@@ -19,7 +19,9 @@ struct PcForkItem {
 // Tokens [first, first + n) of the new message lie from this slot on.
 struct PcForkPiece { int32_t first, n, slot, pad; };
 
-#define PC_COMPACT_BYTES 65536    // what a workgroup moves: it holds all of it in registers
+#define PC_COMPACT_THREADS 512
+#define PC_COMPACT_BYTES (256 * PC_COMPACT_THREADS)       // what a workgroup moves: it holds all of it in registers
+#define PC_COMPACT_COUNTER 64     // words: a counter's cache lines are its own
 // A tile that moves; the tiles are in the order of their slots.
 struct PcCompactTile {
     int32_t src;              // slot / PC_TILE, -1: no tokens there, zeros are written
@@ -33,7 +35,7 @@ struct PcCompact {
     const PcCompactMove *moves;
     int32_t n_tiles, n_moves, n_chunks, n_stores;     // n_stores: KV heads, times two (keys, then values)
     uint32_t epoch, ticket0;
-    uint32_t *ticket;         // counts the workgroups of every launch
+    uint32_t *ticket;         // [n_stores], PC_COMPACT_COUNTER words apart: count a store's workgroups of every launch
     uint32_t *read;           // [n_stores][n_chunks]: epoch once the chunk has been read
     char *k_store, *v_store;
     int64_t head_bytes;       // a head's share of a store

@@ -131,8 +131,8 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
         PcCompact C{};
         C.n_tiles = (int32_t)n_tiles; C.n_moves = (int32_t)moves.size();
         C.n_chunks = (int32_t)((n_tiles + per - 1) / per); C.n_stores = 2 * c->cfg.n_kv_heads;
-        const size_t words = 64 + (size_t)C.n_chunks * C.n_stores;
-        if (words > c->flag_words) {                     // the counter (a cache line of its own), then a flag for every chunk and store
+        const size_t counters = (size_t)PC_COMPACT_COUNTER * C.n_stores, words = counters + (size_t)C.n_chunks * C.n_stores;
+        if (words > c->flag_words) {                     // a counter for every store, then a flag for every chunk and store
             if (c->flags_dev) {
                 PC_HIP(c, hipStreamSynchronize(st));
                 PC_HIP(c, hipDeviceSynchronize());
@@ -151,7 +151,7 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
         if (rc != PC_OK) return rc;
         C.tiles = (const PcCompactTile *)c->tok_dev; C.moves = (const PcCompactMove *)((char *)c->tok_dev + at_moves);
         C.epoch = c->flag_epoch + 1; C.ticket0 = c->tickets;
-        C.ticket = c->flags_dev; C.read = c->flags_dev + 64;
+        C.ticket = c->flags_dev; C.read = c->flags_dev + counters;
         C.k_store = (char *)c->k_store; C.v_store = (char *)c->v_store;
         C.head_bytes = c->slots * c->D * (int64_t)c->esize; C.tile_bytes = tile_bytes;
         C.table = c->table_dev;
@@ -159,7 +159,7 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
         pc_launch_compact(C, st);
         PC_HIP(c, hipGetLastError());
         c->flag_epoch = C.epoch;
-        c->tickets += (uint32_t)C.n_chunks * (uint32_t)C.n_stores;
+        c->tickets += (uint32_t)C.n_chunks;
     }
     if (!moves.empty()) c->dirty_end = std::max(c->dirty_end, c->next_slot);      // (what moved leaves itself behind)
     for (const PcCompactMove &mv : moves) c->msgs[(size_t)mv.rec].slot_start = mv.slot_start;

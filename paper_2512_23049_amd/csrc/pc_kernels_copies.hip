@@ -171,35 +171,36 @@ void pc_launch_fork(int dtype, const PcForkItem *items, const PcForkPiece *piece
 // where it writes have said so.
 //
 // Why every wait ends.  Chunks are numbered by the slots they come from and everything moves down, so what lies where a chunk
-// writes belongs to chunks of lower numbers or to itself.  A workgroup takes its number from a counter when it starts: the holders
-// of all lower numbers have started, and each says that it has read before it waits for anything.  What is passed on is no data,
+// writes belongs to chunks of lower numbers or to itself.  A workgroup takes its number from its store's counter when it starts: the
+// holders of all lower numbers have started, and each says that it has read before it waits for anything.  What is passed on is no data,
 // only that loads have returned (the wait in front of the flag); the tiles written are whole cache lines that nobody
 // reads in this launch any more.
 // Flags hold the launch's number and the counter goes on from launch to launch, so that nothing has to be cleared.
-__global__ __launch_bounds__(256) void pc_compact_kernel(PcCompact C)
+__global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_kernel(PcCompact C)
 {
     __shared__ uint32_t s_ticket;
-    if (threadIdx.x == 0) s_ticket = __hip_atomic_fetch_add(C.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) - C.ticket0;
+    const int store = (int)(blockIdx.x % (unsigned)C.n_stores), H = C.n_stores / 2;
+    if (threadIdx.x == 0) s_ticket = __hip_atomic_fetch_add(C.ticket + store * PC_COMPACT_COUNTER, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) - C.ticket0;
     __syncthreads();
-    const int ticket = __builtin_amdgcn_readfirstlane((int)s_ticket);
-    const int chunk = ticket / C.n_stores, store = ticket % C.n_stores, H = C.n_stores / 2;
+    const int chunk = __builtin_amdgcn_readfirstlane((int)s_ticket);
     const int per = PC_COMPACT_BYTES / C.tile_bytes, tile0 = chunk * per, n = min(per, C.n_tiles - tile0);
-    if (ticket == 0)
-        for (int i = threadIdx.x; i < C.n_moves; i += 256) C.table[C.moves[i].rec].slot_start = C.moves[i].slot_start;
+    if (chunk == 0 && store == 0)
+        for (int i = threadIdx.x; i < C.n_moves; i += PC_COMPACT_THREADS) C.table[C.moves[i].rec].slot_start = C.moves[i].slot_start;
     char *base = (store < H ? C.k_store + store * C.head_bytes : C.v_store + (store - H) * C.head_bytes) + threadIdx.x * 16;
-    const int steps = C.tile_bytes / 4096;               // (2 or 4)
-    u32x4 x[PC_COMPACT_BYTES / 4096];
+    constexpr int PIECE = 16 * PC_COMPACT_THREADS, PIECES = PC_COMPACT_BYTES / PIECE;
+    const int steps = C.tile_bytes / PIECE;              // (1 or 2)
+    u32x4 x[PIECES];
 #pragma unroll
-    for (int j = 0; j < PC_COMPACT_BYTES / 4096; ++j) {
+    for (int j = 0; j < PIECES; ++j) {
         const int t = j / steps;
         x[j] = (u32x4){0u, 0u, 0u, 0u};
         if (t < n) {
             const int src = C.tiles[tile0 + t].src;
-            if (src >= 0) x[j] = *reinterpret_cast<const u32x4 *>(base + (int64_t)src * C.tile_bytes + (j % steps) * 4096);
+            if (src >= 0) x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + (int64_t)src * C.tile_bytes + (j % steps) * PIECE));
         }
     }
 #pragma unroll
-    for (int j = 0; j < PC_COMPACT_BYTES / 4096; ++j) asm volatile("" : "+v"(x[j]));      // every load has returned ...
+    for (int j = 0; j < PIECES; ++j) asm volatile("" : "+v"(x[j]));      // every load has returned ...
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();                                     // ... in every wave
     uint32_t *read = C.read + (int64_t)store * C.n_chunks;
@@ -212,13 +213,13 @@ __global__ __launch_bounds__(256) void pc_compact_kernel(PcCompact C)
     asm volatile("" ::: "memory");
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < PC_COMPACT_BYTES / 4096; ++j) {
+    for (int j = 0; j < PIECES; ++j) {
         const int t = j / steps;
-        if (t < n) *reinterpret_cast<u32x4 *>(base + (int64_t)C.tiles[tile0 + t].dst * C.tile_bytes + (j % steps) * 4096) = x[j];
+        if (t < n) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4 *>(base + (int64_t)C.tiles[tile0 + t].dst * C.tile_bytes + (j % steps) * PIECE));
     }
 }
 
 void pc_launch_compact(const PcCompact &C, hipStream_t st)
 {
-    if (C.n_chunks > 0) pc_compact_kernel<<<(unsigned)(C.n_chunks * C.n_stores), 256, 0, st>>>(C);
+    if (C.n_chunks > 0) pc_compact_kernel<<<(unsigned)(C.n_chunks * C.n_stores), PC_COMPACT_THREADS, 0, st>>>(C);
 }
