@@ -1,8 +1,26 @@
 // Host side of the cache's own copies: forks of messages, and the cache closing up.
 #include "pc_host.h"
 #include "pc_copies.h"
+#include "pc_window.h"
 
 namespace {
+
+// A call's items (a multiple of 16 bytes) to tok_dev, read from the staging slot by a kernel: a copy by the copy engine, between two
+// kernels of the stream, costs 12 us more.
+int32_t fetch_items(pc_cache *c, const void *items, size_t bytes, hipStream_t st)
+{
+    int32_t rc = pc_items_room(c, bytes, st);
+    if (rc != PC_OK) return rc;
+    StageSlot *slot = nullptr;
+    rc = pc_stage_acquire(c, bytes, &slot);
+    if (rc != PC_OK) return rc;
+    std::memcpy(slot->host, items, bytes);
+    PcWinTurns T{};
+    T.from = slot->host; T.ws = c->tok_dev; T.n16 = (int)(bytes / 16); T.D = c->D;
+    pc_launch_win_turns(T, nullptr, st);
+    PC_HIP(c, hipGetLastError());
+    return pc_stage_release(c, slot, st);
+}
 
 int32_t message_fork(pc_cache *c, const pc_fork *forks, int32_t n, int32_t *msg_ids, hipStream_t st)
 {
@@ -51,15 +69,18 @@ int32_t message_fork(pc_cache *c, const pc_fork *forks, int32_t n, int32_t *msg_
         PcDeviceScope on(c);
         if (!on.ok) return pc_fail(c, PC_ERR_HIP, "message_fork: the cache's device cannot be made current");
         if (pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "message_fork: the stream is being captured");
-        const size_t n_items = sizeof(PcForkItem) * items.size();
-        std::vector<char> lists(n_items + sizeof(PcForkPiece) * pieces.size());
-        std::memcpy(lists.data(), items.data(), n_items);
-        std::memcpy(lists.data() + n_items, pieces.data(), sizeof(PcForkPiece) * pieces.size());
-        const int32_t rc = pc_stage_items(c, lists.data(), lists.size(), st);
+        const size_t n_items = sizeof(PcForkItem) * items.size(), bytes = n_items + sizeof(PcForkPiece) * pieces.size();
+        const bool in_args = bytes <= PC_ARG_BYTES;
+        PcArgBlob blob;
+        std::vector<char> lists(in_args ? 0 : bytes);
+        char *at = in_args ? (char *)blob.w : lists.data();
+        std::memcpy(at, items.data(), n_items);
+        std::memcpy(at + n_items, pieces.data(), sizeof(PcForkPiece) * pieces.size());
+        const int32_t rc = in_args ? PC_OK : fetch_items(c, lists.data(), bytes, st);
         if (rc != PC_OK) return rc;
         c->msgs.reserve(c->msgs.size() + (size_t)n);     // (nothing may fail behind the launch)
         ProfScope ps(c, 0, st);
-        pc_launch_fork(c->cfg.dtype, (const PcForkItem *)c->tok_dev, (const PcForkPiece *)((char *)c->tok_dev + n_items), n, max_rows, c->cfg.n_kv_heads, c->D,
+        pc_launch_fork(c->cfg.dtype, in_args ? &blob : nullptr, (const PcForkItem *)c->tok_dev, (const PcForkPiece *)((char *)c->tok_dev + n_items), n, max_rows, c->cfg.n_kv_heads, c->D,
                        c->slots, c->inv_freq_dev, c->k_store, c->v_store, c->table_dev, st);
         PC_HIP(c, hipGetLastError());
     }
@@ -112,7 +133,7 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
         const int32_t tile_bytes = (int32_t)(PC_TILE * c->D * c->esize), per = PC_COMPACT_BYTES / tile_bytes;
         // a list of tiles in slot order, the table's moves behind it
         const size_t n_tiles = (size_t)(moved / PC_TILE), at_moves = sizeof(PcCompactTile) * n_tiles;
-        std::vector<char> lists(at_moves + sizeof(PcCompactMove) * moves.size());
+        std::vector<char> lists(align_up(at_moves + sizeof(PcCompactMove) * moves.size(), 16));
         PcCompactTile *tiles = (PcCompactTile *)lists.data();
         size_t t = 0, behind = 0;                        // behind: the first tile whose source lies at or behind the place being written
         std::vector<int32_t> place(n_tiles);             // where each tile lies now, whether or not it holds tokens
@@ -147,7 +168,7 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
             PC_HIP(c, hipMemsetAsync(c->flags_dev, 0, sizeof(uint32_t) * c->flag_words, st));
             c->tickets = 0; c->flag_epoch = 0;
         }
-        const int32_t rc = pc_stage_items(c, lists.data(), lists.size(), st);
+        const int32_t rc = fetch_items(c, lists.data(), lists.size(), st);
         if (rc != PC_OK) return rc;
         C.tiles = (const PcCompactTile *)c->tok_dev; C.moves = (const PcCompactMove *)((char *)c->tok_dev + at_moves);
         C.epoch = c->flag_epoch + 1; C.ticket0 = c->tickets;

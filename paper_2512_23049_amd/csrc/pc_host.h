@@ -230,6 +230,7 @@ int32_t pc_ensure_ws(pc_cache *c, size_t bytes, hipStream_t st);
 int32_t pc_stage_acquire(pc_cache *c, size_t bytes, StageSlot **out);
 int32_t pc_stage_release(pc_cache *c, StageSlot *s, hipStream_t st);      // what reads the slot has been enqueued on st: its event
 bool pc_recorded(hipStream_t st);
+extern "C" int32_t pc_items_room(pc_cache *c, size_t bytes, hipStream_t st);       // room for a call's items at tok_dev
 extern "C" int32_t pc_stage_items(pc_cache *c, const void *items, size_t bytes, hipStream_t st);
 // pc_attend.hip: the address, on the current device, of the library's fixed scratch array (looked up once per device)
 int32_t pc_static_scratch(void **ptr, size_t *bytes);

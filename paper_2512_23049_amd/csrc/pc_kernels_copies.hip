@@ -128,8 +128,8 @@ __device__ __forceinline__ void fork_f32(const PcForkItem &it, const PcForkPiece
 }
 
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void pc_fork_kernel(const PcForkItem *__restrict__ items, const PcForkPiece *__restrict__ all_pieces, int64_t slots,
-                                                      const double *__restrict__ inv_freq, void *k_store, void *v_store, PcMsgEntry *table)
+__device__ __forceinline__ void fork_copy(const PcForkItem *items, const PcForkPiece *all_pieces, int64_t slots, const double *__restrict__ inv_freq, void *k_store,
+                                          void *v_store, PcMsgEntry *table)
 {
     __shared__ __attribute__((aligned(16))) float2 s_rot[D / 2];
     const PcForkItem it = items[blockIdx.z];
@@ -153,10 +153,30 @@ __global__ __launch_bounds__(256) void pc_fork_kernel(const PcForkItem *__restri
     }
 }
 
-void pc_launch_fork(int dtype, const PcForkItem *items, const PcForkPiece *pieces, int n, int max_rows, int n_kv_heads, int D, int64_t slots,
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void pc_fork_kernel(const PcForkItem *items, const PcForkPiece *pieces, int64_t slots, const double *inv_freq, void *k_store,
+                                                      void *v_store, PcMsgEntry *table)
+{
+    fork_copy<D, BF16>(items, pieces, slots, inv_freq, k_store, v_store, table);
+}
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void pc_fork_arg_kernel(PcArgBlob, int n, int64_t slots, const double *inv_freq, void *k_store, void *v_store, PcMsgEntry *table)
+{
+    const PcForkItem *items = (const PcForkItem *)__builtin_amdgcn_kernarg_segment_ptr();          // (the blob comes first)
+    fork_copy<D, BF16>(items, reinterpret_cast<const PcForkPiece *>(items + n), slots, inv_freq, k_store, v_store, table);
+}
+
+void pc_launch_fork(int dtype, const PcArgBlob *blob, const PcForkItem *items, const PcForkPiece *pieces, int n, int max_rows, int n_kv_heads, int D, int64_t slots,
                     const double *inv_freq, void *k_store, void *v_store, PcMsgEntry *table, hipStream_t st)
 {
     const int tiles = (max_rows + PC_TILE - 1) / PC_TILE;
+    if (blob) {
+        const dim3 grid((unsigned)((tiles + FORK_TILES - 1) / FORK_TILES), (unsigned)n_kv_heads, (unsigned)n);
+        if (dtype == 1) pc_fork_arg_kernel<128, true><<<grid, 256, 0, st>>>(*blob, n, slots, inv_freq, k_store, v_store, table);
+        else if (D == 64) pc_fork_arg_kernel<64, false><<<grid, 256, 0, st>>>(*blob, n, slots, inv_freq, k_store, v_store, table);
+        else pc_fork_arg_kernel<128, false><<<grid, 256, 0, st>>>(*blob, n, slots, inv_freq, k_store, v_store, table);
+        return;
+    }
     for (int at = 0; at < n; at += 65535) {              // (the limit of a grid's third dimension)
         const dim3 grid((unsigned)((tiles + FORK_TILES - 1) / FORK_TILES), (unsigned)n_kv_heads, (unsigned)std::min(n - at, 65535));
         if (dtype == 1) pc_fork_kernel<128, true><<<grid, 256, 0, st>>>(items + at, pieces, slots, inv_freq, k_store, v_store, table);

@@ -307,7 +307,7 @@ int32_t pc_append_message(pc_cache *c, const void *k, const void *v, int32_t len
 }
 
 // small host-built item lists go through the pinned ring into one device buffer that grows on demand
-int32_t pc_stage_items(pc_cache *c, const void *items, size_t bytes, hipStream_t st)
+int32_t pc_items_room(pc_cache *c, size_t bytes, hipStream_t st)
 {
     if (bytes > c->tok_cap) {
         if (c->tok_dev) {                                // work in flight may still use the old one
@@ -320,8 +320,15 @@ int32_t pc_stage_items(pc_cache *c, const void *items, size_t bytes, hipStream_t
         PC_HIP(c, hipMalloc(&c->tok_dev, cap));
         c->tok_cap = cap;
     }
+    return PC_OK;
+}
+
+int32_t pc_stage_items(pc_cache *c, const void *items, size_t bytes, hipStream_t st)
+{
+    int32_t rc = pc_items_room(c, bytes, st);
+    if (rc != PC_OK) return rc;
     StageSlot *slot = nullptr;
-    const int32_t rc = pc_stage_acquire(c, bytes, &slot);
+    rc = pc_stage_acquire(c, bytes, &slot);
     if (rc != PC_OK) return rc;
     std::memcpy(slot->host, items, bytes);
     PC_HIP(c, hipMemcpyAsync(c->tok_dev, slot->host, bytes, hipMemcpyHostToDevice, st));
