@@ -68,7 +68,9 @@ __device__ __forceinline__ void win_turns(const char *from, const PcWinTurns &T)
         } else if (i < n_copy + n_q) {
             const int64_t R = (i - n_copy) / half;
             const int f = (int)((i - n_copy) % half);
-            T.rot_q[T.lanes_order ? win_rot_at(R, f) : R * half + f] = rope_turn(reinterpret_cast<const int32_t *>(from + T.off_q_pos)[R], T.inv_freq[f]);
+            const float2 cs = rope_turn(reinterpret_cast<const int32_t *>(from + T.off_q_pos)[R], T.inv_freq[f]);
+            if (T.rot_q) T.rot_q[R * half + f] = cs;
+            if (T.rot_lanes) T.rot_lanes[win_rot_at(R, f)] = pack_f16(cs.x, cs.y);
         } else {
             const int64_t k = (i - n_copy - n_q) / half;
             const int f = (int)((i - n_copy - n_q) % half);
@@ -105,6 +107,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
 {
     constexpr int RING = 4, AHEAD = 3;
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][2 * TILE_BYTES];
+    __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
     __shared__ int s_again;
 
     const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
@@ -146,8 +149,13 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
     bf16x8 qop[8];
     // (few: in the walk, what is read for all of it at once would not fit the registers)
     auto turn = [&](int rot, auto few) __attribute__((always_inline)) {
-        const float4 *rq = reinterpret_cast<const float4 *>(W.rot_q) + (R >> 5) * 1024 + hh * 32 + (R & 31);
-        const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)rot * (PC_D / 2) + 8 * hh);
+        const uint4 *rq = reinterpret_cast<const uint4 *>(W.rot_lanes) + (R >> 5) * 512 + hh * 32 + (R & 31);
+        // (the run's rotation is the same for all rows: one load a lane, and broadcasts from shared memory)
+        const float2 own = W.rot_run[(int64_t)rot * (PC_D / 2) + lane];
+        asm volatile("" ::: "memory");
+        s_rot[wave][lane] = own;
+        asm volatile("" ::: "memory");                   // (a wave's own LDS accesses happen in order)
+        const float4 *rr = reinterpret_cast<const float4 *>(&s_rot[wave][8 * hh]);
         // the lane's row, as it came (from the cache each time: 32 registers): dims 16 ks + 8 hh + 0..7, then 64 up
         const unsigned char *qp = (const unsigned char *)W.q + (R * W.n_q_heads + h) * (PC_D * 2) + 16 * hh;
 #pragma unroll
@@ -155,10 +163,13 @@ __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
             uint4 lq = ldg16(qp + 32 * ks), hq = ldg16(qp + 32 * ks + 128);
             if (!row_ok) lq = hq = make_uint4(0, 0, 0, 0);
             const uint32_t lw[4] = {lq.x, lq.y, lq.z, lq.w}, hw[4] = {hq.x, hq.y, hq.z, hq.w};
+            const uint4 p0 = rq[ks * 128], p1 = rq[ks * 128 + 64];
+            const uint32_t pw[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
             uint32_t a[4], b[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float4 p = rq[ks * 256 + j * 64], r = rr[8 * ks + j];
+                const float4 p = make_float4(f16_lo(pw[2 * j]), f16_hi(pw[2 * j]), f16_lo(pw[2 * j + 1]), f16_hi(pw[2 * j + 1]));
+                const float4 r = rr[8 * ks + j];
                 const float c0 = p.x * r.x + p.y * r.y, s0 = p.y * r.x - p.x * r.y, c1 = p.z * r.z + p.w * r.w, s1 = p.w * r.z - p.z * r.w;
                 const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
                 a[j] = pack_bf16(x0 * c0 - y0 * s0, x1 * c1 - y1 * s1);

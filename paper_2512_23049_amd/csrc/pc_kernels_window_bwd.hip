@@ -170,6 +170,7 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
 {
     constexpr int RING = 4, AHEAD = 3;
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][2 * TILE_BYTES];
+    __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
 
     const int kh = blockIdx.x % W.n_kv_heads;
     const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
@@ -230,18 +231,25 @@ __global__ __launch_bounds__(256, 2) void pc_win_bwd_dq_bf16_kernel(PcWin W, PcW
     }
     bf16x8 qop[8];
     auto turn = [&](int rot) __attribute__((always_inline)) {       // as in the forward: the same bits but for a rounding of the scale
-        const float4 *rq = reinterpret_cast<const float4 *>(W.rot_q + R * (PC_D / 2) + 8 * hh);
-        const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)rot * (PC_D / 2) + 8 * hh);
+        const uint4 *rq = reinterpret_cast<const uint4 *>(W.rot_lanes) + (R >> 5) * 512 + hh * 32 + (R & 31);
+        // (the run's rotation is the same for all rows: one load a lane, and broadcasts from shared memory)
+        const float2 own = W.rot_run[(int64_t)rot * (PC_D / 2) + lane];
+        asm volatile("" ::: "memory");
+        s_rot[wave][lane] = own;
+        asm volatile("" ::: "memory");                   // (a wave's own LDS accesses happen in order)
+        const float4 *rr = reinterpret_cast<const float4 *>(&s_rot[wave][8 * hh]);
         const unsigned char *qp = (const unsigned char *)W.q + (R * W.n_q_heads + h) * (PC_D * 2) + 16 * hh;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             uint4 lq = ldg16(qp + 32 * ks), hq = ldg16(qp + 32 * ks + 128);
             if (!live) lq = hq = make_uint4(0, 0, 0, 0);
             const uint32_t lw[4] = {lq.x, lq.y, lq.z, lq.w}, hw[4] = {hq.x, hq.y, hq.z, hq.w};
+            const uint4 p0 = rq[ks * 128], p1 = rq[ks * 128 + 64];
+            const uint32_t pw[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
             uint32_t a[4], b[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float4 p = rq[8 * ks + j];
+                const float4 p = make_float4(f16_lo(pw[2 * j]), f16_hi(pw[2 * j]), f16_lo(pw[2 * j + 1]), f16_hi(pw[2 * j + 1]));
                 const float4 r = rr[8 * ks + j];
                 const float c0 = (p.x * r.x + p.y * r.y) * W.scale_log2, s0 = (p.y * r.x - p.x * r.y) * W.scale_log2;
                 const float c1 = (p.z * r.z + p.w * r.w) * W.scale_log2, s1 = (p.w * r.z - p.z * r.w) * W.scale_log2;

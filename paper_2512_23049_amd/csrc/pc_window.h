@@ -35,7 +35,8 @@ struct PcWin {
     const PcWinRun  *runs;
     const PcWinItem *items;
     const int32_t   *q_pos;   // [rows]
-    const float2    *rot_q;   // bf16: in the lanes' order (see win_rot_at); fp32: [rows][D/2]: (cos, sin)(q_pos theta_i)
+    const float2    *rot_q;   // [rows][D/2]: (cos, sin)(q_pos theta_i)
+    const uint32_t  *rot_lanes;       // the same as fp16 in the lanes' order (see win_rot_at)
     const float2    *rot_run; // [rot][D/2]: (cos, sin)(rot_pos theta_i)
     const double    *inv_freq;
     const void      *k_store, *v_store, *q;
@@ -140,11 +141,12 @@ void pc_launch_win_bwd_keys_bf16(const PcWin &W, const PcWinBwd &B, hipStream_t 
 void pc_launch_win_bwd_keys_f32(const PcWin &W, const PcWinBwd &B, int D, hipStream_t st);
 void pc_launch_win_bwd_sums(const PcWin &W, const PcWinBwd &B, int D, hipStream_t st);
 
-// float2 index of pair i of packed row R in the lanes' order of the bf16 prefill kernel (D = 128): 16 bytes a lane, lanes of
-// consecutive rows side by side
+// index of pair i of packed row R in the lanes' order of the bf16 kernels that turn queries (D = 128): 16 bytes a lane, lanes of
+// consecutive rows side by side.  (cos, sin) are fp16 there, off by 2^-12 at most, an eighth of what the turned query's own rounding
+// may take: a run's first tile waits for these bytes.
 __host__ __device__ __forceinline__ int64_t win_rot_at(int64_t R, int i)
 {
-    return ((R / 32 * 1024 + (i / 16) * 256 + (i % 8) / 2 * 64 + (i / 8 % 2) * 32 + R % 32) * 2) + i % 2;
+    return ((R / 32 * 16 + i / 16 * 4 + i % 8 / 4 * 2 + i / 8 % 2) * 32 + R % 32) * 4 + i % 4;
 }
 
 // the least position a row at p sees (but for the sinks)
@@ -158,9 +160,10 @@ __host__ __device__ __forceinline__ int32_t win_low(int32_t p, int32_t window)
 struct PcWinTurns {
     const void *from; void *ws; int n16;
     int off_q_pos, n_rows, off_rot, n_rot;        // within the lists: int32 positions, int64 positions
-    int D, lanes_order;
+    int D;
     float run_scale;                              // rides on the runs' rotations
-    float2 *rot_q, *rot_run;
+    float2 *rot_q, *rot_run;                      // rot_q, rot_lanes: null where nobody reads them
+    uint32_t *rot_lanes;
     const double *inv_freq;
 };
 void pc_launch_win_turns(const PcWinTurns &T, const PcArgBlob *blob, hipStream_t st);
@@ -173,6 +176,8 @@ void pc_launch_win_shared_decode_bf16(const PcWin &W, const PcWinShared &S, hipS
 void pc_launch_win_merge(const PcWin &W, const PcMergeRow *rows, int n_rows, int dtype, int D, hipStream_t st);
 
 #ifdef __HIPCC__
+__device__ __forceinline__ float f16_lo(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)w); }
+__device__ __forceinline__ float f16_hi(uint32_t w) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(w >> 16)); }
 // A walk over the tiles of an item, run after run (uniform over the wave: everything stays in scalar registers).
 struct WinTile { int slot0, pos0, valid, sink, rot, self; int64_t rot_pos; };
 typedef int win_i32x4 __attribute__((ext_vector_type(4)));

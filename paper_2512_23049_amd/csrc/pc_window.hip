@@ -315,7 +315,7 @@ WinLayout lay_out(const pc_cache *c, const WinPlan &P)
     L.lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = P.pre.empty() ? 0 : sizeof(float2) * (size_t)c->half;
-    L.rot_q = big(rot * align_up(P.q_pos.size(), 32));
+    L.rot_q = big((c->cfg.dtype == PC_BF16 ? rot / 2 : rot) * align_up(P.q_pos.size(), 32));         // (bf16: rot_lanes)
     L.rot_run = big(rot * P.rots.size());
     L.part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads * (size_t)c->D);
     L.part_ml = big(sizeof(float) * 2 * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads);
@@ -558,7 +558,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     PcWin W{};
     W.runs = (const PcWinRun *)(ws + L.runs);
     W.q_pos = (const int32_t *)(ws + L.q_pos);
-    W.rot_q = (const float2 *)(ws + L.rot_q); W.rot_run = (const float2 *)(ws + L.rot_run);
+    W.rot_q = (const float2 *)(ws + L.rot_q); W.rot_lanes = (const uint32_t *)(ws + L.rot_q); W.rot_run = (const float2 *)(ws + L.rot_run);
     W.inv_freq = c->inv_freq_dev;
     W.k_store = c->k_store; W.v_store = c->v_store; W.q = q; W.out = out; W.lse = lse;
     W.part_o = (float *)(ws + L.part_o); W.part_ml = (float *)(ws + L.part_ml);
@@ -575,9 +575,11 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         T.from = in_args || recorded ? ws : slot->host; T.ws = ws; T.n16 = (int)(L.lists / 16);
         T.off_q_pos = (int)L.q_pos; T.n_rows = turns ? (int)P.q_pos.size() : 0;
         T.off_rot = (int)L.rots; T.n_rot = turns ? (int)P.rots.size() : 0;
-        T.D = c->D; T.lanes_order = bf16;
+        T.D = c->D;
         T.run_scale = bf16 ? W.scale_log2 : 1.f;
-        T.rot_q = (float2 *)(ws + L.rot_q); T.rot_run = (float2 *)(ws + L.rot_run);
+        if (bf16) T.rot_lanes = (uint32_t *)(ws + L.rot_q);
+        else T.rot_q = (float2 *)(ws + L.rot_q);
+        T.rot_run = (float2 *)(ws + L.rot_run);
         T.inv_freq = c->inv_freq_dev;
         if (!(recorded && !in_args) || turns) pc_launch_win_turns(T, in_args ? &blob : nullptr, st);
         PC_HIP(c, hipGetLastError());
@@ -626,7 +628,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     const size_t blocks = take(of(B.blocks)), apps = take(of(B.apps)), keys = take(of(B.keys)), sums = take(of(B.sums)), bins = take(of(B.bins)), lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = sizeof(float2) * (size_t)c->half, units = B.blocks.size() * (size_t)(bf16 ? Hq : H), unit = 32 * (size_t)c->D * c->esize;
-    const size_t rot_q = big(rot * P.q_pos.size()), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * P.q_pos.size() * (size_t)Hq);
+    const size_t rot_lanes = big(bf16 ? rot / 2 * align_up(P.q_pos.size(), 32) : 0), rot_q = big(rot * P.q_pos.size()), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * P.q_pos.size() * (size_t)Hq);
     const size_t q_abs = big(unit * units), d_o = big(unit * units), stat = big(PC_WIN_STAT_BYTES * units);
     const size_t part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)Hq * (size_t)c->D);
     const size_t key_part = big(sizeof(float) * 2 * PC_WIN_KEY_TILES * PC_TILE * (size_t)B.parts * (size_t)H * (size_t)c->D);
@@ -646,7 +648,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     put(blocks, B.blocks); put(apps, B.apps); put(keys, B.keys); put(sums, B.sums); put(bins, B.bins);
 
     W.items = (const PcWinItem *)(ws + items); W.runs = (const PcWinRun *)(ws + runs); W.q_pos = (const int32_t *)(ws + q_pos);
-    W.rot_q = (const float2 *)(ws + rot_q); W.rot_run = (const float2 *)(ws + rot_run);
+    W.rot_q = (const float2 *)(ws + rot_q); W.rot_lanes = (const uint32_t *)(ws + rot_lanes); W.rot_run = (const float2 *)(ws + rot_run);
     W.part_o = (float *)(ws + part_o);
     G.blocks = (const PcWinBlock *)(ws + blocks); G.apps = (const PcWinApp *)(ws + apps);
     G.key_items = (const PcWinKeyItem *)(ws + keys); G.sums = (const PcWinSum *)(ws + sums); G.bins = (const int32_t *)(ws + bins);
@@ -655,7 +657,8 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     PcWinTurns T{};
     T.from = in_args ? ws : slot->host; T.ws = ws; T.n16 = (int)(lists / 16);
     T.off_q_pos = (int)q_pos; T.n_rows = (int)P.q_pos.size(); T.off_rot = (int)rots; T.n_rot = (int)P.rots.size();
-    T.D = c->D; T.lanes_order = 0; T.run_scale = 1.f;
+    T.D = c->D; T.run_scale = 1.f;
+    if (bf16) T.rot_lanes = (uint32_t *)(ws + rot_lanes);
     T.rot_q = (float2 *)(ws + rot_q); T.rot_run = (float2 *)(ws + rot_run); T.inv_freq = c->inv_freq_dev;
     ProfScope ps(c, 5, st);
     pc_launch_win_turns(T, in_args ? &blob : nullptr, st);
