@@ -171,7 +171,20 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     const bool wide = n_groups > PC_WIN_GROUPS / 2;
     const int32_t set_calls = std::min(n_groups, wide ? PC_WIN_GROUPS : PC_WIN_GROUPS / 2) * per, n_sets = (n_calls + set_calls - 1) / set_calls;
     struct Piece { int32_t slot0, tiles; size_t run; int32_t call; };
-    std::vector<Piece> pieces;
+    std::vector<Piece> pieces, scratch;
+    // pieces [first, size) by their slots, in the calls' order where those are the same: a pass for 11 bits of a tile's number
+    auto by_slot = [](std::vector<Piece> &v, size_t first, std::vector<Piece> &other) {
+        uint32_t most = 0;
+        for (size_t k = first; k < v.size(); ++k) most = std::max(most, (uint32_t)v[k].slot0 / PC_TILE);
+        other.resize(v.size());
+        for (uint32_t shift = 0; shift == 0 || (shift < 32 && most >> shift); shift += 11) {
+            size_t at[2048] = {}, next = first;
+            for (size_t k = first; k < v.size(); ++k) ++at[((uint32_t)v[k].slot0 / PC_TILE >> shift) & 2047];
+            for (size_t &n : at) { const size_t count = n; n = next; next += count; }
+            for (size_t k = first; k < v.size(); ++k) other[at[((uint32_t)v[k].slot0 / PC_TILE >> shift) & 2047]++] = v[k];
+            std::swap_ranges(v.begin() + (ptrdiff_t)first, v.end(), other.begin() + (ptrdiff_t)first);
+        }
+    };
     std::vector<std::pair<size_t, size_t>> of_set;       // a set's pieces, in slot order
     int64_t own = 0, shared = 0;
     for (int32_t s = 0; s < n_sets; ++s) {
@@ -185,7 +198,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
             }
             own += dec[(size_t)j].tiles;
         }
-        std::sort(pieces.begin() + (ptrdiff_t)first, pieces.end(), [](const Piece &x, const Piece &y) { return x.slot0 != y.slot0 ? x.slot0 < y.slot0 : x.run < y.run; });
+        by_slot(pieces, first, scratch);
         int64_t end = -1;
         for (size_t k = first; k < pieces.size(); ++k) {
             const int64_t b = pieces[k].slot0, e = b + (int64_t)PC_TILE * pieces[k].tiles;
@@ -196,6 +209,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     // What both ways read and write, in tiles: a workgroup's partial rows are worth 8 (16 with 16 waves).
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
     if (own * 2 < 3 * (shared + bins * n_sets * (wide ? 16 : 8))) return false;
+    std::vector<std::pair<int32_t, PcWinSee>> seen;      // (call within the set, view) of the visit at hand
     for (int32_t s = 0; s < n_sets; ++s) {
         const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
         int32_t waves = 1;
@@ -223,7 +237,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
             while (left > 0) {
                 const Visit &v = visits[at];
                 const int32_t n = std::min(left, v.tiles - done), slot0 = v.slot0 + PC_TILE * done, slot1 = slot0 + PC_TILE * n;
-                std::vector<std::pair<int32_t, PcWinSee>> seen;                  // (call within the set, view)
+                seen.clear();
                 for (size_t k = v.p0; k < v.p1; ++k) {
                     const Piece &pc = pieces[k];
                     if (pc.slot0 >= slot1 || pc.slot0 + PC_TILE * pc.tiles <= slot0) continue;
@@ -231,16 +245,14 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                     const int32_t d = slot0 - r.slot0;   // (what lies in front of a run is left out by its window)
                     const int32_t j = pc.call - call0, q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)pc.call].call].q_off];
                     PcWinSee e{r.pos0 + d, r.n_tok - d, std::max(0, r.sink > 0 ? r.sink - d : 0), win_low(q_pos, P.window), (int64_t)q_pos - r.rot_pos, j % per, 0};
-                    bool joined = false;
-                    for (auto &o : seen)
-                        if (o.first == j) {              // the sinks of an extent and its end; or a message that is listed twice
-                            if (o.second.pos0 != e.pos0 || o.second.turn != e.turn) return false;
-                            o.second.n_tok = std::max(o.second.n_tok, e.n_tok); o.second.sink = std::max(o.second.sink, e.sink);
-                            joined = true;
-                        }
-                    if (!joined) seen.push_back({j, e});
+                    size_t i = seen.size();              // (nearly in order already)
+                    while (i > 0 && seen[i - 1].first > j) --i;
+                    if (i > 0 && seen[i - 1].first == j) {               // the sinks of an extent and its end; or a message that is listed twice
+                        PcWinSee &o = seen[i - 1].second;
+                        if (o.pos0 != e.pos0 || o.turn != e.turn) return false;
+                        o.n_tok = std::max(o.n_tok, e.n_tok); o.sink = std::max(o.sink, e.sink);
+                    } else seen.insert(seen.begin() + (ptrdiff_t)i, {j, e});
                 }
-                std::sort(seen.begin(), seen.end(), [](const auto &x, const auto &y) { return x.first < y.first; });
                 PcWinVisit pv{slot0, n, (int32_t)P.sh_sees.size(), {}};
                 size_t k = 0;
                 for (int32_t gr = 0; gr <= PC_WIN_GROUPS; ++gr) {
