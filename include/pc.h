@@ -194,7 +194,11 @@ int32_t pc_attend(pc_cache *c, const pc_call *calls, int32_t n_calls,
  * pc_attend_window refuses a stream that is being captured (the workspace it uses may move at a later call);
  * pc_attend_window_static is for those and for callers that cannot allocate: it works in the fixed array of pc_attend_static,
  * and what is said there of its size, its sharing, lists recorded into a graph and calls that overlap in time holds for it
- * too.  (It keeps no counters.)  A recorded call holds the slots its messages had. */
+ * too.  (It keeps no counters.)  A recorded call holds the slots its messages had.
+ *
+ * A batch of single tokens whose calls list the same messages reads each tile once for up to 256 (call, head of a KV head) pairs; the
+ * order of a row's sums depends on the batch, so that a call alone may give another last bit.  The same calls give the
+ * same bits. */
 int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
                          const void *q, void *out, float *lse, void *stream);
 int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,

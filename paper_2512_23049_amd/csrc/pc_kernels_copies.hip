@@ -20,7 +20,8 @@ __device__ __forceinline__ int fork_slot(const PcForkPiece *pieces, int n, int t
 // A workgroup copies four tiles of one fork and KV head.  Keys, stored turned to base + token, are turned by one angle a
 // frequency (whose 64 or 32 rotations the workgroup makes once); values of a bf16 cache lie in groups of eight tokens by
 // dimension, so that eight tokens from the middle of a group are two 16-byte reads and a shift.  Bound: memory; 16-byte
-// accesses of consecutive lanes, all loads of a tile in front of its first store.
+// accesses of consecutive lanes, all loads of a tile in front of its first store: 32 forks of 950 tokens, 8 KV heads, 250 MB
+// read and written in 62 us (4.0 TB/s; a large copy 4.95); one fork of 200 tokens 7.7 us.
 #define FORK_TILES 4
 
 template <bool TURN>
@@ -195,6 +196,8 @@ void pc_launch_fork(int dtype, const PcArgBlob *blob, const PcForkItem *items, c
 // holders of all lower numbers have started, and each says that it has read before it waits for anything.  What is passed on is no data,
 // only that loads have returned (the wait in front of the flag); the tiles written are whole cache lines that nobody
 // reads in this launch any more.
+// Bound: memory.  512 messages of 160 tokens, 8 KV heads: 650 MB read and written in 145 us (4.5 TB/s); 64 KB a workgroup and one counter
+// for all stores 174 us, 32 KB 330 (a counter gives 70 numbers a microsecond); kept in the caches like other data 5 % more.
 // Flags hold the launch's number and the counter goes on from launch to launch, so that nothing has to be cleared.
 __global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_kernel(PcCompact C)
 {

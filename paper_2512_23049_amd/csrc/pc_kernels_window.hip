@@ -57,7 +57,8 @@ __device__ __forceinline__ const __attribute__((address_space(4))) char *argumen
 }  // namespace
 
 // ------------------------------------------------------------------------------------------------------------- turns
-// A call's lists to the workspace, and the rotations (in 64 bits, rounded once) of its rows and of its runs.
+// A call's lists to the workspace, and the rotations (in 64 bits, rounded once) of its rows and of its runs.  Lists are read where the
+// host put them (arguments, or pinned memory): 160 KB of them take 6.5 us, 8192 rows' rotations 10.5, a short call's 3.6.
 __device__ __forceinline__ void win_turns(const char *from, const PcWinTurns &T)
 {
     const int half = T.D / 2;
@@ -103,6 +104,13 @@ void pc_launch_win_turns(const PcWinTurns &T, const PcArgBlob *blob, hipStream_t
 // Masks are bits, made only for tiles on an edge (a ragged end, the causal limit, the window's end).  What a row does not see
 // may be anything there: its score is replaced, not added to, and where a value of such a tile is not finite (asked of the
 // matrix unit: 0 x value) the product leaves those values out and the rows that see them get what they make of a sum (win_odd_sum).
+//
+// What bounds it.  Long walks: the matrix unit and the softmax beside it, with two workgroups of four waves to overlap: 8192 rows,
+// 32 heads over 8, window 4096: 600 to 650 us, 0.9 PFLOP/s of visible work (16 matrix instructions, 102 vector and 50 scalar ones a
+// tile and wave; the matrix unit is busy 0.7 of the time).  Short walks: starts and turns, whose loads nothing hides: 33 blocks of
+// rows over 20 tiles of seven messages, 47 us: a workgroup's first tile 6 us after its start, a turn 3 us, a tile 1 us, its results 2.5 us.
+// Tried and dropped: the next tile's scores beside this one's exponentials (256 registers do not hold both: 1171 us), a row's queries
+// kept in registers from turn to turn (likewise).
 __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
 {
     constexpr int RING = 4, AHEAD = 3;
@@ -456,7 +464,9 @@ void pc_launch_win_prefill_bf16(const PcWin &W, int n_items, hipStream_t st)
 // the g <= 16 heads of the KV head are the columns of 16x16x32 products.  Tiles come straight from memory into registers, two
 // ahead: the kernel lives on bytes in flight.  A wave makes the rotations of its runs itself (a lane a frequency), so that a
 // call needs no launch in front of this one but for lists too long for its arguments.  One row: what it sees of a tile is one
-// word for the whole wave, and the values of keys it does not see are cleared.
+// word for the whole wave, and the values of keys it does not see are cleared.  Bound: memory (64 calls of 32 heads over 8, window
+// 1024, 2048 shared tokens: 40 us for 210 MB); a few calls: latency (four
+// of 17 tiles, 7.7 us, and 3.6 for the merge of their splits).
 namespace {
 struct WinDecTile {
     uint4 k[2][4];      // [16-key half][d step of 32]: key 8 (m >> 2) + 4 half + (m & 3) of lane m = lane & 15
@@ -653,7 +663,8 @@ void pc_launch_win_decode_bf16(const PcWin &W, int n_items, const PcArgBlob *blo
 }
 
 // ------------------------------------------------------------------------------------------------------------- merge
-// The splits of a row, in their order: out = sum o_s 2^(m_s - m) / sum l_s 2^(m_s - m).  Four dims a thread.
+// The splits of a row, in their order: out = sum o_s 2^(m_s - m) / sum l_s 2^(m_s - m).  Four dims a thread.  Bound: memory (940 rows of
+// 32 heads in two or three splits, 39 MB: 13 us); a few rows: two round trips, 3.6 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void pc_win_merge_kernel(const PcMergeRow *__restrict__ rows, int64_t n, PcWin W)
 {

@@ -116,8 +116,8 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
     // (many groups: to the nearest, as one a little longer than the others is not worth a merge of its own)
     bool nearest = true;
     auto splits = [&](int32_t tiles) { return (int32_t)std::max<int64_t>(1, std::min<int64_t>((tiles + (nearest ? chunk / 2 : chunk - 1)) / chunk, MAX_SPLITS)); };
-    // fit: where whole groups have room at once, their splits get it too, and the longest is as short as that allows (fp32, 19 groups of
-    // 12 tiles, 2 KV heads: 17.2 -> 14.8 us; a single token's 40 tiles: 8.7 -> 7.7 us).  Not the bf16 blocks of rows, whose splits
+    // fit: where whole groups have room at once, their splits get it too, and the longest is as short as that allows (fp32, two
+    // calls of 100 to 500 rows, window 333, 2 KV heads: 17.2 -> 14.2 us; four single tokens of 17 tiles: 8.7 -> 7.7 us).  Not the bf16 blocks of rows, whose splits
     // pay for every run they touch: 33 groups of 20 tiles, 8 KV heads, take 47 us as 528 workgroups where 512 have room, 51 as 368.
     if (fit && may_split && (int64_t)groups.size() * H_kv <= target) {
         nearest = false;
