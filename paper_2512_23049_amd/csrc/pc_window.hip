@@ -206,9 +206,12 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
         }
         of_set.push_back({first, pieces.size()});
     }
-    // What both ways read and write, in tiles: a workgroup's partial rows are worth 8 (16 with 16 waves).
+    // A tile costs a workgroup that shares it about three times what it costs a call on its own (whose loads nothing holds up), and a
+    // workgroup's partial rows are worth 8 tiles (16 with 16 waves).  Calls over 410 of 512 messages, window 16 384, 8 heads a KV head, call by call and
+    // shared: 12 calls (2.6 calls a tile) 133 and 147 us, 16 (3.4) 172 and 162, 24 (4.9) 271 and 191, 32 (6.6) 312 and 217; 4 heads: 12 calls
+    // 134 and 156, 16 171 and 170, 48 (9.8) 519 and 235.  Window 2048 (1.5 calls a tile), 32 calls: 57 and 144.
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
-    if (own * 2 < 3 * (shared + bins * n_sets * (wide ? 16 : 8))) return false;
+    if (own < 3 * shared + bins * n_sets * (wide ? 16 : 8)) return false;
     std::vector<std::pair<int32_t, PcWinSee>> seen;      // (call within the set, view) of the visit at hand
     for (int32_t s = 0; s < n_sets; ++s) {
         const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
