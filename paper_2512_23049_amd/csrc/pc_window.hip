@@ -564,7 +564,8 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move: use pc_attend_window_static", what);
     plan_items(c, P, true);
     WinLayout L = lay_out(c, P);
-    if (fixed_ws && L.total > PC_STATIC_WS_BYTES) {
+    // (what cannot grow holds the plan without splits, if not the one with them)
+    if (fixed_ws && (L.total > PC_STATIC_WS_BYTES || (!recorded && L.lists > STAGE_BYTES))) {
         plan_items(c, P, false);
         L = lay_out(c, P);
         if (L.total > PC_STATIC_WS_BYTES)

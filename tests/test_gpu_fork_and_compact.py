@@ -255,3 +255,26 @@ def test_captured_streams_are_refused():
     assert (x == 1).all() and s.cache.message_info(z)[1] == 64
     assert s.cache.compact() == 64
     s.cache.close()
+
+
+@pytest.mark.parametrize("dtype,h_kv,D", TYPES)
+def test_many_forks_at_once_and_calls_in_a_row(dtype, h_kv, D):
+    """More forks than a kernel's arguments hold, from the same messages, some turned; and calls that follow each other without a wait."""
+    s = Store(dtype, h_kv, D, 1 << 16)
+    for i, n in enumerate((40, 100, 33)):
+        s.put(n, i)
+    rng = np.random.default_rng(3)
+    whole = [s.message(m) for m in range(3)]
+    lens = (40, 100, 33)
+
+    def one():
+        m = int(rng.integers(0, 3))
+        first = int(rng.integers(0, lens[m]))
+        return m, first, int(rng.integers(1, lens[m] - first + 1)), int(rng.integers(0, 60)), None
+    batches = [[one() for _ in range(n)] for n in (150, 1, 75, 3, 74, 200, 2)]
+    ids = [s.cache.message_fork(b) for b in batches]
+    stores = s.read()
+    for b, got in zip(batches, ids):
+        for (m, first, n, _, _), f in zip(b, got):
+            assert s.same(s.message(f, stores), tuple(x[:, first:first + n].contiguous() for x in whole[m]))
+    s.cache.close()

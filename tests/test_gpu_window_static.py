@@ -101,3 +101,20 @@ def test_pointers_that_are_refused():
     torch.cuda.synchronize()
     assert not any(t.any() for t in x + [lse, dk])
     layer.cache.close()
+
+
+def test_lists_that_a_staging_slot_does_not_hold():
+    """The static form, which cannot grow, says so; the other takes them."""
+    from paper_2512_23049_amd.binding import PC_ERR_NO_SPACE, PcError
+    layer = Layer("bf16", [2] * 340, 2, 2, 128)
+    calls = [([(int(m), 3 * i) for i, m in enumerate(np.random.default_rng(j).permutation(340))], -1, 1100 + j, 1) for j in range(110)]
+    q = layer.normal(110, 2, 128)
+    out, lse = layer.attend(calls, 1 << 20, 0, q)
+    for i in (0, 57, 109):
+        compare("bf16", out[i:i + 1], lse[i:i + 1], *layer.want([calls[i]], 1 << 20, 0, q[i:i + 1]))
+    with pytest.raises(PcError) as e:
+        layer.attend(calls, 1 << 20, 0, q, static=True)
+    assert e.value.code == PC_ERR_NO_SPACE
+    few, few_lse = layer.attend(calls[:40], 1 << 20, 0, q[:40], static=True)
+    compare("bf16", few, few_lse, out[:40].double().cpu().numpy(), lse[:40].double().cpu().numpy())
+    layer.cache.close()
