@@ -28,17 +28,21 @@ template <bool TURN>
 __device__ __forceinline__ void fork_keys_bf16(const PcForkItem &it, const PcForkPiece *pieces, int tile0, int tile1, const uint16_t *src, uint16_t *dst, const float2 *rot)
 {
     const int r = threadIdx.x >> 3, c = threadIdx.x & 7;             // a row, 8 dims and their partners
+    uint4 lo[FORK_TILES], hi[FORK_TILES];
+#pragma unroll
+    for (int t = 0; t < FORK_TILES; ++t) {
+        const int token = (tile0 + t) * PC_TILE + r;
+        lo[t] = hi[t] = make_uint4(0, 0, 0, 0);
+        if (token < it.len) {                            // (tiles behind the last hold no tokens)
+            const uint16_t *p = src + (int64_t)fork_slot(pieces, it.n_pieces, token) * PC_D + 8 * c;
+            lo[t] = ldg16(p); hi[t] = ldg16(p + 64);
+        }
+    }
 #pragma unroll
     for (int t = 0; t < FORK_TILES; ++t) {
         if (tile0 + t >= tile1) break;
-        const int token = (tile0 + t) * PC_TILE + r;
-        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-        if (token < it.len) {
-            const uint16_t *p = src + (int64_t)fork_slot(pieces, it.n_pieces, token) * PC_D + 8 * c;
-            lo = ldg16(p); hi = ldg16(p + 64);
-        }
         if constexpr (TURN) {
-            uint32_t *lw = reinterpret_cast<uint32_t *>(&lo), *hw = reinterpret_cast<uint32_t *>(&hi);
+            uint32_t *lw = reinterpret_cast<uint32_t *>(&lo[t]), *hw = reinterpret_cast<uint32_t *>(&hi[t]);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const float4 cs = *reinterpret_cast<const float4 *>(&rot[8 * c + 2 * u]);
@@ -47,15 +51,54 @@ __device__ __forceinline__ void fork_keys_bf16(const PcForkItem &it, const PcFor
                 hw[u] = pack_bf16(x0 * cs.y + y0 * cs.x, x1 * cs.w + y1 * cs.z);
             }
         }
-        uint16_t *q = dst + ((int64_t)it.slot0 + token) * PC_D + 8 * c;
-        *reinterpret_cast<uint4 *>(q) = lo;
-        *reinterpret_cast<uint4 *>(q + 64) = hi;
+        uint16_t *q = dst + ((int64_t)it.slot0 + (tile0 + t) * PC_TILE + r) * PC_D + 8 * c;
+        *reinterpret_cast<uint4 *>(q) = lo[t];
+        *reinterpret_cast<uint4 *>(q + 64) = hi[t];
+    }
+}
+
+// Eight consecutive groups of a fork that comes from one piece: what its tokens are shifted by within a group is the same everywhere, so
+// that a group of the source, read once, ends one group of the fork and begins the next.
+template <int WORDS>
+__device__ __forceinline__ void shifted_groups(const uint4 (&x)[9], unsigned bits, int len, int g0, int g1, uint16_t *dst)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t y[9] = {x[j].x, x[j].y, x[j].z, x[j].w, x[j + 1].x, x[j + 1].y, x[j + 1].z, x[j + 1].w, 0u};
+        const int n = len - 8 * (g0 + j);
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            w[k] = __builtin_amdgcn_alignbit(y[k + WORDS + 1], y[k + WORDS], bits);
+            if (n < 8) w[k] &= (2 * k < n ? 0xFFFFu : 0u) | (2 * k + 1 < n ? 0xFFFF0000u : 0u);         // what lies behind the last token is another's
+        }
+        if (g0 + j < g1) *reinterpret_cast<uint4 *>(dst + (int64_t)j * PC_D * PC_VGROUP) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
 __device__ __forceinline__ void fork_values_bf16(const PcForkItem &it, const PcForkPiece *pieces, int tile0, int tile1, const uint16_t *src, uint16_t *dst)
 {
     const int d = threadIdx.x & 127, half = threadIdx.x >> 7;       // a dimension; (the group is the same for all lanes of a wave)
+    if (it.n_pieces == 1) {
+        static_assert(FORK_TILES == 4, "a half of the workgroup takes eight groups");
+        const int g0 = 4 * tile0 + 8 * half, sh = pieces[0].slot & 7;
+        const uint16_t *p = src + ((int64_t)((pieces[0].slot >> 3) + g0) * PC_D + d) * PC_VGROUP;
+        uint16_t *q = dst + ((int64_t)(it.slot0 / PC_VGROUP + g0) * PC_D + d) * PC_VGROUP;
+        uint4 x[9];
+#pragma unroll
+        for (int j = 0; j < 9; ++j) {                    // (a group's first token that is wanted: 8 (g0 + j) - sh)
+            x[j] = make_uint4(0, 0, 0, 0);
+            if (j == 0 ? 8 * g0 < it.len : 8 * (g0 + j) - sh < it.len && (j < 8 || sh > 0)) x[j] = ldg16(p + (int64_t)j * PC_D * PC_VGROUP);
+        }
+        const unsigned bits = 16u * (unsigned)(sh & 1);
+        switch (sh >> 1) {
+        case 0: shifted_groups<0>(x, bits, it.len, g0, 4 * tile1, q); break;
+        case 1: shifted_groups<1>(x, bits, it.len, g0, 4 * tile1, q); break;
+        case 2: shifted_groups<2>(x, bits, it.len, g0, 4 * tile1, q); break;
+        default: shifted_groups<3>(x, bits, it.len, g0, 4 * tile1, q); break;
+        }
+        return;
+    }
     for (int g = 4 * tile0 + half; g < 4 * tile1; g += 2) {
         const int t0 = 8 * g, n = min(8, it.len - t0);
         uint32_t w[4] = {0u, 0u, 0u, 0u};
