@@ -106,7 +106,7 @@ int32_t add_runs(WinPlan &P, const WinCall &wc, int32_t row0, int32_t row1)
 struct Group { int32_t call, unit0, run0, tiles; };
 
 // target: workgroups (of all KV heads) that fill the chip; least: tiles a split is worth
-void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups, std::vector<PcWinItem> &items, int64_t target, int32_t least, bool may_split, bool fit)
+void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups, std::vector<PcWinItem> &items, int64_t target, int32_t least, bool may_split, bool fit, bool tokens)
 {
     const int H_kv = c->cfg.n_kv_heads;
     int64_t all = 0;
@@ -115,7 +115,10 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
     int64_t chunk = may_split ? std::max<int64_t>(least, (all * H_kv + target - 1) / target) : INT32_MAX;            // (INT32_MAX: one)
     // (many groups: to the nearest, as one a little longer than the others is not worth a merge of its own)
     bool nearest = true;
-    auto splits = [&](int32_t tiles) { return (int32_t)std::max<int64_t>(1, std::min<int64_t>((tiles + (nearest ? chunk / 2 : chunk - 1)) / chunk, MAX_SPLITS)); };
+    auto splits = [&](int32_t tiles) {
+        if (tokens && tiles <= least + least / 2) return 1;           // (10 tiles whole 8.0 us, halved 9.5, with the merge)
+        return (int32_t)std::max<int64_t>(1, std::min<int64_t>((tiles + (nearest ? chunk / 2 : chunk - 1)) / chunk, MAX_SPLITS));
+    };
     // fit: where whole groups have room at once, their splits get it too, and the longest is as short as that allows (fp32, two
     // calls of 100 to 500 rows, window 333, 2 KV heads: 17.2 -> 14.2 us; four single tokens of 17 tiles: 8.7 -> 7.7 us).  Not the bf16 blocks of rows, whose splits
     // pay for every run they touch: 33 groups of 20 tiles, 8 KV heads, take 47 us as 528 workgroups where 512 have room, 51 as 368.
@@ -167,7 +170,8 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
 {
     const int H = c->cfg.n_kv_heads, g = c->g, per = 16 / g;
     const int32_t n_calls = (int32_t)dec.size(), n_groups = (n_calls + per - 1) / per;
-    if (n_groups < 3) return false;                      // (waves without columns would have every fourth step at most)
+    // (with two groups, waves would have every fourth step at most)
+    if (c->decode_sharing == 1 || n_calls < 2 || (c->decode_sharing == 0 && n_groups < 3)) return false;
     const bool wide = n_groups > PC_WIN_GROUPS / 2;
     const int32_t set_calls = std::min(n_groups, wide ? PC_WIN_GROUPS : PC_WIN_GROUPS / 2) * per, n_sets = (n_calls + set_calls - 1) / set_calls;
     struct Piece { int32_t slot0, tiles; size_t run; int32_t call; };
@@ -206,12 +210,12 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
         }
         of_set.push_back({first, pieces.size()});
     }
-    // A tile costs a workgroup that shares it about three times what it costs a call on its own (whose loads nothing holds up), and a
-    // workgroup's partial rows are worth 8 tiles (16 with 16 waves).  Calls over 410 of 512 messages, window 16 384, 8 heads a KV head, call by call and
-    // shared: 12 calls (2.6 calls a tile) 133 and 147 us, 16 (3.4) 172 and 162, 24 (4.9) 271 and 191, 32 (6.6) 312 and 217; 4 heads: 12 calls
-    // 134 and 156, 16 171 and 170, 48 (9.8) 519 and 235.  Window 2048 (1.5 calls a tile), 32 calls: 57 and 144.
+    // Microseconds of both ways, of the tiles that calls see on their own and of those that are distinct (8 heads a KV head; calls over 410 of
+    // 512 messages, window 16 384: 8 calls 94 on their own and 130 shared, 12 calls 133 and 147, 16 172 and 162, 24 271 and 191, 32 312 and 217;
+    // 16 calls over 24 of 48 messages, window 4096, 45 and 72).  By the caller's word: pc_set_decode_sharing.
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
-    if (own < 3 * shared + bins * n_sets * (wide ? 16 : 8)) return false;
+    const double heads = H / 8.0, alone = 8 + 0.0175 * (double)own * heads, together = 48 + (0.0227 * (double)shared + 0.0055 * (double)own) * heads;
+    if (shared == 0 || (c->decode_sharing == 0 && alone <= together)) return false;
     std::vector<std::pair<int32_t, PcWinSee>> seen;      // (call within the set, view) of the visit at hand
     for (int32_t s = 0; s < n_sets; ++s) {
         const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
@@ -281,7 +285,8 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
 }
 
 // the rows of a call that units [unit0, unit0 + n) of the bf16 kernels, or block unit0 of 32 columns of the fp32 kernels, hold
-void plan_items(const pc_cache *c, WinPlan &P, bool may_split)
+// least: tiles that a split of a single token is worth
+void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8)
 {
     const int g = c->g;
     P.pre.clear(); P.dec.clear(); P.runs.clear(); P.rots.clear(); P.merge.clear();
@@ -313,7 +318,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split)
             }
         }
     }
-    make_items(c, P, pre, P.pre, 512, c->cfg.dtype == PC_F32 ? 4 : 6, may_split, c->cfg.dtype == PC_F32);
+    make_items(c, P, pre, P.pre, 512, c->cfg.dtype == PC_F32 ? 4 : 6, may_split, c->cfg.dtype == PC_F32, false);
     if (c->cfg.dtype == PC_F32) return;
     const size_t runs = P.runs.size(), rots = P.rots.size(), merge = P.merge.size();
     const int64_t part_rows = P.part_rows;
@@ -326,7 +331,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split)
     if (may_split && plan_shared(c, P, dec)) { P.runs.resize(runs); return; }
     no_shared();
     P.merge.resize(merge); P.part_rows = part_rows;
-    make_items(c, P, dec, P.dec, 512, 8, may_split, true);
+    make_items(c, P, dec, P.dec, 512, least, may_split, true, true);
 }
 
 // lists as they are staged, then what the device makes of them
@@ -421,7 +426,7 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
             }
         }
     }
-    make_items(c, P, groups, P.pre, 512, 6, true, f32);
+    make_items(c, P, groups, P.pre, 512, 6, true, f32, false);
 
     // keys: who lists each extent, extents in slot order
     struct Listed { int32_t slot0; uint32_t call, seg; };
@@ -564,6 +569,19 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move: use pc_attend_window_static", what);
     plan_items(c, P, true);
     WinLayout L = lay_out(c, P);
+    // Lists of single tokens that their launch's arguments do not hold cost a launch in front of it and the event behind that, 7 us: a few
+    // longer splits are better where that helps (4 calls of 130 tiles: 22.5 -> 16.5 us; 16 of 17: 19 -> 12).
+    const size_t whole = sizeof(PcWinRun) * P.runs.size() + (sizeof(PcWinItem) + sizeof(int32_t)) * P.calls.size();
+    if (L.lists > PC_ARG_BYTES && whole + 64 <= PC_ARG_BYTES && P.pre.empty() && P.sh_items.empty()) {
+        for (int32_t least = 16; least <= 40 && L.lists > PC_ARG_BYTES; least += 8) {
+            plan_items(c, P, true, least);
+            L = lay_out(c, P);
+        }
+        if (L.lists > PC_ARG_BYTES) {
+            plan_items(c, P, true);
+            L = lay_out(c, P);
+        }
+    }
     // (what cannot grow holds the plan without splits, if not the one with them)
     if (fixed_ws && (L.total > PC_STATIC_WS_BYTES || (!recorded && L.lists > STAGE_BYTES))) {
         plan_items(c, P, false);

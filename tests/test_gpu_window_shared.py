@@ -1,6 +1,6 @@
 """pc_attend_window for single tokens of many calls over the same messages, which read every tile once (a workgroup multiplies it with
-the queries of all calls that see it), against the fp64 oracle.  Whether calls go that way depends on how much they share; the batches
-here share most of what they see, and the last test's does not."""
+the queries of all calls that see it), against the fp64 oracle.  Whether calls go that way by themselves is a matter of cost; here they are
+told to (pc_set_decode_sharing)."""
 import numpy as np
 import pytest
 
@@ -36,6 +36,7 @@ def test_calls_that_share_their_messages(h_q, h_kv, n_calls):
     rng = np.random.default_rng(n_calls)
     own = [int(x) for x in rng.integers(1, 40, size=(n_calls + 2) // 3)]
     layer = Layer("bf16", LENS + own, h_q, h_kv, 128)
+    layer.cache.set_decode_sharing(2)
     calls = agents(rng, n_calls, len(LENS), LENS, len(LENS))
     for window, n_sink in [(1 << 30, 0), (900, 5), (700, 64), (2031, 300)]:
         run(layer, calls, window, n_sink)
@@ -49,6 +50,7 @@ def test_long_and_short_messages_and_calls_that_see_little():
     rng = np.random.default_rng(5)
     lens = [3000, 1, 2500, 1, 33, 1900] + [20] * 4
     layer = Layer("bf16", lens, 16, 2, 128)
+    layer.cache.set_decode_sharing(2)
     base = [(0, 0), (1, 3000), (2, 3001), (3, 5501), (4, 5502), (5, 5535)]
     calls = [(base, 6 + i % 4, 7435 + i, 1) for i in range(20)]
     calls[3:3] = [([(5, 0)], -1, 1900, 1), ([(0, 0)], -1, 0, 1, [10 ** 6]), (base[:2], -1, 0, 40, list(range(2900, 2940))), ([], 7, 0, 1), (base[::-1], -1, 9000, 1)]
@@ -67,6 +69,7 @@ def test_what_is_not_finite_stays_with_the_calls_that_see_it():
             vs[m][5::9, :, i::5] = [np.inf, np.nan, -np.inf][i]
             ks[m][3::11, 0, 5] = [np.nan, np.inf, np.nan][i]
     layer = Layer("bf16", [300] * 9 + [40], 16, 2, 128, spoil=spoil)
+    layer.cache.set_decode_sharing(2)
     whole = [(m, 300 * m) for m in range(9)]
     clean = [e for e in whole if e[0] not in (1, 4, 7)]
     calls = [(whole if i % 3 == 2 else clean, 9 if i % 2 else -1, 2700, 1) for i in range(33)]
@@ -87,11 +90,17 @@ def test_each_way_gives_the_same():
     """A batch that shares its messages, and each of its calls alone."""
     rng = np.random.default_rng(9)
     layer = Layer("bf16", LENS, 16, 2, 128)
+    layer.cache.set_decode_sharing(2)
     calls = [c for c in agents(rng, 24, len(LENS), LENS, 0) if c[1] < 0]
     q = layer.normal(len(calls), 16, 128)
     for window, n_sink in [(1 << 30, 0), (800, 10)]:
+        layer.cache.set_decode_sharing(2)
         out, lse = layer.attend(calls, window, n_sink, q)
         again, _ = layer.attend(calls, window, n_sink, q)
+        layer.cache.set_decode_sharing(1)
+        own, own_lse = layer.attend(calls, window, n_sink, q)
+        layer.cache.set_decode_sharing(0)
+        assert (out.float() - own.float()).abs().max().item() <= 4e-2 and (lse - own_lse).abs().max().item() <= 2 * 2.0 ** -8
         assert bool((out == again).all())                # (no sum depends on an order that is not fixed)
         for i, c in enumerate(calls):
             o, l = layer.attend([c], window, n_sink, q[i:i + 1])

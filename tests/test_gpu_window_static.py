@@ -34,6 +34,7 @@ def batches():
 def test_replays_give_the_eager_bits(dtype, h_q, h_kv, D, which):
     import torch
     layer = Layer(dtype, LENS + [40, 90], h_q, h_kv, D)
+    layer.cache.set_decode_sharing(2 if which == "shared messages" else 0)
     calls = batches()[which]
     rows, window, n_sink = layer.rows(calls), 700, 5
     qs = [layer.normal(rows, h_q, D) for _ in range(4)]
