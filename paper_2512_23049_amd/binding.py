@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -274,11 +275,11 @@ class Cache:
     def message_fork(self, forks, stream: int = 0):
         """forks: (message, first token, tokens, reserve, base or None to keep the keys turned as they are); the new ids."""
         n = len(forks)
-        arr, ids = (pc_fork * max(n, 1))(), (C.c_int32 * max(n, 1))()
-        for j, (m, first, length, reserve, base) in enumerate(forks):
-            arr[j] = pc_fork(int(m), int(first), int(length), int(reserve), PC_POS_AUTO if base is None else int(base))
-        self._check(lib().pc_message_fork(self.h, arr, n, ids, stream or None))
-        return [ids[i] for i in range(n)]
+        ids = (C.c_int32 * max(n, 1))()
+        # (all of the lists at once: a structure a fork takes 0.6 us)
+        items = array("i", [x for m, first, length, reserve, base in forks for x in (m, first, length, reserve, PC_POS_AUTO if base is None else base)])
+        self._check(lib().pc_message_fork(self.h, C.cast(items.buffer_info()[0], C.POINTER(pc_fork)), n, ids, stream or None))
+        return ids[:n]
 
     def compact(self, max_slots: int = 0, stream: int = 0) -> int:
         moved = C.c_int64(0)
