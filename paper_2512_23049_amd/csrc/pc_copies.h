@@ -46,6 +46,7 @@ struct PcCompact {
 // items, pieces: staged, or (blob not null) in the arguments, the pieces behind the items; max_rows: the longest fork's
 void pc_launch_fork(int dtype, const PcArgBlob *blob, const PcForkItem *items, const PcForkPiece *pieces, int n, int max_rows, int n_kv_heads, int D, int64_t slots,
                     const double *inv_freq, void *k_store, void *v_store, PcMsgEntry *table, hipStream_t st);
-void pc_launch_compact(const PcCompact &C, hipStream_t st);
+// blob: its lists, the moves behind the tiles (C.tiles and C.moves are not read then), or null
+void pc_launch_compact(const PcCompact &C, const PcArgBlob *blob, hipStream_t st);
 
 #endif

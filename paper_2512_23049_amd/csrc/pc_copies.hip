@@ -168,7 +168,10 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
             PC_HIP(c, hipMemsetAsync(c->flags_dev, 0, sizeof(uint32_t) * c->flag_words, st));
             c->tickets = 0; c->flag_epoch = 0;
         }
-        const int32_t rc = fetch_items(c, lists.data(), lists.size(), st);
+        const bool in_args = lists.size() <= PC_ARG_BYTES;
+        PcArgBlob blob;
+        if (in_args) std::memcpy(blob.w, lists.data(), lists.size());
+        const int32_t rc = in_args ? PC_OK : fetch_items(c, lists.data(), lists.size(), st);
         if (rc != PC_OK) return rc;
         C.tiles = (const PcCompactTile *)c->tok_dev; C.moves = (const PcCompactMove *)((char *)c->tok_dev + at_moves);
         C.epoch = c->flag_epoch + 1; C.ticket0 = c->tickets;
@@ -177,7 +180,7 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
         C.head_bytes = c->slots * c->D * (int64_t)c->esize; C.tile_bytes = tile_bytes;
         C.table = c->table_dev;
         ProfScope ps(c, 7, st);
-        pc_launch_compact(C, st);
+        pc_launch_compact(C, in_args ? &blob : nullptr, st);
         PC_HIP(c, hipGetLastError());
         c->flag_epoch = C.epoch;
         c->tickets += (uint32_t)C.n_chunks;

@@ -242,7 +242,7 @@ void pc_launch_fork(int dtype, const PcArgBlob *blob, const PcForkItem *items, c
 // Bound: memory.  512 messages of 160 tokens, 8 KV heads: 650 MB read and written in 145 us (4.5 TB/s); 64 KB a workgroup and one counter
 // for all stores 174 us, 32 KB 330 (a counter gives 70 numbers a microsecond); kept in the caches like other data 5 % more.
 // Flags hold the launch's number and the counter goes on from launch to launch, so that nothing has to be cleared.
-__global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_kernel(PcCompact C)
+__device__ __forceinline__ void compact_chunk(const PcCompact &C)
 {
     __shared__ uint32_t s_ticket;
     const int store = (int)(blockIdx.x % (unsigned)C.n_stores), H = C.n_stores / 2;
@@ -285,7 +285,19 @@ __global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_kernel(PcCompac
     }
 }
 
-void pc_launch_compact(const PcCompact &C, hipStream_t st)
+__global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_kernel(PcCompact C) { compact_chunk(C); }
+__global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_arg_kernel(PcArgBlob, PcCompact C)
 {
-    if (C.n_chunks > 0) pc_compact_kernel<<<(unsigned)(C.n_chunks * C.n_stores), PC_COMPACT_THREADS, 0, st>>>(C);
+    const char *lists = (const char *)__builtin_amdgcn_kernarg_segment_ptr();          // (the blob comes first)
+    C.tiles = reinterpret_cast<const PcCompactTile *>(lists);
+    C.moves = reinterpret_cast<const PcCompactMove *>(C.tiles + C.n_tiles);
+    compact_chunk(C);
+}
+
+void pc_launch_compact(const PcCompact &C, const PcArgBlob *blob, hipStream_t st)
+{
+    if (C.n_chunks <= 0) return;
+    const unsigned grid = (unsigned)(C.n_chunks * C.n_stores);
+    if (blob) pc_compact_arg_kernel<<<grid, PC_COMPACT_THREADS, 0, st>>>(*blob, C);
+    else pc_compact_kernel<<<grid, PC_COMPACT_THREADS, 0, st>>>(C);
 }
