@@ -21,7 +21,7 @@ __device__ __forceinline__ int fork_slot(const PcForkPiece *pieces, int n, int t
 // frequency (whose 64 or 32 rotations the workgroup makes once); values of a bf16 cache lie in groups of eight tokens by
 // dimension, so that eight tokens from the middle of a group are two 16-byte reads and a shift.  Bound: memory; 16-byte
 // accesses of consecutive lanes, all loads of a tile in front of its first store: 32 forks of 950 tokens, 8 KV heads, 250 MB
-// read and written in 62 us (4.0 TB/s; a large copy 4.95); one fork of 200 tokens 7.7 us.
+// read and written in 62 us (4.0 TB/s; a large copy 4.95); one fork of 200 tokens 5.4 us.
 #define FORK_TILES 4
 
 template <bool TURN>

@@ -12,6 +12,11 @@
 //
 // Rotations.  dq is collected in the frame of the present run's keys and turned when the rotation changes; dk in the frame of the
 // turned queries, in which a call's keys are turned once.
+//
+// Few keys.  Those keys are rounded once more than in the forward, so that a row's probabilities do not add up to 1: of two
+// keys, that is as much as what the gradient is left with when Delta is taken off (dk 5.4e-3 off in the 2-norm; 4e-3 from 50 keys
+// up).  Where window and sinks are 32 at most, the queries are turned for each extent as the forward turns them, and keys stay as they
+// are stored: the same scores, and dk in the stored keys' frame.
 #include "pc_window.h"
 #include "pc_bwd_tiles.h"
 #include <type_traits>
@@ -128,7 +133,7 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
     }
     delta += __shfl_xor(delta, 1); delta += __shfl_xor(delta, 2); delta += __shfl_xor(delta, 4);
     const int64_t to = (unit * 32 + r) * D + PER * c;
-    put(B.q_abs, to, x); put(B.q_abs, to + HALF, y);
+    if (!B.turned) { put(B.q_abs, to, x); put(B.q_abs, to + HALF, y); }
     put(B.d_o, to, gx); put(B.d_o, to + HALF, gy);
     const int lo = win_low(W.q_pos[R], W.window);
     char *const st = B.stat + unit * PC_WIN_STAT_BYTES;
@@ -163,6 +168,41 @@ void pc_launch_win_bwd_prep(const PcWin &W, const PcWinBwd &B, int dtype, int D,
     if (dtype == 1) pc_win_bwd_prep_kernel<128, true><<<grid, 256, 0, st>>>(W, B);
     else if (D == 64) pc_win_bwd_prep_kernel<64, false><<<grid, 256, 0, st>>>(W, B);
     else pc_win_bwd_prep_kernel<128, false><<<grid, 256, 0, st>>>(W, B);
+}
+
+// The forward's queries of a block for one extent: the same numbers (row by row, scale included) that its scores were made of.
+__global__ __launch_bounds__(256) void pc_win_bwd_turned_kernel(PcWin W, PcWinBwd B)
+{
+    const PcWinTurned t = B.turned[blockIdx.x];
+    const PcWinBlock blk = B.blocks[t.block];
+    const int r = threadIdx.x >> 3, c = threadIdx.x & 7;             // a row, eight pairs
+    const int64_t h = blockIdx.y, R = (int64_t)blk.q_off + min(32 * (int64_t)blk.block + r, (int64_t)blk.n_q - 1);
+    const bool some = B.lse[R * W.n_q_heads + h] > -INFINITY;
+    const uint16_t *q = (const uint16_t *)W.q + (R * W.n_q_heads + h) * PC_D + 8 * c;
+    const uint4 lq = ldg16(q), hq = ldg16(q + 64);
+    const uint4 *rq = reinterpret_cast<const uint4 *>(W.rot_lanes) + ((R >> 5) * 16 + (c >> 1) * 4 + (c & 1)) * 32 + (R & 31);
+    const uint4 p0 = rq[0], p1 = rq[64];
+    const float4 *rr = reinterpret_cast<const float4 *>(W.rot_run + (int64_t)t.rot * (PC_D / 2) + 8 * c);
+    const uint32_t lw[4] = {lq.x, lq.y, lq.z, lq.w}, hw[4] = {hq.x, hq.y, hq.z, hq.w}, pw[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+    uint32_t a[4], b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float4 p = make_float4(f16_lo(pw[2 * j]), f16_hi(pw[2 * j]), f16_lo(pw[2 * j + 1]), f16_hi(pw[2 * j + 1]));
+        float4 r4 = rr[j];
+        r4.x *= W.scale_log2; r4.y *= W.scale_log2; r4.z *= W.scale_log2; r4.w *= W.scale_log2;
+        const float c0 = p.x * r4.x + p.y * r4.y, s0 = p.y * r4.x - p.x * r4.y, c1 = p.z * r4.z + p.w * r4.w, s1 = p.w * r4.z - p.z * r4.w;
+        const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
+        a[j] = some ? pack_bf16(x0 * c0 - y0 * s0, x1 * c1 - y1 * s1) : 0u;
+        b[j] = some ? pack_bf16(x0 * s0 + y0 * c0, x1 * s1 + y1 * c1) : 0u;
+    }
+    uint16_t *to = (uint16_t *)B.q_abs + (((int64_t)blockIdx.x * W.n_q_heads + h) * 32 + r) * PC_D + 8 * c;
+    *reinterpret_cast<uint4 *>(to) = make_uint4(a[0], a[1], a[2], a[3]);
+    *reinterpret_cast<uint4 *>(to + 64) = make_uint4(b[0], b[1], b[2], b[3]);
+}
+
+void pc_launch_win_bwd_turned(const PcWin &W, const PcWinBwd &B, hipStream_t st)
+{
+    if (B.n_turned > 0) pc_win_bwd_turned_kernel<<<dim3((unsigned)B.n_turned, (unsigned)W.n_q_heads), 256, 0, st>>>(W, B);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- dq
@@ -432,10 +472,11 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
         const bool active = valid > 0;
         const int U = app.n_blocks * g;
         int64_t next = (int64_t)app.block0 * W.n_q_heads + kh * g;       // the unit to ask for, and its head within the group
+        const int64_t q_ahead = ((int64_t)app.q0 - app.block0) * W.n_q_heads;
         int next_j = 0, next_slot = 0;
         auto request = [&]() __attribute__((always_inline)) {
             const unsigned to = ring + next_slot * SLOT + wave * 1024;
-            dma16((const unsigned char *)B.q_abs + next * TILE_BYTES, src, to);
+            dma16((const unsigned char *)B.q_abs + (next + q_ahead) * TILE_BYTES, src, to);
             dma16((const unsigned char *)B.d_o + next * TILE_BYTES, src, to + TILE_BYTES);
             if (!K && wave == 0) dma16(B.stat + next * PC_WIN_STAT_BYTES, lane * 16, to + 2 * TILE_BYTES);
             ++next; ++next_j;
@@ -478,7 +519,7 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float4 r = rr[8 * ks + j];
-                        r.x *= W.scale_log2; r.y *= W.scale_log2; r.z *= W.scale_log2; r.w *= W.scale_log2;
+                        r.x *= B.k_factor; r.y *= B.k_factor; r.z *= B.k_factor; r.w *= B.k_factor;
                         const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
                         x[j] = pack_bf16(x0 * r.x - y0 * r.y, x1 * r.z - y1 * r.w);
                         y[j] = pack_bf16(x0 * r.y + y0 * r.x, x1 * r.w + y1 * r.z);
@@ -608,7 +649,7 @@ __global__ __launch_bounds__(512, 2) void pc_win_bwd_keys_bf16_kernel(PcWin W, P
                 const float c[4] = {a0.x, a0.z, a1.x, a1.z}, s[4] = {a0.y, a0.w, a1.y, a1.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float x = acc[db][4 * q4 + j] * B.scale, y = acc[db + 2][4 * q4 + j] * B.scale;
+                    const float x = acc[db][4 * q4 + j] * B.key_scale, y = acc[db + 2][4 * q4 + j] * B.key_scale;
                     acc[db][4 * q4 + j] = x * c[j] + y * s[j];
                     acc[db + 2][4 * q4 + j] = y * c[j] - x * s[j];
                 }

@@ -96,8 +96,11 @@ struct PcWinApp {
     int32_t rot;              // row of the rotation table
     int32_t self;             // 1: the call's new message
     int32_t block0, n_blocks; // the blocks that may see some of the item's tokens
-    int32_t pad;
+    int32_t q0;               // their queries, in units' blocks: block0, or the first of those turned for this call's rotation
 };
+#define PC_WIN_FEW 32
+// Rows of few keys (window and sinks, PC_WIN_FEW at most): a block's queries turned for one listed extent, as the forward turns them.
+struct PcWinTurned { int32_t block, rot; };
 #define PC_WIN_KEY_TILES 4
 struct PcWinKeyItem {         // up to four tiles of an extent, and calls (or some of their blocks) that see them
     int32_t slot0;
@@ -121,7 +124,8 @@ struct PcWinBwd {
     const PcWinKeyItem *key_items;
     const PcWinSum     *sums;
     const int32_t      *bins; // [n_bins + 1] the first of each workgroup's items
-    int32_t n_blocks, n_bins, n_sums, pad;
+    int32_t n_blocks, n_bins, n_sums, n_turned;
+    const PcWinTurned *turned;        // null: queries are turned by their positions, keys by their extents'
     const void  *out, *d_out;
     const float *lse;
     float       *delta;       // [rows][H_q]
@@ -131,8 +135,10 @@ struct PcWinBwd {
     float       *key_part;    // [part][KV head][keys, values][128][D]
     float       *d_q, *d_k, *d_v;
     float        scale;
+    float        k_factor, key_scale;         // bf16 keys: what rides on the keys for the scores, and on their gradients
 };
 void pc_launch_win_bwd_prep(const PcWin &W, const PcWinBwd &B, int dtype, int D, hipStream_t st);
+void pc_launch_win_bwd_turned(const PcWin &W, const PcWinBwd &B, hipStream_t st);
 void pc_launch_win_bwd_dq_bf16(const PcWin &W, const PcWinBwd &B, int n_items, hipStream_t st);
 void pc_launch_win_bwd_dq_f32(const PcWin &W, const PcWinBwd &B, int n_items, int D, hipStream_t st);
 // the splits of a row's gradient, added up in their order

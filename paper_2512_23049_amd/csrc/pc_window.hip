@@ -378,6 +378,7 @@ struct BwdPlan {
     std::vector<PcWinApp> apps;
     std::vector<PcWinKeyItem> keys;
     std::vector<PcWinSum> sums;
+    std::vector<PcWinTurned> turned;
     std::vector<int32_t> bins;                           // the first of each workgroup's items of keys, and their end
     int32_t parts = 0;
 };
@@ -465,13 +466,25 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
                     if (P.rots.empty() || P.rots.back() != s.rot_pos) P.rots.push_back(s.rot_pos);
                     s.rot = (int32_t)P.rots.size() - 1;
                 }
-                apps.push_back(PcWinApp{s.start + first, end - first, sinks, s.rot, s.self ? 1 : 0, block0[listed[k].call] + b0 - rg.x, b1 - b0, 0});
+                apps.push_back(PcWinApp{s.start + first, end - first, sinks, s.rot, s.self ? 1 : 0, block0[listed[k].call] + b0 - rg.x, b1 - b0, block0[listed[k].call] + b0 - rg.x});
                 t.blocks += b1 - b0;
             }
             t.n_apps = apps.size() - t.app0;
             if (t.n_apps > 0) all.push_back(t);
         }
         a = b;
+    }
+    // Rows of few keys: the forward's queries for every extent (see the kernels), if that is not too many times the blocks.
+    int64_t visits = 0;
+    for (const PcWinApp &a : apps) visits += a.n_blocks;
+    if (!f32 && (int64_t)P.window + P.n_sink <= PC_WIN_FEW && visits <= 8 * (int64_t)B.blocks.size()) {
+        const int32_t none = (int32_t)P.rots.size();
+        P.rots.push_back(0);                             // (keys as they are stored: turned by nothing)
+        for (PcWinApp &a : apps) {
+            a.q0 = (int32_t)B.turned.size();
+            for (int32_t b = 0; b < a.n_blocks; ++b) B.turned.push_back(PcWinTurned{a.block0 + b, a.rot});
+            a.rot = none;
+        }
     }
     // The items go to as many workgroups as run at once (a further one would wait for a place in a part of the chip that is not the
     // first to have one): the longest first, each to the workgroup with the least.  Tiles with more than a share of the work (those
@@ -499,7 +512,7 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
                 while (done < upto) {
                     const int32_t m = (int32_t)std::min<int64_t>(apps[k].n_blocks - taken, upto - done);
                     PcWinApp app = apps[k];
-                    app.block0 += taken; app.n_blocks = m;
+                    app.block0 += taken; app.q0 += taken; app.n_blocks = m;
                     K.apps.push_back(app);
                     done += m; taken += m;
                     if (taken == apps[k].n_blocks) { ++k; taken = 0; }
@@ -679,11 +692,11 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 16); return a; };
     auto of = [](const auto &v) { return sizeof(v[0]) * v.size(); };
     const size_t items = take(of(P.pre)), runs = take(of(P.runs)), merge = take(of(P.merge)), q_pos = take(of(P.q_pos)), rots = take(of(P.rots));
-    const size_t blocks = take(of(B.blocks)), apps = take(of(B.apps)), keys = take(of(B.keys)), sums = take(of(B.sums)), bins = take(of(B.bins)), lists = at;
+    const size_t blocks = take(of(B.blocks)), apps = take(of(B.apps)), keys = take(of(B.keys)), sums = take(of(B.sums)), bins = take(of(B.bins)), turned = take(of(B.turned)), lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = sizeof(float2) * (size_t)c->half, units = B.blocks.size() * (size_t)(bf16 ? Hq : H), unit = 32 * (size_t)c->D * c->esize;
     const size_t rot_lanes = big(bf16 ? rot / 2 * align_up(P.q_pos.size(), 32) : 0), rot_q = big(rot * P.q_pos.size()), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * P.q_pos.size() * (size_t)Hq);
-    const size_t q_abs = big(unit * units), d_o = big(unit * units), stat = big(PC_WIN_STAT_BYTES * units);
+    const size_t q_abs = big(B.turned.empty() ? unit * units : unit * B.turned.size() * (size_t)Hq), d_o = big(unit * units), stat = big(PC_WIN_STAT_BYTES * units);
     const size_t part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)Hq * (size_t)c->D);
     const size_t key_part = big(sizeof(float) * 2 * PC_WIN_KEY_TILES * PC_TILE * (size_t)B.parts * (size_t)H * (size_t)c->D);
     int32_t rc = pc_ensure_ws(c, align_up(at, 256), st);
@@ -699,7 +712,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     char *from = in_args ? (char *)blob.w : (char *)slot->host;
     auto put = [&](size_t to, const auto &v) { if (!v.empty()) std::memcpy(from + to, v.data(), of(v)); };
     put(items, P.pre); put(runs, P.runs); put(merge, P.merge); put(q_pos, P.q_pos); put(rots, P.rots);
-    put(blocks, B.blocks); put(apps, B.apps); put(keys, B.keys); put(sums, B.sums); put(bins, B.bins);
+    put(blocks, B.blocks); put(apps, B.apps); put(keys, B.keys); put(sums, B.sums); put(bins, B.bins); put(turned, B.turned);
 
     W.items = (const PcWinItem *)(ws + items); W.runs = (const PcWinRun *)(ws + runs); W.q_pos = (const int32_t *)(ws + q_pos);
     W.rot_q = (const float2 *)(ws + rot_q); W.rot_lanes = (const uint32_t *)(ws + rot_lanes); W.rot_run = (const float2 *)(ws + rot_run);
@@ -707,6 +720,9 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     G.blocks = (const PcWinBlock *)(ws + blocks); G.apps = (const PcWinApp *)(ws + apps);
     G.key_items = (const PcWinKeyItem *)(ws + keys); G.sums = (const PcWinSum *)(ws + sums); G.bins = (const int32_t *)(ws + bins);
     G.n_blocks = (int32_t)B.blocks.size(); G.n_bins = std::max<int32_t>(0, (int32_t)B.bins.size() - 1); G.n_sums = (int32_t)B.sums.size();
+    G.turned = B.turned.empty() ? nullptr : (const PcWinTurned *)(ws + turned); G.n_turned = (int32_t)B.turned.size();
+    G.k_factor = G.turned ? 1.f : W.scale_log2;
+    G.key_scale = G.turned ? 0.6931471805599453f : c->scale;              // (the queries bring the scale, and log2 e)
     G.delta = (float *)(ws + delta); G.q_abs = ws + q_abs; G.d_o = ws + d_o; G.stat = ws + stat; G.key_part = (float *)(ws + key_part);
     PcWinTurns T{};
     T.from = in_args ? ws : slot->host; T.ws = ws; T.n16 = (int)(lists / 16);
@@ -719,6 +735,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     PC_HIP(c, hipGetLastError());
     if (slot) { rc = pc_stage_release(c, slot, st); if (rc != PC_OK) return rc; }
     pc_launch_win_bwd_prep(W, G, c->cfg.dtype, c->D, st);
+    pc_launch_win_bwd_turned(W, G, st);
     if (bf16) pc_launch_win_bwd_dq_bf16(W, G, (int)P.pre.size(), st);
     else pc_launch_win_bwd_dq_f32(W, G, (int)P.pre.size(), c->D, st);
     pc_launch_win_bwd_rows(W, G, (const PcMergeRow *)(ws + merge), (int)P.merge.size(), c->D, st);
@@ -759,7 +776,7 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
     // Runs of blocks whose workspace fits.  A run ends with a call, or where units and rows end together: after four blocks of 32 rows
     // (a workgroup's units), or the columns of 32 rows.
     const int64_t per_block = (int64_t)(bf16 ? c->cfg.n_q_heads : c->cfg.n_kv_heads) * (2 * 32 * c->D * (int64_t)c->esize + PC_WIN_STAT_BYTES);
-    const int64_t step = bf16 ? 4 : c->g, most = std::max<int64_t>(step, (int64_t)BWD_BYTES / per_block / step * step);
+    const int64_t step = bf16 ? 4 : c->g, most = std::max<int64_t>(step, (int64_t)BWD_BYTES / per_block / (bf16 && (int64_t)window + n_sink <= PC_WIN_FEW ? 4 : 1) / step * step);
     std::vector<int2> range(P.calls.size(), make_int2(0, 0));
     int64_t in_run = 0;
     for (size_t i = 0; i < P.calls.size(); ++i) {
