@@ -71,6 +71,8 @@ __device__ __forceinline__ void turn_columns(f32x16 (&acc)[4], const float2 *a, 
 // -------------------------------------------------------------------------------------------------------------- prep
 // bf16: a block of 32 rows of a head, eight threads a row; fp32: 32 (row, head) columns of a KV head.  Bound: memory (940 rows of 32
 // heads: 38 MB read and written, 12 us).
+// Delta by matrix instructions instead of by the threads' own sums costs nothing there; 160 fp32 rows of 8 heads of 64: 3.5 -> 5.8 us at least (a
+// chain of 32 dependent instructions), of a step of 95.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd B)
 {
@@ -80,23 +82,61 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
     const int g = W.n_q_heads / W.n_kv_heads;
     const int r = threadIdx.x >> 3, c = threadIdx.x & 7;
     const int64_t unit = (int64_t)blockIdx.x * gridDim.y + blockIdx.y;
+    auto place = [&](int i, int64_t &row, int64_t &h, bool &ok) {
+        if constexpr (BF16) {
+            row = 32 * (int64_t)blk.block + i; h = blockIdx.y; ok = row < blk.n_q;
+            row = min(row, (int64_t)blk.n_q - 1);
+        } else {
+            int64_t col = 32 * (int64_t)blk.block + i;
+            ok = col < (int64_t)blk.n_q * g;
+            col = min(col, (int64_t)blk.n_q * g - 1);
+            row = col / g; h = (int64_t)blockIdx.y * g + col % g;
+        }
+    };
     int64_t row, h;
     bool ok;
-    if constexpr (BF16) {
-        row = 32 * (int64_t)blk.block + r; h = blockIdx.y; ok = row < blk.n_q;
-        row = min(row, (int64_t)blk.n_q - 1);
-    } else {
-        int64_t col = 32 * (int64_t)blk.block + r;
-        ok = col < (int64_t)blk.n_q * g;
-        col = min(col, (int64_t)blk.n_q * g - 1);
-        row = col / g; h = (int64_t)blockIdx.y * g + col % g;
-    }
+    place(r, row, h, ok);
     // Behind the last row: its queries again, without a gradient.  What the keys it sees make of it is what they make of the last
     // row, and 0 times that, also where a key is not finite; no tile is masked for its sake.
     const int64_t R = (int64_t)blk.q_off + row, at = (R * W.n_q_heads + h) * D + PER * c;
     const float lse = B.lse[R * W.n_q_heads + h];
     const bool some = lse > -INFINITY, live = ok && some;          // (a row that saw nothing, or whose scores were not numbers, has no gradient)
-    float x[PER], y[PER], gx[PER], gy[PER], delta = 0.f;
+    // Delta = d_out . out, by the instruction and in the order that dp = d_out . v is made with (the diagonal of a product of the 32 rows, by
+    // the first wave): where a row sees one key, out is v, dp - Delta is 0 to the last bit, and so are d_q and d_k.
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x, n = lane & 31, hh = lane >> 5;
+        int64_t row_n, h_n;
+        bool ok_n;
+        place(n, row_n, h_n, ok_n);
+        const int64_t at_n = ((int64_t)blk.q_off + row_n) * W.n_q_heads + h_n;
+        f32x16 prod;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) prod[i] = 0.f;
+        if constexpr (BF16) {
+            const uint16_t *o = (const uint16_t *)B.out + at_n * D + 8 * hh, *d = (const uint16_t *)B.d_out + at_n * D + 8 * hh;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) prod = MFMA32(__builtin_bit_cast(bf16x8, ldg16(o + 16 * ks)), __builtin_bit_cast(bf16x8, ldg16(d + 16 * ks)), prod);
+        } else {
+            const float *o = (const float *)B.out + at_n * D + HALF * hh, *d = (const float *)B.d_out + at_n * D + HALF * hh;
+#pragma unroll 4
+            for (int i = 0; i < HALF; i += 4) {
+                const float4 u = *reinterpret_cast<const float4 *>(o + i), v = *reinterpret_cast<const float4 *>(d + i);
+                prod = __builtin_amdgcn_mfma_f32_32x32x2f32(u.x, v.x, prod, 0, 0, 0);
+                prod = __builtin_amdgcn_mfma_f32_32x32x2f32(u.y, v.y, prod, 0, 0, 0);
+                prod = __builtin_amdgcn_mfma_f32_32x32x2f32(u.z, v.z, prod, 0, 0, 0);
+                prod = __builtin_amdgcn_mfma_f32_32x32x2f32(u.w, v.w, prod, 0, 0, 0);
+            }
+        }
+        float delta = 0.f;                               // element (row n, column n): register 4 (n / 8) + n % 4 of the lane whose half is n / 4 % 2
+#pragma unroll
+        for (int i = 0; i < 16; ++i) delta = i == 4 * (n >> 3) + (n & 3) ? prod[i] : delta;
+        if (hh == ((n >> 2) & 1)) {
+            delta = ok_n && B.lse[at_n] > -INFINITY ? delta : 0.f;
+            reinterpret_cast<PcWinStat *>(B.stat + unit * PC_WIN_STAT_BYTES)->delta[n] = delta;
+            if (ok_n) B.delta[at_n] = delta;
+        }
+    }
+    float x[PER], y[PER], gx[PER], gy[PER];
     // PER numbers at p: pairs' first halves, or (HALF further) their second
     auto get = [&](const void *p, int64_t i, float (&v)[PER]) {
         if constexpr (BF16) {
@@ -117,9 +157,8 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
         }
     };
     {
-        float qx[PER], qy[PER], ox[PER], oy[PER];
+        float qx[PER], qy[PER];
         get(W.q, at, qx); get(W.q, at + HALF, qy);
-        get(B.out, at, ox); get(B.out, at + HALF, oy);
         get(B.d_out, at, gx); get(B.d_out, at + HALF, gy);
         const float4 *rot = reinterpret_cast<const float4 *>(W.rot_q + R * HALF + PER * c);
 #pragma unroll
@@ -127,11 +166,9 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
             const float4 cs2 = rot[i / 2];
             const float co = i & 1 ? cs2.z : cs2.x, si = i & 1 ? cs2.w : cs2.y;
             x[i] = some ? qx[i] * co - qy[i] * si : 0.f; y[i] = some ? qx[i] * si + qy[i] * co : 0.f;
-            delta += live ? gx[i] * ox[i] + gy[i] * oy[i] : 0.f;
             gx[i] = live ? gx[i] : 0.f; gy[i] = live ? gy[i] : 0.f;
         }
     }
-    delta += __shfl_xor(delta, 1); delta += __shfl_xor(delta, 2); delta += __shfl_xor(delta, 4);
     const int64_t to = (unit * 32 + r) * D + PER * c;
     if (!B.turned) { put(B.q_abs, to, x); put(B.q_abs, to + HALF, y); }
     put(B.d_o, to, gx); put(B.d_o, to + HALF, gy);
@@ -139,9 +176,8 @@ __global__ __launch_bounds__(256) void pc_win_bwd_prep_kernel(PcWin W, PcWinBwd 
     char *const st = B.stat + unit * PC_WIN_STAT_BYTES;
     PcWinStat *const to_stat = reinterpret_cast<PcWinStat *>(st);
     if (c == 0) {
-        to_stat->lse2[r] = live ? lse * 1.4426950408889634f : INFINITY; to_stat->delta[r] = live ? delta : 0.f;
+        to_stat->lse2[r] = live ? lse * 1.4426950408889634f : INFINITY;
         to_stat->lo[r] = lo; to_stat->lim[r] = blk.lim0 + (int)row;
-        if (ok) B.delta[R * W.n_q_heads + h] = delta;
         s_lo[r] = lo;
         s_state[r] = live ? 1 : ok ? 2 : 0;
     }
