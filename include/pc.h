@@ -197,9 +197,9 @@ int32_t pc_attend(pc_cache *c, const pc_call *calls, int32_t n_calls,
  * too.  (It keeps no counters.)  A recorded call holds the slots its messages had.
  *
  * A batch of single tokens of a PC_BF16 cache whose calls list the same messages reads each tile once for up to 256 (call, head of a
- * KV head) pairs where that is cheaper (pc_set_decode_sharing: 1 never, 2 whenever there are two such calls); the
- * order of a row's sums depends on the batch, so that a call alone may give another last bit.  The same calls give the
- * same bits. */
+ * KV head) pairs where that is cheaper (pc_set_decode_sharing: 1 never, 2 whenever there are two such calls), unless a call sees
+ * one message from two entries of its list; the order of a row's sums depends on the batch, so that a call alone may give
+ * another last bit.  The same calls give the same bits. */
 int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
                          const void *q, void *out, float *lse, void *stream);
 int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,

@@ -27,6 +27,7 @@ struct WinPlan {
     std::vector<int32_t> q_pos;
     std::vector<PcWinItem> pre, dec;
     std::vector<PcWinRun> runs;
+    std::vector<size_t> run_seg;              // of each run: the entry it is a part of, in segs
     std::vector<int64_t> rots;
     std::vector<PcMergeRow> merge;
     int64_t part_rows = 0;
@@ -89,6 +90,7 @@ int32_t add_runs(WinPlan &P, const WinCall &wc, int32_t row0, int32_t row1)
         }
         auto run = [&](int32_t first, int32_t n_tok) {                  // (first: a multiple of the tile)
             P.runs.push_back(PcWinRun{s.slot0 + first, s.start + first, n_tok, std::max(0, sinks - first), s.rot, s.self ? 1 : 0, s.rot_pos});
+            P.run_seg.push_back(i);
             tiles += (n_tok + PC_TILE - 1) / PC_TILE;
         };
         const int32_t t0 = skip >= end ? end : (int32_t)skip / PC_TILE * PC_TILE, sink_end = (sinks + PC_TILE - 1) / PC_TILE * PC_TILE;
@@ -165,7 +167,7 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
 }
 
 // Single tokens by what they see together: the tiles that the calls of a set see, each once, in as many ranges as workgroups run at
-// once.  False (and nothing is planned) where reading every call's own tiles is less.
+// once.  False (and nothing is planned) where reading every call's own tiles is less, or a call lists a message twice.
 bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
 {
     const int H = c->cfg.n_kv_heads, g = c->g, per = 16 / g;
@@ -216,7 +218,8 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
     const double heads = H / 8.0, alone = 8 + 0.0175 * (double)own * heads, together = 48 + (0.0227 * (double)shared + 0.0055 * (double)own) * heads;
     if (shared == 0 || (c->decode_sharing == 0 && alone <= together)) return false;
-    std::vector<std::pair<int32_t, PcWinSee>> seen;      // (call within the set, view) of the visit at hand
+    struct Seen { int32_t call; size_t seg; PcWinSee see; };         // (call: within the set)
+    std::vector<Seen> seen;                              // who sees the visit at hand, and from which entry of its list
     for (int32_t s = 0; s < n_sets; ++s) {
         const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
         int32_t waves = 1;
@@ -253,20 +256,20 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                     const int32_t j = pc.call - call0, q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)pc.call].call].q_off];
                     PcWinSee e{r.pos0 + d, r.n_tok - d, std::max(0, r.sink > 0 ? r.sink - d : 0), win_low(q_pos, P.window), (int64_t)q_pos - r.rot_pos, j % per, 0};
                     size_t i = seen.size();              // (nearly in order already)
-                    while (i > 0 && seen[i - 1].first > j) --i;
-                    if (i > 0 && seen[i - 1].first == j) {               // the sinks of an extent and its end; or a message that is listed twice
-                        PcWinSee &o = seen[i - 1].second;
-                        if (o.pos0 != e.pos0 || o.turn != e.turn) return false;
-                        o.n_tok = std::max(o.n_tok, e.n_tok); o.sink = std::max(o.sink, e.sink);
-                    } else seen.insert(seen.begin() + (ptrdiff_t)i, {j, e});
+                    while (i > 0 && seen[i - 1].call > j) --i;
+                    if (i > 0 && seen[i - 1].call == j) {                // the sinks of an extent and its end: one view
+                        Seen &o = seen[i - 1];
+                        if (o.seg != P.run_seg[pc.run]) return false;    // listed twice: two views, and a column has room for one
+                        o.see.n_tok = std::max(o.see.n_tok, e.n_tok); o.see.sink = std::max(o.see.sink, e.sink);
+                    } else seen.insert(seen.begin() + (ptrdiff_t)i, Seen{j, P.run_seg[pc.run], e});
                 }
                 PcWinVisit pv{slot0, n, (int32_t)P.sh_sees.size(), {}};
                 size_t k = 0;
                 for (int32_t gr = 0; gr <= PC_WIN_GROUPS; ++gr) {
-                    while (k < seen.size() && seen[k].first / per < gr) ++k;
+                    while (k < seen.size() && seen[k].call / per < gr) ++k;
                     pv.off[gr] = (int32_t)k;
                 }
-                for (const auto &o : seen) P.sh_sees.push_back(o.second);
+                for (const Seen &o : seen) P.sh_sees.push_back(o.see);
                 P.sh_visits.push_back(pv);
                 P.sh_items.back().n_steps += (n + PC_WIN_STEP_TILES - 1) / PC_WIN_STEP_TILES;
                 left -= n; done += n;
@@ -289,7 +292,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
 void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8)
 {
     const int g = c->g;
-    P.pre.clear(); P.dec.clear(); P.runs.clear(); P.rots.clear(); P.merge.clear();
+    P.pre.clear(); P.dec.clear(); P.runs.clear(); P.run_seg.clear(); P.rots.clear(); P.merge.clear();
     auto no_shared = [&] { P.sh_items.clear(); P.sh_visits.clear(); P.sh_sees.clear(); P.sh_calls.clear(); };
     no_shared();
     P.part_rows = 0;
@@ -328,7 +331,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8
         dec.push_back(Group{(int32_t)i, 0, run0, tiles});
     }
     P.rots.resize(rots);                                 // (single tokens' kernels make their rotations themselves)
-    if (may_split && plan_shared(c, P, dec)) { P.runs.resize(runs); return; }
+    if (may_split && plan_shared(c, P, dec)) { P.runs.resize(runs); P.run_seg.resize(runs); return; }
     no_shared();
     P.merge.resize(merge); P.part_rows = part_rows;
     make_items(c, P, dec, P.dec, 512, least, may_split, true, true);
@@ -388,7 +391,7 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
 {
     const int g = c->g, H_kv = c->cfg.n_kv_heads;
     const bool f32 = c->cfg.dtype == PC_F32;
-    P.pre.clear(); P.dec.clear(); P.runs.clear(); P.rots.clear(); P.merge.clear();
+    P.pre.clear(); P.dec.clear(); P.runs.clear(); P.run_seg.clear(); P.rots.clear(); P.merge.clear();
     P.part_rows = 0;
     for (Seg &s : P.segs) s.rot = -1;
     B = BwdPlan{};
