@@ -17,6 +17,7 @@ int32_t fetch_items(pc_cache *c, const void *items, size_t bytes, hipStream_t st
     std::memcpy(slot->host, items, bytes);
     PcWinTurns T{};
     T.from = slot->host; T.ws = c->tok_dev; T.n16 = (int)(bytes / 16); T.D = c->D;
+    pc_forget_error();                                   // (or the slot would not be released, with its reader enqueued)
     pc_launch_win_turns(T, nullptr, st);
     PC_HIP(c, hipGetLastError());
     return pc_stage_release(c, slot, st);
@@ -80,9 +81,14 @@ int32_t message_fork(pc_cache *c, const pc_fork *forks, int32_t n, int32_t *msg_
         if (rc != PC_OK) return rc;
         c->msgs.reserve(c->msgs.size() + (size_t)n);     // (nothing may fail behind the launch)
         ProfScope ps(c, 0, st);
+        pc_forget_error();
         pc_launch_fork(c->cfg.dtype, in_args ? &blob : nullptr, (const PcForkItem *)c->tok_dev, (const PcForkPiece *)((char *)c->tok_dev + n_items), n, max_rows, c->cfg.n_kv_heads, c->D,
                        c->slots, c->inv_freq_dev, c->k_store, c->v_store, c->table_dev, st);
-        PC_HIP(c, hipGetLastError());
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) {                           // (of several launches some may have written: nobody's tokens, in slots that stay free)
+            c->dirty_end = std::max(c->dirty_end, next);
+            return pc_fail(c, PC_ERR_HIP, "message_fork: %s", hipGetErrorString(e));
+        }
     }
     for (int j = 0; j < n; ++j) {
         msg_ids[j] = (int32_t)c->msgs.size();
@@ -162,8 +168,8 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
             c->flags_dev = nullptr; c->flag_words = 0; c->tickets = 0; c->flag_epoch = 0;
             const size_t cap = std::max<size_t>(2 * words, 1 << 14);
             PC_HIP(c, hipMalloc((void **)&c->flags_dev, sizeof(uint32_t) * cap));
-            c->flag_words = cap;
             PC_HIP(c, hipMemsetAsync(c->flags_dev, 0, sizeof(uint32_t) * cap, st));
+            c->flag_words = cap;                         // (cleared: not before, or a further call would take what is there for its flags)
         } else if (c->flag_epoch == UINT32_MAX) {        // the launches' numbers begin anew
             PC_HIP(c, hipMemsetAsync(c->flags_dev, 0, sizeof(uint32_t) * c->flag_words, st));
             c->tickets = 0; c->flag_epoch = 0;
@@ -180,8 +186,9 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
         C.head_bytes = c->slots * c->D * (int64_t)c->esize; C.tile_bytes = tile_bytes;
         C.table = c->table_dev;
         ProfScope ps(c, 7, st);
+        pc_forget_error();
         pc_launch_compact(C, in_args ? &blob : nullptr, st);
-        PC_HIP(c, hipGetLastError());
+        PC_HIP(c, hipGetLastError());                    // (the launch's own: nothing has moved)
         c->flag_epoch = C.epoch;
         c->tickets += (uint32_t)C.n_chunks;
     }

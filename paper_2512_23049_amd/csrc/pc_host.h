@@ -107,16 +107,20 @@ int32_t pc_fail(pc_cache *c, int32_t code, const char *fmt, ...);
 size_t pc_storage_bytes(const pc_config *cfg);
 void pc_prof_collect(pc_cache *c);
 
+// An error that earlier work of the thread left would be taken for that of the launch that follows, and the call refused although
+// its work has been enqueued: it is forgotten in front of a launch behind which the host's books change.
+inline void pc_forget_error() { (void)hipGetLastError(); }
+
 struct ProfScope {
     pc_cache *c; int cls; hipStream_t st; hipEvent_t a = nullptr, b = nullptr;
     ProfScope(pc_cache *c_, int cls_, hipStream_t st_) : c(c_), cls(cls_), st(st_) {
         if (!c->prof) return;
         auto get = [&]() { hipEvent_t e = nullptr;
             if (!c->ev_pool.empty()) { e = c->ev_pool.back(); c->ev_pool.pop_back(); }
-            else if (hipEventCreate(&e) != hipSuccess) e = nullptr;
+            else if (hipEventCreate(&e) != hipSuccess) { e = nullptr; pc_forget_error(); }
             return e; };
         a = get(); b = get();
-        if (a) (void)hipEventRecord(a, st);
+        if (a && hipEventRecord(a, st) != hipSuccess) pc_forget_error();
     }
     ~ProfScope() {
         if (!c->prof || !a || !b) return;

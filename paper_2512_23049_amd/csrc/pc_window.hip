@@ -637,6 +637,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     W.scale_log2 = c->scale * 1.4426950408889634f;
     // Lists in the arguments of the decode launch are read there; everything else reads them from the workspace.
     const bool direct = in_args && P.pre.empty() && P.sh_items.empty();
+    pc_forget_error();
     if (!direct) {
         ProfScope ps(c, 1, st);
         if (recorded && !in_args) pc_launch_store_args(from, L.lists, ws, st);
@@ -734,6 +735,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     if (bf16) T.rot_lanes = (uint32_t *)(ws + rot_lanes);
     T.rot_q = (float2 *)(ws + rot_q); T.rot_run = (float2 *)(ws + rot_run); T.inv_freq = c->inv_freq_dev;
     ProfScope ps(c, 5, st);
+    pc_forget_error();
     pc_launch_win_turns(T, in_args ? &blob : nullptr, st);
     PC_HIP(c, hipGetLastError());
     if (slot) { rc = pc_stage_release(c, slot, st); if (rc != PC_OK) return rc; }
