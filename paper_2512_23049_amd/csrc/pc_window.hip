@@ -30,7 +30,7 @@ struct WinPlan {
     std::vector<size_t> run_seg;              // of each run: the entry it is a part of, in segs
     std::vector<int64_t> rots;
     std::vector<PcMergeRow> merge;
-    int64_t part_rows = 0;
+    int64_t part_rows = 0, part_first = 0;    // partial rows [part_first, part_rows) are used
     int32_t window = 0, n_sink = 0;
     // single tokens of calls that list the same messages
     std::vector<PcWinSharedItem> sh_items;
@@ -144,8 +144,8 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
         int32_t most = 0;
         while (b < groups.size() && groups[b].call == groups[a].call) most = std::max(most, groups[b++].tiles);
         const WinCall &wc = P.calls[(size_t)groups[a].call];
-        const int32_t n = splits(most);
-        const int64_t part0 = P.part_rows;
+        const int32_t n = splits(most), n_rows = wc.row1 - wc.row0;
+        const int64_t part0 = P.part_rows;               // (of row row0: part_rows start at part_first, or row 0's could be negative)
         for (int32_t s = 0; s < n; ++s)
             for (size_t i = a; i < b; ++i) {
                 const Group &gr = groups[i];
@@ -156,11 +156,11 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
                     if (skip < has) break;
                     skip -= has; ++run;
                 }
-                items.push_back(PcWinItem{wc.q_off, wc.n_q, gr.unit0, wc.lim0, run, skip, t1 - t0, n == 1 ? -1 : (int32_t)(part0 + (int64_t)s * wc.n_q)});
+                items.push_back(PcWinItem{wc.q_off, wc.n_q, gr.unit0, wc.lim0, run, skip, t1 - t0, n == 1 ? -1 : (int32_t)(part0 + (int64_t)s * n_rows - wc.row0)});
             }
         if (n > 1) {
-            for (int32_t r = wc.row0; r < wc.row1; ++r) P.merge.push_back(PcMergeRow{wc.q_off + r, (int32_t)(part0 + r), n, wc.n_q});
-            P.part_rows += (int64_t)n * wc.n_q;
+            for (int32_t r = wc.row0; r < wc.row1; ++r) P.merge.push_back(PcMergeRow{wc.q_off + r, (int32_t)(part0 + (r - wc.row0)), n, n_rows});
+            P.part_rows += (int64_t)n * n_rows;
         }
         a = b;
     }
@@ -392,7 +392,6 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
     const int g = c->g, H_kv = c->cfg.n_kv_heads;
     const bool f32 = c->cfg.dtype == PC_F32;
     P.pre.clear(); P.dec.clear(); P.runs.clear(); P.run_seg.clear(); P.rots.clear(); P.merge.clear();
-    P.part_rows = 0;
     for (Seg &s : P.segs) s.rot = -1;
     B = BwdPlan{};
     std::vector<Group> groups;
@@ -430,6 +429,9 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
             }
         }
     }
+    P.part_first = 0;                                    // (a run's first call alone can begin behind its row 0)
+    for (const WinCall &wc : P.calls) P.part_first = std::max<int64_t>(P.part_first, wc.row0);
+    P.part_rows = P.part_first;
     make_items(c, P, groups, P.pre, 512, 6, true, f32, false);
 
     // keys: who lists each extent, extents in slot order
@@ -701,7 +703,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     const size_t rot = sizeof(float2) * (size_t)c->half, units = B.blocks.size() * (size_t)(bf16 ? Hq : H), unit = 32 * (size_t)c->D * c->esize;
     const size_t rot_lanes = big(bf16 ? rot / 2 * align_up(P.q_pos.size(), 32) : 0), rot_q = big(rot * P.q_pos.size()), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * P.q_pos.size() * (size_t)Hq);
     const size_t q_abs = big(B.turned.empty() ? unit * units : unit * B.turned.size() * (size_t)Hq), d_o = big(unit * units), stat = big(PC_WIN_STAT_BYTES * units);
-    const size_t part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)Hq * (size_t)c->D);
+    const size_t part_row = sizeof(float) * (size_t)Hq * (size_t)c->D, part_o = big(part_row * (size_t)(P.part_rows - P.part_first));
     const size_t key_part = big(sizeof(float) * 2 * PC_WIN_KEY_TILES * PC_TILE * (size_t)B.parts * (size_t)H * (size_t)c->D);
     int32_t rc = pc_ensure_ws(c, align_up(at, 256), st);
     if (rc != PC_OK) return rc;
@@ -720,7 +722,7 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
 
     W.items = (const PcWinItem *)(ws + items); W.runs = (const PcWinRun *)(ws + runs); W.q_pos = (const int32_t *)(ws + q_pos);
     W.rot_q = (const float2 *)(ws + rot_q); W.rot_lanes = (const uint32_t *)(ws + rot_lanes); W.rot_run = (const float2 *)(ws + rot_run);
-    W.part_o = (float *)(ws + part_o);
+    W.part_o = (float *)((uintptr_t)(ws + part_o) - part_row * (size_t)P.part_first);
     G.blocks = (const PcWinBlock *)(ws + blocks); G.apps = (const PcWinApp *)(ws + apps);
     G.key_items = (const PcWinKeyItem *)(ws + keys); G.sums = (const PcWinSum *)(ws + sums); G.bins = (const int32_t *)(ws + bins);
     G.n_blocks = (int32_t)B.blocks.size(); G.n_bins = std::max<int32_t>(0, (int32_t)B.bins.size() - 1); G.n_sums = (int32_t)B.sums.size();
