@@ -218,8 +218,8 @@ int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_cal
  * the matrix instructions and summed in fp32 (pc_attend_backward cuts them in three exact pieces instead, at three times the matrix work).
  * Refuses a stream that is being captured; every tensor 16-byte aligned, lse 4-byte (PC_ERR_INVALID_ARG).  Workspace: 17 KB
  * for each block of 32 rows and query head of a PC_BF16 cache (8 KB more for each extent that a block sees, where window and
- * n_sink together are 32 at most), of about 256 MB at a time (longer batches go in several runs), and the parts of tiles of
- * keys that many rows see. */
+ * n_sink together are 32 at most) and 768 bytes a row, of about 256 MB at a time (longer batches go in several runs), and the
+ * parts of tiles of keys that many rows see and of rows whose keys are walked in splits (runs of few rows). */
 int32_t pc_attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
                                   const void *q, const void *out, const float *lse, const void *d_out, float *d_q, float *d_k,
                                   float *d_v, void *stream);

@@ -694,14 +694,20 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     const int Hq = c->cfg.n_q_heads, H = c->cfg.n_kv_heads;
     BwdPlan B;
     plan_backward(c, P, B, range);
+    // the rows of the run (they follow each other), from a multiple of 32 on as the lanes' order asks for
+    int64_t row0 = INT64_MAX, row1 = 0;
+    for (const WinCall &wc : P.calls)
+        if (wc.row1 > wc.row0) { row0 = std::min<int64_t>(row0, wc.q_off + wc.row0); row1 = std::max<int64_t>(row1, wc.q_off + wc.row1); }
+    row0 -= row0 % 32;
+    const size_t rows = (size_t)(row1 - row0);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 16); return a; };
     auto of = [](const auto &v) { return sizeof(v[0]) * v.size(); };
-    const size_t items = take(of(P.pre)), runs = take(of(P.runs)), merge = take(of(P.merge)), q_pos = take(of(P.q_pos)), rots = take(of(P.rots));
+    const size_t items = take(of(P.pre)), runs = take(of(P.runs)), merge = take(of(P.merge)), q_pos = take(sizeof(int32_t) * rows), rots = take(of(P.rots));
     const size_t blocks = take(of(B.blocks)), apps = take(of(B.apps)), keys = take(of(B.keys)), sums = take(of(B.sums)), bins = take(of(B.bins)), turned = take(of(B.turned)), lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = sizeof(float2) * (size_t)c->half, units = B.blocks.size() * (size_t)(bf16 ? Hq : H), unit = 32 * (size_t)c->D * c->esize;
-    const size_t rot_lanes = big(bf16 ? rot / 2 * align_up(P.q_pos.size(), 32) : 0), rot_q = big(rot * P.q_pos.size()), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * P.q_pos.size() * (size_t)Hq);
+    const size_t rot_lanes = big(bf16 ? rot / 2 * align_up(rows, 32) : 0), rot_q = big(rot * rows), rot_run = big(rot * P.rots.size()), delta = big(sizeof(float) * rows * (size_t)Hq);
     const size_t q_abs = big(B.turned.empty() ? unit * units : unit * B.turned.size() * (size_t)Hq), d_o = big(unit * units), stat = big(PC_WIN_STAT_BYTES * units);
     const size_t part_row = sizeof(float) * (size_t)Hq * (size_t)c->D, part_o = big(part_row * (size_t)(P.part_rows - P.part_first));
     const size_t key_part = big(sizeof(float) * 2 * PC_WIN_KEY_TILES * PC_TILE * (size_t)B.parts * (size_t)H * (size_t)c->D);
@@ -717,11 +723,15 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     }
     char *from = in_args ? (char *)blob.w : (char *)slot->host;
     auto put = [&](size_t to, const auto &v) { if (!v.empty()) std::memcpy(from + to, v.data(), of(v)); };
-    put(items, P.pre); put(runs, P.runs); put(merge, P.merge); put(q_pos, P.q_pos); put(rots, P.rots);
+    put(items, P.pre); put(runs, P.runs); put(merge, P.merge); put(rots, P.rots);
+    std::memcpy(from + q_pos, P.q_pos.data() + row0, sizeof(int32_t) * rows);
     put(blocks, B.blocks); put(apps, B.apps); put(keys, B.keys); put(sums, B.sums); put(bins, B.bins); put(turned, B.turned);
 
-    W.items = (const PcWinItem *)(ws + items); W.runs = (const PcWinRun *)(ws + runs); W.q_pos = (const int32_t *)(ws + q_pos);
-    W.rot_q = (const float2 *)(ws + rot_q); W.rot_lanes = (const uint32_t *)(ws + rot_lanes); W.rot_run = (const float2 *)(ws + rot_run);
+    W.items = (const PcWinItem *)(ws + items); W.runs = (const PcWinRun *)(ws + runs);
+    // (tables of rows: the kernels index them by the batch's rows)
+    auto behind = [&](size_t table, size_t row_bytes) { return (uintptr_t)(ws + table) - row_bytes * (size_t)row0; };
+    W.q_pos = (const int32_t *)behind(q_pos, sizeof(int32_t));
+    W.rot_q = (const float2 *)behind(rot_q, rot); W.rot_lanes = (const uint32_t *)behind(rot_lanes, rot / 2); W.rot_run = (const float2 *)(ws + rot_run);
     W.part_o = (float *)((uintptr_t)(ws + part_o) - part_row * (size_t)P.part_first);
     G.blocks = (const PcWinBlock *)(ws + blocks); G.apps = (const PcWinApp *)(ws + apps);
     G.key_items = (const PcWinKeyItem *)(ws + keys); G.sums = (const PcWinSum *)(ws + sums); G.bins = (const int32_t *)(ws + bins);
@@ -729,10 +739,10 @@ int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, Pc
     G.turned = B.turned.empty() ? nullptr : (const PcWinTurned *)(ws + turned); G.n_turned = (int32_t)B.turned.size();
     G.k_factor = G.turned ? 1.f : W.scale_log2;
     G.key_scale = G.turned ? 0.6931471805599453f : c->scale;              // (the queries bring the scale, and log2 e)
-    G.delta = (float *)(ws + delta); G.q_abs = ws + q_abs; G.d_o = ws + d_o; G.stat = ws + stat; G.key_part = (float *)(ws + key_part);
+    G.delta = (float *)behind(delta, sizeof(float) * (size_t)Hq); G.q_abs = ws + q_abs; G.d_o = ws + d_o; G.stat = ws + stat; G.key_part = (float *)(ws + key_part);
     PcWinTurns T{};
     T.from = in_args ? ws : slot->host; T.ws = ws; T.n16 = (int)(lists / 16);
-    T.off_q_pos = (int)q_pos; T.n_rows = (int)P.q_pos.size(); T.off_rot = (int)rots; T.n_rot = (int)P.rots.size();
+    T.off_q_pos = (int)q_pos; T.n_rows = (int)rows; T.off_rot = (int)rots; T.n_rot = (int)P.rots.size();
     T.D = c->D; T.run_scale = 1.f;
     if (bf16) T.rot_lanes = (uint32_t *)(ws + rot_lanes);
     T.rot_q = (float2 *)(ws + rot_q); T.rot_run = (float2 *)(ws + rot_run); T.inv_freq = c->inv_freq_dev;
@@ -782,7 +792,8 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
     G.out = out; G.d_out = d_out; G.lse = lse; G.d_q = d_q; G.d_k = d_k; G.d_v = d_v; G.scale = c->scale;
     // Runs of blocks whose workspace fits.  A run ends with a call, or where units and rows end together: after four blocks of 32 rows
     // (a workgroup's units), or the columns of 32 rows.
-    const int64_t per_block = (int64_t)(bf16 ? c->cfg.n_q_heads : c->cfg.n_kv_heads) * (2 * 32 * c->D * (int64_t)c->esize + PC_WIN_STAT_BYTES);
+    const int64_t per_unit = 2 * 32 * c->D * (int64_t)c->esize + PC_WIN_STAT_BYTES, per_row = (bf16 ? 12 : 8) * c->half + 4 * c->cfg.n_q_heads;     // (rotations, Delta)
+    const int64_t per_block = (bf16 ? c->cfg.n_q_heads : c->cfg.n_kv_heads) * per_unit + (bf16 ? 32 : (32 + c->g - 1) / c->g) * per_row;
     const int64_t step = bf16 ? 4 : c->g, most = std::max<int64_t>(step, (int64_t)BWD_BYTES / per_block / (bf16 && (int64_t)window + n_sink <= PC_WIN_FEW ? 4 : 1) / step * step);
     std::vector<int2> range(P.calls.size(), make_int2(0, 0));
     int64_t in_run = 0;

@@ -44,3 +44,23 @@ def test_a_run_of_a_few_rows_of_a_long_call(dtype, h_q, h_kv, n_q):
         say(f"  rows {r0}: {err:.2e}")
         assert err <= BARS[dtype][0]
     layer.cache.close()
+
+
+@pytest.mark.parametrize("window", [20, 40])
+def test_rotations_are_those_of_a_runs_rows(window):
+    """One head, half a million rows: a row's rotations are more memory than its share of a block."""
+    n_q = 520000
+    layer = Layer("bf16", [64], 1, 1, 128)
+    calls = [([(0, 0)], -1, 0, n_q, [40 + i % 24 for i in range(n_q)])]
+    q = layer.normal(n_q, 1, 128)
+    d_q, extra = taken(layer, calls, window, 2, q, q)
+    say(f"  {extra / MB:.0f} MB")
+    assert extra <= 400 * MB
+    from oracle import window_oracle as win
+    for r0 in (0, 255000, n_q - 40):
+        rows = slice(r0, r0 + 40)
+        a, _, _ = win.attend_call_window_backward(layer.ks, layer.vs, [(0, 0)], -1, 0, 40, calls[0][4][rows], q[rows], q[rows], layer.theta, window, 2)
+        err = np.linalg.norm(d_q[rows].double().cpu().numpy() - a) / np.linalg.norm(a)
+        say(f"  rows {r0}: {err:.2e}")
+        assert err <= BARS["bf16"][0]
+    layer.cache.close()
