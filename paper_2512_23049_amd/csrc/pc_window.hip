@@ -172,10 +172,26 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
 {
     const int H = c->cfg.n_kv_heads, g = c->g, per = 16 / g;
     const int32_t n_calls = (int32_t)dec.size(), n_groups = (n_calls + per - 1) / per;
-    // (with two groups, waves would have every fourth step at most)
+    // (with two groups, waves would have every fourth step at most: 8 heads over 8, calls over 410 of 512 messages as below, call by call and
+    // shared, 8 calls 84 and 160 us, 16 155 and 204, but 24 236 and 196, which are not taken)
     if (c->decode_sharing == 1 || n_calls < 2 || (c->decode_sharing == 0 && n_groups < 3)) return false;
     const bool wide = n_groups > PC_WIN_GROUPS / 2;
     const int32_t set_calls = std::min(n_groups, wide ? PC_WIN_GROUPS : PC_WIN_GROUPS / 2) * per, n_sets = (n_calls + set_calls - 1) / set_calls;
+    // Microseconds of both ways, of the tiles that calls see on their own and of those that are distinct, and of the host: 7 ns for an
+    // entry of a list, whichever way, and 15 for a run of tiles, of which the plan below makes visits.  At their prices before the
+    // tiles are counted it is known of most small batches that sharing cannot gain.  Measured, call by call and shared:
+    //   64 heads over 8, 410 of 512 messages of 160 tokens, window 16 384: 8 calls 83 and 120, 12 118 and 129, 16 155 and 141, 24 239 and 159,
+    //   32 281 and 179; 24 of 48 messages, window 4096: 16 calls 35 and 40, 32 51 and 53, 64 84 and 64;
+    //   32 heads over 8: 16 calls 155 and 147, 32 294 and 162; of 24 messages 32 calls 49 and 45;
+    //   128 over 8: 12 calls 119 and 136, 16 156 and 153, 24 242 and 260, 32 291 and 267;
+    //   16 over 2 (the host's time): 16 calls 66 and 93, 32 111 and 158, 64 203 and 305; 64 calls over 16 messages of 640 tokens 62 and 59.
+    // By the caller's word: pc_set_decode_sharing.
+    int64_t own = 0, listed = 0, shared = 0;
+    for (const Group &gr : dec) { own += gr.tiles; listed += (int64_t)P.calls[(size_t)gr.call].n_seg; }
+    const double heads = H / 8.0, host = 12 + 0.007 * (double)listed, planned = host + 0.015 * (double)(P.runs.size() - (size_t)dec[0].run0);
+    const double alone = std::max(8 + 0.0175 * (double)own * heads, host);
+    auto together = [&](int64_t tiles) { return std::max(48 + (0.0227 * (double)tiles + 0.0055 * (double)own) * heads, planned); };
+    if (c->decode_sharing == 0 && alone <= together(own / set_calls)) return false;
     struct Piece { int32_t slot0, tiles; size_t run; int32_t call; };
     std::vector<Piece> pieces, scratch;
     // pieces [first, size) by their slots, in the calls' order where those are the same: a pass for 11 bits of a tile's number
@@ -192,7 +208,6 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
         }
     };
     std::vector<std::pair<size_t, size_t>> of_set;       // a set's pieces, in slot order
-    int64_t own = 0, shared = 0;
     for (int32_t s = 0; s < n_sets; ++s) {
         const size_t first = pieces.size();
         for (int32_t j = s * set_calls; j < std::min(n_calls, (s + 1) * set_calls); ++j) {
@@ -202,7 +217,6 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                 pieces.push_back(Piece{P.runs[r].slot0, t, r, j});
                 left -= t;
             }
-            own += dec[(size_t)j].tiles;
         }
         by_slot(pieces, first, scratch);
         int64_t end = -1;
@@ -212,12 +226,8 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
         }
         of_set.push_back({first, pieces.size()});
     }
-    // Microseconds of both ways, of the tiles that calls see on their own and of those that are distinct (8 heads a KV head; calls over 410 of
-    // 512 messages, window 16 384: 8 calls 94 on their own and 130 shared, 12 calls 133 and 147, 16 172 and 162, 24 271 and 191, 32 312 and 217;
-    // 16 calls over 24 of 48 messages, window 4096, 45 and 72).  By the caller's word: pc_set_decode_sharing.
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
-    const double heads = H / 8.0, alone = 8 + 0.0175 * (double)own * heads, together = 48 + (0.0227 * (double)shared + 0.0055 * (double)own) * heads;
-    if (shared == 0 || (c->decode_sharing == 0 && alone <= together)) return false;
+    if (shared == 0 || (c->decode_sharing == 0 && alone <= together(shared))) return false;
     struct Seen { int32_t call; size_t seg; PcWinSee see; };         // (call: within the set)
     std::vector<Seen> seen;                              // who sees the visit at hand, and from which entry of its list
     for (int32_t s = 0; s < n_sets; ++s) {
