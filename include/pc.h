@@ -190,11 +190,14 @@ int32_t pc_attend(pc_cache *c, const pc_call *calls, int32_t n_calls,
  * (infinities and NaN too).  window >= 1, n_sink >= 0; q and out 16-byte aligned, lse 4-byte; out must not overlap q
  * (PC_ERR_INVALID_ARG otherwise, but for the overlap, which is not looked for).
  * PC_BF16 caches: queries, once turned to their positions, and probabilities are rounded to bf16 for the matrix instructions;
- * scores, sums and partial results are fp32.  PC_F32 caches: fp32 throughout.
+ * scores, sums and partial results are fp32.  Calls of more than one row take (cos, sin) of their rows' positions in fp16 (made in 64
+ * bits; off by 2^-12 at most, an eighth of the rounding that the turned query meets), calls of one row in fp32.  PC_F32 caches: fp32
+ * throughout.
  * pc_attend_window refuses a stream that is being captured (the workspace it uses may move at a later call);
  * pc_attend_window_static is for those and for callers that cannot allocate: it works in the fixed array of pc_attend_static,
  * and what is said there of its size, its sharing, lists recorded into a graph and calls that overlap in time holds for it
- * too.  (It keeps no counters.)  A recorded call holds the slots its messages had.
+ * too.  (It keeps no counters.)  A recorded call holds its messages as they were: slots, lengths and stored positions; one that has
+ * grown, or been repositioned, moved or freed since has to be recorded anew.
  *
  * A batch of single tokens of a PC_BF16 cache whose calls list the same messages reads each tile once for up to 256 (call, head of a
  * KV head) pairs where that is cheaper (pc_set_decode_sharing: 1 never, 2 whenever there are two such calls), unless a call sees
@@ -215,7 +218,9 @@ int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_cal
  * part in its gradient, whatever is stored there; d_out and out are taken to be finite.  No sum depends on the order in which
  * workgroups run: the same calls give the same bits.
  * PC_F32: fp32 throughout.  PC_BF16: probabilities, their gradients and turned queries and keys are rounded to bf16 for
- * the matrix instructions and summed in fp32 (pc_attend_backward cuts them in three exact pieces instead, at three times the matrix work).
+ * the matrix instructions and summed in fp32 (pc_attend_backward cuts them in three exact pieces instead, at three times the matrix work);
+ * rotations of rows as in pc_attend_window.  Where window and n_sink together are 32 at most, and blocks see eight pieces of extents (128
+ * tokens) or fewer in the mean, keys stay as they are stored and queries are turned for each extent as in the forward.
  * Refuses a stream that is being captured; every tensor 16-byte aligned, lse 4-byte (PC_ERR_INVALID_ARG).  Workspace: 17 KB
  * for each block of 32 rows and query head of a PC_BF16 cache (8 KB more for each extent that a block sees, where window and
  * n_sink together are 32 at most) and 768 bytes a row, of about 256 MB at a time (longer batches go in several runs), and the
@@ -310,7 +315,8 @@ int32_t pc_message_free(pc_cache *c, int32_t msg_id);
  *   base   the position its first token's key is stored at (see pc_reposition): PC_POS_AUTO keeps the keys turned as they are
  *          (base of the source + first), an exact copy; another one turns them on the way, with one more rounding to the
  *          cache dtype.  What pc_attend computes does not depend on it.
- * One launch for all of them; all or nothing.  msg_ids receives n consecutive new ids in list order.
+ * One launch for all of them, with a small one in front that fetches lists too long for its arguments (56 forks from single extents
+ * fit); all or nothing.  msg_ids receives n consecutive new ids in list order.
  * Errors (nothing enqueued): unknown id, first < 0, len < 1, tokens past the message's end, |base| (also the kept one) >
  * max_position (PC_ERR_INVALID_ARG); no room for one of them or in the message table (PC_ERR_NO_SPACE); a stream that is being
  * captured (a replay would copy between slots that may be another message's by then). */
@@ -323,7 +329,7 @@ int32_t pc_message_fork(pc_cache *c, const pc_fork *forks, int32_t n, int32_t *m
  * K and V are bit for bit what they were.  max_slots > 0 stops before more than that many slots have been moved (but never
  * before the first extent that has to move), for a program that closes up a little between its steps; a further call goes on from there.
  * slots_moved (may be NULL) receives the slots moved.  One launch, in which every moved slot is read once and written
- * once; nothing is enqueued where there is no gap.
+ * once (and one in front that fetches lists too long for its arguments); nothing is enqueued where there is no gap.
  * Slots that a caller knows (pc_message_info, pc_message_extents, pc_build_tables, rows of a gradient's d_k and d_v before
  * pc_grad_keys_finalize), and graphs that hold recorded calls, are void afterwards.  Errors: max_slots < 0; a stream that is
  * being captured (PC_ERR_INVALID_ARG). */

@@ -109,8 +109,9 @@ void pc_launch_win_turns(const PcWinTurns &T, const PcArgBlob *blob, hipStream_t
 // 32 heads over 8, window 4096: 600 to 650 us, 0.9 PFLOP/s of visible work (16 matrix instructions, 102 vector and 50 scalar ones a
 // tile and wave; the matrix unit is busy 0.7 of the time).  Short walks: starts and turns, whose loads nothing hides: 33 blocks of
 // rows over 20 tiles of seven messages, 47 us: a workgroup's first tile 6 us after its start, a turn 3 us, a tile 1 us, its results 2.5 us.
-// Tried and dropped: the next tile's scores beside this one's exponentials (256 registers do not hold both: 1171 us), a row's queries
-// kept in registers from turn to turn (likewise).
+// Tried and dropped, in this one loop with its edges and turns: the next tile's scores beside this one's exponentials (spills: 1171 us;
+// pc_attend's packed walk holds both in 210 registers, in a loop of its own over tiles that are seen whole), a row's queries kept in
+// registers from turn to turn (spills).
 __global__ __launch_bounds__(256, 2) void pc_win_prefill_bf16_kernel(PcWin W)
 {
     constexpr int RING = 4, AHEAD = 3;

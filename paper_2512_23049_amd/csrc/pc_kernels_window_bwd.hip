@@ -16,7 +16,9 @@
 // Few keys.  Those keys are rounded once more than in the forward, so that a row's probabilities do not add up to 1: of two
 // keys, that is as much as what the gradient is left with when Delta is taken off (dk 5.4e-3 off in the 2-norm; 4e-3 from 50 keys
 // up).  Where window and sinks are 32 at most, the queries are turned for each extent as the forward turns them, and keys stay as they
-// are stored: the same scores, and dk in the stored keys' frame.
+// are stored: the same scores, and dk in the stored keys' frame.  (Not where a run's blocks see more than eight tiles of four, or parts of
+// them, in the mean: 5.4e-3 at most of twelve messages of two tokens.)  The first rows of a message without parents see few keys under any
+// window: 3.96e-3 over 300 rows.
 #include "pc_window.h"
 #include "pc_bwd_tiles.h"
 #include <type_traits>

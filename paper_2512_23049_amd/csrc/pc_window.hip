@@ -297,8 +297,9 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     return true;
 }
 
-// the rows of a call that units [unit0, unit0 + n) of the bf16 kernels, or block unit0 of 32 columns of the fp32 kernels, hold
-// least: tiles that a split of a single token is worth
+// Everything a forward call launches: rows of prompts in groups of four units (bf16: 32 rows x head; fp32: blocks of 32 columns, single
+// tokens too), with the runs that each group sees, then single tokens, shared or call by call.  may_split: or every group is one
+// item; least: tiles that a split of a single token is worth.
 void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8)
 {
     const int g = c->g;
@@ -489,7 +490,8 @@ void plan_backward(const pc_cache *c, WinPlan &P, BwdPlan &B, const std::vector<
         }
         a = b;
     }
-    // Rows of few keys: the forward's queries for every extent (see the kernels), if that is not too many times the blocks.
+    // Rows of few keys: the forward's queries for every extent (see the kernels), if they are eight times a block's own at most (8 KB each; with
+    // more extents a row mostly sees more keys, and has less need of them).
     int64_t visits = 0;
     for (const PcWinApp &a : apps) visits += a.n_blocks;
     if (!f32 && (int64_t)P.window + P.n_sink <= PC_WIN_FEW && visits <= 8 * (int64_t)B.blocks.size()) {
