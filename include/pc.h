@@ -48,6 +48,7 @@ extern "C" {
 
 #define PC_F32  0
 #define PC_BF16 1
+#define PC_MX4  2   /* k, v, q and out as with PC_BF16, keys and values held in 4 bits, see below */
 
 /* An omitted offset (Sec. 2.3, the rule for offsets that are left out): the position
  * right after the end of the preceding list entry.  For the first entry it means 0; for
@@ -78,19 +79,32 @@ extern "C" {
 typedef struct pc_cache pc_cache;
 
 typedef struct {
-    int32_t  n_q_heads;        /* H_q  (multiple of n_kv_heads; PC_BF16: at most 16 per KV head) */
+    int32_t  n_q_heads;        /* H_q  (multiple of n_kv_heads; PC_BF16, PC_MX4: at most 16 per KV head) */
     int32_t  n_kv_heads;       /* H_kv                                                  */
-    int32_t  head_dim;         /* D: 64 or 128 (PC_BF16: 128); other shapes: PC_ERR_SHAPE */
-    int32_t  dtype;            /* PC_F32 | PC_BF16: type of k, v, q, out and of storage */
+    int32_t  head_dim;         /* D: 64 or 128 (PC_BF16, PC_MX4: 128); other shapes: PC_ERR_SHAPE */
+    int32_t  dtype;            /* PC_F32 | PC_BF16 | PC_MX4: type of k, v, q, out and of storage */
     float    rope_theta;       /* RoPE base, e.g. 1e4 or 5e5                            */
     float    softmax_scale;    /* 0 -> 1/sqrt(D)                                        */
     int64_t  capacity_tokens;  /* slots in the cache (rounded up to PC_SLOT_ALIGN)      */
     int32_t  max_messages;
-    int32_t  max_position;     /* every token / query position p obeys |p| <= this      */
+    int32_t  max_position;     /* every token / query position p obeys |p| <= this (0 -> 2^24; PC_MX4: below 2^30) */
     uint32_t flags;
     void    *arena;            /* optional caller-owned DEVICE memory for K/V storage,  */
     size_t   arena_bytes;      /*   >= pc_cache_storage_bytes(cfg); NULL -> hipMalloc   */
 } pc_config;
+
+/* A PC_MX4 cache holds a head's 128 values as four blocks of 32: a power of two 2^e, the least with max|x| < 7 2^e (-60 <= e <= 60:
+ * larger values are 6 2^60, smaller ones than 2^-62 zeros), and for each value the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times 2^e and
+ * their negatives, ties to the even code: 68 bytes where PC_BF16 has 256.  Keys are quantised as they are stored, turned to their
+ * place (norms, turns and quantisation in 64 bits).  k, v, q and out are bf16.  A token whose key or value holds an infinity or a NaN in some
+ * head has keys of NaN there: rows that see it are NaN in that head's query heads.
+ * Attention (pc_attend, pc_attend_static, pc_attend_window, pc_attend_window_static, pc_decode_step) computes with the values held:
+ * of one row with queries as the sum of two 8-bit numbers (off by 2^-8 of a value at most, as bf16 is), of more rows over a bf16 copy of the
+ * tiles that they see in the workspace, in which every value held is exact (32 KB a tile of 32 tokens and 8 KV heads, half of them keys;
+ * in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Tensors as pc_attend_window asks for them:
+ * q and out 16-byte aligned; and pc_attend, like pc_attend_window, refuses a stream that is being captured.  Messages are appended, grown,
+ * read back, forked (where they stay turned as they are), freed, swapped and closed up over as in other caches.  Their keys cannot be
+ * turned without another rounding: pc_reposition* and turned forks are refused; nor is there a gradient (PC_ERR_INVALID_ARG). */
 
 /* Bytes of device memory the K/V storage needs for this configuration. */
 size_t  pc_cache_storage_bytes(const pc_config *cfg);
@@ -140,6 +154,52 @@ int32_t pc_append_tokens(pc_cache *c, int32_t msg_id, const void *k, const void 
                          void *stream);
 int32_t pc_append_tokens_batch(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, const void *k,
                                const void *v, void *stream);
+
+/* The same from a layer's projections, with the norms that some models have in front of the rotation: of every head of queries and keys
+ *   y = x / sqrt(mean(x^2) + eps) * weight,
+ * keys then turned and stored as an append does (one rounding for norm and turn), values as they are, and the normed queries
+ * written as pc_attend takes them.  All in one launch.
+ *   q, k, v    device rows of [heads][head_dim] in the tensors' type, 16-byte aligned, *_stride elements (a multiple of 16 bytes, at least a row)
+ *              from a row to the next: parts of one fused projection, or tensors of their own.  q NULL (and q_out NULL): keys and values only.
+ *   *_weight   device fp32 [head_dim], NULL: ones.  eps >= 0.
+ *   q_out      device [rows][n_q_heads][head_dim], 16-byte aligned, not overlapping the rows.
+ * pc_append_projected: n new messages, whose tokens are the rows in list order (rows: sum of lens); lens, reserves (may be NULL) and
+ * msg_ids as for pc_append_messages.  pc_append_projected_tokens: one more token for each of n_msgs distinct messages, row j for
+ * msg_ids[j], as pc_append_tokens_batch (same errors).  Norms are computed in 32 bits (PC_MX4: of keys in 64).  A stream that is being captured
+ * is refused (a replay would write to slots that may be another message's by then). */
+typedef struct {
+    const void  *q, *k, *v;
+    int64_t      q_stride, k_stride, v_stride;
+    const float *q_weight, *k_weight;
+    float        eps;
+} pc_projected;
+int32_t pc_append_projected(pc_cache *c, const pc_projected *rows, int32_t n, const int32_t *lens, const int32_t *reserves, int32_t *msg_ids,
+                            void *q_out, void *stream);
+int32_t pc_append_projected_tokens(pc_cache *c, const pc_projected *rows, const int32_t *msg_ids, int32_t n_msgs, void *q_out,
+                                   void *stream);
+
+/* The gradient of pc_append_projected (PC_F32, PC_BF16), behind pc_attend_backward or pc_attend_window_backward and in the place of
+ * pc_grad_keys_finalize:
+ *   rows             as they were appended (v is not read); message j's are lens[j] rows, its first tokens (at most those of its first extent).
+ *   d_q              fp32 [rows][n_q_heads][head_dim], of q_out.
+ *   d_k, d_v         fp32, indexed by slot, as the attention's gradient collected them (keys as stored): read, not changed.  Messages must not
+ *                    have been repositioned, moved, freed or swapped since.
+ *   to               gradients of the rows, written in the tensors' type (strides and alignment as for the rows); q_weight, k_weight: of the
+ *                    weights, fp32 [head_dim], written (NULL: not wanted).  q, d_q and to->q are NULL together.
+ * Sums are fp32, in an order that depends on the lists alone: the same call gives the same bits.  Refuses a stream that is being captured.
+ * n = 0 writes nothing. */
+typedef struct {
+    void   *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    float  *q_weight, *k_weight;
+} pc_projected_grad;
+int32_t pc_projected_backward(pc_cache *c, const pc_projected *rows, int32_t n, const int32_t *msg_ids, const int32_t *lens, const float *d_q,
+                              const float *d_k, const float *d_v, const pc_projected_grad *to, void *stream);
+
+/* What messages hold, as rows in the tensors' type, [tokens of all listed messages][n_kv_heads][head_dim], in list and token order:
+ * keys as they are stored (turned to their stored base + token), values as they are; of a PC_MX4 cache the values that its codes stand for (exact
+ * in bf16).  k or v may be NULL.  16-byte aligned.  A stream that is being captured is refused. */
+int32_t pc_messages_read(pc_cache *c, int32_t n, const int32_t *msg_ids, void *k, void *v, void *stream);
 
 /* One parent of a call: message id and the position of its first token
  * (Sec. 2.3 `parents` and `offsets`). */

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(HERE, "libpc.so")
 
 PC_OK = 0
 PC_ERR_INVALID_ARG, PC_ERR_BAD_MSG_ID, PC_ERR_NO_SPACE, PC_ERR_SHAPE, PC_ERR_HIP = -1, -2, -3, -4, -5
-PC_F32, PC_BF16 = 0, 1
+PC_F32, PC_BF16, PC_MX4 = 0, 1, 2
 PC_POS_AUTO = -(2 ** 31)
 PC_SLOT_ALIGN = 32
 PC_FLAG_HOST_ONLY = 1
@@ -45,6 +45,16 @@ class pc_call(C.Structure):
 
 class pc_fork(C.Structure):
     _fields_ = [("msg_id", C.c_int32), ("first", C.c_int32), ("len", C.c_int32), ("reserve", C.c_int32), ("base", C.c_int32)]
+
+
+class pc_projected(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float)]
+
+
+class pc_projected_grad(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
 
 
 _lib = None
@@ -124,6 +134,14 @@ def lib():
         L.pc_message_fork.argtypes = [vp, C.POINTER(pc_fork), i32, C.POINTER(i32), vp]
         L.pc_cache_compact.restype = i32
         L.pc_cache_compact.argtypes = [vp, i64, C.POINTER(i64), vp]
+        L.pc_append_projected.restype = i32
+        L.pc_append_projected.argtypes = [vp, C.POINTER(pc_projected), i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32), vp, vp]
+        L.pc_append_projected_tokens.restype = i32
+        L.pc_append_projected_tokens.argtypes = [vp, C.POINTER(pc_projected), C.POINTER(i32), i32, vp, vp]
+        L.pc_projected_backward.restype = i32
+        L.pc_projected_backward.argtypes = [vp, C.POINTER(pc_projected), i32, C.POINTER(i32), C.POINTER(i32), vp, vp, vp, C.POINTER(pc_projected_grad), vp]
+        L.pc_messages_read.restype = i32
+        L.pc_messages_read.argtypes = [vp, i32, C.POINTER(i32), vp, vp, vp]
         L.pc_set_decode_sharing.restype = i32
         L.pc_set_decode_sharing.argtypes = [vp, i32]
         L.pc_set_key_gather.restype = i32
@@ -136,6 +154,22 @@ class PcError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"pc error {code}: {msg}")
         self.code = code
+
+
+def projected(q_ptr: int, k_ptr: int, v_ptr: int, q_stride: int, k_stride: int, v_stride: int, q_weight_ptr: int = 0, k_weight_ptr: int = 0,
+              eps: float = 1e-6) -> pc_projected:
+    """Rows of a layer's projections for append_projected* and projected_backward; strides in elements."""
+    return pc_projected(q_ptr or None, k_ptr or None, v_ptr or None, q_stride, k_stride, v_stride, q_weight_ptr or None, k_weight_ptr or None, eps)
+
+
+def projected_grad(q_ptr: int, k_ptr: int, v_ptr: int, q_stride: int, k_stride: int, v_stride: int, q_weight_ptr: int = 0,
+                   k_weight_ptr: int = 0) -> pc_projected_grad:
+    """Where projected_backward writes."""
+    return pc_projected_grad(q_ptr or None, k_ptr or None, v_ptr or None, q_stride, k_stride, v_stride, q_weight_ptr or None, k_weight_ptr or None)
+
+
+def _ints(values):
+    return (C.c_int32 * max(len(values), 1))(*values)
 
 
 def marshal_calls(calls: Sequence):
@@ -337,6 +371,24 @@ class Cache:
 
     def grad_keys_finalize(self, d_k_ptr: int, stream: int = 0):
         self._check(lib().pc_grad_keys_finalize(self.h, d_k_ptr or None, stream or None))
+
+    def append_projected(self, rows: pc_projected, lengths, q_out_ptr: int, reserves=None, stream: int = 0):
+        """New messages of a projection's rows, queries and keys normed head by head; the new ids."""
+        n = len(lengths)
+        ids = (C.c_int32 * max(n, 1))()
+        self._check(lib().pc_append_projected(self.h, C.byref(rows), n, _ints(lengths), _ints(reserves) if reserves is not None else None, ids,
+                                              q_out_ptr or None, stream or None))
+        return ids[:n]
+
+    def append_projected_tokens(self, rows: pc_projected, msg_ids, q_out_ptr: int, stream: int = 0):
+        self._check(lib().pc_append_projected_tokens(self.h, C.byref(rows), _ints(msg_ids), len(msg_ids), q_out_ptr or None, stream or None))
+
+    def projected_backward(self, rows: pc_projected, msg_ids, lengths, d_q_ptr: int, d_k_ptr: int, d_v_ptr: int, to: pc_projected_grad, stream: int = 0):
+        self._check(lib().pc_projected_backward(self.h, C.byref(rows), len(msg_ids), _ints(msg_ids), _ints(lengths), d_q_ptr or None, d_k_ptr or None,
+                                                d_v_ptr or None, C.byref(to), stream or None))
+
+    def messages_read(self, msg_ids, k_ptr: int, v_ptr: int, stream: int = 0):
+        self._check(lib().pc_messages_read(self.h, len(msg_ids), _ints(msg_ids), k_ptr or None, v_ptr or None, stream or None))
 
     def message_extents(self, msg: int, cap: int = 64):
         """[(slot_start, len), ...] of the message's extents in token order."""

@@ -176,6 +176,7 @@ int32_t pc_attend(pc_cache *c, const pc_call *calls, int32_t n_calls, const void
     if (n_calls < 0 || (n_calls > 0 && !calls)) return pc_fail(c, PC_ERR_INVALID_ARG, "attend: bad call list");
     if (n_calls == 0) return PC_OK;
     if (!c->host_only && (!q || !out)) return pc_fail(c, PC_ERR_INVALID_ARG, "attend: null q or out");
+    if (c->cfg.dtype == PC_MX4) return pc_guarded(c, [&] { return pc_attend_mx4(c, "attend", calls, n_calls, q, out, lse, (hipStream_t)stream, nullptr); });
     return attend_impl(c, calls, n_calls, q, out, lse, (hipStream_t)stream, nullptr, 0);
 }
 
@@ -188,6 +189,11 @@ int32_t pc_decode_step(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, cons
     int32_t rc = pc_check_token_batch(c, msg_ids, n_msgs, k, v);
     if (rc != PC_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
+    if (c->cfg.dtype == PC_MX4)
+        return pc_guarded(c, [&] {
+            const int32_t r = n_msgs > 0 ? pc_append_token_items(c, std::vector<int32_t>(msg_ids, msg_ids + n_msgs), k, v, st, nullptr) : PC_OK;
+            return r != PC_OK || n_calls == 0 ? r : pc_attend_mx4(c, "decode_step", calls, n_calls, q, out, lse, st, nullptr);
+        });
     const std::vector<int32_t> ids(msg_ids, msg_ids + std::max(n_msgs, 0));
     // The tokens can be written by a launch of the attend itself (the one launch of a decode batch, else the plan builder's)
     // when nothing that launch reads from the device table changes under it: the new message's length travels with the
@@ -236,12 +242,15 @@ int32_t pc_attend_static(pc_cache *c, const pc_call *calls, int32_t n_calls, con
     if (!c) return PC_ERR_INVALID_ARG;
     if (n_calls < 0 || (n_calls > 0 && !calls)) return pc_fail(c, PC_ERR_INVALID_ARG, "attend_static: bad call list");
     if (n_calls == 0) return PC_OK;
+    const bool mx4 = c->cfg.dtype == PC_MX4;
+    if (c->host_only && mx4) return pc_guarded(c, [&] { return pc_attend_mx4(c, "attend_static", calls, n_calls, q, out, lse, nullptr, nullptr); });
     if (c->host_only) return attend_impl(c, calls, n_calls, q, out, lse, nullptr, nullptr, 0);
     if (!q || !out) return pc_fail(c, PC_ERR_INVALID_ARG, "attend_static: null q or out");
     if (!c->static_ws) return pc_fail(c, PC_ERR_HIP, "attend_static: the fixed scratch array was not found on this device");
     const bool prof = c->prof;                           // kernel timing takes events from a pool that may have to grow
     c->prof = false;
-    const int32_t rc = attend_impl(c, calls, n_calls, q, out, lse, (hipStream_t)stream, c->static_ws, PC_STATIC_WS_BYTES);
+    const int32_t rc = mx4 ? pc_guarded(c, [&] { return pc_attend_mx4(c, "attend_static", calls, n_calls, q, out, lse, (hipStream_t)stream, c->static_ws); })
+                           : attend_impl(c, calls, n_calls, q, out, lse, (hipStream_t)stream, c->static_ws, PC_STATIC_WS_BYTES);
     c->prof = prof;
     return rc;
 }
@@ -250,6 +259,7 @@ int32_t pc_attend_backward(pc_cache *c, const pc_call *calls, int32_t n_calls, c
                            const void *d_out, float *d_q, float *d_k, float *d_v, void *stream)
 {
     if (!c) return PC_ERR_INVALID_ARG;
+    if (c->cfg.dtype == PC_MX4) return pc_fail(c, PC_ERR_INVALID_ARG, "attend_backward: a PC_MX4 cache has no gradient");
     if (n_calls < 0 || (n_calls > 0 && !calls)) return pc_fail(c, PC_ERR_INVALID_ARG, "attend_backward: bad call list");
     if (n_calls == 0) return PC_OK;
     if (!c->host_only && (!q || !lse || !d_out || !d_q || !d_k || !d_v))
@@ -296,6 +306,7 @@ int32_t pc_attend_backward(pc_cache *c, const pc_call *calls, int32_t n_calls, c
 int32_t pc_grad_keys_finalize(pc_cache *c, float *d_k, void *stream)
 {
     if (!c) return PC_ERR_INVALID_ARG;
+    if (c->cfg.dtype == PC_MX4) return pc_fail(c, PC_ERR_INVALID_ARG, "grad_keys_finalize: a PC_MX4 cache has no gradient");
     if (c->host_only) return PC_OK;
     if (!d_k) return pc_fail(c, PC_ERR_INVALID_ARG, "grad_keys_finalize: null d_k");
     std::vector<PcMsgEntry> live;

@@ -47,6 +47,8 @@ int32_t message_fork(pc_cache *c, const pc_fork *forks, int32_t n, int32_t *msg_
         if (base > c->cfg.max_position || base < -(int64_t)c->cfg.max_position)
             return pc_fail(c, PC_ERR_INVALID_ARG, "message_fork: fork %d: position %lld outside [-%d, %d]", j, (long long)base, c->cfg.max_position,
                         c->cfg.max_position);
+        if (c->cfg.dtype == PC_MX4 && base != stored)
+            return pc_fail(c, PC_ERR_INVALID_ARG, "message_fork: fork %d: the keys of a PC_MX4 cache stay as they are (a call may place a message anywhere)", j);
         const int32_t res = std::max(f.reserve, f.len);
         int64_t start = 0;
         if (!pc_take_slots(spans, next, c->slots, res, start))
@@ -136,7 +138,7 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
     if (!moves.empty() && !c->host_only) {
         PcDeviceScope on(c);
         if (!on.ok) return pc_fail(c, PC_ERR_HIP, "cache_compact: the cache's device cannot be made current");
-        const int32_t tile_bytes = (int32_t)(PC_TILE * c->D * c->esize), per = PC_COMPACT_BYTES / tile_bytes;
+        const int32_t tile_bytes = (int32_t)(PC_TILE * c->row_bytes), per = PC_COMPACT_BYTES / tile_bytes;
         // a list of tiles in slot order, the table's moves behind it
         const size_t n_tiles = (size_t)(moved / PC_TILE), at_moves = sizeof(PcCompactTile) * n_tiles;
         std::vector<char> lists(align_up(at_moves + sizeof(PcCompactMove) * moves.size(), 16));
@@ -183,7 +185,7 @@ int32_t compact(pc_cache *c, int64_t max_slots, int64_t *slots_moved, hipStream_
         C.epoch = c->flag_epoch + 1; C.ticket0 = c->tickets;
         C.ticket = c->flags_dev; C.read = c->flags_dev + counters;
         C.k_store = (char *)c->k_store; C.v_store = (char *)c->v_store;
-        C.head_bytes = c->slots * c->D * (int64_t)c->esize; C.tile_bytes = tile_bytes;
+        C.head_bytes = c->slots * (int64_t)c->row_bytes; C.tile_bytes = tile_bytes;
         C.table = c->table_dev;
         ProfScope ps(c, 7, st);
         pc_forget_error();

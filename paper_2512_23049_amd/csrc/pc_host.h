@@ -5,6 +5,8 @@
 
 #include "../../include/pc.h"
 #include "pc_kernels.h"
+#include "pc_mx4.h"
+#include "pc_project.h"
 
 #include <algorithm>
 #include <chrono>
@@ -46,7 +48,8 @@ struct pc_cache {
     bool grow_extents = false;
     int D = 0, half = 0, g = 0;
     int64_t slots = 0;
-    size_t esize = 0;
+    size_t esize = 0;                                // bytes of an element of k, v, q and out
+    size_t row_bytes = 0;                            // bytes of a slot's key (or value) of one KV head as it is stored
     float scale = 0.f;
     std::vector<HostMsg> msgs;
     std::vector<FreeSpan> free_spans;                // sorted by start, neighbours merged, none touches next_slot
@@ -223,8 +226,9 @@ struct Planned {
 
 // pc_lib.hip
 extern "C" int32_t pc_check_token_batch(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, const void *k, const void *v);
+// projected (or null): the tokens are rows of a projection, which go through the norms (q: its queries, or null)
 extern "C" int32_t pc_append_token_items(pc_cache *c, const std::vector<int32_t> &ids, const void *k, const void *v, hipStream_t st,
-                                         std::vector<PcTokenItem> *defer);
+                                         std::vector<PcTokenItem> *defer, const PcRows *projected = nullptr, const void *q = nullptr);
 // Slots of one message out of (spans, next): the first freed span that holds the reserve rounded up to the slot alignment, else the
 // end of the used region.  False (nothing changed) if neither has room.
 bool pc_take_slots(std::vector<FreeSpan> &spans, int64_t &next, int64_t capacity, int32_t res, int64_t &start);
@@ -236,6 +240,10 @@ int32_t pc_stage_release(pc_cache *c, StageSlot *s, hipStream_t st);      // wha
 bool pc_recorded(hipStream_t st);
 extern "C" int32_t pc_items_room(pc_cache *c, size_t bytes, hipStream_t st);       // room for a call's items at tok_dev
 extern "C" int32_t pc_stage_items(pc_cache *c, const void *items, size_t bytes, hipStream_t st);
+// pc_project.hip: items to the cache, in one launch (R: what the call brings; the cache's own is filled in)
+int32_t pc_write_rows(pc_cache *c, PcRows R, std::vector<PcRowsItem> &items, hipStream_t st);
+// pc_window.hip: pc_attend of a PC_MX4 cache (fixed_ws: null, or the array of pc_attend_static)
+int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws);
 // pc_attend.hip: the address, on the current device, of the library's fixed scratch array (looked up once per device)
 int32_t pc_static_scratch(void **ptr, size_t *bytes);
 // pc_plan.hip

@@ -1,5 +1,6 @@
 // The cache's own copies (gfx950): forks of messages, and the cache closing up.
 #include "pc_copies.h"
+#include "pc_mx4.h"
 #include "pc_mfma_common.h"
 
 namespace {
@@ -171,6 +172,50 @@ __device__ __forceinline__ void fork_f32(const PcForkItem &it, const PcForkPiece
     }
 }
 
+// Four bits: codes and exponents as they are; a word of values is put together from the places its eight tokens have where they come from.
+__device__ __forceinline__ void fork_mx4(const PcForkItem &it, const PcForkPiece *pieces, int tile0, int tile1, char *k, char *v)
+{
+    __shared__ int s_from[PC_TILE];                      // where each token of the tile comes from, -1: there is none
+    for (int tile = tile0; tile < tile1; ++tile) {
+        __syncthreads();
+        if (threadIdx.x < PC_TILE) {
+            const int t = tile * PC_TILE + threadIdx.x;
+            int from = -1;
+            if (t < it.len) {
+                int p = 0;
+                while (p + 1 < it.n_pieces && pieces[p + 1].first <= t) ++p;
+                from = pieces[p].slot + t - pieces[p].first;
+            }
+            s_from[threadIdx.x] = from;
+        }
+        __syncthreads();
+        char *kt = k + ((int64_t)it.slot0 / PC_TILE + tile) * PC_MX4_TILE, *vt = v + ((int64_t)it.slot0 / PC_TILE + tile) * PC_MX4_TILE;
+        auto place = [](char *store, int slot) { return store + (int64_t)(slot / PC_TILE) * PC_MX4_TILE; };
+        {
+            const int row = threadIdx.x >> 3, part = threadIdx.x & 7, from = s_from[row];
+            uint2 x = make_uint2(0, 0);
+            if (from >= 0) x = *reinterpret_cast<const uint2 *>(place(k, from) + from % PC_TILE * 64 + 8 * part);
+            *reinterpret_cast<uint2 *>(kt + row * 64 + 8 * part) = x;
+        }
+        if (threadIdx.x < PC_TILE) {
+            const int from = s_from[threadIdx.x];
+            *reinterpret_cast<uint32_t *>(kt + PC_MX4_CODES + threadIdx.x * 4) = from < 0 ? 0u : *reinterpret_cast<const uint32_t *>(place(k, from) + PC_MX4_CODES + from % PC_TILE * 4);
+        } else if (threadIdx.x < PC_TILE + 128) {
+            const int b = threadIdx.x - PC_TILE, from = s_from[b / 32 * 8 + b % 8];        // byte b: group, block, slot
+            vt[PC_MX4_CODES + b] = from < 0 ? 0 : place(v, from)[PC_MX4_CODES + from % PC_TILE / 8 * 32 + b / 8 % 4 * 8 + from % 8];
+        }
+        for (int e = threadIdx.x; e < 512; e += 256) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int from = s_from[e / 128 * 8 + j];
+                if (from >= 0) w |= (reinterpret_cast<const uint32_t *>(place(v, from) + from % PC_TILE / 8 * 512)[e % 128] >> 4 * (from % 8) & 15u) << 4 * j;
+            }
+            reinterpret_cast<uint32_t *>(vt)[e] = w;
+        }
+    }
+}
+
 template <int D, bool BF16>
 __device__ __forceinline__ void fork_copy(const PcForkItem *items, const PcForkPiece *all_pieces, int64_t slots, const double *__restrict__ inv_freq, void *k_store,
                                           void *v_store, PcMsgEntry *table)
@@ -210,20 +255,40 @@ __global__ __launch_bounds__(256) void pc_fork_arg_kernel(PcArgBlob, int n, int6
     fork_copy<D, BF16>(items, reinterpret_cast<const PcForkPiece *>(items + n), slots, inv_freq, k_store, v_store, table);
 }
 
+__device__ __forceinline__ void fork_copy_mx4(const PcForkItem *items, const PcForkPiece *all_pieces, int64_t slots, char *k_store, char *v_store, PcMsgEntry *table)
+{
+    const PcForkItem it = items[blockIdx.z];
+    const int tile0 = blockIdx.x * FORK_TILES, tiles = (it.rows + PC_TILE - 1) / PC_TILE, tile1 = min(tile0 + FORK_TILES, tiles);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) table[it.msg] = PcMsgEntry{it.slot0, it.len, it.base, 0};
+    const int64_t head = (int64_t)blockIdx.y * (slots / PC_TILE) * PC_MX4_TILE;
+    fork_mx4(it, all_pieces + it.piece0, tile0, tile1, k_store + head, v_store + head);
+}
+__global__ __launch_bounds__(256) void pc_fork_mx4_kernel(const PcForkItem *items, const PcForkPiece *pieces, int64_t slots, char *k_store, char *v_store, PcMsgEntry *table)
+{
+    fork_copy_mx4(items, pieces, slots, k_store, v_store, table);
+}
+__global__ __launch_bounds__(256) void pc_fork_mx4_arg_kernel(PcArgBlob, int n, int64_t slots, char *k_store, char *v_store, PcMsgEntry *table)
+{
+    const PcForkItem *items = (const PcForkItem *)__builtin_amdgcn_kernarg_segment_ptr();          // (the blob comes first)
+    fork_copy_mx4(items, reinterpret_cast<const PcForkPiece *>(items + n), slots, k_store, v_store, table);
+}
+
 void pc_launch_fork(int dtype, const PcArgBlob *blob, const PcForkItem *items, const PcForkPiece *pieces, int n, int max_rows, int n_kv_heads, int D, int64_t slots,
                     const double *inv_freq, void *k_store, void *v_store, PcMsgEntry *table, hipStream_t st)
 {
     const int tiles = (max_rows + PC_TILE - 1) / PC_TILE;
     if (blob) {
         const dim3 grid((unsigned)((tiles + FORK_TILES - 1) / FORK_TILES), (unsigned)n_kv_heads, (unsigned)n);
-        if (dtype == 1) pc_fork_arg_kernel<128, true><<<grid, 256, 0, st>>>(*blob, n, slots, inv_freq, k_store, v_store, table);
+        if (dtype == 2) pc_fork_mx4_arg_kernel<<<grid, 256, 0, st>>>(*blob, n, slots, (char *)k_store, (char *)v_store, table);
+        else if (dtype == 1) pc_fork_arg_kernel<128, true><<<grid, 256, 0, st>>>(*blob, n, slots, inv_freq, k_store, v_store, table);
         else if (D == 64) pc_fork_arg_kernel<64, false><<<grid, 256, 0, st>>>(*blob, n, slots, inv_freq, k_store, v_store, table);
         else pc_fork_arg_kernel<128, false><<<grid, 256, 0, st>>>(*blob, n, slots, inv_freq, k_store, v_store, table);
         return;
     }
     for (int at = 0; at < n; at += 65535) {              // (the limit of a grid's third dimension)
         const dim3 grid((unsigned)((tiles + FORK_TILES - 1) / FORK_TILES), (unsigned)n_kv_heads, (unsigned)std::min(n - at, 65535));
-        if (dtype == 1) pc_fork_kernel<128, true><<<grid, 256, 0, st>>>(items + at, pieces, slots, inv_freq, k_store, v_store, table);
+        if (dtype == 2) pc_fork_mx4_kernel<<<grid, 256, 0, st>>>(items + at, pieces, slots, (char *)k_store, (char *)v_store, table);
+        else if (dtype == 1) pc_fork_kernel<128, true><<<grid, 256, 0, st>>>(items + at, pieces, slots, inv_freq, k_store, v_store, table);
         else if (D == 64) pc_fork_kernel<64, false><<<grid, 256, 0, st>>>(items + at, pieces, slots, inv_freq, k_store, v_store, table);
         else pc_fork_kernel<128, false><<<grid, 256, 0, st>>>(items + at, pieces, slots, inv_freq, k_store, v_store, table);
     }
@@ -242,7 +307,8 @@ void pc_launch_fork(int dtype, const PcArgBlob *blob, const PcForkItem *items, c
 // Bound: memory.  512 messages of 160 tokens, 8 KV heads: 650 MB read and written in 145 us (4.5 TB/s); 64 KB a workgroup and one counter
 // for all stores 174 us, 32 KB 330 (a counter gives 70 numbers a microsecond); kept in the caches like other data 5 % more.
 // Flags hold the launch's number and the counter goes on from launch to launch, so that nothing has to be cleared.
-__device__ __forceinline__ void compact_chunk(const PcCompact &C)
+// TILE: pieces of 16 bytes in a tile that do not fill a step of the workgroup (4 bits), 0: those that do
+template <int TILE> __device__ __forceinline__ void compact_chunk(const PcCompact &C)
 {
     __shared__ uint32_t s_ticket;
     const int store = (int)(blockIdx.x % (unsigned)C.n_stores), H = C.n_stores / 2;
@@ -252,17 +318,20 @@ __device__ __forceinline__ void compact_chunk(const PcCompact &C)
     const int per = PC_COMPACT_BYTES / C.tile_bytes, tile0 = chunk * per, n = min(per, C.n_tiles - tile0);
     if (chunk == 0 && store == 0)
         for (int i = threadIdx.x; i < C.n_moves; i += PC_COMPACT_THREADS) C.table[C.moves[i].rec].slot_start = C.moves[i].slot_start;
-    char *base = (store < H ? C.k_store + store * C.head_bytes : C.v_store + (store - H) * C.head_bytes) + threadIdx.x * 16;
+    char *base = store < H ? C.k_store + store * C.head_bytes : C.v_store + (store - H) * C.head_bytes;
     constexpr int PIECE = 16 * PC_COMPACT_THREADS, PIECES = PC_COMPACT_BYTES / PIECE;
-    const int steps = C.tile_bytes / PIECE;              // (1 or 2)
+    const int steps = TILE ? 1 : C.tile_bytes / PIECE;   // (1 or 2)
+    // piece j of the thread: of which tile, and where in it
+    auto tile_of = [&](int j) { return TILE ? (j * PC_COMPACT_THREADS + (int)threadIdx.x) / (TILE ? TILE : 1) : j / steps; };
+    auto byte_of = [&](int j) { return TILE ? (j * PC_COMPACT_THREADS + (int)threadIdx.x) % (TILE ? TILE : 1) * 16 : (j % steps) * PIECE + (int)threadIdx.x * 16; };
     u32x4 x[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-        const int t = j / steps;
+        const int t = tile_of(j);
         x[j] = (u32x4){0u, 0u, 0u, 0u};
         if (t < n) {
             const int src = C.tiles[tile0 + t].src;
-            if (src >= 0) x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + (int64_t)src * C.tile_bytes + (j % steps) * PIECE));
+            if (src >= 0) x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + (int64_t)src * C.tile_bytes + byte_of(j)));
         }
     }
 #pragma unroll
@@ -280,24 +349,28 @@ __device__ __forceinline__ void compact_chunk(const PcCompact &C)
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
-        const int t = j / steps;
-        if (t < n) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4 *>(base + (int64_t)C.tiles[tile0 + t].dst * C.tile_bytes + (j % steps) * PIECE));
+        const int t = tile_of(j);
+        if (t < n) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4 *>(base + (int64_t)C.tiles[tile0 + t].dst * C.tile_bytes + byte_of(j)));
     }
 }
 
-__global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_kernel(PcCompact C) { compact_chunk(C); }
-__global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_arg_kernel(PcArgBlob, PcCompact C)
+template <int TILE> __global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_kernel(PcCompact C) { compact_chunk<TILE>(C); }
+template <int TILE> __global__ __launch_bounds__(PC_COMPACT_THREADS) void pc_compact_arg_kernel(PcArgBlob, PcCompact C)
 {
     const char *lists = (const char *)__builtin_amdgcn_kernarg_segment_ptr();          // (the blob comes first)
     C.tiles = reinterpret_cast<const PcCompactTile *>(lists);
     C.moves = reinterpret_cast<const PcCompactMove *>(C.tiles + C.n_tiles);
-    compact_chunk(C);
+    compact_chunk<TILE>(C);
 }
 
 void pc_launch_compact(const PcCompact &C, const PcArgBlob *blob, hipStream_t st)
 {
     if (C.n_chunks <= 0) return;
     const unsigned grid = (unsigned)(C.n_chunks * C.n_stores);
-    if (blob) pc_compact_arg_kernel<<<grid, PC_COMPACT_THREADS, 0, st>>>(*blob, C);
-    else pc_compact_kernel<<<grid, PC_COMPACT_THREADS, 0, st>>>(C);
+    constexpr int MX4 = PC_MX4_TILE / 16;
+    if (C.tile_bytes == PC_MX4_TILE) {
+        if (blob) pc_compact_arg_kernel<MX4><<<grid, PC_COMPACT_THREADS, 0, st>>>(*blob, C);
+        else pc_compact_kernel<MX4><<<grid, PC_COMPACT_THREADS, 0, st>>>(C);
+    } else if (blob) pc_compact_arg_kernel<0><<<grid, PC_COMPACT_THREADS, 0, st>>>(*blob, C);
+    else pc_compact_kernel<0><<<grid, PC_COMPACT_THREADS, 0, st>>>(C);
 }

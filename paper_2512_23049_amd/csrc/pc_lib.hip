@@ -12,11 +12,12 @@ int32_t pc_fail(pc_cache *c, int32_t code, const char *fmt, ...)
     return code;
 }
 
+static size_t row_bytes(int32_t dtype, int32_t D) { return dtype == PC_MX4 ? PC_MX4_ROW : (size_t)D * (dtype == PC_BF16 ? 2 : 4); }
+
 size_t pc_storage_bytes(const pc_config *cfg)
 {
     const int64_t slots = (int64_t)align_up((size_t)std::max<int64_t>(cfg->capacity_tokens, 1), PC_SLOT_ALIGN);
-    const size_t es = cfg->dtype == PC_BF16 ? 2 : 4;
-    return 2 * (size_t)slots * cfg->n_kv_heads * cfg->head_dim * es;
+    return 2 * (size_t)slots * cfg->n_kv_heads * row_bytes(cfg->dtype, cfg->head_dim);
 }
 
 void pc_prof_collect(pc_cache *c)
@@ -138,9 +139,10 @@ int32_t pc_cache_create(const pc_config *cfg, pc_cache **out)
     *out = nullptr;
     if (cfg->n_q_heads <= 0 || cfg->n_kv_heads <= 0 || cfg->n_q_heads % cfg->n_kv_heads) return PC_ERR_SHAPE;
     if (cfg->head_dim != 64 && cfg->head_dim != 128) return PC_ERR_SHAPE;
-    if (cfg->dtype != PC_F32 && cfg->dtype != PC_BF16) return PC_ERR_INVALID_ARG;
-    if (cfg->dtype == PC_BF16 && cfg->head_dim != 128) return PC_ERR_SHAPE;
-    if (cfg->dtype == PC_BF16 && cfg->n_q_heads / cfg->n_kv_heads > 16) return PC_ERR_SHAPE;
+    if (cfg->dtype != PC_F32 && cfg->dtype != PC_BF16 && cfg->dtype != PC_MX4) return PC_ERR_INVALID_ARG;
+    if (cfg->dtype != PC_F32 && cfg->head_dim != 128) return PC_ERR_SHAPE;
+    if (cfg->dtype != PC_F32 && cfg->n_q_heads / cfg->n_kv_heads > 16) return PC_ERR_SHAPE;
+    if (cfg->dtype == PC_MX4 && cfg->max_position >= 1 << 30) return PC_ERR_INVALID_ARG;          // (pc_attend is a window of 2^31 - 1 there)
     if (cfg->capacity_tokens <= 0 || cfg->max_messages <= 0 || !(cfg->rope_theta > 0.f)) return PC_ERR_INVALID_ARG;
     pc_cache *c = new pc_cache();
     c->cfg = *cfg;
@@ -150,7 +152,8 @@ int32_t pc_cache_create(const pc_config *cfg, pc_cache **out)
     c->D = cfg->head_dim; c->half = c->D / 2; c->g = cfg->n_q_heads / cfg->n_kv_heads;
     c->slots = (int64_t)align_up((size_t)cfg->capacity_tokens, PC_SLOT_ALIGN);
     if (c->slots > INT32_MAX) { delete c; return PC_ERR_SHAPE; }
-    c->esize = cfg->dtype == PC_BF16 ? 2 : 4;
+    c->esize = cfg->dtype == PC_F32 ? 4 : 2;
+    c->row_bytes = row_bytes(cfg->dtype, c->D);
     c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt((float)c->D);
     c->msgs.reserve((size_t)cfg->max_messages);
     *out = c;
@@ -262,7 +265,7 @@ static int32_t pc_append_rows(const pc_cache *c, int64_t start, int32_t len, int
 // A further extent's tokens come one by one: its span is cleared by launches of their own in front of them.
 static void clear_if_reused(pc_cache *c, int64_t start, int32_t res, hipStream_t st)
 {
-    const int64_t n = c->host_only ? 0 : reused_slots(c, start, res);
+    const int64_t n = c->host_only || c->cfg.dtype == PC_MX4 ? 0 : reused_slots(c, start, res);          // (4 bits: no code is anything but finite)
     if (n == 0) return;
     pc_launch_zero_span(c->cfg.dtype, c->k_store, c->slots, c->cfg.n_kv_heads, c->D, start, n, st);
     pc_launch_zero_span(c->cfg.dtype, c->v_store, c->slots, c->cfg.n_kv_heads, c->D, start, n, st);
@@ -272,6 +275,18 @@ static void clear_if_reused(pc_cache *c, int64_t start, int32_t res, hipStream_t
 bool pc_take_slots(std::vector<FreeSpan> &spans, int64_t &next, int64_t capacity, int32_t res, int64_t &start) { return take_slots(spans, next, capacity, res, start); }
 int32_t pc_rows_to_write(const pc_cache *c, int64_t start, int32_t len, int32_t res) { return pc_append_rows(c, start, len, res); }
 extern "C" {
+
+// Whole messages of a PC_MX4 cache, from contiguous rows, without norms.
+static PcRowsItem plain_rows(const pc_cache *, const void *k, const void *v, int64_t start, int32_t len, int32_t id)
+{
+    return PcRowsItem{nullptr, k, v, 0, (int32_t)start, 0, len, len, id, len, 0, 1};
+}
+static PcRows plain_launch(const pc_cache *c)
+{
+    PcRows R{};
+    R.k_stride = R.v_stride = (int64_t)c->cfg.n_kv_heads * c->D;
+    return R;
+}
 
 int32_t pc_append_message(pc_cache *c, const void *k, const void *v, int32_t len, int32_t reserve,
                           int32_t *msg_id, void *stream)
@@ -293,10 +308,16 @@ int32_t pc_append_message(pc_cache *c, const void *k, const void *v, int32_t len
     const int id = (int)c->msgs.size();
     if (!c->host_only) {
         hipStream_t st = (hipStream_t)stream;
+        if (c->cfg.dtype == PC_MX4) {
+            std::vector<PcRowsItem> rows{plain_rows(c, k, v, start, len, id)};
+            const int32_t rc = pc_write_rows(c, plain_launch(c), rows, st);
+            if (rc != PC_OK) return rc;
+        } else {
         ProfScope ps(c, 0, st);
         pc_launch_append(c->cfg.dtype, k, v, len, pc_append_rows(c, start, len, res), c->cfg.n_kv_heads, c->D, start, c->slots, c->inv_freq_dev,
                          c->k_store, c->v_store, c->table_dev, id, st);
         PC_HIP(c, hipGetLastError());
+        }
     }
     if (!c->msgs.empty() && start < c->msgs.back().slot_start) c->slots_in_id_order = false;
     c->msgs.push_back({start, len, res, 0, true});
@@ -369,6 +390,12 @@ int32_t pc_append_messages(pc_cache *c, int32_t n, const void *const *k, const v
     }
     if (!c->host_only) {
         hipStream_t st = (hipStream_t)stream;
+        if (c->cfg.dtype == PC_MX4) {
+            std::vector<PcRowsItem> rows;
+            for (const PcAppendItem &it : items) rows.push_back(plain_rows(c, it.k, it.v, it.slot_start, it.len, it.msg));
+            const int32_t rc = pc_write_rows(c, plain_launch(c), rows, st);
+            if (rc != PC_OK) return rc;
+        } else {
         const bool in_args = sizeof(PcAppendItem) * (size_t)n <= PC_ARG_BYTES;
         const int32_t rc = in_args ? PC_OK : pc_stage_items(c, items.data(), sizeof(PcAppendItem) * (size_t)n, st);
         if (rc != PC_OK) return rc;
@@ -376,6 +403,7 @@ int32_t pc_append_messages(pc_cache *c, int32_t n, const void *const *k, const v
         pc_launch_append_batch(c->cfg.dtype, (const PcAppendItem *)c->tok_dev, in_args ? items.data() : nullptr, n, max_rows, c->cfg.n_kv_heads, c->D, c->slots,
                                c->inv_freq_dev, c->k_store, c->v_store, c->table_dev, st);
         PC_HIP(c, hipGetLastError());
+        }
     }
     for (int j = 0; j < n; ++j) {
         msg_ids[j] = (int32_t)c->msgs.size();
@@ -394,7 +422,7 @@ int32_t pc_append_messages(pc_cache *c, int32_t n, const void *const *k, const v
 // back for the caller to write them with a kernel of its own (the decode step's plan builder); the host bookkeeping is
 // done either way.  An empty *defer on return means the append was enqueued here.
 int32_t pc_append_token_items(pc_cache *c, const std::vector<int32_t> &ids, const void *k, const void *v, hipStream_t st,
-                              std::vector<PcTokenItem> *defer)
+                              std::vector<PcTokenItem> *defer, const PcRows *projected, const void *q)
 {
     if (defer) defer->clear();
     const int n = (int)ids.size();
@@ -461,7 +489,18 @@ int32_t pc_append_token_items(pc_cache *c, const std::vector<int32_t> &ids, cons
             PC_HIP(c, hipEventRecord(slot->ev, st));
             slot->used = true;
         }
-        if (n <= PC_TOKEN_PACK) {                            // a decode step's handful of tokens rides in the kernel arguments
+        if (projected || c->cfg.dtype == PC_MX4) {           // runs of tokens of one extent
+            const PcRows R = projected ? *projected : plain_launch(c);
+            auto row = [&](const void *p, int j, int64_t stride) { return p ? (const char *)p + (int64_t)j * stride * (int64_t)c->esize : nullptr; };
+            std::vector<PcRowsItem> rows;
+            for (int j = 0; j < n; ++j) {
+                const PcTokenItem &t = items[(size_t)j];
+                if (!rows.empty() && rows.back().msg == t.msg && rows.back().slot0 + rows.back().n == t.slot) { ++rows.back().n; continue; }
+                rows.push_back(PcRowsItem{row(q, j, R.q_stride), row(k, j, R.k_stride), row(v, j, R.v_stride), j, t.slot, t.pos, 1, 0, t.msg, t.new_len, 0, 0});
+            }
+            const int32_t rc = pc_write_rows(c, R, rows, st);
+            if (rc != PC_OK) return rc;
+        } else if (n <= PC_TOKEN_PACK) {                     // a decode step's handful of tokens rides in the kernel arguments
             PcTokenPack pack;
             std::memcpy(pack.it, items.data(), sizeof(PcTokenItem) * (size_t)n);
             ProfScope ps(c, 0, st);
@@ -494,6 +533,7 @@ int32_t pc_append_tokens(pc_cache *c, int32_t msg_id, const void *k, const void 
     if (!known(c, msg_id)) return pc_fail(c, PC_ERR_BAD_MSG_ID, "append_tokens: unknown message %d", msg_id);
     if (n < 1) return pc_fail(c, PC_ERR_INVALID_ARG, "append_tokens: n = %d must be >= 1", n);
     if (!c->host_only && (!k || !v)) return pc_fail(c, PC_ERR_INVALID_ARG, "append_tokens: null k or v");
+    if (c->cfg.dtype == PC_MX4 && (((uintptr_t)k | (uintptr_t)v) & 15)) return pc_fail(c, PC_ERR_INVALID_ARG, "append_tokens: k and v must be 16-byte aligned");
     return pc_append_token_items(c, std::vector<int32_t>((size_t)n, msg_id), k, v, (hipStream_t)stream, nullptr);
 }
 
@@ -502,6 +542,7 @@ int32_t pc_check_token_batch(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs
     if (n_msgs < 0 || (n_msgs > 0 && !msg_ids)) return pc_fail(c, PC_ERR_INVALID_ARG, "append_tokens_batch: bad id list");
     if (n_msgs == 0) return PC_OK;
     if (!c->host_only && (!k || !v)) return pc_fail(c, PC_ERR_INVALID_ARG, "append_tokens_batch: null k or v");
+    if (c->cfg.dtype == PC_MX4 && (((uintptr_t)k | (uintptr_t)v) & 15)) return pc_fail(c, PC_ERR_INVALID_ARG, "append_tokens_batch: k and v must be 16-byte aligned");
     for (int j = 0; j < n_msgs; ++j)
         if (!known(c, msg_ids[j])) return pc_fail(c, PC_ERR_BAD_MSG_ID, "append_tokens_batch: unknown message %d", msg_ids[j]);
     std::vector<int32_t> sorted(msg_ids, msg_ids + n_msgs);
@@ -568,6 +609,7 @@ int32_t pc_reposition(pc_cache *c, int32_t msg_id, int32_t new_base, void *strea
     HostMsg &m = c->msgs[(size_t)msg_id];
     const int64_t delta = (int64_t)new_base - m.base_pos;
     if (delta == 0) return PC_OK;
+    if (c->cfg.dtype == PC_MX4) return pc_fail(c, PC_ERR_INVALID_ARG, "reposition: the keys of a PC_MX4 cache stay as they are (a call may place a message anywhere)");
     if (!c->host_only) {
         hipStream_t st = (hipStream_t)stream;
         ProfScope ps(c, 7, st);
@@ -594,6 +636,8 @@ int32_t pc_reposition_batch(pc_cache *c, const int32_t *msg_ids, const int32_t *
             return pc_fail(c, PC_ERR_INVALID_ARG, "reposition_batch: position %d outside [-%d, %d]", new_bases[j],
                         c->cfg.max_position, c->cfg.max_position);
         const int64_t delta = (int64_t)new_bases[j] - c->msgs[(size_t)m].base_pos;
+        if (delta != 0 && c->cfg.dtype == PC_MX4)
+            return pc_fail(c, PC_ERR_INVALID_ARG, "reposition: the keys of a PC_MX4 cache stay as they are (a call may place a message anywhere)");
         if (delta != 0)
             for (int32_t r = m; r >= 0; r = c->msgs[(size_t)r].next) {          // every extent turns by the same angle
                 const HostMsg &hm = c->msgs[(size_t)r];
@@ -657,16 +701,16 @@ int64_t pc_message_swap_bytes(pc_cache *c, int32_t msg_id)
         return pc_fail(c, PC_ERR_BAD_MSG_ID, "swap_bytes: unknown message %d", msg_id);
     int64_t span = 0;                                    // every extent's reserved span, one after the other
     for (int32_t r = msg_id; r >= 0; r = c->msgs[(size_t)r].next) span += (int64_t)align_up((size_t)c->msgs[(size_t)r].reserve, PC_SLOT_ALIGN);
-    return 2 * span * c->cfg.n_kv_heads * c->D * (int64_t)c->esize;
+    return 2 * span * c->cfg.n_kv_heads * (int64_t)c->row_bytes;
 }
 
 // the span [slot_start, slot_start + span) of every KV head, K heads first then V heads; both stores keep a
 // head's slots contiguous (V in groups of 8 slots, and spans are multiples of 32), so each is one strided copy
 static int32_t copy_span(pc_cache *c, int64_t slot_start, int64_t span, void *blob, bool out, hipStream_t st)
 {
-    const size_t row = (size_t)span * (size_t)c->D * c->esize;                 // one head's share of the span
-    const size_t pitch = (size_t)c->slots * (size_t)c->D * c->esize;           // one head's share of the store
-    const size_t at = (size_t)slot_start * (size_t)c->D * c->esize;
+    const size_t row = (size_t)span * c->row_bytes;                            // one head's share of the span
+    const size_t pitch = (size_t)c->slots * c->row_bytes;                      // one head's share of the store
+    const size_t at = (size_t)slot_start * c->row_bytes;
     char *bk = (char *)blob, *bv = bk + row * (size_t)c->cfg.n_kv_heads;
     char *sk = (char *)c->k_store + at, *sv = (char *)c->v_store + at;
     if (out) {
@@ -684,7 +728,7 @@ int32_t pc_message_swap_out(pc_cache *c, int32_t msg_id, void *blob, void *strea
     if (!c) return PC_ERR_INVALID_ARG;
     if (!known(c, msg_id)) return pc_fail(c, PC_ERR_BAD_MSG_ID, "swap_out: unknown message %d", msg_id);
     if (!c->host_only && !blob) return pc_fail(c, PC_ERR_INVALID_ARG, "swap_out: null blob");
-    const size_t per_slot = 2 * (size_t)c->cfg.n_kv_heads * (size_t)c->D * c->esize;
+    const size_t per_slot = 2 * (size_t)c->cfg.n_kv_heads * c->row_bytes;
     if (!c->host_only) {
         char *at = (char *)blob;
         for (int32_t r = msg_id; r >= 0; r = c->msgs[(size_t)r].next) {
@@ -722,7 +766,7 @@ int32_t pc_message_swap_in(pc_cache *c, int32_t msg_id, const void *blob, void *
     }
     if (!c->host_only) {
         hipStream_t st = (hipStream_t)stream;
-        const size_t per_slot = 2 * (size_t)c->cfg.n_kv_heads * (size_t)c->D * c->esize;
+        const size_t per_slot = 2 * (size_t)c->cfg.n_kv_heads * c->row_bytes;
         const char *at = (const char *)blob;
         for (const auto &pl : placed) {
             const HostMsg &m = c->msgs[(size_t)pl.first];

@@ -31,6 +31,7 @@ struct WinPlan {
     std::vector<int64_t> rots;
     std::vector<PcMergeRow> merge;
     int64_t part_rows = 0, part_first = 0;    // partial rows [part_first, part_rows) are used
+    std::vector<int32_t> unpack;              // PC_MX4: first slots of the tiles that rows of prompts see, each once; their runs name places among these
     int32_t window = 0, n_sink = 0;
     // single tokens of calls that list the same messages
     std::vector<PcWinSharedItem> sh_items;
@@ -297,6 +298,25 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     return true;
 }
 
+// The tiles that the runs name, each once, in slot order; the runs then name their places among these (runs of consecutive tiles stay
+// consecutive).
+void unpacked(WinPlan &P)
+{
+    std::vector<std::pair<int32_t, int32_t>> spans;      // slots [first, second)
+    for (const PcWinRun &r : P.runs) spans.push_back({r.slot0, r.slot0 + (r.n_tok + PC_TILE - 1) / PC_TILE * PC_TILE});
+    std::sort(spans.begin(), spans.end());
+    std::vector<std::pair<int32_t, int32_t>> first;      // a joined span's first slot, and its place
+    int32_t end = -1;
+    for (const auto &s : spans) {
+        if (s.first > end || first.empty()) { first.push_back({s.first, (int32_t)P.unpack.size() * PC_TILE}); end = s.first; }
+        for (; end < s.second; end += PC_TILE) P.unpack.push_back(end);
+    }
+    for (PcWinRun &r : P.runs) {
+        const auto it = std::upper_bound(first.begin(), first.end(), std::make_pair(r.slot0, INT32_MAX)) - 1;
+        r.slot0 = it->second + (r.slot0 - it->first);
+    }
+}
+
 // Everything a forward call launches: rows of prompts in groups of four units (bf16: 32 rows x head; fp32: blocks of 32 columns, single
 // tokens too), with the runs that each group sees, then single tokens, shared or call by call.  may_split: or every group is one
 // item; least: tiles that a split of a single token is worth.
@@ -336,20 +356,22 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8
     if (c->cfg.dtype == PC_F32) return;
     const size_t runs = P.runs.size(), rots = P.rots.size(), merge = P.merge.size();
     const int64_t part_rows = P.part_rows;
+    P.unpack.clear();
+    if (c->cfg.dtype == PC_MX4) unpacked(P);
     for (size_t i = 0; i < P.calls.size(); ++i) {
         if (P.calls[i].n_q != 1) continue;
         const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, P.calls[i], 0, 1);
         dec.push_back(Group{(int32_t)i, 0, run0, tiles});
     }
     P.rots.resize(rots);                                 // (single tokens' kernels make their rotations themselves)
-    if (may_split && plan_shared(c, P, dec)) { P.runs.resize(runs); P.run_seg.resize(runs); return; }
+    if (may_split && c->cfg.dtype == PC_BF16 && plan_shared(c, P, dec)) { P.runs.resize(runs); P.run_seg.resize(runs); return; }
     no_shared();
     P.merge.resize(merge); P.part_rows = part_rows;
     make_items(c, P, dec, P.dec, 512, least, may_split, true, true);
 }
 
 // lists as they are staged, then what the device makes of them
-struct WinLayout { size_t pre, dec, runs, merge, q_pos, rots, sh_items, sh_visits, sh_sees, sh_calls, lists, rot_q, rot_run, part_o, part_ml, total; };
+struct WinLayout { size_t pre, dec, runs, merge, q_pos, rots, sh_items, sh_visits, sh_sees, sh_calls, unpack, lists, rot_q, rot_run, part_o, part_ml, k_copy, v_copy, total; };
 
 WinLayout lay_out(const pc_cache *c, const WinPlan &P)
 {
@@ -366,13 +388,17 @@ WinLayout lay_out(const pc_cache *c, const WinPlan &P)
     L.sh_visits = take(sizeof(PcWinVisit) * P.sh_visits.size());
     L.sh_sees = take(sizeof(PcWinSee) * P.sh_sees.size());
     L.sh_calls = take(sizeof(PcWinSharedCall) * P.sh_calls.size());
+    L.unpack = take(sizeof(int32_t) * P.unpack.size());
     L.lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = P.pre.empty() ? 0 : sizeof(float2) * (size_t)c->half;
-    L.rot_q = big((c->cfg.dtype == PC_BF16 ? rot / 2 : rot) * align_up(P.q_pos.size(), 32));         // (bf16: rot_lanes)
+    L.rot_q = big((c->cfg.dtype != PC_F32 ? rot / 2 : rot) * align_up(P.q_pos.size(), 32));         // (bf16: rot_lanes)
     L.rot_run = big(rot * P.rots.size());
     L.part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads * (size_t)c->D);
     L.part_ml = big(sizeof(float) * 2 * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads);
+    const size_t copy = (size_t)PC_TILE * (size_t)c->D * c->esize * (size_t)c->cfg.n_kv_heads * P.unpack.size();
+    L.k_copy = big(copy);
+    L.v_copy = big(copy);
     L.total = align_up(at, 256);
     return L;
 }
@@ -381,7 +407,7 @@ void write_lists(const WinPlan &P, const WinLayout &L, char *to)
 {
     auto put = [&](size_t at, const auto &v) { if (!v.empty()) std::memcpy(to + at, v.data(), sizeof(v[0]) * v.size()); };
     put(L.pre, P.pre); put(L.dec, P.dec); put(L.runs, P.runs); put(L.merge, P.merge); put(L.q_pos, P.q_pos); put(L.rots, P.rots);
-    put(L.sh_items, P.sh_items); put(L.sh_visits, P.sh_visits); put(L.sh_sees, P.sh_sees); put(L.sh_calls, P.sh_calls);
+    put(L.sh_items, P.sh_items); put(L.sh_visits, P.sh_visits); put(L.sh_sees, P.sh_sees); put(L.sh_calls, P.sh_calls); put(L.unpack, P.unpack);
 }
 
 // ---- the gradient -------------------------------------------------------------------------------------------------
@@ -638,7 +664,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     char *from = in_args ? (char *)blob.w : recorded ? held.data() : (char *)slot->host;
     write_lists(P, L, from);
 
-    const bool bf16 = c->cfg.dtype == PC_BF16;
+    const bool bf16 = c->cfg.dtype != PC_F32, mx4 = c->cfg.dtype == PC_MX4;
     PcWin W{};
     W.runs = (const PcWinRun *)(ws + L.runs);
     W.q_pos = (const int32_t *)(ws + L.q_pos);
@@ -675,8 +701,16 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         W.items = (const PcWinItem *)(ws + L.dec);
         const PcWinDecode O{(int32_t)L.dec, (int32_t)L.runs, (int32_t)L.q_pos, direct && !P.merge.empty() ? (int32_t)(L.lists / 16) : 0, ws};
         static_assert(PC_ARG_BYTES / 16 <= 256, "a thread for every 16 bytes");
-        pc_launch_win_decode_bf16(W, (int)P.dec.size(), direct ? &blob : nullptr, O, st);
+        if (mx4) pc_launch_win_decode_mx4(W, (int)P.dec.size(), direct ? &blob : nullptr, O, st);
+        else pc_launch_win_decode_bf16(W, (int)P.dec.size(), direct ? &blob : nullptr, O, st);
         PC_HIP(c, hipGetLastError());
+    }
+    if (mx4 && !P.pre.empty()) {                         // rows of prompts go over a bf16 copy of the tiles they see
+        ProfScope ps(c, 8, st);
+        const PcMx4Unpack U{(const int32_t *)(ws + L.unpack), (int32_t)P.unpack.size(), W.n_kv_heads, c->slots, c->k_store, c->v_store, ws + L.k_copy, ws + L.v_copy};
+        pc_launch_mx4_unpack(U, st);
+        PC_HIP(c, hipGetLastError());
+        W.k_store = U.k_to; W.v_store = U.v_to; W.slots = (int64_t)PC_TILE * U.n_tiles;
     }
     if (!P.sh_items.empty()) {
         ProfScope ps(c, 3, st);
@@ -694,7 +728,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     }
     if (!P.merge.empty()) {
         ProfScope ps(c, 4, st);
-        pc_launch_win_merge(W, (const PcMergeRow *)(ws + L.merge), (int)P.merge.size(), c->cfg.dtype, c->D, st);
+        pc_launch_win_merge(W, (const PcMergeRow *)(ws + L.merge), (int)P.merge.size(), bf16 ? PC_BF16 : PC_F32, c->D, st);
         PC_HIP(c, hipGetLastError());
     }
     return PC_OK;
@@ -779,6 +813,7 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
                                const float *lse, const void *d_out, float *d_q, float *d_k, float *d_v, hipStream_t st)
 {
     const char *what = "attend_window_backward";
+    if (c->cfg.dtype == PC_MX4) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: a PC_MX4 cache has no gradient", what);
     int32_t rc = check(c, what, calls, n_calls, window, n_sink);
     if (rc != PC_OK || n_calls == 0) return rc;
     if (!c->host_only) {
@@ -829,6 +864,12 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
 }
 
 }  // namespace
+
+// What a call lists is all in a window of 2^31 - 1 (positions are below 2^30 in magnitude: pc_cache_create).
+int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws)
+{
+    return attend_window(c, what, calls, n_calls, INT32_MAX, 0, q, out, lse, st, fixed_ws);
+}
 
 extern "C" {
 
