@@ -1,0 +1,147 @@
+"""What pc_append_projected*, pc_projected_backward, pc_messages_read and PC_MX4 caches refuse, before anything is enqueued (caches without a
+device: bookkeeping and validation)."""
+import ctypes as C
+
+import pytest
+
+from paper_2512_23049_amd import binding as b
+
+
+def cache(dtype=b.PC_BF16, flags=b.PC_FLAG_HOST_ONLY, capacity=512, messages=8, **kw):
+    return b.Cache(8, 2, 128, dtype, 1e4, capacity, messages, flags=flags, **kw)
+
+
+def rows(**kw):
+    return b.projected(0, 0, 0, 0, 0, 0, **kw)
+
+
+def code(f, *a, **kw):
+    with pytest.raises(b.PcError) as e:
+        f(*a, **kw)
+    return e.value.code
+
+
+@pytest.mark.parametrize("dtype", [b.PC_F32, b.PC_BF16, b.PC_MX4])
+def test_append_projected_keeps_the_books(dtype):
+    c = cache(dtype)
+    assert c.append_projected(rows(), [40, 1, 33], 0, reserves=[64, 0, 0]) == [0, 1, 2]
+    assert [c.message_info(m) for m in range(3)] == [(40, 0, 64), (1, 64, 1), (33, 96, 33)]
+    c.append_projected_tokens(rows(), [0], 0)
+    assert c.message_info(0)[0] == 41
+    assert code(c.append_projected_tokens, rows(), [0, 0], 0) == b.PC_ERR_INVALID_ARG
+    assert code(c.append_projected_tokens, rows(), [0, 7], 0) == b.PC_ERR_BAD_MSG_ID
+    assert code(c.append_projected_tokens, rows(), [1], 0) == b.PC_ERR_NO_SPACE
+    assert code(c.append_projected, rows(), [5, 0], 0) == b.PC_ERR_INVALID_ARG
+    assert code(c.append_projected, rows(), [500], 0) == b.PC_ERR_NO_SPACE
+    assert code(c.append_projected, rows(), [1] * 6, 0) == b.PC_ERR_NO_SPACE
+    for eps in (-1e-6, float("inf"), float("nan")):
+        assert code(c.append_projected, rows(eps=eps), [1], 0) == b.PC_ERR_INVALID_ARG
+    assert c.append_projected(rows(), [], 0) == []
+    assert c.cache_info()[:2] == (3, 160)
+
+
+def test_null_lists():
+    c, L = cache(), b.lib()
+    ids = (C.c_int32 * 1)()
+    p, to = rows(), b.projected_grad(0, 0, 0, 0, 0, 0)
+    one = (C.c_int32 * 1)(1)
+    assert L.pc_append_projected(c.h, None, 1, one, None, ids, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_append_projected(c.h, C.byref(p), 1, None, None, ids, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_append_projected(c.h, C.byref(p), 1, one, None, None, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_append_projected(c.h, C.byref(p), -1, one, None, ids, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_append_projected(None, C.byref(p), 1, one, None, ids, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_append_projected_tokens(c.h, C.byref(p), None, 1, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_projected_backward(c.h, C.byref(p), 1, one, None, None, None, None, C.byref(to), None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_projected_backward(c.h, C.byref(p), 1, one, one, None, None, None, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_messages_read(c.h, 1, None, None, None, None) == b.PC_ERR_INVALID_ARG
+    assert L.pc_messages_read(c.h, -1, one, None, None, None) == b.PC_ERR_INVALID_ARG
+
+
+def test_backward_lists():
+    c = cache()
+    to = b.projected_grad(0, 0, 0, 0, 0, 0)
+    c.append_projected(rows(), [40, 5], 0)
+    c.projected_backward(rows(), [0, 1], [40, 5], 0, 0, 0, to)
+    c.projected_backward(rows(), [0], [7], 0, 0, 0, to)
+    assert code(c.projected_backward, rows(), [0], [41], 0, 0, 0, to) == b.PC_ERR_SHAPE
+    assert code(c.projected_backward, rows(), [0], [0], 0, 0, 0, to) == b.PC_ERR_SHAPE
+    assert code(c.projected_backward, rows(), [2], [1], 0, 0, 0, to) == b.PC_ERR_BAD_MSG_ID
+    c.message_free(1)
+    assert code(c.projected_backward, rows(), [1], [1], 0, 0, 0, to) == b.PC_ERR_BAD_MSG_ID
+    assert code(c.messages_read, [0, 1], 0, 0) == b.PC_ERR_BAD_MSG_ID
+
+
+def test_four_bit_caches():
+    with pytest.raises(b.PcError):
+        b.Cache(8, 2, 64, b.PC_MX4, 1e4, 512, 8, flags=b.PC_FLAG_HOST_ONLY)
+    with pytest.raises(b.PcError):
+        b.Cache(34, 2, 128, b.PC_MX4, 1e4, 512, 8, flags=b.PC_FLAG_HOST_ONLY)
+    with pytest.raises(b.PcError):
+        cache(b.PC_MX4, max_position=1 << 30)
+    c = cache(b.PC_MX4)
+    cfg = c.cfg
+    assert b.lib().pc_cache_storage_bytes(C.byref(cfg)) == 2 * 512 * 2 * 68
+    c.append_projected(rows(), [40], 0)
+    c.reposition(0, 0)                                   # (where it is)
+    assert code(c.reposition, 0, 5) == b.PC_ERR_INVALID_ARG
+    assert code(c.reposition_batch, [0], [5]) == b.PC_ERR_INVALID_ARG
+    assert code(c.message_fork, [(0, 3, 10, 0, 7)]) == b.PC_ERR_INVALID_ARG
+    assert c.message_fork([(0, 3, 10, 0, 3), (0, 3, 10, 0, None)]) == [1, 2]
+    assert c.message_base(1) == 3
+    assert c.message_swap_bytes(0) == 2 * 64 * 2 * 68
+    to = b.projected_grad(0, 0, 0, 0, 0, 0)
+    assert code(c.projected_backward, rows(), [0], [40], 0, 0, 0, to) == b.PC_ERR_INVALID_ARG
+    assert code(c.attend_backward, [], 0, 0, 0, 0, 0, 0) == b.PC_ERR_INVALID_ARG
+    assert code(c.attend_window_backward, [], 5, 0, 0, 0, 0, 0, 0, 0, 0) == b.PC_ERR_INVALID_ARG
+    assert code(c.grad_keys_finalize, 0) == b.PC_ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_pointers_and_strides():
+    import torch
+    L, D, H, Hq = b.lib(), 128, 2, 8
+    for dtype, kind in ((b.PC_BF16, torch.bfloat16), (b.PC_MX4, torch.bfloat16), (b.PC_F32, torch.float32)):
+        c = cache(dtype, flags=0)
+        x = torch.zeros(4, (Hq + 2 * H) * D + 64, dtype=kind, device="cuda:0")
+        out = torch.zeros(4, Hq, D, dtype=kind, device="cuda:0")
+        es, p, s = x.element_size(), x.data_ptr(), x.stride(0)
+        k, v = p + Hq * D * es, p + (Hq + H) * D * es
+
+        def ask(q=p, k=k, v=v, qs=s, ks=s, vs=s, to=out.data_ptr(), **kw):
+            return c.append_projected(b.projected(q, k, v, qs, ks, vs, **kw), [4], to)
+        bad = [dict(q=p + es), dict(k=k + es), dict(v=v + 8), dict(k=0), dict(v=0), dict(q=0), dict(to=0), dict(to=out.data_ptr() + es), dict(qs=s + 1), dict(ks=s + 2),
+               dict(q_weight_ptr=p + 2), dict(k_weight_ptr=p + 1)]
+        for kw in bad:
+            assert code(ask, **kw) == b.PC_ERR_INVALID_ARG, kw
+        short = 16 // es
+        for kw in (dict(qs=Hq * D - short), dict(ks=H * D - short), dict(vs=0), dict(ks=-s)):
+            assert code(ask, **kw) == b.PC_ERR_SHAPE, kw
+        assert ask() == [0] and ask(q=0, to=0) == [1]
+        stream = torch.cuda.Stream()
+        if dtype != b.PC_MX4:
+            g = torch.zeros(512 * H * D, device="cuda:0")
+            to = b.projected_grad(p, k, v, s, s, s)
+            assert code(c.projected_backward, b.projected(p, k, v, s, s, s), [0], [4], 0, g.data_ptr(), g.data_ptr(), to) == b.PC_ERR_INVALID_ARG
+            assert code(c.projected_backward, b.projected(p, k, v, s, s, s), [0], [4], g.data_ptr(), 0, g.data_ptr(), to) == b.PC_ERR_INVALID_ARG
+            assert code(c.projected_backward, b.projected(p, k, v, s, s, s), [0], [4], g.data_ptr() + 4, g.data_ptr(), g.data_ptr(), to) == b.PC_ERR_INVALID_ARG
+            assert code(c.projected_backward, b.projected(p, k, v, s, s, s), [0], [4], g.data_ptr(), g.data_ptr(), g.data_ptr(),
+                        b.projected_grad(p, k, v, s, s - 1, s)) == b.PC_ERR_INVALID_ARG
+        else:
+            small = torch.zeros(64, Hq, D, dtype=kind, device="cuda:0")
+            from pc_inputs import Call
+            assert code(c.attend, [Call([], 0, 0, 4, None)], small.data_ptr() + 2, small.data_ptr()) == b.PC_ERR_INVALID_ARG
+            assert code(c.append_tokens, 0, k + es, v, 1) == b.PC_ERR_INVALID_ARG
+        graph = torch.cuda.CUDAGraph()
+        keep = torch.zeros(8, device="cuda:0")
+        with torch.cuda.graph(graph, stream=stream):     # refused, and what is captured stays whole
+            keep.add_(1)
+            st = torch.cuda.current_stream().cuda_stream
+            P = b.projected(p, k, v, s, s, s)
+            assert code(c.append_projected, P, [4], out.data_ptr(), stream=st) == b.PC_ERR_INVALID_ARG
+            assert code(c.append_projected_tokens, P, [0], out.data_ptr(), stream=st) == b.PC_ERR_INVALID_ARG
+            assert code(c.messages_read, [0], out.data_ptr(), 0, stream=st) == b.PC_ERR_INVALID_ARG
+        graph.replay()
+        torch.cuda.synchronize()
+        assert keep.sum().item() == 8
+        assert c.cache_info()[0] == 2
+        c.close()
