@@ -1,8 +1,11 @@
-// Attention of single tokens over a PC_MX4 cache, and its tiles unpacked for the kernels of many rows (gfx950).  What a row sees, and how
+// Attention over a PC_MX4 cache: single tokens, and rows of prompts (gfx950).  What a row sees, and how
 // the host states it: pc_window.h; how the cache holds keys and values: pc_mx4.h.
 #include "pc_window.h"
 #include "pc_mx4.h"
 #include "pc_mfma_common.h"
+
+#include <algorithm>
+#include <type_traits>
 
 #define MFMA16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
 
@@ -260,35 +263,82 @@ void pc_launch_win_decode_mx4(const PcWin &W, int n_items, const PcArgBlob *blob
     else pc_mx4_decode_kernel<<<grid, 256, 0, st>>>(W);
 }
 
-// ------------------------------------------------------------------------------------------------------------ unpack
-// A tile of one KV head as a bf16 cache has it: what the codes stand for is exact there.  Bound: memory (68 bytes read and 256
-// written for each key and value).
-__global__ __launch_bounds__(256) void pc_mx4_unpack_kernel(PcMx4Unpack U)
+// ----------------------------------------------------------------------------------------------------------- prepare
+// In front of the attention of rows: the call's lists to the workspace and the rotations of its runs (as win_turns), its queries turned
+// by their positions and the unit that their 8-bit pieces are in, and the values of the tiles that rows see, as a bf16 cache has them (what the
+// codes stand for is exact there; 68 bytes read and 256 written for each, once, where every workgroup of rows would convert them again).
+__device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare &P)
 {
-    const int kh = blockIdx.y;
-    const int64_t from = ((int64_t)kh * U.slots_from + U.slots[blockIdx.x]) / PC_TILE * PC_MX4_TILE;
-    const char *kt = (const char *)U.k_store + from, *vt = (const char *)U.v_store + from;
-    const int64_t to = ((int64_t)kh * U.n_tiles + blockIdx.x) * (PC_TILE * PC_D * 2);
-    {
-        const int row = threadIdx.x >> 3, c = threadIdx.x & 7;           // values 16 c to 16 c + 15
-        const uint2 w = *reinterpret_cast<const uint2 *>(kt + row * 64 + 8 * c);
-        const int e = (uint8_t)kt[PC_MX4_CODES + row * 4 + (c >> 1)];
-        const float unit = __uint_as_float((uint32_t)min(e, 254) << 23);
-        uint4 x[2];
-        uint32_t *o = reinterpret_cast<uint32_t *>(x);
-        const uint32_t words[2] = {w.x, w.y};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            o[4 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[i], unit, 0));
-            o[4 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[i], unit, 1));
-            o[4 * i + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[i], unit, 2));
-            o[4 * i + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[i], unit, 3));
+    __shared__ __attribute__((aligned(16))) float2 s_rot[PC_D / 2][33];           // [frequency][row]
+    int block = blockIdx.x;
+    if (block < P.list_blocks) {
+        const int64_t n_copy = from != P.ws ? P.n16 : 0, n_all = n_copy + (int64_t)P.n_rot * (PC_D / 2);
+        for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n_all; i += (int64_t)P.list_blocks * 256) {
+            if (i < n_copy) { reinterpret_cast<uint4 *>(P.ws)[i] = reinterpret_cast<const uint4 *>(from)[i]; continue; }
+            const int64_t k = (i - n_copy) / (PC_D / 2);
+            const int f = (int)((i - n_copy) % (PC_D / 2));
+            const float2 cs = rope_angle((double)reinterpret_cast<const int64_t *>(from + P.off_rot)[k] * P.inv_freq[f]);
+            P.rot_run[k * (PC_D / 2) + f] = make_float2(cs.x * P.scale_log2, cs.y * P.scale_log2);
         }
-        if (e == PC_MX4_NAN) x[0] = x[1] = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
-        uint4 *dst = reinterpret_cast<uint4 *>((char *)U.k_to + to + threadIdx.x * 32);
-        dst[0] = x[0];
-        dst[1] = x[1];
+        return;
     }
+    block -= P.list_blocks;
+    if (block < P.query_blocks) {                        // 32 rows, eight heads
+        const int chunks = (P.n_q_heads + 7) / 8;
+        const int64_t group = block / chunks, groups = ((int64_t)P.n_rows + 31) / 32;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, hh = lane >> 5;
+        for (int e = threadIdx.x; e < 32 * (PC_D / 2); e += 256) {
+            const int64_t R = group * 32 + e % 32;
+            if (R < P.n_rows) s_rot[e / 32][e % 32] = rope_turn(reinterpret_cast<const int32_t *>(from + P.off_q_pos)[R], P.inv_freq[e / 32]);
+        }
+        __syncthreads();
+        const int64_t R = group * 32 + n, row = R < P.n_rows ? R : P.n_rows - 1;
+#pragma unroll 1
+        for (int h = block % chunks * 8 + wave; h < min(P.n_q_heads, block % chunks * 8 + 8); h += 4) {
+            const unsigned char *qp = (const unsigned char *)P.q + (row * P.n_q_heads + h) * (PC_D * 2) + 32 * hh;
+            uint4 raw[8];                                // dims 16 hh, 32 + 16 hh, and 64 up, 16 each
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[i] = ldg16(qp + (i >> 1) * 64 + (i & 1) * 16);
+            float top = 0.f;
+            bool fine = true;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    top = fmaxf(top, fmaxf(fabsf(bf_lo(w[j])), fabsf(bf_hi(w[j]))));
+                    fine &= ((w[j] & 0x7F80u) != 0x7F80u) & ((w[j] & 0x7F800000u) != 0x7F800000u);
+                }
+            }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            fine &= __shfl_xor((int)fine, 32) != 0;
+            // a turn keeps a pair's norm, sqrt(2) times the larger value at most: the row's largest, scaled, between 128 and 256 (448 is the
+            // largest number of the pieces)
+            const int e = max(-100, min(100, (int)(__float_as_uint(top * P.scale_log2 * 1.4142137f) >> 23 & 255) - 134));
+            if (hh == 0) P.q_unit[(int64_t)h * groups * 32 + R] = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const uint4 lo = raw[(s >> 2) * 2 + (s >> 1 & 1)], hi = raw[4 + (s >> 2) * 2 + (s >> 1 & 1)];
+                const uint32_t lw[2] = {s & 1 ? lo.z : lo.x, s & 1 ? lo.w : lo.y}, hw[2] = {s & 1 ? hi.z : hi.x, s & 1 ? hi.w : hi.y};
+                float x[4], y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 cs = s_rot[(s >> 2) * 32 + 16 * hh + 4 * (s & 3) + j][n];
+                    const float a = j & 1 ? bf_hi(lw[j >> 1]) : bf_lo(lw[j >> 1]), b = j & 1 ? bf_hi(hw[j >> 1]) : bf_lo(hw[j >> 1]);
+                    x[j] = fine ? a * cs.x - b * cs.y : __builtin_nanf("");
+                    y[j] = fine ? a * cs.y + b * cs.x : __builtin_nanf("");
+                }
+                P.q_abs[mx4_query_at(groups, h, R, hh, s)] = make_float4(x[0], x[1], x[2], x[3]);
+                P.q_abs[mx4_query_at(groups, h, R, hh, s + 8)] = make_float4(y[0], y[1], y[2], y[3]);
+            }
+        }
+        return;
+    }
+    block -= P.query_blocks;
+    const int kh = block / P.n_tiles, tile = block % P.n_tiles;
+    const int slot0 = reinterpret_cast<const int32_t *>(from + P.off_tiles)[tile];
+    const char *vt = (const char *)P.v_store + ((int64_t)kh * P.slots + slot0) / PC_TILE * PC_MX4_TILE;
+    char *to = (char *)P.v_to + ((int64_t)kh * P.n_tiles + tile) * (PC_TILE * PC_D * 2);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int grp = (threadIdx.x >> 7) + 2 * i, d = threadIdx.x & 127;
@@ -303,11 +353,371 @@ __global__ __launch_bounds__(256) void pc_mx4_unpack_kernel(PcMx4Unpack U)
             const float u0 = __uint_as_float((187u - min(es & 255u, 120u)) << 23), u1 = __uint_as_float((187u - min(es >> 8 & 255u, 120u)) << 23);
             o[j] = pack_bf16(bf_lo(cw[j]) * u0, bf_hi(cw[j]) * u1);
         }
-        *reinterpret_cast<uint4 *>((char *)U.v_to + to + (grp * 128 + d) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<uint4 *>(to + (grp * 128 + d) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
-void pc_launch_mx4_unpack(const PcMx4Unpack &U, hipStream_t st)
+__global__ __launch_bounds__(256) void pc_mx4_prepare_kernel(PcMx4Prepare P) { mx4_prepare((const char *)P.from, P); }
+__global__ __launch_bounds__(256) void pc_mx4_prepare_arg_kernel(PcArgBlob, PcMx4Prepare P) { mx4_prepare((const char *)arguments(), P); }       // (the blob comes first)
+
+void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st)
 {
-    if (U.n_tiles > 0) pc_mx4_unpack_kernel<<<dim3((unsigned)U.n_tiles, (unsigned)U.n_kv_heads), 256, 0, st>>>(U);
+    P.list_blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>((P.n16 + (int64_t)P.n_rot * (PC_D / 2) + 255) / 256, 1024));
+    P.query_blocks = (P.n_rows + 31) / 32 * ((P.n_q_heads + 7) / 8);
+    const unsigned grid = (unsigned)(P.list_blocks + P.query_blocks + P.n_tiles * P.n_kv_heads);
+    if (blob) pc_mx4_prepare_arg_kernel<<<grid, 256, 0, st>>>(*blob, P);
+    else pc_mx4_prepare_kernel<<<grid, 256, 0, st>>>(P);
+}
+
+// -------------------------------------------------------------------------------------------------------------- rows
+// A workgroup is 4 waves = 4 consecutive units (32 rows x head, heads of a KV head fastest) over the same run of tiles, two
+// workgroups a compute unit: the transposed problem of the bf16 kernel (S^T = K . Q^T, O^T = V^T . P^T, see pc_kernels_window.hip, which
+// this one follows in its softmax, masks and ring of direct loads).  What is its own:
+//   scores   codes of keys straight from the ring to v_mfma_scale 32x32x64, by two e4m3 pieces of the turned queries: as long on the matrix unit
+//            as bf16 keys would be (twice the work at twice the rate), a quarter of the reads from shared memory;
+//   queries  come turned by their positions (pc_mx4_prepare_kernel) and are turned back by a run's rotation in 32 bits, then cut in pieces under one
+//            power of two for the row, the same for every turn;
+//   values   come from the copy; they are finite, so that a probability of zero takes a key out.
+#define LAZY_LOG2 64.0f
+#define MFMA32(a, b, c) __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0)
+
+namespace {
+__device__ __forceinline__ int imax3(int a, int b, int c) { return max(max(a, b), c); }
+template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
+__device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "memory"); }
+// One 16-byte (4-byte) per lane direct load: lane l's bytes land at lds_wave_base + 16 l (4 l); completion is awaited with wait_vm.
+__device__ __forceinline__ void dma16(const void *gbase_uniform, unsigned lane_off, unsigned lds_wave_base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 ::"s"(lds_wave_base), "v"(lane_off), "s"(gbase_uniform) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const void *gbase_uniform, unsigned lane_off, unsigned lds_wave_base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 ::"s"(lds_wave_base), "v"(lane_off), "s"(gbase_uniform) : "memory", "m0");
+}
+template <int BYTE> __device__ __forceinline__ f32x16 scores32(uint4 codes, int e_codes, i32x8 q, int e_q, f32x16 c)
+{
+    const i32x8 a = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, c, 4, 0, BYTE, e_codes, 0, e_q);
+}
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+// four values as e4m3 in units of `unit`
+__device__ __forceinline__ int pieces4(const float (&x)[4], float unit)
+{
+    s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[0], x[1], unit, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[2], x[3], unit, true);
+    return __builtin_bit_cast(int, r);
+}
+}  // namespace
+
+__global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Rows M)
+{
+    constexpr int RING = 4, AHEAD = 3, LOADS = 3;
+    constexpr int VALUES = PC_MX4_CODES, EXPS = VALUES + PC_TILE * PC_D * 2, SLOT = EXPS + 256;        // of a place in the ring: codes of keys, values, exponents
+    __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING * SLOT];
+    __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
+
+    const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
+    const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
+    const int g = W.n_q_heads / W.n_kv_heads;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int n_units = ((item.n_q + 31) >> 5) * g;
+    const bool unit_ok = item.unit0 + wave < n_units;
+    const int unit = unit_ok ? item.unit0 + wave : item.unit0;
+    const int ub = unit / g, h = kh * g + (unit - ub * g);
+    const int last_row = min(32 * ub + 31, item.n_q - 1), row = min(32 * ub + n, last_row);
+    const bool row_ok = unit_ok && 32 * ub + n < item.n_q;
+    const int64_t R = (int64_t)item.q_off + row;
+    const int lim = item.lim0 + row, lim_first = item.lim0 + 32 * ub;       // (lim_first: uniform)
+    int lo = 0, lo_max = 0;                              // the least position the row sees; the largest such of the wave's rows
+    auto look_up_rows = [&]() __attribute__((always_inline)) {
+        lo = win_low(W.q_pos[R], W.window);
+        lo_max = lo;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o));
+        lo_max = uniform(lo_max);
+    };
+    const int64_t groups = ((int64_t)M.n_rows + 31) / 32;
+    const float4 *q_abs = M.q_abs + mx4_query_at(groups, h, R, hh, 0);
+    const float q_unit = M.q_unit[(int64_t)h * groups * 32 + R], q_rest = q_unit * 0.0625f;
+    const int e_hi = (int)(__float_as_uint(q_unit) >> 23), e_lo = e_hi - 4;
+
+    const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * (W.slots / PC_TILE) * PC_MX4_TILE;
+    const unsigned char *vb = (const unsigned char *)M.v_tiles + (int64_t)kh * M.v_slots * (PC_D * 2);
+    // position p of a tile's codes (16 bytes each) holds block (p & 3) ^ (p >> 4 & 3) of key p >> 2: four keys fill the banks
+    const unsigned lds0 = (unsigned)(uintptr_t)&s_kv[0];
+    const unsigned k_src = (unsigned)((threadIdx.x & 127) >> 2) * 64 + (((threadIdx.x & 3) ^ (threadIdx.x >> 4 & 3)) << 4), v_src = threadIdx.x * 16;
+    const unsigned e_src = PC_MX4_CODES + (unsigned)(lane & 31) * 4;
+    auto request = [&](int slot0, int place, int at) __attribute__((always_inline)) {
+        const unsigned char *kt = kb + (int64_t)(slot0 / PC_TILE) * PC_MX4_TILE, *vt = vb + (int64_t)(slot0 + place) * (PC_D * 2);
+        const unsigned to = lds0 + at * SLOT;
+        if (wave < 2) dma16(kt, k_src, to + wave * 1024);
+        else dma4(kt, e_src, to + EXPS);                 // (both waves the same: every wave asks as often)
+        dma16(vt, v_src, to + VALUES + wave * 1024);
+        dma16(vt + 4096, v_src, to + VALUES + 4096 + wave * 1024);
+    };
+
+    i32x8 q_hi[2], q_lo[2];
+    // (few: in the walk, what is read for all of it at once would not fit the registers)
+    auto turn = [&](int rot, auto few) __attribute__((always_inline)) {
+        const float2 own = W.rot_run[(int64_t)rot * (PC_D / 2) + lane];
+        const float4 *from = q_abs;
+        asm volatile("" : "+v"(from));                   // (sixteen addresses, made once and kept, would not fit the registers)
+        in_order();
+        s_rot[wave][lane] = own;
+        in_order();
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float4 a = from[64 * s], b = from[64 * (s + 8)];
+            const float4 *r = reinterpret_cast<const float4 *>(&s_rot[wave][(s >> 2) * 32 + 16 * hh + 4 * (s & 3)]);
+            const float4 r0 = r[0], r1 = r[1];
+            const float x[4] = {a.x * r0.x + b.x * r0.y, a.y * r0.z + b.y * r0.w, a.z * r1.x + b.z * r1.y, a.w * r1.z + b.w * r1.w};
+            const float y[4] = {b.x * r0.x - a.x * r0.y, b.y * r0.z - a.y * r0.w, b.z * r1.x - a.z * r1.y, b.w * r1.z - a.w * r1.w};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const float (&z)[4] = half ? y : x;
+                const int hi = pieces4(z, q_unit);
+                const auto b0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, q_unit, false), b1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, q_unit, true);
+                const float rest[4] = {z[0] - b0[0], z[1] - b0[1], z[2] - b1[0], z[3] - b1[1]};
+                q_hi[half][s] = hi;
+                q_lo[half][s] = pieces4(rest, q_rest);
+            }
+            if (decltype(few)::value && (s & 1)) __builtin_amdgcn_sched_barrier(0);
+        }
+        in_order();
+    };
+
+    // K row of the lane's MFMA row: permuted so that score registers 0..7 / 8..15 are keys 8 hh + 0..7 / 16 + 8 hh + 0..7
+    const int krow = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+    typedef const __attribute__((address_space(3))) bf16x8 *lds_frag;
+    typedef const __attribute__((address_space(3))) int *lds_word;
+    unsigned k_rd = lds0 + krow * 64 + ((hh ^ (krow >> 2 & 3)) << 4);          // block hh; block 2 + hh: at k_rd ^ 32
+    asm volatile("" : "+v"(k_rd));
+    unsigned v_rd = lds0 + VALUES + (hh * PC_D + n) * 16;
+    asm volatile("" : "+v"(v_rd));
+    unsigned e_rd = lds0 + EXPS + krow * 4;
+    asm volatile("" : "+v"(e_rd));
+
+    float m_ref = 0.f, l_run = 0.f;
+    bool seen = false, all_seen = false, shifted = false;          // the row has met a key; every row of the wave has; some row's reference has moved
+    f32x16 acc[4];
+    const f32x16 zeros = (f32x16){0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int db = 0; db < 4; ++db) acc[db] = zeros;
+
+    auto fi = [](float x) { return __float_as_int(x); };
+    auto largest = [&](const f32x16 &s) __attribute__((always_inline)) {        // (on the bit patterns: right wherever some score is positive)
+        int m = imax3(fi(s[0]), fi(s[1]), fi(s[2]));
+#pragma unroll
+        for (int r = 3; r < 15; r += 2) m = imax3(m, fi(s[r]), fi(s[r + 1]));
+        return max(m, fi(s[15]));
+    };
+    // the reference moves, if a row's scores ask for it; s: scores less the reference
+    auto rebase = [&](f32x16 &s) __attribute__((always_inline)) {
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const bool now = mx > -INFINITY, need = mx > LAZY_LOG2 || (!seen && now && mx < -LAZY_LOG2);
+        seen |= now;
+        all_seen = __builtin_amdgcn_ballot_w64(seen) == ~0ull;
+        if (__builtin_amdgcn_ballot_w64(need) != 0) {
+            const float shift = need ? mx : 0.f, alpha = ex2(-fmaxf(shift, 0.f));       // (down: nothing has been added yet)
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < 4; ++db) acc[db] *= alpha;
+            m_ref += shift;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] -= shift;
+            shifted = __builtin_amdgcn_ballot_w64(m_ref != 0.f) != 0;
+        }
+    };
+    auto less_reference = [&](f32x16 &s) __attribute__((always_inline)) {
+        if (__builtin_expect(shifted, 0)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] -= m_ref;
+        }
+    };
+    auto score = [&](unsigned at) __attribute__((always_inline)) {
+        const uint4 k0 = __builtin_bit_cast(uint4, *(lds_frag)(k_rd + at)), k1 = __builtin_bit_cast(uint4, *(lds_frag)((k_rd ^ 32) + at));
+        const int e = (int)((unsigned)*(lds_word)(e_rd + at) >> (8 * hh));
+        f32x16 s = scores32<0>(k0, e, q_lo[0], e_lo, zeros);
+        s = scores32<2>(k1, e, q_lo[1], e_lo, s);
+        s = scores32<0>(k0, e, q_hi[0], e_hi, s);
+        return scores32<2>(k1, e, q_hi[1], e_hi, s);
+    };
+    const int T = item.n_tiles;
+    if (T > 0) {
+        // two walks over the same runs: of the tiles that are asked for, and of those that are worked on
+        WinWalk ahead(W.runs + item.run0, item.skip, T), walk = ahead;
+        auto place_of = [&](const WinWalk &w) __attribute__((always_inline)) {
+            return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(M.places) +
+                                                                                     (w.run - reinterpret_cast<uintptr_t>(W.runs)) / sizeof(PcWinRun) * sizeof(int32_t));
+        };
+        int asked = 0, place = place_of(ahead);
+        auto further = [&]() __attribute__((always_inline)) {
+            const bool same = ahead.a.z > PC_TILE;
+            ahead.next();
+            if (!same) place = place_of(ahead);
+        };
+        auto ask = [&](int at) __attribute__((always_inline)) {
+            if (asked >= T) return;
+            request(ahead.a.x, place, at);
+            if (++asked < T) further();
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) ask(i);
+        int cur = walk.rot;
+        turn(cur, std::false_type{});
+        look_up_rows();                                  // (behind the first requests: its latency is not theirs)
+        int t = 0;
+#pragma unroll 1
+        while (t < T) {
+            // Four tiles of which every row sees everything, the ring's places as constants: nothing is looked up, masked or turned.
+            if ((t & (RING - 1)) == 0 && walk.a.z >= RING * PC_TILE && walk.rot == cur && all_seen && !shifted &&
+                (lo_max <= walk.a.y || walk.a.w >= RING * PC_TILE) && (!walk.self || lim_first - walk.a.y >= RING * PC_TILE - 1) &&
+                T - asked >= RING && ahead.a.z > (RING - 1) * PC_TILE) {
+                const int slot0 = ahead.a.x;
+#pragma unroll
+                for (int u = 0; u < RING; ++u) {
+                    const int at = u * SLOT;
+                    wait_vm<LOADS * (AHEAD - 1)>();
+                    ring_barrier();
+                    request(slot0 + PC_TILE * u, place, (u + AHEAD) & (RING - 1));
+                    f32x16 s = score(at);
+                    bf16x8 fr[8];
+#pragma unroll
+                    for (int f = 0; f < 8; ++f) fr[f] = *(lds_frag)(v_rd + at + ((f >> 2) * 2 * PC_D + 32 * (f & 3)) * 16);
+                    less_reference(s);
+                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(largest(s) > fi(LAZY_LOG2)) != 0, 0)) rebase(s);
+                    uint32_t pk[8];
+                    float ps = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const float a = ex2(s[2 * r]), b = ex2(s[2 * r + 1]);
+                        ps += a;
+                        ps += b;
+                        pk[r] = pack_bf16(a, b);
+                    }
+                    l_run += ps;
+                    const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
+#pragma unroll
+                    for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(fr[f], p[f >> 2], acc[f & 3]);
+                }
+                asked += RING;
+                ahead.pass(RING - 1);
+                if (asked < T) further();
+                t += RING;
+                walk.pass(RING - 1);
+                if (t < T) walk.next();
+                continue;
+            }
+            const int u = t & (RING - 1);
+            const unsigned at = u * SLOT;
+            if (t + AHEAD <= T) wait_vm<LOADS * (AHEAD - 1)>();        // this wave's share of tile t has landed
+            else wait_vm<0>();
+            ring_barrier();                              // ... every wave's has, and tile t - 1 is no longer read
+            const WinTile e = walk.tile();
+            if (__builtin_expect(e.rot != cur, 0)) { cur = e.rot; turn(cur, std::true_type{}); }
+            ask((u + AHEAD) & (RING - 1));
+            f32x16 s = score(at);
+            less_reference(s);
+            const bool edge = e.valid < PC_TILE || (e.self && lim_first - e.pos0 < PC_TILE - 1) || (lo_max > e.pos0 && e.sink < PC_TILE);
+            bool none = false;
+            if (__builtin_expect(edge, 0)) {
+                const uint32_t sees = win_sees(e.pos0, e.valid, e.sink, e.self != 0, lo, lim);
+                none = __builtin_amdgcn_ballot_w64(sees != 0) == 0;
+                const int mine = (int)(sees >> (8 * hh));
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = (mine >> (16 * (r >> 3) + (r & 7))) & 1 ? s[r] : -INFINITY;
+            }
+            if (!none) {
+                if (__builtin_expect(!all_seen || __builtin_amdgcn_ballot_w64(largest(s) > fi(LAZY_LOG2)) != 0, 0)) rebase(s);
+                uint32_t pk[8];
+                float ps = 0.f;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float a = ex2(s[2 * r]), b = ex2(s[2 * r + 1]);
+                    ps += a;
+                    ps += b;
+                    pk[r] = pack_bf16(a, b);
+                }
+                if (__builtin_expect(edge, 0)) {
+                    // (a row of few keys: the sum of the probabilities as the products take them, so that their rounding cancels)
+                    ps = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) ps += bf_lo(pk[r]) + bf_hi(pk[r]);
+                }
+                const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
+                bf16x8 fr[8];
+#pragma unroll
+                for (int f = 0; f < 8; ++f) fr[f] = *(lds_frag)(v_rd + at + ((f >> 2) * 2 * PC_D + 32 * (f & 3)) * 16);
+                l_run += ps;
+#pragma unroll
+                for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(fr[f], p[f >> 2], acc[f & 3]);
+            }
+            ++t;
+            if (t < T) walk.next();
+        }
+    }
+    ring_barrier();
+
+    // results leave as whole cache lines, turned round in the wave's quarter of the ring: chunk c (16 bytes) of row r at c ^ (r & 15)
+    const float l = l_run + __shfl_xor(l_run, 32);
+    unsigned char *stg = &s_kv[0] + wave * 8192;
+    const int r4 = lane >> 4, c = lane & 15;
+    if (item.part < 0) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                uint2 w;
+                w.x = pack_bf16(acc[db][4 * q4] * inv, acc[db][4 * q4 + 1] * inv);
+                w.y = pack_bf16(acc[db][4 * q4 + 2] * inv, acc[db][4 * q4 + 3] * inv);
+                *reinterpret_cast<uint2 *>(stg + n * 256 + (((4 * db + q4) ^ (n & 15)) << 4) + 8 * hh) = w;
+            }
+        in_order();
+        unsigned char *dst = (unsigned char *)W.out + ((int64_t)item.q_off * W.n_q_heads + h) * (PC_D * 2) + 16 * c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + r4, rw = 32 * ub + r;
+            const uint4 v = *reinterpret_cast<const uint4 *>(stg + r * 256 + ((c ^ (r & 15)) << 4));
+            if (unit_ok && rw < item.n_q) *reinterpret_cast<uint4 *>(dst + (int64_t)rw * W.n_q_heads * (PC_D * 2)) = v;
+        }
+        if (W.lse && row_ok && hh == 0) W.lse[R * W.n_q_heads + h] = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
+        return;
+    }
+    float *dst = W.part_o + ((int64_t)item.part * W.n_q_heads + h) * PC_D + 4 * c;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {               // half a row is 256 bytes
+        in_order();
+#pragma unroll
+        for (int db = 0; db < 2; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x16 &a = acc[2 * half + db];
+                *reinterpret_cast<float4 *>(stg + n * 256 + (((8 * db + 2 * q4 + hh) ^ (n & 15)) << 4)) = make_float4(a[4 * q4], a[4 * q4 + 1], a[4 * q4 + 2], a[4 * q4 + 3]);
+            }
+        in_order();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + r4, rw = 32 * ub + r;
+            const float4 v = *reinterpret_cast<const float4 *>(stg + r * 256 + ((c ^ (r & 15)) << 4));
+            if (unit_ok && rw < item.n_q) *reinterpret_cast<float4 *>(dst + (int64_t)rw * W.n_q_heads * PC_D + 64 * half) = v;
+        }
+    }
+    if (row_ok && hh == 0) {
+        float *ml = W.part_ml + (((int64_t)item.part + row) * W.n_q_heads + h) * 2;
+        ml[0] = l == 0.f ? -INFINITY : m_ref;
+        ml[1] = l;
+    }
+}
+
+void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, hipStream_t st)
+{
+    if (n_items > 0) pc_mx4_prefill_kernel<<<(unsigned)n_items * W.n_kv_heads, 256, 0, st>>>(W, M);
 }

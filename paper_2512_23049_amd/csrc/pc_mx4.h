@@ -20,16 +20,37 @@
 #define PC_MX4_E_MAX 60
 #define PC_MX4_NAN 255                // exponent of a block of keys that are NaN
 
-// Tiles whose keys and values are laid out as a bf16 cache has them, for the kernels of many rows.
-struct PcMx4Unpack {
-    const int32_t *slots;             // [n_tiles] first slot of each
-    int32_t        n_tiles;
-    int32_t        n_kv_heads;
-    int64_t        slots_from;        // capacity of the cache
-    const void    *k_store, *v_store;
-    void          *k_to, *v_to;       // [n_kv_heads][32 n_tiles][128], [n_kv_heads][4 n_tiles][128][8]
+struct PcWin;
+// Rows of prompts: what a launch makes in front of their attention.
+struct PcMx4Prepare {
+    const void   *from;               // the call's lists (n16 pieces of 16 bytes), or null: in the arguments
+    void         *ws;                 // where they go
+    int32_t       n16;
+    int32_t       off_q_pos, off_rot, off_tiles;      // within them: positions (int32), runs' rotations (int64), first slots of the tiles that rows see (int32)
+    int32_t       n_rows, n_rot, n_tiles;
+    int32_t       n_q_heads, n_kv_heads;
+    float         scale_log2;         // rides on the runs' rotations
+    float2       *rot_run;            // [n_rot][64]
+    const void   *q;
+    float4       *q_abs;              // queries turned by their positions (see mx4_query_at)
+    float        *q_unit;             // [n_q_heads][rows, rounded up to 32]: 2^e
+    const double *inv_freq;
+    int64_t       slots;
+    const void   *v_store;
+    void         *v_to;               // [n_kv_heads][4 n_tiles][128][8]: the tiles' values as a bf16 cache has them
+    int32_t       list_blocks, query_blocks;          // of the grid
 };
-void pc_launch_mx4_unpack(const PcMx4Unpack &U, hipStream_t st);
+void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st);
+// What the attention of rows needs besides PcWin (whose v_store and rot_q are not read).
+struct PcMx4Rows {
+    const float4  *q_abs;
+    const float   *q_unit;
+    const int32_t *places;            // of each run: what is added to a slot for its place among v_tiles' slots
+    const void    *v_tiles;
+    int64_t        v_slots;
+    int32_t        n_rows;
+};
+void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, hipStream_t st);
 
 #ifdef __HIPCC__
 // the code of |x| 2^-e (a, not NaN), without its sign
@@ -62,6 +83,10 @@ __device__ __forceinline__ int mx4_exponent(double top)
 }
 __device__ __forceinline__ float mx4_power(float, int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 __device__ __forceinline__ double mx4_power(double, int e) { return __hiloint2double((int)((uint32_t)(e + 1023) << 20), 0); }
+// Where a query's dims stand among those that are turned by their positions: four of them (lane half hh, s = 0..3: 16 hh + 4 s, s = 4..7:
+// 32 + 16 hh + 4 (s - 4), s + 8: 64 further), rows side by side.  So lanes have what the matrix instruction takes from them as bytes
+// (its k of a half hh: 16 hh to 16 hh + 15, and 32 further), and a pair of a turn is in one lane.
+__device__ __forceinline__ int64_t mx4_query_at(int64_t groups, int h, int64_t R, int hh, int s) { return ((h * groups + (R >> 5)) * 16 + s) * 64 + hh * 32 + (R & 31); }
 // where word (m, db) of a value's dimension d stands in its group
 __device__ __forceinline__ int mx4_word(int d) { return (d & 15) * 8 + (d >> 4); }
 #endif

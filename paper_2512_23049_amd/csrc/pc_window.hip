@@ -31,7 +31,8 @@ struct WinPlan {
     std::vector<int64_t> rots;
     std::vector<PcMergeRow> merge;
     int64_t part_rows = 0, part_first = 0;    // partial rows [part_first, part_rows) are used
-    std::vector<int32_t> unpack;              // PC_MX4: first slots of the tiles that rows of prompts see, each once; their runs name places among these
+    std::vector<int32_t> tiles, places;       // PC_MX4: first slots of the tiles that rows of prompts see, each once; of each of their runs, what is added to a slot
+                                              // for its place among these
     int32_t window = 0, n_sink = 0;
     // single tokens of calls that list the same messages
     std::vector<PcWinSharedItem> sh_items;
@@ -298,22 +299,22 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     return true;
 }
 
-// The tiles that the runs name, each once, in slot order; the runs then name their places among these (runs of consecutive tiles stay
-// consecutive).
-void unpacked(WinPlan &P)
+// The tiles that the runs name, each once, in slot order, and the runs' places among these (consecutive tiles stay consecutive).
+void list_tiles(WinPlan &P)
 {
+    P.tiles.clear(); P.places.clear();
     std::vector<std::pair<int32_t, int32_t>> spans;      // slots [first, second)
     for (const PcWinRun &r : P.runs) spans.push_back({r.slot0, r.slot0 + (r.n_tok + PC_TILE - 1) / PC_TILE * PC_TILE});
     std::sort(spans.begin(), spans.end());
     std::vector<std::pair<int32_t, int32_t>> first;      // a joined span's first slot, and its place
     int32_t end = -1;
     for (const auto &s : spans) {
-        if (s.first > end || first.empty()) { first.push_back({s.first, (int32_t)P.unpack.size() * PC_TILE}); end = s.first; }
-        for (; end < s.second; end += PC_TILE) P.unpack.push_back(end);
+        if (s.first > end || first.empty()) { first.push_back({s.first, (int32_t)P.tiles.size() * PC_TILE}); end = s.first; }
+        for (; end < s.second; end += PC_TILE) P.tiles.push_back(end);
     }
-    for (PcWinRun &r : P.runs) {
+    for (const PcWinRun &r : P.runs) {
         const auto it = std::upper_bound(first.begin(), first.end(), std::make_pair(r.slot0, INT32_MAX)) - 1;
-        r.slot0 = it->second + (r.slot0 - it->first);
+        P.places.push_back(it->second - it->first);
     }
 }
 
@@ -356,8 +357,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8
     if (c->cfg.dtype == PC_F32) return;
     const size_t runs = P.runs.size(), rots = P.rots.size(), merge = P.merge.size();
     const int64_t part_rows = P.part_rows;
-    P.unpack.clear();
-    if (c->cfg.dtype == PC_MX4) unpacked(P);
+    if (c->cfg.dtype == PC_MX4) list_tiles(P);
     for (size_t i = 0; i < P.calls.size(); ++i) {
         if (P.calls[i].n_q != 1) continue;
         const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, P.calls[i], 0, 1);
@@ -371,7 +371,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8
 }
 
 // lists as they are staged, then what the device makes of them
-struct WinLayout { size_t pre, dec, runs, merge, q_pos, rots, sh_items, sh_visits, sh_sees, sh_calls, unpack, lists, rot_q, rot_run, part_o, part_ml, k_copy, v_copy, total; };
+struct WinLayout { size_t pre, dec, runs, merge, q_pos, rots, sh_items, sh_visits, sh_sees, sh_calls, tiles, places, lists, rot_q, rot_run, part_o, part_ml, q_abs, q_unit, v_tiles, total; };
 
 WinLayout lay_out(const pc_cache *c, const WinPlan &P)
 {
@@ -388,17 +388,20 @@ WinLayout lay_out(const pc_cache *c, const WinPlan &P)
     L.sh_visits = take(sizeof(PcWinVisit) * P.sh_visits.size());
     L.sh_sees = take(sizeof(PcWinSee) * P.sh_sees.size());
     L.sh_calls = take(sizeof(PcWinSharedCall) * P.sh_calls.size());
-    L.unpack = take(sizeof(int32_t) * P.unpack.size());
+    L.tiles = take(sizeof(int32_t) * P.tiles.size());
+    L.places = take(sizeof(int32_t) * P.places.size());
     L.lists = at;
     auto big = [&](size_t bytes) { const size_t a = align_up(at, 256); at = a + bytes; return a; };
     const size_t rot = P.pre.empty() ? 0 : sizeof(float2) * (size_t)c->half;
-    L.rot_q = big((c->cfg.dtype != PC_F32 ? rot / 2 : rot) * align_up(P.q_pos.size(), 32));         // (bf16: rot_lanes)
+    const bool mx4 = c->cfg.dtype == PC_MX4;
+    L.rot_q = big(mx4 ? 0 : (c->cfg.dtype == PC_BF16 ? rot / 2 : rot) * align_up(P.q_pos.size(), 32));         // (bf16: rot_lanes)
     L.rot_run = big(rot * P.rots.size());
     L.part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads * (size_t)c->D);
     L.part_ml = big(sizeof(float) * 2 * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads);
-    const size_t copy = (size_t)PC_TILE * (size_t)c->D * c->esize * (size_t)c->cfg.n_kv_heads * P.unpack.size();
-    L.k_copy = big(copy);
-    L.v_copy = big(copy);
+    const size_t turned = mx4 && !P.pre.empty() ? align_up(P.q_pos.size(), 32) * (size_t)c->cfg.n_q_heads : 0;
+    L.q_abs = big(sizeof(float) * (size_t)c->D * turned);
+    L.q_unit = big(sizeof(float) * turned);
+    L.v_tiles = big((size_t)PC_TILE * (size_t)c->D * c->esize * (size_t)c->cfg.n_kv_heads * P.tiles.size());
     L.total = align_up(at, 256);
     return L;
 }
@@ -407,7 +410,7 @@ void write_lists(const WinPlan &P, const WinLayout &L, char *to)
 {
     auto put = [&](size_t at, const auto &v) { if (!v.empty()) std::memcpy(to + at, v.data(), sizeof(v[0]) * v.size()); };
     put(L.pre, P.pre); put(L.dec, P.dec); put(L.runs, P.runs); put(L.merge, P.merge); put(L.q_pos, P.q_pos); put(L.rots, P.rots);
-    put(L.sh_items, P.sh_items); put(L.sh_visits, P.sh_visits); put(L.sh_sees, P.sh_sees); put(L.sh_calls, P.sh_calls); put(L.unpack, P.unpack);
+    put(L.sh_items, P.sh_items); put(L.sh_visits, P.sh_visits); put(L.sh_sees, P.sh_sees); put(L.sh_calls, P.sh_calls); put(L.tiles, P.tiles); put(L.places, P.places);
 }
 
 // ---- the gradient -------------------------------------------------------------------------------------------------
@@ -682,6 +685,17 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         ProfScope ps(c, 1, st);
         if (recorded && !in_args) pc_launch_store_args(from, L.lists, ws, st);
         const bool turns = !P.pre.empty();
+        if (mx4 && turns) {
+            PcMx4Prepare T{};
+            T.from = in_args || recorded ? ws : slot->host; T.ws = ws; T.n16 = (int)(L.lists / 16);
+            T.off_q_pos = (int)L.q_pos; T.off_rot = (int)L.rots; T.off_tiles = (int)L.tiles;
+            T.n_rows = (int)P.q_pos.size(); T.n_rot = (int)P.rots.size(); T.n_tiles = (int)P.tiles.size();
+            T.n_q_heads = W.n_q_heads; T.n_kv_heads = W.n_kv_heads; T.scale_log2 = W.scale_log2;
+            T.rot_run = (float2 *)(ws + L.rot_run);
+            T.q = q; T.q_abs = (float4 *)(ws + L.q_abs); T.q_unit = (float *)(ws + L.q_unit);
+            T.inv_freq = c->inv_freq_dev; T.slots = c->slots; T.v_store = c->v_store; T.v_to = ws + L.v_tiles;
+            pc_launch_mx4_prepare(T, in_args ? &blob : nullptr, st);
+        } else {
         PcWinTurns T{};
         T.from = in_args || recorded ? ws : slot->host; T.ws = ws; T.n16 = (int)(L.lists / 16);
         T.off_q_pos = (int)L.q_pos; T.n_rows = turns ? (int)P.q_pos.size() : 0;
@@ -693,6 +707,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         T.rot_run = (float2 *)(ws + L.rot_run);
         T.inv_freq = c->inv_freq_dev;
         if (!(recorded && !in_args) || turns) pc_launch_win_turns(T, in_args ? &blob : nullptr, st);
+        }
         PC_HIP(c, hipGetLastError());
         if (slot) { rc = pc_stage_release(c, slot, st); if (rc != PC_OK) return rc; }
     }
@@ -705,13 +720,6 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         else pc_launch_win_decode_bf16(W, (int)P.dec.size(), direct ? &blob : nullptr, O, st);
         PC_HIP(c, hipGetLastError());
     }
-    if (mx4 && !P.pre.empty()) {                         // rows of prompts go over a bf16 copy of the tiles they see
-        ProfScope ps(c, 8, st);
-        const PcMx4Unpack U{(const int32_t *)(ws + L.unpack), (int32_t)P.unpack.size(), W.n_kv_heads, c->slots, c->k_store, c->v_store, ws + L.k_copy, ws + L.v_copy};
-        pc_launch_mx4_unpack(U, st);
-        PC_HIP(c, hipGetLastError());
-        W.k_store = U.k_to; W.v_store = U.v_to; W.slots = (int64_t)PC_TILE * U.n_tiles;
-    }
     if (!P.sh_items.empty()) {
         ProfScope ps(c, 3, st);
         const PcWinShared S{(const PcWinSharedItem *)(ws + L.sh_items), (const PcWinVisit *)(ws + L.sh_visits), (const PcWinSee *)(ws + L.sh_sees),
@@ -722,7 +730,9 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     if (!P.pre.empty()) {
         ProfScope ps(c, bf16 ? 2 : 5, st);
         W.items = (const PcWinItem *)(ws + L.pre);
-        if (bf16) pc_launch_win_prefill_bf16(W, (int)P.pre.size(), st);
+        const PcMx4Rows M{(const float4 *)(ws + L.q_abs), (const float *)(ws + L.q_unit), (const int32_t *)(ws + L.places), ws + L.v_tiles, (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size()};
+        if (mx4) pc_launch_win_prefill_mx4(W, M, (int)P.pre.size(), st);
+        else if (bf16) pc_launch_win_prefill_bf16(W, (int)P.pre.size(), st);
         else pc_launch_win_attend_f32(W, (int)P.pre.size(), c->D, st);
         PC_HIP(c, hipGetLastError());
     }
