@@ -336,7 +336,7 @@ void pc_launch_rows(int dtype, const PcRows &R, const PcArgBlob *blob, hipStream
 
 // ---------------------------------------------------------------------------------------------------------- gradient
 // With r = 1 / sqrt(mean(x^2) + eps), u = x r, g = dy w:   dx = r (g - u mean(g u)),   dw = the sum of dy u over rows and heads.
-// Of keys dy is the gradient of the keys as stored, turned back.  A block takes PC_ROWS_BWD rows and eight heads of one kind
+// Of keys dy is the gradient of the keys as stored, turned back.  A block takes block_rows rows and eight heads of one kind
 // (blockIdx.y: queries' chunks of heads, then keys', then values'); its sums for the weights leave as one row of partial results, which a
 // second launch adds up in order.
 template <typename T, int D>
@@ -349,7 +349,7 @@ __device__ __forceinline__ void rows_backward(const PcRowsBwd &B, const PcRowsBw
     const int nq = B.q ? (B.n_q_heads + 7) / 8 : 0, nk = (B.n_kv_heads + 7) / 8;
     const int c = threadIdx.x & 7, hd = threadIdx.x >> 3 & 7, wave = threadIdx.x >> 6;
     const int lo = E * c, hi = HALF + E * c;
-    const int t0 = ((int)blockIdx.x - it.block0) * PC_ROWS_BWD, t1 = min(t0 + PC_ROWS_BWD, it.n);
+    const int t0 = ((int)blockIdx.x - it.block0) * B.block_rows, t1 = min(t0 + B.block_rows, it.n);
     const int kind = (int)blockIdx.y < nq ? 0 : (int)blockIdx.y < nq + nk ? 1 : 2;
     const int chunk = (int)blockIdx.y - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk);
     const int heads = kind == 0 ? B.n_q_heads : B.n_kv_heads, h = min(8 * chunk + hd, heads - 1);
@@ -432,23 +432,29 @@ template <typename T, int D> __global__ __launch_bounds__(256) void pc_rows_bwd_
     rows_backward<T, D>(B, (const PcRowsBwdItem *)arguments());         // (the blob comes first)
 }
 
-// The partial sums of the weights' gradients, in order: a block 16 dims of one of them, 16 threads a dim.
-__global__ __launch_bounds__(256) void pc_rows_bwd_sum_kernel(PcRowsBwd B)
+// The partial sums of the weights' gradients, in order: a block 16 dims of one of them, 64 threads a dim.
+__global__ __launch_bounds__(1024) void pc_rows_bwd_sum_kernel(PcRowsBwd B)
 {
-    __shared__ float s_sum[16][17];
+    __shared__ float s_sum[64][17];
     float *to = blockIdx.y == 0 ? B.to_q_weight : B.to_k_weight;
     if (!to) return;
     const float *part = blockIdx.y == 0 ? B.q_part : B.k_part;
     const int n = B.n_blocks * ((blockIdx.y == 0 ? B.n_q_heads : B.n_kv_heads) + 7 >> 3);
     const int d = blockIdx.x * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
-    const int a = (int)((int64_t)n * share / 16), b = (int)((int64_t)n * (share + 1) / 16);
     float x = 0.f;
-    for (int i = a; i < b; ++i) x += part[(int64_t)i * B.D + d];
+    for (int i = share; i < n; i += 8 * 64) {            // (eight at a time: the loads' latency is what this costs)
+        float y[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) y[u] = i + 64 * u < n ? part[(int64_t)(i + 64 * u) * B.D + d] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x += y[u];
+    }
     s_sum[share][threadIdx.x & 15] = x;
     __syncthreads();
     if (share == 0) {
+        x = 0.f;
 #pragma unroll
-        for (int k = 1; k < 16; ++k) x += s_sum[k][threadIdx.x];
+        for (int k = 0; k < 64; ++k) x += s_sum[k][threadIdx.x];
         to[d] = x;
     }
 }
@@ -468,56 +474,76 @@ void pc_launch_rows_backward(int dtype, const PcRowsBwd &B, const PcArgBlob *blo
     if (dtype == 1) go((uint16_t)0, integral_constant<int, 128>{});
     else if (B.D == 64) go(0.f, integral_constant<int, 64>{});
     else go(0.f, integral_constant<int, 128>{});
-    if (B.to_q_weight || B.to_k_weight) pc_rows_bwd_sum_kernel<<<dim3((unsigned)B.D / 16, 2), 256, 0, st>>>(B);
+    if (B.to_q_weight || B.to_k_weight) pc_rows_bwd_sum_kernel<<<dim3((unsigned)B.D / 16, 2), 1024, 0, st>>>(B);
 }
 
 // -------------------------------------------------------------------------------------------------------------- read
-// What extents hold, as rows of tokens: a block eight slots, a thread 16 dims of a head's row (as the append has them).
+// What extents hold, as rows of tokens: a block eight slots and eight heads.  Keys: a thread 16 dims of two tokens' rows (as the append has
+// them).  Values: of 4 bits, and of bf16, a thread has eight tokens of its dims at hand, and writes its part of eight rows.
 template <int STORE, int D> __device__ __forceinline__ void read_block(const PcRead &R, const PcReadItem *items)
 {
     using T = std::conditional_t<STORE == 0, float, uint16_t>;
     constexpr int E = D / 16, HALF = D / 2;
     const PcReadItem it = item_of(items, R.n_items, blockIdx.x);
-    const int c = threadIdx.x & 7, h = (int)blockIdx.y * 8 + (threadIdx.x >> 3 & 7), t0 = 8 * ((int)blockIdx.x - it.block0);
-    if (h >= R.n_kv_heads) return;
+    const int t0 = 8 * ((int)blockIdx.x - it.block0);
+    {
+        const int c = threadIdx.x & 7, h = (int)blockIdx.y * 8 + (threadIdx.x >> 3 & 7);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int t = t0 + (threadIdx.x >> 6) + 4 * u;
-        if (t >= it.n) continue;
-        const int64_t at = (int64_t)h * R.slots + it.slot0 + t;
-        const int row = (it.slot0 + t) % PC_TILE;
+        for (int u = 0; u < 2; ++u) {
+            const int t = t0 + (threadIdx.x >> 6) + 4 * u;
+            if (t >= it.n || h >= R.n_kv_heads) continue;
+            const int64_t at = (int64_t)h * R.slots + it.slot0 + t, to = ((it.row0 + t) * R.n_kv_heads + h) * D;
+            const int row = (it.slot0 + t) % PC_TILE;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int d = half * HALF + E * c;
-            float k[E], v[E];
-            if constexpr (STORE == 2) {
-                const char *kt = (const char *)R.k_store + at / PC_TILE * PC_MX4_TILE, *vt = (const char *)R.v_store + at / PC_TILE * PC_MX4_TILE;
-                const uint32_t codes = *reinterpret_cast<const uint32_t *>(kt + row * 64 + d / 2);
-                const int ek = (uint8_t)kt[PC_MX4_CODES + row * 4 + d / 32], ev = PC_MX4_E_MAX - (uint8_t)vt[PC_MX4_CODES + row / 8 * 32 + d / 32 * 8 + row % 8];
-                const uint32_t *words = reinterpret_cast<const uint32_t *>(vt + row / 8 * 512);
-                auto value = [](uint32_t code, int e) {
-                    const uint32_t m = code & 7;
-                    const float a = m < 4 ? 0.5f * (float)m : m < 6 ? (float)m - 2.f : 2.f * (float)m - 8.f;
-                    return (code & 8 ? -a : a) * mx4_power(0.f, e);
-                };
+            for (int half = 0; half < 2; ++half) {
+                const int d = half * HALF + E * c;
+                float k[E];
+                if constexpr (STORE == 2) {
+                    const char *kt = (const char *)R.k_store + at / PC_TILE * PC_MX4_TILE;
+                    const uint32_t codes = *reinterpret_cast<const uint32_t *>(kt + row * 64 + d / 2);
+                    const int e = (uint8_t)kt[PC_MX4_CODES + row * 4 + d / 32];
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    k[j] = ek == PC_MX4_NAN ? __builtin_nanf("") : value(codes >> 4 * j, ek - 127);
-                    v[j] = value(words[mx4_word(d + j)] >> 4 * (row % 8), ev);
-                }
-            } else {
-                load_run<T, E>((const T *)R.k_store + at * D + d, k);
-                if constexpr (STORE == 0) {
-                    load_run<T, E>((const T *)R.v_store + at * D + d, v);
+                    for (int j = 0; j < E; ++j) k[j] = e == PC_MX4_NAN ? __builtin_nanf("") : mx4_value(codes >> 4 * j, e - 127);
                 } else {
-                    const uint16_t *src = (const uint16_t *)R.v_store + (at / 8 * D + d) * 8 + at % 8;
-#pragma unroll
-                    for (int j = 0; j < E; ++j) v[j] = bf_lo(src[8 * j]);
+                    load_run<T, E>((const T *)R.k_store + at * D + d, k);
+                }
+                if (R.k) store_run<T, E>((T *)R.k + to + d, k);
+                if constexpr (STORE == 0) {
+                    load_run<T, E>((const T *)R.v_store + at * D + d, k);
+                    if (R.v) store_run<T, E>((T *)R.v + to + d, k);
                 }
             }
-            const int64_t to = ((it.row0 + t) * R.n_kv_heads + h) * D + d;
-            if (R.k) store_run<T, E>((T *)R.k + to, k);
-            if (R.v) store_run<T, E>((T *)R.v + to, v);
+        }
+    }
+    if constexpr (STORE != 0) {
+        if (!R.v) return;
+        const int h = (int)blockIdx.y * 8 + (threadIdx.x >> 4 & 7), d = 8 * (threadIdx.x & 15), half = threadIdx.x >> 7;           // (half: tokens 4 half + 0..3)
+        if (h >= R.n_kv_heads) return;
+        const int64_t at = (int64_t)h * R.slots + it.slot0 + t0;
+        [[maybe_unused]] uint32_t w[8];
+        [[maybe_unused]] uint2 x[8];
+        [[maybe_unused]] uint32_t ex = 0;
+        if constexpr (STORE == 2) {
+            const char *vt = (const char *)R.v_store + at / PC_TILE * PC_MX4_TILE;
+            const int grp = (it.slot0 + t0) % PC_TILE / 8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = reinterpret_cast<const uint32_t *>(vt + grp * 512)[mx4_word(d + j)];
+            ex = *reinterpret_cast<const uint32_t *>(vt + PC_MX4_CODES + grp * 32 + d / 32 * 8 + 4 * half);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint2 *>((const uint16_t *)R.v_store + (at / 8 * D + d + j) * 8 + 4 * half);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + 4 * half + i;
+            if (t >= it.n) break;
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (STORE == 2) v[j] = mx4_value(w[j] >> 4 * (4 * half + i), PC_MX4_E_MAX - (int)(ex >> 8 * i & 255u));
+                else { const uint32_t p = i < 2 ? x[j].x : x[j].y; v[j] = i & 1 ? bf_hi(p) : bf_lo(p); }
+            }
+            store_run<uint16_t, 8>((uint16_t *)R.v + ((it.row0 + t) * R.n_kv_heads + h) * D + d, v);
         }
     }
 }

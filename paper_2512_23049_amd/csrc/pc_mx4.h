@@ -83,6 +83,13 @@ __device__ __forceinline__ int mx4_exponent(double top)
 }
 __device__ __forceinline__ float mx4_power(float, int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 __device__ __forceinline__ double mx4_power(double, int e) { return __hiloint2double((int)((uint32_t)(e + 1023) << 20), 0); }
+// what a code (in the low bits) stands for under 2^e
+__device__ __forceinline__ float mx4_value(uint32_t code, int e)
+{
+    const uint32_t m = code & 7;
+    const float a = m < 4 ? 0.5f * (float)m : m < 6 ? (float)m - 2.f : 2.f * (float)m - 8.f;
+    return (code & 8 ? -a : a) * mx4_power(0.f, e);
+}
 // Where a query's dims stand among those that are turned by their positions: four of them (lane half hh, s = 0..3: 16 hh + 4 s, s = 4..7:
 // 32 + 16 hh + 4 (s - 4), s + 8: 64 further), rows side by side.  So lanes have what the matrix instruction takes from them as bytes
 // (its k of a half hh: 16 hh to 16 hh + 15, and 32 further), and a pair of a turn is in one lane.

@@ -38,7 +38,6 @@ struct PcRows {
 void pc_launch_rows(int dtype, const PcRows &R, const PcArgBlob *blob, hipStream_t st);
 
 // The gradient.
-#define PC_ROWS_BWD 32        // rows that a block takes
 struct PcRowsBwdItem {
     int64_t row0;             // the first token's row
     int32_t slot0, pos0, n;
@@ -47,6 +46,7 @@ struct PcRowsBwdItem {
 struct PcRowsBwd {
     const PcRowsBwdItem *items;
     int32_t n_items, n_blocks;
+    int32_t block_rows;                       // rows that a block takes
     const void *q, *k;
     int64_t q_stride, k_stride;
     const float *q_weight, *k_weight;
