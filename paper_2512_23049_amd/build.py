@@ -13,7 +13,7 @@ SOURCES = ["pc_lib.hip", "pc_plan.hip", "pc_attend.hip", "pc_kernels_basic.hip",
            "pc_kernels_bwd_mfma.hip", "pc_kernels_mfma.hip", "pc_kernels_prefill.hip",
            "pc_kernels_shared.hip", "pc_window.hip", "pc_kernels_window.hip", "pc_kernels_window_f32.hip", "pc_kernels_window_shared.hip",
            "pc_kernels_window_bwd.hip", "pc_kernels_window_bwd_f32.hip", "pc_copies.hip", "pc_kernels_copies.hip",
-           "pc_project.hip", "pc_kernels_project.hip", "pc_kernels_mx4.hip"]
+           "pc_project.hip", "pc_kernels_project.hip", "pc_kernels_mx4.hip", "pc_kernels_mx4_shared.hip"]
 # the prefill kernel never produces NaNs in its max reductions: let the compiler drop the
 # canonicalising v_max x, x in front of every fmax
 # the gradient's key kernels hold more than 256 registers: results of their matrix instructions stay in vector registers
@@ -21,7 +21,8 @@ SOURCES = ["pc_lib.hip", "pc_plan.hip", "pc_attend.hip", "pc_kernels_basic.hip",
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 FILE_FLAGS = {"pc_kernels_prefill.hip": ["-fno-honor-nans"], "pc_kernels_bwd_mfma.hip": VGPR_FORM, "pc_kernels_backward.hip": VGPR_FORM,
               # (constants of the rotations, moved out of the loop over tiles, would not fit the registers)
-              "pc_kernels_window_shared.hip": ["-mllvm", "-disable-machine-licm"]}
+              "pc_kernels_window_shared.hip": ["-mllvm", "-disable-machine-licm"],
+              "pc_kernels_mx4_shared.hip": ["-mllvm", "-disable-machine-licm"]}
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-result"]

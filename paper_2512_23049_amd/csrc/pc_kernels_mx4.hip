@@ -1,49 +1,17 @@
 // Attention over a PC_MX4 cache: single tokens, and rows of prompts (gfx950).  What a row sees, and how
 // the host states it: pc_window.h; how the cache holds keys and values: pc_mx4.h.
 #include "pc_window.h"
-#include "pc_mx4.h"
-#include "pc_mfma_common.h"
+#include "pc_mx4_products.h"
 
 #include <algorithm>
 #include <type_traits>
 
-#define MFMA16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
-
 namespace {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-// a wave's own LDS accesses happen in the order they are issued: the compiler is to keep it
-__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 __device__ __forceinline__ const __attribute__((address_space(4))) char *arguments()
 {
     return (const __attribute__((address_space(4))) char *)__builtin_amdgcn_kernarg_segment_ptr();
 }
-// codes (cbsz 4) by e4m3 (blgp 0), each with the exponent in the low byte of its scale
-__device__ __forceinline__ f32x4 scores16(uint4 codes, int e_codes, i32x8 q, int e_q, f32x4 c)
-{
-    const i32x8 a = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, c, 4, 0, 0, e_codes, 0, e_q);
-}
-// the eight slots of a dimension, in bf16 and in units of their powers
-__device__ __forceinline__ bf16x8 of_codes(uint32_t w)
-{
-    const uint4 u = make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 0)),
-                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 1)),
-                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 2)),
-                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3)));
-    return __builtin_bit_cast(bf16x8, u);
-}
-// bf16 x 2^(60 - d): d as bytes 0 and 1 (or 2 and 3) of `d`; what would be below the least normal number is zero
-template <int PAIR> __device__ __forceinline__ uint32_t lowered(uint32_t p, uint32_t d)
-{
-    const uint32_t e = __builtin_amdgcn_perm(0u, d, PAIR == 0 ? 0x010C000Cu : 0x030C020Cu) >> 1;
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, p), __builtin_bit_cast(u16x2, e)));
-}
-
 struct Mx4Tile {
     uint4 k[2];               // lane (m, a): block a of key 8 (m >> 2) + 4 half + (m & 3), its codes
     uint32_t ke[2];           // and the exponents of that key's four blocks
@@ -116,9 +84,25 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
         Mx4Tile A, B;
         fetch(A);
         if (n_tiles > 1) fetch(B);
-        int cur = -1, e_hi = 127, e_lo = 127;
+        // the row's unit, the same for every turn; a query that holds what is no number is all NaN
+        bool fine = true;
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 u = ldg16(qp + 128 * (i >> 1) + 16 * (i & 1));
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = mx4_top(top, w[j], fine);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        fine &= __shfl_xor((int)fine, 16) != 0;
+        fine &= __shfl_xor((int)fine, 32) != 0;
+        const float unit = mx4_unit(top * W.scale_log2);
+        const int e_hi = (int)(__float_as_uint(unit) >> 23), e_lo = e_hi - 4;
+        int cur = -1;
         int64_t cur_turn = 0;
-        i32x8 q_hi, q_lo;
+        mx4_i32x8 q_hi, q_lo;
         auto compute = [&](Mx4Tile &T) __attribute__((always_inline)) {
             if (T.d.rot != cur) {                        // another run: another rotation?
                 const int64_t turn = pos - T.d.rot_pos;
@@ -128,48 +112,32 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
                     const float2 cs = rope_angle((double)turn * freq);
                     s_rot[wave][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
                     in_order();
-                    float x[16], y[16], top = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint4 lq = ldg16(qp + 16 * i), hq = ldg16(qp + 128 + 16 * i);
-                        if (n >= g) lq = hq = make_uint4(0, 0, 0, 0);
-                        const uint32_t lw[4] = {lq.x, lq.y, lq.z, lq.w}, hw[4] = {hq.x, hq.y, hq.z, hq.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float4 r = *reinterpret_cast<const float4 *>(&s_rot[wave][16 * a + 8 * i + 2 * j]);
-                            const float x0 = bf_lo(lw[j]), x1 = bf_hi(lw[j]), y0 = bf_lo(hw[j]), y1 = bf_hi(hw[j]);
-                            x[8 * i + 2 * j] = x0 * r.x - y0 * r.y; x[8 * i + 2 * j + 1] = x1 * r.z - y1 * r.w;
-                            y[8 * i + 2 * j] = x0 * r.y + y0 * r.x; y[8 * i + 2 * j + 1] = x1 * r.w + y1 * r.z;
-                        }
+                    for (int s = 0; s < 4; ++s) {        // dims 16 a + 4 s, and 64 up
+                        uint2 lq = *reinterpret_cast<const uint2 *>(qp + 8 * s), hq = *reinterpret_cast<const uint2 *>(qp + 128 + 8 * s);
+                        if (n >= g) lq = hq = make_uint2(0, 0);
+                        if (!fine) lq = hq = make_uint2(0x7FC07FC0u, 0x7FC07FC0u);
+                        const float4 *r = reinterpret_cast<const float4 *>(&s_rot[wave][16 * a + 4 * s]);
+                        const float4 r0 = r[0], r1 = r[1];
+                        const float x0 = bf_lo(lq.x), x1 = bf_hi(lq.x), x2 = bf_lo(lq.y), x3 = bf_hi(lq.y);
+                        const float y0 = bf_lo(hq.x), y1 = bf_hi(hq.x), y2 = bf_lo(hq.y), y3 = bf_hi(hq.y);
+                        const float u[4] = {x0 * r0.x - y0 * r0.y, x1 * r0.z - y1 * r0.w, x2 * r1.x - y2 * r1.y, x3 * r1.z - y3 * r1.w};
+                        const float v[4] = {x0 * r0.y + y0 * r0.x, x1 * r0.w + y1 * r0.z, x2 * r1.y + y2 * r1.x, x3 * r1.w + y3 * r1.z};
+                        int hi, rest;
+                        mx4_pieces(u, unit, hi, rest);
+                        q_hi[s] = hi; q_lo[s] = rest;
+                        mx4_pieces(v, unit, hi, rest);
+                        q_hi[4 + s] = hi; q_lo[4 + s] = rest;
                     }
                     in_order();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, fmaxf(fabsf(x[i]), fabsf(y[i])));
-                    top = fmaxf(top, __shfl_xor(top, 16));
-                    top = fmaxf(top, __shfl_xor(top, 32));
-                    // the row's largest value between 128 and 256 (the largest number there is: 448)
-                    const int e = max(-100, min(100, (int)(__float_as_uint(top) >> 23 & 255) - 134));
-                    const float unit = __uint_as_float((uint32_t)(127 - e) << 23) * (top < INFINITY ? 1.f : __builtin_nanf(""));
-                    e_hi = 127 + e; e_lo = 123 + e;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float *p = i < 4 ? x + 4 * i : y + 4 * (i - 4);
-                        const float f0 = p[0] * unit, f1 = p[1] * unit, f2 = p[2] * unit, f3 = p[3] * unit;
-                        int hi = __builtin_amdgcn_cvt_pk_fp8_f32(f0, f1, 0, false);
-                        hi = __builtin_amdgcn_cvt_pk_fp8_f32(f2, f3, hi, true);
-                        const auto b0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-                        int rest = __builtin_amdgcn_cvt_pk_fp8_f32((f0 - b0[0]) * 16.f, (f1 - b0[1]) * 16.f, 0, false);
-                        rest = __builtin_amdgcn_cvt_pk_fp8_f32((f2 - b1[0]) * 16.f, (f3 - b1[1]) * 16.f, rest, true);
-                        q_hi[i] = hi; q_lo[i] = rest;
-                    }
                 }
             }
             f32x4 s[2];
 #pragma unroll
             for (int tau = 0; tau < 2; ++tau) {
                 const int e = (int)(T.ke[tau] >> (8 * a));
-                s[tau] = scores16(T.k[tau], e, q_lo, e_lo, (f32x4){0.f, 0.f, 0.f, 0.f});
-                s[tau] = scores16(T.k[tau], e, q_hi, e_hi, s[tau]);
+                s[tau] = mx4_scores16(T.k[tau], e, q_lo, e_lo, (f32x4){0.f, 0.f, 0.f, 0.f});
+                s[tau] = mx4_scores16(T.k[tau], e, q_hi, e_hi, s[tau]);
             }
             float sc[8];                                 // keys 8 a + 0..7 of column n
 #pragma unroll
@@ -201,10 +169,10 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
             const uint32_t ew[8] = {T.ve[0].x, T.ve[0].y, T.ve[0].z, T.ve[0].w, T.ve[1].x, T.ve[1].y, T.ve[1].z, T.ve[1].w};
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(lowered<0>(pk[0], ew[2 * b]), lowered<1>(pk[1], ew[2 * b]),
-                                                                       lowered<0>(pk[2], ew[2 * b + 1]), lowered<1>(pk[3], ew[2 * b + 1])));
+                const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(mx4_lowered<0>(pk[0], ew[2 * b]), mx4_lowered<1>(pk[1], ew[2 * b]),
+                                                                       mx4_lowered<0>(pk[2], ew[2 * b + 1]), mx4_lowered<1>(pk[3], ew[2 * b + 1])));
 #pragma unroll
-                for (int i = 0; i < 2; ++i) acc[2 * b + i] = MFMA16(of_codes(vw[2 * b + i]), p, acc[2 * b + i]);
+                for (int i = 0; i < 2; ++i) acc[2 * b + i] = MFMA16(mx4_of_codes(vw[2 * b + i]), p, acc[2 * b + i]);
             }
         };
         for (int t = 0;;) {
@@ -305,17 +273,11 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
             for (int i = 0; i < 8; ++i) {
                 const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    top = fmaxf(top, fmaxf(fabsf(bf_lo(w[j])), fabsf(bf_hi(w[j]))));
-                    fine &= ((w[j] & 0x7F80u) != 0x7F80u) & ((w[j] & 0x7F800000u) != 0x7F800000u);
-                }
+                for (int j = 0; j < 4; ++j) top = mx4_top(top, w[j], fine);
             }
             top = fmaxf(top, __shfl_xor(top, 32));
             fine &= __shfl_xor((int)fine, 32) != 0;
-            // a turn keeps a pair's norm, sqrt(2) times the larger value at most: the row's largest, scaled, between 128 and 256 (448 is the
-            // largest number of the pieces)
-            const int e = max(-100, min(100, (int)(__float_as_uint(top * P.scale_log2 * 1.4142137f) >> 23 & 255) - 134));
-            if (hh == 0) P.q_unit[(int64_t)h * groups * 32 + R] = __uint_as_float((uint32_t)(127 + e) << 23);
+            if (hh == 0) P.q_unit[(int64_t)h * groups * 32 + R] = mx4_unit(top * P.scale_log2);
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
                 const uint4 lo = raw[(s >> 2) * 2 + (s >> 1 & 1)], hi = raw[4 + (s >> 2) * 2 + (s >> 1 & 1)];
@@ -344,16 +306,10 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
         const int grp = (threadIdx.x >> 7) + 2 * i, d = threadIdx.x & 127;
         const uint32_t w = reinterpret_cast<const uint32_t *>(vt + grp * 512)[mx4_word(d)];
         const uint2 ex = *reinterpret_cast<const uint2 *>(vt + PC_MX4_CODES + grp * 32 + d / 32 * 8);
-        const uint4 codes = __builtin_bit_cast(uint4, of_codes(w));
-        const uint32_t cw[4] = {codes.x, codes.y, codes.z, codes.w};
-        uint32_t o[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t es = (j < 2 ? ex.x : ex.y) >> 16 * (j & 1);
-            const float u0 = __uint_as_float((187u - min(es & 255u, 120u)) << 23), u1 = __uint_as_float((187u - min(es >> 8 & 255u, 120u)) << 23);
-            o[j] = pack_bf16(bf_lo(cw[j]) * u0, bf_hi(cw[j]) * u1);
-        }
-        *reinterpret_cast<uint4 *>(to + (grp * 128 + d) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+        uint4 x;
+        x.x = mx4_values(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_values(w, ex.x, std::integral_constant<int, 1>{});
+        x.z = mx4_values(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_values(w, ex.y, std::integral_constant<int, 3>{});
+        *reinterpret_cast<uint4 *>(to + (grp * 128 + d) * 16) = x;
     }
 }
 
@@ -385,31 +341,6 @@ namespace {
 __device__ __forceinline__ int imax3(int a, int b, int c) { return max(max(a, b), c); }
 template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
 __device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "memory"); }
-// One 16-byte (4-byte) per lane direct load: lane l's bytes land at lds_wave_base + 16 l (4 l); completion is awaited with wait_vm.
-__device__ __forceinline__ void dma16(const void *gbase_uniform, unsigned lane_off, unsigned lds_wave_base)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 ::"s"(lds_wave_base), "v"(lane_off), "s"(gbase_uniform) : "memory", "m0");
-}
-__device__ __forceinline__ void dma4(const void *gbase_uniform, unsigned lane_off, unsigned lds_wave_base)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-                 ::"s"(lds_wave_base), "v"(lane_off), "s"(gbase_uniform) : "memory", "m0");
-}
-template <int BYTE> __device__ __forceinline__ f32x16 scores32(uint4 codes, int e_codes, i32x8 q, int e_q, f32x16 c)
-{
-    const i32x8 a = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, c, 4, 0, BYTE, e_codes, 0, e_q);
-}
-typedef short s16x2 __attribute__((ext_vector_type(2)));
-// four values as e4m3 in units of `unit`
-__device__ __forceinline__ int pieces4(const float (&x)[4], float unit)
-{
-    s16x2 r = {0, 0};
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[0], x[1], unit, false);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[2], x[3], unit, true);
-    return __builtin_bit_cast(int, r);
-}
 }  // namespace
 
 __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Rows M)
@@ -442,7 +373,7 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
     };
     const int64_t groups = ((int64_t)M.n_rows + 31) / 32;
     const float4 *q_abs = M.q_abs + mx4_query_at(groups, h, R, hh, 0);
-    const float q_unit = M.q_unit[(int64_t)h * groups * 32 + R], q_rest = q_unit * 0.0625f;
+    const float q_unit = M.q_unit[(int64_t)h * groups * 32 + R];
     const int e_hi = (int)(__float_as_uint(q_unit) >> 23), e_lo = e_hi - 4;
 
     const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * (W.slots / PC_TILE) * PC_MX4_TILE;
@@ -454,13 +385,13 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
     auto request = [&](int slot0, int place, int at) __attribute__((always_inline)) {
         const unsigned char *kt = kb + (int64_t)(slot0 / PC_TILE) * PC_MX4_TILE, *vt = vb + (int64_t)(slot0 + place) * (PC_D * 2);
         const unsigned to = lds0 + at * SLOT;
-        if (wave < 2) dma16(kt, k_src, to + wave * 1024);
-        else dma4(kt, e_src, to + EXPS);                 // (both waves the same: every wave asks as often)
-        dma16(vt, v_src, to + VALUES + wave * 1024);
-        dma16(vt + 4096, v_src, to + VALUES + 4096 + wave * 1024);
+        if (wave < 2) mx4_dma16(kt, k_src, to + wave * 1024);
+        else mx4_dma4(kt, e_src, to + EXPS);                 // (both waves the same: every wave asks as often)
+        mx4_dma16(vt, v_src, to + VALUES + wave * 1024);
+        mx4_dma16(vt + 4096, v_src, to + VALUES + 4096 + wave * 1024);
     };
 
-    i32x8 q_hi[2], q_lo[2];
+    mx4_i32x8 q_hi[2], q_lo[2];
     // (few: in the walk, what is read for all of it at once would not fit the registers)
     auto turn = [&](int rot, auto few) __attribute__((always_inline)) {
         const float2 own = W.rot_run[(int64_t)rot * (PC_D / 2) + lane];
@@ -479,11 +410,10 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const float (&z)[4] = half ? y : x;
-                const int hi = pieces4(z, q_unit);
-                const auto b0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, q_unit, false), b1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, q_unit, true);
-                const float rest[4] = {z[0] - b0[0], z[1] - b0[1], z[2] - b1[0], z[3] - b1[1]};
+                int hi, rest;
+                mx4_pieces(z, q_unit, hi, rest);
                 q_hi[half][s] = hi;
-                q_lo[half][s] = pieces4(rest, q_rest);
+                q_lo[half][s] = rest;
             }
             if (decltype(few)::value && (s & 1)) __builtin_amdgcn_sched_barrier(0);
         }
@@ -544,10 +474,10 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
     auto score = [&](unsigned at) __attribute__((always_inline)) {
         const uint4 k0 = __builtin_bit_cast(uint4, *(lds_frag)(k_rd + at)), k1 = __builtin_bit_cast(uint4, *(lds_frag)((k_rd ^ 32) + at));
         const int e = (int)((unsigned)*(lds_word)(e_rd + at) >> (8 * hh));
-        f32x16 s = scores32<0>(k0, e, q_lo[0], e_lo, zeros);
-        s = scores32<2>(k1, e, q_lo[1], e_lo, s);
-        s = scores32<0>(k0, e, q_hi[0], e_hi, s);
-        return scores32<2>(k1, e, q_hi[1], e_hi, s);
+        f32x16 s = mx4_scores32<0>(k0, e, q_lo[0], e_lo, zeros);
+        s = mx4_scores32<2>(k1, e, q_lo[1], e_lo, s);
+        s = mx4_scores32<0>(k0, e, q_hi[0], e_hi, s);
+        return mx4_scores32<2>(k1, e, q_hi[1], e_hi, s);
     };
     const int T = item.n_tiles;
     if (T > 0) {

@@ -1,0 +1,320 @@
+// Single tokens of many calls that list the same messages, over a PC_MX4 cache (gfx950): every tile once, as pc_kernels_window_shared.hip has
+// it for bf16 (its lists, its walk over visits, its lazy reference), with the products of pc_kernels_mx4.hip.
+//
+// A workgroup takes a range of the tiles that any of a set of calls (up to 256 columns) see; a wave holds a group of 16 columns and
+// their sums for its whole life.  Tiles come as they are stored, 4352 bytes, by direct loads into a ring of four steps of two; the
+// workgroup converts a step's values to bf16 together, one step ahead, so that no wave has their codes and powers to take apart.  A
+// wave's queries are turned for all of a visit's calls at once, each lane by its own call's rotation.
+#include "pc_window.h"
+#include "pc_mx4.h"
+#include "pc_mx4_products.h"
+
+#include <type_traits>
+
+#define LAZY_LOG2 64.0f
+#define TURNS 4               // rotations that a wave has at hand at once
+
+namespace {
+
+typedef const __attribute__((address_space(3))) win_i32x4 *lds16;
+typedef const __attribute__((address_space(3))) uint32_t *lds4;
+typedef uint32_t mx4_u32x2 __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(3))) mx4_u32x2 *lds8;
+template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
+__device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "memory"); }
+// the lane's number, made where it stands: kept from the kernel's start it would wait in memory, and who fetches a register from
+// there waits for all loads before it
+__device__ __forceinline__ int lane_again()
+{
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+    return x;
+}
+// list entries, uniform: scalar loads (a vector load's wait would be one for all direct loads)
+__device__ __forceinline__ int32_t listed(const int32_t *p) { return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(p)); }
+__device__ __forceinline__ win_i32x4 listed4(const void *p) { return *reinterpret_cast<const __attribute__((address_space(4))) win_i32x4 *>(reinterpret_cast<uintptr_t>(p)); }
+
+}  // namespace
+
+template <int NW>
+__global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(PcWin W, PcWinShared S)
+{
+    constexpr int TILES = PC_WIN_STEP_TILES, RING = 4, AHEAD = RING - 1, LOADS = 16 / NW;
+    // of a tile in the ring: codes of keys and of values, exponents of keys and of values (256 bytes each: a direct load's lanes)
+    constexpr int VALUES = PC_MX4_CODES, K_EXPS = 2 * PC_MX4_CODES, V_EXPS = K_EXPS + 256, TILE = V_EXPS + 256, SLOT = TILES * TILE;
+    __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][SLOT];
+    __shared__ __attribute__((aligned(1024))) unsigned char s_v[2][TILES][PC_TILE * PC_D * 2];        // values as a bf16 cache has them, of this step and the next
+    __shared__ __attribute__((aligned(16))) float2 s_rot[NW][TURNS][PC_D / 2];
+    __shared__ int4 s_see[NW][16];                       // what a column's call sees of the wave's visit: pos0, n_tok, sink, lo
+    __shared__ double s_freq[PC_D / 2];
+
+    const int kh = blockIdx.x % W.n_kv_heads;
+    const win_i32x4 i0 = listed4(S.items + blockIdx.x / W.n_kv_heads), i1 = listed4((const char *)(S.items + blockIdx.x / W.n_kv_heads) + 16);
+    const int visit0 = i0.x, n_steps = i0.y, call0 = i0.z, n_calls = i0.w, waves = i1.x, split0 = i1.y;
+    const int g = W.n_q_heads / W.n_kv_heads, per = 16 / g;          // calls a group of columns
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int n = lane & 15, a = lane >> 4, sub = n / g;
+    const int my = wave % waves, rep = wave / waves, reps = NW / waves;      // its group of columns; its share of the steps
+
+    const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * (W.slots / PC_TILE) * PC_MX4_TILE;
+    const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * (W.slots / PC_TILE) * PC_MX4_TILE;
+    const unsigned ring = (unsigned)(uintptr_t)&s_kv[0][0];
+
+    // the columns' queries, as they came: dims 16 a + 0..15, then 64 up
+    const int call = my * per + sub;
+    const bool real = sub < per && call < n_calls;
+    uint4 q[4];
+    {
+        const int row = S.calls[call0 + (real ? call : 0)].row;
+        const unsigned char *qp = (const unsigned char *)W.q + ((int64_t)row * W.n_q_heads + kh * g + n % g) * (PC_D * 2) + 32 * a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = real ? ldg16(qp + 128 * (i >> 1) + 16 * (i & 1)) : make_uint4(0, 0, 0, 0);
+    }
+    if (wave == 0) s_freq[lane] = W.inv_freq[lane];
+    // (all of it is here before the first direct load is asked for: the compiler's wait would be one for all of those)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(q[i].x), "+v"(q[i].y), "+v"(q[i].z), "+v"(q[i].w));
+    // the row's unit, for every turn (which keeps a pair's norm): its largest value, scaled, between 128 and 256
+    float unit;
+    {
+        float top = 0.f;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = mx4_top(top, w[j], fine);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        unit = mx4_unit(top * W.scale_log2);
+        // (a query that holds what is no number: all of it is NaN)
+        int all = fine;
+        all &= __shfl_xor(all, 16);
+        all &= __shfl_xor(all, 32);
+        if (!all) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
+        }
+    }
+    __syncthreads();
+
+    int to_visit = visit0, to_tile = 0, to_asked = 0, to_slot = 0, to_has = 0;
+    if (n_steps > 0) { to_slot = listed(&S.visits[visit0].slot0); to_has = listed(&S.visits[visit0].n_tiles); }
+    auto request = [&](int place) __attribute__((always_inline)) {
+        const int l = lane_again();
+        if (to_asked > 0) {
+            to_tile += TILES;
+            if (to_tile >= to_has) {
+                ++to_visit; to_tile = 0;
+                to_slot = listed(&S.visits[to_visit].slot0); to_has = listed(&S.visits[to_visit].n_tiles);
+            }
+        }
+        ++to_asked;
+        // a tile is eight loads: two of codes of keys, two of values, and their exponents (twice, so that every wave asks as often)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int job = wave + NW * i, t = job >> 3, part = job & 7;
+            const bool of_keys = part < 4;
+            // (behind a visit's last tile: it again)
+            const unsigned char *from = (of_keys ? kb : vb) + (int64_t)(to_slot / PC_TILE + min(to_tile + t, to_has - 1)) * PC_MX4_TILE;
+            const unsigned to = (unsigned)uniform((int)(ring + place * SLOT + t * TILE));
+            if ((part & 2) == 0) {
+                // position p of the keys' codes holds block (p & 3) ^ (key >> 3) of key p >> 2; of the values' half (p & 1) ^ (m >> 3) of m = p / 2 % 16:
+                // what the lanes of a fragment read at once hits different banks
+                const int p = (part & 1) * 64 + l;
+                const unsigned key_at = (unsigned)((p >> 2) * 64 + (((p & 3) ^ (p >> 5)) << 4)), value_at = (unsigned)((p >> 1) * 32 + (((p & 1) ^ (p >> 4 & 1)) << 4));
+                mx4_dma16(from, of_keys ? key_at : value_at, to + (of_keys ? 0 : VALUES) + (part & 1) * 1024);
+            } else mx4_dma4(from, (unsigned)(PC_MX4_CODES + (l & 31) * 4), to + (of_keys ? K_EXPS : V_EXPS));
+        }
+    };
+    // a step's values: a thread eight slots of a dimension (or of two)
+    auto convert = [&](int place, int to) __attribute__((always_inline)) {
+        const int thread = wave * 64 + lane_again();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int e = thread + 64 * NW * i, t = e >> 9, grp = e >> 7 & 3, d = e & 127, m = d & 15, db = d >> 4;
+            const unsigned from = ring + place * SLOT + t * TILE;
+            const uint32_t w = *(lds4)(uintptr_t)(from + VALUES + grp * 512 + m * 32 + (((db >> 2) ^ (m >> 3)) << 4) + (db & 3) * 4);
+            const mx4_u32x2 ex = *(lds8)(uintptr_t)(from + V_EXPS + grp * 32 + (d >> 5) * 8);
+            uint4 x;
+            x.x = mx4_values(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_values(w, ex.x, std::integral_constant<int, 1>{});
+            x.z = mx4_values(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_values(w, ex.y, std::integral_constant<int, 3>{});
+            *reinterpret_cast<uint4 *>(&s_v[to][t][(grp * PC_D + d) * 16]) = x;
+        }
+    };
+    for (int i = 0; i < min(AHEAD, n_steps); ++i) request(i);
+    if (n_steps > 0) {
+        if (n_steps >= AHEAD) wait_vm<LOADS * (AHEAD - 1)>();
+        else wait_vm<0>();
+        ring_barrier();
+        convert(0, 0);
+    }
+
+    float m_ref = -INFINITY;
+    f32x4 sums = {0.f, 0.f, 0.f, 0.f};                   // of the column's probabilities (four times the same)
+    f32x4 acc[8];
+    mx4_i32x8 q_hi, q_lo;                                // turned and scaled, in two pieces
+    int listers = 0;                                     // entries of the group
+#pragma unroll
+    for (int db = 0; db < 8; ++db) acc[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q_hi[i] = q_lo[i] = 0;
+    const int e_hi = (int)(__float_as_uint(unit) >> 23), e_lo = e_hi - 4;
+    int visit = visit0 - 1, tile = 0, has = 0;           // the walk of what is computed
+#pragma unroll 1
+    for (int step = 0, place = 0; step < n_steps; ++step, place = place == RING - 1 ? 0 : place + 1) {
+        if (step + AHEAD <= n_steps) wait_vm<LOADS * (AHEAD - 2)>();           // (the next step's tiles too)
+        else wait_vm<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        ring_barrier();
+        const int before = place == 0 ? RING - 1 : place - 1;            // (free: the next but one step's)
+        tile += TILES;
+        if (tile >= has) {
+            ++visit; tile = 0;
+            has = listed(&S.visits[visit].n_tiles);
+            const int e0 = listed(&S.visits[visit].e0);
+            const int first = listed(&S.visits[visit].off[my]), end = listed(&S.visits[visit].off[my + 1]);
+            listers = end - first;
+            asm volatile("" ::: "memory");               // (a wave's own LDS accesses happen in order)
+            if (a == 0) s_see[wave][n] = make_int4(0, 0, 0, 0);
+#pragma unroll 1
+            for (int e = first; e < end; e += TURNS) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)              // (its 32 numbers, taken apart once and kept, would not fit the registers)
+                    asm volatile("" : "+v"(q[i].x), "+v"(q[i].y), "+v"(q[i].z), "+v"(q[i].w));
+                int of = -1;                             // which of the rotations is the lane's
+                asm volatile("" ::: "memory");
+#pragma unroll 1
+                for (int i = 0; i < min(TURNS, end - e); ++i) {
+                    const win_i32x4 x = listed4(S.sees + e0 + e + i), y = listed4((const char *)(S.sees + e0 + e + i) + 16);
+                    const bool mine = sub == y.z;
+                    if (mine && a == 0) s_see[wave][n] = make_int4(x.x, x.y, x.z, x.w);
+                    of = mine ? i : of;
+                    const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y.y << 32) | (uint32_t)y.x);
+                    const float2 cs = rope_angle((double)turn * s_freq[lane]);
+                    s_rot[wave][i][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
+                }
+                asm volatile("" ::: "memory");
+                const float4 *rot = reinterpret_cast<const float4 *>(&s_rot[wave][max(of, 0)][16 * a]);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {            // dims 16 a + 4 s, and 64 up
+                    const uint4 lq = q[s >> 1], hq = q[2 + (s >> 1)];
+                    const uint32_t lw[2] = {s & 1 ? lq.z : lq.x, s & 1 ? lq.w : lq.y}, hw[2] = {s & 1 ? hq.z : hq.x, s & 1 ? hq.w : hq.y};
+                    const float4 r0 = rot[2 * s], r1 = rot[2 * s + 1];
+                    const float x0 = bf_lo(lw[0]), x1 = bf_hi(lw[0]), x2 = bf_lo(lw[1]), x3 = bf_hi(lw[1]);
+                    const float y0 = bf_lo(hw[0]), y1 = bf_hi(hw[0]), y2 = bf_lo(hw[1]), y3 = bf_hi(hw[1]);
+                    const float u[4] = {x0 * r0.x - y0 * r0.y, x1 * r0.z - y1 * r0.w, x2 * r1.x - y2 * r1.y, x3 * r1.z - y3 * r1.w};
+                    const float v[4] = {x0 * r0.y + y0 * r0.x, x1 * r0.w + y1 * r0.z, x2 * r1.y + y2 * r1.x, x3 * r1.w + y3 * r1.z};
+                    int hi, rest;
+                    mx4_pieces(u, unit, hi, rest);
+                    q_hi[s] = of >= 0 ? hi : q_hi[s]; q_lo[s] = of >= 0 ? rest : q_lo[s];
+                    mx4_pieces(v, unit, hi, rest);
+                    q_hi[4 + s] = of >= 0 ? hi : q_hi[4 + s]; q_lo[4 + s] = of >= 0 ? rest : q_lo[4 + s];
+                }
+                asm volatile("" ::: "memory");
+            }
+        }
+        uint32_t sees[TILES], some = 0, all = ~0u;       // bit: key of a tile; of any tile, of all there are
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) sees[t] = 0;
+        if (listers > 0 && (reps == 1 || step % reps == rep)) {
+            auto first = [](unsigned k) { return k >= 32u ? ~0u : (1u << k) - 1u; };
+            asm volatile("" ::: "memory");
+            const int4 w = s_see[wave][n];
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const int skip = PC_TILE * (tile + t), p = w.x + skip;
+                const unsigned below = w.w <= p ? 0u : (unsigned)w.w - (unsigned)p;
+                sees[t] = tile + t >= has ? 0u : first((unsigned)max(w.y - skip, 0)) & (~first(below) | first((unsigned)max(w.z - skip, 0)));
+            }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) { some |= sees[t]; all &= sees[t]; }
+        }
+        if (__builtin_amdgcn_ballot_w64(some != 0) != 0) {
+            const unsigned kt = ring + place * SLOT;
+            float sc[8 * TILES];                         // keys 32 t + 8 a + 0..7 of column n
+            {
+                const int l = lane_again(), m = l & 15, key = 8 * (m >> 2) + (m & 3);
+                const unsigned at = (unsigned)(key * 64 + (((l >> 4) ^ (key >> 3)) << 4));
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int tau = 0; tau < 2; ++tau) {
+                        const uint4 codes = __builtin_bit_cast(uint4, *(lds16)(uintptr_t)(kt + t * TILE + at + tau * 256));
+                        const int e = (int)(*(lds4)(uintptr_t)(kt + t * TILE + K_EXPS + key * 4 + tau * 16) >> (8 * (l >> 4)));
+                        f32x4 s = mx4_scores16(codes, e, q_lo, e_lo, (f32x4){0.f, 0.f, 0.f, 0.f});
+                        s = mx4_scores16(codes, e, q_hi, e_hi, s);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sc[8 * t + 4 * tau + j] = s[j];
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const bool whole = all == ~0u;
+            if (__builtin_amdgcn_ballot_w64(some != 0 && !whole) == 0) {     // (all or nothing)
+#pragma unroll
+                for (int j = 0; j < 8 * TILES; ++j) sc[j] = whole ? sc[j] : -INFINITY;
+            } else {
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    const uint32_t mine = sees[t] >> (8 * a);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sc[8 * t + j] = (mine >> j) & 1 ? sc[8 * t + j] : -INFINITY;
+                }
+            }
+            float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+#pragma unroll
+            for (int j = 4; j < 8 * TILES; j += 4) mx = fmaxf(mx, fmaxf(fmaxf(sc[j], sc[j + 1]), fmaxf(sc[j + 2], sc[j + 3])));
+            // The reference of a column's exponents moves only where a score is 2^LAZY above it (a column's first always is):
+            // probabilities up to that are as exact, and the lanes of a column need not agree on a maximum step by step.
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_ref + LAZY_LOG2) != 0, 0)) {
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float m_new = mx > m_ref + LAZY_LOG2 ? mx : m_ref, f = m_new == m_ref ? 1.f : ex2(m_ref - m_new);
+                m_ref = m_new;
+                sums *= f;
+#pragma unroll
+                for (int db = 0; db < 8; ++db) acc[db] *= f;
+            }
+            const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+            bf16x8 p[TILES];
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                uint32_t pk[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) pk[j] = pack_bf16(ex2(sc[8 * t + 2 * j] - ref), ex2(sc[8 * t + 2 * j + 1] - ref));
+                p[t] = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+            }
+            // (the denominator: of the probabilities as the products take them, so that their rounding cancels)
+            const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) sums = MFMA16(ones, p[t], sums);
+            __builtin_amdgcn_sched_barrier(0);           // (values read any earlier would not fit the registers)
+            const int lv = lane_again();
+            const unsigned vt = (unsigned)(uintptr_t)&s_v[step & 1][0][0] + (unsigned)(((lv >> 4) * PC_D + (lv & 15)) * 16);
+#pragma unroll
+            for (int db = 0; db < 8; ++db)
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+                    acc[db] = MFMA16(__builtin_bit_cast(bf16x8, *(lds16)(uintptr_t)(vt + t * (PC_TILE * PC_D * 2) + 256 * db)), p[t], acc[db]);
+        }
+        if (step + 1 < n_steps) convert(place == RING - 1 ? 0 : place + 1, (step + 1) & 1);
+        // (what is asked for comes behind this step's products: the waves that have none are at it meanwhile)
+        if (step + AHEAD < n_steps) request(before);
+    }
+    if (!real) return;
+    const float l = sums[0];
+    const int64_t at = ((int64_t)S.calls[call0 + call].part0 + split0 + rep) * W.n_q_heads + kh * g + n % g;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(W.part_o + at * PC_D + 16 * db + 4 * a) = acc[db];
+    if (a == 0) *reinterpret_cast<float2 *>(W.part_ml + at * 2) = make_float2(l == 0.f ? -INFINITY : m_ref, l);
+}
+
+void pc_launch_win_shared_decode_mx4(const PcWin &W, const PcWinShared &S, hipStream_t st)
+{
+    if (S.n_items <= 0) return;
+    const unsigned grid = (unsigned)S.n_items * W.n_kv_heads;
+    if (S.wide) pc_mx4_shared_decode_kernel<16><<<grid, 1024, 0, st>>>(W, S);
+    else pc_mx4_shared_decode_kernel<8><<<grid, 512, 0, st>>>(W, S);
+}

@@ -1,0 +1,98 @@
+// What the kernels that read a PC_MX4 cache multiply with (gfx950): codes by 8-bit pieces of queries, values by probabilities.
+#ifndef PC_MX4_PRODUCTS_H_
+#define PC_MX4_PRODUCTS_H_
+
+#include "pc_mx4.h"
+#include "pc_mfma_common.h"
+
+#include <type_traits>
+
+#define MFMA16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
+
+typedef int mx4_i32x8 __attribute__((ext_vector_type(8)));
+typedef uint16_t mx4_u16x2 __attribute__((ext_vector_type(2)));
+typedef short mx4_s16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// a wave's own LDS accesses happen in the order they are issued: the compiler is to keep it
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+// One 16-byte (4-byte) per lane direct load: lane l's bytes land at lds_wave_base + 16 l (4 l); completion is awaited by its count.
+__device__ __forceinline__ void mx4_dma16(const void *gbase_uniform, unsigned lane_off, unsigned lds_wave_base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 ::"s"(lds_wave_base), "v"(lane_off), "s"(gbase_uniform) : "memory", "m0");
+}
+__device__ __forceinline__ void mx4_dma4(const void *gbase_uniform, unsigned lane_off, unsigned lds_wave_base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 ::"s"(lds_wave_base), "v"(lane_off), "s"(gbase_uniform) : "memory", "m0");
+}
+
+// Codes (cbsz 4) by e4m3 (blgp 0), each with the exponent in a byte of its scale.  16 keys of 128 dims: lane (m, a) has block a of key m; of the
+// queries lane (n, a) has dims 16 a + 0..15 and 64 + 16 a + 0..15 of column n.  32 keys of 64 dims: lane (m, h) has block h;
+// lane (n, h) dims 16 h + 0..15 and 32 + 16 h + 0..15.
+__device__ __forceinline__ f32x4 mx4_scores16(uint4 codes, int e_codes, mx4_i32x8 q, int e_q, f32x4 c)
+{
+    const mx4_i32x8 a = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, c, 4, 0, 0, e_codes, 0, e_q);
+}
+template <int BYTE> __device__ __forceinline__ f32x16 mx4_scores32(uint4 codes, int e_codes, mx4_i32x8 q, int e_q, f32x16 c)
+{
+    const mx4_i32x8 a = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, c, 4, 0, BYTE, e_codes, 0, e_q);
+}
+// the eight slots of a dimension, in bf16 and in units of their powers
+__device__ __forceinline__ bf16x8 mx4_of_codes(uint32_t w)
+{
+    const uint4 u = make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 0)),
+                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 1)),
+                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 2)),
+                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3)));
+    return __builtin_bit_cast(bf16x8, u);
+}
+// Two slots of a dimension in bf16 (pair PAIR of the word's four), by their powers: 60 - exponent as bytes of d (pairs 0 and 1: of slots 0 to 3; 2 and 3: of 4 to 7).
+template <int PAIR> __device__ __forceinline__ uint32_t mx4_values(uint32_t w, uint32_t d, std::integral_constant<int, PAIR>)
+{
+    const auto x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, PAIR);
+    // (a slot behind a message's last token holds codes of zero, or another owner's: any finite power will do)
+    const uint32_t d0 = d >> 16 * (PAIR & 1) & 255u, d1 = d >> (16 * (PAIR & 1) + 8) & 255u;
+    return pack_bf16(x[0] * __uint_as_float((187u - min(d0, 120u)) << 23), x[1] * __uint_as_float((187u - min(d1, 120u)) << 23));
+}
+// bf16 x 2^(60 - d) for two probabilities: d as bytes 0 and 1 (or 2 and 3) of `d`; what would be below the least normal number is zero
+template <int PAIR> __device__ __forceinline__ uint32_t mx4_lowered(uint32_t p, uint32_t d)
+{
+    const uint32_t e = __builtin_amdgcn_perm(0u, d, PAIR == 0 ? 0x010C000Cu : 0x030C020Cu) >> 1;
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(mx4_u16x2, p), __builtin_bit_cast(mx4_u16x2, e)));
+}
+
+// The larger of top and two bf16 numbers' magnitudes; fine: they are numbers.
+__device__ __forceinline__ float mx4_top(float top, uint32_t w, bool &fine)
+{
+    fine &= ((w & 0x7F80u) != 0x7F80u) & ((w & 0x7F800000u) != 0x7F800000u);
+    return fmaxf(top, fmaxf(fabsf(bf_lo(w)), fabsf(bf_hi(w))));
+}
+// The unit of a row's pieces, the same for every turn: a turn keeps a pair's norm, sqrt(2) times the larger value at most, and the row's largest comes
+// between 128 and 256 of it (448 is the largest number of the pieces; one above is NaN).
+__device__ __forceinline__ float mx4_unit(float top)
+{
+    const int e = max(-100, min(100, (int)(__float_as_uint(top * 1.4142137f) >> 23 & 255) - 134));
+    return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+__device__ __forceinline__ int mx4_e4m3(const float (&x)[4], float unit)
+{
+    mx4_s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[0], x[1], unit, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[2], x[3], unit, true);
+    return __builtin_bit_cast(int, r);
+}
+// Four values as e4m3 in that unit, and what is left of them in a sixteenth of it: off by 2^-4 of 2^-4 of a value.
+__device__ __forceinline__ void mx4_pieces(const float (&x)[4], float unit, int &hi, int &rest)
+{
+    hi = mx4_e4m3(x, unit);
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, unit, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, unit, true);
+    const float y[4] = {x[0] - a[0], x[1] - a[1], x[2] - b[0], x[3] - b[1]};
+    rest = mx4_e4m3(y, unit * 0.0625f);
+}
+
+#endif

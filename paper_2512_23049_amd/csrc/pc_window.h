@@ -180,6 +180,7 @@ void pc_launch_win_decode_bf16(const PcWin &W, int n_items, const PcArgBlob *blo
 void pc_launch_win_decode_mx4(const PcWin &W, int n_items, const PcArgBlob *blob, const PcWinDecode &O, hipStream_t st);
 void pc_launch_win_attend_f32(const PcWin &W, int n_items, int D, hipStream_t st);
 void pc_launch_win_shared_decode_bf16(const PcWin &W, const PcWinShared &S, hipStream_t st);
+void pc_launch_win_shared_decode_mx4(const PcWin &W, const PcWinShared &S, hipStream_t st);
 void pc_launch_win_merge(const PcWin &W, const PcMergeRow *rows, int n_rows, int dtype, int D, hipStream_t st);
 
 #ifdef __HIPCC__

@@ -364,7 +364,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8
         dec.push_back(Group{(int32_t)i, 0, run0, tiles});
     }
     P.rots.resize(rots);                                 // (single tokens' kernels make their rotations themselves)
-    if (may_split && c->cfg.dtype == PC_BF16 && plan_shared(c, P, dec)) { P.runs.resize(runs); P.run_seg.resize(runs); return; }
+    if (may_split && plan_shared(c, P, dec)) { P.runs.resize(runs); P.run_seg.resize(runs); return; }
     no_shared();
     P.merge.resize(merge); P.part_rows = part_rows;
     make_items(c, P, dec, P.dec, 512, least, may_split, true, true);
@@ -724,7 +724,8 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         ProfScope ps(c, 3, st);
         const PcWinShared S{(const PcWinSharedItem *)(ws + L.sh_items), (const PcWinVisit *)(ws + L.sh_visits), (const PcWinSee *)(ws + L.sh_sees),
                             (const PcWinSharedCall *)(ws + L.sh_calls), (int32_t)P.sh_items.size(), P.sh_wide};
-        pc_launch_win_shared_decode_bf16(W, S, st);
+        if (mx4) pc_launch_win_shared_decode_mx4(W, S, st);
+        else pc_launch_win_shared_decode_bf16(W, S, st);
         PC_HIP(c, hipGetLastError());
     }
     if (!P.pre.empty()) {
