@@ -83,7 +83,7 @@ typedef struct {
     int32_t  n_kv_heads;       /* H_kv                                                  */
     int32_t  head_dim;         /* D: 64 or 128 (PC_BF16, PC_MX4: 128); other shapes: PC_ERR_SHAPE */
     int32_t  dtype;            /* PC_F32 | PC_BF16 | PC_MX4: type of k, v, q, out and of storage */
-    float    rope_theta;       /* RoPE base, e.g. 1e4 or 5e5                            */
+    float    rope_theta;       /* RoPE base, e.g. 1e4 or 5e5 (PC_MX4: at least 1)       */
     float    softmax_scale;    /* 0 -> 1/sqrt(D)                                        */
     int64_t  capacity_tokens;  /* slots in the cache (rounded up to PC_SLOT_ALIGN)      */
     int32_t  max_messages;

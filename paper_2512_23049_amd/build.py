@@ -22,7 +22,7 @@ VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 FILE_FLAGS = {"pc_kernels_prefill.hip": ["-fno-honor-nans"], "pc_kernels_bwd_mfma.hip": VGPR_FORM, "pc_kernels_backward.hip": VGPR_FORM,
               # (constants of the rotations, moved out of the loop over tiles, would not fit the registers)
               "pc_kernels_window_shared.hip": ["-mllvm", "-disable-machine-licm"],
-              "pc_kernels_mx4_shared.hip": ["-mllvm", "-disable-machine-licm"]}
+              "pc_kernels_mx4_shared.hip": ["-mllvm", "-disable-machine-licm"], "pc_kernels_mx4.hip": ["-mllvm", "-disable-machine-licm"]}
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-result"]

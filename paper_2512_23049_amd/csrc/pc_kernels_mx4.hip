@@ -12,30 +12,31 @@ __device__ __forceinline__ const __attribute__((address_space(4))) char *argumen
 {
     return (const __attribute__((address_space(4))) char *)__builtin_amdgcn_kernarg_segment_ptr();
 }
-struct Mx4Tile {
-    uint4 k[2];               // lane (m, a): block a of key 8 (m >> 2) + 4 half + (m & 3), its codes
-    uint32_t ke[2];           // and the exponents of that key's four blocks
-    uint4 v[2];               // dimensions 16 db + m of keys 8 a + 0..7: words of db 0..3, 4..7
-    uint4 ve[2];              // 60 - exponent: blocks 0 and 1 (keys 8 a + 0..7 each), 2 and 3
-    WinTile d;
-};
+typedef const __attribute__((address_space(3))) win_i32x4 *lds16;
+typedef const __attribute__((address_space(3))) uint32_t *lds4;
+template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
 
 }  // namespace
 
-// One query row a call.  A workgroup is 4 waves over one item of one KV head, each with a contiguous share of its tiles; the g <= 16
+#define DEC_WAVES 8
+// One query row a call.  A workgroup is 8 waves over one item of one KV head, each with a contiguous share of its tiles; the g <= 16
 // heads of the KV head are the columns of the products.
-//   scores   codes of keys as they are stored, by the turned query as the sum of two e4m3 numbers under one power of two for the row
-//            (the second has what the first leaves, at 1/16: off by 2^-8 of a value, like bf16): v_mfma_scale 16x16x128, a key's blocks and
-//            exponents where the instruction wants them, nothing is unpacked;
+//   scores   codes of keys as they are stored, by the turned query as the sum of two e4m3 numbers under one power of two for the row:
+//            v_mfma_scale 16x16x128, a key's blocks and exponents where the instruction wants them, nothing is unpacked;
 //   values   eight slots of a dimension are a word: four conversions make the operand, in units of the slots' powers.  The powers ride
 //            on the probabilities, by block of 32 dimensions: probabilities are held 2^60 times as large, and a saturating
 //            subtraction from their exponents takes the powers (-60 to 60) off again.
-// Bound: memory, 4352 bytes a tile and KV head.
+// Tiles come by direct loads, two places a wave of its own: no registers wait for them (two tiles in registers left room for two waves a
+// SIMD, see below), and no wave for another.  Bound: memory, 4352 bytes a tile and KV head.
 __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *items, const PcWinRun *runs, const int32_t *q_pos)
 {
-    __shared__ __attribute__((aligned(16))) float s_acc[4][16][PC_D + 4];
-    __shared__ float s_m[4][16], s_l[4][16];
-    __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
+    // of a tile: codes of keys and of values, exponents of keys and of values (256 bytes each: a direct load's lanes)
+    constexpr int VALUES = PC_MX4_CODES, K_EXPS = 2 * PC_MX4_CODES, V_EXPS = K_EXPS + 256, TILE = V_EXPS + 256, LOADS = 6;
+    constexpr int RING = 2 * TILE, COLUMN = PC_D + 4;
+    static_assert(16 * COLUMN * 4 <= RING, "a wave's results take the place of its tiles");
+    __shared__ __attribute__((aligned(1024))) unsigned char s_ring[DEC_WAVES][RING];
+    __shared__ float s_m[DEC_WAVES][16], s_l[DEC_WAVES][16];
+    __shared__ __attribute__((aligned(16))) float2 s_rot[DEC_WAVES][PC_D / 2];
 
     const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
     const int which = blockIdx.x / W.n_kv_heads;
@@ -50,8 +51,9 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
     const int n = lane & 15, a = lane >> 4;
     const int pos = *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(q_pos + item.q_off));
     const int lo = win_low(pos, W.window);
-    const int share = item.n_tiles / 4, more = item.n_tiles % 4;
+    const int share = item.n_tiles / DEC_WAVES, more = item.n_tiles % DEC_WAVES;
     const int n_tiles = share + (wave < more), skip = item.skip + wave * share + min(wave, more);
+    const unsigned ring = (unsigned)uniform((int)(unsigned)(uintptr_t)&s_ring[wave][0]);
 
     float m_run = -INFINITY, l_run = 0.f;
     f32x4 acc[8];
@@ -60,37 +62,39 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
     if (n_tiles > 0) {
         const unsigned char *kb = (const unsigned char *)W.k_store + (int64_t)kh * (W.slots / PC_TILE) * PC_MX4_TILE;
         const unsigned char *vb = (const unsigned char *)W.v_store + (int64_t)kh * (W.slots / PC_TILE) * PC_MX4_TILE;
-        WinWalk walk(runs + item.run0, skip, n_tiles);
-        int asked = 0;
-        const unsigned k_at = (unsigned)((8 * (n >> 2) + (n & 3)) * 64 + 16 * a), ke_at = (unsigned)(PC_MX4_CODES + (8 * (n >> 2) + (n & 3)) * 4);
-        const unsigned v_at = (unsigned)(a * 512 + n * 32), ve_at = (unsigned)(PC_MX4_CODES + a * 32);
-        auto fetch = [&](Mx4Tile &T) __attribute__((always_inline)) {
-            if (asked > 0 && asked < n_tiles) walk.next();
-            ++asked;
-            T.d = walk.tile();
-            T.d.rot = (int)((walk.run - reinterpret_cast<uintptr_t>(runs)) / sizeof(PcWinRun));       // (the run)
-            const unsigned char *kt = kb + (int64_t)(T.d.slot0 / PC_TILE) * PC_MX4_TILE, *vt = vb + (int64_t)(T.d.slot0 / PC_TILE) * PC_MX4_TILE;
-#pragma unroll
-            for (int tau = 0; tau < 2; ++tau) {
-                T.k[tau] = ldg16(kt + k_at + tau * 256);
-                T.ke[tau] = *reinterpret_cast<const uint32_t *>(kt + ke_at + tau * 16);
-                T.v[tau] = ldg16(vt + v_at + tau * 16);
-                T.ve[tau] = ldg16(vt + ve_at + tau * 16);
-            }
+        // position p of the keys' codes holds block (p & 3) ^ (key >> 3) of key p >> 2; of the values' half (p & 1) ^ (m >> 3) of m = p / 2 % 16:
+        // what the lanes of a fragment read at once hits different banks (the second 64 positions: 16 keys, and two groups of slots, on)
+        const unsigned k_src = (unsigned)((lane >> 2) * 64 + (((lane & 3) ^ (lane >> 5)) << 4)), v_src = (unsigned)((lane >> 1) * 32 + (((lane & 1) ^ (lane >> 4 & 1)) << 4));
+        const unsigned e_src = (unsigned)(PC_MX4_CODES + (lane & 31) * 4);
+        auto request = [&](int slot0, int place) __attribute__((always_inline)) {
+            const unsigned char *kt = kb + (int64_t)(slot0 / PC_TILE) * PC_MX4_TILE, *vt = vb + (int64_t)(slot0 / PC_TILE) * PC_MX4_TILE;
+            const unsigned to = ring + place * TILE;
+            mx4_dma16(kt, k_src, to);
+            mx4_dma16(kt, (k_src ^ 32) + 1024, to + 1024);
+            mx4_dma4(kt, e_src, to + K_EXPS);
+            mx4_dma16(vt, v_src, to + VALUES);
+            mx4_dma16(vt + 1024, v_src, to + VALUES + 1024);
+            mx4_dma4(vt, e_src, to + V_EXPS);
         };
         // the column's head, as it came (from the cache each time: registers): dims 16 a + 0..15, then 64 up
         const unsigned char *qp = (const unsigned char *)W.q + ((int64_t)item.q_off * W.n_q_heads + kh * g + min(n, g - 1)) * (PC_D * 2) + 32 * a;
         const double freq = W.inv_freq[lane];
-        Mx4Tile A, B;
-        fetch(A);
-        if (n_tiles > 1) fetch(B);
+        uint4 raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[i] = ldg16(qp + 128 * (i >> 1) + 16 * (i & 1));
+        // two walks over the same runs: of the tiles that are asked for, and of those that are worked on
+        WinWalk ahead(runs + item.run0, skip, n_tiles), walk = ahead;
+        request(ahead.a.x, 0);
+        if (n_tiles > 1) {
+            ahead.next();
+            request(ahead.a.x, 1);
+        }
         // the row's unit, the same for every turn; a query that holds what is no number is all NaN
         bool fine = true;
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4 u = ldg16(qp + 128 * (i >> 1) + 16 * (i & 1));
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = mx4_top(top, w[j], fine);
         }
@@ -100,49 +104,71 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
         fine &= __shfl_xor((int)fine, 32) != 0;
         const float unit = mx4_unit(top * W.scale_log2);
         const int e_hi = (int)(__float_as_uint(unit) >> 23), e_lo = e_hi - 4;
-        int cur = -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                    // (columns behind the last head are zeros)
+            raw[i].x = n >= g ? 0u : fine ? raw[i].x : 0x7FC07FC0u; raw[i].y = n >= g ? 0u : fine ? raw[i].y : 0x7FC07FC0u;
+            raw[i].z = n >= g ? 0u : fine ? raw[i].z : 0x7FC07FC0u; raw[i].w = n >= g ? 0u : fine ? raw[i].w : 0x7FC07FC0u;
+        }
+        const int key = 8 * (n >> 2) + (n & 3);
+        const unsigned k_rd = ring + (unsigned)(key * 64 + ((a ^ (key >> 3)) << 4)), ke_rd = ring + K_EXPS + key * 4;
+        const unsigned v_rd = ring + VALUES + (unsigned)(a * 512 + n * 32 + ((n >> 3) << 4)), ve_rd = ring + V_EXPS + a * 32;
+        bool turned = false;
         int64_t cur_turn = 0;
         mx4_i32x8 q_hi, q_lo;
-        auto compute = [&](Mx4Tile &T) __attribute__((always_inline)) {
-            if (T.d.rot != cur) {                        // another run: another rotation?
-                const int64_t turn = pos - T.d.rot_pos;
-                const bool fresh = cur < 0 || turn != cur_turn;
-                cur = T.d.rot; cur_turn = turn;
-                if (fresh) {
-                    const float2 cs = rope_angle((double)turn * freq);
-                    s_rot[wave][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
-                    in_order();
+#pragma unroll 1
+        for (int t = 0; t < n_tiles; ++t) {
+            const WinTile e = walk.tile();
+            const int64_t turn = pos - e.rot_pos;
+            if (!turned || turn != cur_turn) {           // another run: another rotation?
+                turned = true; cur_turn = turn;
+                const float2 cs = mx4_rotation((double)turn * freq);
+                in_order();
+                s_rot[wave][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
+                in_order();
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {        // dims 16 a + 4 s, and 64 up
-                        uint2 lq = *reinterpret_cast<const uint2 *>(qp + 8 * s), hq = *reinterpret_cast<const uint2 *>(qp + 128 + 8 * s);
-                        if (n >= g) lq = hq = make_uint2(0, 0);
-                        if (!fine) lq = hq = make_uint2(0x7FC07FC0u, 0x7FC07FC0u);
-                        const float4 *r = reinterpret_cast<const float4 *>(&s_rot[wave][16 * a + 4 * s]);
-                        const float4 r0 = r[0], r1 = r[1];
-                        const float x0 = bf_lo(lq.x), x1 = bf_hi(lq.x), x2 = bf_lo(lq.y), x3 = bf_hi(lq.y);
-                        const float y0 = bf_lo(hq.x), y1 = bf_hi(hq.x), y2 = bf_lo(hq.y), y3 = bf_hi(hq.y);
-                        const float u[4] = {x0 * r0.x - y0 * r0.y, x1 * r0.z - y1 * r0.w, x2 * r1.x - y2 * r1.y, x3 * r1.z - y3 * r1.w};
-                        const float v[4] = {x0 * r0.y + y0 * r0.x, x1 * r0.w + y1 * r0.z, x2 * r1.y + y2 * r1.x, x3 * r1.w + y3 * r1.z};
-                        int hi, rest;
-                        mx4_pieces(u, unit, hi, rest);
-                        q_hi[s] = hi; q_lo[s] = rest;
-                        mx4_pieces(v, unit, hi, rest);
-                        q_hi[4 + s] = hi; q_lo[4 + s] = rest;
-                    }
-                    in_order();
+                for (int i = 0; i < 4; ++i)              // (its 32 numbers, taken apart once and kept, would not fit the registers)
+                    asm volatile("" : "+v"(raw[i].x), "+v"(raw[i].y), "+v"(raw[i].z), "+v"(raw[i].w));
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {            // dims 16 a + 4 s, and 64 up
+                    const uint4 lq = raw[s >> 1], hq = raw[2 + (s >> 1)];
+                    const uint32_t lw[2] = {s & 1 ? lq.z : lq.x, s & 1 ? lq.w : lq.y}, hw[2] = {s & 1 ? hq.z : hq.x, s & 1 ? hq.w : hq.y};
+                    const float4 *r = reinterpret_cast<const float4 *>(&s_rot[wave][16 * a + 4 * s]);
+                    const float4 r0 = r[0], r1 = r[1];
+                    const float x0 = bf_lo(lw[0]), x1 = bf_hi(lw[0]), x2 = bf_lo(lw[1]), x3 = bf_hi(lw[1]);
+                    const float y0 = bf_lo(hw[0]), y1 = bf_hi(hw[0]), y2 = bf_lo(hw[1]), y3 = bf_hi(hw[1]);
+                    const float u[4] = {x0 * r0.x - y0 * r0.y, x1 * r0.z - y1 * r0.w, x2 * r1.x - y2 * r1.y, x3 * r1.z - y3 * r1.w};
+                    const float v[4] = {x0 * r0.y + y0 * r0.x, x1 * r0.w + y1 * r0.z, x2 * r1.y + y2 * r1.x, x3 * r1.w + y3 * r1.z};
+                    int hi, rest;
+                    mx4_pieces(u, unit, hi, rest);
+                    q_hi[s] = hi; q_lo[s] = rest;
+                    mx4_pieces(v, unit, hi, rest);
+                    q_hi[4 + s] = hi; q_lo[4 + s] = rest;
                 }
+                in_order();
             }
+            if (t + 1 < n_tiles) wait_vm<LOADS>();       // this tile has landed
+            else wait_vm<0>();
+            in_order();
+            const unsigned at = (t & 1) * TILE;
             f32x4 s[2];
 #pragma unroll
             for (int tau = 0; tau < 2; ++tau) {
-                const int e = (int)(T.ke[tau] >> (8 * a));
-                s[tau] = mx4_scores16(T.k[tau], e, q_lo, e_lo, (f32x4){0.f, 0.f, 0.f, 0.f});
-                s[tau] = mx4_scores16(T.k[tau], e, q_hi, e_hi, s[tau]);
+                const uint4 codes = __builtin_bit_cast(uint4, *(lds16)(uintptr_t)(k_rd + at + tau * 256));
+                const int ek = (int)(*(lds4)(uintptr_t)(ke_rd + at + tau * 16) >> (8 * a));
+                s[tau] = mx4_scores16(codes, ek, q_lo, e_lo, (f32x4){0.f, 0.f, 0.f, 0.f});
+                s[tau] = mx4_scores16(codes, ek, q_hi, e_hi, s[tau]);
+            }
+            uint32_t vw[8], ew[8];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const win_i32x4 w = *(lds16)(uintptr_t)((v_rd ^ (half << 4)) + at), x = *(lds16)(uintptr_t)(ve_rd + at + half * 16);
+                vw[4 * half] = (uint32_t)w.x; vw[4 * half + 1] = (uint32_t)w.y; vw[4 * half + 2] = (uint32_t)w.z; vw[4 * half + 3] = (uint32_t)w.w;
+                ew[4 * half] = (uint32_t)x.x; ew[4 * half + 1] = (uint32_t)x.y; ew[4 * half + 2] = (uint32_t)x.z; ew[4 * half + 3] = (uint32_t)x.w;
             }
             float sc[8];                                 // keys 8 a + 0..7 of column n
 #pragma unroll
             for (int j = 0; j < 8; ++j) sc[j] = s[j >> 2][j & 3];
-            const uint32_t sees = win_sees(T.d.pos0, T.d.valid, T.d.sink, false, lo, 0);        // (the only row sees all of the new message)
+            const uint32_t sees = win_sees(e.pos0, e.valid, e.sink, false, lo, 0);        // (the only row sees all of the new message)
             if (sees != ~0u) {                           // (uniform; values need no mask: codes are finite)
                 const uint32_t mine = sees >> (8 * a);
 #pragma unroll
@@ -165,8 +191,13 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
 #pragma unroll
                 for (int db = 0; db < 8; ++db) acc[db] *= alpha;
             }
-            const uint32_t vw[8] = {T.v[0].x, T.v[0].y, T.v[0].z, T.v[0].w, T.v[1].x, T.v[1].y, T.v[1].z, T.v[1].w};
-            const uint32_t ew[8] = {T.ve[0].x, T.ve[0].y, T.ve[0].z, T.ve[0].w, T.ve[1].x, T.ve[1].y, T.ve[1].z, T.ve[1].w};
+            // (the tile's last numbers are in registers: its place is free)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(vw[j]), "+v"(ew[j]));
+            if (t + 2 < n_tiles) {
+                ahead.next();
+                request(ahead.a.x, t & 1);
+            }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const bf16x8 p = __builtin_bit_cast(bf16x8, make_uint4(mx4_lowered<0>(pk[0], ew[2 * b]), mx4_lowered<1>(pk[1], ew[2 * b]),
@@ -174,33 +205,27 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
 #pragma unroll
                 for (int i = 0; i < 2; ++i) acc[2 * b + i] = MFMA16(mx4_of_codes(vw[2 * b + i]), p, acc[2 * b + i]);
             }
-        };
-        for (int t = 0;;) {
-            compute(A);
-            if (t + 2 < n_tiles) fetch(A);
-            if (++t >= n_tiles) break;
-            compute(B);
-            if (t + 2 < n_tiles) fetch(B);
-            if (++t >= n_tiles) break;
+            if (t + 1 < n_tiles) walk.next();
         }
     }
     l_run += __shfl_xor(l_run, 16);
     l_run += __shfl_xor(l_run, 32);
+    float (*s_acc)[COLUMN] = reinterpret_cast<float (*)[COLUMN]>(&s_ring[wave][0]);      // (no load of its own is on its way to it)
     if (a == 0) { s_m[wave][n] = m_run; s_l[wave][n] = l_run * 0x1p-60f; }
 #pragma unroll
-    for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(&s_acc[wave][n][16 * db + 4 * a]) = acc[db];
+    for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(&s_acc[n][16 * db + 4 * a]) = acc[db];
     __syncthreads();
-    for (int idx = threadIdx.x; idx < g * (PC_D / 2); idx += 256) {
+    for (int idx = threadIdx.x; idx < g * (PC_D / 2); idx += 64 * DEC_WAVES) {
         const int col = idx / (PC_D / 2), dim = 2 * (idx % (PC_D / 2)), h = kh * g + col;
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, s_m[w][col]);
+        for (int w = 0; w < DEC_WAVES; ++w) m = fmaxf(m, s_m[w][col]);
         float o0 = 0.f, o1 = 0.f, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < DEC_WAVES; ++w) {
             // (a wave whose scores were not numbers has a sum that is none; one that saw nothing has a sum of 0)
             const float f = s_l[w][col] == 0.f ? 0.f : ex2(s_m[w][col] - (m == -INFINITY ? 0.f : m));
-            const float2 x = *reinterpret_cast<const float2 *>(&s_acc[w][col][dim]);
+            const float2 x = *reinterpret_cast<const float2 *>(&s_ring[w][(col * COLUMN + dim) * 4]);
             if (s_l[w][col] != 0.f) { o0 += x.x * f; o1 += x.y * f; l += s_l[w][col] * f; }
         }
         if (item.part < 0) {
@@ -214,8 +239,8 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
     }
 }
 
-__global__ __launch_bounds__(256, 2) void pc_mx4_decode_kernel(PcWin W) { mx4_decode(W, W.items, W.runs, W.q_pos); }
-__global__ __launch_bounds__(256, 2) void pc_mx4_decode_arg_kernel(PcArgBlob, PcWinDecode O, PcWin W)
+__global__ __launch_bounds__(64 * DEC_WAVES, 4) void pc_mx4_decode_kernel(PcWin W) { mx4_decode(W, W.items, W.runs, W.q_pos); }
+__global__ __launch_bounds__(64 * DEC_WAVES, 4) void pc_mx4_decode_arg_kernel(PcArgBlob, PcWinDecode O, PcWin W)
 {
     const char *lists = (const char *)arguments();       // (the blob comes first)
     if (blockIdx.x == 0 && (int)threadIdx.x < O.n16) reinterpret_cast<uint4 *>(O.ws)[threadIdx.x] = reinterpret_cast<const uint4 *>(lists)[threadIdx.x];
@@ -227,8 +252,8 @@ void pc_launch_win_decode_mx4(const PcWin &W, int n_items, const PcArgBlob *blob
 {
     if (n_items <= 0) return;
     const unsigned grid = (unsigned)n_items * W.n_kv_heads;
-    if (blob) pc_mx4_decode_arg_kernel<<<grid, 256, 0, st>>>(*blob, O, W);
-    else pc_mx4_decode_kernel<<<grid, 256, 0, st>>>(W);
+    if (blob) pc_mx4_decode_arg_kernel<<<grid, 64 * DEC_WAVES, 0, st>>>(*blob, O, W);
+    else pc_mx4_decode_kernel<<<grid, 64 * DEC_WAVES, 0, st>>>(W);
 }
 
 // ----------------------------------------------------------------------------------------------------------- prepare
@@ -245,7 +270,7 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
             if (i < n_copy) { reinterpret_cast<uint4 *>(P.ws)[i] = reinterpret_cast<const uint4 *>(from)[i]; continue; }
             const int64_t k = (i - n_copy) / (PC_D / 2);
             const int f = (int)((i - n_copy) % (PC_D / 2));
-            const float2 cs = rope_angle((double)reinterpret_cast<const int64_t *>(from + P.off_rot)[k] * P.inv_freq[f]);
+            const float2 cs = mx4_rotation((double)reinterpret_cast<const int64_t *>(from + P.off_rot)[k] * P.inv_freq[f]);
             P.rot_run[k * (PC_D / 2) + f] = make_float2(cs.x * P.scale_log2, cs.y * P.scale_log2);
         }
         return;
@@ -339,7 +364,6 @@ void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st
 
 namespace {
 __device__ __forceinline__ int imax3(int a, int b, int c) { return max(max(a, b), c); }
-template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14)); }
 __device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "memory"); }
 }  // namespace
 

@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
                     if (mine && a == 0) s_see[wave][n] = make_int4(x.x, x.y, x.z, x.w);
                     of = mine ? i : of;
                     const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y.y << 32) | (uint32_t)y.x);
-                    const float2 cs = rope_angle((double)turn * s_freq[lane]);
+                    const float2 cs = mx4_rotation((double)turn * s_freq[lane]);
                     s_rot[wave][i][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
                 }
                 asm volatile("" ::: "memory");

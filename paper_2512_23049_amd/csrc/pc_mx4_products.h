@@ -66,6 +66,10 @@ template <int PAIR> __device__ __forceinline__ uint32_t mx4_lowered(uint32_t p, 
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(mx4_u16x2, p), __builtin_bit_cast(mx4_u16x2, e)));
 }
 
+// (cos, sin) of a turn: positions are below 2^30 and theta is at least 1 (pc_cache_create), so that what queries are turned by is below 3 x 2^30
+// radians, and its quarter turns fit 32 bits.  The branch for other angles would cost the kernels their registers.
+__device__ __forceinline__ float2 mx4_rotation(double x) { return rope_small(x); }
+
 // The larger of top and two bf16 numbers' magnitudes; fine: they are numbers.
 __device__ __forceinline__ float mx4_top(float top, uint32_t w, bool &fine)
 {

@@ -47,6 +47,9 @@ int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan 
     P.res.resize((size_t)n_calls);
     P.calls.resize((size_t)n_calls);
     int64_t total_q = 0;
+    size_t entries = 0;
+    for (int i = 0; i < n_calls; ++i) entries += (size_t)std::max(calls[i].n_sel, 0) + 1;
+    P.segs.reserve(entries);
     for (int i = 0; i < n_calls; ++i) {
         const int32_t rc = pc_resolve(c, &calls[i], i, P.res[(size_t)i]);
         if (rc != PC_OK) return rc;
@@ -73,8 +76,9 @@ int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan 
     return PC_OK;
 }
 
-// The runs that rows [row0, row1) of a call see, behind those there are; the number of their tiles.
-int32_t add_runs(WinPlan &P, const WinCall &wc, int32_t row0, int32_t row1)
+// The runs that rows [row0, row1) of a call see, behind those there are; the number of their tiles.  rotations: their rows of the
+// rotation table (single tokens' kernels make them themselves).
+int32_t add_runs(WinPlan &P, const WinCall &wc, int32_t row0, int32_t row1, bool rotations = true)
 {
     int32_t p_min = P.q_pos[(size_t)wc.q_off + row0];
     for (int32_t r = row0 + 1; r < row1; ++r) p_min = std::min(p_min, P.q_pos[(size_t)wc.q_off + r]);
@@ -86,7 +90,7 @@ int32_t add_runs(WinPlan &P, const WinCall &wc, int32_t row0, int32_t row1)
         const int64_t skip = std::max<int64_t>(0, low - s.start);       // tokens in front of the window
         const int32_t sinks = (int32_t)std::min<int64_t>(std::max<int64_t>(0, P.n_sink - s.before), end);
         if (skip >= end && sinks == 0) continue;
-        if (s.rot < 0) {
+        if (s.rot < 0 && rotations) {
             if (P.rots.empty() || P.rots.back() != s.rot_pos) P.rots.push_back(s.rot_pos);
             s.rot = (int32_t)P.rots.size() - 1;
         }
@@ -120,7 +124,7 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
     // (many groups: to the nearest, as one a little longer than the others is not worth a merge of its own)
     bool nearest = true;
     auto splits = [&](int32_t tiles) {
-        if (tokens && tiles <= least + least / 2) return 1;           // (10 tiles whole 8.0 us, halved 9.5, with the merge)
+        if (tokens && tiles <= least + least / 2) return 1;           // (bf16: 10 tiles whole 8.0 us, halved 9.5, with the merge)
         return (int32_t)std::max<int64_t>(1, std::min<int64_t>((tiles + (nearest ? chunk / 2 : chunk - 1)) / chunk, MAX_SPLITS));
     };
     // fit: where whole groups have room at once, their splits get it too, and the longest is as short as that allows (fp32, two
@@ -194,19 +198,24 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     const double alone = std::max(8 + 0.0175 * (double)own * heads, host);
     auto together = [&](int64_t tiles) { return std::max(48 + (0.0227 * (double)tiles + 0.0055 * (double)own) * heads, planned); };
     if (c->decode_sharing == 0 && alone <= together(own / set_calls)) return false;
-    struct Piece { int32_t slot0, tiles; size_t run; int32_t call; };
+    struct Piece { int32_t slot0, tiles; uint32_t run; int32_t call; };
     std::vector<Piece> pieces, scratch;
-    // pieces [first, size) by their slots, in the calls' order where those are the same: a pass for 11 bits of a tile's number
-    auto by_slot = [](std::vector<Piece> &v, size_t first, std::vector<Piece> &other) {
+    pieces.reserve(P.runs.size() - (size_t)dec[0].run0);
+    // pieces [first, size) by their slots, in the calls' order where those are the same: a pass for 13 bits of a tile's number
+    constexpr uint32_t DIGIT = 13;
+    std::vector<uint32_t> digits(1u << DIGIT);
+    auto by_slot = [&](std::vector<Piece> &v, size_t first, std::vector<Piece> &other) {
         uint32_t most = 0;
         for (size_t k = first; k < v.size(); ++k) most = std::max(most, (uint32_t)v[k].slot0 / PC_TILE);
         other.resize(v.size());
-        for (uint32_t shift = 0; shift == 0 || (shift < 32 && most >> shift); shift += 11) {
-            size_t at[2048] = {}, next = first;
-            for (size_t k = first; k < v.size(); ++k) ++at[((uint32_t)v[k].slot0 / PC_TILE >> shift) & 2047];
-            for (size_t &n : at) { const size_t count = n; n = next; next += count; }
-            for (size_t k = first; k < v.size(); ++k) other[at[((uint32_t)v[k].slot0 / PC_TILE >> shift) & 2047]++] = v[k];
-            std::swap_ranges(v.begin() + (ptrdiff_t)first, v.end(), other.begin() + (ptrdiff_t)first);
+        for (uint32_t shift = 0; shift == 0 || (shift < 32 && most >> shift); shift += DIGIT) {
+            const uint32_t mask = (1u << DIGIT) - 1, used = std::min(mask, most >> shift);
+            std::fill(digits.begin(), digits.begin() + used + 1, 0u);
+            for (size_t k = first; k < v.size(); ++k) ++digits[((uint32_t)v[k].slot0 / PC_TILE >> shift) & mask];
+            uint32_t next = (uint32_t)first;
+            for (uint32_t d = 0; d <= used; ++d) { const uint32_t count = digits[d]; digits[d] = next; next += count; }
+            for (size_t k = first; k < v.size(); ++k) other[digits[((uint32_t)v[k].slot0 / PC_TILE >> shift) & mask]++] = v[k];
+            std::memcpy(v.data() + first, other.data() + first, sizeof(Piece) * (v.size() - first));
         }
     };
     std::vector<std::pair<size_t, size_t>> of_set;       // a set's pieces, in slot order
@@ -216,7 +225,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
             int32_t left = dec[(size_t)j].tiles;
             for (size_t r = (size_t)dec[(size_t)j].run0; left > 0; ++r) {
                 const int32_t t = (P.runs[r].n_tok + PC_TILE - 1) / PC_TILE;
-                pieces.push_back(Piece{P.runs[r].slot0, t, r, j});
+                pieces.push_back(Piece{P.runs[r].slot0, t, (uint32_t)r, j});
                 left -= t;
             }
         }
@@ -230,8 +239,9 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     }
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
     if (shared == 0 || (c->decode_sharing == 0 && alone <= together(shared))) return false;
-    struct Seen { int32_t call; size_t seg; PcWinSee see; };         // (call: within the set)
-    std::vector<Seen> seen;                              // who sees the visit at hand, and from which entry of its list
+    struct Seen { int32_t call; uint32_t seg; };                     // (call: within the set)
+    std::vector<Seen> seen;                              // who sees the visit at hand, and from which entry of its list; its views: P.sh_sees from e0 on
+    P.sh_sees.reserve(pieces.size() + pieces.size() / 4);
     for (int32_t s = 0; s < n_sets; ++s) {
         const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
         int32_t waves = 1;
@@ -260,6 +270,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                 const Visit &v = visits[at];
                 const int32_t n = std::min(left, v.tiles - done), slot0 = v.slot0 + PC_TILE * done, slot1 = slot0 + PC_TILE * n;
                 seen.clear();
+                const size_t e0 = P.sh_sees.size();
                 for (size_t k = v.p0; k < v.p1; ++k) {
                     const Piece &pc = pieces[k];
                     if (pc.slot0 >= slot1 || pc.slot0 + PC_TILE * pc.tiles <= slot0) continue;
@@ -267,21 +278,29 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                     const int32_t d = slot0 - r.slot0;   // (what lies in front of a run is left out by its window)
                     const int32_t j = pc.call - call0, q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)pc.call].call].q_off];
                     PcWinSee e{r.pos0 + d, r.n_tok - d, std::max(0, r.sink > 0 ? r.sink - d : 0), win_low(q_pos, P.window), (int64_t)q_pos - r.rot_pos, j % per, 0};
-                    size_t i = seen.size();              // (nearly in order already)
+                    const uint32_t seg = (uint32_t)P.run_seg[pc.run];
+                    if (seen.empty() || seen.back().call < j) {          // (in order, mostly)
+                        seen.push_back(Seen{j, seg});
+                        P.sh_sees.push_back(e);
+                        continue;
+                    }
+                    size_t i = seen.size();
                     while (i > 0 && seen[i - 1].call > j) --i;
                     if (i > 0 && seen[i - 1].call == j) {                // the sinks of an extent and its end: one view
-                        Seen &o = seen[i - 1];
-                        if (o.seg != P.run_seg[pc.run]) return false;    // listed twice: two views, and a column has room for one
-                        o.see.n_tok = std::max(o.see.n_tok, e.n_tok); o.see.sink = std::max(o.see.sink, e.sink);
-                    } else seen.insert(seen.begin() + (ptrdiff_t)i, Seen{j, P.run_seg[pc.run], e});
+                        PcWinSee &o = P.sh_sees[e0 + i - 1];
+                        if (seen[i - 1].seg != seg) return false;        // listed twice: two views, and a column has room for one
+                        o.n_tok = std::max(o.n_tok, e.n_tok); o.sink = std::max(o.sink, e.sink);
+                    } else {
+                        seen.insert(seen.begin() + (ptrdiff_t)i, Seen{j, seg});
+                        P.sh_sees.insert(P.sh_sees.begin() + (ptrdiff_t)(e0 + i), e);
+                    }
                 }
-                PcWinVisit pv{slot0, n, (int32_t)P.sh_sees.size(), {}};
+                PcWinVisit pv{slot0, n, (int32_t)e0, {}};
                 size_t k = 0;
                 for (int32_t gr = 0; gr <= PC_WIN_GROUPS; ++gr) {
                     while (k < seen.size() && seen[k].call / per < gr) ++k;
                     pv.off[gr] = (int32_t)k;
                 }
-                for (const Seen &o : seen) P.sh_sees.push_back(o.see);
                 P.sh_visits.push_back(pv);
                 P.sh_items.back().n_steps += (n + PC_WIN_STEP_TILES - 1) / PC_WIN_STEP_TILES;
                 left -= n; done += n;
@@ -321,8 +340,9 @@ void list_tiles(WinPlan &P)
 // Everything a forward call launches: rows of prompts in groups of four units (bf16: 32 rows x head; fp32: blocks of 32 columns, single
 // tokens too), with the runs that each group sees, then single tokens, shared or call by call.  may_split: or every group is one
 // item; least: tiles that a split of a single token is worth.
-void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8)
+void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 0)
 {
+    if (least == 0) least = c->cfg.dtype == PC_MX4 ? 24 : 8;             // (a workgroup of a 4-bit cache's tokens is eight waves: three tiles each)
     const int g = c->g;
     P.pre.clear(); P.dec.clear(); P.runs.clear(); P.run_seg.clear(); P.rots.clear(); P.merge.clear();
     auto no_shared = [&] { P.sh_items.clear(); P.sh_visits.clear(); P.sh_sees.clear(); P.sh_calls.clear(); };
@@ -358,9 +378,12 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 8
     const size_t runs = P.runs.size(), rots = P.rots.size(), merge = P.merge.size();
     const int64_t part_rows = P.part_rows;
     if (c->cfg.dtype == PC_MX4) list_tiles(P);
+    size_t entries = 0;
+    for (const WinCall &wc : P.calls) if (wc.n_q == 1) entries += wc.n_seg;
+    P.runs.reserve(runs + entries); P.run_seg.reserve(runs + entries);           // (a little more where calls have sinks in front of their windows)
     for (size_t i = 0; i < P.calls.size(); ++i) {
         if (P.calls[i].n_q != 1) continue;
-        const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, P.calls[i], 0, 1);
+        const int32_t run0 = (int32_t)P.runs.size(), tiles = add_runs(P, P.calls[i], 0, 1, false);
         dec.push_back(Group{(int32_t)i, 0, run0, tiles});
     }
     P.rots.resize(rots);                                 // (single tokens' kernels make their rotations themselves)
