@@ -139,13 +139,17 @@ static int32_t attend_impl(pc_cache *c, const pc_call *calls, int32_t n_calls, c
     if (fork) PC_HIP(c, hipEventRecord(c->ev_join, c->side));
     if (P.n_kg_items > 0) {
         ProfScope ps(c, 8, st);
-        pc_launch_gather(L, (const PcGatherItem *)(w + P.lay.kg_items), P.n_kg_items, P.kg_tiles, (const int32_t *)(w + P.lay.seg_kvoff), st);
+        const PcGatherItem *items = (const PcGatherItem *)(w + P.lay.kg_items);
+        const int32_t *off = (const int32_t *)(w + P.lay.seg_kvoff);
+        if (P.mx4_rows) pc_launch_gather_mx4(L, items, P.n_kg_items, P.kg_tiles, off, c->counters_dev + 2 * PC_ONE_COUNTERS, P.mark_value, st);
+        else pc_launch_gather(L, items, P.n_kg_items, P.kg_tiles, off, st);
         PC_HIP(c, hipGetLastError());
     }
     if (P.n_pre_pk > 0) {
         ProfScope ps(c, 2, st);
         L.items = (const PcItem *)(w + P.lay.items_pk);
-        pc_launch_prefill_bf16(L, P.n_pre_pk, true, st);
+        if (P.mx4_rows) pc_launch_prefill_f16(L, P.n_pre_pk, c->counters_dev + 2 * PC_ONE_COUNTERS, P.mark_value, st);
+        else pc_launch_prefill_bf16(L, P.n_pre_pk, true, st);
         PC_HIP(c, hipGetLastError());
     }
     if (P.n_pre > 0) {
@@ -160,12 +164,20 @@ static int32_t attend_impl(pc_cache *c, const pc_call *calls, int32_t n_calls, c
         const PcMergeRow *rows = (const PcMergeRow *)(w + P.lay.merge_rows);
         const int few = P.n_merge_few, many = P.n_merge_rows - few;
         const PcMergeDone done = release.done();         // (either launch comes behind what reads the slot)
-        pc_launch_merge(c->cfg.dtype, rows, few, 1, false, L.part_o, L.part_ml, out, lse, c->cfg.n_q_heads, c->D, many > 0 ? PcMergeDone{} : done, st);
-        pc_launch_merge(c->cfg.dtype, rows + few, many, 4, P.n_sh_items > 0, L.part_o, L.part_ml, out, lse, c->cfg.n_q_heads, c->D, done, st);
+        const int dtype = P.mx4_rows ? PC_BF16 : c->cfg.dtype;
+        pc_launch_merge(dtype, rows, few, 1, false, L.part_o, L.part_ml, out, lse, c->cfg.n_q_heads, c->D, many > 0 ? PcMergeDone{} : done, st);
+        pc_launch_merge(dtype, rows + few, many, 4, P.n_sh_items > 0, L.part_o, L.part_ml, out, lse, c->cfg.n_q_heads, c->D, done, st);
         PC_HIP(c, hipGetLastError());
         release.launched(done);
     }
     return PC_OK;
+}
+
+int32_t pc_attend_gathered_mx4(pc_cache *c, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, uint32_t value)
+{
+    Planned P;
+    P.mx4_rows = true; P.mark_value = value;
+    return attend_impl(c, calls, n_calls, q, out, lse, st, nullptr, 0, &P);
 }
 
 extern "C" {

@@ -60,7 +60,8 @@ struct pc_cache {
     void *storage = nullptr; bool owns_storage = false;
     void *k_store = nullptr, *v_store = nullptr;
     PcMsgEntry *table_dev = nullptr;
-    uint32_t *counters_dev = nullptr;                    // PcOne::counters of pc_attend, then those of pc_attend_static
+    uint32_t *counters_dev = nullptr;                    // PcOne::counters of pc_attend, then those of pc_attend_static, then the mark of pc_attend_mx4
+    uint32_t mark_epoch_mx4 = 0;                         // what its last call marks with
     double *inv_freq_dev = nullptr;
     void *ws = nullptr; size_t ws_cap = 0;
     size_t ws_refused = SIZE_MAX;                        // a gradient's workspace the device had no room for
@@ -201,6 +202,8 @@ struct Planned {
     const void *q = nullptr;                             // the caller's queries, where the way depends on their alignment
     // The gradient of a bf16 batch (set backward before planning): its launches, each over a run of row blocks
     bool backward = false;
+    // Long prefills of a PC_MX4 cache (set before planning): every call gathers, and is marked with mark_value where the copy does not hold it
+    bool mx4_rows = false; uint32_t mark_value = 0;
     // A slot of the ring that the call's merge is to release, where the caller asks for it (merge_releases) and there is one: an event behind
     // the launch that reads the slot holds up the launch after it for 2.1 us
     bool merge_releases = false; StageSlot *merge_slot = nullptr;
@@ -224,6 +227,8 @@ struct Planned {
     std::vector<PcTokenItem> tok_items; const void *tok_k = nullptr, *tok_v = nullptr; bool tok_done = false;
 };
 
+// pc_attend.hip: calls of many rows of a PC_MX4 cache over a packed copy of what they list; marked with value (see PcRange) where that does not hold it
+int32_t pc_attend_gathered_mx4(pc_cache *c, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, uint32_t value);
 // pc_lib.hip
 extern "C" int32_t pc_check_token_batch(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, const void *k, const void *v);
 // projected (or null): the tokens are rows of a projection, which go through the norms (q: its queries, or null)

@@ -263,6 +263,7 @@ void pc_launch_win_decode_mx4(const PcWin &W, int n_items, const PcArgBlob *blob
 __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare &P)
 {
     __shared__ __attribute__((aligned(16))) float2 s_rot[PC_D / 2][33];           // [frequency][row]
+    if (P.mark && *P.mark != P.mark_value) return;       // (the walk in front of this one served every call)
     int block = blockIdx.x;
     if (block < P.list_blocks) {
         const int64_t n_copy = from != P.ws ? P.n16 : 0, n_all = n_copy + (int64_t)P.n_rot * (PC_D / 2);
@@ -374,6 +375,7 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING * SLOT];
     __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
 
+    if (M.mark && *M.mark != M.mark_value) return;       // (the walk in front of this one served every call)
     const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
     const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
     const int g = W.n_q_heads / W.n_kv_heads;
@@ -674,4 +676,126 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
 void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, hipStream_t st)
 {
     if (n_items > 0) pc_mx4_prefill_kernel<<<(unsigned)n_items * W.n_kv_heads, 256, 0, st>>>(W, M);
+}
+
+// ------------------------------------------------------------------------------------------------------------ gather
+// Long prefills (see pc_attend_mx4): the call's keys and values copied token after token into a packed copy, as pc_gather_kernel does it for bf16,
+// keys turned to the positions that the call gives them and rounded to fp16 (off by 2^-12 of a value), values as the bf16 that they stand for.
+// Keys above 6 x 2^7, and those that are no number (which that walk would add to masks), mark the call for the walk behind it: below, what
+// queries under fp16's normal numbers are off by, 2^-25, moves a score by 2^-25 x 2^10 x sqrt(128) at most.
+// Bound: memory, 136 bytes read and 512 written a token and KV head.
+__global__ __launch_bounds__(256) void pc_mx4_gather_kernel(PcLaunch L, const PcGatherItem *__restrict__ items, int n_items, const int32_t *__restrict__ seg_kvoff,
+                                                            uint32_t *mark, uint32_t value)
+{
+    __shared__ int s_slot[PC_TILE], s_seg[PC_TILE];
+    __shared__ float s_norm[4];
+    const int G = blockIdx.x, kh = blockIdx.y;
+    int j = 0;
+    while (j + 1 < n_items && items[j + 1].kg_tile0 <= G) ++j;           // few calls gather: a short scan
+    const PcGatherItem it = items[j];
+    const PcCallDesc cd = L.calls[it.call];
+    const int t = G - it.kg_tile0;
+    const int p_tiles = (it.n_par + PC_TILE - 1) / PC_TILE;
+    if (threadIdx.x < PC_TILE) {
+        const int r = threadIdx.x;
+        int slot = -1, seg = 0;
+        if (t < p_tiles) {
+            const int i = PC_TILE * t + r - (p_tiles * PC_TILE - it.n_par);   // token of the parents' part (the padding comes first)
+            if (i >= 0) {
+                const int32_t *off = seg_kvoff + cd.seg_off;
+                int lo = 0, hi = cd.n_sel - 1;
+                while (lo < hi) {                          // last parent whose first token is <= i (empty ones share their successor's offset)
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (off[mid] <= i) lo = mid; else hi = mid - 1;
+                }
+                seg = lo;
+                slot = L.segs[cd.seg_off + lo].slot_start + (i - off[lo]);
+            }
+        } else {
+            const int i = PC_TILE * (t - p_tiles) + r;     // token of the new message
+            if (i < cd.self_len) { seg = cd.n_seg - 1; slot = L.segs[cd.seg_off + seg].slot_start + i; }
+        }
+        s_slot[r] = slot; s_seg[r] = seg;
+    }
+    __syncthreads();
+    const int64_t head = (int64_t)kh * (L.slots / PC_TILE) * PC_MX4_TILE;
+    const char *ks = (const char *)L.k_store + head, *vs = (const char *)L.v_store + head;
+    {
+        const int r = threadIdx.x >> 3, c = threadIdx.x & 7;
+        const int slot = s_slot[r];
+        uint16_t *dst = (uint16_t *)L.k_gather + ((int64_t)kh * L.kg_slots + (int64_t)G * PC_TILE + r) * PC_D + 8 * c;
+        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+        float ss = 0.f;
+        if (slot >= 0) {
+            const char *kt = ks + (int64_t)(slot / PC_TILE) * PC_MX4_TILE;
+            const uint32_t a = *reinterpret_cast<const uint32_t *>(kt + slot % PC_TILE * 64 + 4 * c), b = *reinterpret_cast<const uint32_t *>(kt + slot % PC_TILE * 64 + 32 + 4 * c);
+            const uint32_t ex = *reinterpret_cast<const uint32_t *>(kt + PC_MX4_CODES + slot % PC_TILE * 4) >> 8 * (c >> 2);
+            const uint32_t ea = ex & 255u, eb = ex >> 16 & 255u;
+            if (max(ea, eb) > 127u + 7u) *mark = value;     // (255: no number)
+            const float ua = __uint_as_float(min(ea, 127u + 7u) << 23), ub = __uint_as_float(min(eb, 127u + 7u) << 23);
+            const float4 *rot = reinterpret_cast<const float4 *>(L.rot_seg + (int64_t)(cd.seg_off + s_seg[r]) * (PC_D / 2) + 8 * c);
+            uint32_t *lw = reinterpret_cast<uint32_t *>(&lo), *hw = reinterpret_cast<uint32_t *>(&hi);
+            auto pair = [&](auto u) __attribute__((always_inline)) {
+                constexpr int U = decltype(u)::value;
+                const float4 cs = rot[U];                    // (cos, sin) of pairs 2 U and 2 U + 1
+                const auto xs = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(a, 1.f, U), ys = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(b, 1.f, U);
+                const float x0 = xs[0] * ua, x1 = xs[1] * ua, y0 = ys[0] * ub, y1 = ys[1] * ub;
+                ss += x0 * x0 + x1 * x1 + y0 * y0 + y1 * y1;                 // (a turn keeps it)
+                lw[U] = pack_f16(x0 * cs.x - y0 * cs.y, x1 * cs.z - y1 * cs.w);
+                hw[U] = pack_f16(x0 * cs.y + y0 * cs.x, x1 * cs.w + y1 * cs.z);
+            };
+            pair(std::integral_constant<int, 0>{}); pair(std::integral_constant<int, 1>{}); pair(std::integral_constant<int, 2>{}); pair(std::integral_constant<int, 3>{});
+        }
+        *reinterpret_cast<uint4 *>(dst) = lo;
+        *reinterpret_cast<uint4 *>(dst + 64) = hi;
+        // The largest squared norm of the tile's keys (see pc_gather_kernel).  Eight lanes hold a row.
+        ss += __shfl_xor(ss, 1); ss += __shfl_xor(ss, 2); ss += __shfl_xor(ss, 4);
+        ss = fmaxf(ss, __shfl_xor(ss, 8)); ss = fmaxf(ss, __shfl_xor(ss, 16)); ss = fmaxf(ss, __shfl_xor(ss, 32));
+        if ((threadIdx.x & 63) == 0) s_norm[threadIdx.x >> 6] = ss;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+        L.kg_norm[(int64_t)kh * (L.kg_slots / PC_TILE) + G] = fmaxf(fmaxf(s_norm[0], s_norm[1]), fmaxf(s_norm[2], s_norm[3]));
+#pragma unroll
+    for (int rep = 0; rep < 2; ++rep) {
+        const int idx = threadIdx.x + 256 * rep;
+        const int q = idx >> 7, d = idx & 127;             // (q is the same for all lanes of a wave)
+        auto word_of = [&](int slot) { return *reinterpret_cast<const uint32_t *>(vs + (int64_t)(slot / PC_TILE) * PC_MX4_TILE + slot % PC_TILE / 8 * 512 + mx4_word(d) * 4); };
+        auto exps_of = [&](int slot) { return *reinterpret_cast<const uint64_t *>(vs + (int64_t)(slot / PC_TILE) * PC_MX4_TILE + PC_MX4_CODES + slot % PC_TILE / 8 * 32 + d / 32 * 8); };
+        int sl[PC_VGROUP];
+        bool run = true;                                   // the group's 8 tokens sit in 8 consecutive slots of the cache
+#pragma unroll
+        for (int k = 0; k < PC_VGROUP; ++k) {
+            sl[k] = s_slot[PC_VGROUP * q + k];
+            run = run && sl[0] >= 0 && sl[k] == sl[0] + k;
+        }
+        uint32_t w = 0;
+        uint64_t ex = 0;
+        if (run) {                                         // of two groups of the cache
+            const int sh = sl[0] & 7;
+            w = word_of(sl[0]) >> 4 * sh;
+            ex = exps_of(sl[0]) >> 8 * sh;
+            if (sh > 0) {
+                w |= word_of(sl[7]) << (32 - 4 * sh);
+                ex |= exps_of(sl[7]) << (64 - 8 * sh);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < PC_VGROUP; ++k)
+                if (sl[k] >= 0) {
+                    w |= (word_of(sl[k]) >> 4 * (sl[k] & 7) & 15u) << 4 * k;
+                    ex |= (exps_of(sl[k]) >> 8 * (sl[k] & 7) & 255u) << 8 * k;
+                }
+        }
+        const uint32_t e0 = (uint32_t)ex, e1 = (uint32_t)(ex >> 32);
+        uint4 x;
+        x.x = mx4_values(w, e0, std::integral_constant<int, 0>{}); x.y = mx4_values(w, e0, std::integral_constant<int, 1>{});
+        x.z = mx4_values(w, e1, std::integral_constant<int, 2>{}); x.w = mx4_values(w, e1, std::integral_constant<int, 3>{});
+        *reinterpret_cast<uint4 *>((uint16_t *)L.v_gather + (((int64_t)kh * L.kg_slots + (int64_t)G * PC_TILE) / PC_VGROUP + q) * PC_D * PC_VGROUP + (int64_t)d * PC_VGROUP) = x;
+    }
+}
+
+void pc_launch_gather_mx4(const PcLaunch &L, const PcGatherItem *items, int n_items, int64_t n_tiles, const int32_t *seg_kvoff, uint32_t *mark, uint32_t value, hipStream_t st)
+{
+    if (n_items > 0 && n_tiles > 0) pc_mx4_gather_kernel<<<dim3((unsigned)n_tiles, (unsigned)L.n_kv_heads), 256, 0, st>>>(L, items, n_items, seg_kvoff, mark, value);
 }

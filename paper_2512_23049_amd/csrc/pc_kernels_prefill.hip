@@ -104,13 +104,29 @@ __device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "m
 
 template <int I> using IC = std::integral_constant<int, I>;
 
+// The product of the scores: bf16, or fp16 (keys of a 4-bit cache, turned, and queries: 11 bits where bf16 has 8, at the same rate).
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+template <bool F16> __device__ __forceinline__ f32x16 score32(bf16x8 k, bf16x8 q, f32x16 c)
+{
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, k), __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
+    else return MFMA32(k, q, c);
+}
+template <bool F16> __device__ __forceinline__ uint32_t pack_query(float a, float b)
+{
+    if constexpr (F16) return pack_f16(a, b);
+    else return pack_bf16(a, b);
+}
+
 // PACKED: the call's keys and values were copied by the gather pass into a buffer of their own, token after token in
 // the order the call lists them (keys already turned to the positions the call gives them), the parents' part padded
 // to whole tiles, then the new message.  Tile t of the call then sits at slot 32 t of that copy, only the last tile
 // of each part can be ragged, the queries are turned once by their own position, and nothing has to be looked up per
 // tile: no tile table, no rotation tables, no fp32 copy of the queries.
-template <bool PACKED>
-__global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L)
+// F16 (with PACKED): the copy's keys are fp16, and so are the queries here: both hold what there is of magnitudes that matter, and where a row's
+// query does not fit, the call is marked (R) for the walk behind this one, which takes any.
+struct PcRange { uint32_t *mark; uint32_t value; };
+template <bool PACKED, bool F16>
+__global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcRange range)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char s_k[RING][TILE_BYTES];
     __shared__ __attribute__((aligned(1024))) unsigned char s_v[RING][TILE_BYTES];
@@ -171,8 +187,8 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L)
                 yy[j] = x * cs.y + y * cs.x;
                 ss += xx[j] * xx[j] + yy[j] * yy[j];
             }
-            qop[ks] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(xx[0], xx[1]), pack_bf16(xx[2], xx[3]), pack_bf16(xx[4], xx[5]), pack_bf16(xx[6], xx[7])));
-            qop[ks + 4] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(yy[0], yy[1]), pack_bf16(yy[2], yy[3]), pack_bf16(yy[4], yy[5]), pack_bf16(yy[6], yy[7])));
+            qop[ks] = __builtin_bit_cast(bf16x8, make_uint4(pack_query<F16>(xx[0], xx[1]), pack_query<F16>(xx[2], xx[3]), pack_query<F16>(xx[4], xx[5]), pack_query<F16>(xx[6], xx[7])));
+            qop[ks + 4] = __builtin_bit_cast(bf16x8, make_uint4(pack_query<F16>(yy[0], yy[1]), pack_query<F16>(yy[2], yy[3]), pack_query<F16>(yy[4], yy[5]), pack_query<F16>(yy[6], yy[7])));
         }
         ss = sum_across_halves(ss);                      // the row's squared norm, then the largest of the wave's 32 rows
 #pragma unroll
@@ -456,7 +472,7 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L)
         ps = 0.f;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-            sn = MFMA32(fr[ks], qop[ks], sn);
+            sn = score32<F16>(fr[ks], qop[ks], sn);
             fr[ks] = vfrag(v_slot, ks);
             if (ks == 1) between();
 #pragma unroll
@@ -575,6 +591,9 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L)
 #pragma unroll
             for (int w8 = 1; w8 < 8; ++w8) kn2 = __builtin_fmaxf(kn2, s_red[w8]);
             bounded = qn2 * kn2 * 1.05f <= LAZY_LOG2 * LAZY_LOG2;
+            // (a query of norm 2^10 at most: its values fit, and what keys below fp16's normal numbers are off by, 2^-25, moves a
+            // score by no more than 2^-25 x 2^10 x sqrt(128))
+            if (F16 && qn2 > 0x1p20f && lane == 0) *range.mark = range.value;
         }
 
         // tile 0: scores and softmax part 1, nothing to overlap with yet; leaves the K fragments
@@ -587,7 +606,7 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L)
         for (int r = 0; r < 16; ++r) sc[r] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-            sc = MFMA32(fr[ks], qop[ks], sc);
+            sc = score32<F16>(fr[ks], qop[ks], sc);
             fr[ks] = kfrag(1, ks);
         }
         if constexpr (!PACKED) { if (d1.fresh()) turn_query(1); }   // (from tile 2 on the queries are turned at the end of an iteration)
@@ -685,7 +704,7 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sn[r] = 0.f;
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) sn = MFMA32(fr[ks], qop[ks], sn);       // scores of tile i+1
+                for (int ks = 0; ks < 8; ++ks) sn = score32<F16>(fr[ks], qop[ks], sn);       // scores of tile i+1
 #pragma unroll
                 for (int f = 0; f < 8; ++f) fr[f] = vfrag(s0, f);
                 dma_v(dsc(tile0 + i + 4), s4);           // V(i+4) takes the slot of V(i-1)
@@ -816,6 +835,11 @@ void pc_launch_prefill_bf16(const PcLaunch &L, int n_items, bool packed, hipStre
 {
     if (n_items <= 0) return;
     dim3 grid((unsigned)n_items * L.n_kv_heads);
-    if (packed) pc_prefill_bf16_kernel<true><<<grid, 512, 0, st>>>(L);
-    else pc_prefill_bf16_kernel<false><<<grid, 512, 0, st>>>(L);
+    if (packed) pc_prefill_bf16_kernel<true, false><<<grid, 512, 0, st>>>(L, PcRange{});
+    else pc_prefill_bf16_kernel<false, false><<<grid, 512, 0, st>>>(L, PcRange{});
+}
+
+void pc_launch_prefill_f16(const PcLaunch &L, int n_items, uint32_t *mark, uint32_t value, hipStream_t st)
+{
+    if (n_items > 0) pc_prefill_bf16_kernel<true, true><<<(unsigned)n_items * L.n_kv_heads, 512, 0, st>>>(L, PcRange{mark, value});
 }

@@ -39,6 +39,8 @@ struct PcMx4Prepare {
     const void   *v_store;
     void         *v_to;               // [n_kv_heads][4 n_tiles][128][8]: the tiles' values as a bf16 cache has them
     int32_t       list_blocks, query_blocks;          // of the grid
+    const uint32_t *mark;             // null, or: nothing is done unless *mark is mark_value
+    uint32_t      mark_value;
 };
 void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st);
 // What the attention of rows needs besides PcWin (whose v_store and rot_q are not read).
@@ -49,6 +51,8 @@ struct PcMx4Rows {
     const void    *v_tiles;
     int64_t        v_slots;
     int32_t        n_rows;
+    uint32_t       mark_value;        // as in PcMx4Prepare
+    const uint32_t *mark;
 };
 void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, hipStream_t st);
 

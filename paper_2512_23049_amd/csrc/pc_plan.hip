@@ -746,7 +746,7 @@ static int own_tiles_of(const Resolved &r) { return r.self_msg >= 0 ? (r.self_le
 // workspace, which the copy may not fit into.)
 static bool gathers(const pc_cache *c, const Planned &P, const Resolved &r)
 {
-    return r.tiles > 0 && !P.fixed_ws && (c->key_gather == 2 || (c->key_gather == 0 && (int64_t)r.n_q * c->cfg.n_q_heads >= 32768));
+    return P.mx4_rows || (r.tiles > 0 && !P.fixed_ws && (c->key_gather == 2 || (c->key_gather == 0 && (int64_t)r.n_q * c->cfg.n_q_heads >= 32768)));
 }
 // Tiles the prefill kernel walks for a call: those of the copy, or those of the cache
 static int walked_tiles(const pc_cache *c, const Planned &P, const Resolved &r)
@@ -1156,7 +1156,7 @@ int32_t pc_plan_and_stage(pc_cache *c, const pc_call *calls, int32_t n_calls, bo
         P.total_q += P.res[i].n_q;
     }
     const int g = c->g, H_kv = c->cfg.n_kv_heads;
-    const bool bf16 = c->cfg.dtype == PC_BF16;
+    const bool bf16 = c->cfg.dtype == PC_BF16 || P.mx4_rows;
     // work-group shape of the prefill kernel: 8 row units (32 rows x 1 q head each) per group
     P.pre_waves = 8;
     std::vector<PcCallDesc> cds((size_t)n_calls);

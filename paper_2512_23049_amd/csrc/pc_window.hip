@@ -191,12 +191,18 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     //   32 heads over 8: 16 calls 155 and 147, 32 294 and 162; of 24 messages 32 calls 49 and 45;
     //   128 over 8: 12 calls 119 and 136, 16 156 and 153, 24 242 and 260, 32 291 and 267;
     //   16 over 2 (the host's time): 16 calls 66 and 93, 32 111 and 158, 64 203 and 305; 64 calls over 16 messages of 640 tokens 62 and 59.
+    // 4 bits: a call's own tiles cost a quarter, a shared one what its waves need for it (call by call and shared, of 410 of 512 messages: 64 heads
+    // over 8, 8 calls 112 and 154, 16 200 and 177, 32 365 and 268, 64 680 and 540; of 24 messages 16 calls 29 and 44, 64 calls 53 and 57; 64 calls
+    // over 32 of 64 messages of 400 tokens 128 and 108, 16 calls 49 and 79; a message of 2048 tokens and 8 of 512, 16 calls 31 and 88, 64 calls 57 and 205).
     // By the caller's word: pc_set_decode_sharing.
     int64_t own = 0, listed = 0, shared = 0;
     for (const Group &gr : dec) { own += gr.tiles; listed += (int64_t)P.calls[(size_t)gr.call].n_seg; }
-    const double heads = H / 8.0, host = 12 + 0.007 * (double)listed, planned = host + 0.015 * (double)(P.runs.size() - (size_t)dec[0].run0);
-    const double alone = std::max(8 + 0.0175 * (double)own * heads, host);
-    auto together = [&](int64_t tiles) { return std::max(48 + (0.0227 * (double)tiles + 0.0055 * (double)own) * heads, planned); };
+    const bool mx4 = c->cfg.dtype == PC_MX4;
+    const double heads = H / 8.0, host = 12 + (mx4 ? 0.009 : 0.007) * (double)listed, planned = host + (mx4 ? 0.01 : 0.015) * (double)(P.runs.size() - (size_t)dec[0].run0);
+    const double alone = std::max(mx4 ? 20 + 0.0047 * (double)own * heads : 8 + 0.0175 * (double)own * heads, host);
+    auto together = [&](int64_t tiles) {
+        return std::max(mx4 ? 36 + (0.047 * (double)tiles + 0.0008 * (double)own) * heads : 48 + (0.0227 * (double)tiles + 0.0055 * (double)own) * heads, planned);
+    };
     if (c->decode_sharing == 0 && alone <= together(own / set_calls)) return false;
     struct Piece { int32_t slot0, tiles; uint32_t run; int32_t call; };
     std::vector<Piece> pieces, scratch;
@@ -632,8 +638,9 @@ int32_t check(pc_cache *c, const char *what, const pc_call *calls, int32_t n_cal
     return PC_OK;
 }
 
+// mark: 0, or: nothing is done unless the cache's mark is that (PC_MX4, calls of many rows)
 int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out,
-                      float *lse, hipStream_t st, void *fixed_ws)
+                      float *lse, hipStream_t st, void *fixed_ws, uint32_t mark = 0)
 {
     int32_t rc = check(c, what, calls, n_calls, window, n_sink);
     if (rc != PC_OK || n_calls == 0) return rc;
@@ -649,7 +656,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     const bool recorded = pc_recorded(st);
     if (recorded && !fixed_ws)
         return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move: use pc_attend_window_static", what);
-    plan_items(c, P, true);
+    plan_items(c, P, mark == 0);                         // (marked: no splits, and with them no merge)
     WinLayout L = lay_out(c, P);
     // Lists of single tokens that their launch's arguments do not hold cost a launch in front of it and the event behind that, 7 us: a few
     // longer splits are better where that helps (4 calls of 130 tiles: 22.5 -> 16.5 us; 16 of 17: 19 -> 12).
@@ -717,6 +724,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
             T.rot_run = (float2 *)(ws + L.rot_run);
             T.q = q; T.q_abs = (float4 *)(ws + L.q_abs); T.q_unit = (float *)(ws + L.q_unit);
             T.inv_freq = c->inv_freq_dev; T.slots = c->slots; T.v_store = c->v_store; T.v_to = ws + L.v_tiles;
+            if (mark) { T.mark = c->counters_dev + 2 * PC_ONE_COUNTERS; T.mark_value = mark; }
             pc_launch_mx4_prepare(T, in_args ? &blob : nullptr, st);
         } else {
         PcWinTurns T{};
@@ -754,7 +762,8 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     if (!P.pre.empty()) {
         ProfScope ps(c, bf16 ? 2 : 5, st);
         W.items = (const PcWinItem *)(ws + L.pre);
-        const PcMx4Rows M{(const float4 *)(ws + L.q_abs), (const float *)(ws + L.q_unit), (const int32_t *)(ws + L.places), ws + L.v_tiles, (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size()};
+        const PcMx4Rows M{(const float4 *)(ws + L.q_abs), (const float *)(ws + L.q_unit), (const int32_t *)(ws + L.places), ws + L.v_tiles,
+                          (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size(), mark, mark ? c->counters_dev + 2 * PC_ONE_COUNTERS : nullptr};
         if (mx4) pc_launch_win_prefill_mx4(W, M, (int)P.pre.size(), st);
         else if (bf16) pc_launch_win_prefill_bf16(W, (int)P.pre.size(), st);
         else pc_launch_win_attend_f32(W, (int)P.pre.size(), c->D, st);
@@ -900,9 +909,58 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
 }  // namespace
 
 // What a call lists is all in a window of 2^31 - 1 (positions are below 2^30 in magnitude: pc_cache_create).
+//
+// Long prefills go over a packed copy, as in a bf16 cache: there a message's turn costs its keys once, and not every row and head once a
+// message.  The copy's keys and the queries are fp16 for the matrix instructions, whose range keys and queries of models are in; where one is not, the
+// device marks the call, and the walk over the cache itself, which takes any, follows and does nothing otherwise.
+// Taken from rows x heads x listed tokens of LONG_PREFILL on.
+constexpr double LONG_PREFILL = 1.2e8;
 int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws)
 {
-    return attend_window(c, what, calls, n_calls, INT32_MAX, 0, q, out, lse, st, fixed_ws);
+    auto in_place = [&](int32_t first, int32_t n, int64_t row, uint32_t mark) {
+        const int64_t at = row * c->cfg.n_q_heads;
+        return attend_window(c, what, calls + first, n, INT32_MAX, 0, q ? (const uint16_t *)q + at * c->D : nullptr, out ? (uint16_t *)out + at * c->D : nullptr,
+                             lse ? lse + at : nullptr, st, fixed_ws, mark);
+    };
+    auto is_long = [&](const pc_call &call) {
+        if (fixed_ws || c->host_only || call.n_q * (int64_t)c->g <= 16 || call.n_sel < 0 || (call.n_sel > 0 && !call.sel)) return false;
+        double tokens = 0;
+        auto add = [&](int32_t m) { if (known(c, m)) tokens += chain_len(c, m); };
+        for (int32_t e = 0; e < call.n_sel; ++e) add(call.sel[e].msg_id);
+        add(call.self_msg);
+        return tokens > 0 && tokens < 1e8 && tokens * call.n_q * c->cfg.n_q_heads >= LONG_PREFILL;
+    };
+    bool some = false;
+    for (int32_t i = 0; i < n_calls && calls; ++i) some |= calls[i].n_q > 1 && is_long(calls[i]);
+    if (!some) return in_place(0, n_calls, 0, 0);
+    // (runs of calls of a kind follow each other: nothing may be refused behind the first)
+    if ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
+    if (pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move", what);
+    {
+        WinPlan P;
+        const int32_t rc = resolve_all(c, calls, n_calls, P);
+        if (rc != PC_OK) return rc;
+    }
+    PcDeviceScope on(c);
+    if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
+    int64_t row = 0;
+    for (int32_t a = 0; a < n_calls;) {
+        const bool kind = is_long(calls[a]);
+        int32_t b = a;
+        int64_t rows = 0;
+        for (; b < n_calls && is_long(calls[b]) == kind; ++b) rows += calls[b].n_q;
+        int32_t rc = PC_OK;
+        if (kind) {
+            if (++c->mark_epoch_mx4 == 0) c->mark_epoch_mx4 = 1;
+            const int64_t at = row * c->cfg.n_q_heads;
+            rc = pc_attend_gathered_mx4(c, calls + a, b - a, (const uint16_t *)q + at * c->D, (uint16_t *)out + at * c->D, lse ? lse + at : nullptr, st, c->mark_epoch_mx4);
+        }
+        if (rc == PC_OK) rc = in_place(a, b - a, row, kind ? c->mark_epoch_mx4 : 0);
+        if (rc != PC_OK) return rc;
+        row += rows;
+        a = b;
+    }
+    return PC_OK;
 }
 
 extern "C" {

@@ -99,6 +99,54 @@ def test_large_scores_and_powers():
     layer.cache.close()
 
 
+@pytest.mark.parametrize("spoilt", ["", "keys", "query", "no number"])
+def test_many_rows_over_long_lists(spoilt):
+    """Calls of 1.3e8 scores among short ones, with a message twice, one of a single token, parts of messages grown and placed at odd positions; and keys
+    and queries outside what 16 bits hold, or none at all, which any call may have."""
+
+    def spoil(i, k, v):
+        if spoilt == "keys" and i == 1:
+            k[5] *= 1e6
+        if spoilt == "no number" and i == 1:
+            v[5, 0, 3] = np.nan
+    lens = [1900, 33, 2500, 1, 1030, 70, 1100, 1099, 40]
+    layer = Layer4(lens, 16, 2, spoil=spoil)
+    long = [(0, 0), (4, 2000), (2, 3007), (3, 9000), (5, 5600), (0, 5700)]
+    calls = [([(0, 3)], 8, 1950, 40), (long, 6, 8000, 1100), (long[:3], -1, 7000, 1), (long + [(1, -70)], 7, 8100, 1000), (long, 7, 8000, 1001), ([], 8, 0, 1)]
+    q = layer.normal(sum(c[3] for c in calls), 16, 128)
+    if spoilt == "query":
+        q[40 + 1100 + 1 + 7] *= 3e4
+    if spoilt in ("keys", "query"):
+        out, lse = layer.attend(calls, q)
+        want, want_lse = layer.want(calls, q)
+        # rows that see a large key, or are large: one key takes all, or two near each other do; a score is off by 2^-8 |q| |k| / sqrt(128)
+        far = np.abs(want_lse) > 60
+        assert far.any() and (far.sum(axis=1) == 0).sum() > 2000
+        rows = ~far.any(axis=1)
+        same(out[rows], lse[rows], want[rows], want_lse[rows], spoilt)
+        assert out.isfinite().all()
+        top = 1e6 * 20 if spoilt == "keys" else 20.0
+        norm = np.linalg.norm(q, axis=-1)
+        assert (np.abs(lse.double().cpu().numpy() - want_lse)[far] <= (2.0 ** -8 + 1e-6) * (norm * top / np.sqrt(128))[far] + 1e-3).all()
+        # where the large key's score is below all others it is not seen; it comes within its own error of them, 2^-8 x 11 deviations, in 4 rows of 100
+        off = np.abs(out.double().cpu().numpy() - want).max(axis=-1)[~far] > 4e-2
+        assert off.mean() < 0.05
+        return
+    if spoilt:
+        out, lse = layer.attend(calls, q)
+        rows = np.zeros(len(q), bool)
+        rows[1141:2141] = True                           # (the call that lists it)
+        assert out[rows][:, :8].isnan().all() and out[rows][:, 8:].isfinite().all()
+        layer.ks[1][np.isnan(layer.ks[1])] = 0
+        layer.vs[1][np.isnan(layer.vs[1])] = 0
+        want, want_lse = layer.want(calls, q)
+        same(out[~rows], lse[~rows], want[~rows], want_lse[~rows], "the others")
+        same(out[rows][:, 8:], lse[rows][:, 8:], want[rows][:, 8:], want_lse[rows][:, 8:], "the other head")
+        return
+    layer.run(calls, q=q)
+    layer.cache.close()
+
+
 @pytest.mark.parametrize("n_q", [1, 5, 40])
 def test_tokens_that_are_no_numbers(n_q):
     """Rows that see one are NaN in that head's query heads; what others do not see does not touch them."""
