@@ -913,8 +913,13 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
 // Long prefills go over a packed copy, as in a bf16 cache: there a message's turn costs its keys once, and not every row and head once a
 // message.  The copy's keys and the queries are fp16 for the matrix instructions, whose range keys and queries of models are in; where one is not, the
 // device marks the call, and the walk over the cache itself, which takes any, follows and does nothing otherwise.
-// Taken from rows x heads x listed tokens of LONG_PREFILL on.
-constexpr double LONG_PREFILL = 1.2e8;
+// Taken by calls of LONG_ROWS rows x query heads of a KV head (each copied token is read that often), where those that stand together have
+// LONG_SCORES scores in all (two more launches are to be earned back).  In place and copied, us: 8 calls of 64 rows over 12064 tokens, 64 heads on 8: 337, 311; 32 on
+// 8 (256): 185, 250; one call of 256 rows over 2256 tokens, 64 heads (3.7e7): 64, 62; 32 heads (1.85e7): 53, 56; 8 calls of it: 152, 113;
+// of 1024 rows over 13024 tokens, 64 heads: 5227, 2848.
+constexpr int64_t LONG_ROWS = 512;
+constexpr double LONG_SCORES = 3e7;
+constexpr int64_t LONG_TOKENS = (int64_t)1 << 22;        // a copy's, where it has more calls than one: 16 GiB of 8 KV heads
 int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws)
 {
     auto in_place = [&](int32_t first, int32_t n, int64_t row, uint32_t mark) {
@@ -922,16 +927,30 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
         return attend_window(c, what, calls + first, n, INT32_MAX, 0, q ? (const uint16_t *)q + at * c->D : nullptr, out ? (uint16_t *)out + at * c->D : nullptr,
                              lse ? lse + at : nullptr, st, fixed_ws, mark);
     };
-    auto is_long = [&](const pc_call &call) {
-        if (fixed_ws || c->host_only || call.n_q * (int64_t)c->g <= 16 || call.n_sel < 0 || (call.n_sel > 0 && !call.sel)) return false;
-        double tokens = 0;
+    // tokens that a call lists, if it is long
+    auto long_tokens = [&](const pc_call &call) -> int64_t {
+        if (fixed_ws || c->host_only || call.n_q <= 1 || call.n_q * (int64_t)c->g < LONG_ROWS || call.n_sel < 0 || (call.n_sel > 0 && !call.sel)) return 0;
+        int64_t tokens = 0;
         auto add = [&](int32_t m) { if (known(c, m)) tokens += chain_len(c, m); };
         for (int32_t e = 0; e < call.n_sel; ++e) add(call.sel[e].msg_id);
         add(call.self_msg);
-        return tokens > 0 && tokens < 1e8 && tokens * call.n_q * c->cfg.n_q_heads >= LONG_PREFILL;
+        return tokens < 100000000 ? tokens : 0;
     };
+    std::vector<int64_t> tokens((size_t)std::max(n_calls, 0));
+    for (int32_t i = 0; i < n_calls && calls; ++i) tokens[(size_t)i] = long_tokens(calls[i]);
+    // runs of long calls; each ends the launches that the calls before and behind it would share: several have to earn more
+    int runs = 0;
+    for (size_t i = 0; i < tokens.size(); ++i) runs += tokens[i] > 0 && (i == 0 || tokens[i - 1] == 0);
     bool some = false;
-    for (int32_t i = 0; i < n_calls && calls; ++i) some |= calls[i].n_q > 1 && is_long(calls[i]);
+    for (size_t i = 0; i < tokens.size();) {
+        size_t e = i;
+        double scores = 0;
+        for (; e < tokens.size() && tokens[e] > 0; ++e) scores += (double)tokens[e] * calls[e].n_q * c->cfg.n_q_heads;
+        const bool kept = scores >= (runs > 1 ? 4 : 1) * LONG_SCORES;
+        some |= kept;
+        if (!kept) std::fill(tokens.begin() + (ptrdiff_t)i, tokens.begin() + (ptrdiff_t)e, 0);
+        i = std::max(e, i + 1);
+    }
     if (!some) return in_place(0, n_calls, 0, 0);
     // (runs of calls of a kind follow each other: nothing may be refused behind the first)
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
@@ -945,10 +964,13 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
     if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
     int64_t row = 0;
     for (int32_t a = 0; a < n_calls;) {
-        const bool kind = is_long(calls[a]);
+        const bool kind = tokens[(size_t)a] > 0;
         int32_t b = a;
-        int64_t rows = 0;
-        for (; b < n_calls && is_long(calls[b]) == kind; ++b) rows += calls[b].n_q;
+        int64_t rows = 0, copied = 0;
+        for (; b < n_calls && (tokens[(size_t)b] > 0) == kind && (b == a || copied + tokens[(size_t)b] <= LONG_TOKENS); ++b) {
+            rows += calls[b].n_q;
+            copied += tokens[(size_t)b];
+        }
         int32_t rc = PC_OK;
         if (kind) {
             if (++c->mark_epoch_mx4 == 0) c->mark_epoch_mx4 = 1;

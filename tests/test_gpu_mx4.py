@@ -289,6 +289,31 @@ def test_growth_forks_moves_and_swaps():
     layer.cache.close()
 
 
+def test_many_rows_over_grown_and_forked_messages():
+    """Rows of a long prefill over a message of several extents, one that grew in its last tile, forks from their middles on, and behind a compaction."""
+    from paper_2512_23049_amd import binding as b
+    layer = Layer4([1500, 70, 45, 512], 32, 2, reserves=[1500, 70, 64, 512], flags=b.PC_FLAG_GROW_EXTENTS, room=3000)
+    for n in (9, 1, 40):
+        for m in (1, 2):
+            k, v = layer.normal(n, 2, 128), layer.normal(n, 2, 128)
+            tk, tv = layer.dev(k), layer.dev(v)
+            layer.cache.append_tokens(layer.ids[m], tk.data_ptr(), tv.data_ptr(), n)
+            layer.torch.cuda.synchronize()
+            layer.grow(m, k, v)
+    assert len(layer.cache.message_extents(layer.ids[1])) > 1
+    for m, first, n in [(0, 333, 777), (1, 65, 50)]:
+        layer.ids += layer.cache.message_fork([(layer.ids[m], first, n, n, None)])
+        layer.raw.append(tuple(x[first:first + n] for x in layer.raw[m]))
+        layer.ks.append(layer.ks[m][first:first + n].copy())
+        layer.vs.append(layer.vs[m][first:first + n].copy())
+    sel = [(1, 5), (0, 100), (4, 1500), (5, 2300), (2, 2301)]
+    layer.run([(sel, 3, 2500, 500), ([(0, 0)], -1, 1500, 2), (sel[::-1], 3, 2600, 512), (sel[1:], 3, 2000, 1)], what="grown")
+    layer.cache.message_free(layer.ids[4])
+    assert layer.cache.compact() > 0
+    layer.run([(sel[:2] + sel[3:], 3, 2500, 512), (sel[:2] + [(0, 1700)], 3, 2500, 511)], what="closed up")
+    layer.cache.close()
+
+
 def test_many_moves():
     """Closing up over many messages, in steps and at once: chunks of tiles that do not end with a message."""
     rng = np.random.default_rng(1)
