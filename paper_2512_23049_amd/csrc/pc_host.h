@@ -166,6 +166,11 @@ struct Resolved {
     int32_t tiles = 0;            // KV tiles incl. the new message
 };
 
+// Lists that a thread keeps from one call to the next (fresh pages for them cost more than filling them) are given back when a batch made them
+// longer than KEPT_BYTES each.
+constexpr size_t KEPT_BYTES = (size_t)4 << 20;
+template <typename T> void keep(std::vector<T> &v) { if (v.capacity() * sizeof(T) > KEPT_BYTES) std::vector<T>().swap(v); }
+
 inline bool known(const pc_cache *c, int32_t m)
 {
     return m >= 0 && m < (int32_t)c->msgs.size() && c->msgs[(size_t)m].live && !c->msgs[(size_t)m].is_ext;

@@ -219,10 +219,6 @@ constexpr size_t UNION_ENTRIES = (size_t)1 << 19;
 // rows with more splits than this are merged by four lanes per 8 dimensions
 constexpr int MERGE_MANY_SPLITS = 8;
 
-// Lists that a thread keeps from one call to the next (fresh pages for them cost more than filling them) are given back when a batch made them
-// longer than KEPT_BYTES each.
-constexpr size_t KEPT_BYTES = (size_t)4 << 20;
-template <typename T> static void keep(std::vector<T> &v) { if (v.capacity() * sizeof(T) > KEPT_BYTES) std::vector<T>().swap(v); }
 
 // The union of the lists of some one-row calls: which messages there are, who lists each, and where.
 struct Union {

@@ -40,6 +40,27 @@ struct WinPlan {
     std::vector<PcWinSee> sh_sees;
     std::vector<PcWinSharedCall> sh_calls;
     bool sh_wide = false;
+
+    void clear()
+    {
+        each([](auto &v) { v.clear(); });
+        part_rows = part_first = 0;
+        sh_wide = false;
+    }
+    // what is not worth keeping from one call to the next
+    void trim()
+    {
+        size_t held = 0;
+        for (const Resolved &r : res) held += sizeof(Resolved) + 8 * (r.sel.capacity() + r.entry_start.capacity()) + 4 * r.q_pos.capacity();
+        if (held > KEPT_BYTES) std::vector<Resolved>().swap(res);
+        each([](auto &v) { keep(v); });
+    }
+
+private:
+    template <typename F> void each(F &&f)               // (not res: its lists are written over)
+    {
+        f(calls); f(segs); f(q_pos); f(pre); f(dec); f(runs); f(run_seg); f(rots); f(merge); f(tiles); f(places); f(sh_items); f(sh_visits); f(sh_sees); f(sh_calls);
+    }
 };
 
 int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan &P)
@@ -205,11 +226,30 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     };
     if (c->decode_sharing == 0 && alone <= together(own / set_calls)) return false;
     struct Piece { int32_t slot0, tiles; uint32_t run; int32_t call; };
-    std::vector<Piece> pieces, scratch;
+    struct Visit { int32_t slot0, tiles; size_t p0, p1; };           // a range of consecutive tiles, and the pieces of it
+    struct Seen { int32_t call; uint32_t seg; };                     // (call: within the set)
+    struct Caller { int32_t q_pos, low, group, sub; };               // a call's place among the columns of its set
+    struct Lists {
+        std::vector<Piece> pieces, scratch;
+        std::vector<uint32_t> digits;
+        std::vector<std::pair<size_t, size_t>> of_set;   // a set's pieces, in slot order
+        std::vector<Seen> seen;                          // who sees the visit at hand, and from which entry of its list; its views: P.sh_sees from e0 on
+        std::vector<Visit> visits;
+        std::vector<Caller> callers;
+    };
+    static thread_local Lists kept;
+    struct Kept { ~Kept() { keep(kept.pieces); keep(kept.scratch); keep(kept.of_set); keep(kept.seen); keep(kept.visits); } } trim;
+    auto &pieces = kept.pieces, &scratch = kept.scratch;
+    auto &digits = kept.digits;
+    auto &of_set = kept.of_set;
+    auto &seen = kept.seen;
+    auto &visits = kept.visits;
+    auto &callers = kept.callers;
+    pieces.clear(); of_set.clear();
     pieces.reserve(P.runs.size() - (size_t)dec[0].run0);
     // pieces [first, size) by their slots, in the calls' order where those are the same: a pass for 13 bits of a tile's number
     constexpr uint32_t DIGIT = 13;
-    std::vector<uint32_t> digits(1u << DIGIT);
+    digits.resize(1u << DIGIT);
     auto by_slot = [&](std::vector<Piece> &v, size_t first, std::vector<Piece> &other) {
         uint32_t most = 0;
         for (size_t k = first; k < v.size(); ++k) most = std::max(most, (uint32_t)v[k].slot0 / PC_TILE);
@@ -224,7 +264,6 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
             std::memcpy(v.data() + first, other.data() + first, sizeof(Piece) * (v.size() - first));
         }
     };
-    std::vector<std::pair<size_t, size_t>> of_set;       // a set's pieces, in slot order
     for (int32_t s = 0; s < n_sets; ++s) {
         const size_t first = pieces.size();
         for (int32_t j = s * set_calls; j < std::min(n_calls, (s + 1) * set_calls); ++j) {
@@ -245,8 +284,6 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     }
     const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
     if (shared == 0 || (c->decode_sharing == 0 && alone <= together(shared))) return false;
-    struct Seen { int32_t call; uint32_t seg; };                     // (call: within the set)
-    std::vector<Seen> seen;                              // who sees the visit at hand, and from which entry of its list; its views: P.sh_sees from e0 on
     P.sh_sees.reserve(pieces.size() + pieces.size() / 4);
     for (int32_t s = 0; s < n_sets; ++s) {
         const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
@@ -254,8 +291,12 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
         while (waves < groups) waves *= 2;
         const int32_t reps = (wide ? 16 : 8) / waves;
         // ranges of consecutive tiles
-        struct Visit { int32_t slot0, tiles; size_t p0, p1; };
-        std::vector<Visit> visits;
+        visits.clear();
+        callers.clear();
+        for (int32_t j = 0; j < in_set; ++j) {
+            const int32_t q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)(call0 + j)].call].q_off];
+            callers.push_back(Caller{q_pos, win_low(q_pos, P.window), j / per, j % per});
+        }
         int64_t total = 0;
         for (size_t k = of_set[(size_t)s].first; k < of_set[(size_t)s].second;) {
             Visit v{pieces[k].slot0, 0, k, k};
@@ -278,12 +319,14 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                 seen.clear();
                 const size_t e0 = P.sh_sees.size();
                 for (size_t k = v.p0; k < v.p1; ++k) {
-                    const Piece &pc = pieces[k];
+                    const Piece pc = pieces[k];
+                    if (k + 12 < pieces.size()) __builtin_prefetch(&P.runs[pieces[k + 12].run]);     // (they lie in the calls' order)
                     if (pc.slot0 >= slot1 || pc.slot0 + PC_TILE * pc.tiles <= slot0) continue;
                     const PcWinRun &r = P.runs[pc.run];
                     const int32_t d = slot0 - r.slot0;   // (what lies in front of a run is left out by its window)
-                    const int32_t j = pc.call - call0, q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)pc.call].call].q_off];
-                    PcWinSee e{r.pos0 + d, r.n_tok - d, std::max(0, r.sink > 0 ? r.sink - d : 0), win_low(q_pos, P.window), (int64_t)q_pos - r.rot_pos, j % per, 0};
+                    const int32_t j = pc.call - call0;
+                    const Caller &from = callers[(size_t)j];
+                    const PcWinSee e{r.pos0 + d, r.n_tok - d, std::max(0, r.sink > 0 ? r.sink - d : 0), from.low, (int64_t)from.q_pos - r.rot_pos, from.sub, 0};
                     const uint32_t seg = (uint32_t)P.run_seg[pc.run];
                     if (seen.empty() || seen.back().call < j) {          // (in order, mostly)
                         seen.push_back(Seen{j, seg});
@@ -304,7 +347,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                 PcWinVisit pv{slot0, n, (int32_t)e0, {}};
                 size_t k = 0;
                 for (int32_t gr = 0; gr <= PC_WIN_GROUPS; ++gr) {
-                    while (k < seen.size() && seen[k].call / per < gr) ++k;
+                    while (k < seen.size() && callers[(size_t)seen[k].call].group < gr) ++k;
                     pv.off[gr] = (int32_t)k;
                 }
                 P.sh_visits.push_back(pv);
@@ -647,7 +690,9 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     if (!c->host_only && (!q || !out)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: null q or out", what);
     if (!c->host_only && ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)))
         return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
-    WinPlan P;
+    static thread_local WinPlan P;                       // (32 calls over 410 messages, 64 heads: 264 us a call with fresh lists, 256 with these)
+    struct Kept { ~Kept() { P.trim(); } } kept;
+    P.clear();
     P.window = window; P.n_sink = n_sink;
     rc = resolve_all(c, calls, n_calls, P);
     if (rc != PC_OK || c->host_only) return rc;
