@@ -277,22 +277,28 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
         return;
     }
     block -= P.list_blocks;
-    if (block < P.query_blocks) {                        // 32 rows, eight heads
-        const int chunks = (P.n_q_heads + 7) / 8;
+    if (block < P.query_blocks) {                        // 32 rows, a head a wave
+        const int chunks = (P.n_q_heads + 3) / 4;
         const int64_t group = block / chunks, groups = ((int64_t)P.n_rows + 31) / 32;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, hh = lane >> 5;
-        for (int e = threadIdx.x; e < 32 * (PC_D / 2); e += 256) {
-            const int64_t R = group * 32 + e % 32;
-            if (R < P.n_rows) s_rot[e / 32][e % 32] = rope_turn(reinterpret_cast<const int32_t *>(from + P.off_q_pos)[R], P.inv_freq[e / 32]);
-        }
-        __syncthreads();
         const int64_t R = group * 32 + n, row = R < P.n_rows ? R : P.n_rows - 1;
-#pragma unroll 1
-        for (int h = block % chunks * 8 + wave; h < min(P.n_q_heads, block % chunks * 8 + 8); h += 4) {
+        const int h = block % chunks * 4 + wave;
+        uint4 raw[8];                                    // dims 16 hh, 32 + 16 hh, and 64 up, 16 each (on their way while the rotations are made)
+        if (h < P.n_q_heads) {
             const unsigned char *qp = (const unsigned char *)P.q + (row * P.n_q_heads + h) * (PC_D * 2) + 32 * hh;
-            uint4 raw[8];                                // dims 16 hh, 32 + 16 hh, and 64 up, 16 each
 #pragma unroll
             for (int i = 0; i < 8; ++i) raw[i] = ldg16(qp + (i >> 1) * 64 + (i & 1) * 16);
+        }
+        {   // a frequency a lane, eight rows a wave
+            const double freq = P.inv_freq[lane];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int64_t r = group * 32 + wave * 8 + i;
+                if (r < P.n_rows) s_rot[lane][wave * 8 + i] = mx4_rotation((double)reinterpret_cast<const int32_t *>(from + P.off_q_pos)[r] * freq);
+            }
+        }
+        __syncthreads();
+        if (h < P.n_q_heads) {
             float top = 0.f;
             bool fine = true;
 #pragma unroll
@@ -345,7 +351,7 @@ __global__ __launch_bounds__(256) void pc_mx4_prepare_arg_kernel(PcArgBlob, PcMx
 void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st)
 {
     P.list_blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>((P.n16 + (int64_t)P.n_rot * (PC_D / 2) + 255) / 256, 1024));
-    P.query_blocks = (P.n_rows + 31) / 32 * ((P.n_q_heads + 7) / 8);
+    P.query_blocks = (P.n_rows + 31) / 32 * ((P.n_q_heads + 3) / 4);
     const unsigned grid = (unsigned)(P.list_blocks + P.query_blocks + P.n_tiles * P.n_kv_heads);
     if (blob) pc_mx4_prepare_arg_kernel<<<grid, 256, 0, st>>>(*blob, P);
     else pc_mx4_prepare_kernel<<<grid, 256, 0, st>>>(P);

@@ -51,24 +51,27 @@ __device__ __forceinline__ bf16x8 mx4_of_codes(uint32_t w)
                                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3)));
     return __builtin_bit_cast(bf16x8, u);
 }
-// Two slots of a dimension in bf16 (pair PAIR of the word's four), by their powers: 60 - exponent as bytes of d (pairs 0 and 1: of slots 0 to 3; 2 and 3: of 4 to 7).
-template <int PAIR> __device__ __forceinline__ uint32_t mx4_values(uint32_t w, uint32_t d, std::integral_constant<int, PAIR>)
-{
-    const auto x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, PAIR);
-    // (a slot behind a message's last token holds codes of zero, or another owner's: any finite power will do)
-    const uint32_t d0 = d >> 16 * (PAIR & 1) & 255u, d1 = d >> (16 * (PAIR & 1) + 8) & 255u;
-    return pack_bf16(x[0] * __uint_as_float((187u - min(d0, 120u)) << 23), x[1] * __uint_as_float((187u - min(d1, 120u)) << 23));
-}
 // bf16 x 2^(60 - d) for two probabilities: d as bytes 0 and 1 (or 2 and 3) of `d`; what would be below the least normal number is zero
 template <int PAIR> __device__ __forceinline__ uint32_t mx4_lowered(uint32_t p, uint32_t d)
 {
     const uint32_t e = __builtin_amdgcn_perm(0u, d, PAIR == 0 ? 0x010C000Cu : 0x030C020Cu) >> 1;
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(mx4_u16x2, p), __builtin_bit_cast(mx4_u16x2, e)));
 }
+// Two slots of a dimension in bf16 (pair PAIR of the word's four), by their powers: 60 - exponent as bytes of d (pairs 0 and 1: of slots 0 to 3; 2 and
+// 3: of 4 to 7).  (A slot behind a message's last token holds codes of zero, or another owner's: any number will do.)
+template <int PAIR> __device__ __forceinline__ uint32_t mx4_values(uint32_t w, uint32_t d, std::integral_constant<int, PAIR>)
+{
+    const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 0x1p60f, PAIR));
+    return mx4_lowered<PAIR & 1>(x & 0x7FFF7FFFu, d) | (x & 0x80008000u);
+}
 
 // (cos, sin) of a turn: positions are below 2^30 and theta is at least 1 (pc_cache_create), so that what queries are turned by is below 3 x 2^30
-// radians, and its quarter turns fit 32 bits.  The branch for other angles would cost the kernels their registers.
-__device__ __forceinline__ float2 mx4_rotation(double x) { return rope_small(x); }
+// radians, and its turns are off by 2^-24 of one in fp64.  (As polynomials in fp64: 40 instructions where these are 7.)
+__device__ __forceinline__ float2 mx4_rotation(double x)
+{
+    const float part = (float)__builtin_amdgcn_fract(x * 0.15915494309189533577);        // 1 / (2 pi)
+    return make_float2(__builtin_amdgcn_cosf(part), __builtin_amdgcn_sinf(part));
+}
 
 // The larger of top and two bf16 numbers' magnitudes; fine: they are numbers.
 __device__ __forceinline__ float mx4_top(float top, uint32_t w, bool &fine)
