@@ -98,10 +98,13 @@ typedef struct {
  * their negatives, ties to the even code: 68 bytes where PC_BF16 has 256.  Keys are quantised as they are stored, turned to their
  * place (norms, turns and quantisation in 64 bits).  k, v, q and out are bf16.  A token whose key or value holds an infinity or a NaN in some
  * head has keys of NaN there: rows that see it are NaN in that head's query heads.
- * Attention (pc_attend, pc_attend_static, pc_attend_window, pc_attend_window_static, pc_decode_step) computes with the values held:
- * of one row with queries as the sum of two 8-bit numbers (off by 2^-8 of a value at most, as bf16 is), of more rows over a bf16 copy of the
- * tiles that they see in the workspace, in which every value held is exact (32 KB a tile of 32 tokens and 8 KV heads, half of them keys;
- * in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Tensors as pc_attend_window asks for them:
+ * Attention (pc_attend, pc_attend_static, pc_attend_window, pc_attend_window_static, pc_decode_step) computes with the values held, and with turned
+ * queries as the sum of two 8-bit numbers (off by 2^-8 of a value at most, as bf16 is).  Calls of more rows than one have the values of the
+ * tiles that they see laid out in bf16, which holds them exactly, and their queries turned in the workspace: 8 KB a tile of 32 tokens and KV head, 512
+ * bytes a row and query head (in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Long prefills of pc_attend
+ * (calls of at least 512 rows x query heads of a KV head that see 3e7 scores or more) go over a copy of all that they list, 512 bytes a token and KV
+ * head besides: there turned keys and queries are fp16 (off by 2^-12 of a value), but for keys above 700 and rows of queries whose norm, scaled, is above 700,
+ * which are served as the others are.  Tensors as pc_attend_window asks for them:
  * q and out 16-byte aligned; and pc_attend, like pc_attend_window, refuses a stream that is being captured.  Messages are appended, grown,
  * read back, forked (where they stay turned as they are), freed, swapped and closed up over as in other caches.  Their keys cannot be
  * turned without another rounding: pc_reposition* and turned forks are refused; nor is there a gradient (PC_ERR_INVALID_ARG). */
@@ -259,8 +262,8 @@ int32_t pc_attend(pc_cache *c, const pc_call *calls, int32_t n_calls,
  * too.  (It keeps no counters.)  A recorded call holds its messages as they were: slots, lengths and stored positions; one that has
  * grown, or been repositioned, moved or freed since has to be recorded anew.
  *
- * A batch of single tokens of a PC_BF16 cache whose calls list the same messages reads each tile once for up to 256 (call, head of a
- * KV head) pairs where that is cheaper (pc_set_decode_sharing: 1 never, 2 whenever there are two such calls), unless a call sees
+ * A batch of single tokens of a PC_BF16 or PC_MX4 cache (there of pc_attend too) whose calls list the same messages reads each tile once
+ * for up to 256 (call, head of a KV head) pairs where that is cheaper (pc_set_decode_sharing: 1 never, 2 whenever there are two such calls), unless a call sees
  * one message from two entries of its list; the order of a row's sums depends on the batch, so that a call alone may give
  * another last bit.  The same calls give the same bits. */
 int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink,
@@ -449,8 +452,9 @@ int32_t pc_set_tuning(pc_cache *c, int32_t decode_tiles_per_split, int32_t prefi
  * messages, every key turned to the position the call gives it.  The attention kernel then reads plain tiles of the
  * copy and turns the queries by their own position only, instead of once more per listed message.  The cache itself
  * is not changed; results are the same up to one more rounding of the copied keys to bf16.  mode 0 (default): calls
- * with rows x query heads >= 32768 (below that the copy costs more than it saves); 1: never; 2: every prefill call.
- * PC_BF16 caches only; pc_attend_static never gathers (the copy may not fit its fixed workspace). */
+ * with rows x query heads >= 32768 (below that the copy costs more than it saves); 1: never; 2: every prefill call (more than 16 rows x
+ * query heads of a KV head).  PC_MX4 caches: the long prefills described there (the copied keys in fp16).
+ * Of pc_attend in PC_BF16 and PC_MX4 caches only; pc_attend_static never gathers (the copy may not fit its fixed workspace). */
 int32_t pc_set_key_gather(pc_cache *c, int32_t mode);
 
 /* Gradient of pc_attend for fine-tuning (Sec. 2.4: while fine-tuning, a position update is
@@ -487,8 +491,8 @@ int32_t pc_grad_keys_finalize(pc_cache *c, float *d_k, void *stream);
  * calls alone goes whichever way is the cheapest for its lists (every call on its own, message
  * by message for a few calls at a time, or the shared walk).  1: every call on its own; 2: the
  * shared walk whenever the shape allows it.  (Calls whose query position, less a message's start,
- * plus the position its keys are stored at does not fit 32 bits walk on their own.)  Applies to PC_BF16 caches; other calls are
- * unaffected. */
+ * plus the position its keys are stored at does not fit 32 bits walk on their own.)  Applies to PC_BF16 caches (and, with the
+ * walk that pc_attend_window describes, to PC_MX4 caches); other calls are unaffected. */
 int32_t pc_set_decode_sharing(pc_cache *c, int32_t mode);
 
 #ifdef __cplusplus

@@ -962,6 +962,7 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
 // LONG_SCORES scores in all (two more launches are to be earned back).  In place and copied, us: 8 calls of 64 rows over 12064 tokens, 64 heads on 8: 337, 311; 32 on
 // 8 (256): 185, 250; one call of 256 rows over 2256 tokens, 64 heads (3.7e7): 64, 62; 32 heads (1.85e7): 53, 56; 8 calls of it: 152, 113;
 // of 1024 rows over 13024 tokens, 64 heads: 5227, 2848.
+// By the caller's word: pc_set_key_gather.
 constexpr int64_t LONG_ROWS = 512;
 constexpr double LONG_SCORES = 3e7;
 constexpr int64_t LONG_TOKENS = (int64_t)1 << 22;        // a copy's, where it has more calls than one: 16 GiB of 8 KV heads
@@ -974,7 +975,7 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
     };
     // tokens that a call lists, if it is long
     auto long_tokens = [&](const pc_call &call) -> int64_t {
-        if (fixed_ws || c->host_only || call.n_q <= 1 || call.n_q * (int64_t)c->g < LONG_ROWS || call.n_sel < 0 || (call.n_sel > 0 && !call.sel)) return 0;
+        if (fixed_ws || c->host_only || call.n_q <= 1 || c->key_gather == 1 || call.n_q * (int64_t)c->g < (c->key_gather == 2 ? 17 : LONG_ROWS) || call.n_sel < 0 || (call.n_sel > 0 && !call.sel)) return 0;
         int64_t tokens = 0;
         auto add = [&](int32_t m) { if (known(c, m)) tokens += chain_len(c, m); };
         for (int32_t e = 0; e < call.n_sel; ++e) add(call.sel[e].msg_id);
@@ -991,7 +992,7 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
         size_t e = i;
         double scores = 0;
         for (; e < tokens.size() && tokens[e] > 0; ++e) scores += (double)tokens[e] * calls[e].n_q * c->cfg.n_q_heads;
-        const bool kept = scores >= (runs > 1 ? 4 : 1) * LONG_SCORES;
+        const bool kept = c->key_gather == 2 ? scores > 0 : scores >= (runs > 1 ? 4 : 1) * LONG_SCORES;
         some |= kept;
         if (!kept) std::fill(tokens.begin() + (ptrdiff_t)i, tokens.begin() + (ptrdiff_t)e, 0);
         i = std::max(e, i + 1);

@@ -23,6 +23,19 @@ def test_heads_rows_and_windows(h_q, h_kv, n_q):
     layer.cache.close()
 
 
+@pytest.mark.parametrize("h_q,h_kv", HEADS)
+def test_rows_over_a_copy(h_q, h_kv):
+    """Every prefill call over a copy of what it lists (the caller's word), with single tokens, short and empty calls among them; and none of them."""
+    layer = Layer4(LENS, h_q, h_kv)
+    calls = [(SEL, 5, 600, 90), ([], 5, 0, 90), (SEL, 5, 600, 1), (SEL[2:], 3, 300, 33), ([], -1, 5, 70), (SEL[:1], -1, 40, 65, [-7 * i for i in range(65)]), (SEL, 4, -10 ** 6, 17)]
+    for mode in (2, 1, 0):
+        layer.cache.set_key_gather(mode)
+        layer.run(calls, what=f"mode {mode}")
+        for n_q in (2, 5, 18, 32, 64, 90):
+            layer.run([(SEL, 5, 600, n_q)], what=f"mode {mode} rows {n_q}")
+    layer.cache.close()
+
+
 @pytest.mark.parametrize("h_q,h_kv", [(8, 2), (4, 4)])
 @pytest.mark.parametrize("static", [False, True])
 def test_batches(h_q, h_kv, static):
