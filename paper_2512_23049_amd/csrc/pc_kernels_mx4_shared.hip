@@ -100,15 +100,25 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
     }
     __syncthreads();
 
-    int to_visit = visit0, to_tile = 0, to_asked = 0, to_slot = 0, to_has = 0;
-    if (n_steps > 0) { to_slot = listed(&S.visits[visit0].slot0); to_has = listed(&S.visits[visit0].n_tiles); }
+    // (what the walks need of a visit they ask for a visit ahead: a latency each otherwise)
+    const int last = visit0 + i1.z - 1;
+    int to_visit = visit0, to_tile = 0, to_asked = 0, to_slot = 0, to_has = 0, to_next_slot = 0, to_next_has = 0;
+    auto ahead = [&]() __attribute__((always_inline)) {
+        const PcWinVisit *v = S.visits + min(to_visit + 1, last);
+        to_next_slot = listed(&v->slot0); to_next_has = listed(&v->n_tiles);
+    };
+    if (n_steps > 0) {
+        to_slot = listed(&S.visits[visit0].slot0); to_has = listed(&S.visits[visit0].n_tiles);
+        ahead();
+    }
     auto request = [&](int place) __attribute__((always_inline)) {
         const int l = lane_again();
         if (to_asked > 0) {
             to_tile += TILES;
             if (to_tile >= to_has) {
                 ++to_visit; to_tile = 0;
-                to_slot = listed(&S.visits[to_visit].slot0); to_has = listed(&S.visits[to_visit].n_tiles);
+                to_slot = to_next_slot; to_has = to_next_has;
+                ahead();
             }
         }
         ++to_asked;
@@ -163,6 +173,12 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
     for (int i = 0; i < 8; ++i) q_hi[i] = q_lo[i] = 0;
     const int e_hi = (int)(__float_as_uint(unit) >> 23), e_lo = e_hi - 4;
     int visit = visit0 - 1, tile = 0, has = 0;           // the walk of what is computed
+    int next_has = 0, next_e0 = 0, next_first = 0, next_end = 0;
+    auto header = [&]() __attribute__((always_inline)) {
+        const PcWinVisit *v = S.visits + min(visit + 1, last);
+        next_has = listed(&v->n_tiles); next_e0 = listed(&v->e0); next_first = listed(&v->off[my]); next_end = listed(&v->off[my + 1]);
+    };
+    if (n_steps > 0) header();
 #pragma unroll 1
     for (int step = 0, place = 0; step < n_steps; ++step, place = place == RING - 1 ? 0 : place + 1) {
         if (step + AHEAD <= n_steps) wait_vm<LOADS * (AHEAD - 2)>();           // (the next step's tiles too)
@@ -173,9 +189,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
         tile += TILES;
         if (tile >= has) {
             ++visit; tile = 0;
-            has = listed(&S.visits[visit].n_tiles);
-            const int e0 = listed(&S.visits[visit].e0);
-            const int first = listed(&S.visits[visit].off[my]), end = listed(&S.visits[visit].off[my + 1]);
+            has = next_has;
+            const int e0 = next_e0, first = next_first, end = next_end;
+            header();
             listers = end - first;
             asm volatile("" ::: "memory");               // (a wave's own LDS accesses happen in order)
             if (a == 0) s_see[wave][n] = make_int4(0, 0, 0, 0);
@@ -186,13 +202,19 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
                     asm volatile("" : "+v"(q[i].x), "+v"(q[i].y), "+v"(q[i].z), "+v"(q[i].w));
                 int of = -1;                             // which of the rotations is the lane's
                 asm volatile("" ::: "memory");
-#pragma unroll 1
-                for (int i = 0; i < min(TURNS, end - e); ++i) {
-                    const win_i32x4 x = listed4(S.sees + e0 + e + i), y = listed4((const char *)(S.sees + e0 + e + i) + 16);
-                    const bool mine = sub == y.z;
-                    if (mine && a == 0) s_see[wave][n] = make_int4(x.x, x.y, x.z, x.w);
+                win_i32x4 x[TURNS], y[TURNS];            // (all at once: one latency)
+#pragma unroll
+                for (int i = 0; i < TURNS; ++i) {
+                    const PcWinSee *see = S.sees + e0 + min(e + i, end - 1);
+                    x[i] = listed4(see); y[i] = listed4((const char *)see + 16);
+                }
+#pragma unroll
+                for (int i = 0; i < TURNS; ++i) {
+                    if (e + i >= end) break;
+                    const bool mine = sub == y[i].z;
+                    if (mine && a == 0) s_see[wave][n] = make_int4(x[i].x, x[i].y, x[i].z, x[i].w);
                     of = mine ? i : of;
-                    const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y.y << 32) | (uint32_t)y.x);
+                    const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y[i].y << 32) | (uint32_t)y[i].x);
                     const float2 cs = mx4_rotation((double)turn * s_freq[lane]);
                     s_rot[wave][i][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
                 }
@@ -234,7 +256,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
         }
         if (__builtin_amdgcn_ballot_w64(some != 0) != 0) {
             const unsigned kt = ring + place * SLOT;
-            float sc[8 * TILES];                         // keys 32 t + 8 a + 0..7 of column n
+            float sc[8 * TILES];                         // keys 32 t + 8 a + 0..7 of column n, less the column's reference
+            const float ref = m_ref == -INFINITY ? 0.f : m_ref;
             {
                 const int l = lane_again(), m = l & 15, key = 8 * (m >> 2) + (m & 3);
                 const unsigned at = (unsigned)(key * 64 + (((l >> 4) ^ (key >> 3)) << 4));
@@ -244,7 +267,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
                     for (int tau = 0; tau < 2; ++tau) {
                         const uint4 codes = __builtin_bit_cast(uint4, *(lds16)(uintptr_t)(kt + t * TILE + at + tau * 256));
                         const int e = (int)(*(lds4)(uintptr_t)(kt + t * TILE + K_EXPS + key * 4 + tau * 16) >> (8 * (l >> 4)));
-                        f32x4 s = mx4_scores16(codes, e, q_lo, e_lo, (f32x4){0.f, 0.f, 0.f, 0.f});
+                        f32x4 s = mx4_scores16(codes, e, q_lo, e_lo, (f32x4){-ref, -ref, -ref, -ref});
                         s = mx4_scores16(codes, e, q_hi, e_hi, s);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) sc[8 * t + 4 * tau + j] = s[j];
@@ -252,7 +275,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             }
             __builtin_amdgcn_sched_barrier(0);
             const bool whole = all == ~0u;
-            if (__builtin_amdgcn_ballot_w64(some != 0 && !whole) == 0) {     // (all or nothing)
+            if (__builtin_amdgcn_ballot_w64(!whole) == 0) {                  // (nothing is masked)
+            } else if (__builtin_amdgcn_ballot_w64(some != 0 && !whole) == 0) {          // (all or nothing)
 #pragma unroll
                 for (int j = 0; j < 8 * TILES; ++j) sc[j] = whole ? sc[j] : -INFINITY;
             } else {
@@ -268,22 +292,25 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             for (int j = 4; j < 8 * TILES; j += 4) mx = fmaxf(mx, fmaxf(fmaxf(sc[j], sc[j + 1]), fmaxf(sc[j + 2], sc[j + 3])));
             // The reference of a column's exponents moves only where a score is 2^LAZY above it (a column's first always is):
             // probabilities up to that are as exact, and the lanes of a column need not agree on a maximum step by step.
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > m_ref + LAZY_LOG2) != 0, 0)) {
+            const float limit = m_ref == -INFINITY ? -INFINITY : LAZY_LOG2;
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float m_new = mx > m_ref + LAZY_LOG2 ? mx : m_ref, f = m_new == m_ref ? 1.f : ex2(m_ref - m_new);
+                const bool up = mx > limit;
+                const float m_new = up ? ref + mx : m_ref, by = up ? m_new - ref : 0.f, f = !up ? 1.f : m_ref == -INFINITY ? 0.f : ex2(-by);
                 m_ref = m_new;
                 sums *= f;
 #pragma unroll
                 for (int db = 0; db < 8; ++db) acc[db] *= f;
+#pragma unroll
+                for (int j = 0; j < 8 * TILES; ++j) sc[j] -= by;
             }
-            const float ref = m_ref == -INFINITY ? 0.f : m_ref;
             bf16x8 p[TILES];
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 uint32_t pk[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) pk[j] = pack_bf16(ex2(sc[8 * t + 2 * j] - ref), ex2(sc[8 * t + 2 * j + 1] - ref));
+                for (int j = 0; j < 4; ++j) pk[j] = pack_bf16(ex2(sc[8 * t + 2 * j]), ex2(sc[8 * t + 2 * j + 1]));
                 p[t] = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
             }
             // (the denominator: of the probabilities as the products take them, so that their rounding cancels)

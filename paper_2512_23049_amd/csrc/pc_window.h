@@ -73,7 +73,7 @@ struct PcWinSharedItem {      // one workgroup's tiles, for each KV head
     int32_t call0, n_calls;   // its set of calls
     int32_t waves;            // that hold all groups of columns (a power of two); the others share its steps
     int32_t split0;
-    int32_t pad[2];
+    int32_t n_visits, pad;
 };
 struct PcWinSharedCall { int32_t row, part0; };         // packed row, partial row of split 0
 struct PcWinShared {

@@ -312,7 +312,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
         int32_t done = 0;                                // tiles of visits[at] that earlier workgroups have
         for (int64_t b = 0; b < n_bins; ++b) {
             int32_t left = (int32_t)(total * (b + 1) / n_bins - total * b / n_bins);
-            P.sh_items.push_back(PcWinSharedItem{(int32_t)P.sh_visits.size(), 0, call0, in_set, waves, (int32_t)b * reps, {0, 0}});
+            P.sh_items.push_back(PcWinSharedItem{(int32_t)P.sh_visits.size(), 0, call0, in_set, waves, (int32_t)b * reps, 0, 0});
             while (left > 0) {
                 const Visit &v = visits[at];
                 const int32_t n = std::min(left, v.tiles - done), slot0 = v.slot0 + PC_TILE * done, slot1 = slot0 + PC_TILE * n;
@@ -351,6 +351,7 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                     pv.off[gr] = (int32_t)k;
                 }
                 P.sh_visits.push_back(pv);
+                ++P.sh_items.back().n_visits;
                 P.sh_items.back().n_steps += (n + PC_WIN_STEP_TILES - 1) / PC_WIN_STEP_TILES;
                 left -= n; done += n;
                 if (done == v.tiles) { ++at; done = 0; }

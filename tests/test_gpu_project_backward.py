@@ -39,7 +39,7 @@ class Grads:
 
 # 32 bits: as the forward's, some 40 roundings of 2^-24 of the largest terms; a result is the difference of two terms as large as the row's
 # largest g r, so that is what errors are measured in.  A bf16 result is off by 2^-8 of itself besides.  A weight's gradient is a
-# sum of N terms, added up in pieces of 32 rows and then 16 shares: relative to the root of the sum of their squares 1e-6.
+# sum of N terms, added up in pieces of 4 to 64 rows and then 64 shares: relative to the root of the sum of their squares 1e-6.
 def check_rows(got, want, terms, dtype, what):
     bar = 5e-6 * terms + (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0)
     far = (np.abs(got - want) / np.maximum(bar, 1e-30)).max()

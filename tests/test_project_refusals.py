@@ -78,6 +78,10 @@ def test_four_bit_caches():
         b.Cache(34, 2, 128, b.PC_MX4, 1e4, 512, 8, flags=b.PC_FLAG_HOST_ONLY)
     with pytest.raises(b.PcError):
         cache(b.PC_MX4, max_position=1 << 30)
+    for theta in (0.5, 0.999, 0.0, -1.0, float("nan")):  # (its frequencies are to be 1 at most)
+        with pytest.raises(b.PcError):
+            b.Cache(8, 2, 128, b.PC_MX4, theta, 512, 8, flags=b.PC_FLAG_HOST_ONLY)
+    b.Cache(8, 2, 128, b.PC_MX4, 1.0, 512, 8, flags=b.PC_FLAG_HOST_ONLY).close()
     c = cache(b.PC_MX4)
     cfg = c.cfg
     assert b.lib().pc_cache_storage_bytes(C.byref(cfg)) == 2 * 512 * 2 * 68
