@@ -168,7 +168,8 @@ int32_t pc_append_tokens_batch(pc_cache *c, const int32_t *msg_ids, int32_t n_ms
  *   q_out      device [rows][n_q_heads][head_dim], 16-byte aligned, not overlapping the rows.
  * pc_append_projected: n new messages, whose tokens are the rows in list order (rows: sum of lens); lens, reserves (may be NULL) and
  * msg_ids as for pc_append_messages.  pc_append_projected_tokens: one more token for each of n_msgs distinct messages, row j for
- * msg_ids[j], as pc_append_tokens_batch (same errors).  Norms are computed in 32 bits (PC_MX4: of keys in 64).  A stream that is being captured
+ * msg_ids[j], as pc_append_tokens_batch (same errors).  Norms are computed in 32 bits, which the squares of a head's values have to fit
+ * (PC_MX4: of keys in 64).  A stream that is being captured
  * is refused (a replay would write to slots that may be another message's by then). */
 typedef struct {
     const void  *q, *k, *v;

@@ -1000,6 +1000,7 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
     }
     if (!some) return in_place(0, n_calls, 0, 0);
     // (runs of calls of a kind follow each other: nothing may be refused behind the first)
+    if (!q || !out) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: null q or out", what);
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
     if (pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move", what);
     {
@@ -1011,7 +1012,7 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
     if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
     int64_t row = 0;
     for (int32_t a = 0; a < n_calls;) {
-        const bool kind = tokens[(size_t)a] > 0;
+        bool kind = tokens[(size_t)a] > 0;
         int32_t b = a;
         int64_t rows = 0, copied = 0;
         for (; b < n_calls && (tokens[(size_t)b] > 0) == kind && (b == a || copied + tokens[(size_t)b] <= LONG_TOKENS); ++b) {
@@ -1023,6 +1024,7 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
             if (++c->mark_epoch_mx4 == 0) c->mark_epoch_mx4 = 1;
             const int64_t at = row * c->cfg.n_q_heads;
             rc = pc_attend_gathered_mx4(c, calls + a, b - a, (const uint16_t *)q + at * c->D, (uint16_t *)out + at * c->D, lse ? lse + at : nullptr, st, c->mark_epoch_mx4);
+            if (rc == PC_ERR_HIP) { kind = false; rc = PC_OK; }          // (no room for the copy: what else may have failed fails again)
         }
         if (rc == PC_OK) rc = in_place(a, b - a, row, kind ? c->mark_epoch_mx4 : 0);
         if (rc != PC_OK) return rc;

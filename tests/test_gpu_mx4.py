@@ -122,6 +122,7 @@ def test_many_rows_over_long_lists(spoilt):
             k[5] *= 1e6
         if spoilt == "no number" and i == 1:
             v[5, 0, 3] = np.nan
+    from paper_2512_23049_amd import binding as b
     lens = [1900, 33, 2500, 1, 1030, 70, 1100, 1099, 40]
     layer = Layer4(lens, 16, 2, spoil=spoil)
     long = [(0, 0), (4, 2000), (2, 3007), (3, 9000), (5, 5600), (0, 5700)]
@@ -156,7 +157,15 @@ def test_many_rows_over_long_lists(spoilt):
         same(out[~rows], lse[~rows], want[~rows], want_lse[~rows], "the others")
         same(out[rows][:, 8:], lse[rows][:, 8:], want[rows][:, 8:], want_lse[rows][:, 8:], "the other head")
         return
-    layer.run(calls, q=q)
+    out, _ = layer.run(calls, q=q)
+    tq = layer.dev(q)
+    again = layer.torch.full_like(tq, 7.0)
+    layer.cache.attend(layer.calls(calls), tq.data_ptr(), again.data_ptr())              # (no sums asked for; the same bits)
+    layer.torch.cuda.synchronize()
+    assert layer.torch.equal(again, out)
+    for q_ptr, out_ptr in ((0, again.data_ptr()), (tq.data_ptr(), 0), (tq.data_ptr() + 2, again.data_ptr())):
+        with pytest.raises(b.PcError):
+            layer.cache.attend(layer.calls(calls), q_ptr, out_ptr)
     layer.cache.close()
 
 
