@@ -559,10 +559,8 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
                     float ps = 0.f;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
-                        const float a = ex2(s[2 * r]), b = ex2(s[2 * r + 1]);
-                        ps += a;
-                        ps += b;
-                        pk[r] = pack_bf16(a, b);
+                        pk[r] = pack_bf16(ex2(s[2 * r]), ex2(s[2 * r + 1]));
+                        ps = mx4_sum(pk[r], ps);
                     }
                     l_run += ps;
                     const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
@@ -602,16 +600,8 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
                 float ps = 0.f;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
-                    const float a = ex2(s[2 * r]), b = ex2(s[2 * r + 1]);
-                    ps += a;
-                    ps += b;
-                    pk[r] = pack_bf16(a, b);
-                }
-                if (__builtin_expect(edge, 0)) {
-                    // (a row of few keys: the sum of the probabilities as the products take them, so that their rounding cancels)
-                    ps = 0.f;
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) ps += bf_lo(pk[r]) + bf_hi(pk[r]);
+                    pk[r] = pack_bf16(ex2(s[2 * r]), ex2(s[2 * r + 1]));
+                    ps = mx4_sum(pk[r], ps);
                 }
                 const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
                 bf16x8 fr[8];

@@ -65,6 +65,14 @@ template <int PAIR> __device__ __forceinline__ uint32_t mx4_values(uint32_t w, u
     return mx4_lowered<PAIR & 1>(x & 0x7FFF7FFFu, d) | (x & 0x80008000u);
 }
 
+// c + the two probabilities, as the products take them: their rounding cancels where a row has few large ones (errors against 64 bits, 40
+// rows: 2.43e-3 -> 2.41e-3; calls of 8 to 200 rows take 1.2 us less than with two additions of what was not rounded yet)
+typedef __bf16 mx4_bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float mx4_sum(uint32_t p, float c)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx4_bf16x2, p), __builtin_bit_cast(mx4_bf16x2, 0x3F803F80u), c, false);
+}
+
 // (cos, sin) of a turn: positions are below 2^30 and theta is at least 1 (pc_cache_create), so that what queries are turned by is below 3 x 2^30
 // radians, and its turns are off by 2^-24 of one in fp64.  (As polynomials in fp64: 40 instructions where these are 7.)
 __device__ __forceinline__ float2 mx4_rotation(double x)
