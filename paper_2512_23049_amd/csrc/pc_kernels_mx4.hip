@@ -27,7 +27,9 @@ template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_
 //            on the probabilities, by block of 32 dimensions: probabilities are held 2^60 times as large, and a saturating
 //            subtraction from their exponents takes the powers (-60 to 60) off again.
 // Tiles come by direct loads, two places a wave of its own: no registers wait for them (two tiles in registers left room for two waves a
-// SIMD, see below), and no wave for another.  Bound: memory, 4352 bytes a tile and KV head.
+// SIMD: 66 us where this takes 50), and no wave for another.  Bound: memory, 4352 bytes a tile and KV head, where there are many (64
+// calls of 150 tiles, 32 heads over 8: 334 MB call by call, of which 119 are distinct, in 50 us: 6.7 TB/s out of the caches); latency where
+// there are few (4 calls, window 512: 9 us, of which a launch of nothing takes 3).
 __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *items, const PcWinRun *runs, const int32_t *q_pos)
 {
     // of a tile: codes of keys and of values, exponents of keys and of values (256 bytes each: a direct load's lanes)
@@ -260,6 +262,7 @@ void pc_launch_win_decode_mx4(const PcWin &W, int n_items, const PcArgBlob *blob
 // In front of the attention of rows: the call's lists to the workspace and the rotations of its runs (as win_turns), its queries turned
 // by their positions and the unit that their 8-bit pieces are in, and the values of the tiles that rows see, as a bf16 cache has them (what the
 // codes stand for is exact there; 68 bytes read and 256 written for each, once, where every workgroup of rows would convert them again).
+// Bound: latency (77 rows over 5 messages, 32 heads over 8: 5.6 us, with eight heads a block 8.3).
 __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare &P)
 {
     __shared__ __attribute__((aligned(16))) float2 s_rot[PC_D / 2][33];           // [frequency][row]
@@ -366,6 +369,9 @@ void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st
 //   queries  come turned by their positions (pc_mx4_prepare_kernel) and are turned back by a run's rotation in 32 bits, then cut in pieces under one
 //            power of two for the row, the same for every turn;
 //   values   come from the copy; they are finite, so that a probability of zero takes a key out.
+// Bound: the vector unit, 140 instructions a tile and wave of which 49 turn queries (messages of 160 tokens: every fifth tile is another's), beside
+// 512 cycles of matrix work; 64 heads over 8, 1024 rows over 13k tokens: 0.6 PFLOP/s, which is why long prefills go another way.  Small ones
+// are chains of latencies: 77 rows over 5 messages 16.5 us, in splits of six tiles (of four, three or two no less, and more to merge).
 #define LAZY_LOG2 64.0f
 #define MFMA32(a, b, c) __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0)
 
@@ -679,7 +685,8 @@ void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, 
 // keys turned to the positions that the call gives them and rounded to fp16 (off by 2^-12 of a value), values as the bf16 that they stand for.
 // Keys above 6 x 2^7, and those that are no number (which that walk would add to masks), mark the call for the walk behind it: below, what
 // queries under fp16's normal numbers are off by, 2^-25, moves a score by 2^-25 x 2^10 x sqrt(128) at most.
-// Bound: memory, 136 bytes read and 512 written a token and KV head.
+// Bound: memory, 136 bytes read and 512 written a token and KV head (9.9k tokens of 8 KV heads: 22 us; the walk behind it, pc_prefill_bf16_kernel, 2048
+// rows of 64 heads: 490 us, 1.2 PFLOP/s, where the walk over the cache itself takes 930).
 __global__ __launch_bounds__(256) void pc_mx4_gather_kernel(PcLaunch L, const PcGatherItem *__restrict__ items, int n_items, const int32_t *__restrict__ seg_kvoff,
                                                             uint32_t *mark, uint32_t value)
 {
