@@ -287,18 +287,25 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             } else {
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
-                    const uint32_t mine = sees[t] >> (8 * a);
+                    uint32_t mine = sees[t] >> (8 * a);
+                    asm volatile("" : "+v"(mine));       // (or the masks are made in every step, and chosen from behind)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sc[8 * t + j] = (mine >> j) & 1 ? sc[8 * t + j] : -INFINITY;
                 }
             }
-            float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+            // (on the bit patterns, which take no care of NaN: right wherever some score is above the reference)
+            auto fi = [](float x) { return __float_as_int(x); };
+            int top = imax3(fi(sc[0]), fi(sc[1]), fi(sc[2]));
 #pragma unroll
-            for (int j = 4; j < 8 * TILES; j += 4) mx = fmaxf(mx, fmaxf(fmaxf(sc[j], sc[j + 1]), fmaxf(sc[j + 2], sc[j + 3])));
+            for (int j = 3; j < 8 * TILES - 1; j += 2) top = imax3(top, fi(sc[j]), fi(sc[j + 1]));
+            top = max(top, fi(sc[8 * TILES - 1]));
             // The reference of a column's exponents moves only where a score is 2^LAZY above it (a column's first always is):
             // probabilities up to that are as exact, and the lanes of a column need not agree on a maximum step by step.
-            const float limit = m_ref == -INFINITY ? -INFINITY : LAZY_LOG2;
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > fi(LAZY_LOG2) || (m_ref == -INFINITY && some != 0)) != 0, 0)) {
+                const float limit = m_ref == -INFINITY ? -INFINITY : LAZY_LOG2;
+                float mx = sc[0];
+#pragma unroll
+                for (int j = 1; j < 8 * TILES; ++j) mx = fmaxf(mx, sc[j]);
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
                 const bool up = mx > limit;

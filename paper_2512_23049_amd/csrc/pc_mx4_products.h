@@ -14,6 +14,7 @@ typedef uint16_t mx4_u16x2 __attribute__((ext_vector_type(2)));
 typedef short mx4_s16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int imax3(int a, int b, int c) { return max(max(a, b), c); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // a wave's own LDS accesses happen in the order they are issued: the compiler is to keep it
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
@@ -96,7 +97,8 @@ __device__ __forceinline__ float mx4_unit(float top)
 }
 __device__ __forceinline__ int mx4_e4m3(const float (&x)[4], float unit)
 {
-    mx4_s16x2 r = {0, 0};
+    mx4_s16x2 r;
+    asm("" : "=v"(r));                                // (both halves are written: nothing to start from)
     r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[0], x[1], unit, false);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, x[2], x[3], unit, true);
     return __builtin_bit_cast(int, r);
