@@ -22,6 +22,7 @@
 namespace {
 
 typedef const __attribute__((address_space(3))) win_i32x4 *lds16;
+typedef __attribute__((address_space(3))) win_i32x4 *lds16_out;
 typedef const __attribute__((address_space(3))) uint32_t *lds4;
 typedef uint32_t mx4_u32x2 __attribute__((ext_vector_type(2)));
 typedef const __attribute__((address_space(3))) mx4_u32x2 *lds8;
@@ -145,18 +146,25 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
         }
     };
     // a step's values: a thread eight slots of a dimension (or of two)
+    // (where a thread's part of a step stands is worked out once)
+    unsigned conv_codes, conv_exps, conv_to;
+    {
+        const int thread = wave * 64 + lane_again(), t = thread >> 9, grp = thread >> 7 & 3, d = thread & 127, m = d & 15, db = d >> 4;
+        conv_codes = ring + t * TILE + VALUES + grp * 512 + m * 32 + (((db >> 2) ^ (m >> 3)) << 4) + (db & 3) * 4;
+        conv_exps = ring + t * TILE + V_EXPS + grp * 32 + (d >> 5) * 8;
+        conv_to = (unsigned)(uintptr_t)&s_v[0][0][0] + thread * 16;
+        asm volatile("" : "+v"(conv_codes), "+v"(conv_exps), "+v"(conv_to));
+    }
     auto convert = [&](int place, int to) __attribute__((always_inline)) {
-        const int thread = wave * 64 + lane_again();
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int e = thread + 64 * NW * i, t = e >> 9, grp = e >> 7 & 3, d = e & 127, m = d & 15, db = d >> 4;
-            const unsigned from = ring + place * SLOT + t * TILE;
-            const uint32_t w = *(lds4)(uintptr_t)(from + VALUES + grp * 512 + m * 32 + (((db >> 2) ^ (m >> 3)) << 4) + (db & 3) * 4);
-            const mx4_u32x2 ex = *(lds8)(uintptr_t)(from + V_EXPS + grp * 32 + (d >> 5) * 8);
+            const unsigned at = place * SLOT + (64 * NW * i >> 9) * TILE;
+            const uint32_t w = *(lds4)(uintptr_t)(conv_codes + at);
+            const mx4_u32x2 ex = *(lds8)(uintptr_t)(conv_exps + at);
             uint4 x;
             x.x = mx4_values(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_values(w, ex.x, std::integral_constant<int, 1>{});
             x.z = mx4_values(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_values(w, ex.y, std::integral_constant<int, 3>{});
-            *reinterpret_cast<uint4 *>(&s_v[to][t][(grp * PC_D + d) * 16]) = x;
+            *(lds16_out)(uintptr_t)(conv_to + to * (TILES * PC_TILE * PC_D * 2) + 64 * NW * i * 16) = __builtin_bit_cast(win_i32x4, x);
         }
     };
     for (int i = 0; i < min(AHEAD, n_steps); ++i) request(i);
@@ -172,6 +180,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
     f32x4 acc[8];
     mx4_i32x8 q_hi, q_lo;                                // turned and scaled, in two pieces
     int listers = 0;                                     // entries of the group
+    int whole_to = 0;                                    // tiles of the visit that the column sees whole, from the first one on; -1: it sees nothing of the visit
 #pragma unroll
     for (int db = 0; db < 8; ++db) acc[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -242,11 +251,16 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
                 }
                 asm volatile("" ::: "memory");
             }
+            const int4 w = s_see[wave][n];
+            whole_to = w.y <= 0 ? -1 : w.w <= w.x ? min(w.y / PC_TILE, has) : 0;
         }
         uint32_t sees[TILES], some = 0, all = ~0u;       // bit: key of a tile; of any tile, of all there are
 #pragma unroll
         for (int t = 0; t < TILES; ++t) sees[t] = 0;
-        if (listers > 0 && (reps == 1 || step % reps == rep)) {
+        if (listers == 0 || (reps > 1 && step % reps != rep)) {
+        } else if (__builtin_amdgcn_ballot_w64(whole_to >= 0 && tile + TILES > whole_to) == 0) {
+            some = all = whole_to < 0 ? 0u : ~0u;
+        } else {
             auto first = [](unsigned k) { return k >= 32u ? ~0u : (1u << k) - 1u; };
             asm volatile("" ::: "memory");
             const int4 w = s_see[wave][n];
@@ -287,8 +301,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             } else {
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) {
-                    uint32_t mine = sees[t] >> (8 * a);
-                    asm volatile("" : "+v"(mine));       // (or the masks are made in every step, and chosen from behind)
+                    const uint32_t mine = sees[t] >> (8 * a);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sc[8 * t + j] = (mine >> j) & 1 ? sc[8 * t + j] : -INFINITY;
                 }
