@@ -6,9 +6,9 @@
 // workgroup converts a step's values to bf16 together, one step ahead, so that no wave has their codes and powers to take apart.  A
 // wave's queries are turned for all of a visit's calls at once, each lane by its own call's rotation.
 //
-// Bound: no unit alone.  32 calls over 410 of 512 messages of 160 tokens each, 64 heads over 8 (2850 distinct tiles): 209 us, of which
+// Bound: no unit alone.  32 calls over 410 of 512 messages of 160 tokens each, 64 heads over 8 (2850 distinct tiles): 201 us, of which
 // the vector unit is busy in 58 %, shared memory in 33 % and the matrix unit in 20 %: sixteen waves meet at a barrier a step and do the same at the
-// same time.  Without the products of the values it takes 28 us less, without the turned queries' pieces 31, without the conversion of values 18, without
+// same time.  (At 217 us:) without the products of the values it takes 28 us less, without the turned queries' pieces 31, without the conversion of values 18, without
 // exponentials 13, without loads 8; 16 are its start and the partial results.  Call by call the same batch takes 365 us and reads 26 times as much.
 #include "pc_window.h"
 #include "pc_mx4.h"

@@ -70,10 +70,11 @@ template <typename F> __device__ __forceinline__ F sum8(F x)
 }  // namespace
 
 // ------------------------------------------------------------------------------------------------------------ append
-// A block takes a group of eight slots and eight heads of one kind: blockIdx.y below `kv`: keys and values, else queries.  A head's
+// A block takes a group of eight slots and eight heads of one kind: part below `kv`: keys and values, else queries.  Parts of a group follow each
+// other, so that the work on keys hides behind the queries' traffic (8192 rows into 4 bits: all keys first 74 us, so 68).  A head's
 // row is eight lanes, each with E values of the lower half and their partners in the upper half: turns stay in a lane, sums
 // take three steps.  Rotations are made once a block (8 tokens x D/2) and shared by its heads.
-// Bound: memory, where there are many rows (bf16, 2208 rows of 32 heads over 8, 54 MB: 11.7 us, 4.6 TB/s; 4 bits, 8192 rows of 64 heads over 8, 268 MB: 71 us,
+// Bound: memory, where there are many rows (bf16, 2208 rows of 32 heads over 8, 54 MB: 11.7 us, 4.6 TB/s; 4 bits, 8192 rows of 64 heads over 8, 311 MB: 66 us, 4.7 TB/s,
 // keys in 64 bits: a key next to the middle of two codes goes to the one that its exact value is nearer to); latency where there are few
 // (four rows 5.2 us, a launch of nothing 3).
 template <int STORE, int D>           // STORE: PC_F32, PC_BF16, PC_MX4
@@ -84,14 +85,15 @@ __device__ __forceinline__ void rows_block(const PcRows &R, const PcRowsItem *it
     constexpr int E = D / 16, HALF = D / 2;
     struct Turn { F c, s; };
     __shared__ __attribute__((aligned(16))) Turn s_turn[PC_ROWS_GROUP][HALF];
-    const PcRowsItem it = item_of(items, R.n_items, blockIdx.x);
-    const int kv = (R.n_kv_heads + PC_ROWS_HEADS - 1) / PC_ROWS_HEADS;
-    const int t0 = 8 * (it.slot0 / 8 + (int)blockIdx.x - it.block0) - it.slot0;          // the group's first token (may lie in front of the item's)
+    const int kv = (R.n_kv_heads + PC_ROWS_HEADS - 1) / PC_ROWS_HEADS, chunks = kv + (R.q_out ? (R.n_q_heads + PC_ROWS_HEADS - 1) / PC_ROWS_HEADS : 0);
+    const int block = R.block0 + (int)blockIdx.x / chunks, part = (int)blockIdx.x % chunks;
+    const PcRowsItem it = item_of(items, R.n_items, block);
+    const int t0 = 8 * (it.slot0 / 8 + block - it.block0) - it.slot0;          // the group's first token (may lie in front of the item's)
     const int c = threadIdx.x & 7, hd = threadIdx.x >> 3 & 7, tt0 = threadIdx.x >> 6;     // the thread's tokens: t0 + tt0, and four on
     const int lo = E * c, hi = HALF + E * c;
 
-    if ((int)blockIdx.y >= kv) {
-        const int h = ((int)blockIdx.y - kv) * PC_ROWS_HEADS + hd;
+    if (part >= kv) {
+        const int h = (part - kv) * PC_ROWS_HEADS + hd;
         if (h >= R.n_q_heads) return;
         float w0[E], w1[E], x0[2][E], x1[2][E];
         load_weight<E>(R.q_weight, lo, w0);
@@ -120,7 +122,7 @@ __device__ __forceinline__ void rows_block(const PcRows &R, const PcRowsItem *it
         return;
     }
 
-    if (blockIdx.y == 0 && (int)blockIdx.x == it.block0 && threadIdx.x == 0) {
+    if (part == 0 && block == it.block0 && threadIdx.x == 0) {
         if (it.fresh) R.table[it.msg] = PcMsgEntry{it.slot0, it.len, 0, 0};
         else R.table[it.msg].len = it.len;
     }
@@ -136,7 +138,7 @@ __device__ __forceinline__ void rows_block(const PcRows &R, const PcRowsItem *it
             s_turn[e / HALF][e % HALF] = Turn{cs.x, cs.y};
         }
     }
-    const int h0 = (int)blockIdx.y * PC_ROWS_HEADS, h = min(h0 + hd, R.n_kv_heads - 1);
+    const int h0 = part * PC_ROWS_HEADS, h = min(h0 + hd, R.n_kv_heads - 1);
     const bool head_ok = h0 + hd < R.n_kv_heads;
     [[maybe_unused]] bool bad[2] = {false, false};       // (4 bits) the value holds what is no number
 
@@ -320,21 +322,23 @@ template <int STORE, int D> __global__ __launch_bounds__(256) void pc_rows_arg_k
     rows_block<STORE, D>(R, (const PcRowsItem *)arguments());           // (the blob comes first)
 }
 
-void pc_launch_rows(int dtype, const PcRows &R, const PcArgBlob *blob, hipStream_t st)
+void pc_launch_rows(int dtype, PcRows R, const PcArgBlob *blob, hipStream_t st)
 {
-    if (R.n_blocks <= 0) return;
-    auto chunks = [](int heads) { return (unsigned)((heads + PC_ROWS_HEADS - 1) / PC_ROWS_HEADS); };
-    const dim3 grid((unsigned)R.n_blocks, chunks(R.n_kv_heads) + (R.q_out ? chunks(R.n_q_heads) : 0u));
-    auto go = [&](auto store, auto dim) {
-        constexpr int S = decltype(store)::value, D = decltype(dim)::value;
-        if (blob) pc_rows_arg_kernel<S, D><<<grid, 256, 0, st>>>(*blob, R);
-        else pc_rows_kernel<S, D><<<grid, 256, 0, st>>>(R);
-    };
-    using std::integral_constant;
-    if (dtype == 2) go(integral_constant<int, 2>{}, integral_constant<int, 128>{});
-    else if (dtype == 1) go(integral_constant<int, 1>{}, integral_constant<int, 128>{});
-    else if (R.D == 64) go(integral_constant<int, 0>{}, integral_constant<int, 64>{});
-    else go(integral_constant<int, 0>{}, integral_constant<int, 128>{});
+    auto chunks = [](int heads) { return (heads + PC_ROWS_HEADS - 1) / PC_ROWS_HEADS; };
+    const int parts = chunks(R.n_kv_heads) + (R.q_out ? chunks(R.n_q_heads) : 0), most = std::max(1, (1 << 23) / parts);       // (a launch has fewer than 2^32 threads)
+    for (R.block0 = 0; R.block0 < R.n_blocks; R.block0 += most) {
+        const unsigned grid = (unsigned)(std::min(most, R.n_blocks - R.block0) * parts);
+        auto go = [&](auto store, auto dim) {
+            constexpr int S = decltype(store)::value, D = decltype(dim)::value;
+            if (blob) pc_rows_arg_kernel<S, D><<<grid, 256, 0, st>>>(*blob, R);
+            else pc_rows_kernel<S, D><<<grid, 256, 0, st>>>(R);
+        };
+        using std::integral_constant;
+        if (dtype == 2) go(integral_constant<int, 2>{}, integral_constant<int, 128>{});
+        else if (dtype == 1) go(integral_constant<int, 1>{}, integral_constant<int, 128>{});
+        else if (R.D == 64) go(integral_constant<int, 0>{}, integral_constant<int, 64>{});
+        else go(integral_constant<int, 0>{}, integral_constant<int, 128>{});
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------- gradient

@@ -22,7 +22,7 @@ static_assert(sizeof(PcRowsItem) == 64, "");
 
 struct PcRows {
     const PcRowsItem *items;
-    int32_t n_items, n_blocks;
+    int32_t n_items, n_blocks, block0;        // (block0: the launch's first)
     int64_t q_stride, k_stride, v_stride;     // elements from a row to the next
     const float *q_weight, *k_weight;         // [D] or null: ones
     float   eps;
@@ -35,7 +35,7 @@ struct PcRows {
     PcMsgEntry *table;
 };
 // blob: the items in the arguments (R.items is not read then), or null
-void pc_launch_rows(int dtype, const PcRows &R, const PcArgBlob *blob, hipStream_t st);
+void pc_launch_rows(int dtype, PcRows R, const PcArgBlob *blob, hipStream_t st);
 
 // The gradient.
 struct PcRowsBwdItem {
