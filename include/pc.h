@@ -105,7 +105,7 @@ typedef struct {
  * (calls of at least 512 rows x query heads of a KV head that see 3e7 scores or more) go over a copy of all that they list, 512 bytes a token and KV
  * head besides: there turned keys and queries are fp16 (off by 2^-12 of a value), but for keys above 700 and rows of queries whose norm, scaled, is above 700,
  * which are served as the others are.  Tensors as pc_attend_window asks for them:
- * q and out 16-byte aligned; and pc_attend, like pc_attend_window, refuses a stream that is being captured.  Messages are appended, grown,
+ * q and out 16-byte aligned; and pc_attend and pc_decode_step, like pc_attend_window, refuse a stream that is being captured.  Messages are appended, grown,
  * read back, forked (where they stay turned as they are), freed, swapped and closed up over as in other caches.  Their keys cannot be
  * turned without another rounding: pc_reposition* and turned forks are refused; nor is there a gradient (PC_ERR_INVALID_ARG). */
 

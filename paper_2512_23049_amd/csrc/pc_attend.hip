@@ -203,6 +203,7 @@ int32_t pc_decode_step(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, cons
     hipStream_t st = (hipStream_t)stream;
     if (c->cfg.dtype == PC_MX4)
         return pc_guarded(c, [&] {
+            if (!c->host_only && pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "decode_step: the stream is being captured, and the cache's workspace may move");
             const int32_t r = n_msgs > 0 ? pc_append_token_items(c, std::vector<int32_t>(msg_ids, msg_ids + n_msgs), k, v, st, nullptr) : PC_OK;
             return r != PC_OK || n_calls == 0 ? r : pc_attend_mx4(c, "decode_step", calls, n_calls, q, out, lse, st, nullptr);
         });

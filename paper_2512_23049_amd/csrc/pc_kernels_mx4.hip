@@ -331,20 +331,21 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
         }
         return;
     }
-    block -= P.query_blocks;
-    const int kh = block / P.n_tiles, tile = block % P.n_tiles;
-    const int slot0 = reinterpret_cast<const int32_t *>(from + P.off_tiles)[tile];
-    const char *vt = (const char *)P.v_store + ((int64_t)kh * P.slots + slot0) / PC_TILE * PC_MX4_TILE;
-    char *to = (char *)P.v_to + ((int64_t)kh * P.n_tiles + tile) * (PC_TILE * PC_D * 2);
+    for (int64_t at = block - P.query_blocks; at < (int64_t)P.n_tiles * P.n_kv_heads; at += gridDim.x - P.list_blocks - P.query_blocks) {
+        const int kh = (int)(at / P.n_tiles), tile = (int)(at % P.n_tiles);
+        const int slot0 = reinterpret_cast<const int32_t *>(from + P.off_tiles)[tile];
+        const char *vt = (const char *)P.v_store + ((int64_t)kh * P.slots + slot0) / PC_TILE * PC_MX4_TILE;
+        char *to = (char *)P.v_to + ((int64_t)kh * P.n_tiles + tile) * (PC_TILE * PC_D * 2);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int grp = (threadIdx.x >> 7) + 2 * i, d = threadIdx.x & 127;
-        const uint32_t w = reinterpret_cast<const uint32_t *>(vt + grp * 512)[mx4_word(d)];
-        const uint2 ex = *reinterpret_cast<const uint2 *>(vt + PC_MX4_CODES + grp * 32 + d / 32 * 8);
-        uint4 x;
-        x.x = mx4_values(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_values(w, ex.x, std::integral_constant<int, 1>{});
-        x.z = mx4_values(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_values(w, ex.y, std::integral_constant<int, 3>{});
-        *reinterpret_cast<uint4 *>(to + (grp * 128 + d) * 16) = x;
+        for (int i = 0; i < 2; ++i) {
+            const int grp = (threadIdx.x >> 7) + 2 * i, d = threadIdx.x & 127;
+            const uint32_t w = reinterpret_cast<const uint32_t *>(vt + grp * 512)[mx4_word(d)];
+            const uint2 ex = *reinterpret_cast<const uint2 *>(vt + PC_MX4_CODES + grp * 32 + d / 32 * 8);
+            uint4 x;
+            x.x = mx4_values(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_values(w, ex.x, std::integral_constant<int, 1>{});
+            x.z = mx4_values(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_values(w, ex.y, std::integral_constant<int, 3>{});
+            *reinterpret_cast<uint4 *>(to + (grp * 128 + d) * 16) = x;
+        }
     }
 }
 
@@ -355,7 +356,7 @@ void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st
 {
     P.list_blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>((P.n16 + (int64_t)P.n_rot * (PC_D / 2) + 255) / 256, 1024));
     P.query_blocks = (P.n_rows + 31) / 32 * ((P.n_q_heads + 3) / 4);
-    const unsigned grid = (unsigned)(P.list_blocks + P.query_blocks + P.n_tiles * P.n_kv_heads);
+    const unsigned grid = (unsigned)(P.list_blocks + P.query_blocks + std::min<int64_t>((int64_t)P.n_tiles * P.n_kv_heads, 1 << 20));
     if (blob) pc_mx4_prepare_arg_kernel<<<grid, 256, 0, st>>>(*blob, P);
     else pc_mx4_prepare_kernel<<<grid, 256, 0, st>>>(P);
 }

@@ -5,6 +5,8 @@
 
 namespace {
 
+constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;           // of 256 threads, in one dimension of a launch
+
 bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 // a strided tensor of rows of heads, each 16-byte aligned
@@ -37,7 +39,10 @@ template <class Item> int32_t stage(pc_cache *c, const std::vector<Item> &items,
 {
     const size_t bytes = sizeof(Item) * items.size();
     in_args = bytes <= PC_ARG_BYTES;
-    if (!in_args) return pc_stage_items(c, items.data(), bytes, st);
+    if (!in_args) {
+        if (pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "lists of %zu bytes: the stream is being captured, and a replay would find others in their place", bytes);
+        return pc_stage_items(c, items.data(), bytes, st);
+    }
     std::memcpy(blob.w, items.data(), bytes);
     return PC_OK;
 }
@@ -159,6 +164,7 @@ int32_t projected_backward(pc_cache *c, const pc_projected *p, int32_t n, const 
         it.block0 = (int32_t)blocks;
         blocks += (it.n + block_rows - 1) / block_rows;
     }
+    if (blocks > MOST_BLOCKS) return pc_fail(c, PC_ERR_SHAPE, "%s: too many rows", what);
     PcRowsBwd B{};
     B.block_rows = block_rows;
     B.n_items = n; B.n_blocks = (int32_t)blocks;
@@ -202,7 +208,7 @@ int32_t messages_read(pc_cache *c, int32_t n, const int32_t *msg_ids, void *k, v
             items.push_back(PcReadItem{row, (int32_t)m.slot_start, m.len, (int32_t)blocks, 0});
             row += m.len;
             blocks += (m.len + 7) / 8;
-            if (blocks > INT32_MAX / 2) return pc_fail(c, PC_ERR_SHAPE, "%s: too many tokens", what);
+            if (blocks > MOST_BLOCKS) return pc_fail(c, PC_ERR_SHAPE, "%s: too many tokens", what);
         }
     }
     if (c->host_only || items.empty() || (!k && !v)) return PC_OK;

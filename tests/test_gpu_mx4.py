@@ -227,6 +227,33 @@ def test_recorded_and_replayed():
     layer.cache.close()
 
 
+def test_what_is_not_recorded():
+    """A decode step, and what brings long lists, is refused on a stream that is being captured, before the books change."""
+    from paper_2512_23049_amd import binding as b
+    torch = __import__("torch")
+    layer = Layer4([40, 33, 64] + [1] * 200, 8, 2, reserves=[64, 64, 64] + [32] * 200)
+    k = layer.dev(layer.normal(300, 2, 128))
+    q = layer.dev(layer.normal(1, 8, 128))
+    out = torch.zeros_like(q)
+    call = layer.calls([([(0, 0)], 1, 40, 1)])
+    layer.cache.attend(call, q.data_ptr(), out.data_ptr())
+    before = [layer.cache.message_info(i) for i in layer.ids]
+    s = torch.cuda.Stream()
+    with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
+        st = torch.cuda.current_stream().cuda_stream
+        out.zero_()
+        with pytest.raises(b.PcError):
+            layer.cache.decode_step([layer.ids[1]], k.data_ptr(), k.data_ptr(), call, q.data_ptr(), out.data_ptr(), stream=st)
+        with pytest.raises(b.PcError):
+            layer.cache.append_tokens_batch(layer.ids[3:], k.data_ptr(), k.data_ptr(), stream=st)
+        with pytest.raises(b.PcError):
+            layer.cache.messages_read(layer.ids, k.data_ptr(), k.data_ptr(), stream=st)
+    torch.cuda.synchronize()
+    assert [layer.cache.message_info(i) for i in layer.ids] == before
+    layer.run([([(0, 0), (2, 50)], 1, 140, 1)], what="behind it")
+    layer.cache.close()
+
+
 def test_recorded_long_lists():
     """Lists that neither arguments nor a slot hold are recorded with the call."""
     torch = __import__("torch")
