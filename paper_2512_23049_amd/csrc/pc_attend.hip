@@ -141,14 +141,14 @@ static int32_t attend_impl(pc_cache *c, const pc_call *calls, int32_t n_calls, c
         ProfScope ps(c, 8, st);
         const PcGatherItem *items = (const PcGatherItem *)(w + P.lay.kg_items);
         const int32_t *off = (const int32_t *)(w + P.lay.seg_kvoff);
-        if (P.mx4_rows) pc_launch_gather_mx4(L, items, P.n_kg_items, P.kg_tiles, off, c->counters_dev + 2 * PC_ONE_COUNTERS, P.mark_value, st);
+        if (P.mx4_rows) pc_launch_gather_mx4(L, items, P.n_kg_items, P.kg_tiles, off, c->counters_dev + PC_MX4_MARK, P.mark_value, st);
         else pc_launch_gather(L, items, P.n_kg_items, P.kg_tiles, off, st);
         PC_HIP(c, hipGetLastError());
     }
     if (P.n_pre_pk > 0) {
         ProfScope ps(c, 2, st);
         L.items = (const PcItem *)(w + P.lay.items_pk);
-        if (P.mx4_rows) pc_launch_prefill_f16(L, P.n_pre_pk, c->counters_dev + 2 * PC_ONE_COUNTERS, P.mark_value, st);
+        if (P.mx4_rows) pc_launch_prefill_f16(L, P.n_pre_pk, c->counters_dev + PC_MX4_MARK, P.mark_value, st);
         else pc_launch_prefill_bf16(L, P.n_pre_pk, true, st);
         PC_HIP(c, hipGetLastError());
     }

@@ -60,7 +60,7 @@ struct pc_cache {
     void *storage = nullptr; bool owns_storage = false;
     void *k_store = nullptr, *v_store = nullptr;
     PcMsgEntry *table_dev = nullptr;
-    uint32_t *counters_dev = nullptr;                    // PcOne::counters of pc_attend, then those of pc_attend_static, then the mark of pc_attend_mx4
+    uint32_t *counters_dev = nullptr;                    // PC_CACHE_WORDS
     uint32_t mark_epoch_mx4 = 0;                         // what its last call marks with
     double *inv_freq_dev = nullptr;
     void *ws = nullptr; size_t ws_cap = 0;

@@ -16,7 +16,6 @@
 
 #include <type_traits>
 
-#define LAZY_LOG2 64.0f
 #define TURNS 4               // rotations that a wave has at hand at once
 
 namespace {
@@ -40,19 +39,31 @@ __device__ __forceinline__ int lane_again()
 __device__ __forceinline__ int32_t listed(const int32_t *p) { return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(p)); }
 __device__ __forceinline__ win_i32x4 listed4(const void *p) { return *reinterpret_cast<const __attribute__((address_space(4))) win_i32x4 *>(reinterpret_cast<uintptr_t>(p)); }
 
+
+constexpr int TILES = PC_WIN_STEP_TILES, RING = 4, AHEAD = RING - 1;
+// of a tile in the ring: codes of keys and of values, exponents of keys and of values (256 bytes each: a direct load's lanes)
+constexpr int VALUES = PC_MX4_CODES, K_EXPS = 2 * PC_MX4_CODES, V_EXPS = K_EXPS + 256, TILE = V_EXPS + 256, SLOT = TILES * TILE;
+
 }  // namespace
 
-template <int NW>
-__global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(PcWin W, PcWinShared S)
+template <int NW> struct SharedLds {
+    unsigned char kv[RING][SLOT] __attribute__((aligned(1024)));
+    unsigned char v[2][TILES][PC_TILE * PC_D * 2] __attribute__((aligned(1024)));       // values as a bf16 cache has them (or in fp16), of this step and the next
+    _Float16 rot[NW][TURNS][2][PC_D / 2] __attribute__((aligned(16)));                  // cosines, sines
+    int4 see[NW][16];                                    // what a column's call sees of the wave's visit: pos0, n_tok, sink, lo
+    double freq[PC_D / 2];
+};
+// HALF: probabilities and values in fp16, where no value of the cache is outside it.  A probability of a column's reference is 2^6 then, and the reference
+// moves where one would be above 2^15: what is 2^20 below a column's largest still is a normal number, and 2^31 below it one of a few bits.
+template <int NW, bool HALF> __device__ __forceinline__ void shared_decode(const PcWin &W, const PcWinShared &S, SharedLds<NW> &lds)
 {
-    constexpr int TILES = PC_WIN_STEP_TILES, RING = 4, AHEAD = RING - 1, LOADS = 16 / NW;
-    // of a tile in the ring: codes of keys and of values, exponents of keys and of values (256 bytes each: a direct load's lanes)
-    constexpr int VALUES = PC_MX4_CODES, K_EXPS = 2 * PC_MX4_CODES, V_EXPS = K_EXPS + 256, TILE = V_EXPS + 256, SLOT = TILES * TILE;
-    __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING][SLOT];
-    __shared__ __attribute__((aligned(1024))) unsigned char s_v[2][TILES][PC_TILE * PC_D * 2];        // values as a bf16 cache has them, of this step and the next
-    __shared__ __attribute__((aligned(16))) float2 s_rot[NW][TURNS][PC_D / 2];
-    __shared__ int4 s_see[NW][16];                       // what a column's call sees of the wave's visit: pos0, n_tok, sink, lo
-    __shared__ double s_freq[PC_D / 2];
+    constexpr int LOADS = 16 / NW;
+    constexpr float LAZY_LOG2 = HALF ? 15.f : 64.f, ABOVE = HALF ? 6.f : 0.f;
+    auto &s_kv = lds.kv;
+    auto &s_v = lds.v;
+    auto &s_rot = lds.rot;
+    auto &s_see = lds.see;
+    auto &s_freq = lds.freq;
 
     const int kh = blockIdx.x % W.n_kv_heads;
     const win_i32x4 i0 = listed4(S.items + blockIdx.x / W.n_kv_heads), i1 = listed4((const char *)(S.items + blockIdx.x / W.n_kv_heads) + 16);
@@ -99,10 +110,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
         int all = fine;
         all &= __shfl_xor(all, 16);
         all &= __shfl_xor(all, 32);
-        if (!all) {
+        const float by = W.scale_log2 / unit;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
-        }
+        for (int i = 0; i < 4; ++i) q[i] = all ? mx4_halves(q[i], by) : make_uint4(0x7E007E00u, 0x7E007E00u, 0x7E007E00u, 0x7E007E00u);
     }
     __syncthreads();
 
@@ -162,8 +172,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             const uint32_t w = *(lds4)(uintptr_t)(conv_codes + at);
             const mx4_u32x2 ex = *(lds8)(uintptr_t)(conv_exps + at);
             uint4 x;
-            x.x = mx4_values(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_values(w, ex.x, std::integral_constant<int, 1>{});
-            x.z = mx4_values(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_values(w, ex.y, std::integral_constant<int, 3>{});
+            x.x = mx4_numbers<HALF>(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_numbers<HALF>(w, ex.x, std::integral_constant<int, 1>{});
+            x.z = mx4_numbers<HALF>(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_numbers<HALF>(w, ex.y, std::integral_constant<int, 3>{});
             *(lds16_out)(uintptr_t)(conv_to + to * (TILES * PC_TILE * PC_D * 2) + 64 * NW * i * 16) = __builtin_bit_cast(win_i32x4, x);
         }
     };
@@ -211,9 +221,6 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             if (a == 0) s_see[wave][n] = make_int4(0, 0, 0, 0);
 #pragma unroll 1
             for (int e = first; e < end; e += TURNS) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)              // (its 32 numbers, taken apart once and kept, would not fit the registers)
-                    asm volatile("" : "+v"(q[i].x), "+v"(q[i].y), "+v"(q[i].z), "+v"(q[i].w));
                 int of = -1;                             // which of the rotations is the lane's
                 asm volatile("" ::: "memory");
                 win_i32x4 x[TURNS], y[TURNS];            // (all at once: one latency)
@@ -230,24 +237,18 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
                     of = mine ? i : of;
                     const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y[i].y << 32) | (uint32_t)y[i].x);
                     const float2 cs = mx4_rotation((double)turn * s_freq[lane]);
-                    s_rot[wave][i][lane] = make_float2(cs.x * W.scale_log2, cs.y * W.scale_log2);
+                    s_rot[wave][i][0][lane] = (_Float16)cs.x; s_rot[wave][i][1][lane] = (_Float16)cs.y;
                 }
                 asm volatile("" ::: "memory");
-                const float4 *rot = reinterpret_cast<const float4 *>(&s_rot[wave][max(of, 0)][16 * a]);
+                const uint4 *rot = reinterpret_cast<const uint4 *>(&s_rot[wave][max(of, 0)][0][16 * a]);          // (sines: eight further)
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {            // dims 16 a + 4 s, and 64 up
-                    const uint4 lq = q[s >> 1], hq = q[2 + (s >> 1)];
-                    const uint32_t lw[2] = {s & 1 ? lq.z : lq.x, s & 1 ? lq.w : lq.y}, hw[2] = {s & 1 ? hq.z : hq.x, s & 1 ? hq.w : hq.y};
-                    const float4 r0 = rot[2 * s], r1 = rot[2 * s + 1];
-                    const float x0 = bf_lo(lw[0]), x1 = bf_hi(lw[0]), x2 = bf_lo(lw[1]), x3 = bf_hi(lw[1]);
-                    const float y0 = bf_lo(hw[0]), y1 = bf_hi(hw[0]), y2 = bf_lo(hw[1]), y3 = bf_hi(hw[1]);
-                    const float u[4] = {x0 * r0.x - y0 * r0.y, x1 * r0.z - y1 * r0.w, x2 * r1.x - y2 * r1.y, x3 * r1.z - y3 * r1.w};
-                    const float v[4] = {x0 * r0.y + y0 * r0.x, x1 * r0.w + y1 * r0.z, x2 * r1.y + y2 * r1.x, x3 * r1.w + y3 * r1.z};
-                    int hi, rest;
-                    mx4_pieces(u, unit, hi, rest);
-                    q_hi[s] = of >= 0 ? hi : q_hi[s]; q_lo[s] = of >= 0 ? rest : q_lo[s];
-                    mx4_pieces(v, unit, hi, rest);
-                    q_hi[4 + s] = of >= 0 ? hi : q_hi[4 + s]; q_lo[4 + s] = of >= 0 ? rest : q_lo[4 + s];
+                    int u_hi, u_rest, v_hi, v_rest;
+                    const uint4 c = rot[s >> 1], t = rot[8 + (s >> 1)];
+                    if (s & 1) mx4_turned<2>(q[s >> 1], q[2 + (s >> 1)], c, t, u_hi, u_rest, v_hi, v_rest);
+                    else mx4_turned<0>(q[s >> 1], q[2 + (s >> 1)], c, t, u_hi, u_rest, v_hi, v_rest);
+                    q_hi[s] = of >= 0 ? u_hi : q_hi[s]; q_lo[s] = of >= 0 ? u_rest : q_lo[s];
+                    q_hi[4 + s] = of >= 0 ? v_hi : q_hi[4 + s]; q_lo[4 + s] = of >= 0 ? v_rest : q_lo[4 + s];
                 }
                 asm volatile("" ::: "memory");
             }
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
                 const bool up = mx > limit;
-                const float m_new = up ? ref + mx : m_ref, by = up ? m_new - ref : 0.f, f = !up ? 1.f : m_ref == -INFINITY ? 0.f : ex2(-by);
+                const float m_new = up ? ref + mx - ABOVE : m_ref, by = up ? m_new - ref : 0.f, f = !up ? 1.f : m_ref == -INFINITY ? 0.f : ex2(-by);
                 m_ref = m_new;
                 sums *= f;
 #pragma unroll
@@ -335,13 +336,14 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             for (int t = 0; t < TILES; ++t) {
                 uint32_t pk[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) pk[j] = pack_bf16(ex2(sc[8 * t + 2 * j]), ex2(sc[8 * t + 2 * j + 1]));
+                for (int j = 0; j < 4; ++j) pk[j] = mx4_pack<HALF>(ex2(sc[8 * t + 2 * j]), ex2(sc[8 * t + 2 * j + 1]));
                 p[t] = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
             }
             // (the denominator: of the probabilities as the products take them, so that their rounding cancels)
-            const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+            constexpr uint32_t ONES = HALF ? 0x3C003C00u : 0x3F803F80u;
+            const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(ONES, ONES, ONES, ONES));
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) sums = MFMA16(ones, p[t], sums);
+            for (int t = 0; t < TILES; ++t) sums = mx4_mfma16<HALF>(ones, p[t], sums);
             __builtin_amdgcn_sched_barrier(0);           // (values read any earlier would not fit the registers)
             const int lv = lane_again();
             const unsigned vt = (unsigned)(uintptr_t)&s_v[step & 1][0][0] + (unsigned)(((lv >> 4) * PC_D + (lv & 15)) * 16);
@@ -349,7 +351,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
             for (int db = 0; db < 8; ++db)
 #pragma unroll
                 for (int t = 0; t < TILES; ++t)
-                    acc[db] = MFMA16(__builtin_bit_cast(bf16x8, *(lds16)(uintptr_t)(vt + t * (PC_TILE * PC_D * 2) + 256 * db)), p[t], acc[db]);
+                    acc[db] = mx4_mfma16<HALF>(__builtin_bit_cast(bf16x8, *(lds16)(uintptr_t)(vt + t * (PC_TILE * PC_D * 2) + 256 * db)), p[t], acc[db]);
         }
         if (step + 1 < n_steps) convert(place == RING - 1 ? 0 : place + 1, (step + 1) & 1);
         // (what is asked for comes behind this step's products: the waves that have none are at it meanwhile)
@@ -361,6 +363,13 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(P
 #pragma unroll
     for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(W.part_o + at * PC_D + 16 * db + 4 * a) = acc[db];
     if (a == 0) *reinterpret_cast<float2 *>(W.part_ml + at * 2) = make_float2(l == 0.f ? -INFINITY : m_ref, l);
+}
+
+template <int NW> __global__ __launch_bounds__(64 * NW, NW / 4) void pc_mx4_shared_decode_kernel(PcWin W, PcWinShared S)
+{
+    __shared__ SharedLds<NW> lds;
+    if (listed((const int32_t *)S.bf16_only) == 0) shared_decode<NW, true>(W, S, lds);
+    else shared_decode<NW, false>(W, S, lds);
 }
 
 void pc_launch_win_shared_decode_mx4(const PcWin &W, const PcWinShared &S, hipStream_t st)

@@ -172,6 +172,7 @@ __device__ __forceinline__ void rows_block(const PcRows &R, const PcRowsItem *it
             bad[u] = all != 0;
             const int e0 = mx4_exponent(m0), e1 = mx4_exponent(m1);
             const float p0 = mx4_power(0.f, -e0), p1 = mx4_power(0.f, -e1);
+            if (there && head_ok && !bad[u] && ((m0 > 0.f && abs(e0) > PC_MX4_HALF) || (m1 > 0.f && abs(e1) > PC_MX4_HALF))) *R.wide = 1;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
                 const bool none = bad[u] || !there;

@@ -18,6 +18,7 @@
 #define PC_MX4_CODES 2048             // bytes of codes in a tile of keys or of values
 #define PC_MX4_TILE (PC_TILE * PC_MX4_ROW)
 #define PC_MX4_E_MAX 60
+#define PC_MX4_HALF 13                // exponents from -13 to 13: the values are exact, and normal numbers, in fp16
 #define PC_MX4_NAN 255                // exponent of a block of keys that are NaN
 
 struct PcWin;

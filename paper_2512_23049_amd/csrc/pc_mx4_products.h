@@ -66,6 +66,36 @@ template <int PAIR> __device__ __forceinline__ uint32_t mx4_values(uint32_t w, u
     return mx4_lowered<PAIR & 1>(x & 0x7FFF7FFFu, d) | (x & 0x80008000u);
 }
 
+// The same in fp16, which holds probabilities to 2^-12 where bf16 has 2^-8: exponents from -13 to 13 (others give any number).
+template <int PAIR> __device__ __forceinline__ uint32_t mx4_halfs(uint32_t w, uint32_t d, std::integral_constant<int, PAIR>)
+{
+    static_assert(PC_MX4_HALF == 13 && PC_MX4_E_MAX == 60, "");
+    const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 0x1p13f, PAIR));
+    const mx4_u16x2 e = __builtin_bit_cast(mx4_u16x2, __builtin_amdgcn_perm(0u, d, (PAIR & 1) == 0 ? 0x0C010C00u : 0x0C030C02u));
+    const mx4_u16x2 by = __builtin_elementwise_sub_sat(e, (mx4_u16x2){47, 47}) << (mx4_u16x2){10, 10};
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(mx4_u16x2, x & 0x7FFF7FFFu), by)) | (x & 0x80008000u);
+}
+// two probabilities for the products, and the products, in fp16 or bf16
+typedef _Float16 mx4_f16x8 __attribute__((ext_vector_type(8)));
+template <bool HALF> __device__ __forceinline__ uint32_t mx4_pack(float a, float b)
+{
+    if constexpr (HALF) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
+    } else return pack_bf16(a, b);
+}
+template <bool HALF> __device__ __forceinline__ f32x4 mx4_mfma16(bf16x8 a, bf16x8 b, f32x4 c)
+{
+    if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(mx4_f16x8, a), __builtin_bit_cast(mx4_f16x8, b), c, 0, 0, 0);
+    else return MFMA16(a, b, c);
+}
+template <bool HALF, int PAIR> __device__ __forceinline__ uint32_t mx4_numbers(uint32_t w, uint32_t d, std::integral_constant<int, PAIR> p)
+{
+    if constexpr (HALF) return mx4_halfs(w, d, p);
+    else return mx4_values(w, d, p);
+}
+
 // c + the two probabilities, as the products take them: their rounding cancels where a row has few large ones (errors against 64 bits, 40
 // rows: 2.43e-3 -> 2.41e-3; calls of 8 to 200 rows take 1.2 us less than with two additions of what was not rounded yet)
 typedef __bf16 mx4_bf16x2 __attribute__((ext_vector_type(2)));
@@ -92,7 +122,7 @@ __device__ __forceinline__ float mx4_top(float top, uint32_t w, bool &fine)
 // between 128 and 256 of it (448 is the largest number of the pieces; one above is NaN).
 __device__ __forceinline__ float mx4_unit(float top)
 {
-    const int e = max(-100, min(100, (int)(__float_as_uint(top * 1.4142137f) >> 23 & 255) - 134));
+    const int e = max(-100, min(121, (int)(__float_as_uint(top * 1.4142137f) >> 23 & 255) - 134));
     return __uint_as_float((uint32_t)(127 + e) << 23);
 }
 __device__ __forceinline__ int mx4_e4m3(const float (&x)[4], float unit)
@@ -110,6 +140,39 @@ __device__ __forceinline__ void mx4_pieces(const float (&x)[4], float unit, int 
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, unit, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, unit, true);
     const float y[4] = {x[0] - a[0], x[1] - a[1], x[2] - b[0], x[3] - b[1]};
     rest = mx4_e4m3(y, unit * 0.0625f);
+}
+
+// The same of a row of queries in fp16, in that unit (128 to 256 at most: off by 2^-12 of a value, a sixteenth of what pieces are off by), two values
+// an instruction: 16 values and their partners in the upper half, from what came, scaled, by 16 rotations (cosines and sines, in fp16).
+typedef _Float16 mx4_f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ mx4_f16x2 mx4_half(uint32_t x) { return __builtin_bit_cast(mx4_f16x2, x); }
+// eight bf16 numbers times `by`
+__device__ __forceinline__ uint4 mx4_halves(uint4 x, float by)
+{
+    return make_uint4(pack_f16(bf_lo(x.x) * by, bf_hi(x.x) * by), pack_f16(bf_lo(x.y) * by, bf_hi(x.y) * by),
+                      pack_f16(bf_lo(x.z) * by, bf_hi(x.z) * by), pack_f16(bf_lo(x.w) * by, bf_hi(x.w) * by));
+}
+__device__ __forceinline__ int mx4_e4m3(mx4_f16x2 x, mx4_f16x2 y, float unit)
+{
+    mx4_s16x2 r;
+    asm("" : "=v"(r));
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, x, unit, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, y, unit, true);
+    return __builtin_bit_cast(int, r);
+}
+__device__ __forceinline__ void mx4_pieces(mx4_f16x2 x, mx4_f16x2 y, int &hi, int &rest)
+{
+    hi = mx4_e4m3(x, y, 1.f);
+    rest = mx4_e4m3(x - __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), y - __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true), 0.0625f);
+}
+// four values (words A and A + 1 of eight) and their partners
+template <int A> __device__ __forceinline__ void mx4_turned(uint4 low, uint4 high, uint4 c, uint4 s, int &u_hi, int &u_rest, int &v_hi, int &v_rest)
+{
+    auto word = [](uint4 x, int i) __attribute__((always_inline)) { return mx4_half(i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w); };
+    const mx4_f16x2 x0 = word(low, A), x1 = word(low, A + 1), y0 = word(high, A), y1 = word(high, A + 1);
+    const mx4_f16x2 c0 = word(c, A), c1 = word(c, A + 1), s0 = word(s, A), s1 = word(s, A + 1);
+    mx4_pieces(x0 * c0 - y0 * s0, x1 * c1 - y1 * s1, u_hi, u_rest);
+    mx4_pieces(x0 * s0 + y0 * c0, x1 * s1 + y1 * c1, v_hi, v_rest);
 }
 
 #endif

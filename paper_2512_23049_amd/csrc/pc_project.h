@@ -33,6 +33,7 @@ struct PcRows {
     const double *inv_freq;
     void   *k_store, *v_store;
     PcMsgEntry *table;
+    uint32_t *wide;                           // (4 bits) set where a value is outside what PC_MX4_HALF says
 };
 // blob: the items in the arguments (R.items is not read then), or null
 void pc_launch_rows(int dtype, PcRows R, const PcArgBlob *blob, hipStream_t st);

@@ -242,7 +242,7 @@ int32_t pc_write_rows(pc_cache *c, PcRows R, std::vector<PcRowsItem> &items, hip
     }
     R.n_items = (int32_t)items.size(); R.n_blocks = (int32_t)blocks;
     R.n_q_heads = c->cfg.n_q_heads; R.n_kv_heads = c->cfg.n_kv_heads; R.D = c->D;
-    R.slots = c->slots; R.inv_freq = c->inv_freq_dev; R.k_store = c->k_store; R.v_store = c->v_store; R.table = c->table_dev;
+    R.slots = c->slots; R.inv_freq = c->inv_freq_dev; R.k_store = c->k_store; R.v_store = c->v_store; R.table = c->table_dev; R.wide = c->counters_dev + PC_MX4_WIDE;
     PcArgBlob blob;
     bool in_args = false;
     const int32_t rc = stage(c, items, blob, in_args, st);

@@ -83,6 +83,7 @@ struct PcWinShared {
     const PcWinSharedCall *calls;
     int32_t n_items;
     int32_t wide;             // 1: 16 waves (groups of columns) a workgroup, 0: 8
+    const uint32_t        *bf16_only;         // (4 bits) not 0: some values are outside fp16
 };
 
 // ---- the gradient ----

@@ -770,7 +770,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
             T.rot_run = (float2 *)(ws + L.rot_run);
             T.q = q; T.q_abs = (float4 *)(ws + L.q_abs); T.q_unit = (float *)(ws + L.q_unit);
             T.inv_freq = c->inv_freq_dev; T.slots = c->slots; T.v_store = c->v_store; T.v_to = ws + L.v_tiles;
-            if (mark) { T.mark = c->counters_dev + 2 * PC_ONE_COUNTERS; T.mark_value = mark; }
+            if (mark) { T.mark = c->counters_dev + PC_MX4_MARK; T.mark_value = mark; }
             pc_launch_mx4_prepare(T, in_args ? &blob : nullptr, st);
         } else {
         PcWinTurns T{};
@@ -800,7 +800,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     if (!P.sh_items.empty()) {
         ProfScope ps(c, 3, st);
         const PcWinShared S{(const PcWinSharedItem *)(ws + L.sh_items), (const PcWinVisit *)(ws + L.sh_visits), (const PcWinSee *)(ws + L.sh_sees),
-                            (const PcWinSharedCall *)(ws + L.sh_calls), (int32_t)P.sh_items.size(), P.sh_wide};
+                            (const PcWinSharedCall *)(ws + L.sh_calls), (int32_t)P.sh_items.size(), P.sh_wide, c->counters_dev + PC_MX4_WIDE};
         if (mx4) pc_launch_win_shared_decode_mx4(W, S, st);
         else pc_launch_win_shared_decode_bf16(W, S, st);
         PC_HIP(c, hipGetLastError());
@@ -809,7 +809,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         ProfScope ps(c, bf16 ? 2 : 5, st);
         W.items = (const PcWinItem *)(ws + L.pre);
         const PcMx4Rows M{(const float4 *)(ws + L.q_abs), (const float *)(ws + L.q_unit), (const int32_t *)(ws + L.places), ws + L.v_tiles,
-                          (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size(), mark, mark ? c->counters_dev + 2 * PC_ONE_COUNTERS : nullptr};
+                          (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size(), mark, mark ? c->counters_dev + PC_MX4_MARK : nullptr};
         if (mx4) pc_launch_win_prefill_mx4(W, M, (int)P.pre.size(), st);
         else if (bf16) pc_launch_win_prefill_bf16(W, (int)P.pre.size(), st);
         else pc_launch_win_attend_f32(W, (int)P.pre.size(), c->D, st);
