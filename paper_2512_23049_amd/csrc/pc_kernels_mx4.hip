@@ -331,6 +331,7 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
         }
         return;
     }
+    const bool half = *P.bf16_only == 0;
     for (int64_t at = block - P.query_blocks; at < (int64_t)P.n_tiles * P.n_kv_heads; at += gridDim.x - P.list_blocks - P.query_blocks) {
         const int kh = (int)(at / P.n_tiles), tile = (int)(at % P.n_tiles);
         const int slot0 = reinterpret_cast<const int32_t *>(from + P.off_tiles)[tile];
@@ -342,8 +343,13 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
             const uint32_t w = reinterpret_cast<const uint32_t *>(vt + grp * 512)[mx4_word(d)];
             const uint2 ex = *reinterpret_cast<const uint2 *>(vt + PC_MX4_CODES + grp * 32 + d / 32 * 8);
             uint4 x;
-            x.x = mx4_values(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_values(w, ex.x, std::integral_constant<int, 1>{});
-            x.z = mx4_values(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_values(w, ex.y, std::integral_constant<int, 3>{});
+            auto numbers = [&](auto half) __attribute__((always_inline)) {
+                constexpr bool HALF = decltype(half)::value;
+                x.x = mx4_numbers<HALF>(w, ex.x, std::integral_constant<int, 0>{}); x.y = mx4_numbers<HALF>(w, ex.x, std::integral_constant<int, 1>{});
+                x.z = mx4_numbers<HALF>(w, ex.y, std::integral_constant<int, 2>{}); x.w = mx4_numbers<HALF>(w, ex.y, std::integral_constant<int, 3>{});
+            };
+            if (half) numbers(std::true_type{});
+            else numbers(std::false_type{});
             *reinterpret_cast<uint4 *>(to + (grp * 128 + d) * 16) = x;
         }
     }
@@ -373,21 +379,20 @@ void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st
 // Bound: the vector unit, 140 instructions a tile and wave of which 49 turn queries (messages of 160 tokens: every fifth tile is another's), beside
 // 512 cycles of matrix work; 64 heads over 8, 1024 rows over 13k tokens: 0.6 PFLOP/s, which is why long prefills go another way.  Small ones
 // are chains of latencies: 77 rows over 5 messages 16.5 us, in splits of six tiles (of four, three or two no less, and more to merge).
-#define LAZY_LOG2 64.0f
-#define MFMA32(a, b, c) __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0)
 
 namespace {
 __device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "memory"); }
+// a tile's place in the ring: codes of keys, values, exponents
+constexpr int ROWS_RING = 4, ROWS_SLOT = PC_MX4_CODES + PC_TILE * PC_D * 2 + 256;
 }  // namespace
 
-__global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Rows M)
+// HALF: probabilities and values in fp16, where no value of the cache is outside it; the reference of a row keeps its largest probability between 2^-4
+// (none yet seen) and 2^15.
+template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, const PcMx4Rows &M, unsigned char *s_kv, float2 (*s_rot)[PC_D / 2])
 {
-    constexpr int RING = 4, AHEAD = 3, LOADS = 3;
-    constexpr int VALUES = PC_MX4_CODES, EXPS = VALUES + PC_TILE * PC_D * 2, SLOT = EXPS + 256;        // of a place in the ring: codes of keys, values, exponents
-    __shared__ __attribute__((aligned(1024))) unsigned char s_kv[RING * SLOT];
-    __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
-
-    if (M.mark && *M.mark != M.mark_value) return;       // (the walk in front of this one served every call)
+    constexpr int RING = ROWS_RING, AHEAD = 3, LOADS = 3;
+    constexpr int VALUES = PC_MX4_CODES, EXPS = VALUES + PC_TILE * PC_D * 2, SLOT = ROWS_SLOT;
+    constexpr float LAZY_LOG2 = HALF ? 15.f : 64.f, LOWEST = HALF ? -4.f : -64.f, ABOVE = HALF ? 6.f : 0.f;
     const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
     const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
     const int g = W.n_q_heads / W.n_kv_heads;
@@ -489,11 +494,11 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const bool now = mx > -INFINITY, need = mx > LAZY_LOG2 || (!seen && now && mx < -LAZY_LOG2);
+        const bool now = mx > -INFINITY, need = mx > LAZY_LOG2 || (!seen && now && mx < LOWEST);
         seen |= now;
         all_seen = __builtin_amdgcn_ballot_w64(seen) == ~0ull;
         if (__builtin_amdgcn_ballot_w64(need) != 0) {
-            const float shift = need ? mx : 0.f, alpha = ex2(-fmaxf(shift, 0.f));       // (down: nothing has been added yet)
+            const float shift = !need ? 0.f : mx > 0.f ? mx - ABOVE : mx, alpha = ex2(-fmaxf(shift, 0.f));       // (down: nothing has been added yet)
             l_run *= alpha;
 #pragma unroll
             for (int db = 0; db < 4; ++db) acc[db] *= alpha;
@@ -565,13 +570,13 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
                     float ps = 0.f;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
-                        pk[r] = pack_bf16(ex2(s[2 * r]), ex2(s[2 * r + 1]));
-                        ps = mx4_sum(pk[r], ps);
+                        pk[r] = mx4_pack<HALF>(ex2(s[2 * r]), ex2(s[2 * r + 1]));
+                        ps = mx4_sum<HALF>(pk[r], ps);
                     }
                     l_run += ps;
                     const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
 #pragma unroll
-                    for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(fr[f], p[f >> 2], acc[f & 3]);
+                    for (int f = 0; f < 8; ++f) acc[f & 3] = mx4_mfma32<HALF>(fr[f], p[f >> 2], acc[f & 3]);
                 }
                 asked += RING;
                 ahead.pass(RING - 1);
@@ -606,8 +611,8 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
                 float ps = 0.f;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
-                    pk[r] = pack_bf16(ex2(s[2 * r]), ex2(s[2 * r + 1]));
-                    ps = mx4_sum(pk[r], ps);
+                    pk[r] = mx4_pack<HALF>(ex2(s[2 * r]), ex2(s[2 * r + 1]));
+                    ps = mx4_sum<HALF>(pk[r], ps);
                 }
                 const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
                 bf16x8 fr[8];
@@ -615,7 +620,7 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
                 for (int f = 0; f < 8; ++f) fr[f] = *(lds_frag)(v_rd + at + ((f >> 2) * 2 * PC_D + 32 * (f & 3)) * 16);
                 l_run += ps;
 #pragma unroll
-                for (int f = 0; f < 8; ++f) acc[f & 3] = MFMA32(fr[f], p[f >> 2], acc[f & 3]);
+                for (int f = 0; f < 8; ++f) acc[f & 3] = mx4_mfma32<HALF>(fr[f], p[f >> 2], acc[f & 3]);
             }
             ++t;
             if (t < T) walk.next();
@@ -673,6 +678,15 @@ __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Ro
         ml[0] = l == 0.f ? -INFINITY : m_ref;
         ml[1] = l;
     }
+}
+
+__global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Rows M)
+{
+    __shared__ __attribute__((aligned(1024))) unsigned char s_kv[ROWS_RING * ROWS_SLOT];
+    __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
+    if (M.mark && *M.mark != M.mark_value) return;       // (the walk in front of this one served every call)
+    if (*M.bf16_only == 0) mx4_rows<true>(W, M, s_kv, s_rot);
+    else mx4_rows<false>(W, M, s_kv, s_rot);
 }
 
 void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, hipStream_t st)

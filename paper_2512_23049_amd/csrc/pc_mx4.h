@@ -38,10 +38,11 @@ struct PcMx4Prepare {
     const double *inv_freq;
     int64_t       slots;
     const void   *v_store;
-    void         *v_to;               // [n_kv_heads][4 n_tiles][128][8]: the tiles' values as a bf16 cache has them
+    void         *v_to;               // [n_kv_heads][4 n_tiles][128][8]: the tiles' values as a bf16 cache has them, or so in fp16
     int32_t       list_blocks, query_blocks;          // of the grid
     const uint32_t *mark;             // null, or: nothing is done unless *mark is mark_value
     uint32_t      mark_value;
+    const uint32_t *bf16_only;        // not 0: some values of the cache are outside fp16
 };
 void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st);
 // What the attention of rows needs besides PcWin (whose v_store and rot_q are not read).
@@ -53,7 +54,7 @@ struct PcMx4Rows {
     int64_t        v_slots;
     int32_t        n_rows;
     uint32_t       mark_value;        // as in PcMx4Prepare
-    const uint32_t *mark;
+    const uint32_t *mark, *bf16_only; // (as there)
 };
 void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, hipStream_t st);
 

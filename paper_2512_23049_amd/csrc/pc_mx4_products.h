@@ -96,12 +96,19 @@ template <bool HALF, int PAIR> __device__ __forceinline__ uint32_t mx4_numbers(u
     else return mx4_values(w, d, p);
 }
 
-// c + the two probabilities, as the products take them: their rounding cancels where a row has few large ones (errors against 64 bits, 40
-// rows: 2.43e-3 -> 2.41e-3; calls of 8 to 200 rows take 1.2 us less than with two additions of what was not rounded yet)
+// c + the two probabilities, as the products take them: their rounding cancels where a row has few large ones (calls of 8 to 200 rows take 1.2 us
+// less than with two additions of what was not rounded yet)
 typedef __bf16 mx4_bf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ float mx4_sum(uint32_t p, float c)
+typedef _Float16 mx4_f16x2 __attribute__((ext_vector_type(2)));
+template <bool HALF> __device__ __forceinline__ float mx4_sum(uint32_t p, float c)
 {
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx4_bf16x2, p), __builtin_bit_cast(mx4_bf16x2, 0x3F803F80u), c, false);
+    if constexpr (HALF) return __builtin_amdgcn_fdot2(__builtin_bit_cast(mx4_f16x2, p), (mx4_f16x2){(_Float16)1.f, (_Float16)1.f}, c, false);
+    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(mx4_bf16x2, p), __builtin_bit_cast(mx4_bf16x2, 0x3F803F80u), c, false);
+}
+template <bool HALF> __device__ __forceinline__ f32x16 mx4_mfma32(bf16x8 a, bf16x8 b, f32x16 c)
+{
+    if constexpr (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(mx4_f16x8, a), __builtin_bit_cast(mx4_f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
 // (cos, sin) of a turn: positions are below 2^30 and theta is at least 1 (pc_cache_create), so that what queries are turned by is below 3 x 2^30
@@ -144,7 +151,6 @@ __device__ __forceinline__ void mx4_pieces(const float (&x)[4], float unit, int 
 
 // The same of a row of queries in fp16, in that unit (128 to 256 at most: off by 2^-12 of a value, a sixteenth of what pieces are off by), two values
 // an instruction: 16 values and their partners in the upper half, from what came, scaled, by 16 rotations (cosines and sines, in fp16).
-typedef _Float16 mx4_f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ mx4_f16x2 mx4_half(uint32_t x) { return __builtin_bit_cast(mx4_f16x2, x); }
 // eight bf16 numbers times `by`
 __device__ __forceinline__ uint4 mx4_halves(uint4 x, float by)

@@ -770,6 +770,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
             T.rot_run = (float2 *)(ws + L.rot_run);
             T.q = q; T.q_abs = (float4 *)(ws + L.q_abs); T.q_unit = (float *)(ws + L.q_unit);
             T.inv_freq = c->inv_freq_dev; T.slots = c->slots; T.v_store = c->v_store; T.v_to = ws + L.v_tiles;
+            T.bf16_only = c->counters_dev + PC_MX4_WIDE;
             if (mark) { T.mark = c->counters_dev + PC_MX4_MARK; T.mark_value = mark; }
             pc_launch_mx4_prepare(T, in_args ? &blob : nullptr, st);
         } else {
@@ -809,7 +810,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         ProfScope ps(c, bf16 ? 2 : 5, st);
         W.items = (const PcWinItem *)(ws + L.pre);
         const PcMx4Rows M{(const float4 *)(ws + L.q_abs), (const float *)(ws + L.q_unit), (const int32_t *)(ws + L.places), ws + L.v_tiles,
-                          (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size(), mark, mark ? c->counters_dev + PC_MX4_MARK : nullptr};
+                          (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size(), mark, mark ? c->counters_dev + PC_MX4_MARK : nullptr, c->counters_dev + PC_MX4_WIDE};
         if (mx4) pc_launch_win_prefill_mx4(W, M, (int)P.pre.size(), st);
         else if (bf16) pc_launch_win_prefill_bf16(W, (int)P.pre.size(), st);
         else pc_launch_win_attend_f32(W, (int)P.pre.size(), c->D, st);

@@ -169,6 +169,38 @@ def test_many_rows_over_long_lists(spoilt):
     layer.cache.close()
 
 
+@pytest.mark.parametrize("powers", [(13, -11), (14, 0), (0, -16), (40, -40)])
+def test_values_inside_and_outside_fp16(powers):
+    """Values by powers of two that fp16 holds, and that it does not, for single tokens that share their messages and for rows, short and long: each sees
+    those of one power alone, with scores from near zero to some tens, and long lists of keys of small probabilities beside one of a large one."""
+    up, down = powers
+
+    def spoil(i, k, v):
+        v *= np.float32(2.0) ** {1: up - 2, 2: down}.get(i, 0)       # (normal values: blocks of 32 have exponents of 0 or 1 below theirs)
+        if i == 3:
+            k[::40] *= 6
+    layer = Layer4([300, 300, 300, 1500, 20, 20, 20, 20], 16, 2, spoil=spoil)
+    layer.cache.set_decode_sharing(2)
+    for m, power in ((0, 0), (1, up - 2), (2, down), (3, 0)):
+        unit = 2.0 ** power
+        for calls in ([([(m, 5 * i)], -1, 300 + i, 1) for i in range(4)], [([(m, 0)], -1, 400, 50), ([(m, 7)], -1, 200, 3)]):
+            q = layer.normal(sum(c[3] for c in calls), 16, 128)
+            out, lse = layer.attend(calls, q)
+            want, want_lse = layer.want(calls, q)
+            same(out.double() / unit, lse, want / unit, want_lse, f"values by {unit}") if m != 3 else None
+            if m == 3:                                   # (scores of some tens: errors by their size, 2^-8 |q| |k| / sqrt(128), as far as one key takes all)
+                size = np.linalg.norm(q, axis=-1) * np.linalg.norm(layer.ks[3], axis=-1).max() / np.sqrt(128)
+                assert (np.abs(lse.double().cpu().numpy() - want_lse) <= (2.0 ** -8 + 1e-6) * size).all()
+                assert out.isfinite().all()
+            layer.cache.set_key_gather(2)
+            if calls[0][3] > 1 and m != 3:
+                out, lse = layer.attend(calls, q)
+                same(out.double() / unit, lse, want / unit, want_lse, f"values by {unit}, copied")
+            layer.cache.set_key_gather(0)
+    layer.run([([(0, 3 * i)], 4 + i, 320, 1) for i in range(4)], what="with tails")
+    layer.cache.close()
+
+
 @pytest.mark.parametrize("n_q", [1, 5, 40])
 def test_tokens_that_are_no_numbers(n_q):
     """Rows that see one are NaN in that head's query heads; what others do not see does not touch them."""
