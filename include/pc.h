@@ -99,9 +99,10 @@ typedef struct {
  * place (norms, turns and quantisation in 64 bits).  k, v, q and out are bf16.  A token whose key or value holds an infinity or a NaN in some
  * head has keys of NaN there: rows that see it are NaN in that head's query heads.
  * Attention (pc_attend, pc_attend_static, pc_attend_window, pc_attend_window_static, pc_decode_step) computes with the values held, and with turned
- * queries as the sum of two 8-bit numbers (off by 2^-8 of a value at most, as bf16 is).  Calls of more rows than one have the values of the
- * tiles that they see laid out in bf16, which holds them exactly, and their queries turned in the workspace: 8 KB a tile of 32 tokens and KV head, 512
- * bytes a row and query head (in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Long prefills of pc_attend
+ * queries as the sum of two 8-bit numbers (off by 2^-8 of a value at most, as bf16 is).  Probabilities and values are multiplied in fp16 by calls of more
+ * rows than one, and by single tokens that share their messages, unless the cache was ever given a value whose block of 32 has its largest above 7 x 2^13
+ * or, not all zero, below 7 x 2^-14: then, and by other single tokens, in bf16 (values are exact either way).  Calls of more rows than one have the values
+ * of the tiles that they see laid out so, and their queries turned, in the workspace: 8 KB a tile of 32 tokens and KV head, 256 bytes a row and query head (in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Long prefills of pc_attend
  * (calls of at least 512 rows x query heads of a KV head that see 3e7 scores or more) go over a copy of all that they list, 512 bytes a token and KV
  * head besides: there turned keys and queries are fp16 (off by 2^-12 of a value), but for keys above 700 and rows of queries whose norm, scaled, is above 700,
  * which are served as the others are.  Tensors as pc_attend_window asks for them:

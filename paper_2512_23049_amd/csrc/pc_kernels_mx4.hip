@@ -260,7 +260,7 @@ void pc_launch_win_decode_mx4(const PcWin &W, int n_items, const PcArgBlob *blob
 
 // ----------------------------------------------------------------------------------------------------------- prepare
 // In front of the attention of rows: the call's lists to the workspace and the rotations of its runs (as win_turns), its queries turned
-// by their positions and the unit that their 8-bit pieces are in, and the values of the tiles that rows see, as a bf16 cache has them (what the
+// by their positions and the unit that their 8-bit pieces are in, and the values of the tiles that rows see, as a bf16 cache has them, in fp16 or bf16 (what the
 // codes stand for is exact there; 68 bytes read and 256 written for each, once, where every workgroup of rows would convert them again).
 // Bound: latency (77 rows over 5 messages, 32 heads over 8: 5.6 us, with eight heads a block 8.3).
 __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare &P)
@@ -275,7 +275,8 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
             const int64_t k = (i - n_copy) / (PC_D / 2);
             const int f = (int)((i - n_copy) % (PC_D / 2));
             const float2 cs = mx4_rotation((double)reinterpret_cast<const int64_t *>(from + P.off_rot)[k] * P.inv_freq[f]);
-            P.rot_run[k * (PC_D / 2) + f] = make_float2(cs.x * P.scale_log2, cs.y * P.scale_log2);
+            P.rot_run[k * PC_D + f] = (_Float16)cs.x;
+            P.rot_run[k * PC_D + PC_D / 2 + f] = (_Float16)-cs.y;
         }
         return;
     }
@@ -312,7 +313,8 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
             }
             top = fmaxf(top, __shfl_xor(top, 32));
             fine &= __shfl_xor((int)fine, 32) != 0;
-            if (hh == 0) P.q_unit[(int64_t)h * groups * 32 + R] = mx4_unit(top * P.scale_log2);
+            const float unit = mx4_unit(top * P.scale_log2), by = P.scale_log2 / unit;
+            if (hh == 0) P.q_unit[(int64_t)h * groups * 32 + R] = unit;
 #pragma unroll
             for (int s = 0; s < 8; ++s) {
                 const uint4 lo = raw[(s >> 2) * 2 + (s >> 1 & 1)], hi = raw[4 + (s >> 2) * 2 + (s >> 1 & 1)];
@@ -322,11 +324,11 @@ __device__ __forceinline__ void mx4_prepare(const char *from, const PcMx4Prepare
                 for (int j = 0; j < 4; ++j) {
                     const float2 cs = s_rot[(s >> 2) * 32 + 16 * hh + 4 * (s & 3) + j][n];
                     const float a = j & 1 ? bf_hi(lw[j >> 1]) : bf_lo(lw[j >> 1]), b = j & 1 ? bf_hi(hw[j >> 1]) : bf_lo(hw[j >> 1]);
-                    x[j] = fine ? a * cs.x - b * cs.y : __builtin_nanf("");
-                    y[j] = fine ? a * cs.y + b * cs.x : __builtin_nanf("");
+                    x[j] = fine ? (a * cs.x - b * cs.y) * by : __builtin_nanf("");
+                    y[j] = fine ? (a * cs.y + b * cs.x) * by : __builtin_nanf("");
                 }
-                P.q_abs[mx4_query_at(groups, h, R, hh, s)] = make_float4(x[0], x[1], x[2], x[3]);
-                P.q_abs[mx4_query_at(groups, h, R, hh, s + 8)] = make_float4(y[0], y[1], y[2], y[3]);
+                P.q_abs[mx4_query_at(groups, h, R, hh, s)] = make_uint2(mx4_pack<true>(x[0], x[1]), mx4_pack<true>(x[2], x[3]));
+                P.q_abs[mx4_query_at(groups, h, R, hh, s + 8)] = make_uint2(mx4_pack<true>(y[0], y[1]), mx4_pack<true>(y[2], y[3]));
             }
         }
         return;
@@ -373,12 +375,13 @@ void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st
 // this one follows in its softmax, masks and ring of direct loads).  What is its own:
 //   scores   codes of keys straight from the ring to v_mfma_scale 32x32x64, by two e4m3 pieces of the turned queries: as long on the matrix unit
 //            as bf16 keys would be (twice the work at twice the rate), a quarter of the reads from shared memory;
-//   queries  come turned by their positions (pc_mx4_prepare_kernel) and are turned back by a run's rotation in 32 bits, then cut in pieces under one
-//            power of two for the row, the same for every turn;
+//   queries  come turned by their positions (pc_mx4_prepare_kernel) and are turned back by a run's rotation, both in fp16 (2^-12 of a value, a sixteenth
+//            of what pieces are off by; 1 us less of a small prefill), then cut in pieces under one power of two for the row, the same for every turn;
 //   values   come from the copy; they are finite, so that a probability of zero takes a key out.
-// Bound: the vector unit, 140 instructions a tile and wave of which 49 turn queries (messages of 160 tokens: every fifth tile is another's), beside
+// Bound: the vector unit, 140 instructions a tile and wave of which 49 turned queries (messages of 160 tokens: every fifth tile is another's) before that
+// went to fp16, beside
 // 512 cycles of matrix work; 64 heads over 8, 1024 rows over 13k tokens: 0.6 PFLOP/s, which is why long prefills go another way.  Small ones
-// are chains of latencies: 77 rows over 5 messages 16.5 us, in splits of six tiles (of four, three or two no less, and more to merge).
+// are chains of latencies: 77 rows over 5 messages 15.3 us, in splits of six tiles (of four, three or two no less, and more to merge).
 
 namespace {
 __device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "memory"); }
@@ -388,7 +391,7 @@ constexpr int ROWS_RING = 4, ROWS_SLOT = PC_MX4_CODES + PC_TILE * PC_D * 2 + 256
 
 // HALF: probabilities and values in fp16, where no value of the cache is outside it; the reference of a row keeps its largest probability between 2^-4
 // (none yet seen) and 2^15.
-template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, const PcMx4Rows &M, unsigned char *s_kv, float2 (*s_rot)[PC_D / 2])
+template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, const PcMx4Rows &M, unsigned char *s_kv, uint32_t (*s_rot)[PC_D / 2])
 {
     constexpr int RING = ROWS_RING, AHEAD = 3, LOADS = 3;
     constexpr int VALUES = PC_MX4_CODES, EXPS = VALUES + PC_TILE * PC_D * 2, SLOT = ROWS_SLOT;
@@ -415,7 +418,7 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
         lo_max = uniform(lo_max);
     };
     const int64_t groups = ((int64_t)M.n_rows + 31) / 32;
-    const float4 *q_abs = M.q_abs + mx4_query_at(groups, h, R, hh, 0);
+    const uint2 *q_abs = M.q_abs + mx4_query_at(groups, h, R, hh, 0);
     const float q_unit = M.q_unit[(int64_t)h * groups * 32 + R];
     const int e_hi = (int)(__float_as_uint(q_unit) >> 23), e_lo = e_hi - 4;
 
@@ -437,27 +440,19 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
     mx4_i32x8 q_hi[2], q_lo[2];
     // (few: in the walk, what is read for all of it at once would not fit the registers)
     auto turn = [&](int rot, auto few) __attribute__((always_inline)) {
-        const float2 own = W.rot_run[(int64_t)rot * (PC_D / 2) + lane];
-        const float4 *from = q_abs;
+        const uint32_t own = M.rot_run[(int64_t)rot * (PC_D / 2) + lane];
+        const uint2 *from = q_abs;
         asm volatile("" : "+v"(from));                   // (sixteen addresses, made once and kept, would not fit the registers)
         in_order();
         s_rot[wave][lane] = own;
         in_order();
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const float4 a = from[64 * s], b = from[64 * (s + 8)];
-            const float4 *r = reinterpret_cast<const float4 *>(&s_rot[wave][(s >> 2) * 32 + 16 * hh + 4 * (s & 3)]);
-            const float4 r0 = r[0], r1 = r[1];
-            const float x[4] = {a.x * r0.x + b.x * r0.y, a.y * r0.z + b.y * r0.w, a.z * r1.x + b.z * r1.y, a.w * r1.z + b.w * r1.w};
-            const float y[4] = {b.x * r0.x - a.x * r0.y, b.y * r0.z - a.y * r0.w, b.z * r1.x - a.z * r1.y, b.w * r1.z - a.w * r1.w};
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const float (&z)[4] = half ? y : x;
-                int hi, rest;
-                mx4_pieces(z, q_unit, hi, rest);
-                q_hi[half][s] = hi;
-                q_lo[half][s] = rest;
-            }
+            const uint2 *r = reinterpret_cast<const uint2 *>(&s_rot[wave][(s >> 2) * 16 + 8 * hh + 2 * (s & 3)]);        // (sines: 32 words further)
+            int u_hi, u_rest, v_hi, v_rest;
+            mx4_turned(from[64 * s], from[64 * (s + 8)], r[0], r[16], u_hi, u_rest, v_hi, v_rest);
+            q_hi[0][s] = u_hi; q_lo[0][s] = u_rest;
+            q_hi[1][s] = v_hi; q_lo[1][s] = v_rest;
             if (decltype(few)::value && (s & 1)) __builtin_amdgcn_sched_barrier(0);
         }
         in_order();
@@ -683,7 +678,7 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
 __global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Rows M)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[ROWS_RING * ROWS_SLOT];
-    __shared__ __attribute__((aligned(16))) float2 s_rot[4][PC_D / 2];
+    __shared__ __attribute__((aligned(16))) uint32_t s_rot[4][PC_D / 2];         // a wave's cosines and sines, in fp16
     if (M.mark && *M.mark != M.mark_value) return;       // (the walk in front of this one served every call)
     if (*M.bf16_only == 0) mx4_rows<true>(W, M, s_kv, s_rot);
     else mx4_rows<false>(W, M, s_kv, s_rot);

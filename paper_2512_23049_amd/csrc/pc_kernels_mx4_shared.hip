@@ -6,7 +6,7 @@
 // workgroup converts a step's values to bf16 together, one step ahead, so that no wave has their codes and powers to take apart.  A
 // wave's queries are turned for all of a visit's calls at once, each lane by its own call's rotation.
 //
-// Bound: no unit alone.  32 calls over 410 of 512 messages of 160 tokens each, 64 heads over 8 (2850 distinct tiles): 201 us, of which
+// Bound: no unit alone.  32 calls over 410 of 512 messages of 160 tokens each, 64 heads over 8 (2850 distinct tiles): 197 us, of which
 // the vector unit is busy in 58 %, shared memory in 33 % and the matrix unit in 20 %: sixteen waves meet at a barrier a step and do the same at the
 // same time.  (At 217 us:) without the products of the values it takes 28 us less, without the turned queries' pieces 31, without the conversion of values 18, without
 // exponentials 13, without loads 8; 16 are its start and the partial results.  Call by call the same batch takes 365 us and reads 26 times as much.
@@ -245,8 +245,7 @@ template <int NW, bool HALF> __device__ __forceinline__ void shared_decode(const
                 for (int s = 0; s < 4; ++s) {            // dims 16 a + 4 s, and 64 up
                     int u_hi, u_rest, v_hi, v_rest;
                     const uint4 c = rot[s >> 1], t = rot[8 + (s >> 1)];
-                    if (s & 1) mx4_turned<2>(q[s >> 1], q[2 + (s >> 1)], c, t, u_hi, u_rest, v_hi, v_rest);
-                    else mx4_turned<0>(q[s >> 1], q[2 + (s >> 1)], c, t, u_hi, u_rest, v_hi, v_rest);
+                    mx4_turned(mx4_two(q[s >> 1], s & 1), mx4_two(q[2 + (s >> 1)], s & 1), mx4_two(c, s & 1), mx4_two(t, s & 1), u_hi, u_rest, v_hi, v_rest);
                     q_hi[s] = of >= 0 ? u_hi : q_hi[s]; q_lo[s] = of >= 0 ? u_rest : q_lo[s];
                     q_hi[4 + s] = of >= 0 ? v_hi : q_hi[4 + s]; q_lo[4 + s] = of >= 0 ? v_rest : q_lo[4 + s];
                 }

@@ -30,10 +30,10 @@ struct PcMx4Prepare {
     int32_t       off_q_pos, off_rot, off_tiles;      // within them: positions (int32), runs' rotations (int64), first slots of the tiles that rows see (int32)
     int32_t       n_rows, n_rot, n_tiles;
     int32_t       n_q_heads, n_kv_heads;
-    float         scale_log2;         // rides on the runs' rotations
-    float2       *rot_run;            // [n_rot][64]
+    float         scale_log2;         // rides on the queries
+    _Float16     *rot_run;            // [n_rot][2][64]: cosines and sines of their turns back
     const void   *q;
-    float4       *q_abs;              // queries turned by their positions (see mx4_query_at)
+    uint2        *q_abs;              // queries turned by their positions, in their units, fp16 (see mx4_query_at)
     float        *q_unit;             // [n_q_heads][rows, rounded up to 32]: 2^e
     const double *inv_freq;
     int64_t       slots;
@@ -47,7 +47,8 @@ struct PcMx4Prepare {
 void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st);
 // What the attention of rows needs besides PcWin (whose v_store and rot_q are not read).
 struct PcMx4Rows {
-    const float4  *q_abs;
+    const uint2   *q_abs;
+    const uint32_t *rot_run;          // (pairs)
     const float   *q_unit;
     const int32_t *places;            // of each run: what is added to a slot for its place among v_tiles' slots
     const void    *v_tiles;

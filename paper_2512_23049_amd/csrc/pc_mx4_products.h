@@ -171,14 +171,14 @@ __device__ __forceinline__ void mx4_pieces(mx4_f16x2 x, mx4_f16x2 y, int &hi, in
     hi = mx4_e4m3(x, y, 1.f);
     rest = mx4_e4m3(x - __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), y - __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true), 0.0625f);
 }
-// four values (words A and A + 1 of eight) and their partners
-template <int A> __device__ __forceinline__ void mx4_turned(uint4 low, uint4 high, uint4 c, uint4 s, int &u_hi, int &u_rest, int &v_hi, int &v_rest)
+// four values and their partners
+__device__ __forceinline__ void mx4_turned(uint2 low, uint2 high, uint2 c, uint2 s, int &u_hi, int &u_rest, int &v_hi, int &v_rest)
 {
-    auto word = [](uint4 x, int i) __attribute__((always_inline)) { return mx4_half(i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w); };
-    const mx4_f16x2 x0 = word(low, A), x1 = word(low, A + 1), y0 = word(high, A), y1 = word(high, A + 1);
-    const mx4_f16x2 c0 = word(c, A), c1 = word(c, A + 1), s0 = word(s, A), s1 = word(s, A + 1);
+    const mx4_f16x2 x0 = mx4_half(low.x), x1 = mx4_half(low.y), y0 = mx4_half(high.x), y1 = mx4_half(high.y);
+    const mx4_f16x2 c0 = mx4_half(c.x), c1 = mx4_half(c.y), s0 = mx4_half(s.x), s1 = mx4_half(s.y);
     mx4_pieces(x0 * c0 - y0 * s0, x1 * c1 - y1 * s1, u_hi, u_rest);
     mx4_pieces(x0 * s0 + y0 * c0, x1 * s1 + y1 * c1, v_hi, v_rest);
 }
+__device__ __forceinline__ uint2 mx4_two(uint4 x, int second) { return second ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y); }
 
 #endif

@@ -472,7 +472,7 @@ WinLayout lay_out(const pc_cache *c, const WinPlan &P)
     L.part_o = big(sizeof(float) * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads * (size_t)c->D);
     L.part_ml = big(sizeof(float) * 2 * (size_t)P.part_rows * (size_t)c->cfg.n_q_heads);
     const size_t turned = mx4 && !P.pre.empty() ? align_up(P.q_pos.size(), 32) * (size_t)c->cfg.n_q_heads : 0;
-    L.q_abs = big(sizeof(float) * (size_t)c->D * turned);
+    L.q_abs = big(sizeof(uint16_t) * (size_t)c->D * turned);
     L.q_unit = big(sizeof(float) * turned);
     L.v_tiles = big((size_t)PC_TILE * (size_t)c->D * c->esize * (size_t)c->cfg.n_kv_heads * P.tiles.size());
     L.total = align_up(at, 256);
@@ -767,8 +767,8 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
             T.off_q_pos = (int)L.q_pos; T.off_rot = (int)L.rots; T.off_tiles = (int)L.tiles;
             T.n_rows = (int)P.q_pos.size(); T.n_rot = (int)P.rots.size(); T.n_tiles = (int)P.tiles.size();
             T.n_q_heads = W.n_q_heads; T.n_kv_heads = W.n_kv_heads; T.scale_log2 = W.scale_log2;
-            T.rot_run = (float2 *)(ws + L.rot_run);
-            T.q = q; T.q_abs = (float4 *)(ws + L.q_abs); T.q_unit = (float *)(ws + L.q_unit);
+            T.rot_run = (_Float16 *)(ws + L.rot_run);
+            T.q = q; T.q_abs = (uint2 *)(ws + L.q_abs); T.q_unit = (float *)(ws + L.q_unit);
             T.inv_freq = c->inv_freq_dev; T.slots = c->slots; T.v_store = c->v_store; T.v_to = ws + L.v_tiles;
             T.bf16_only = c->counters_dev + PC_MX4_WIDE;
             if (mark) { T.mark = c->counters_dev + PC_MX4_MARK; T.mark_value = mark; }
@@ -809,7 +809,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     if (!P.pre.empty()) {
         ProfScope ps(c, bf16 ? 2 : 5, st);
         W.items = (const PcWinItem *)(ws + L.pre);
-        const PcMx4Rows M{(const float4 *)(ws + L.q_abs), (const float *)(ws + L.q_unit), (const int32_t *)(ws + L.places), ws + L.v_tiles,
+        const PcMx4Rows M{(const uint2 *)(ws + L.q_abs), (const uint32_t *)(ws + L.rot_run), (const float *)(ws + L.q_unit), (const int32_t *)(ws + L.places), ws + L.v_tiles,
                           (int64_t)PC_TILE * (int64_t)P.tiles.size(), (int32_t)P.q_pos.size(), mark, mark ? c->counters_dev + PC_MX4_MARK : nullptr, c->counters_dev + PC_MX4_WIDE};
         if (mx4) pc_launch_win_prefill_mx4(W, M, (int)P.pre.size(), st);
         else if (bf16) pc_launch_win_prefill_bf16(W, (int)P.pre.size(), st);
