@@ -3,7 +3,7 @@
 //
 // A workgroup takes a range of the tiles that any of a set of calls (up to 256 columns) see; a wave holds a group of 16 columns and
 // their sums for its whole life.  Tiles come as they are stored, 4352 bytes, by direct loads into a ring of four steps of two; the
-// workgroup converts a step's values to bf16 together, one step ahead, so that no wave has their codes and powers to take apart.  A
+// workgroup converts a step's values to fp16 (or bf16, where fp16 does not hold them) together, one step ahead, so that no wave has their codes and powers to take apart.  A
 // wave's queries are turned for all of a visit's calls at once, each lane by its own call's rotation.
 //
 // Bound: no unit alone.  32 calls over 410 of 512 messages of 160 tokens each, 64 heads over 8 (2850 distinct tiles): 197 us, of which

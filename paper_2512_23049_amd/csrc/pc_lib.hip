@@ -142,7 +142,7 @@ int32_t pc_cache_create(const pc_config *cfg, pc_cache **out)
     if (cfg->dtype != PC_F32 && cfg->dtype != PC_BF16 && cfg->dtype != PC_MX4) return PC_ERR_INVALID_ARG;
     if (cfg->dtype != PC_F32 && cfg->head_dim != 128) return PC_ERR_SHAPE;
     if (cfg->dtype != PC_F32 && cfg->n_q_heads / cfg->n_kv_heads > 16) return PC_ERR_SHAPE;
-    // (pc_attend is a window of 2^31 - 1 there, and angles take the short series)
+    // (pc_attend is a window of 2^31 - 1 there, and angles are to keep 24 bits behind the point of their turns in fp64, see mx4_rotation)
     if (cfg->dtype == PC_MX4 && (cfg->max_position >= 1 << 30 || cfg->rope_theta < 1.f)) return PC_ERR_INVALID_ARG;
     if (cfg->capacity_tokens <= 0 || cfg->max_messages <= 0 || !(cfg->rope_theta > 0.f)) return PC_ERR_INVALID_ARG;
     pc_cache *c = new pc_cache();

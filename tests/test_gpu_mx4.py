@@ -169,6 +169,27 @@ def test_many_rows_over_long_lists(spoilt):
     layer.cache.close()
 
 
+def test_queries_that_are_no_numbers():
+    """A row's head whose query holds a NaN or an infinity is NaN, and no other is touched: tokens on their own and shared, rows, rows over a copy."""
+    layer = Layer4([300, 90, 40, 40, 40, 40], 16, 2)
+    sel = [(0, 0), (1, 310)]
+    tokens, rows = [(sel, 2 + i, 400, 1) for i in range(4)], [(sel, 2, 400, 40), (sel[::-1], 3, 420, 33)]
+    for calls, sharing, gather in ((tokens, 1, 0), (tokens, 2, 0), (rows, 0, 1), (rows, 0, 2)):
+        layer.cache.set_decode_sharing(sharing)
+        layer.cache.set_key_gather(gather)
+        n = sum(c[3] for c in calls)
+        q = layer.normal(n, 16, 128)
+        spoilt = q.copy()
+        bad = np.zeros((n, 16), bool)
+        for r, h, d, x in ((0, 3, 5, np.nan), (1, 9, 127, np.inf), (n - 1, 15, 64, -np.inf), (n - 2, 0, 0, np.nan)):
+            spoilt[r, h, d], bad[r, h] = x, True
+        out, lse = layer.attend(calls, spoilt)
+        want, want_lse = layer.want(calls, q)
+        assert out[layer.torch.from_numpy(bad)].isnan().all()
+        same(out[layer.torch.from_numpy(~bad)], lse[layer.torch.from_numpy(~bad)], want[~bad], want_lse[~bad], f"sharing {sharing} gather {gather}")
+    layer.cache.close()
+
+
 @pytest.mark.parametrize("powers", [(13, -11), (14, 0), (0, -16), (40, -40)])
 def test_values_inside_and_outside_fp16(powers):
     """Values by powers of two that fp16 holds, and that it does not, for single tokens that share their messages and for rows, short and long: each sees
