@@ -57,7 +57,10 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
     const int n_tiles = share + (wave < more), skip = item.skip + wave * share + min(wave, more);
     const unsigned ring = (unsigned)uniform((int)(unsigned)(uintptr_t)&s_ring[wave][0]);
 
-    float m_run = -INFINITY, l_run = 0.f;
+    // Probabilities are 2^60 times 2^(score - m_ref); the reference moves where one would be above 2^16 of that (a column's first always does): the lanes
+    // of a column need not agree on a maximum tile by tile.
+    constexpr float LAZY_LOG2 = 16.f;
+    float m_ref = -INFINITY, l_run = 0.f;
     f32x4 acc[8];
 #pragma unroll
     for (int db = 0; db < 8; ++db) acc[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -153,11 +156,12 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
             in_order();
             const unsigned at = (t & 1) * TILE;
             f32x4 s[2];
+            const float ref = m_ref == -INFINITY ? 0.f : m_ref, start = PC_MX4_E_MAX - ref;
 #pragma unroll
             for (int tau = 0; tau < 2; ++tau) {
                 const uint4 codes = __builtin_bit_cast(uint4, *(lds16)(uintptr_t)(k_rd + at + tau * 256));
                 const int ek = (int)(*(lds4)(uintptr_t)(ke_rd + at + tau * 16) >> (8 * a));
-                s[tau] = mx4_scores16(codes, ek, q_lo, e_lo, (f32x4){0.f, 0.f, 0.f, 0.f});
+                s[tau] = mx4_scores16(codes, ek, q_lo, e_lo, (f32x4){start, start, start, start});
                 s[tau] = mx4_scores16(codes, ek, q_hi, e_hi, s[tau]);
             }
             uint32_t vw[8], ew[8];
@@ -167,7 +171,7 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
                 vw[4 * half] = (uint32_t)w.x; vw[4 * half + 1] = (uint32_t)w.y; vw[4 * half + 2] = (uint32_t)w.z; vw[4 * half + 3] = (uint32_t)w.w;
                 ew[4 * half] = (uint32_t)x.x; ew[4 * half + 1] = (uint32_t)x.y; ew[4 * half + 2] = (uint32_t)x.z; ew[4 * half + 3] = (uint32_t)x.w;
             }
-            float sc[8];                                 // keys 8 a + 0..7 of column n
+            float sc[8];                                 // keys 8 a + 0..7 of column n, less the reference, and 60
 #pragma unroll
             for (int j = 0; j < 8; ++j) sc[j] = s[j >> 2][j & 3];
             const uint32_t sees = win_sees(e.pos0, e.valid, e.sink, false, lo, 0);        // (the only row sees all of the new message)
@@ -176,22 +180,27 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sc[j] = (mine >> j) & 1 ? sc[j] : -INFINITY;
             }
-            float mx = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float m_new = fmaxf(m_run, mx), m_safe = m_new == -INFINITY ? 0.f : m_new, alpha = ex2(m_run - m_safe), m_up = m_safe - PC_MX4_E_MAX;
-            uint32_t pk[4];
-            float ps = 0.f;                              // (of the probabilities as the products take them: their rounding cancels)
+            // (on the bit patterns, which take no care of NaN: right wherever some score is above the reference)
+            auto fi = [](float x) { return __float_as_int(x); };
+            const int top = max(imax3(imax3(fi(sc[0]), fi(sc[1]), fi(sc[2])), fi(sc[3]), fi(sc[4])), imax3(fi(sc[5]), fi(sc[6]), fi(sc[7])));
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > fi(PC_MX4_E_MAX + LAZY_LOG2) || m_ref == -INFINITY) != 0, 0)) {
+                float mx = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32)) - PC_MX4_E_MAX;
+                const bool up = mx > (m_ref == -INFINITY ? -INFINITY : LAZY_LOG2);
+                const float m_new = up ? ref + mx : m_ref, by = up ? m_new - ref : 0.f, f = !up ? 1.f : m_ref == -INFINITY ? 0.f : ex2(-by);
+                m_ref = m_new;
+                l_run *= f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                pk[j] = pack_bf16(ex2(sc[2 * j] - m_up), ex2(sc[2 * j + 1] - m_up));
-                ps += bf_lo(pk[j]) + bf_hi(pk[j]);
+                for (int db = 0; db < 8; ++db) acc[db] *= f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sc[j] -= by;
             }
-            l_run = l_run * alpha + ps;
-            m_run = m_new;
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {           // rare once the running maxima have settled
+            uint32_t pk[4];
 #pragma unroll
-                for (int db = 0; db < 8; ++db) acc[db] *= alpha;
+            for (int j = 0; j < 4; ++j) {                // (summed as the products take them: their rounding cancels)
+                pk[j] = pack_bf16(ex2(sc[2 * j]), ex2(sc[2 * j + 1]));
+                l_run = mx4_sum<false>(pk[j], l_run);
             }
             // (the tile's last numbers are in registers: its place is free)
 #pragma unroll
@@ -213,7 +222,7 @@ __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *item
     l_run += __shfl_xor(l_run, 16);
     l_run += __shfl_xor(l_run, 32);
     float (*s_acc)[COLUMN] = reinterpret_cast<float (*)[COLUMN]>(&s_ring[wave][0]);      // (no load of its own is on its way to it)
-    if (a == 0) { s_m[wave][n] = m_run; s_l[wave][n] = l_run * 0x1p-60f; }
+    if (a == 0) { s_m[wave][n] = m_ref; s_l[wave][n] = l_run * 0x1p-60f; }
 #pragma unroll
     for (int db = 0; db < 8; ++db) *reinterpret_cast<f32x4 *>(&s_acc[n][16 * db + 4 * a]) = acc[db];
     __syncthreads();
