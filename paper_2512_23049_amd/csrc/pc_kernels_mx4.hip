@@ -27,8 +27,9 @@ template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_
 //            on the probabilities, by block of 32 dimensions: probabilities are held 2^60 times as large, and a saturating
 //            subtraction from their exponents takes the powers (-60 to 60) off again.
 // Tiles come by direct loads, two places a wave of its own: no registers wait for them (two tiles in registers left room for two waves a
-// SIMD: 66 us where this takes 50), and no wave for another.  Bound: memory, 4352 bytes a tile and KV head, where there are many (64
-// calls of 150 tiles, 32 heads over 8: 334 MB call by call, of which 119 are distinct, in 50 us: 6.7 TB/s out of the caches); latency where
+// SIMD: 66 us where this took 50), and no wave for another.  Bound: memory, 4352 bytes a tile and KV head, where there are many (64
+// calls of 150 tiles, 32 heads over 8: 334 MB call by call, of which 119 are distinct, in 45 us: 7.4 TB/s out of the caches, and the vector unit half of the time; with a maximum across lanes a
+// tile it was 51); latency where
 // there are few (4 calls, window 512: 9 us, of which a launch of nothing takes 3).
 __device__ __forceinline__ void mx4_decode(const PcWin &W, const PcWinItem *items, const PcWinRun *runs, const int32_t *q_pos)
 {

@@ -213,15 +213,15 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     //   128 over 8: 12 calls 119 and 136, 16 156 and 153, 24 242 and 260, 32 291 and 267;
     //   16 over 2 (the host's time): 16 calls 66 and 93, 32 111 and 158, 64 203 and 305; 64 calls over 16 messages of 640 tokens 62 and 59.
     // 4 bits: a call's own tiles cost a quarter, a shared one what its waves need for it (call by call and shared, of 410 of 512 messages: 64 heads
-    // over 8, 8 calls 110 and 142, 16 195 and 161, 32 364 and 228, 64 658 and 448; 128 over 8, 32 calls 377 and 346; of 24 messages 16 calls 28 and 43, 64 calls
-    // 49 and 56; 64 calls over 32 of 64 messages of 400 tokens 120 and 102, 16 calls 47 and 73; a message of 2048 tokens and 8 of 512, 16 calls 30 and 83, 64 calls
-    // 58 and 190).
+    // over 8, 8 calls 102 and 142, 12 145 and 153, 16 181 and 160, 32 334 and 226, 64 614 and 448; 128 over 8, 32 calls 341 and 346; of 24 messages 16 calls 28
+    // and 43, 64 calls 45 and 55; 64 calls over 32 of 64 messages of 400 tokens 115 and 102, 16 calls 44 and 73; a message of 2048 tokens and 8 of 512, 16 calls
+    // 32 and 83, 64 calls 53 and 191).
     // By the caller's word: pc_set_decode_sharing.
     int64_t own = 0, listed = 0, shared = 0;
     for (const Group &gr : dec) { own += gr.tiles; listed += (int64_t)P.calls[(size_t)gr.call].n_seg; }
     const bool mx4 = c->cfg.dtype == PC_MX4;
     const double heads = H / 8.0, host = 12 + (mx4 ? 0.009 : 0.007) * (double)listed, planned = host + (mx4 ? 0.0075 : 0.015) * (double)(P.runs.size() - (size_t)dec[0].run0);
-    const double alone = std::max(mx4 ? 20 + 0.0047 * (double)own * heads : 8 + 0.0175 * (double)own * heads, host);
+    const double alone = std::max(mx4 ? 20 + 0.0043 * (double)own * heads : 8 + 0.0175 * (double)own * heads, host);
     auto together = [&](int64_t tiles) {
         return std::max(mx4 ? 45 + (0.036 * (double)tiles + 0.0006 * (double)own) * heads : 48 + (0.0227 * (double)tiles + 0.0055 * (double)own) * heads, planned);
     };
