@@ -6,8 +6,8 @@
 // workgroup converts a step's values to fp16 (or bf16, where fp16 does not hold them) together, one step ahead, so that no wave has their codes and powers to take apart.  A
 // wave's queries are turned for all of a visit's calls at once, each lane by its own call's rotation.
 //
-// Bound: no unit alone.  32 calls over 410 of 512 messages of 160 tokens each, 64 heads over 8 (2850 distinct tiles): 197 us, of which
-// the vector unit is busy in 58 %, shared memory in 33 % and the matrix unit in 20 %: sixteen waves meet at a barrier a step and do the same at the
+// Bound: no unit alone.  32 calls over 410 of 512 messages of 160 tokens each, 64 heads over 8 (2850 distinct tiles): 195 us, of which
+// the vector unit is busy in 48 %, shared memory in 33 % and the matrix unit in 22 %: sixteen waves meet at a barrier a step and do the same at the
 // same time.  (At 217 us:) without the products of the values it takes 28 us less, without the turned queries' pieces 31, without the conversion of values 18, without
 // exponentials 13, without loads 8; 16 are its start and the partial results.  Call by call the same batch takes 365 us and reads 26 times as much.
 #include "pc_window.h"
@@ -81,8 +81,10 @@ template <int NW, bool HALF> __device__ __forceinline__ void shared_decode(const
     const int call = my * per + sub;
     const bool real = sub < per && call < n_calls;
     uint4 q[4];
+    int low;                                             // the least position that its call sees but for sinks
     {
         const int row = S.calls[call0 + (real ? call : 0)].row;
+        low = win_low(W.q_pos[row], W.window);
         const unsigned char *qp = (const unsigned char *)W.q + ((int64_t)row * W.n_q_heads + kh * g + n % g) * (PC_D * 2) + 32 * a;
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[i] = real ? ldg16(qp + 128 * (i >> 1) + 16 * (i & 1)) : make_uint4(0, 0, 0, 0);
@@ -223,19 +225,19 @@ template <int NW, bool HALF> __device__ __forceinline__ void shared_decode(const
             for (int e = first; e < end; e += TURNS) {
                 int of = -1;                             // which of the rotations is the lane's
                 asm volatile("" ::: "memory");
-                win_i32x4 x[TURNS], y[TURNS];            // (all at once: one latency)
+                win_i32x4 x[TURNS];                      // (all at once: one latency)
 #pragma unroll
                 for (int i = 0; i < TURNS; ++i) {
-                    const PcWinSee *see = S.sees + e0 + min(e + i, end - 1);
-                    x[i] = listed4(see); y[i] = listed4((const char *)see + 16);
+                    x[i] = listed4((const PcMx4See *)S.sees + e0 + min(e + i, end - 1));
                 }
 #pragma unroll
                 for (int i = 0; i < TURNS; ++i) {
                     if (e + i >= end) break;
-                    const bool mine = sub == y[i].z;
-                    if (mine && a == 0) s_see[wave][n] = make_int4(x[i].x, x[i].y, x[i].z, x[i].w);
+                    const uint32_t packed = (uint32_t)x[i].y;
+                    const bool mine = sub == (int)(packed >> 28);
+                    if (mine && a == 0) s_see[wave][n] = make_int4(x[i].x, (int)(packed & PC_MX4_SEE_TOKENS), x[i].z, low);
                     of = mine ? i : of;
-                    const int64_t turn = (int64_t)(((uint64_t)(uint32_t)y[i].y << 32) | (uint32_t)y[i].x);
+                    const int64_t turn = (int64_t)((uint64_t)(packed >> 26 & 3) << 62 | (uint64_t)(uint32_t)x[i].w << 30) >> 30;
                     const float2 cs = mx4_rotation((double)turn * s_freq[lane]);
                     s_rot[wave][i][0][lane] = (_Float16)cs.x; s_rot[wave][i][1][lane] = (_Float16)cs.y;
                 }

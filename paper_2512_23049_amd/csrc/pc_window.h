@@ -68,6 +68,14 @@ struct PcWinSee {             // a call's view of a visit
     int32_t sub;              // the call's place in its group of columns
     int32_t pad;
 };
+// The same of a PC_MX4 cache, whose positions are below 2^30 (lists of long decodes are read from the host's memory: half of them).
+#define PC_MX4_SEE_TOKENS ((1 << 26) - 1)
+struct PcMx4See {
+    int32_t  pos0;
+    uint32_t packed;          // n_tok (at most PC_MX4_SEE_TOKENS), bits 32 and 33 of the turn from bit 26 on, sub from bit 28 on
+    int32_t  sink;
+    uint32_t turn;            // its low bits
+};
 struct PcWinSharedItem {      // one workgroup's tiles, for each KV head
     int32_t visit0, n_steps;  // (a step: PC_WIN_STEP_TILES tiles of a visit)
     int32_t call0, n_calls;   // its set of calls
@@ -79,7 +87,7 @@ struct PcWinSharedCall { int32_t row, part0; };         // packed row, partial r
 struct PcWinShared {
     const PcWinSharedItem *items;
     const PcWinVisit      *visits;
-    const PcWinSee        *sees;
+    const PcWinSee        *sees;              // (PC_MX4: PcMx4See)
     const PcWinSharedCall *calls;
     int32_t n_items;
     int32_t wide;             // 1: 16 waves (groups of columns) a workgroup, 0: 8

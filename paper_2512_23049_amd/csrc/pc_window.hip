@@ -38,6 +38,7 @@ struct WinPlan {
     std::vector<PcWinSharedItem> sh_items;
     std::vector<PcWinVisit> sh_visits;
     std::vector<PcWinSee> sh_sees;
+    std::vector<PcMx4See> sh_sees4;           // (PC_MX4) in their place
     std::vector<PcWinSharedCall> sh_calls;
     bool sh_wide = false;
 
@@ -59,7 +60,7 @@ struct WinPlan {
 private:
     template <typename F> void each(F &&f)               // (not res: its lists are written over)
     {
-        f(calls); f(segs); f(q_pos); f(pre); f(dec); f(runs); f(run_seg); f(rots); f(merge); f(tiles); f(places); f(sh_items); f(sh_visits); f(sh_sees); f(sh_calls);
+        f(calls); f(segs); f(q_pos); f(pre); f(dec); f(runs); f(run_seg); f(rots); f(merge); f(tiles); f(places); f(sh_items); f(sh_visits); f(sh_sees); f(sh_sees4); f(sh_calls);
     }
 };
 
@@ -193,6 +194,11 @@ void make_items(const pc_cache *c, WinPlan &P, const std::vector<Group> &groups,
     }
 }
 
+PcMx4See mx4_see(const PcWinSee &e)
+{
+    return PcMx4See{e.pos0, (uint32_t)std::min(e.n_tok, PC_MX4_SEE_TOKENS) | (uint32_t)((uint64_t)e.turn >> 32 & 3) << 26 | (uint32_t)e.sub << 28, e.sink, (uint32_t)e.turn};
+}
+
 // Single tokens by what they see together: the tiles that the calls of a set see, each once, in as many ranges as workgroups run at
 // once.  False (and nothing is planned) where reading every call's own tiles is less, or a call lists a message twice.
 bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
@@ -228,12 +234,13 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     if (c->decode_sharing == 0 && alone <= together(own / set_calls)) return false;
     struct Piece { int32_t slot0, tiles; uint32_t run; int32_t call; };
     struct Visit { int32_t slot0, tiles; size_t p0, p1; };           // a range of consecutive tiles, and the pieces of it
+    struct SetOf { size_t visit0; int64_t total; };                  // a set of calls: its first visit, and their tiles
     struct Seen { int32_t call; uint32_t seg; };                     // (call: within the set)
     struct Caller { int32_t q_pos, low, group, sub; };               // a call's place among the columns of its set
     struct Lists {
         std::vector<Piece> pieces, scratch;
         std::vector<uint32_t> digits;
-        std::vector<std::pair<size_t, size_t>> of_set;   // a set's pieces, in slot order
+        std::vector<SetOf> of_set;
         std::vector<Seen> seen;                          // who sees the visit at hand, and from which entry of its list; its views: P.sh_sees from e0 on
         std::vector<Visit> visits;
         std::vector<Caller> callers;
@@ -246,79 +253,86 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
     auto &seen = kept.seen;
     auto &visits = kept.visits;
     auto &callers = kept.callers;
-    pieces.clear(); of_set.clear();
+    pieces.clear(); of_set.clear(); visits.clear();
     pieces.reserve(P.runs.size() - (size_t)dec[0].run0);
     // pieces [first, size) by their slots, in the calls' order where those are the same: a pass for 13 bits of a tile's number
     constexpr uint32_t DIGIT = 13;
     digits.resize(1u << DIGIT);
-    auto by_slot = [&](std::vector<Piece> &v, size_t first, std::vector<Piece> &other) {
-        uint32_t most = 0;
-        for (size_t k = first; k < v.size(); ++k) most = std::max(most, (uint32_t)v[k].slot0 / PC_TILE);
-        other.resize(v.size());
+    constexpr uint32_t MASK = (1u << DIGIT) - 1;
+    auto by_slot = [&](size_t first, uint32_t most) {    // (digits: how often the lowest ones occur)
+        scratch.resize(pieces.size());
         for (uint32_t shift = 0; shift == 0 || (shift < 32 && most >> shift); shift += DIGIT) {
-            const uint32_t mask = (1u << DIGIT) - 1, used = std::min(mask, most >> shift);
-            std::fill(digits.begin(), digits.begin() + used + 1, 0u);
-            for (size_t k = first; k < v.size(); ++k) ++digits[((uint32_t)v[k].slot0 / PC_TILE >> shift) & mask];
+            const uint32_t used = std::min(MASK, most >> shift);
+            if (shift > 0) {
+                std::fill(digits.begin(), digits.begin() + used + 1, 0u);
+                for (size_t k = first; k < pieces.size(); ++k) ++digits[((uint32_t)pieces[k].slot0 / PC_TILE >> shift) & MASK];
+            }
             uint32_t next = (uint32_t)first;
             for (uint32_t d = 0; d <= used; ++d) { const uint32_t count = digits[d]; digits[d] = next; next += count; }
-            for (size_t k = first; k < v.size(); ++k) other[digits[((uint32_t)v[k].slot0 / PC_TILE >> shift) & mask]++] = v[k];
-            std::memcpy(v.data() + first, other.data() + first, sizeof(Piece) * (v.size() - first));
+            for (size_t k = first; k < pieces.size(); ++k) scratch[digits[((uint32_t)pieces[k].slot0 / PC_TILE >> shift) & MASK]++] = pieces[k];
+            if (first == 0) pieces.swap(scratch);
+            else std::memcpy(pieces.data() + first, scratch.data() + first, sizeof(Piece) * (pieces.size() - first));
         }
     };
     for (int32_t s = 0; s < n_sets; ++s) {
         const size_t first = pieces.size();
+        uint32_t most = 0;
+        std::fill(digits.begin(), digits.end(), 0u);
         for (int32_t j = s * set_calls; j < std::min(n_calls, (s + 1) * set_calls); ++j) {
             int32_t left = dec[(size_t)j].tiles;
             for (size_t r = (size_t)dec[(size_t)j].run0; left > 0; ++r) {
                 const int32_t t = (P.runs[r].n_tok + PC_TILE - 1) / PC_TILE;
+                const uint32_t tile = (uint32_t)P.runs[r].slot0 / PC_TILE;
                 pieces.push_back(Piece{P.runs[r].slot0, t, (uint32_t)r, j});
+                ++digits[tile & MASK];
+                most = std::max(most, tile);
                 left -= t;
             }
         }
-        by_slot(pieces, first, scratch);
-        int64_t end = -1;
-        for (size_t k = first; k < pieces.size(); ++k) {
-            const int64_t b = pieces[k].slot0, e = b + (int64_t)PC_TILE * pieces[k].tiles;
-            if (e > end) { shared += (e - std::max(b, end)) / PC_TILE; end = e; }
-        }
-        of_set.push_back({first, pieces.size()});
-    }
-    const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
-    if (shared == 0 || (c->decode_sharing == 0 && alone <= together(shared))) return false;
-    P.sh_sees.reserve(pieces.size() + pieces.size() / 4);
-    for (int32_t s = 0; s < n_sets; ++s) {
-        const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
-        int32_t waves = 1;
-        while (waves < groups) waves *= 2;
-        const int32_t reps = (wide ? 16 : 8) / waves;
+        by_slot(first, most);
         // ranges of consecutive tiles
-        visits.clear();
-        callers.clear();
-        for (int32_t j = 0; j < in_set; ++j) {
-            const int32_t q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)(call0 + j)].call].q_off];
-            callers.push_back(Caller{q_pos, win_low(q_pos, P.window), j / per, j % per});
-        }
+        const size_t visit0 = visits.size();
         int64_t total = 0;
-        for (size_t k = of_set[(size_t)s].first; k < of_set[(size_t)s].second;) {
+        for (size_t k = first; k < pieces.size();) {
             Visit v{pieces[k].slot0, 0, k, k};
-            for (; v.p1 < of_set[(size_t)s].second && (v.p1 == v.p0 || pieces[v.p1].slot0 < v.slot0 + PC_TILE * v.tiles); ++v.p1)
+            for (; v.p1 < pieces.size() && (v.p1 == v.p0 || pieces[v.p1].slot0 < v.slot0 + PC_TILE * v.tiles); ++v.p1)
                 v.tiles = std::max(v.tiles, (pieces[v.p1].slot0 - v.slot0) / PC_TILE + pieces[v.p1].tiles);
             total += v.tiles;
             visits.push_back(v);
             k = v.p1;
         }
+        shared += total;
+        of_set.push_back(SetOf{visit0, total});
+    }
+    const int64_t bins = std::max<int64_t>(1, std::min<int64_t>(256 / (H * n_sets), shared / n_sets / 8));
+    if (shared == 0 || (c->decode_sharing == 0 && alone <= together(shared))) return false;
+    if (mx4) P.sh_sees4.reserve(pieces.size() + pieces.size() / 4);
+    else P.sh_sees.reserve(pieces.size() + pieces.size() / 4);
+    for (int32_t s = 0; s < n_sets; ++s) {
+        const int32_t call0 = s * set_calls, in_set = std::min(n_calls - call0, set_calls), groups = (in_set + per - 1) / per;
+        int32_t waves = 1;
+        while (waves < groups) waves *= 2;
+        const int32_t reps = (wide ? 16 : 8) / waves;
+        callers.clear();
+        for (int32_t j = 0; j < in_set; ++j) {
+            const int32_t q_pos = P.q_pos[(size_t)P.calls[(size_t)dec[(size_t)(call0 + j)].call].q_off];
+            callers.push_back(Caller{q_pos, win_low(q_pos, P.window), j / per, j % per});
+        }
+        const int64_t total = of_set[(size_t)s].total;
         const int64_t n_bins = std::max<int64_t>(1, std::min(bins, total));
         const int32_t splits = (int32_t)n_bins * reps;
-        size_t at = 0;
+        size_t at = of_set[(size_t)s].visit0;
         int32_t done = 0;                                // tiles of visits[at] that earlier workgroups have
         for (int64_t b = 0; b < n_bins; ++b) {
             int32_t left = (int32_t)(total * (b + 1) / n_bins - total * b / n_bins);
             P.sh_items.push_back(PcWinSharedItem{(int32_t)P.sh_visits.size(), 0, call0, in_set, waves, (int32_t)b * reps, 0, 0});
             while (left > 0) {
                 const Visit &v = visits[at];
-                const int32_t n = std::min(left, v.tiles - done), slot0 = v.slot0 + PC_TILE * done, slot1 = slot0 + PC_TILE * n;
+                const int32_t n = std::min(left, v.tiles - done);
+                if (mx4 && n > PC_MX4_SEE_TOKENS / PC_TILE) return false;
+                const int32_t slot0 = v.slot0 + PC_TILE * done, slot1 = slot0 + PC_TILE * n;
                 seen.clear();
-                const size_t e0 = P.sh_sees.size();
+                const size_t e0 = mx4 ? P.sh_sees4.size() : P.sh_sees.size();
                 for (size_t k = v.p0; k < v.p1; ++k) {
                     const Piece pc = pieces[k];
                     if (k + 12 < pieces.size()) __builtin_prefetch(&P.runs[pieces[k + 12].run]);     // (they lie in the calls' order)
@@ -331,18 +345,27 @@ bool plan_shared(const pc_cache *c, WinPlan &P, const std::vector<Group> &dec)
                     const uint32_t seg = (uint32_t)P.run_seg[pc.run];
                     if (seen.empty() || seen.back().call < j) {          // (in order, mostly)
                         seen.push_back(Seen{j, seg});
-                        P.sh_sees.push_back(e);
+                        if (mx4) P.sh_sees4.push_back(mx4_see(e));
+                        else P.sh_sees.push_back(e);
                         continue;
                     }
                     size_t i = seen.size();
                     while (i > 0 && seen[i - 1].call > j) --i;
                     if (i > 0 && seen[i - 1].call == j) {                // the sinks of an extent and its end: one view
-                        PcWinSee &o = P.sh_sees[e0 + i - 1];
                         if (seen[i - 1].seg != seg) return false;        // listed twice: two views, and a column has room for one
-                        o.n_tok = std::max(o.n_tok, e.n_tok); o.sink = std::max(o.sink, e.sink);
+                        if (mx4) {
+                            PcMx4See &o = P.sh_sees4[e0 + i - 1];
+                            const PcMx4See w = mx4_see(e);
+                            if ((w.packed & PC_MX4_SEE_TOKENS) > (o.packed & PC_MX4_SEE_TOKENS)) o.packed = w.packed;          // (a call's views of an extent are alike but for that)
+                            o.sink = std::max(o.sink, w.sink);
+                        } else {
+                            PcWinSee &o = P.sh_sees[e0 + i - 1];
+                            o.n_tok = std::max(o.n_tok, e.n_tok); o.sink = std::max(o.sink, e.sink);
+                        }
                     } else {
                         seen.insert(seen.begin() + (ptrdiff_t)i, Seen{j, seg});
-                        P.sh_sees.insert(P.sh_sees.begin() + (ptrdiff_t)(e0 + i), e);
+                        if (mx4) P.sh_sees4.insert(P.sh_sees4.begin() + (ptrdiff_t)(e0 + i), mx4_see(e));
+                        else P.sh_sees.insert(P.sh_sees.begin() + (ptrdiff_t)(e0 + i), e);
                     }
                 }
                 PcWinVisit pv{slot0, n, (int32_t)e0, {}};
@@ -396,7 +419,7 @@ void plan_items(const pc_cache *c, WinPlan &P, bool may_split, int32_t least = 0
     if (least == 0) least = c->cfg.dtype == PC_MX4 ? 24 : 8;             // (a workgroup of a 4-bit cache's tokens is eight waves: three tiles each)
     const int g = c->g;
     P.pre.clear(); P.dec.clear(); P.runs.clear(); P.run_seg.clear(); P.rots.clear(); P.merge.clear();
-    auto no_shared = [&] { P.sh_items.clear(); P.sh_visits.clear(); P.sh_sees.clear(); P.sh_calls.clear(); };
+    auto no_shared = [&] { P.sh_items.clear(); P.sh_visits.clear(); P.sh_sees.clear(); P.sh_sees4.clear(); P.sh_calls.clear(); };
     no_shared();
     P.part_rows = 0;
     for (Seg &s : P.segs) s.rot = -1;
@@ -460,7 +483,7 @@ WinLayout lay_out(const pc_cache *c, const WinPlan &P)
     L.rots = take(sizeof(int64_t) * P.rots.size());
     L.sh_items = take(sizeof(PcWinSharedItem) * P.sh_items.size());
     L.sh_visits = take(sizeof(PcWinVisit) * P.sh_visits.size());
-    L.sh_sees = take(sizeof(PcWinSee) * P.sh_sees.size());
+    L.sh_sees = take(sizeof(PcWinSee) * P.sh_sees.size() + sizeof(PcMx4See) * P.sh_sees4.size());         // (one of them)
     L.sh_calls = take(sizeof(PcWinSharedCall) * P.sh_calls.size());
     L.tiles = take(sizeof(int32_t) * P.tiles.size());
     L.places = take(sizeof(int32_t) * P.places.size());
@@ -484,7 +507,7 @@ void write_lists(const WinPlan &P, const WinLayout &L, char *to)
 {
     auto put = [&](size_t at, const auto &v) { if (!v.empty()) std::memcpy(to + at, v.data(), sizeof(v[0]) * v.size()); };
     put(L.pre, P.pre); put(L.dec, P.dec); put(L.runs, P.runs); put(L.merge, P.merge); put(L.q_pos, P.q_pos); put(L.rots, P.rots);
-    put(L.sh_items, P.sh_items); put(L.sh_visits, P.sh_visits); put(L.sh_sees, P.sh_sees); put(L.sh_calls, P.sh_calls); put(L.tiles, P.tiles); put(L.places, P.places);
+    put(L.sh_items, P.sh_items); put(L.sh_visits, P.sh_visits); put(L.sh_sees, P.sh_sees); put(L.sh_sees, P.sh_sees4); put(L.sh_calls, P.sh_calls); put(L.tiles, P.tiles); put(L.places, P.places);
 }
 
 // ---- the gradient -------------------------------------------------------------------------------------------------
