@@ -36,6 +36,22 @@ def test_rows_over_a_copy(h_q, h_kv):
     layer.cache.close()
 
 
+def test_tuned_and_timed():
+    """The same calls in splits of the caller's length, with kernels timed: rows over the cache and over a copy, tokens."""
+    layer = Layer4(LENS, 8, 2)
+    calls = [(SEL, 5, 600, 90), (SEL, 5, 600, 1), (SEL[::-1], 4, 500, 100)]
+    for tiles, gather in ((0, 2), (1, 2), (3, 2), (1, 1)):
+        layer.cache.set_tuning(tiles, tiles)
+        layer.cache.set_key_gather(gather)
+        layer.cache.profile_enable(True)
+        layer.run(calls, what=f"splits of {tiles} gather {gather}")
+        of = list(layer.cache.profile_read().values())   # (by class: 2 rows, 3 tokens, 8 copies)
+        layer.cache.profile_enable(False)
+        assert of[2][1] >= 1 and of[3][1] >= 1 and of[8][1] == (2 if gather == 2 else 0)
+        assert sum(ms for ms, _ in of) > 0
+    layer.cache.close()
+
+
 @pytest.mark.parametrize("h_q,h_kv", [(8, 2), (4, 4)])
 @pytest.mark.parametrize("static", [False, True])
 def test_batches(h_q, h_kv, static):
