@@ -192,11 +192,12 @@ struct PcOneItem {
 };
 #define PC_ONE_SEGS 64        // most of them (a wave holds them, one a lane)
 #define PC_ONE_COUNTERS 256   // (call, KV head) pairs of a batch whose calls are split (two splits each: two rounds of workgroups)
-// A cache's words on the device: two sets of those counters (pc_attend, pc_attend_static), the mark of long prefills of a PC_MX4 cache, and whether it
-// has been given values that fp16 does not hold.
+// A cache's words on the device: two sets of those counters (pc_attend, pc_attend_static), the mark of long prefills of a PC_MX4 cache, whether it
+// has been given values that fp16 does not hold, and the blocks of pc_projected_backward that are done (0 between calls).
 #define PC_MX4_MARK (2 * PC_ONE_COUNTERS)
 #define PC_MX4_WIDE (2 * PC_ONE_COUNTERS + 1)
-#define PC_CACHE_WORDS (2 * PC_ONE_COUNTERS + 2)
+#define PC_ROWS_DONE (2 * PC_ONE_COUNTERS + 2)
+#define PC_CACHE_WORDS (2 * PC_ONE_COUNTERS + 3)
 
 // ---- a decode batch by message: a wave streams a run of tiles of one message for up to PC_RUN_ROWS of the one-row calls that list it ----
 #define PC_RUN_ROWS 4

@@ -345,8 +345,8 @@ void pc_launch_rows(int dtype, PcRows R, const PcArgBlob *blob, hipStream_t st)
 // ---------------------------------------------------------------------------------------------------------- gradient
 // With r = 1 / sqrt(mean(x^2) + eps), u = x r, g = dy w:   dx = r (g - u mean(g u)),   dw = the sum of dy u over rows and heads.
 // Of keys dy is the gradient of the keys as stored, turned back.  A block takes block_rows rows and eight heads of one kind
-// (blockIdx.y: queries' chunks of heads, then keys', then values'); its sums for the weights leave as one row of partial results, which a
-// second launch adds up in order.
+// (blockIdx.y: queries' chunks of heads, then keys', then values'); its sums for the weights leave as one row of partial results, which the
+// last block, or a second launch, adds up in order.
 // Bound: memory (8192 rows of 64 heads over 8, 654 MB: 129 us, 5.1 TB/s; 939 rows of 32 heads over 8: 11 us; sums behind them 6.5 and 3.7: 64 threads
 // a dimension, eight loads each at once).
 template <typename T, int D>
@@ -433,7 +433,49 @@ __device__ __forceinline__ void rows_backward(const PcRowsBwd &B, const PcRowsBw
     }
     __syncthreads();
     float *to = kind == 0 ? B.q_part + ((int64_t)blockIdx.x * nq + chunk) * D : B.k_part + ((int64_t)blockIdx.x * nk + chunk) * D;
-    for (int d = threadIdx.x; d < D; d += 256) to[d] = s_sum[0][d] + s_sum[1][d] + s_sum[2][d] + s_sum[3][d];
+    const int d = threadIdx.x;
+    const float sum = d < D ? s_sum[0][d] + s_sum[1][d] + s_sum[2][d] + s_sum[3][d] : 0.f;
+    if (B.n_done == 0) {
+        if (d < D) to[d] = sum;
+        return;
+    }
+    __shared__ bool s_last;
+    if (d < D) __hip_atomic_store(to + d, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): this wave's part is out
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        s_last = atomicInc(B.done, B.n_done - 1) == B.n_done - 1;        // (wraps to zero with the last block: ready for the next call)
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    // (in shares of parts, and these in order: the same sum whichever block is last)
+    constexpr int SHARES = 256 / D;
+    const int share = threadIdx.x / D, e = threadIdx.x % D;
+    for (int w = 0; w < 2; ++w) {
+        float *out = w == 0 ? B.to_q_weight : B.to_k_weight;
+        if (!out) continue;
+        const float *part = w == 0 ? B.q_part : B.k_part;
+        const int n = B.n_blocks * (w == 0 ? nq : nk);
+        float x = 0.f;
+        for (int i = share; i < n; i += 16 * SHARES) {
+            float y[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) y[u] = i + SHARES * u < n ? part[(int64_t)(i + SHARES * u) * D + e] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 16; ++u) x += y[u];
+        }
+        __syncthreads();
+        s_sum[share][e] = x;
+        __syncthreads();
+        if (share == 0) {
+            x = 0.f;
+#pragma unroll
+            for (int k = 0; k < SHARES; ++k) x += s_sum[k][e];
+            out[e] = x;
+        }
+    }
 }
 
 template <typename T, int D> __global__ __launch_bounds__(256) void pc_rows_bwd_kernel(PcRowsBwd B) { rows_backward<T, D>(B, B.items); }
@@ -484,7 +526,7 @@ void pc_launch_rows_backward(int dtype, const PcRowsBwd &B, const PcArgBlob *blo
     if (dtype == 1) go((uint16_t)0, integral_constant<int, 128>{});
     else if (B.D == 64) go(0.f, integral_constant<int, 64>{});
     else go(0.f, integral_constant<int, 128>{});
-    if (B.to_q_weight || B.to_k_weight) pc_rows_bwd_sum_kernel<<<dim3((unsigned)B.D / 16, 2), 1024, 0, st>>>(B);
+    if (B.n_done == 0 && (B.to_q_weight || B.to_k_weight)) pc_rows_bwd_sum_kernel<<<dim3((unsigned)B.D / 16, 2), 1024, 0, st>>>(B);
 }
 
 // -------------------------------------------------------------------------------------------------------------- read

@@ -58,6 +58,7 @@ struct PcRowsBwd {
     int64_t to_q_stride, to_k_stride, to_v_stride;
     float  *q_part, *k_part;                  // a block's sums for the weights: [block][chunk of heads][D]
     float  *to_q_weight, *to_k_weight;        // null: not asked for
+    uint32_t *done, n_done;                   // n_done > 0: the last of so many blocks adds the sums up
     const double *inv_freq;
 };
 void pc_launch_rows_backward(int dtype, const PcRowsBwd &B, const PcArgBlob *blob, hipStream_t st);

@@ -5,6 +5,7 @@
 
 namespace {
 
+constexpr int64_t FEW_SUMS = 64;
 constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;           // of 256 threads, in one dimension of a launch
 
 bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -176,6 +177,10 @@ int32_t projected_backward(pc_cache *c, const pc_projected *p, int32_t n, const 
     B.to_q_stride = to->q_stride; B.to_k_stride = to->k_stride; B.to_v_stride = to->v_stride;
     B.to_q_weight = to->q_weight; B.to_k_weight = to->k_weight;
     B.inv_freq = c->inv_freq_dev;
+    // A few sums are added up by the block that is done last (a launch of its own is 4 us with what lies between the two), many by a second launch: one
+    // block would read them one latency after the other.
+    const int64_t q_chunks = to->q_weight ? (c->cfg.n_q_heads + 7) / 8 : 0, k_chunks = to->k_weight ? (c->cfg.n_kv_heads + 7) / 8 : 0;
+    if (blocks * std::max(q_chunks, k_chunks) <= FEW_SUMS) { B.done = c->counters_dev + PC_ROWS_DONE; B.n_done = (uint32_t)(blocks * (q_chunks + k_chunks)); }
     const size_t part = sizeof(float) * (size_t)c->D * (size_t)blocks;
     const size_t q_bytes = align_up(part * (((size_t)c->cfg.n_q_heads + 7) / 8), 256), k_bytes = part * (((size_t)c->cfg.n_kv_heads + 7) / 8);
     rc = pc_ensure_ws(c, q_bytes + k_bytes, st);
