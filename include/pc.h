@@ -102,8 +102,8 @@ typedef struct {
  * queries as the sum of two 8-bit numbers (off by 2^-8 of a value at most, as bf16 is).  Probabilities and values are multiplied in fp16 by calls of more
  * rows than one, and by single tokens that share their messages, unless the cache was ever given a value whose block of 32 has its largest above 7 x 2^13
  * or, not all zero, below 7 x 2^-14: then, and by other single tokens, in bf16 (values are exact either way).  Calls of more rows than one have the values
- * of the tiles that they see laid out so, and their queries turned, in the workspace: 8 KB a tile of 32 tokens and KV head, 256 bytes a row and query head (in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Long prefills of pc_attend
- * (calls of at least 512 rows x query heads of a KV head that see 3e7 scores or more) go over a copy of all that they list, 512 bytes a token and KV
+ * of the tiles that they see laid out so, and their queries turned, in the workspace: 8 KB a tile of 32 tokens and KV head, 256 bytes a row and query head (in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Long prefills of pc_attend,
+ * and of pc_attend_window where the window leaves rows all that they list (calls of at least 512 rows x query heads of a KV head that see 3e7 scores or more), go over a copy of all that they list, 512 bytes a token and KV
  * head besides: there turned keys and queries are fp16 (off by 2^-12 of a value), but for keys above 700 and rows of queries whose norm, scaled, is above 700,
  * which are served as the others are.  Tensors as pc_attend_window asks for them:
  * q and out 16-byte aligned; and pc_attend and pc_decode_step, like pc_attend_window, refuse a stream that is being captured.  Messages are appended, grown,
@@ -456,7 +456,7 @@ int32_t pc_set_tuning(pc_cache *c, int32_t decode_tiles_per_split, int32_t prefi
  * is not changed; results are the same up to one more rounding of the copied keys to bf16.  mode 0 (default): calls
  * with rows x query heads >= 32768 (below that the copy costs more than it saves); 1: never; 2: every prefill call (more than 16 rows x
  * query heads of a KV head).  PC_MX4 caches: the long prefills described there (the copied keys in fp16).
- * Of pc_attend in PC_BF16 and PC_MX4 caches only; pc_attend_static never gathers (the copy may not fit its fixed workspace). */
+ * Of pc_attend in PC_BF16 and PC_MX4 caches only (and pc_attend_window, see there); pc_attend_static never gathers (the copy may not fit its fixed workspace). */
 int32_t pc_set_key_gather(pc_cache *c, int32_t mode);
 
 /* Gradient of pc_attend for fine-tuning (Sec. 2.4: while fine-tuning, a position update is

@@ -188,7 +188,7 @@ int32_t pc_attend(pc_cache *c, const pc_call *calls, int32_t n_calls, const void
     if (n_calls < 0 || (n_calls > 0 && !calls)) return pc_fail(c, PC_ERR_INVALID_ARG, "attend: bad call list");
     if (n_calls == 0) return PC_OK;
     if (!c->host_only && (!q || !out)) return pc_fail(c, PC_ERR_INVALID_ARG, "attend: null q or out");
-    if (c->cfg.dtype == PC_MX4) return pc_guarded(c, [&] { return pc_attend_mx4(c, "attend", calls, n_calls, q, out, lse, (hipStream_t)stream, nullptr); });
+    if (c->cfg.dtype == PC_MX4) return pc_guarded(c, [&] { return pc_attend_mx4(c, "attend", calls, n_calls, INT32_MAX, 0, q, out, lse, (hipStream_t)stream, nullptr); });
     return attend_impl(c, calls, n_calls, q, out, lse, (hipStream_t)stream, nullptr, 0);
 }
 
@@ -205,7 +205,7 @@ int32_t pc_decode_step(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, cons
         return pc_guarded(c, [&] {
             if (!c->host_only && pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "decode_step: the stream is being captured, and the cache's workspace may move");
             const int32_t r = n_msgs > 0 ? pc_append_token_items(c, std::vector<int32_t>(msg_ids, msg_ids + n_msgs), k, v, st, nullptr) : PC_OK;
-            return r != PC_OK || n_calls == 0 ? r : pc_attend_mx4(c, "decode_step", calls, n_calls, q, out, lse, st, nullptr);
+            return r != PC_OK || n_calls == 0 ? r : pc_attend_mx4(c, "decode_step", calls, n_calls, INT32_MAX, 0, q, out, lse, st, nullptr);
         });
     const std::vector<int32_t> ids(msg_ids, msg_ids + std::max(n_msgs, 0));
     // The tokens can be written by a launch of the attend itself (the one launch of a decode batch, else the plan builder's)
@@ -256,13 +256,13 @@ int32_t pc_attend_static(pc_cache *c, const pc_call *calls, int32_t n_calls, con
     if (n_calls < 0 || (n_calls > 0 && !calls)) return pc_fail(c, PC_ERR_INVALID_ARG, "attend_static: bad call list");
     if (n_calls == 0) return PC_OK;
     const bool mx4 = c->cfg.dtype == PC_MX4;
-    if (c->host_only && mx4) return pc_guarded(c, [&] { return pc_attend_mx4(c, "attend_static", calls, n_calls, q, out, lse, nullptr, nullptr); });
+    if (c->host_only && mx4) return pc_guarded(c, [&] { return pc_attend_mx4(c, "attend_static", calls, n_calls, INT32_MAX, 0, q, out, lse, nullptr, nullptr); });
     if (c->host_only) return attend_impl(c, calls, n_calls, q, out, lse, nullptr, nullptr, 0);
     if (!q || !out) return pc_fail(c, PC_ERR_INVALID_ARG, "attend_static: null q or out");
     if (!c->static_ws) return pc_fail(c, PC_ERR_HIP, "attend_static: the fixed scratch array was not found on this device");
     const bool prof = c->prof;                           // kernel timing takes events from a pool that may have to grow
     c->prof = false;
-    const int32_t rc = mx4 ? pc_guarded(c, [&] { return pc_attend_mx4(c, "attend_static", calls, n_calls, q, out, lse, (hipStream_t)stream, c->static_ws); })
+    const int32_t rc = mx4 ? pc_guarded(c, [&] { return pc_attend_mx4(c, "attend_static", calls, n_calls, INT32_MAX, 0, q, out, lse, (hipStream_t)stream, c->static_ws); })
                            : attend_impl(c, calls, n_calls, q, out, lse, (hipStream_t)stream, c->static_ws, PC_STATIC_WS_BYTES);
     c->prof = prof;
     return rc;

@@ -252,8 +252,8 @@ extern "C" int32_t pc_items_room(pc_cache *c, size_t bytes, hipStream_t st);    
 extern "C" int32_t pc_stage_items(pc_cache *c, const void *items, size_t bytes, hipStream_t st);
 // pc_project.hip: items to the cache, in one launch (R: what the call brings; the cache's own is filled in)
 int32_t pc_write_rows(pc_cache *c, PcRows R, std::vector<PcRowsItem> &items, hipStream_t st);
-// pc_window.hip: pc_attend of a PC_MX4 cache (fixed_ws: null, or the array of pc_attend_static)
-int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws);
+// pc_window.hip: pc_attend (window INT32_MAX) or pc_attend_window of a PC_MX4 cache (fixed_ws: null, or the array of pc_attend_static)
+int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws);
 // pc_attend.hip: the address, on the current device, of the library's fixed scratch array (looked up once per device)
 int32_t pc_static_scratch(void **ptr, size_t *bytes);
 // pc_plan.hip

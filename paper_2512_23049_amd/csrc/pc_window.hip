@@ -981,7 +981,7 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
 
 // What a call lists is all in a window of 2^31 - 1 (positions are below 2^30 in magnitude: pc_cache_create).
 //
-// Long prefills go over a packed copy, as in a bf16 cache: there a message's turn costs its keys once, and not every row and head once a
+// Long prefills (whose rows a window leaves all that they list) go over a packed copy, as in a bf16 cache: there a message's turn costs its keys once, and not every row and head once a
 // message.  The copy's keys and the queries are fp16 for the matrix instructions, whose range keys and queries of models are in; where one is not, the
 // device marks the call, and the walk over the cache itself, which takes any, follows and does nothing otherwise.
 // Taken by calls of LONG_ROWS rows x query heads of a KV head (each copied token is read that often), where those that stand together have
@@ -992,12 +992,26 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
 constexpr int64_t LONG_ROWS = 512;
 constexpr double LONG_SCORES = 3e7;
 constexpr int64_t LONG_TOKENS = (int64_t)1 << 22;        // a copy's, where it has more calls than one: 16 GiB of 8 KV heads
-int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws)
+int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out, float *lse,
+                      hipStream_t st, void *fixed_ws)
 {
+    {
+        const int32_t rc = check(c, what, calls, n_calls, window, n_sink);
+        if (rc != PC_OK) return rc;
+    }
     auto in_place = [&](int32_t first, int32_t n, int64_t row, uint32_t mark) {
         const int64_t at = row * c->cfg.n_q_heads;
-        return attend_window(c, what, calls + first, n, INT32_MAX, 0, q ? (const uint16_t *)q + at * c->D : nullptr, out ? (uint16_t *)out + at * c->D : nullptr,
+        return attend_window(c, what, calls + first, n, window, n_sink, q ? (const uint16_t *)q + at * c->D : nullptr, out ? (uint16_t *)out + at * c->D : nullptr,
                              lse ? lse + at : nullptr, st, fixed_ws, mark);
+    };
+    // every row of the call sees all that it lists (and of the new message what is not behind it)
+    auto sees_all = [&](const pc_call &call) {
+        if (window == INT32_MAX) return true;
+        Resolved r;
+        if (pc_resolve(c, &call, 0, r) != PC_OK) return false;           // (refused where it is planned)
+        const int32_t low = win_low(*std::max_element(r.q_pos.begin(), r.q_pos.end()), window);
+        for (const int2 &s : r.sel) if (s.y < low) return false;
+        return r.self_msg < 0 || r.self_start >= low;
     };
     // tokens that a call lists, if it is long
     auto long_tokens = [&](const pc_call &call) -> int64_t {
@@ -1006,10 +1020,10 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
         auto add = [&](int32_t m) { if (known(c, m)) tokens += chain_len(c, m); };
         for (int32_t e = 0; e < call.n_sel; ++e) add(call.sel[e].msg_id);
         add(call.self_msg);
-        return tokens < 100000000 ? tokens : 0;
+        return tokens < 100000000 && sees_all(call) ? tokens : 0;
     };
     std::vector<int64_t> tokens((size_t)std::max(n_calls, 0));
-    for (int32_t i = 0; i < n_calls && calls; ++i) tokens[(size_t)i] = long_tokens(calls[i]);
+    for (int32_t i = 0; i < n_calls; ++i) tokens[(size_t)i] = long_tokens(calls[i]);
     // runs of long calls; each ends the launches that the calls before and behind it would share: several have to earn more
     int runs = 0;
     for (size_t i = 0; i < tokens.size(); ++i) runs += tokens[i] > 0 && (i == 0 || tokens[i - 1] == 0);
@@ -1074,7 +1088,10 @@ int32_t pc_attend_window(pc_cache *c, const pc_call *calls, int32_t n_calls, int
                          void *stream)
 {
     if (!c) return PC_ERR_INVALID_ARG;
-    return pc_guarded(c, [&] { return attend_window(c, "attend_window", calls, n_calls, window, n_sink, q, out, lse, (hipStream_t)stream, nullptr); });
+    return pc_guarded(c, [&] {
+        if (c->cfg.dtype == PC_MX4) return pc_attend_mx4(c, "attend_window", calls, n_calls, window, n_sink, q, out, lse, (hipStream_t)stream, nullptr);
+        return attend_window(c, "attend_window", calls, n_calls, window, n_sink, q, out, lse, (hipStream_t)stream, nullptr);
+    });
 }
 
 int32_t pc_attend_window_static(pc_cache *c, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out, float *lse,

@@ -206,6 +206,18 @@ def test_queries_that_are_no_numbers():
     layer.cache.close()
 
 
+def test_windows_that_leave_all():
+    """Rows whose window reaches just to the first token that they list, and one short of it; positions that a call states, sinks, messages in front."""
+    layer = Layer4([100, 90, 200, 70], 16, 2)
+    layer.cache.set_key_gather(2)
+    sel = [(0, 0), (1, 130)]
+    for window in (299, 300, 301, 369, 370, 371, 1 << 20, 2147483647):
+        # rows at 300 to 369: the last sees all from a window of 370 on
+        layer.run([(sel, 3, 300, 70)], window, 0)
+        layer.run([(sel, 3, 300, 70), (sel, -1, 300, 1), (sel, 2, -50, 200), (sel[:1], -1, 0, 40, [100 + 5 * i for i in range(40)])], window, 3)
+    layer.cache.close()
+
+
 @pytest.mark.parametrize("powers", [(13, -11), (14, 0), (0, -16), (40, -40)])
 def test_values_inside_and_outside_fp16(powers):
     """Values by powers of two that fp16 holds, and that it does not, for single tokens that share their messages and for rows, short and long: each sees
