@@ -1297,7 +1297,7 @@ int32_t pc_plan_and_stage(pc_cache *c, const pc_call *calls, int32_t n_calls, bo
                 // divide THAT count evenly, so the groups with early rows do not end up with a nearly empty
                 // last split.
                 const int parent_tiles = Tc - own_tiles;
-                wide = ns > 1 && small_splits && c->prefill_tiles_per_split == 0 && plain_splits(pre_groups, Tc) == 1;
+                wide = ns > 1 && (P.mx4_rows || (small_splits && c->prefill_tiles_per_split == 0 && plain_splits(pre_groups, Tc) == 1));
                 for (int gidx = 0; gidx < groups; ++gidx, --items_left) {
                     int Tg = Tc;
                     if (r.self_msg >= 0) {
@@ -1331,7 +1331,7 @@ int32_t pc_plan_and_stage(pc_cache *c, const pc_call *calls, int32_t n_calls, bo
             }
             // Partial results are fp32 where the plain rule would not have split the rows at all, so that no sum is held in fewer
             // bits for being split; the others, fp16, are bound by the bytes they move (512 rows x 32 heads in 4 splits: 17 MB,
-            // 8 us).
+            // 8 us).  The values of a PC_MX4 cache go far beyond fp16's (6 x 2^60 to 2^-61): always fp32.
             cd.part_wide = wide;
             if (cd.n_splits > 1) {
                 const int64_t n = ((int64_t)cd.n_splits * cd.n_q) << cd.part_wide;
