@@ -117,6 +117,9 @@ template <bool F16> __device__ __forceinline__ uint32_t pack_query(float a, floa
     else return pack_bf16(a, b);
 }
 
+// two bf16 values hold neither an infinity nor a NaN
+__device__ __forceinline__ bool are_numbers(uint32_t w) { return ((w & 0x7F80u) != 0x7F80u) & ((w & 0x7F800000u) != 0x7F800000u); }
+
 // PACKED: the call's keys and values were copied by the gather pass into a buffer of their own, token after token in
 // the order the call lists them (keys already turned to the positions the call gives them), the parents' part padded
 // to whole tiles, then the new message.  Tile t of the call then sits at slot 32 t of that copy, only the last tile
@@ -168,8 +171,10 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcR
     bf16x8 qop[8];
     // PACKED: the same values go straight into the bf16 MFMA operands (qop[ks]: dims 16 ks + 8 hh + j, qop[ks + 4]: 64 up)
     float qn2 = 0.f;                                     // PACKED: the largest squared norm of the wave's query rows (scaled, turned)
+    bool outside = false;                                // F16: some row of the wave holds what is no number, or has a norm above 2^10
     auto load_query_direct = [&]() __attribute__((always_inline)) {
         float ss = 0.f;
+        bool numbers = true;
         const uint16_t *qp = (const uint16_t *)L.q + ((int64_t)Rg * L.n_q_heads + h) * PC_D + 8 * hh;
         const float2 *rq = L.rot_q + (int64_t)Rg * (PC_D / 2) + 8 * hh;
         const float sc = row_ok ? L.scale_log2 : 0.f;
@@ -177,6 +182,10 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcR
         for (int ks = 0; ks < 4; ++ks) {
             uint4 lo = ldg16(qp + 16 * ks), hi = ldg16(qp + 16 * ks + 64);
             const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
+            if constexpr (F16) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) numbers = numbers && are_numbers(lw[j]) && are_numbers(hw[j]);
+            }
             float xx[8], yy[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -191,6 +200,9 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcR
             qop[ks + 4] = __builtin_bit_cast(bf16x8, make_uint4(pack_query<F16>(yy[0], yy[1]), pack_query<F16>(yy[2], yy[3]), pack_query<F16>(yy[4], yy[5]), pack_query<F16>(yy[6], yy[7])));
         }
         ss = sum_across_halves(ss);                      // the row's squared norm, then the largest of the wave's 32 rows
+        // (row by row, in front of a maximum that drops what is no number, and on the bits, as this file's floats are taken to be numbers; a query of norm 2^10
+        // at most: its values fit, and what keys below fp16's normal numbers are off by, 2^-25, moves a score by no more than 2^-25 x 2^10 x sqrt(128))
+        if constexpr (F16) outside = __builtin_amdgcn_ballot_w64(!numbers || (__float_as_uint(ss) & 0x7FFFFFFFu) > __float_as_uint(0x1p20f)) != 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) ss = __builtin_fmaxf(ss, __shfl_xor(ss, o));
         qn2 = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(ss)));
@@ -591,9 +603,7 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcR
 #pragma unroll
             for (int w8 = 1; w8 < 8; ++w8) kn2 = __builtin_fmaxf(kn2, s_red[w8]);
             bounded = qn2 * kn2 * 1.05f <= LAZY_LOG2 * LAZY_LOG2;
-            // (a query of norm 2^10 at most: its values fit, and what keys below fp16's normal numbers are off by, 2^-25, moves a
-            // score by no more than 2^-25 x 2^10 x sqrt(128))
-            if (F16 && qn2 > 0x1p20f && lane == 0) *range.mark = range.value;
+            if (F16 && outside && lane == 0) *range.mark = range.value;
         }
 
         // tile 0: scores and softmax part 1, nothing to overlap with yet; leaves the K fragments

@@ -39,3 +39,26 @@ def test_values_outside_fp16_over_a_copy_in_splits(power):
         want, want_lse = layer.want(calls, q)
         same(out.double() / unit, lse, want / unit, want_lse, f"values by 2^{power}, {rows} rows")
     layer.cache.close()
+
+
+@pytest.mark.parametrize("what", ["NaN", "infinities at position 0", "both"])
+def test_queries_that_are_no_numbers_over_a_copy_in_splits(what):
+    """A row's head whose query holds a NaN or an infinity is NaN, its log-sum-exp too, and no other is touched: NaN of either sign, infinities where a
+    turn's sine is zero and elsewhere, in first, middle and last rows and dims."""
+    layer = Layer4(LENS, 16, 2)
+    for gather, tiles, rows in WAYS:
+        layer.cache.set_key_gather(gather)
+        layer.cache.set_tuning(0, tiles)
+        calls = [(SEL, -1, 0, rows)]
+        q = layer.normal(rows, 16, 128)
+        spoilt, bad = q.copy(), np.zeros((rows, 16), bool)
+        places = {"NaN": [(0, 9, 127, np.nan), (31, 0, 64, -np.nan), (rows - 1, 15, 0, np.nan)], "infinities at position 0": [(0, 3, 5, np.inf), (0, 15, 127, -np.inf)],
+                  "both": [(0, 3, 5, np.inf), (2, 9, 1, np.nan), (rows - 2, 15, 63, -np.inf)]}[what]
+        for r, h, d, x in places:
+            spoilt[r, h, d], bad[r, h] = x, True
+        out, lse = split(layer, calls, spoilt)
+        want, want_lse = layer.want(calls, q)
+        some, rest = layer.torch.from_numpy(bad), layer.torch.from_numpy(~bad)
+        assert out[some].isnan().all() and lse[some].isnan().all(), f"{rows} rows"
+        same(out[rest], lse[rest], want[~bad], want_lse[~bad], f"{rows} rows")
+    layer.cache.close()
