@@ -399,13 +399,14 @@ __device__ __forceinline__ void ring_barrier() { asm volatile("s_barrier" ::: "m
 constexpr int ROWS_RING = 4, ROWS_SLOT = PC_MX4_CODES + PC_TILE * PC_D * 2 + 256;
 }  // namespace
 
-// HALF: probabilities and values in fp16, where no value of the cache is outside it; the reference of a row keeps its largest probability between 2^-4
-// (none yet seen) and 2^15.
+// HALF: probabilities and values in fp16, where no value of the cache is outside it.  A row's first scores put their largest at 2^ABOVE, and the reference
+// moves where one would be above 2^LAZY_LOG2: what is 2^20 below a row's largest still is a normal number, and 2^30 below it one of a few bits.  (With a
+// reference that stays at zero where a row's first scores are near it, what is 2^21 below a row's largest would be lost; less work, but no less time.)
 template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, const PcMx4Rows &M, unsigned char *s_kv, uint32_t (*s_rot)[PC_D / 2])
 {
     constexpr int RING = ROWS_RING, AHEAD = 3, LOADS = 3;
     constexpr int VALUES = PC_MX4_CODES, EXPS = VALUES + PC_TILE * PC_D * 2, SLOT = ROWS_SLOT;
-    constexpr float LAZY_LOG2 = HALF ? 15.f : 64.f, LOWEST = HALF ? -4.f : -64.f, ABOVE = HALF ? 6.f : 0.f;
+    constexpr float LAZY_LOG2 = HALF ? 15.f : 64.f, ABOVE = HALF ? 6.f : 0.f;
     const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
     const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
     const int g = W.n_q_heads / W.n_kv_heads;
@@ -480,7 +481,7 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
     asm volatile("" : "+v"(e_rd));
 
     float m_ref = 0.f, l_run = 0.f;
-    bool seen = false, all_seen = false, shifted = false;          // the row has met a key; every row of the wave has; some row's reference has moved
+    bool seen = false, all_seen = false;                 // the row has met a key; every row of the wave has
     f32x16 acc[4];
     const f32x16 zeros = (f32x16){0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -499,24 +500,17 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const bool now = mx > -INFINITY, need = mx > LAZY_LOG2 || (!seen && now && mx < LOWEST);
+        const bool now = mx > -INFINITY, need = mx > LAZY_LOG2 || (!seen && now);
         seen |= now;
         all_seen = __builtin_amdgcn_ballot_w64(seen) == ~0ull;
         if (__builtin_amdgcn_ballot_w64(need) != 0) {
-            const float shift = !need ? 0.f : mx > 0.f ? mx - ABOVE : mx, alpha = ex2(-fmaxf(shift, 0.f));       // (down: nothing has been added yet)
+            const float shift = need ? mx - ABOVE : 0.f, alpha = ex2(-fmaxf(shift, 0.f));       // (down: nothing has been added yet)
             l_run *= alpha;
 #pragma unroll
             for (int db = 0; db < 4; ++db) acc[db] *= alpha;
             m_ref += shift;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] -= shift;
-            shifted = __builtin_amdgcn_ballot_w64(m_ref != 0.f) != 0;
-        }
-    };
-    auto less_reference = [&](f32x16 &s) __attribute__((always_inline)) {
-        if (__builtin_expect(shifted, 0)) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] -= m_ref;
         }
     };
     auto score = [&](unsigned at) __attribute__((always_inline)) {
@@ -554,43 +548,6 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
         int t = 0;
 #pragma unroll 1
         while (t < T) {
-            // Four tiles of which every row sees everything, the ring's places as constants: nothing is looked up, masked or turned.
-            if ((t & (RING - 1)) == 0 && walk.a.z >= RING * PC_TILE && walk.rot == cur && all_seen && !shifted &&
-                (lo_max <= walk.a.y || walk.a.w >= RING * PC_TILE) && (!walk.self || lim_first - walk.a.y >= RING * PC_TILE - 1) &&
-                T - asked >= RING && ahead.a.z > (RING - 1) * PC_TILE) {
-                const int slot0 = ahead.a.x;
-#pragma unroll
-                for (int u = 0; u < RING; ++u) {
-                    const int at = u * SLOT;
-                    wait_vm<LOADS * (AHEAD - 1)>();
-                    ring_barrier();
-                    request(slot0 + PC_TILE * u, place, (u + AHEAD) & (RING - 1));
-                    f32x16 s = score(at);
-                    bf16x8 fr[8];
-#pragma unroll
-                    for (int f = 0; f < 8; ++f) fr[f] = *(lds_frag)(v_rd + at + ((f >> 2) * 2 * PC_D + 32 * (f & 3)) * 16);
-                    less_reference(s);
-                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(largest(s) > fi(LAZY_LOG2)) != 0, 0)) rebase(s);
-                    uint32_t pk[8];
-                    float ps = 0.f;
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        pk[r] = mx4_pack<HALF>(ex2(s[2 * r]), ex2(s[2 * r + 1]));
-                        ps = mx4_sum<HALF>(pk[r], ps);
-                    }
-                    l_run += ps;
-                    const bf16x8 p[2] = {__builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3])), __builtin_bit_cast(bf16x8, make_uint4(pk[4], pk[5], pk[6], pk[7]))};
-#pragma unroll
-                    for (int f = 0; f < 8; ++f) acc[f & 3] = mx4_mfma32<HALF>(fr[f], p[f >> 2], acc[f & 3]);
-                }
-                asked += RING;
-                ahead.pass(RING - 1);
-                if (asked < T) further();
-                t += RING;
-                walk.pass(RING - 1);
-                if (t < T) walk.next();
-                continue;
-            }
             const int u = t & (RING - 1);
             const unsigned at = u * SLOT;
             if (t + AHEAD <= T) wait_vm<LOADS * (AHEAD - 1)>();        // this wave's share of tile t has landed
@@ -600,7 +557,8 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
             if (__builtin_expect(e.rot != cur, 0)) { cur = e.rot; turn(cur, std::true_type{}); }
             ask((u + AHEAD) & (RING - 1));
             f32x16 s = score(at);
-            less_reference(s);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] -= m_ref;
             const bool edge = e.valid < PC_TILE || (e.self && lim_first - e.pos0 < PC_TILE - 1) || (lo_max > e.pos0 && e.sink < PC_TILE);
             bool none = false;
             if (__builtin_expect(edge, 0)) {
@@ -685,7 +643,8 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
     }
 }
 
-__global__ __launch_bounds__(256, 2) void pc_mx4_prefill_kernel(PcWin W, PcMx4Rows M)
+// (two waves a SIMD and not three, for which there were registers: 2048 rows of 64 heads over one message of 13k tokens 809 us, so 855; windows of 4096 270 and 300)
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(2, 2))) void pc_mx4_prefill_kernel(PcWin W, PcMx4Rows M)
 {
     __shared__ __attribute__((aligned(1024))) unsigned char s_kv[ROWS_RING * ROWS_SLOT];
     __shared__ __attribute__((aligned(16))) uint32_t s_rot[4][PC_D / 2];         // a wave's cosines and sines, in fp16
