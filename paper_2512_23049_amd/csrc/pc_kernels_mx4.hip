@@ -406,7 +406,7 @@ template <bool HALF> __device__ __forceinline__ void mx4_rows(const PcWin &W, co
 {
     constexpr int RING = ROWS_RING, AHEAD = 3, LOADS = 3;
     constexpr int VALUES = PC_MX4_CODES, EXPS = VALUES + PC_TILE * PC_D * 2, SLOT = ROWS_SLOT;
-    constexpr float LAZY_LOG2 = HALF ? 15.f : 64.f, ABOVE = HALF ? 6.f : 0.f;
+    constexpr float LAZY_LOG2 = HALF ? 15.f : 32.f, ABOVE = HALF ? 6.f : 0.f;         // (2^31 keys of 2^32 x 6 x 2^60 fit 32 bits)
     const int kh = blockIdx.x % W.n_kv_heads;          // consecutive workgroups (one per XCD) take different KV heads
     const PcWinItem item = W.items[blockIdx.x / W.n_kv_heads];
     const int g = W.n_q_heads / W.n_kv_heads;
@@ -661,7 +661,8 @@ void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, 
 // ------------------------------------------------------------------------------------------------------------ gather
 // Long prefills (see pc_attend_mx4): the call's keys and values copied token after token into a packed copy, as pc_gather_kernel does it for bf16,
 // keys turned to the positions that the call gives them and rounded to fp16 (off by 2^-12 of a value), values as the bf16 that they stand for.
-// Keys above 6 x 2^7, and those that are no number (which that walk would add to masks), mark the call for the walk behind it: below, what
+// Values above 7 x 2^24 (times probabilities of 2^64, where that walk's reference need not move, and 2^31 keys, they would not fit 32 bits), keys above 6 x 2^7, and
+// those that are no number (which that walk would add to masks), mark the call for the walk behind it: below, what
 // queries under fp16's normal numbers are off by, 2^-25, moves a score by 2^-25 x 2^10 x sqrt(128) at most.
 // Bound: memory, 136 bytes read and 512 written a token and KV head (9.9k tokens of 8 KV heads: 22 us; the walk behind it, pc_prefill_bf16_kernel, 2048
 // rows of 64 heads: 490 us, 1.2 PFLOP/s, where the walk over the cache itself takes 930).
@@ -751,7 +752,7 @@ __global__ __launch_bounds__(256) void pc_mx4_gather_kernel(PcLaunch L, const Pc
             run = run && sl[0] >= 0 && sl[k] == sl[0] + k;
         }
         uint32_t w = 0;
-        uint64_t ex = 0;
+        uint64_t ex = 0;                                   // (60 less the exponents)
         if (run) {                                         // of two groups of the cache
             const int sh = sl[0] & 7;
             w = word_of(sl[0]) >> 4 * sh;
@@ -762,12 +763,14 @@ __global__ __launch_bounds__(256) void pc_mx4_gather_kernel(PcLaunch L, const Pc
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < PC_VGROUP; ++k)
-                if (sl[k] >= 0) {
-                    w |= (word_of(sl[k]) >> 4 * (sl[k] & 7) & 15u) << 4 * k;
-                    ex |= (exps_of(sl[k]) >> 8 * (sl[k] & 7) & 255u) << 8 * k;
-                }
+            for (int k = 0; k < PC_VGROUP; ++k) {
+                if (sl[k] >= 0) w |= (word_of(sl[k]) >> 4 * (sl[k] & 7) & 15u) << 4 * k;
+                ex |= (sl[k] >= 0 ? exps_of(sl[k]) >> 8 * (sl[k] & 7) & 255u : (uint64_t)PC_MX4_E_MAX) << 8 * k;
+            }
         }
+        // some exponent of the eight is above PC_MX4_COPIED
+        constexpr uint64_t EACH = 0x0101010101010101ull;
+        if (~((ex | 0x80 * EACH) - (PC_MX4_E_MAX - PC_MX4_COPIED) * EACH) & 0x80 * EACH) *mark = value;
         const uint32_t e0 = (uint32_t)ex, e1 = (uint32_t)(ex >> 32);
         uint4 x;
         x.x = mx4_values(w, e0, std::integral_constant<int, 0>{}); x.y = mx4_values(w, e0, std::integral_constant<int, 1>{});

@@ -58,7 +58,7 @@ template <int NW> struct SharedLds {
 template <int NW, bool HALF> __device__ __forceinline__ void shared_decode(const PcWin &W, const PcWinShared &S, SharedLds<NW> &lds)
 {
     constexpr int LOADS = 16 / NW;
-    constexpr float LAZY_LOG2 = HALF ? 15.f : 64.f, ABOVE = HALF ? 6.f : 0.f;
+    constexpr float LAZY_LOG2 = HALF ? 15.f : 32.f, ABOVE = HALF ? 6.f : 0.f;         // (2^31 keys of 2^32 x 6 x 2^60 fit 32 bits)
     auto &s_kv = lds.kv;
     auto &s_v = lds.v;
     auto &s_rot = lds.rot;

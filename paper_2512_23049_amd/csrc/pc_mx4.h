@@ -19,6 +19,7 @@
 #define PC_MX4_TILE (PC_TILE * PC_MX4_ROW)
 #define PC_MX4_E_MAX 60
 #define PC_MX4_HALF 13                // exponents from -13 to 13: the values are exact, and normal numbers, in fp16
+#define PC_MX4_COPIED 24              // exponents of values that a long prefill's walk over a copy takes, at most
 #define PC_MX4_NAN 255                // exponent of a block of keys that are NaN
 
 struct PcWin;
