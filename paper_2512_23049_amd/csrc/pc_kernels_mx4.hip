@@ -661,9 +661,9 @@ void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, 
 // ------------------------------------------------------------------------------------------------------------ gather
 // Long prefills (see pc_attend_mx4): the call's keys and values copied token after token into a packed copy, as pc_gather_kernel does it for bf16,
 // keys turned to the positions that the call gives them and rounded to fp16 (off by 2^-12 of a value), values as the bf16 that they stand for.
-// Values above 7 x 2^24 (times probabilities of 2^64, where that walk's reference need not move, and 2^31 keys, they would not fit 32 bits), keys above 6 x 2^7, and
-// those that are no number (which that walk would add to masks), mark the call for the walk behind it: below, what
-// queries under fp16's normal numbers are off by, 2^-25, moves a score by 2^-25 x 2^10 x sqrt(128) at most.
+// Values above 7 x 2^24 (times probabilities of 2^64, where that walk's reference need not move, and 2^31 keys, they would not fit 32 bits), keys of a norm
+// above 2^10, and those that are no number (which that walk would add to masks), mark the call for the walk behind it: below, what queries under
+// fp16's normal numbers are off by, 2^-25, moves a score by 2^-25 x 2^10 x sqrt(128) at most.
 // Bound: memory, 136 bytes read and 512 written a token and KV head (9.9k tokens of 8 KV heads: 22 us; the walk behind it, pc_prefill_bf16_kernel, 2048
 // rows of 64 heads: 490 us, 1.2 PFLOP/s, where the walk over the cache itself takes 930).
 __global__ __launch_bounds__(256) void pc_mx4_gather_kernel(PcLaunch L, const PcGatherItem *__restrict__ items, int n_items, const int32_t *__restrict__ seg_kvoff,
@@ -713,8 +713,9 @@ __global__ __launch_bounds__(256) void pc_mx4_gather_kernel(PcLaunch L, const Pc
             const uint32_t a = *reinterpret_cast<const uint32_t *>(kt + slot % PC_TILE * 64 + 4 * c), b = *reinterpret_cast<const uint32_t *>(kt + slot % PC_TILE * 64 + 32 + 4 * c);
             const uint32_t ex = *reinterpret_cast<const uint32_t *>(kt + PC_MX4_CODES + slot % PC_TILE * 4) >> 8 * (c >> 2);
             const uint32_t ea = ex & 255u, eb = ex >> 16 & 255u;
-            if (max(ea, eb) > 127u + 7u) *mark = value;     // (255: no number)
-            const float ua = __uint_as_float(min(ea, 127u + 7u) << 23), ub = __uint_as_float(min(eb, 127u + 7u) << 23);
+            // (255: no number, which has codes of zero; a block of 2^10 holds one above 2^10, whose square marks the call: larger ones need no more)
+            if (max(ea, eb) == (uint32_t)PC_MX4_NAN) *mark = value;
+            const float ua = __uint_as_float(min(ea, 127u + 10u) << 23), ub = __uint_as_float(min(eb, 127u + 10u) << 23);
             const float4 *rot = reinterpret_cast<const float4 *>(L.rot_seg + (int64_t)(cd.seg_off + s_seg[r]) * (PC_D / 2) + 8 * c);
             uint32_t *lw = reinterpret_cast<uint32_t *>(&lo), *hw = reinterpret_cast<uint32_t *>(&hi);
             auto pair = [&](auto u) __attribute__((always_inline)) {
@@ -732,6 +733,7 @@ __global__ __launch_bounds__(256) void pc_mx4_gather_kernel(PcLaunch L, const Pc
         *reinterpret_cast<uint4 *>(dst + 64) = hi;
         // The largest squared norm of the tile's keys (see pc_gather_kernel).  Eight lanes hold a row.
         ss += __shfl_xor(ss, 1); ss += __shfl_xor(ss, 2); ss += __shfl_xor(ss, 4);
+        if (ss > 0x1p20f) *mark = value;
         ss = fmaxf(ss, __shfl_xor(ss, 8)); ss = fmaxf(ss, __shfl_xor(ss, 16)); ss = fmaxf(ss, __shfl_xor(ss, 32));
         if ((threadIdx.x & 63) == 0) s_norm[threadIdx.x >> 6] = ss;
     }
