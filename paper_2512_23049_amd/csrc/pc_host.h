@@ -65,6 +65,7 @@ struct pc_cache {
     double *inv_freq_dev = nullptr;
     void *ws = nullptr; size_t ws_cap = 0;
     size_t ws_refused = SIZE_MAX;                        // a gradient's workspace the device had no room for
+    size_t copy_refused = SIZE_MAX;                      // likewise, with the copy of a long prefill of a PC_MX4 cache
     void *tok_dev = nullptr; size_t tok_cap = 0;          // staged items of pc_append_tokens* / pc_reposition_batch (bytes)
     StageSlot stage[N_STAGE]; int stage_next = 0;
     uint32_t *stage_done = nullptr;                     // what the slots' done point to

@@ -1469,7 +1469,10 @@ int32_t pc_plan_and_stage(pc_cache *c, const pc_call *calls, int32_t n_calls, bo
                            P.lay.h2d_bytes, c->stage[c->stage_next].cap);
         P.ws = P.fixed_ws;
     } else {
+        // (a copy that the device had no room for is not asked for again: its calls are served without one)
+        if (P.mx4_rows && P.lay.total > c->ws_cap && P.lay.total >= c->copy_refused) return pc_fail(c, PC_ERR_HIP, "workspace of %zu bytes: refused before", P.lay.total);
         rc = pc_ensure_ws(c, P.lay.total, st);
+        if (rc != PC_OK && P.mx4_rows) c->copy_refused = std::min(c->copy_refused, P.lay.total);
         if (rc != PC_OK) return rc;
         P.ws = c->ws;
     }

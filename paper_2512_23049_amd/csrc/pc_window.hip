@@ -64,7 +64,8 @@ private:
     }
 };
 
-int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan &P)
+// (first: the number of calls[0] in the caller's list)
+int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan &P, int32_t first = 0)
 {
     P.res.resize((size_t)n_calls);
     P.calls.resize((size_t)n_calls);
@@ -73,7 +74,7 @@ int32_t resolve_all(pc_cache *c, const pc_call *calls, int32_t n_calls, WinPlan 
     for (int i = 0; i < n_calls; ++i) entries += (size_t)std::max(calls[i].n_sel, 0) + 1;
     P.segs.reserve(entries);
     for (int i = 0; i < n_calls; ++i) {
-        const int32_t rc = pc_resolve(c, &calls[i], i, P.res[(size_t)i]);
+        const int32_t rc = pc_resolve(c, &calls[i], first + i, P.res[(size_t)i]);
         if (rc != PC_OK) return rc;
         const Resolved &r = P.res[(size_t)i];
         WinCall &wc = P.calls[(size_t)i];
@@ -706,28 +707,11 @@ int32_t check(pc_cache *c, const char *what, const pc_call *calls, int32_t n_cal
     return PC_OK;
 }
 
-// mark: 0, or: nothing is done unless the cache's mark is that (PC_MX4, calls of many rows)
-int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out,
-                      float *lse, hipStream_t st, void *fixed_ws, uint32_t mark = 0)
+// What the resolved calls launch, and where it stands in the workspace.  marked: for a walk that mostly does nothing: no splits, and with them no merge.
+int32_t plan_window(pc_cache *c, const char *what, const void *fixed_ws, bool recorded, bool marked, WinPlan &P, WinLayout &L)
 {
-    int32_t rc = check(c, what, calls, n_calls, window, n_sink);
-    if (rc != PC_OK || n_calls == 0) return rc;
-    if (!c->host_only && (!q || !out)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: null q or out", what);
-    if (!c->host_only && ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)))
-        return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
-    static thread_local WinPlan P;                       // (32 calls over 410 messages, 64 heads: 264 us a call with fresh lists, 256 with these)
-    struct Kept { ~Kept() { P.trim(); } } kept;
-    P.clear();
-    P.window = window; P.n_sink = n_sink;
-    rc = resolve_all(c, calls, n_calls, P);
-    if (rc != PC_OK || c->host_only) return rc;
-    PcDeviceScope on(c);
-    if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
-    const bool recorded = pc_recorded(st);
-    if (recorded && !fixed_ws)
-        return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move: use pc_attend_window_static", what);
-    plan_items(c, P, mark == 0);                         // (marked: no splits, and with them no merge)
-    WinLayout L = lay_out(c, P);
+    plan_items(c, P, !marked);
+    L = lay_out(c, P);
     // Lists of single tokens that their launch's arguments do not hold cost a launch in front of it and the event behind that, 7 us: a few
     // longer splits are better where that helps (4 calls of 130 tiles: 22.5 -> 16.5 us; 16 of 17: 19 -> 12).
     const size_t whole = sizeof(PcWinRun) * P.runs.size() + (sizeof(PcWinItem) + sizeof(int32_t)) * P.calls.size();
@@ -748,6 +732,14 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         if (L.total > PC_STATIC_WS_BYTES)
             return pc_fail(c, PC_ERR_NO_SPACE, "%s: needs a workspace of %zu bytes, the fixed one has %zu", what, L.total, PC_STATIC_WS_BYTES);
     }
+    return PC_OK;
+}
+
+// The launches of a planned call.  mark: 0, or: nothing is done unless the cache's mark is that (PC_MX4, calls of many rows)
+int32_t launch_window(pc_cache *c, const char *what, const WinPlan &P, const WinLayout &L, const void *q, void *out, float *lse, hipStream_t st, void *fixed_ws,
+                      bool recorded, uint32_t mark)
+{
+    int32_t rc = PC_OK;
     const bool in_args = L.lists <= PC_ARG_BYTES;
     StageSlot *slot = nullptr;
     std::vector<char> held;                              // lists of a call that is recorded (see pc_recorded)
@@ -776,7 +768,7 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
     W.k_store = c->k_store; W.v_store = c->v_store; W.q = q; W.out = out; W.lse = lse;
     W.part_o = (float *)(ws + L.part_o); W.part_ml = (float *)(ws + L.part_ml);
     W.slots = c->slots; W.n_q_heads = c->cfg.n_q_heads; W.n_kv_heads = c->cfg.n_kv_heads;
-    W.window = window;
+    W.window = P.window;
     W.scale_log2 = c->scale * 1.4426950408889634f;
     // Lists in the arguments of the decode launch are read there; everything else reads them from the workspace.
     const bool direct = in_args && P.pre.empty() && P.sh_items.empty();
@@ -846,6 +838,31 @@ int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32
         PC_HIP(c, hipGetLastError());
     }
     return PC_OK;
+}
+
+int32_t attend_window(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out,
+                      float *lse, hipStream_t st, void *fixed_ws)
+{
+    int32_t rc = check(c, what, calls, n_calls, window, n_sink);
+    if (rc != PC_OK || n_calls == 0) return rc;
+    if (!c->host_only && (!q || !out)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: null q or out", what);
+    if (!c->host_only && ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)))
+        return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
+    static thread_local WinPlan P;                       // (32 calls over 410 messages, 64 heads: 264 us a call with fresh lists, 256 with these)
+    struct Kept { ~Kept() { P.trim(); } } kept;
+    P.clear();
+    P.window = window; P.n_sink = n_sink;
+    rc = resolve_all(c, calls, n_calls, P);
+    if (rc != PC_OK || c->host_only) return rc;
+    PcDeviceScope on(c);
+    if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
+    const bool recorded = pc_recorded(st);
+    if (recorded && !fixed_ws)
+        return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move: use pc_attend_window_static", what);
+    WinLayout L;
+    rc = plan_window(c, what, fixed_ws, recorded, false, P, L);
+    if (rc != PC_OK) return rc;
+    return launch_window(c, what, P, L, q, out, lse, st, fixed_ws, recorded, 0);
 }
 
 int32_t backward_run(pc_cache *c, WinPlan &P, const std::vector<int2> &range, PcWin W, PcWinBwd G, hipStream_t st)
@@ -999,11 +1016,6 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
         const int32_t rc = check(c, what, calls, n_calls, window, n_sink);
         if (rc != PC_OK) return rc;
     }
-    auto in_place = [&](int32_t first, int32_t n, int64_t row, uint32_t mark) {
-        const int64_t at = row * c->cfg.n_q_heads;
-        return attend_window(c, what, calls + first, n, window, n_sink, q ? (const uint16_t *)q + at * c->D : nullptr, out ? (uint16_t *)out + at * c->D : nullptr,
-                             lse ? lse + at : nullptr, st, fixed_ws, mark);
-    };
     // every row of the call sees all that it lists (and of the new message what is not behind it)
     auto sees_all = [&](const pc_call &call) {
         if (window == INT32_MAX) return true;
@@ -1037,38 +1049,69 @@ int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32
         if (!kept) std::fill(tokens.begin() + (ptrdiff_t)i, tokens.begin() + (ptrdiff_t)e, 0);
         i = std::max(e, i + 1);
     }
-    if (!some) return in_place(0, n_calls, 0, 0);
-    // (runs of calls of a kind follow each other: nothing may be refused behind the first)
+    if (!some) return attend_window(c, what, calls, n_calls, window, n_sink, q, out, lse, st, fixed_ws);
+    // Runs of calls of a kind follow each other.  Nothing may be refused behind the first: all are planned, and have room for the walk over the cache, before it.
     if (!q || !out) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: null q or out", what);
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned, lse 4-byte", what);
-    if (pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move", what);
-    {
-        WinPlan P;
-        const int32_t rc = resolve_all(c, calls, n_calls, P);
-        if (rc != PC_OK) return rc;
-    }
-    PcDeviceScope on(c);
-    if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
+    struct Run { int32_t first, n; int64_t row; bool copied; WinPlan P; WinLayout L; };
+    static thread_local std::vector<Run> kept;           // (lists as in attend_window)
+    struct Kept { ~Kept() { for (Run &r : kept) r.P.trim(); if (kept.size() > 4) kept.resize(4); } } trim;
+    size_t n_runs = 0;
     int64_t row = 0;
-    for (int32_t a = 0; a < n_calls;) {
-        bool kind = tokens[(size_t)a] > 0;
+    for (int32_t a = 0; a < n_calls; ++n_runs) {
+        if (n_runs == kept.size()) kept.emplace_back();
+        Run &r = kept[n_runs];
+        r.first = a; r.row = row; r.copied = tokens[(size_t)a] > 0;
         int32_t b = a;
-        int64_t rows = 0, copied = 0;
-        for (; b < n_calls && (tokens[(size_t)b] > 0) == kind && (b == a || copied + tokens[(size_t)b] <= LONG_TOKENS); ++b) {
-            rows += calls[b].n_q;
+        int64_t copied = 0;
+        for (; b < n_calls && (tokens[(size_t)b] > 0) == r.copied && (b == a || copied + tokens[(size_t)b] <= LONG_TOKENS); ++b) {
+            row += std::max(calls[b].n_q, 0);
             copied += tokens[(size_t)b];
         }
-        int32_t rc = PC_OK;
-        if (kind) {
-            if (++c->mark_epoch_mx4 == 0) c->mark_epoch_mx4 = 1;
-            const int64_t at = row * c->cfg.n_q_heads;
-            rc = pc_attend_gathered_mx4(c, calls + a, b - a, (const uint16_t *)q + at * c->D, (uint16_t *)out + at * c->D, lse ? lse + at : nullptr, st, c->mark_epoch_mx4);
-            if (rc == PC_ERR_HIP) { kind = false; rc = PC_OK; }          // (no room for the copy: what else may have failed fails again)
-        }
-        if (rc == PC_OK) rc = in_place(a, b - a, row, kind ? c->mark_epoch_mx4 : 0);
+        r.n = b - a;
+        r.P.clear();
+        r.P.window = window; r.P.n_sink = n_sink;
+        const int32_t rc = resolve_all(c, calls + a, r.n, r.P, a);
         if (rc != PC_OK) return rc;
-        row += rows;
         a = b;
+    }
+    if (row > INT32_MAX / 2) return pc_fail(c, PC_ERR_SHAPE, "%s: too many query rows", what);
+    PcDeviceScope on(c);
+    if (!on.ok) return pc_fail(c, PC_ERR_HIP, "%s: the cache's device cannot be made current", what);
+    if (pc_recorded(st)) return pc_fail(c, PC_ERR_INVALID_ARG, "%s: the stream is being captured, and the cache's workspace may move", what);
+    size_t need = 0;
+    for (size_t i = 0; i < n_runs; ++i) {
+        const int32_t rc = plan_window(c, what, nullptr, false, kept[i].copied, kept[i].P, kept[i].L);
+        if (rc != PC_OK) return rc;
+        need = std::max(need, kept[i].L.total);
+    }
+    {
+        const int32_t rc = pc_ensure_ws(c, need, st);
+        if (rc != PC_OK) return rc;
+    }
+    for (size_t i = 0; i < n_runs; ++i) {
+        Run &r = kept[i];
+        const int64_t at = r.row * c->cfg.n_q_heads;
+        const uint16_t *rq = (const uint16_t *)q + at * c->D;
+        uint16_t *ro = (uint16_t *)out + at * c->D;
+        float *rl = lse ? lse + at : nullptr;
+        uint32_t mark = 0;
+        if (r.copied) {
+            if (++c->mark_epoch_mx4 == 0) c->mark_epoch_mx4 = 1;
+            mark = c->mark_epoch_mx4;
+            if (pc_attend_gathered_mx4(c, calls + r.first, r.n, rq, ro, rl, st, mark) != PC_OK) {
+                mark = 0;                                // (no room for the copy: what else may have failed fails again)
+                WinPlan P;                               // in splits, if the workspace holds them
+                WinLayout L;
+                P.window = window; P.n_sink = n_sink;
+                if (resolve_all(c, calls + r.first, r.n, P) == PC_OK && plan_window(c, what, nullptr, false, false, P, L) == PC_OK && L.total <= c->ws_cap) {
+                    std::swap(r.P, P);
+                    r.L = L;
+                }
+            }
+        }
+        const int32_t rc = launch_window(c, what, r.P, r.L, rq, ro, rl, st, nullptr, false, mark);
+        if (rc != PC_OK) return rc;
     }
     return PC_OK;
 }
