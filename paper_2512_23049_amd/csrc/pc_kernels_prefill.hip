@@ -117,8 +117,9 @@ template <bool F16> __device__ __forceinline__ uint32_t pack_query(float a, floa
     else return pack_bf16(a, b);
 }
 
-// two bf16 values hold neither an infinity nor a NaN
-__device__ __forceinline__ bool are_numbers(uint32_t w) { return ((w & 0x7F80u) != 0x7F80u) & ((w & 0x7F800000u) != 0x7F800000u); }
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+// the larger magnitudes of two bf16 pairs, as bits: from 0x7F80 on they are no numbers
+__device__ __forceinline__ u16x2 larger_of(u16x2 top, uint32_t w) { return __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)); }
 
 // PACKED: the call's keys and values were copied by the gather pass into a buffer of their own, token after token in
 // the order the call lists them (keys already turned to the positions the call gives them), the parents' part padded
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcR
     bool outside = false;                                // F16: some row of the wave holds what is no number, or has a norm above 2^10
     auto load_query_direct = [&]() __attribute__((always_inline)) {
         float ss = 0.f;
-        bool numbers = true;
+        u16x2 top = {0, 0};
         const uint16_t *qp = (const uint16_t *)L.q + ((int64_t)Rg * L.n_q_heads + h) * PC_D + 8 * hh;
         const float2 *rq = L.rot_q + (int64_t)Rg * (PC_D / 2) + 8 * hh;
         const float sc = row_ok ? L.scale_log2 : 0.f;
@@ -184,7 +185,7 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcR
             const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
             if constexpr (F16) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) numbers = numbers && are_numbers(lw[j]) && are_numbers(hw[j]);
+                for (int j = 0; j < 4; ++j) top = larger_of(larger_of(top, lw[j]), hw[j]);
             }
             float xx[8], yy[8];
 #pragma unroll
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(512, 1) void pc_prefill_bf16_kernel(PcLaunch L, PcR
         ss = sum_across_halves(ss);                      // the row's squared norm, then the largest of the wave's 32 rows
         // (row by row, in front of a maximum that drops what is no number, and on the bits, as this file's floats are taken to be numbers; a query of norm 2^10
         // at most: its values fit, and what keys below fp16's normal numbers are off by, 2^-25, moves a score by no more than 2^-25 x 2^10 x sqrt(128))
-        if constexpr (F16) outside = __builtin_amdgcn_ballot_w64(!numbers || (__float_as_uint(ss) & 0x7FFFFFFFu) > __float_as_uint(0x1p20f)) != 0;
+        if constexpr (F16) outside = __builtin_amdgcn_ballot_w64(top.x >= 0x7F80 || top.y >= 0x7F80 || (__float_as_uint(ss) & 0x7FFFFFFFu) > __float_as_uint(0x1p20f)) != 0;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) ss = __builtin_fmaxf(ss, __shfl_xor(ss, o));
         qn2 = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(ss)));
