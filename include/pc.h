@@ -103,7 +103,7 @@ typedef struct {
  * rows than one, and by single tokens that share their messages, unless the cache was ever given a value whose block of 32 has its largest above 7 x 2^13
  * or, not all zero, below 7 x 2^-14: then, and by other single tokens, in bf16 (values are exact either way).  Calls of more rows than one have the values
  * of the tiles that they see laid out so, and their queries turned, in the workspace: 8 KB a tile of 32 tokens and KV head, 256 bytes a row and query head (in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Long prefills of pc_attend,
- * and of pc_attend_window where the window leaves rows all that they list (calls of at least 512 rows x query heads of a KV head that see 3e7 scores or more), go over a copy of all that they list, 512 bytes a token and KV
+ * and of pc_attend_window where the window leaves rows all that they list (calls of at least 1024 rows x query heads of a KV head that see 3e7 scores or more), go over a copy of all that they list, 512 bytes a token and KV
  * head besides: there turned keys and queries are fp16 (off by 2^-11 of a value), but for values above 7 x 2^24, keys of a norm above 2^10 and rows of queries
  * whose norm, scaled, is above 700, which are served as the others are.  Tensors as pc_attend_window asks for them:
  * q and out 16-byte aligned; and pc_attend and pc_decode_step, like pc_attend_window, refuse a stream that is being captured.  Messages are appended, grown,

@@ -1002,11 +1002,14 @@ int32_t attend_window_backward(pc_cache *c, const pc_call *calls, int32_t n_call
 // message.  The copy's keys and the queries are fp16 for the matrix instructions, whose range keys and queries of models are in; where one is not, the
 // device marks the call, and the walk over the cache itself, which takes any, follows and does nothing otherwise.
 // Taken by calls of LONG_ROWS rows x query heads of a KV head (each copied token is read that often), where those that stand together have
-// LONG_SCORES scores in all (two more launches are to be earned back).  In place and copied, us: 8 calls of 64 rows over 12064 tokens, 64 heads on 8: 337, 311; 32 on
-// 8 (256): 185, 250; one call of 256 rows over 2256 tokens, 64 heads (3.7e7): 64, 62; 32 heads (1.85e7): 53, 56; 8 calls of it: 152, 113;
-// of 1024 rows over 13024 tokens, 64 heads: 5227, 2848.
+// LONG_SCORES scores in all (two more launches are to be earned back).  In place and copied, us, over messages of 64 to 256 tokens, by rows x query heads of
+// a KV head:
+//   512: 8 calls of 64 rows over 12064 tokens, 64 heads on 8, 326 and 347; one over 7.7k 55 and 66, over 30k 130 and 136; 128 rows of 32 heads over 12064 71 and 86;
+//   1024: 128 rows of 64 heads over 12064 105 and 103, over 30k 206 and 187, 8 calls of it over 12064 546 and 489; 4 over 5000 150 and 139; 256 rows of 32 heads 106 and 103;
+//   2048 and more: 256 rows of 64 heads over 2256 (3.7e7 scores) 60 and 67, two calls of it 87 and 82, eight 228 and 191; over 5000 92 and 85; 384 rows over 2256 92 and 73;
+//     512 over 1024 (3.4e7) 60 and 51; 1024 over 13024 573 and 398, 8 calls of it 4450 and 2960.
 // By the caller's word: pc_set_key_gather.
-constexpr int64_t LONG_ROWS = 512;
+constexpr int64_t LONG_ROWS = 1024;
 constexpr double LONG_SCORES = 3e7;
 constexpr int64_t LONG_TOKENS = (int64_t)1 << 22;        // a copy's, where it has more calls than one: 16 GiB of 8 KV heads
 int32_t pc_attend_mx4(pc_cache *c, const char *what, const pc_call *calls, int32_t n_calls, int32_t window, int32_t n_sink, const void *q, void *out, float *lse,

@@ -68,7 +68,7 @@ def test_no_room_for_the_walk_behind_a_copy():
 
 def test_no_room_for_a_copy():
     """A call whose copy has no room is served by the walk over the cache, then and at the next call."""
-    q, out, cache = layer(65536, 64)                     # (268 MB of copy, half of it for the walk)
+    q, out, cache = layer(65536, 128)                    # (268 MB of copy, half of it for the walk)
     first, calls = cache()
     attend(first, calls, q, out)
     first.set_key_gather(1)
