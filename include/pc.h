@@ -101,7 +101,8 @@ typedef struct {
  * Attention (pc_attend, pc_attend_static, pc_attend_window, pc_attend_window_static, pc_decode_step) computes with the values held, and with turned
  * queries as the sum of two 8-bit numbers (off by 2^-8 of a value at most, as bf16 is).  Probabilities and values are multiplied in fp16 by calls of more
  * rows than one, and by single tokens that share their messages, unless the cache was ever given a value whose block of 32 has its largest above 7 x 2^13
- * or, not all zero, below 7 x 2^-14: then, and by other single tokens, in bf16 (values are exact either way).  Calls of more rows than one have the values
+ * or, not all zero, below 7 x 2^-14: then, and by other single tokens, in bf16 (values are exact either way).  In fp16 a key of 2^-30 of a row's largest
+ * probability, or less, may count as none, and one below 2^-20 of it has fewer bits.  Calls of more rows than one have the values
  * of the tiles that they see laid out so, and their queries turned, in the workspace: 8 KB a tile of 32 tokens and KV head, 256 bytes a row and query head (in pc_attend_static and pc_attend_window_static it has to fit PC_STATIC_WS_BYTES).  Long prefills of pc_attend,
  * and of pc_attend_window where the window leaves rows all that they list (calls of at least 1024 rows x query heads of a KV head that see 3e7 scores or more), go over a copy of all that they list, 512 bytes a token and KV
  * head besides: there turned keys and queries are fp16 (off by 2^-11 of a value), but for values above 7 x 2^24, keys of a norm above 2^10 and rows of queries
@@ -307,7 +308,8 @@ int32_t pc_decode_step(pc_cache *c, const int32_t *msg_ids, int32_t n_msgs, cons
 
 /* pc_attend for callers that cannot allocate device memory: code under HIP graph capture, tight serving loops,
  * harnesses that forbid hipMalloc.  Same arguments, same kernels, same results (bit for bit) as pc_attend, but for calls
- * that pc_attend gathers (see pc_set_key_gather); the per-call workspace (staged descriptors, the device-built plan, split
+ * that pc_attend gathers (see pc_set_key_gather) and, of a PC_MX4 cache, those whose splits this call leaves out because the
+ * array, or their lists a slot, does not hold them (other last bits); the per-call workspace (staged descriptors, the device-built plan, split
  * partials) lives in a fixed array of PC_STATIC_WS_BYTES (32 MiB) that the library holds on every GPU it runs on until the
  * process ends, and the function calls no hipMalloc, hipFree or other allocating routine.  A batch whose workspace exceeds
  * that size with its calls split by the plain rule (at least 16 tiles of 32 keys a split, as many splits as bring the batch
@@ -446,7 +448,7 @@ int32_t pc_profile_read(pc_cache *c, double ms_total[PC_N_KERNEL_CLASSES],
                         int64_t launches[PC_N_KERNEL_CLASSES], int32_t reset);
 
 /* Tuning knobs (0 keeps the default): KV tiles (of 32 keys) per split for decode
- * and for prefill work items. */
+ * and for prefill work items of pc_attend (PC_MX4 caches: of long prefills over a copy alone). */
 int32_t pc_set_tuning(pc_cache *c, int32_t decode_tiles_per_split, int32_t prefill_tiles_per_split);
 
 /* Gather pass (Sec. 2.4 "Position Updates", applied to a copy).  A prefill call with many query rows can have the

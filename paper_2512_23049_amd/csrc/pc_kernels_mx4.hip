@@ -385,12 +385,12 @@ void pc_launch_mx4_prepare(PcMx4Prepare P, const PcArgBlob *blob, hipStream_t st
 // this one follows in its softmax, masks and ring of direct loads).  What is its own:
 //   scores   codes of keys straight from the ring to v_mfma_scale 32x32x64, by two e4m3 pieces of the turned queries: as long on the matrix unit
 //            as bf16 keys would be (twice the work at twice the rate), a quarter of the reads from shared memory;
-//   queries  come turned by their positions (pc_mx4_prepare_kernel) and are turned back by a run's rotation, both in fp16 (2^-12 of a value, a sixteenth
+//   queries  come turned by their positions (pc_mx4_prepare_kernel) and are turned back by a run's rotation, both in fp16 (2^-11 of a value, an eighth
 //            of what pieces are off by; 1 us less of a small prefill), then cut in pieces under one power of two for the row, the same for every turn;
 //   values   come from the copy; they are finite, so that a probability of zero takes a key out.
 // Bound: the vector unit, 140 instructions a tile and wave of which 49 turned queries (messages of 160 tokens: every fifth tile is another's) before that
 // went to fp16, beside
-// 512 cycles of matrix work; 64 heads over 8, 1024 rows over 13k tokens: 0.6 PFLOP/s, which is why long prefills go another way.  Small ones
+// 512 cycles of matrix work; 64 heads over 8, 1024 rows over 13k tokens of such messages: 573 us, 0.76 PFLOP/s, which is why long prefills go another way.  Small ones
 // are chains of latencies: 77 rows over 5 messages 15.3 us, in splits of six tiles (of four, three or two no less, and more to merge).
 
 namespace {
@@ -660,7 +660,7 @@ void pc_launch_win_prefill_mx4(const PcWin &W, const PcMx4Rows &M, int n_items, 
 
 // ------------------------------------------------------------------------------------------------------------ gather
 // Long prefills (see pc_attend_mx4): the call's keys and values copied token after token into a packed copy, as pc_gather_kernel does it for bf16,
-// keys turned to the positions that the call gives them and rounded to fp16 (off by 2^-12 of a value), values as the bf16 that they stand for.
+// keys turned to the positions that the call gives them and rounded to fp16 (off by 2^-11 of a value), values as the bf16 that they stand for.
 // Values above 7 x 2^24 (times probabilities of 2^64, where that walk's reference need not move, and 2^31 keys, they would not fit 32 bits), keys of a norm
 // above 2^10, and those that are no number (which that walk would add to masks), mark the call for the walk behind it: below, what queries under
 // fp16's normal numbers are off by, 2^-25, moves a score by 2^-25 x 2^10 x sqrt(128) at most.

@@ -66,7 +66,7 @@ template <int PAIR> __device__ __forceinline__ uint32_t mx4_values(uint32_t w, u
     return mx4_lowered<PAIR & 1>(x & 0x7FFF7FFFu, d) | (x & 0x80008000u);
 }
 
-// The same in fp16, which holds probabilities to 2^-12 where bf16 has 2^-8: exponents from -13 to 13 (others give any number).
+// The same in fp16, which holds probabilities to 2^-11 where bf16 has 2^-8: exponents from -13 to 13 (others give any number).
 template <int PAIR> __device__ __forceinline__ uint32_t mx4_halfs(uint32_t w, uint32_t d, std::integral_constant<int, PAIR>)
 {
     static_assert(PC_MX4_HALF == 13 && PC_MX4_E_MAX == 60, "");
@@ -149,7 +149,7 @@ __device__ __forceinline__ void mx4_pieces(const float (&x)[4], float unit, int 
     rest = mx4_e4m3(y, unit * 0.0625f);
 }
 
-// The same of a row of queries in fp16, in that unit (128 to 256 at most: off by 2^-12 of a value, a sixteenth of what pieces are off by), two values
+// The same of a row of queries in fp16, in that unit (128 to 256 at most: off by 2^-11 of a value, an eighth of what pieces are off by), two values
 // an instruction: 16 values and their partners in the upper half, from what came, scaled, by 16 rotations (cosines and sines, in fp16).
 __device__ __forceinline__ mx4_f16x2 mx4_half(uint32_t x) { return __builtin_bit_cast(mx4_f16x2, x); }
 // eight bf16 numbers times `by`
