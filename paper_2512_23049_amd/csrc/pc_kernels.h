@@ -108,7 +108,7 @@ void pc_launch_runs_prepare(const void *lists, void *to, size_t rest, int n_runs
 void pc_launch_decode_runs_bf16(const PcLaunch &L, const PcRuns &O, const PcRunStarts &starts, hipStream_t st);
 // the packed walk over a copy whose keys are fp16; *mark = value where a query does not fit
 void pc_launch_prefill_f16(const PcLaunch &L, int n_items, uint32_t *mark, uint32_t value, hipStream_t st);
-// the gather pass of a PC_MX4 cache: keys, turned, as fp16, values as bf16; *mark = value where a key does not fit
+// the gather pass of a PC_MX4 cache: keys, turned, as fp16, values as bf16; *mark = value where a key or a value does not fit
 void pc_launch_gather_mx4(const PcLaunch &L, const PcGatherItem *items, int n_items, int64_t n_tiles, const int32_t *seg_kvoff, uint32_t *mark, uint32_t value, hipStream_t st);
 void pc_launch_prefill_bf16(const PcLaunch &L, int n_items, bool packed, hipStream_t st);   // packed: the items of calls that gathered
 

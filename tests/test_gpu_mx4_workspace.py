@@ -85,3 +85,26 @@ def test_no_room_for_a_copy():
         for x in outs:
             assert (x.float() - want.float()).norm() <= 5.8e-3 * want.float().norm()
     c.close()
+
+
+def test_a_refused_call_behind_others():
+    """A batch of short and long calls, of which a later one is refused: it is named by its place in the batch, and nothing has been written."""
+    import torch
+    from paper_2512_23049_amd import binding as b
+    q, out, cache = layer(4096, 1600)
+    c, calls = cache()
+    msg = calls[0].sel[0][0]
+    batch = [Call([(msg, 0)], -1, 4096, 3, None), Call([(msg, 0)], -1, 4096, 1024, None), Call([(msg, 5)], -1, 4200, 1, None), Call([(msg + 1, 0)], -1, 4096, 572, None)]
+    with pytest.raises(b.PcError) as e:
+        attend(c, batch, q, out)
+    torch.cuda.synchronize()
+    assert e.value.code == b.PC_ERR_BAD_MSG_ID and "call 3" in str(e.value)
+    assert (out == 7).all()
+    batch[3] = Call([(msg, 0)], -1, 4096, 572, None)
+    attend(c, batch, q, out)
+    want = out.clone()
+    for first, n, call in ((0, 3, 0), (3, 1024, 1), (1027, 1, 2), (1028, 572, 3)):
+        out.fill_(7)
+        attend(c, [batch[call]], q[first:first + n], out[first:first + n])
+        assert (out[first:first + n].float() - want[first:first + n].float()).norm() <= 5.8e-3 * want[first:first + n].float().norm()
+    c.close()
